@@ -399,6 +399,111 @@ int64_t som_launch_count(const som_handle* h);
 int64_t som_last_uncertain(const som_handle* h);
 int som_set_option(som_handle* h, int key, int64_t value);
 
+/*
+ * Dense layers around a map: a matrix product with everything in its epilogue, the learned choice of a few experts for
+ * every token, and the chosen experts' products, each with its gradient.  (No counterpart in the paper.  They are to
+ * learned dense features what the search is to sparse binary samples: som_route picks the best few of E experts where
+ * som_bmu2 picks the two best units, its bias keeps experts from going unused as units of a map go dead, and
+ * som_experts computes per expert what som_update sums per unit.)
+ *
+ * Common to all of them
+ *   - `type` is the element type of the tensors passed as void*: SOM_BF16 or SOM_F16, for som_route also SOM_F32.
+ *     Sums, scores and statistics are carried in fp32 or more.
+ *   - Matrices are row-major; `ld*` is the distance of two rows in elements, at least the row's length.  A 16-bit
+ *     matrix starts on a 16-byte boundary and its ld, D, F and I are multiples of 8 (else SOM_ERR_UNSUPPORTED); weights
+ *     and the gradients written are contiguous.
+ *   - Calls only enqueue work on `stream`, except that the handle's workspace grows (with a device synchronisation) when
+ *     a call needs more than any before.  Calls on one handle must not overlap on the GPU.  Outputs must not overlap inputs.
+ *   - Results are bit-identical from run to run for the same inputs.
+ *   - T == 0 is a successful no-op, except that gradients of weights are written (zeros) and counts are cleared.
+ */
+typedef struct som_layers som_layers; /* opaque: workspace and status of the calls below, for the current device */
+
+enum som_type { SOM_F32 = 0, SOM_F16 = 1, SOM_BF16 = 2 };
+enum som_act { SOM_ACT_NONE = 0, SOM_ACT_RELU = 1, SOM_ACT_GELU = 2 /* with the error function */, SOM_ACT_SILU = 3 };
+enum som_score { SOM_SCORE_SOFTMAX = 0, SOM_SCORE_SIGMOID = 1 };
+
+int som_layers_create(som_layers** out);
+int som_layers_destroy(som_layers* l); /* NULL is accepted */
+int som_layers_last_cuda_error(const som_layers* l);
+int64_t som_layers_launch_count(const som_layers* l);
+/* What earlier calls skipped on the device, like som_device_flags: SOM_ERR_INVALID_ARG if an expert index outside
+ * [-1, E) was met (it was treated as -1), SOM_ERR_CUDA if a wait inside a kernel ran out (the outputs of that call are
+ * not valid).  Synchronises `stream` and clears the record. */
+int som_layers_device_flags(som_layers* l, void* stream);
+
+/*
+ * som_linear - y = h + r with z = x W^T + b and h = act(z), or with `gated` h[f] = act(z[f]) * z[F + f].
+ *   x [T][D] (ldx), w [rows][D] with rows = gated ? 2 F : F, bias [rows] or NULL, residual [T][F] (ldr) or NULL,
+ *   y [T][F] (ldy).  z, act and the sum with r stay in fp32; y is rounded once.
+ */
+int som_linear(som_layers* l, int type, int act, int gated, int64_t T, int64_t D, int64_t F, const void* x, int64_t ldx,
+               const void* w, const void* bias, const void* residual, int64_t ldr, void* y, int64_t ldy, void* stream);
+
+/*
+ * som_linear_backward - the gradient of som_linear (r's is dy itself): dx = dz W, dw = dz^T x, dbias = sum_t dz, where
+ * dz is dy times the derivative of h by z.  z is computed again (unless act is none and not gated), so the forward call
+ * keeps nothing.  dz is rounded to `type` before the two products: the matrix instructions take 16-bit operands.
+ *   dy [T][F] (lddy); dx [T][D], dw [rows][D], dbias [rows]: contiguous outputs, NULL = not wanted.
+ */
+int som_linear_backward(som_layers* l, int type, int act, int gated, int64_t T, int64_t D, int64_t F, const void* x,
+                        int64_t ldx, const void* w, const void* bias, const void* dy, int64_t lddy, void* dx, void* dw,
+                        void* dbias, void* stream);
+
+/*
+ * som_route - choose k of E experts for every token.
+ *   logits   [T][E] (ld), any alignment; `type` SOM_F32, SOM_F16 or SOM_BF16.  A logit of -inf or NaN masks the expert out
+ *            for that token: it has no part in the scores and is never chosen.
+ *   scores   s = softmax(logits) over the row's unmasked experts, or sigmoid(logits).
+ *   keys     what the choice goes by: s + bias (bias fp32 [E] or NULL), both in fp32, s rounded from 64 bits so that the
+ *            order of two near scores is that of their exact values; without a bias (and with groups == 1 or group_best == 1)
+ *            the logits themselves, which order the experts the same way without a rounding.
+ *   groups   E / groups consecutive experts form a group (E % groups == 0); a group's key is the sum of its group_best
+ *            (1 or 2) largest keys, and only experts of the top_groups best groups can be chosen.
+ *   choice   the k largest keys, best first; ties go to the lowest index, among groups too.
+ *   indices  int32 [T][k], -1 where fewer than k experts are left.
+ *   weights  fp32 [T][k]: scale * s of the chosen experts, divided by their sum if renorm (0 if the sum is 0); 0 beside
+ *            an index of -1.  The bias does not enter the weights.
+ *   counts   int32 [E] or NULL: tokens that chose each expert (the bias for balance is moved by them).
+ * 1 <= E <= 1024, 1 <= k <= min(32, E), 1 <= top_groups <= groups <= 32.
+ */
+int som_route(som_layers* l, int type, int score, int64_t T, int32_t E, int32_t k, const void* logits, int64_t ld,
+              const float* bias, int32_t groups, int32_t top_groups, int32_t group_best, int renorm, float scale,
+              float* weights, int32_t* indices, int32_t* counts, void* stream);
+
+/*
+ * som_route_backward - dlogits [T][E] (contiguous, `type`) from dweights fp32 [T][k] and som_route's indices: the
+ * gradient through scores, renormalisation and scale (the choice itself is held fixed).  Every element is written; masked
+ * experts get 0.  An index outside [-1, E) is treated as -1 and recorded (som_layers_device_flags).
+ */
+int som_route_backward(som_layers* l, int type, int score, int64_t T, int32_t E, int32_t k, const void* logits, int64_t ld,
+                       const int32_t* indices, const float* dweights, int renorm, float scale, void* dlogits, void* stream);
+
+/*
+ * som_experts - y_t = r_t + sum_j weights[t][j] * (W2_e h_e(x_t) + b2_e) with e = indices[t][j] and h_e as in som_linear
+ * with W1_e, b1_e; an index of -1 adds nothing.
+ *   x [T][D] (ldx), indices int32 [T][k], weights [T][k] of weights_type (SOM_F32 or `type`),
+ *   w1 [E][rows][D] with rows = gated ? 2 I : I, b1 [E][rows] or NULL, w2 [E][D][I], b2 [E][D] or NULL,
+ *   residual [T][D] (ldr) or NULL, y [T][D] (ldy).
+ * The hidden values, times their weight, are rounded to `type` once, as operands of the second product; its results are
+ * kept in fp32, summed in the order of j and rounded once.  1 <= E <= 1024, 1 <= k <= 32, T * k + 128 E < 2^30.
+ */
+int som_experts(som_layers* l, int type, int act, int gated, int64_t T, int32_t E, int32_t k, int64_t D, int64_t I,
+                const void* x, int64_t ldx, const int32_t* indices, const void* weights, int weights_type, const void* w1,
+                const void* b1, const void* w2, const void* b2, const void* residual, int64_t ldr, void* y, int64_t ldy,
+                void* stream);
+
+/*
+ * som_experts_backward - the gradient of som_experts (r's is dy itself).  Nothing of the forward call is kept: z, h and
+ * W2^T dy are computed again in fp32.  dz and the weighted h are rounded to `type` as operands of the remaining products.
+ *   dy [T][D] (lddy); dx [T][D], dweights [T][k] (weights_type), dw1, dw2 and, unless NULL, db1, db2: contiguous outputs
+ *   of the shapes above, all elements written (zeros for experts without a token and for an index of -1).
+ */
+int som_experts_backward(som_layers* l, int type, int act, int gated, int64_t T, int32_t E, int32_t k, int64_t D, int64_t I,
+                         const void* x, int64_t ldx, const int32_t* indices, const void* weights, int weights_type,
+                         const void* w1, const void* b1, const void* w2, const void* b2, const void* dy, int64_t lddy,
+                         void* dx, void* dweights, void* dw1, void* db1, void* dw2, void* db2, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

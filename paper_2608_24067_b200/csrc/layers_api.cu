@@ -1,0 +1,525 @@
+// Host side of the dense operators declared in include/som.h: handle, argument checks, workspace, tensor maps, launches.
+#include <new>
+
+#include "layers_product.cuh"
+#include "layers_slots.cuh"
+
+namespace lay {
+
+int make_map(som_layers* l, CUtensorMap* map, const void* base, int bytes, int64_t cols, int64_t rows, int64_t batch, int64_t ld,
+             int64_t batch_stride, int box_cols, int box_rows)
+{
+    using Encode = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                                const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+    const cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)batch};
+    const cuuint64_t strides[2] = {(cuuint64_t)(ld * bytes), (cuuint64_t)(batch_stride * bytes)};
+    const cuuint32_t box[3] = {(cuuint32_t)box_cols, (cuuint32_t)box_rows, 1u};
+    const cuuint32_t step[3] = {1u, 1u, 1u};
+    const CUresult r = reinterpret_cast<Encode>(l->encode)(
+        map, bytes == 4 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims,
+        strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
+        box_cols * bytes == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+        CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (r == CUDA_SUCCESS) return SOM_OK;
+    l->last_cuda_error = (int)cudaErrorInvalidValue;
+    return SOM_ERR_CUDA;
+}
+
+namespace {
+
+struct Guard {  // the handle's device for the length of a call
+    int prev;
+    bool switched;
+    explicit Guard(int dev) : prev(-1), switched(false)
+    {
+        if (cudaGetDevice(&prev) == cudaSuccess && prev != dev) switched = cudaSetDevice(dev) == cudaSuccess;
+    }
+    ~Guard()
+    {
+        if (switched) cudaSetDevice(prev);
+    }
+};
+
+// Hands out pieces of the workspace; run once without a base to learn the size.
+struct Carver {
+    unsigned char* base;
+    size_t used;
+    template <class T>
+    T* take(int64_t n)
+    {
+        T* p = base ? reinterpret_cast<T*>(base + used) : nullptr;
+        used += som_align_up((size_t)n * sizeof(T), 1024);
+        return p;
+    }
+};
+
+int ensure(som_layers* l, size_t need)
+{
+    if (need <= l->ws_bytes) return SOM_OK;
+    if (l->ws) {
+        SOM_CK(l, cudaFree(l->ws));  // synchronises: earlier work in it is done
+        l->ws = nullptr;
+        l->ws_bytes = 0;
+    }
+    need = som_align_up(need + need / 8, 1 << 20);
+    SOM_CK(l, cudaMalloc(&l->ws, need));
+    l->ws_bytes = need;
+    return SOM_OK;
+}
+
+#define LAY_TRY(call)                   \
+    do {                                \
+        const int rc__ = (call);        \
+        if (rc__ != SOM_OK) return rc__; \
+    } while (0)
+
+bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+bool half_type(int type) { return type == SOM_F16 || type == SOM_BF16; }
+constexpr int64_t MOST_ROWS = (int64_t)1 << 30, MOST_COLS = (int64_t)1 << 24;
+
+int check_common(const som_layers* l, int type, int act, int64_t T)
+{
+    if (!l || T < 0 || act < SOM_ACT_NONE || act > SOM_ACT_SILU || !half_type(type)) return SOM_ERR_INVALID_ARG;
+    return SOM_OK;
+}
+
+// a [T][cols] 16-bit operand of a product: present, long enough rows, and laid out as the copies need it
+int check_rows(const void* p, int64_t ld, int64_t cols, int64_t T)
+{
+    if (T == 0) return SOM_OK;
+    if (!p || ld < cols) return SOM_ERR_INVALID_ARG;
+    if (!aligned16(p) || ld % 8 != 0 || ld >= (int64_t)1 << 32) return SOM_ERR_UNSUPPORTED;
+    return SOM_OK;
+}
+
+int check_weight(const void* p)
+{
+    if (!p) return SOM_ERR_INVALID_ARG;
+    return aligned16(p) ? SOM_OK : SOM_ERR_UNSUPPORTED;
+}
+
+int check_sizes(int64_t a, int64_t b)
+{
+    if (a <= 0 || b <= 0) return SOM_ERR_INVALID_ARG;
+    if (a % 8 != 0 || b % 8 != 0 || a > MOST_COLS || b > MOST_COLS) return SOM_ERR_UNSUPPORTED;
+    return SOM_OK;
+}
+
+int tiles_of(int64_t n, int64_t width) { return (int)((n + width - 1) / width); }
+
+// rows x cols 16-bit matrix as the K-major operand of a product (boxes of 128 rows) or M/N-major (64 rows)
+int map_k(som_layers* l, CUtensorMap* m, const void* p, int64_t cols, int64_t rows, int64_t ld, int64_t batch = 1)
+{
+    return make_map(l, m, p, 2, cols, rows, batch, ld, rows * ld, 64, 128);
+}
+int map_mn(som_layers* l, CUtensorMap* m, const void* p, int64_t cols, int64_t rows, int64_t ld, int64_t batch = 1)
+{
+    return make_map(l, m, p, 2, cols, rows, batch, ld, rows * ld, 64, 64);
+}
+int map_out(som_layers* l, CUtensorMap* m, void* p, int bytes, int64_t cols, int64_t rows, int64_t ld, int64_t batch = 1)
+{
+    return make_map(l, m, p, bytes, cols, rows, batch, ld, rows * ld, 32, 32);
+}
+
+}  // namespace
+}  // namespace lay
+
+using namespace lay;
+
+extern "C" {
+
+int som_layers_create(som_layers** out)
+{
+    if (!out) return SOM_ERR_INVALID_ARG;
+    *out = nullptr;
+    int dev = 0, major = 0, sms = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess ||
+        cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev) != cudaSuccess ||
+        cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || major != 10)
+        return SOM_ERR_NO_DEVICE;
+    som_layers* l = new (std::nothrow) som_layers();
+    if (!l) return SOM_ERR_INVALID_ARG;
+    l->device = dev;
+    l->sm_count = sms;
+    cudaDriverEntryPointQueryResult found;
+    cudaError_t e = cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &l->encode, cudaEnableDefault, &found);
+    if (e == cudaSuccess && (found != cudaDriverEntryPointSuccess || !l->encode)) e = cudaErrorNotSupported;
+    if (e == cudaSuccess) e = cudaMalloc(reinterpret_cast<void**>(&l->flags), 256);
+    if (e == cudaSuccess) e = cudaMemset(l->flags, 0, 256);
+    if (e != cudaSuccess) {
+        som_layers_destroy(l);
+        return SOM_ERR_CUDA;
+    }
+    *out = l;
+    return SOM_OK;
+}
+
+int som_layers_destroy(som_layers* l)
+{
+    if (!l) return SOM_OK;
+    Guard g(l->device);
+    cudaFree(l->flags);
+    cudaFree(l->ws);
+    delete l;
+    return SOM_OK;
+}
+
+int som_layers_last_cuda_error(const som_layers* l) { return l ? l->last_cuda_error : 0; }
+int64_t som_layers_launch_count(const som_layers* l) { return l ? l->launches : 0; }
+
+int som_layers_device_flags(som_layers* l, void* stream)
+{
+    if (!l) return SOM_ERR_INVALID_ARG;
+    Guard g(l->device);
+    cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+    int flags = 0;
+    SOM_CK(l, cudaMemcpyAsync(&flags, l->flags, sizeof(int), cudaMemcpyDeviceToHost, st));
+    SOM_CK(l, cudaMemsetAsync(l->flags, 0, sizeof(int), st));
+    SOM_CK(l, cudaStreamSynchronize(st));
+    if (flags & LAY_FLAG_GAVE_UP) return SOM_ERR_CUDA;
+    return flags & LAY_FLAG_BAD_EXPERT ? SOM_ERR_INVALID_ARG : SOM_OK;
+}
+
+int som_linear(som_layers* l, int type, int act, int gated, int64_t T, int64_t D, int64_t F, const void* x, int64_t ldx,
+               const void* w, const void* bias, const void* residual, int64_t ldr, void* y, int64_t ldy, void* stream)
+{
+    LAY_TRY(check_common(l, type, act, T));
+    LAY_TRY(check_sizes(D, F));
+    LAY_TRY(check_weight(w));
+    LAY_TRY(check_rows(x, ldx, D, T));
+    LAY_TRY(check_rows(y, ldy, F, T));
+    if (residual) LAY_TRY(check_rows(residual, ldr, F, T));
+    if (!aligned16(bias) || T >= MOST_ROWS) return SOM_ERR_UNSUPPORTED;
+    if (T == 0) return SOM_OK;
+    Guard g(l->device);
+    cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+    const int64_t rows = gated ? 2 * F : F;
+    ProdArgs a = {};
+    LAY_TRY(map_k(l, &a.a, x, D, T, ldx));
+    LAY_TRY(map_k(l, &a.b, w, D, rows, D));
+    LAY_TRY(map_out(l, &a.o0, y, 2, F, T, ldy));
+    a.bias = static_cast<const uint16_t*>(bias);
+    a.extra = static_cast<const uint16_t*>(residual);
+    a.ld_extra = ldr;
+    a.row_tiles = tiles_of(T, 128);
+    a.col_tiles = tiles_of(F, gated ? 128 : 256);
+    a.experts = 1;
+    a.rows = (int)T;
+    a.cols = (int)F;
+    a.gate_rows = gated ? (int)F : 0;
+    a.k1 = (int)D;
+    a.act = act;
+    a.bf16 = type == SOM_BF16;
+    a.flags = l->flags;
+    return launch_product(l, PROD_FWD, a, st);
+}
+
+int som_linear_backward(som_layers* l, int type, int act, int gated, int64_t T, int64_t D, int64_t F, const void* x,
+                        int64_t ldx, const void* w, const void* bias, const void* dy, int64_t lddy, void* dx, void* dw,
+                        void* dbias, void* stream)
+{
+    LAY_TRY(check_common(l, type, act, T));
+    LAY_TRY(check_sizes(D, F));
+    LAY_TRY(check_weight(w));
+    LAY_TRY(check_rows(x, ldx, D, T));
+    LAY_TRY(check_rows(dy, lddy, F, T));
+    if (!aligned16(bias) || !aligned16(dx) || !aligned16(dw) || T >= MOST_ROWS) return SOM_ERR_UNSUPPORTED;
+    Guard g(l->device);
+    cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+    const int64_t rows = gated ? 2 * F : F;
+    if (T == 0) {
+        if (dw) SOM_CK(l, cudaMemsetAsync(dw, 0, (size_t)rows * D * 2, st));
+        if (dbias) SOM_CK(l, cudaMemsetAsync(dbias, 0, (size_t)rows * 2, st));
+        return SOM_OK;
+    }
+    const bool again = act != SOM_ACT_NONE || gated;  // dz is not dy itself
+    const void* dz = dy;
+    int64_t lddz = lddy;
+    ProdArgs a = {};
+    a.experts = 1;
+    a.act = act;
+    a.bf16 = type == SOM_BF16;
+    a.flags = l->flags;
+    if (again) {
+        LAY_TRY(ensure(l, (size_t)T * rows * 2));
+        dz = l->ws;
+        lddz = rows;
+        ProdArgs z = a;
+        LAY_TRY(map_k(l, &z.a, x, D, T, ldx));
+        LAY_TRY(map_k(l, &z.b, w, D, rows, D));
+        LAY_TRY(map_out(l, &z.o0, l->ws, 2, F, T, rows));
+        if (gated) LAY_TRY(map_out(l, &z.o1, static_cast<uint16_t*>(l->ws) + F, 2, F, T, rows));
+        z.bias = static_cast<const uint16_t*>(bias);
+        z.extra = static_cast<const uint16_t*>(dy);
+        z.ld_extra = lddy;
+        z.row_tiles = tiles_of(T, 128);
+        z.col_tiles = tiles_of(F, gated ? 128 : 256);
+        z.rows = (int)T;
+        z.cols = (int)F;
+        z.gate_rows = gated ? (int)F : 0;
+        z.k1 = (int)D;
+        LAY_TRY(launch_product(l, PROD_DZ, z, st));
+    }
+    if (dx) {
+        ProdArgs p = a;
+        LAY_TRY(map_k(l, &p.a, dz, rows, T, lddz));
+        LAY_TRY(map_mn(l, &p.b, w, D, rows, D));
+        LAY_TRY(map_out(l, &p.o0, dx, 2, D, T, D));
+        p.row_tiles = tiles_of(T, 128);
+        p.col_tiles = tiles_of(D, 256);
+        p.rows = (int)T;
+        p.cols = (int)D;
+        p.k1 = (int)rows;
+        LAY_TRY(launch_product(l, PROD_DX, p, st));
+    }
+    if (dw) {
+        ProdArgs p = a;
+        LAY_TRY(map_mn(l, &p.a, dz, rows, T, lddz));
+        LAY_TRY(map_mn(l, &p.b, x, D, T, ldx));
+        LAY_TRY(map_out(l, &p.o0, dw, 2, D, rows, D));
+        p.row_tiles = tiles_of(rows, 128);
+        p.col_tiles = tiles_of(D, 256);
+        p.rows = (int)rows;
+        p.cols = (int)D;
+        p.k1 = (int)T;
+        LAY_TRY(launch_product(l, PROD_DW, p, st));
+    }
+    if (dbias) LAY_TRY(launch_column_sums(l, nullptr, 1, T, dz, lddz, nullptr, rows, dbias, a.bf16, st));
+    return SOM_OK;
+}
+
+static int check_route(const som_layers* l, int type, int score, int64_t T, int32_t E, int32_t k, const void* logits, int64_t ld)
+{
+    if (!l || type < SOM_F32 || type > SOM_BF16 || (score != SOM_SCORE_SOFTMAX && score != SOM_SCORE_SIGMOID) || T < 0 || E < 1 ||
+        k < 1 || k > E || (T > 0 && (!logits || ld < E)))
+        return SOM_ERR_INVALID_ARG;
+    return E > 1024 || k > 32 || T >= MOST_ROWS ? SOM_ERR_UNSUPPORTED : SOM_OK;
+}
+
+int som_route(som_layers* l, int type, int score, int64_t T, int32_t E, int32_t k, const void* logits, int64_t ld,
+              const float* bias, int32_t groups, int32_t top_groups, int32_t group_best, int renorm, float scale,
+              float* weights, int32_t* indices, int32_t* counts, void* stream)
+{
+    LAY_TRY(check_route(l, type, score, T, E, k, logits, ld));
+    if (groups < 1 || E % groups != 0 || top_groups < 1 || top_groups > groups || (group_best != 1 && group_best != 2) ||
+        (T > 0 && (!weights || !indices)))
+        return SOM_ERR_INVALID_ARG;
+    if (groups > 32) return SOM_ERR_UNSUPPORTED;
+    Guard g(l->device);
+    return launch_route(l, type, score, T, E, k, logits, ld, bias, groups, top_groups, group_best, renorm, scale, weights, indices,
+                        counts, reinterpret_cast<cudaStream_t>(stream));
+}
+
+int som_route_backward(som_layers* l, int type, int score, int64_t T, int32_t E, int32_t k, const void* logits, int64_t ld,
+                       const int32_t* indices, const float* dweights, int renorm, float scale, void* dlogits, void* stream)
+{
+    LAY_TRY(check_route(l, type, score, T, E, k, logits, ld));
+    if (T > 0 && (!indices || !dweights || !dlogits)) return SOM_ERR_INVALID_ARG;
+    Guard g(l->device);
+    return launch_route_backward(l, type, score, T, E, k, logits, ld, indices, dweights, renorm, scale, dlogits,
+                                 reinterpret_cast<cudaStream_t>(stream));
+}
+
+static int check_experts(const som_layers* l, int type, int act, int64_t T, int32_t E, int32_t k, int64_t D, int64_t I,
+                         const void* x, int64_t ldx, const int32_t* indices, const void* weights, int weights_type,
+                         const void* w1, const void* b1, const void* w2, const void* b2)
+{
+    LAY_TRY(check_common(l, type, act, T));
+    if (E < 1 || k < 1 || (weights_type != SOM_F32 && weights_type != type) || (T > 0 && (!indices || !weights)))
+        return SOM_ERR_INVALID_ARG;
+    LAY_TRY(check_sizes(D, I));
+    LAY_TRY(check_weight(w1));
+    LAY_TRY(check_weight(w2));
+    LAY_TRY(check_rows(x, ldx, D, T));
+    if (!aligned16(b1) || !aligned16(b2) || E > 1024 || k > 32 || T * k >= MOST_ROWS - (int64_t)E * 128) return SOM_ERR_UNSUPPORTED;
+    return SOM_OK;
+}
+
+// the plan's arrays for row tiles of `tile` rows
+static SlotPlan carve_plan(Carver& c, int64_t T, int E, int k, int tile)
+{
+    SlotPlan p = {};
+    const int64_t slots = T * k, used = slots < E ? slots : E;  // experts that can have a slot
+    p.tile = tile;
+    p.max_rows = (int)((slots + used * (tile - 1)) / tile * tile);
+    p.seg = c.take<int>(E + 1);
+    p.count = c.take<int>(E);
+    p.tiles = c.take<int>(1);
+    p.tile_expert = c.take<int>(p.max_rows / tile);
+    p.pos = c.take<int>(slots);
+    p.row_slot = c.take<int>(p.max_rows);
+    p.row_weight = c.take<float>(p.max_rows);
+    return p;
+}
+
+static ProdArgs grouped(const som_layers* l, const SlotPlan& p, int type)
+{
+    ProdArgs a = {};
+    a.tiles = p.tiles;
+    a.tile_expert = p.tile_expert;
+    a.row_weight = p.row_weight;
+    a.row_slot = p.row_slot;
+    a.row_tiles = p.max_rows / p.tile;
+    a.rows = p.max_rows;
+    a.bf16 = type == SOM_BF16;
+    a.flags = l->flags;
+    return a;
+}
+
+int som_experts(som_layers* l, int type, int act, int gated, int64_t T, int32_t E, int32_t k, int64_t D, int64_t I,
+                const void* x, int64_t ldx, const int32_t* indices, const void* weights, int weights_type, const void* w1,
+                const void* b1, const void* w2, const void* b2, const void* residual, int64_t ldr, void* y, int64_t ldy,
+                void* stream)
+{
+    LAY_TRY(check_experts(l, type, act, T, E, k, D, I, x, ldx, indices, weights, weights_type, w1, b1, w2, b2));
+    LAY_TRY(check_rows(y, ldy, D, T));
+    if (residual) LAY_TRY(check_rows(residual, ldr, D, T));
+    if (T == 0) return SOM_OK;
+    Guard g(l->device);
+    cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+    const int64_t rows1 = gated ? 2 * I : I;
+    SlotPlan p;
+    uint16_t *xp, *h;
+    float* part;
+    Carver c{nullptr, 0};
+    for (int pass = 0; pass < 2; ++pass) {
+        c.used = 0;
+        p = carve_plan(c, T, E, k, 128);
+        xp = c.take<uint16_t>((int64_t)p.max_rows * D);
+        h = c.take<uint16_t>((int64_t)p.max_rows * I);
+        part = c.take<float>((int64_t)p.max_rows * D);
+        if (pass == 0) {
+            LAY_TRY(ensure(l, c.used));
+            c.base = static_cast<unsigned char*>(l->ws);
+        }
+    }
+    LAY_TRY(launch_plan(l, p, indices, weights, weights_type, T, k, E, st));
+    LAY_TRY(launch_gather(l, p, E, k, D, x, ldx, xp, nullptr, 0, nullptr, st));
+    ProdArgs a = grouped(l, p, type);
+    LAY_TRY(map_k(l, &a.a, xp, D, p.max_rows, D));
+    LAY_TRY(map_k(l, &a.b, w1, D, rows1, D, E));
+    LAY_TRY(map_out(l, &a.o0, h, 2, I, p.max_rows, I));
+    a.bias = static_cast<const uint16_t*>(b1);
+    a.bias_ld = (int)rows1;
+    a.col_tiles = tiles_of(I, gated ? 128 : 256);
+    a.cols = (int)I;
+    a.gate_rows = gated ? (int)I : 0;
+    a.k1 = (int)D;
+    a.act = act;
+    a.weigh = 1;
+    LAY_TRY(launch_product(l, PROD_FWD, a, st));
+    a = grouped(l, p, type);
+    LAY_TRY(map_k(l, &a.a, h, I, p.max_rows, I));
+    LAY_TRY(map_k(l, &a.b, w2, I, D, I, E));
+    LAY_TRY(map_out(l, &a.o0, part, 4, D, p.max_rows, D));
+    a.bias = static_cast<const uint16_t*>(b2);
+    a.bias_ld = (int)D;
+    a.col_tiles = tiles_of(D, 256);
+    a.cols = (int)D;
+    a.k1 = (int)I;
+    a.weigh = 2;
+    a.out32 = 1;
+    LAY_TRY(launch_product(l, PROD_FWD, a, st));
+    return launch_join(l, p, T, k, D, part, residual, ldr, y, ldy, a.bf16, st);
+}
+
+int som_experts_backward(som_layers* l, int type, int act, int gated, int64_t T, int32_t E, int32_t k, int64_t D, int64_t I,
+                         const void* x, int64_t ldx, const int32_t* indices, const void* weights, int weights_type,
+                         const void* w1, const void* b1, const void* w2, const void* b2, const void* dy, int64_t lddy,
+                         void* dx, void* dweights, void* dw1, void* db1, void* dw2, void* db2, void* stream)
+{
+    LAY_TRY(check_experts(l, type, act, T, E, k, D, I, x, ldx, indices, weights, weights_type, w1, b1, w2, b2));
+    LAY_TRY(check_rows(dy, lddy, D, T));
+    if (!dw1 || !dw2 || (T > 0 && (!dx || !dweights))) return SOM_ERR_INVALID_ARG;
+    if (!aligned16(dx) || !aligned16(dw1) || !aligned16(dw2)) return SOM_ERR_UNSUPPORTED;
+    Guard g(l->device);
+    cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+    const int64_t rows1 = gated ? 2 * I : I;
+    if (T == 0) {
+        SOM_CK(l, cudaMemsetAsync(dw1, 0, (size_t)E * rows1 * D * 2, st));
+        SOM_CK(l, cudaMemsetAsync(dw2, 0, (size_t)E * D * I * 2, st));
+        if (db1) SOM_CK(l, cudaMemsetAsync(db1, 0, (size_t)E * rows1 * 2, st));
+        if (db2) SOM_CK(l, cudaMemsetAsync(db2, 0, (size_t)E * D * 2, st));
+        return SOM_OK;
+    }
+    const int col_tiles = tiles_of(I, gated ? 128 : 256);
+    SlotPlan p;
+    uint16_t *xp, *dyp, *h, *dz;
+    float *part, *dot;
+    Carver c{nullptr, 0};
+    for (int pass = 0; pass < 2; ++pass) {
+        c.used = 0;
+        p = carve_plan(c, T, E, k, 128);
+        xp = c.take<uint16_t>((int64_t)p.max_rows * D);
+        dyp = c.take<uint16_t>((int64_t)p.max_rows * D);
+        h = c.take<uint16_t>((int64_t)p.max_rows * I);
+        dz = c.take<uint16_t>((int64_t)p.max_rows * rows1);
+        part = c.take<float>((int64_t)p.max_rows * D);
+        dot = c.take<float>((int64_t)p.max_rows * 2 * col_tiles);
+        if (pass == 0) {
+            LAY_TRY(ensure(l, c.used));
+            c.base = static_cast<unsigned char*>(l->ws);
+        }
+    }
+    LAY_TRY(launch_plan(l, p, indices, weights, weights_type, T, k, E, st));
+    LAY_TRY(launch_gather(l, p, E, k, D, x, ldx, xp, dy, lddy, dyp, st));
+    // z and g = W2^T dy side by side -> dz, the weighted h, partial sums of <h, g>
+    ProdArgs a = grouped(l, p, type);
+    LAY_TRY(map_k(l, &a.a, xp, D, p.max_rows, D));
+    LAY_TRY(map_k(l, &a.b, w1, D, rows1, D, E));
+    LAY_TRY(map_k(l, &a.a2, dyp, D, p.max_rows, D));
+    LAY_TRY(map_mn(l, &a.b2, w2, I, D, I, E));
+    LAY_TRY(map_out(l, &a.o0, dz, 2, I, p.max_rows, rows1));
+    if (gated) LAY_TRY(map_out(l, &a.o1, dz + I, 2, I, p.max_rows, rows1));
+    LAY_TRY(map_out(l, &a.o2, h, 2, I, p.max_rows, I));
+    a.bias = static_cast<const uint16_t*>(b1);
+    a.bias_ld = (int)rows1;
+    a.dot = dot;
+    a.col_tiles = col_tiles;
+    a.cols = (int)I;
+    a.gate_rows = gated ? (int)I : 0;
+    a.k1 = a.k2 = (int)D;
+    a.act = act;
+    LAY_TRY(launch_product(l, PROD_DZ_PAIR, a, st));
+    LAY_TRY(launch_dweights(l, p, indices, T, k, D, dot, 2 * col_tiles, b2, dy, lddy, dweights, weights_type, a.bf16, st));
+    // dx
+    a = grouped(l, p, type);
+    LAY_TRY(map_k(l, &a.a, dz, rows1, p.max_rows, rows1));
+    LAY_TRY(map_mn(l, &a.b, w1, D, rows1, D, E));
+    LAY_TRY(map_out(l, &a.o0, part, 4, D, p.max_rows, D));
+    a.col_tiles = tiles_of(D, 256);
+    a.cols = (int)D;
+    a.k1 = (int)rows1;
+    a.out32 = 1;
+    LAY_TRY(launch_product(l, PROD_DX, a, st));
+    LAY_TRY(launch_join(l, p, T, k, D, part, nullptr, 0, dx, D, a.bf16, st));
+    // dw1 = dz^T x, dw2 = dy^T (weighted h)
+    a = grouped(l, p, type);
+    a.seg = p.seg;
+    a.experts = E;
+    a.row_weight = nullptr;
+    a.row_slot = nullptr;
+    ProdArgs b = a;
+    LAY_TRY(map_mn(l, &a.a, dz, rows1, p.max_rows, rows1));
+    LAY_TRY(map_mn(l, &a.b, xp, D, p.max_rows, D));
+    LAY_TRY(map_out(l, &a.o0, dw1, 2, D, rows1, D, E));
+    a.row_tiles = tiles_of(rows1, 128);
+    a.col_tiles = tiles_of(D, 256);
+    a.rows = (int)rows1;
+    a.cols = (int)D;
+    LAY_TRY(launch_product(l, PROD_DW, a, st));
+    LAY_TRY(map_mn(l, &b.a, dyp, D, p.max_rows, D));
+    LAY_TRY(map_mn(l, &b.b, h, I, p.max_rows, I));
+    LAY_TRY(map_out(l, &b.o0, dw2, 2, I, D, I, E));
+    b.row_tiles = tiles_of(D, 128);
+    b.col_tiles = tiles_of(I, 256);
+    b.rows = (int)D;
+    b.cols = (int)I;
+    LAY_TRY(launch_product(l, PROD_DW, b, st));
+    if (db1) LAY_TRY(launch_column_sums(l, p.seg, E, 0, dz, rows1, nullptr, rows1, db1, a.bf16, st));
+    if (db2) LAY_TRY(launch_column_sums(l, p.seg, E, 0, dyp, D, p.row_weight, D, db2, a.bf16, st));
+    return SOM_OK;
+}
+
+}  // extern "C"

@@ -1,0 +1,46 @@
+// The matrix products of the dense operators on tcgen05: launch descriptions shared by the kernels and the C ABI.
+#pragma once
+
+#include "layers_internal.cuh"
+
+namespace lay {
+
+enum ProdMode {
+    PROD_FWD = 0,      // out[row, n] = epilogue(sum_k A[row, k] B[n, k])
+    PROD_DZ = 1,       // the same product, epilogue multiplies dy by the activation's derivative
+    PROD_DZ_PAIR = 2,  // two products over the same rows: z = x W1^T and g = dy W2; epilogue of the experts' gradient
+    PROD_DX = 3,       // out[row, n] = sum_k A[row, k] B[k, n]
+    PROD_DW = 4        // out[e][m, n] = sum_rows A[row, m] B[row, n] over the rows of expert e
+};
+
+struct ProdArgs {
+    CUtensorMap a, b;        // operands (of the first product)
+    CUtensorMap a2, b2;      // second product of PROD_DZ_PAIR
+    CUtensorMap o0, o1, o2;  // outputs
+    const int* tiles;        // grouped rows: number of row tiles on the device; nullptr = row_tiles
+    const int* tile_expert;  // grouped rows: expert of a row tile; nullptr = 0
+    const int* seg;          // PROD_DW: rows [seg[e], seg[e + 1]) of expert e; nullptr = [0, k1)
+    const uint16_t* bias;    // [experts][bias_ld] or nullptr
+    const uint16_t* extra;   // residual (PROD_FWD) or dy (PROD_DZ), [rows][ld_extra], or nullptr
+    const float* row_weight; // [rows] or nullptr
+    const int* row_slot;     // [rows] -1 = padding; nullptr = every row counts
+    float* dot;              // PROD_DZ_PAIR: [rows][2 * col_tiles] partial sums of h * g
+    int64_t ld_extra;
+    int bias_ld;
+    int row_tiles, col_tiles, experts;
+    int rows, cols;  // extent of the outputs (PROD_DW: of one expert's)
+    int gate_rows;   // gated: rows of B between a feature's gate row and its other row; 0 = not gated
+    int k1, k2;      // length of the products' sums
+    int act, bf16, out32;
+    int weigh;  // row_weight multiplies: 1 the result, 2 the bias
+    int* flags;
+};
+
+int launch_product(som_layers* l, ProdMode mode, const ProdArgs& args, cudaStream_t st);
+
+// 3-d tensor map over [batch][rows][cols] of 16-bit (bytes = 2) or fp32 (4) elements in boxes of [1][box_rows][box_cols],
+// box_cols * bytes = 64 or 128 (the swizzle)
+int make_map(som_layers* l, CUtensorMap* map, const void* base, int bytes, int64_t cols, int64_t rows, int64_t batch,
+             int64_t ld, int64_t batch_stride, int box_cols, int box_rows);
+
+}  // namespace lay

@@ -1,0 +1,269 @@
+// What surrounds the experts' products: the plan that orders the tokens' slots by expert, the gather into that order, the
+// join of a token's results and the small gradients.
+#include "layers_math.cuh"
+#include "layers_slots.cuh"
+
+namespace lay {
+namespace {
+
+constexpr int PLAN_THREADS = 1024, PLAN_WARPS = PLAN_THREADS / 32;
+
+__device__ __forceinline__ float load_weight(const void* w, int type, int64_t i)
+{
+    if (type == SOM_F32) return __ldg(static_cast<const float*>(w) + i);
+    return unpack1(__ldg(static_cast<const uint16_t*>(w) + i), type == SOM_BF16);
+}
+
+// A stable counting sort of the slots by expert in one block: every warp owns a contiguous run of slots, counts it into a
+// row of its own in shared memory, the rows are turned into starting places, and the warp walks its run again.
+// Stable, so that the rows of an expert (and the sums over them) have one order.
+__global__ void __launch_bounds__(PLAN_THREADS) k_slot_plan(SlotPlan p, const int32_t* indices, const void* weights,
+                                                           int weights_type, int64_t slots, int E, int* flags)
+{
+    extern __shared__ int hist[];  // [PLAN_WARPS][E], then [E] segment starts
+    __shared__ int warp_sum[PLAN_WARPS];
+    int* start = hist + PLAN_WARPS * E;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    for (int i = threadIdx.x; i < PLAN_WARPS * E; i += PLAN_THREADS) hist[i] = 0;
+    __syncthreads();
+    const int64_t run = (slots + PLAN_THREADS - 1) / PLAN_THREADS * 32;
+    const int64_t lo = warp * run, hi = lo + run < slots ? lo + run : slots;
+    int* mine = hist + warp * E;
+    bool bad = false;
+    for (int64_t s = lo + lane; s < hi; s += 32) {
+        const int e = indices[s];
+        if (e >= 0 && e < E) atomicAdd(&mine[e], 1);
+        bad |= e < -1 || e >= E;
+    }
+    som_raise(flags, bad, LAY_FLAG_BAD_EXPERT);
+    __syncthreads();
+    // thread e: starting places of expert e's slots by warp; segments padded to whole tiles
+    int count = 0;
+    const int e = threadIdx.x;
+    if (e < E)
+        for (int w = 0; w < PLAN_WARPS; ++w) {
+            const int c = hist[w * E + e];
+            hist[w * E + e] = count;
+            count += c;
+        }
+    const int tiles = (count + p.tile - 1) / p.tile;
+    int sum = tiles;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+        const int v = __shfl_up_sync(0xffffffffu, sum, d);
+        if (lane >= d) sum += v;
+    }
+    if (lane == 31) warp_sum[warp] = sum;
+    __syncthreads();
+    int before = sum - tiles;
+    for (int w = 0; w < warp; ++w) before += warp_sum[w];
+    if (e < E) {
+        start[e] = before * p.tile;
+        p.seg[e] = before * p.tile;
+        p.count[e] = count;
+        for (int i = 0; i < tiles; ++i) p.tile_expert[before + i] = e;
+        for (int r = before * p.tile + count; r < (before + tiles) * p.tile; ++r) {
+            p.row_slot[r] = -1;
+            p.row_weight[r] = 0.f;
+        }
+        if (e == E - 1) {
+            p.seg[E] = (before + tiles) * p.tile;
+            *p.tiles = before + tiles;
+        }
+    }
+    __syncthreads();
+    for (int64_t s0 = lo; s0 < hi; s0 += 32) {
+        const int64_t s = s0 + lane;
+        int x = s < hi ? indices[s] : -1;
+        if (x < 0 || x >= E) x = -1;
+        const unsigned same = __match_any_sync(0xffffffffu, x);
+        const int rank = __popc(same & ((1u << lane) - 1u));
+        int at = 0;
+        if (x >= 0) at = mine[x];
+        __syncwarp();
+        if (x >= 0 && rank == 0) mine[x] = at + __popc(same);
+        __syncwarp();
+        if (s < hi) {
+            const int row = x >= 0 ? start[x] + at + rank : -1;
+            p.pos[s] = row;
+            if (row >= 0) {
+                p.row_slot[row] = (int)s;
+                p.row_weight[row] = load_weight(weights, weights_type, s);
+            }
+        }
+    }
+}
+
+// rows of x (blockIdx.y == 0) and of dy (1) in the slots' order; zeros in padding rows
+__global__ void __launch_bounds__(256) k_gather(SlotPlan p, int E, int k, int D, const uint16_t* x, int64_t ldx, uint16_t* xp,
+                                                const uint16_t* dy, int64_t lddy, uint16_t* dyp)
+{
+    const int rows = p.seg[E], chunks = D / 8;
+    const uint16_t* from = blockIdx.y ? dy : x;
+    const int64_t ld = blockIdx.y ? lddy : ldx;
+    uint16_t* to = blockIdx.y ? dyp : xp;
+    for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < (int64_t)rows * chunks; i += (int64_t)gridDim.x * blockDim.x) {
+        const int row = (int)(i / chunks), c = (int)(i % chunks);
+        const int slot = p.row_slot[row];
+        uint4 v = make_uint4(0u, 0u, 0u, 0u);
+        if (slot >= 0) v = __ldg(reinterpret_cast<const uint4*>(from + (size_t)(slot / k) * ld) + c);
+        *(reinterpret_cast<uint4*>(to + (size_t)row * D) + c) = v;
+    }
+}
+
+// y[t] = residual[t] + sum over j of part[pos[t][j]], in the order of j
+__global__ void __launch_bounds__(256) k_join(const int* pos, int64_t T, int k, int D, const float* part, const uint16_t* residual,
+                                              int64_t ldr, uint16_t* y, int64_t ldy, int bf16)
+{
+    const int chunks = D / 8;
+    for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < T * chunks; i += (int64_t)gridDim.x * blockDim.x) {
+        const int64_t t = i / chunks;
+        const int c = (int)(i % chunks);
+        float v[8];
+        if (residual) {
+            load8(residual + (size_t)t * ldr + 8 * c, v, bf16);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = 0.f;
+        }
+        for (int j = 0; j < k; ++j) {
+            const int row = pos[t * k + j];
+            if (row < 0) continue;
+            const float4* q = reinterpret_cast<const float4*>(part + (size_t)row * D + 8 * c);
+            const float4 a = q[0], b = q[1];
+            v[0] += a.x, v[1] += a.y, v[2] += a.z, v[3] += a.w;
+            v[4] += b.x, v[5] += b.y, v[6] += b.z, v[7] += b.w;
+        }
+        uint4 u;
+        u.x = pack2(v[0], v[1], bf16);
+        u.y = pack2(v[2], v[3], bf16);
+        u.z = pack2(v[4], v[5], bf16);
+        u.w = pack2(v[6], v[7], bf16);
+        *reinterpret_cast<uint4*>(y + (size_t)t * ldy + 8 * c) = u;
+    }
+}
+
+// dweights[slot] = sum of the slot's partial <h, W2^T dy> + <b2, dy>; one warp a slot
+__global__ void __launch_bounds__(256) k_dweights(const int* pos, const int32_t* indices, int64_t slots, int k, int D,
+                                                  const float* dot, int parts, const uint16_t* b2, const uint16_t* dy,
+                                                  int64_t lddy, void* dweights, int weights_type, int bf16)
+{
+    const int lane = threadIdx.x & 31;
+    for (int64_t s = ((int64_t)blockIdx.x * blockDim.x + threadIdx.x) >> 5; s < slots; s += ((int64_t)gridDim.x * blockDim.x) >> 5) {
+        const int row = pos[s];
+        float v = 0.f;
+        if (row >= 0) {
+            for (int i = lane; i < parts; i += 32) v += dot[(size_t)row * parts + i];
+            if (b2) {
+                const uint16_t* b = b2 + (size_t)indices[s] * D;
+                const uint16_t* g = dy + (size_t)(s / k) * lddy;
+                for (int i = lane * 8; i < D; i += 256) {
+                    float u[8], w[8];
+                    load8(b + i, u, bf16);
+                    load8(g + i, w, bf16);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) v = fmaf(u[j], w[j], v);
+                }
+            }
+        }
+#pragma unroll
+        for (int d = 16; d > 0; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
+        if (lane == 0) {
+            if (weights_type == SOM_F32) static_cast<float*>(dweights)[s] = v;
+            else static_cast<uint16_t*>(dweights)[s] = (uint16_t)pack2(v, 0.f, bf16);
+        }
+    }
+}
+
+// out[e][c] = sum over the rows of expert e of weight[row] * v[row][c]; a block sums 64 columns of one expert, 32 rows at
+// a time, in a fixed order
+__global__ void __launch_bounds__(256) k_column_sums(const int* seg, int64_t rows, const uint16_t* v, int64_t ld, const float* weight,
+                                                     int cols, uint16_t* out, int bf16)
+{
+    __shared__ float part[32][65];
+    const int e = blockIdx.y, c = blockIdx.x * 64 + (threadIdx.x & 7) * 8, r = threadIdx.x >> 3;
+    const int64_t lo = seg ? seg[e] : 0, hi = seg ? seg[e + 1] : rows;
+    float a[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    if (c < cols)
+        for (int64_t i = lo + r; i < hi; i += 32) {
+            float u[8];
+            load8(v + (size_t)i * ld + c, u, bf16);
+            const float w = weight ? weight[i] : 1.f;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) a[j] = fmaf(w, u[j], a[j]);
+        }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) part[r][(threadIdx.x & 7) * 8 + j] = a[j];
+    __syncthreads();
+    if (threadIdx.x < 64 && blockIdx.x * 64 + threadIdx.x < cols) {
+        float s = 0.f;
+        for (int i = 0; i < 32; ++i) s += part[i][threadIdx.x];
+        out[(size_t)e * cols + blockIdx.x * 64 + threadIdx.x] = (uint16_t)pack2(s, 0.f, bf16);
+    }
+}
+
+int done(som_layers* l)
+{
+    ++l->launches;
+    const cudaError_t e = cudaGetLastError();
+    if (e == cudaSuccess) return SOM_OK;
+    l->last_cuda_error = (int)e;
+    return SOM_ERR_CUDA;
+}
+
+// blocks of `per` items each, at most eight per SM: the kernels walk the rest
+int grid_for(const som_layers* l, int64_t items, int per)
+{
+    const int64_t want = (items + per - 1) / per, most = (int64_t)l->sm_count * 8;
+    return (int)(want < 1 ? 1 : want < most ? want : most);
+}
+
+}  // namespace
+
+int launch_plan(som_layers* l, const SlotPlan& p, const int32_t* indices, const void* weights, int weights_type, int64_t T,
+                int k, int E, cudaStream_t st)
+{
+    const size_t smem = (size_t)(PLAN_WARPS + 1) * E * sizeof(int);
+    const cudaError_t e = cudaFuncSetAttribute(k_slot_plan, cudaFuncAttributeMaxDynamicSharedMemorySize, (PLAN_WARPS + 1) * 1024 * (int)sizeof(int));
+    if (e != cudaSuccess) {
+        l->last_cuda_error = (int)e;
+        return SOM_ERR_CUDA;
+    }
+    k_slot_plan<<<1, PLAN_THREADS, smem, st>>>(p, indices, weights, weights_type, T * k, E, l->flags);
+    return done(l);
+}
+
+int launch_gather(som_layers* l, const SlotPlan& p, int E, int k, int64_t D, const void* x, int64_t ldx, void* xp, const void* dy,
+                  int64_t lddy, void* dyp, cudaStream_t st)
+{
+    const dim3 grid(grid_for(l, (int64_t)p.max_rows * (D / 8), 256 * 4), dy ? 2 : 1);
+    k_gather<<<grid, 256, 0, st>>>(p, E, k, (int)D, static_cast<const uint16_t*>(x), ldx, static_cast<uint16_t*>(xp),
+                                   static_cast<const uint16_t*>(dy), lddy, static_cast<uint16_t*>(dyp));
+    return done(l);
+}
+
+int launch_join(som_layers* l, const SlotPlan& p, int64_t T, int k, int64_t D, const float* part, const void* residual, int64_t ldr,
+                void* y, int64_t ldy, int bf16, cudaStream_t st)
+{
+    k_join<<<grid_for(l, T * (D / 8), 256), 256, 0, st>>>(p.pos, T, k, (int)D, part, static_cast<const uint16_t*>(residual), ldr,
+                                                         static_cast<uint16_t*>(y), ldy, bf16);
+    return done(l);
+}
+
+int launch_dweights(som_layers* l, const SlotPlan& p, const int32_t* indices, int64_t T, int k, int64_t D, const float* dot, int parts,
+                    const void* b2, const void* dy, int64_t lddy, void* dweights, int weights_type, int bf16, cudaStream_t st)
+{
+    k_dweights<<<grid_for(l, T * k, 8), 256, 0, st>>>(p.pos, indices, T * k, k, (int)D, dot, parts, static_cast<const uint16_t*>(b2),
+                                                     static_cast<const uint16_t*>(dy), lddy, dweights, weights_type, bf16);
+    return done(l);
+}
+
+int launch_column_sums(som_layers* l, const int* seg, int E, int64_t rows, const void* v, int64_t ld, const float* weight, int64_t cols,
+                       void* out, int bf16, cudaStream_t st)
+{
+    const dim3 grid((unsigned)((cols + 63) / 64), (unsigned)E);
+    k_column_sums<<<grid, 256, 0, st>>>(seg, rows, static_cast<const uint16_t*>(v), ld, weight, (int)cols, static_cast<uint16_t*>(out), bf16);
+    return done(l);
+}
+
+}  // namespace lay

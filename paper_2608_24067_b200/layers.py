@@ -1,0 +1,222 @@
+"""Thin Python binding of the dense operators in ``include/som.h``: a linear layer with its epilogue, routing to experts,
+the experts' products, and their gradients.
+
+Argument marshalling only, like ``som``: the library computes, PyTorch supplies memory and streams, and there is no
+fallback.  Matrices are 2-d CUDA tensors whose rows are contiguous (``stride(1) == 1``); rows may lie further apart.
+"""
+from __future__ import annotations
+
+import ctypes
+
+import torch
+
+from .som import SOM_OK, SomError, load_library
+
+_TYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
+_ACTS = {"none": 0, "relu": 1, "gelu": 2, "silu": 3}
+_SCORES = {"softmax": 0, "sigmoid": 1}
+
+
+def _matrix(t, shape, dtype, name):
+    """(address, distance of rows) of a [rows][cols] tensor."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype != dtype or t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise TypeError("%s must be a 2-d CUDA tensor of %s with contiguous rows" % (name, dtype))
+    if tuple(t.shape) != shape:
+        raise ValueError("%s must have shape %s, not %s" % (name, shape, tuple(t.shape)))
+    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+def _whole(t, shape, dtype, name):
+    """Address of a contiguous tensor; 0 for None."""
+    if t is None:
+        return 0
+    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype != dtype or not t.is_contiguous():
+        raise TypeError("%s must be a contiguous CUDA tensor of %s" % (name, dtype))
+    if tuple(t.shape) != shape:
+        raise ValueError("%s must have shape %s, not %s" % (name, shape, tuple(t.shape)))
+    return t.data_ptr()
+
+
+def _code(table, key, name):
+    try:
+        return table[key]
+    except KeyError:
+        raise ValueError("%s must be one of %s" % (name, sorted(str(k) for k in table))) from None
+
+
+class Layers:
+    """Handle of the dense operators on one device (``som_layers_create``): workspace and status.
+
+    Calls on one handle must not overlap on the GPU: issue them on one stream or order the streams."""
+
+    def __init__(self, device=None):
+        self._lib = load_library()
+        self._h = ctypes.c_void_p()
+        self.device = torch.device("cuda", torch.cuda.current_device()) if device is None else torch.device(device)
+        if self.device.index is None:
+            self.device = torch.device("cuda", torch.cuda.current_device())
+        with torch.cuda.device(self.device):
+            rc = self._lib.som_layers_create(ctypes.byref(self._h))
+        if rc != SOM_OK:
+            self._h = ctypes.c_void_p()
+            raise SomError(rc, "som_layers_create")
+
+    def _check(self, rc: int, where: str):
+        if rc != SOM_OK:
+            raise SomError(rc, where, self._lib.som_layers_last_cuda_error(self._h))
+
+    def _stream(self, stream) -> int:
+        return (torch.cuda.current_stream(self.device) if stream is None else stream).cuda_stream
+
+    def _empty(self, shape, dtype):
+        return torch.empty(shape, dtype=dtype, device=self.device)
+
+    def _half(self, x, name="x"):
+        if not isinstance(x, torch.Tensor) or x.dtype not in (torch.float16, torch.bfloat16) or x.dim() != 2:
+            raise TypeError("%s must be a 2-d float16 or bfloat16 CUDA tensor" % name)
+        if x.device != self.device:
+            raise ValueError("%s is on %s, the handle on %s" % (name, x.device, self.device))
+        return _TYPES[x.dtype]
+
+    def linear(self, x, weight, bias=None, residual=None, act="none", gated=False, out=None, stream=None):
+        """som_linear: act(x weight^T + bias) + residual; gated: weight's first half of rows is activated and multiplies
+        the products of the second.  Returns [T, F]."""
+        kind = self._half(x)
+        if weight.dim() != 2:
+            raise ValueError("weight must be 2-d")
+        T, D = x.shape
+        rows = weight.shape[0]
+        if gated and rows % 2:
+            raise ValueError("a gated weight has an even number of rows")
+        F = rows // 2 if gated else rows
+        xp, ldx = _matrix(x, (T, D), x.dtype, "x")
+        if out is None:
+            out = self._empty((T, F), x.dtype)
+        yp, ldy = _matrix(out, (T, F), x.dtype, "out")
+        rp, ldr = (0, 0) if residual is None else _matrix(residual, (T, F), x.dtype, "residual")
+        rc = self._lib.som_linear(self._h, kind, _code(_ACTS, act, "act"), int(gated), T, D, F, xp, ldx,
+                                  _whole(weight, (rows, D), x.dtype, "weight"), _whole(bias, (rows,), x.dtype, "bias"),
+                                  rp, ldr, yp, ldy, self._stream(stream))
+        self._check(rc, "som_linear")
+        return out
+
+    def linear_backward(self, x, weight, dy, bias=None, act="none", gated=False, stream=None):
+        """som_linear_backward: {"dx", "dweight"} and, with a bias, "dbias" (the residual's gradient is dy)."""
+        kind = self._half(x)
+        if weight.dim() != 2:
+            raise ValueError("weight must be 2-d")
+        T, D = x.shape
+        rows = weight.shape[0]
+        if gated and rows % 2:
+            raise ValueError("a gated weight has an even number of rows")
+        F = rows // 2 if gated else rows
+        xp, ldx = _matrix(x, (T, D), x.dtype, "x")
+        gp, ldg = _matrix(dy, (T, F), x.dtype, "dy")
+        wp = _whole(weight, (rows, D), x.dtype, "weight")
+        out = {"dx": self._empty((T, D), x.dtype), "dweight": self._empty((rows, D), x.dtype)}
+        if bias is not None:
+            out["dbias"] = self._empty((rows,), x.dtype)
+        rc = self._lib.som_linear_backward(self._h, kind, _code(_ACTS, act, "act"), int(gated), T, D, F, xp, ldx, wp,
+                                           _whole(bias, (rows,), x.dtype, "bias"), gp, ldg, out["dx"].data_ptr(),
+                                           out["dweight"].data_ptr(), out["dbias"].data_ptr() if bias is not None else 0,
+                                           self._stream(stream))
+        self._check(rc, "som_linear_backward")
+        return out
+
+    def route(self, logits, k, score="softmax", bias=None, groups=1, top_groups=1, group_best=1, renorm=True, scale=1.0,
+              stream=None):
+        """som_route: {"weights" fp32 [T, k], "indices" int32 [T, k], "counts" int32 [E]}."""
+        if not isinstance(logits, torch.Tensor) or logits.dim() != 2:
+            raise TypeError("logits must be a 2-d CUDA tensor")
+        T, E = logits.shape
+        lp, ld = _matrix(logits, (T, E), logits.dtype, "logits")
+        kind = _code(_TYPES, logits.dtype, "logits' type")
+        out = {"weights": self._empty((T, k), torch.float32), "indices": self._empty((T, k), torch.int32),
+               "counts": self._empty((E,), torch.int32)}
+        rc = self._lib.som_route(self._h, kind, _code(_SCORES, score, "score"), T, E, k, lp, ld,
+                                 _whole(bias, (E,), torch.float32, "bias"), groups, top_groups, group_best, int(renorm), scale,
+                                 out["weights"].data_ptr(), out["indices"].data_ptr(), out["counts"].data_ptr(),
+                                 self._stream(stream))
+        self._check(rc, "som_route")
+        return out
+
+    def route_backward(self, logits, indices, dweights, score="softmax", renorm=True, scale=1.0, stream=None):
+        """som_route_backward: the logits' gradient [T, E]."""
+        if not isinstance(logits, torch.Tensor) or logits.dim() != 2:
+            raise TypeError("logits must be a 2-d CUDA tensor")
+        T, E = logits.shape
+        lp, ld = _matrix(logits, (T, E), logits.dtype, "logits")
+        kind = _code(_TYPES, logits.dtype, "logits' type")
+        k = indices.shape[-1]
+        out = self._empty((T, E), logits.dtype)
+        rc = self._lib.som_route_backward(self._h, kind, _code(_SCORES, score, "score"), T, E, k, lp, ld,
+                                          _whole(indices, (T, k), torch.int32, "indices"),
+                                          _whole(dweights, (T, k), torch.float32, "dweights"), int(renorm), scale,
+                                          out.data_ptr(), self._stream(stream))
+        self._check(rc, "som_route_backward")
+        return out
+
+    def _experts(self, x, indices, weights, w1, w2, b1, b2, gated):
+        kind = self._half(x)
+        if w1.dim() != 3 or w2.dim() != 3 or indices.dim() != 2:
+            raise ValueError("w1 and w2 must be 3-d, indices 2-d")
+        T, D = x.shape
+        E, rows = w1.shape[:2]
+        if gated and rows % 2:
+            raise ValueError("a gated w1 has an even number of rows")
+        I = rows // 2 if gated else rows
+        k = indices.shape[1]
+        if weights.dtype not in (torch.float32, x.dtype):
+            raise TypeError("weights must be float32 or of x's type")
+        xp, ldx = _matrix(x, (T, D), x.dtype, "x")
+        return kind, T, E, k, D, I, rows, (xp, ldx, _whole(indices, (T, k), torch.int32, "indices"),
+                                           _whole(weights, (T, k), weights.dtype, "weights"), _TYPES[weights.dtype],
+                                           _whole(w1, (E, rows, D), x.dtype, "w1"), _whole(b1, (E, rows), x.dtype, "b1"),
+                                           _whole(w2, (E, D, I), x.dtype, "w2"), _whole(b2, (E, D), x.dtype, "b2"))
+
+    def experts(self, x, indices, weights, w1, w2, b1=None, b2=None, residual=None, act="silu", gated=True, out=None, stream=None):
+        """som_experts: residual + sum over a token's experts of weight * (w2 act(w1 x + b1) + b2).  Returns [T, D]."""
+        kind, T, E, k, D, I, rows, p = self._experts(x, indices, weights, w1, w2, b1, b2, gated)
+        if out is None:
+            out = self._empty((T, D), x.dtype)
+        yp, ldy = _matrix(out, (T, D), x.dtype, "out")
+        rp, ldr = (0, 0) if residual is None else _matrix(residual, (T, D), x.dtype, "residual")
+        rc = self._lib.som_experts(self._h, kind, _code(_ACTS, act, "act"), int(gated), T, E, k, D, I, *p, rp, ldr, yp, ldy,
+                                   self._stream(stream))
+        self._check(rc, "som_experts")
+        return out
+
+    def experts_backward(self, x, indices, weights, w1, w2, dy, b1=None, b2=None, act="silu", gated=True, stream=None):
+        """som_experts_backward: {"dx", "dweights", "dw1", "dw2"} and, with biases, "db1", "db2"."""
+        kind, T, E, k, D, I, rows, p = self._experts(x, indices, weights, w1, w2, b1, b2, gated)
+        gp, ldg = _matrix(dy, (T, D), x.dtype, "dy")
+        out = {"dx": self._empty((T, D), x.dtype), "dweights": self._empty((T, k), weights.dtype),
+               "dw1": self._empty((E, rows, D), x.dtype), "dw2": self._empty((E, D, I), x.dtype)}
+        if b1 is not None:
+            out["db1"] = self._empty((E, rows), x.dtype)
+        if b2 is not None:
+            out["db2"] = self._empty((E, D), x.dtype)
+        at = lambda n: out[n].data_ptr() if n in out else 0  # noqa: E731
+        rc = self._lib.som_experts_backward(self._h, kind, _code(_ACTS, act, "act"), int(gated), T, E, k, D, I, *p, gp, ldg,
+                                            at("dx"), at("dweights"), at("dw1"), at("db1"), at("dw2"), at("db2"),
+                                            self._stream(stream))
+        self._check(rc, "som_experts_backward")
+        return out
+
+    def device_flags(self, stream=None) -> int:
+        """som_layers_device_flags: status of what earlier calls skipped on the device (0 = nothing); synchronises."""
+        return int(self._lib.som_layers_device_flags(self._h, self._stream(stream)))
+
+    def launch_count(self) -> int:
+        return int(self._lib.som_layers_launch_count(self._h))
+
+    def destroy(self):
+        if self._h:
+            self._lib.som_layers_destroy(self._h)
+            self._h = ctypes.c_void_p()
+
+    def __del__(self):
+        try:
+            self.destroy()
+        except Exception:
+            pass

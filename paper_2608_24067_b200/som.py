@@ -27,6 +27,9 @@ EXPORTS = [
     "som_launch_count", "som_set_option", "som_norms_noalloc", "som_bmu2", "som_create_f16", "som_update", "som_last_uncertain", "som_bmu_values",
     "som_bmu_host_async", "som_host_sync", "som_plan_create", "som_bmu_planned", "som_plan_destroy",
     "som_device_flags", "som_measure_fadd_peak", "som_measure_operand_paths", "som_tc_probe",
+    "som_layers_create", "som_layers_destroy", "som_layers_last_cuda_error", "som_layers_launch_count",
+    "som_layers_device_flags", "som_linear", "som_linear_backward", "som_route", "som_route_backward", "som_experts",
+    "som_experts_backward",
 ]
 
 NOALLOC_MAX_M = 524288
@@ -100,6 +103,24 @@ def load_library():
     lib.som_device_flags.restype = INT
     lib.som_norms_noalloc.argtypes = [I32, I64, P, P, P]
     lib.som_norms_noalloc.restype = INT
+    F32 = ctypes.c_float
+    lib.som_layers_create.argtypes = [ctypes.POINTER(P)]
+    lib.som_layers_destroy.argtypes = [P]
+    lib.som_layers_last_cuda_error.argtypes = [P]
+    lib.som_layers_launch_count.argtypes = [P]
+    lib.som_layers_device_flags.argtypes = [P, P]
+    lib.som_linear.argtypes = [P, INT, INT, INT, I64, I64, I64, P, I64, P, P, P, I64, P, I64, P]
+    lib.som_linear_backward.argtypes = [P, INT, INT, INT, I64, I64, I64, P, I64, P, P, P, I64, P, P, P, P]
+    lib.som_route.argtypes = [P, INT, INT, I64, I32, I32, P, I64, P, I32, I32, I32, INT, F32, P, P, P, P]
+    lib.som_route_backward.argtypes = [P, INT, INT, I64, I32, I32, P, I64, P, P, INT, F32, P, P]
+    experts = [P, INT, INT, INT, I64, I32, I32, I64, I64, P, I64, P, P, INT, P, P, P, P, P, I64]
+    lib.som_experts.argtypes = experts + [P, I64, P]
+    lib.som_experts_backward.argtypes = experts + [P, P, P, P, P, P, P]
+    for name in ("som_layers_create", "som_layers_destroy", "som_layers_last_cuda_error", "som_layers_device_flags",
+                 "som_linear", "som_linear_backward", "som_route", "som_route_backward", "som_experts",
+                 "som_experts_backward"):
+        getattr(lib, name).restype = INT
+    lib.som_layers_launch_count.restype = I64
     for name in ("som_create", "som_norms", "som_bmu", "som_bmu_host", "som_validate_csr",
                  "som_get_norms", "som_destroy", "som_last_cuda_error", "som_set_timing",
                  "som_get_timing", "som_set_option"):
