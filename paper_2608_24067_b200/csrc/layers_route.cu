@@ -169,7 +169,7 @@ __global__ void __launch_bounds__(32 * ROUTE_WARPS) k_route(const RouteArgs a)
             float m = xj;
 #pragma unroll
             for (int d = 16; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor_sync(ALL, m, d));
-            if (at >= 0) s = exp_from(xj, m);
+            if (at >= 0 && (m == top || top < INFINITY)) s = exp_from(xj, m);  // (beside an infinite logit all others score 0)
         } else if (at >= 0) {
             s = exp_from(xj, top) / total;
         }
