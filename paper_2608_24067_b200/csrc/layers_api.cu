@@ -108,18 +108,30 @@ int check_sizes(int64_t a, int64_t b)
 
 int tiles_of(int64_t n, int64_t width) { return (int)((n + width - 1) / width); }
 
-// rows x cols 16-bit matrix as the K-major operand of a product (boxes of 128 rows) or M/N-major (64 rows)
-int map_k(som_layers* l, CUtensorMap* m, const void* p, int64_t cols, int64_t rows, int64_t ld, int64_t batch = 1)
+// 16-bit operands of the products: the left one K-major in boxes of 128 rows; the right one, and M/N-major ones, of 64
+int map_left(som_layers* l, CUtensorMap* m, const void* p, int64_t cols, int64_t rows, int64_t ld)
 {
-    return make_map(l, m, p, 2, cols, rows, batch, ld, rows * ld, 64, 128);
+    return make_map(l, m, p, 2, cols, rows, 1, ld, rows * ld, 64, 128);
 }
-int map_mn(som_layers* l, CUtensorMap* m, const void* p, int64_t cols, int64_t rows, int64_t ld, int64_t batch = 1)
+int map_64(som_layers* l, CUtensorMap* m, const void* p, int64_t cols, int64_t rows, int64_t ld, int64_t batch = 1)
 {
     return make_map(l, m, p, 2, cols, rows, batch, ld, rows * ld, 64, 64);
 }
 int map_out(som_layers* l, CUtensorMap* m, void* p, int bytes, int64_t cols, int64_t rows, int64_t ld, int64_t batch = 1)
 {
     return make_map(l, m, p, bytes, cols, rows, batch, ld, rows * ld, 32, 32);
+}
+
+// The tiles of a product of `rows` x `cols` outputs (`batch` of them).  Pairs of blocks do twice a single block's work per
+// byte that they load, but need tiles enough for every SM: singles where pairs would leave more than a third of them idle.
+void set_tiles(const som_layers* l, ProdArgs* a, int64_t rows, int64_t cols, bool gated, int64_t batch = 1)
+{
+    const int64_t pr = tiles_of(rows, PAIR_ROWS), pc = tiles_of(cols, gated ? PAIR_COLS / 2 : PAIR_COLS);
+    a->pair = 3 * pr * pc * batch >= 2 * l->pairs;
+    a->row_tiles = a->pair ? (int)pr : tiles_of(rows, SINGLE_ROWS);
+    a->col_tiles = a->pair ? (int)pc : tiles_of(cols, gated ? SINGLE_COLS / 2 : SINGLE_COLS);
+    a->rows = (int)rows;
+    a->cols = (int)cols;
 }
 
 }  // namespace
@@ -145,6 +157,7 @@ int som_layers_create(som_layers** out)
     cudaDriverEntryPointQueryResult found;
     cudaError_t e = cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &l->encode, cudaEnableDefault, &found);
     if (e == cudaSuccess && (found != cudaDriverEntryPointSuccess || !l->encode)) e = cudaErrorNotSupported;
+    if (e == cudaSuccess) e = prepare_product(l);
     if (e == cudaSuccess) e = cudaMalloc(reinterpret_cast<void**>(&l->flags), 256);
     if (e == cudaSuccess) e = cudaMemset(l->flags, 0, 256);
     if (e != cudaSuccess) {
@@ -196,17 +209,14 @@ int som_linear(som_layers* l, int type, int act, int gated, int64_t T, int64_t D
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
     const int64_t rows = gated ? 2 * F : F;
     ProdArgs a = {};
-    LAY_TRY(map_k(l, &a.a, x, D, T, ldx));
-    LAY_TRY(map_k(l, &a.b, w, D, rows, D));
+    LAY_TRY(map_left(l, &a.a, x, D, T, ldx));
+    LAY_TRY(map_64(l, &a.b, w, D, rows, D));
     LAY_TRY(map_out(l, &a.o0, y, 2, F, T, ldy));
     a.bias = static_cast<const uint16_t*>(bias);
     a.extra = static_cast<const uint16_t*>(residual);
     a.ld_extra = ldr;
-    a.row_tiles = tiles_of(T, 128);
-    a.col_tiles = tiles_of(F, gated ? 128 : 256);
+    set_tiles(l, &a, T, F, gated);
     a.experts = 1;
-    a.rows = (int)T;
-    a.cols = (int)F;
     a.gate_rows = gated ? (int)F : 0;
     a.k1 = (int)D;
     a.act = act;
@@ -242,50 +252,55 @@ int som_linear_backward(som_layers* l, int type, int act, int gated, int64_t T, 
     a.bf16 = type == SOM_BF16;
     a.flags = l->flags;
     if (again) {
-        LAY_TRY(ensure(l, (size_t)T * rows * 2));
-        dz = l->ws;
+        uint16_t* z_grad;
+        float* sums;
+        Carver c{nullptr, 0};
+        for (int pass = 0; pass < 2; ++pass) {
+            c.used = 0;
+            z_grad = c.take<uint16_t>(T * rows);
+            sums = c.take<float>(dbias ? tiles_of(T, 32) * rows : 0);
+            if (pass == 0) {
+                LAY_TRY(ensure(l, c.used));
+                c.base = static_cast<unsigned char*>(l->ws);
+            }
+        }
+        dz = z_grad;
         lddz = rows;
         ProdArgs z = a;
-        LAY_TRY(map_k(l, &z.a, x, D, T, ldx));
-        LAY_TRY(map_k(l, &z.b, w, D, rows, D));
-        LAY_TRY(map_out(l, &z.o0, l->ws, 2, F, T, rows));
-        if (gated) LAY_TRY(map_out(l, &z.o1, static_cast<uint16_t*>(l->ws) + F, 2, F, T, rows));
+        LAY_TRY(map_left(l, &z.a, x, D, T, ldx));
+        LAY_TRY(map_64(l, &z.b, w, D, rows, D));
+        LAY_TRY(map_out(l, &z.o0, z_grad, 2, F, T, rows));
+        if (gated) LAY_TRY(map_out(l, &z.o1, z_grad + F, 2, F, T, rows));
         z.bias = static_cast<const uint16_t*>(bias);
         z.extra = static_cast<const uint16_t*>(dy);
         z.ld_extra = lddy;
-        z.row_tiles = tiles_of(T, 128);
-        z.col_tiles = tiles_of(F, gated ? 128 : 256);
-        z.rows = (int)T;
-        z.cols = (int)F;
+        z.column_sums = dbias ? sums : nullptr;
+        set_tiles(l, &z, T, F, gated);
         z.gate_rows = gated ? (int)F : 0;
         z.k1 = (int)D;
         LAY_TRY(launch_product(l, PROD_DZ, z, st));
+        if (dbias) LAY_TRY(launch_join_sums(l, SlotPlan(), 1, T, sums, rows, dbias, a.bf16, st));
+    } else if (dbias) {
+        LAY_TRY(launch_column_sums(l, SlotPlan(), 1, T, dy, lddy, rows, dbias, a.bf16, st));
     }
     if (dx) {
         ProdArgs p = a;
-        LAY_TRY(map_k(l, &p.a, dz, rows, T, lddz));
-        LAY_TRY(map_mn(l, &p.b, w, D, rows, D));
+        LAY_TRY(map_left(l, &p.a, dz, rows, T, lddz));
+        LAY_TRY(map_64(l, &p.b, w, D, rows, D));
         LAY_TRY(map_out(l, &p.o0, dx, 2, D, T, D));
-        p.row_tiles = tiles_of(T, 128);
-        p.col_tiles = tiles_of(D, 256);
-        p.rows = (int)T;
-        p.cols = (int)D;
+        set_tiles(l, &p, T, D, false);
         p.k1 = (int)rows;
         LAY_TRY(launch_product(l, PROD_DX, p, st));
     }
     if (dw) {
         ProdArgs p = a;
-        LAY_TRY(map_mn(l, &p.a, dz, rows, T, lddz));
-        LAY_TRY(map_mn(l, &p.b, x, D, T, ldx));
+        LAY_TRY(map_64(l, &p.a, dz, rows, T, lddz));
+        LAY_TRY(map_64(l, &p.b, x, D, T, ldx));
         LAY_TRY(map_out(l, &p.o0, dw, 2, D, rows, D));
-        p.row_tiles = tiles_of(rows, 128);
-        p.col_tiles = tiles_of(D, 256);
-        p.rows = (int)rows;
-        p.cols = (int)D;
+        set_tiles(l, &p, rows, D, false);
         p.k1 = (int)T;
         LAY_TRY(launch_product(l, PROD_DW, p, st));
     }
-    if (dbias) LAY_TRY(launch_column_sums(l, nullptr, 1, T, dz, lddz, nullptr, rows, dbias, a.bf16, st));
     return SOM_OK;
 }
 
@@ -353,15 +368,23 @@ static SlotPlan carve_plan(Carver& c, int64_t T, int E, int k, int tile)
     return p;
 }
 
-static ProdArgs grouped(const som_layers* l, const SlotPlan& p, int type)
+// Pairs of blocks once the experts have rows enough for their tiles (256 rows); with fewer, a pair would mostly multiply
+// padding, and the weights' bytes bound the product, not the tensor cores.
+static bool pair_rows(int64_t T, int E, int k) { return T * k >= (int64_t)128 * E; }
+
+static ProdArgs grouped(const som_layers* l, const SlotPlan& p, int type, int64_t cols, bool gated)
 {
     ProdArgs a = {};
     a.tiles = p.tiles;
     a.tile_expert = p.tile_expert;
+    a.seg = p.seg;
+    a.count = p.count;
     a.row_weight = p.row_weight;
-    a.row_slot = p.row_slot;
+    a.pair = p.tile == PAIR_ROWS;
     a.row_tiles = p.max_rows / p.tile;
+    a.col_tiles = tiles_of(cols, (a.pair ? PAIR_COLS : SINGLE_COLS) / (gated ? 2 : 1));
     a.rows = p.max_rows;
+    a.cols = (int)cols;
     a.bf16 = type == SOM_BF16;
     a.flags = l->flags;
     return a;
@@ -385,7 +408,7 @@ int som_experts(som_layers* l, int type, int act, int gated, int64_t T, int32_t 
     Carver c{nullptr, 0};
     for (int pass = 0; pass < 2; ++pass) {
         c.used = 0;
-        p = carve_plan(c, T, E, k, 128);
+        p = carve_plan(c, T, E, k, pair_rows(T, E, k) ? PAIR_ROWS : SINGLE_ROWS);
         xp = c.take<uint16_t>((int64_t)p.max_rows * D);
         h = c.take<uint16_t>((int64_t)p.max_rows * I);
         part = c.take<float>((int64_t)p.max_rows * D);
@@ -395,28 +418,24 @@ int som_experts(som_layers* l, int type, int act, int gated, int64_t T, int32_t 
         }
     }
     LAY_TRY(launch_plan(l, p, indices, weights, weights_type, T, k, E, st));
-    LAY_TRY(launch_gather(l, p, E, k, D, x, ldx, xp, nullptr, 0, nullptr, st));
-    ProdArgs a = grouped(l, p, type);
-    LAY_TRY(map_k(l, &a.a, xp, D, p.max_rows, D));
-    LAY_TRY(map_k(l, &a.b, w1, D, rows1, D, E));
+    LAY_TRY(launch_gather(l, p, k, D, x, ldx, xp, nullptr, 0, nullptr, st));
+    ProdArgs a = grouped(l, p, type, I, gated);
+    LAY_TRY(map_left(l, &a.a, xp, D, p.max_rows, D));
+    LAY_TRY(map_64(l, &a.b, w1, D, rows1, D, E));
     LAY_TRY(map_out(l, &a.o0, h, 2, I, p.max_rows, I));
     a.bias = static_cast<const uint16_t*>(b1);
     a.bias_ld = (int)rows1;
-    a.col_tiles = tiles_of(I, gated ? 128 : 256);
-    a.cols = (int)I;
     a.gate_rows = gated ? (int)I : 0;
     a.k1 = (int)D;
     a.act = act;
     a.weigh = 1;
     LAY_TRY(launch_product(l, PROD_FWD, a, st));
-    a = grouped(l, p, type);
-    LAY_TRY(map_k(l, &a.a, h, I, p.max_rows, I));
-    LAY_TRY(map_k(l, &a.b, w2, I, D, I, E));
+    a = grouped(l, p, type, D, false);
+    LAY_TRY(map_left(l, &a.a, h, I, p.max_rows, I));
+    LAY_TRY(map_64(l, &a.b, w2, I, D, I, E));
     LAY_TRY(map_out(l, &a.o0, part, 4, D, p.max_rows, D));
     a.bias = static_cast<const uint16_t*>(b2);
     a.bias_ld = (int)D;
-    a.col_tiles = tiles_of(D, 256);
-    a.cols = (int)D;
     a.k1 = (int)I;
     a.weigh = 2;
     a.out32 = 1;
@@ -443,83 +462,76 @@ int som_experts_backward(som_layers* l, int type, int act, int gated, int64_t T,
         if (db2) SOM_CK(l, cudaMemsetAsync(db2, 0, (size_t)E * D * 2, st));
         return SOM_OK;
     }
-    const int col_tiles = tiles_of(I, gated ? 128 : 256);
     SlotPlan p;
     uint16_t *xp, *dyp, *h, *dz;
-    float *part, *dot;
+    float *part, *dot, *sums;
+    const bool pair = pair_rows(T, E, k);
+    const int col_tiles = tiles_of(I, (pair ? PAIR_COLS : SINGLE_COLS) / (gated ? 2 : 1));
     Carver c{nullptr, 0};
     for (int pass = 0; pass < 2; ++pass) {
         c.used = 0;
-        p = carve_plan(c, T, E, k, 128);
+        p = carve_plan(c, T, E, k, pair ? PAIR_ROWS : SINGLE_ROWS);
         xp = c.take<uint16_t>((int64_t)p.max_rows * D);
         dyp = c.take<uint16_t>((int64_t)p.max_rows * D);
         h = c.take<uint16_t>((int64_t)p.max_rows * I);
         dz = c.take<uint16_t>((int64_t)p.max_rows * rows1);
         part = c.take<float>((int64_t)p.max_rows * D);
         dot = c.take<float>((int64_t)p.max_rows * 2 * col_tiles);
+        sums = c.take<float>(db1 ? p.max_rows / 32 * rows1 : 0);
         if (pass == 0) {
             LAY_TRY(ensure(l, c.used));
             c.base = static_cast<unsigned char*>(l->ws);
         }
     }
     LAY_TRY(launch_plan(l, p, indices, weights, weights_type, T, k, E, st));
-    LAY_TRY(launch_gather(l, p, E, k, D, x, ldx, xp, dy, lddy, dyp, st));
+    LAY_TRY(launch_gather(l, p, k, D, x, ldx, xp, dy, lddy, dyp, st));
     // z and g = W2^T dy side by side -> dz, the weighted h, partial sums of <h, g>
-    ProdArgs a = grouped(l, p, type);
-    LAY_TRY(map_k(l, &a.a, xp, D, p.max_rows, D));
-    LAY_TRY(map_k(l, &a.b, w1, D, rows1, D, E));
-    LAY_TRY(map_k(l, &a.a2, dyp, D, p.max_rows, D));
-    LAY_TRY(map_mn(l, &a.b2, w2, I, D, I, E));
+    ProdArgs a = grouped(l, p, type, I, gated);
+    LAY_TRY(map_left(l, &a.a, xp, D, p.max_rows, D));
+    LAY_TRY(map_64(l, &a.b, w1, D, rows1, D, E));
+    LAY_TRY(map_left(l, &a.a2, dyp, D, p.max_rows, D));
+    LAY_TRY(map_64(l, &a.b2, w2, I, D, I, E));
     LAY_TRY(map_out(l, &a.o0, dz, 2, I, p.max_rows, rows1));
     if (gated) LAY_TRY(map_out(l, &a.o1, dz + I, 2, I, p.max_rows, rows1));
     LAY_TRY(map_out(l, &a.o2, h, 2, I, p.max_rows, I));
     a.bias = static_cast<const uint16_t*>(b1);
     a.bias_ld = (int)rows1;
     a.dot = dot;
-    a.col_tiles = col_tiles;
-    a.cols = (int)I;
+    a.column_sums = db1 ? sums : nullptr;
     a.gate_rows = gated ? (int)I : 0;
     a.k1 = a.k2 = (int)D;
     a.act = act;
-    LAY_TRY(launch_product(l, PROD_DZ_PAIR, a, st));
+    LAY_TRY(launch_product(l, PROD_DZ_TWO, a, st));
     LAY_TRY(launch_dweights(l, p, indices, T, k, D, dot, 2 * col_tiles, b2, dy, lddy, dweights, weights_type, a.bf16, st));
+    if (db1) LAY_TRY(launch_join_sums(l, p, E, 0, sums, rows1, db1, a.bf16, st));
+    if (db2) LAY_TRY(launch_column_sums(l, p, E, 0, dyp, D, D, db2, a.bf16, st));
     // dx
-    a = grouped(l, p, type);
-    LAY_TRY(map_k(l, &a.a, dz, rows1, p.max_rows, rows1));
-    LAY_TRY(map_mn(l, &a.b, w1, D, rows1, D, E));
+    a = grouped(l, p, type, D, false);
+    LAY_TRY(map_left(l, &a.a, dz, rows1, p.max_rows, rows1));
+    LAY_TRY(map_64(l, &a.b, w1, D, rows1, D, E));
     LAY_TRY(map_out(l, &a.o0, part, 4, D, p.max_rows, D));
-    a.col_tiles = tiles_of(D, 256);
-    a.cols = (int)D;
     a.k1 = (int)rows1;
     a.out32 = 1;
     LAY_TRY(launch_product(l, PROD_DX, a, st));
     LAY_TRY(launch_join(l, p, T, k, D, part, nullptr, 0, dx, D, a.bf16, st));
     // dw1 = dz^T x, dw2 = dy^T (weighted h)
-    a = grouped(l, p, type);
+    a = ProdArgs();
     a.seg = p.seg;
+    a.count = p.count;
     a.experts = E;
-    a.row_weight = nullptr;
-    a.row_slot = nullptr;
+    a.bf16 = type == SOM_BF16;
+    a.flags = l->flags;
     ProdArgs b = a;
-    LAY_TRY(map_mn(l, &a.a, dz, rows1, p.max_rows, rows1));
-    LAY_TRY(map_mn(l, &a.b, xp, D, p.max_rows, D));
+    LAY_TRY(map_64(l, &a.a, dz, rows1, p.max_rows, rows1));
+    LAY_TRY(map_64(l, &a.b, xp, D, p.max_rows, D));
     LAY_TRY(map_out(l, &a.o0, dw1, 2, D, rows1, D, E));
-    a.row_tiles = tiles_of(rows1, 128);
-    a.col_tiles = tiles_of(D, 256);
-    a.rows = (int)rows1;
-    a.cols = (int)D;
+    set_tiles(l, &a, rows1, D, false, E);
     LAY_TRY(launch_product(l, PROD_DW, a, st));
-    LAY_TRY(map_mn(l, &b.a, dyp, D, p.max_rows, D));
-    LAY_TRY(map_mn(l, &b.b, h, I, p.max_rows, I));
+    LAY_TRY(map_64(l, &b.a, dyp, D, p.max_rows, D));
+    LAY_TRY(map_64(l, &b.b, h, I, p.max_rows, I));
     LAY_TRY(map_out(l, &b.o0, dw2, 2, I, D, I, E));
-    b.row_tiles = tiles_of(D, 128);
-    b.col_tiles = tiles_of(I, 256);
-    b.rows = (int)D;
-    b.cols = (int)I;
-    LAY_TRY(launch_product(l, PROD_DW, b, st));
-    if (db1) LAY_TRY(launch_column_sums(l, p.seg, E, 0, dz, rows1, nullptr, rows1, db1, a.bf16, st));
-    if (db2) LAY_TRY(launch_column_sums(l, p.seg, E, 0, dyp, D, p.row_weight, D, db2, a.bf16, st));
-    return SOM_OK;
+    set_tiles(l, &b, D, I, false, E);
+    return launch_product(l, PROD_DW, b, st);
 }
 
 }  // extern "C"

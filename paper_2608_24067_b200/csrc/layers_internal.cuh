@@ -15,6 +15,7 @@
 struct som_layers {
     int device;
     int sm_count;
+    int pairs;  // pairs of blocks that the products' kernels can have resident
     void* ws;  // grow-only device workspace of all calls on the handle
     size_t ws_bytes;
     int* flags;  // device, sticky LAY_FLAG_* bits
@@ -33,11 +34,13 @@ struct SlotPlan {
     int* tiles;        // [1] row tiles in use
     int* tile_expert;  // [max tiles]
     int* pos;          // [T * k] row of a slot, -1 = none
-    int* row_slot;     // [max rows] slot of a row, -1 = padding
-    float* row_weight; // [max rows] the slot's routing weight, 0 in padding
+    int* row_slot;     // [max rows] slot of a row in use
+    float* row_weight; // [max rows] the slot's routing weight
     int max_rows;      // upper bound that the host sizes buffers and grids by
     int tile;          // rows of a tile
 };
+
+cudaError_t prepare_product(som_layers* l);  // once per handle
 
 int launch_plan(som_layers* l, const SlotPlan& p, const int32_t* indices, const void* weights, int weights_type, int64_t T,
                 int k, int E, cudaStream_t st);

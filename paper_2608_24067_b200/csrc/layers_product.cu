@@ -1,12 +1,17 @@
 // Matrix products of the dense operators on the 5th-generation tensor cores.
 //
-// One persistent block per SM walks the output tiles (128 rows x 256 columns of accumulator).  Warp 0 issues the TMA
-// copies of a four-stage ring (64 k of both operands a stage, 48 KB, 128-byte swizzle), warp 1 issues the matrix
-// instructions (tcgen05.mma, 128 x 256 x 16, fp32 accumulators in tensor memory), eight warps run the epilogue.  The
-// accumulator is double-buffered (2 x 256 of the 512 columns of tensor memory), so that the epilogue of a tile runs
-// under the products of the next; PROD_DZ_PAIR keeps two products of a tile side by side and has one buffer.  Operands
-// enter K-major (a row holds consecutive k) or M/N-major (a row holds consecutive rows of the product), as they lie in
-// memory: no operand is transposed beforehand.  Every wait is bounded.
+// Persistent blocks, one per SM, walk the output tiles.  Warp 0 issues the TMA copies of a six-stage ring (64 k of both
+// operands a stage, 32 KB, 128-byte swizzle), warp 1 issues the matrix instructions (tcgen05.mma, fp32 accumulators in
+// tensor memory), eight warps run the epilogue.  The accumulator is double-buffered, so that the epilogue of a tile runs
+// under the products of the next; PROD_DZ_TWO keeps two products of a tile side by side and has one buffer.  Operands enter
+// K-major (a row holds consecutive k) or M/N-major (a row holds consecutive rows of the product), as they lie in memory: no
+// operand is transposed beforehand.  Every wait is bounded.
+//
+// Two tile shapes.  PAIR: two blocks of a cluster share a tile of 256 x 256; each loads its own 128 rows of A and one half of
+// B, and the matrix instruction reads both halves (cta_group::2).  A single block on 128 x 256 moves 48 KB into and 48 KB out
+// of its shared memory for 512 clocks of matrix work, 192 bytes a clock where shared memory gives 128: 4096 x 4096 x 4096
+// took 134 us so.  With the pair it is 32 KB each way, 128 bytes a clock.  SINGLE: 128 x 128 by one block, for products
+// that have too few tiles to fill the SMs with pairs or too few rows per expert.
 #include "layers_math.cuh"
 #include "layers_product.cuh"
 #include "layers_ptx.cuh"
@@ -14,17 +19,21 @@
 namespace lay {
 namespace {
 
-constexpr int BM = 128, BN = 256, BK = 64, STAGES = 4;
-constexpr int A_BYTES = BM * BK * 2, B_BYTES = BN * BK * 2, STAGE_BYTES = A_BYTES + B_BYTES;
+constexpr int BM = 128, BK = 64, STAGES = 6;
+constexpr int HALF = 128 * BK * 2;  // bytes of a block's share of an operand in a stage
+constexpr int STAGE_BYTES = 2 * HALF;
 constexpr int BOX = 64 * 128;  // bytes of a box of 64 rows
 constexpr int EPI_WARPS = 8, THREADS = 32 * (2 + EPI_WARPS);
 constexpr int OUT_BYTES = 32 * 128;  // an epilogue warp's staged output: 32 rows of 128 bytes
 constexpr int SMEM = 1024 + STAGES * STAGE_BYTES + EPI_WARPS * OUT_BYTES;
 
 struct Tile {
-    int row, col, expert;  // first row and column of the output, expert
-    int k0, k;             // PROD_DW: first row of the sum and its length
+    int row, col, expert;  // this block's first row and the tile's first column of the output, expert
+    int k0, k;             // PROD_DW: first row of the sum; length of the first product's sum
+    int live, store;       // rows below `live` are in use, rows below `store` are written (zeros from `live` on)
 };
+
+__device__ __forceinline__ int round64(int n) { return (n + 63) & ~63; }
 
 template <int MODE>
 __device__ __forceinline__ int tile_count(const ProdArgs& p)
@@ -33,25 +42,34 @@ __device__ __forceinline__ int tile_count(const ProdArgs& p)
     return (p.tiles ? *p.tiles : p.row_tiles) * p.col_tiles;
 }
 
-template <int MODE>
-__device__ __forceinline__ Tile tile_at(const ProdArgs& p, int idx, int width)
+template <int MODE, bool PAIR>
+__device__ __forceinline__ Tile tile_at(const ProdArgs& p, int idx, int width, int rank)
 {
+    constexpr int ROWS = PAIR ? PAIR_ROWS : SINGLE_ROWS;
     Tile t;
     if (MODE == PROD_DW) {
         const int per = p.row_tiles * p.col_tiles;
         t.expert = idx / per;
-        const int rest = idx - t.expert * per;
-        t.row = (rest / p.col_tiles) * BM;
-        t.col = (rest % p.col_tiles) * width;
+        const int rest = idx - t.expert * per, rt = rest / p.col_tiles;
+        t.row = rt * ROWS + rank * BM;
+        t.col = (rest - rt * p.col_tiles) * width;
         t.k0 = p.seg ? p.seg[t.expert] : 0;
-        t.k = p.seg ? p.seg[t.expert + 1] - t.k0 : p.k1;
+        t.k = p.seg ? round64(p.count[t.expert]) : p.k1;
+        t.live = t.store = p.rows;
     } else {
         const int rt = idx / p.col_tiles;
-        t.row = rt * BM;
+        t.row = rt * ROWS + rank * BM;
         t.col = (idx - rt * p.col_tiles) * width;
         t.expert = p.tile_expert ? p.tile_expert[rt] : 0;
         t.k0 = 0;
         t.k = p.k1;
+        t.live = t.store = p.rows;
+        if (p.seg) {
+            const int s = p.seg[t.expert], n = p.count[t.expert];
+            t.live = s + n;
+            // the sums over an expert's rows (PROD_DW) run over whole steps of 64 rows
+            t.store = MODE == PROD_DZ_TWO ? s + round64(n) : t.live;
+        }
     }
     return t;
 }
@@ -100,24 +118,53 @@ struct Stager {
     }
 };
 
-// v[j] += bias[col + j] * s for the columns below `cols` (a multiple of 8)
-__device__ __forceinline__ void add_row(float (&v)[32], const uint16_t* bias, int col, int cols, float s, int bf16)
+// 32 values of a row of a 16-bit matrix, fetched before they are needed; zeros beyond `cols` (a multiple of 8)
+struct Row32 {
+    uint4 w[4];
+    __device__ __forceinline__ void fetch(const uint16_t* row, int col, int cols, bool want)
+    {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            w[j] = want && col + 8 * j < cols ? __ldg(reinterpret_cast<const uint4*>(row + col) + j) : make_uint4(0u, 0u, 0u, 0u);
+    }
+    // v += s * values
+    __device__ __forceinline__ void add(float (&v)[32], float s, int bf16) const
+    {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const uint32_t u[4] = {w[j].x, w[j].y, w[j].z, w[j].w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float2 f = unpack2(u[i], bf16);
+                v[8 * j + 2 * i] = fmaf(f.x, s, v[8 * j + 2 * i]);
+                v[8 * j + 2 * i + 1] = fmaf(f.y, s, v[8 * j + 2 * i + 1]);
+            }
+        }
+    }
+};
+
+// Lane l holds v[0..31] of row l; returns to lane l the sum of column l over the 32 rows (31 exchanges, fixed order).
+__device__ __forceinline__ float column_sum(float (&v)[32], int lane)
 {
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
-        if (col + 8 * j < cols) {
-            float b[8];
-            load8(bias + col + 8 * j, b, bf16);
+    for (int h = 16; h >= 1; h >>= 1) {
+        const bool up = lane & h;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[8 * j + i] = fmaf(b[i], s, v[8 * j + i]);
+        for (int j = 0; j < h; ++j) {
+            const float give = up ? v[j] : v[j + h], keep = up ? v[j + h] : v[j];
+            v[j] = keep + __shfl_xor_sync(0xffffffffu, give, h);
         }
+    }
+    return v[0];
 }
 
-template <int MODE>
+template <int MODE, bool PAIR>
 __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ ProdArgs p)
 {
     constexpr bool A_MN = MODE == PROD_DW, B_MN = MODE == PROD_DX || MODE == PROD_DW;
-    constexpr int BUFFERS = MODE == PROD_DZ_PAIR ? 1 : 2;
+    constexpr int BUFFERS = MODE == PROD_DZ_TWO ? 1 : 2;
+    constexpr int BN = PAIR ? PAIR_COLS : SINGLE_COLS;
+    constexpr uint32_t TMEM_COLUMNS = 2 * BN;
     extern __shared__ unsigned char smem_raw[];
     __shared__ __align__(8) uint64_t full[STAGES], empty[STAGES], acc_full[2], acc_empty[2], drained;
     __shared__ uint32_t tmem_sh;
@@ -126,6 +173,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
     unsigned char* staged = ring + STAGES * STAGE_BYTES;
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int rank = PAIR ? (int)cluster_rank() : 0;
     if (threadIdx.x == 0) {
         for (int i = 0; i < STAGES; ++i) {
             bar_init(&full[i], 1);
@@ -133,24 +181,27 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
         }
         for (int i = 0; i < 2; ++i) {
             bar_init(&acc_full[i], 1);
-            bar_init(&acc_empty[i], EPI_WARPS);
+            bar_init(&acc_empty[i], EPI_WARPS * (PAIR ? 2 : 1));
         }
         bar_init(&drained, 1);
         gave_up_sh = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    if (warp == 1) tmem_alloc(&tmem_sh, 512);
+    if (warp == 1) tmem_alloc<PAIR>(&tmem_sh, TMEM_COLUMNS);
     tc_fence_before();
     __syncthreads();
+    if (PAIR) cluster_sync();  // the other block's barriers are ready
     tc_fence_after();
     const uint32_t tmem = tmem_sh;
     volatile int* gave_up = &gave_up_sh;
 
     const bool gated = p.gate_rows != 0;
     // output columns of a tile: a gated product spends half of the accumulator's columns on the other half of its rows
-    const int width = gated && (MODE == PROD_FWD || MODE == PROD_DZ || MODE == PROD_DZ_PAIR) ? BN / 2 : BN;
+    const int width = gated && (MODE == PROD_FWD || MODE == PROD_DZ || MODE == PROD_DZ_TWO) ? BN / 2 : BN;
     const int total = tile_count<MODE>(p);
-    const int n2 = width;  // columns of the second product of PROD_DZ_PAIR
+    const int n2 = width;  // columns of the second product of PROD_DZ_TWO
+    const int step = PAIR ? gridDim.x >> 1 : gridDim.x, first_tile = PAIR ? blockIdx.x >> 1 : blockIdx.x;
+    const int share2 = PAIR ? n2 / 2 : n2;  // columns of the second product's B in this block
 
     if (warp == 0) {
         if (lane == 0) {
@@ -158,37 +209,41 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
             uint32_t phase = 0;
             int64_t issued = 0;
             bool ok = true;
-            for (int idx = blockIdx.x; ok && idx < total; idx += gridDim.x) {
-                const Tile t = tile_at<MODE>(p, idx, width);
-                const int it1 = (t.k + BK - 1) / BK, it2 = MODE == PROD_DZ_PAIR ? (p.k2 + BK - 1) / BK : 0;
+            for (int idx = first_tile; ok && idx < total; idx += step) {
+                const Tile t = tile_at<MODE, PAIR>(p, idx, width, rank);
+                // first row (K-major) or column of this block's 128 columns of B
+                const int b0 = !PAIR ? t.col : gated && !B_MN ? t.col + rank * p.gate_rows : t.col + rank * 128;
+                const int b1 = !PAIR && gated && !B_MN ? t.col + p.gate_rows : b0 + 64;
+                const int it1 = (t.k + BK - 1) / BK, it2 = MODE == PROD_DZ_TWO ? (p.k2 + BK - 1) / BK : 0;
                 for (int it = 0; it < it1 + it2; ++it) {
                     if (!bar_wait(&empty[stage], phase ^ 1u, gave_up)) {
                         ok = false;
                         break;
                     }
                     unsigned char* sa = ring + stage * STAGE_BYTES;
-                    unsigned char* sb = sa + A_BYTES;
-                    uint64_t* bar = &full[stage];
-                    if (MODE == PROD_DZ_PAIR && it >= it1) {
+                    unsigned char* sb = sa + HALF;
+                    // the leader's barrier counts both blocks' bytes
+                    const uint32_t bar = PAIR ? cluster_addr(smem_addr(&full[stage]), 0) : smem_addr(&full[stage]);
+                    if (MODE == PROD_DZ_TWO && it >= it1) {
                         const int k = (it - it1) * BK;
-                        bar_expect(bar, A_BYTES + n2 * BK * 2);
-                        tma_load(sa, &p.a2, bar, k, t.row, 0);
-                        for (int j = 0; j < n2 / 64; ++j) tma_load(sb + j * BOX, &p.b2, bar, t.col + 64 * j, k, t.expert);
+                        if (rank == 0) bar_expect(&full[stage], (PAIR ? 2 : 1) * (HALF + share2 * BK * 2));
+                        tma_load<PAIR>(sa, &p.a2, bar, k, t.row, 0);
+                        for (int j = 0; j < share2; j += 64) tma_load<PAIR>(sb + j * 128, &p.b2, bar, t.col + rank * share2 + j, k, t.expert);
                     } else {
                         const int k = t.k0 + it * BK;
-                        bar_expect(bar, STAGE_BYTES);
+                        if (rank == 0) bar_expect(&full[stage], (PAIR ? 2 : 1) * STAGE_BYTES);
                         if (A_MN) {
-                            tma_load(sa, &p.a, bar, t.row, k, 0);
-                            tma_load(sa + BOX, &p.a, bar, t.row + 64, k, 0);
+                            tma_load<PAIR>(sa, &p.a, bar, t.row, k, 0);
+                            tma_load<PAIR>(sa + BOX, &p.a, bar, t.row + 64, k, 0);
                         } else {
-                            tma_load(sa, &p.a, bar, k, t.row, 0);
+                            tma_load<PAIR>(sa, &p.a, bar, k, t.row, 0);
                         }
                         if (B_MN) {
-                            for (int j = 0; j < 4; ++j)
-                                tma_load(sb + j * BOX, &p.b, bar, t.col + 64 * j, k, MODE == PROD_DW ? 0 : t.expert);
+                            tma_load<PAIR>(sb, &p.b, bar, b0, k, MODE == PROD_DW ? 0 : t.expert);
+                            tma_load<PAIR>(sb + BOX, &p.b, bar, b1, k, MODE == PROD_DW ? 0 : t.expert);
                         } else {
-                            tma_load(sb, &p.b, bar, k, t.col, t.expert);
-                            tma_load(sb + 2 * BOX, &p.b, bar, k, gated ? t.col + p.gate_rows : t.col + 128, t.expert);
+                            tma_load<PAIR>(sb, &p.b, bar, k, b0, t.expert);
+                            tma_load<PAIR>(sb + BOX, &p.b, bar, k, b1, t.expert);
                         }
                     }
                     ++issued;
@@ -198,7 +253,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
                     }
                 }
             }
-            if (!ok) {  // copies still in flight write this block's shared memory: let them land before it leaves
+            if (!ok && rank == 0) {  // copies still in flight write shared memory: let them land before the block leaves
                 const long long t0 = clock64();
                 for (int s = 0; s < STAGES; ++s) {
                     const int64_t uses = issued / STAGES + (s < (int)(issued % STAGES) ? 1 : 0);
@@ -207,14 +262,14 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
             }
         }
     } else if (warp == 1) {
-        if (lane == 0) {
+        if (lane == 0 && rank == 0) {
             int stage = 0, n_acc = 0;
             uint32_t phase = 0;
             bool ok = true;
-            const uint32_t idesc1 = mma_desc(p.bf16, A_MN, B_MN, BM, BN);
-            const uint32_t idesc2 = mma_desc(p.bf16, 0, 1, BM, n2);
-            for (int idx = blockIdx.x; ok && idx < total; idx += gridDim.x, ++n_acc) {
-                const Tile t = tile_at<MODE>(p, idx, width);
+            const uint32_t idesc1 = mma_desc(p.bf16, A_MN, B_MN, PAIR ? 256 : 128, BN);
+            const uint32_t idesc2 = mma_desc(p.bf16, 0, 1, PAIR ? 256 : 128, n2);
+            for (int idx = first_tile; ok && idx < total; idx += step, ++n_acc) {
+                const Tile t = tile_at<MODE, PAIR>(p, idx, width, rank);
                 const int buf = BUFFERS == 2 ? n_acc & 1 : 0;
                 const uint32_t use = (uint32_t)(n_acc / BUFFERS) & 1u;
                 if (!bar_wait(&acc_empty[buf], use ^ 1u, gave_up)) {
@@ -222,34 +277,34 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
                     break;
                 }
                 tc_fence_after();
-                const int it1 = (t.k + BK - 1) / BK, it2 = MODE == PROD_DZ_PAIR ? (p.k2 + BK - 1) / BK : 0;
+                const int it1 = (t.k + BK - 1) / BK, it2 = MODE == PROD_DZ_TWO ? (p.k2 + BK - 1) / BK : 0;
                 for (int it = 0; it < it1 + it2; ++it) {
                     if (!bar_wait(&full[stage], phase, gave_up)) {
                         ok = false;
                         break;
                     }
                     tc_fence_after();
-                    const uint32_t sa = smem_addr(ring + stage * STAGE_BYTES), sb = sa + A_BYTES;
-                    const bool second = MODE == PROD_DZ_PAIR && it >= it1;
+                    const uint32_t sa = smem_addr(ring + stage * STAGE_BYTES), sb = sa + HALF;
+                    const bool second = MODE == PROD_DZ_TWO && it >= it1;
                     const uint32_t d = tmem + (uint32_t)(buf * BN) + (second ? (uint32_t)BN : 0u);
-                    const bool first = it == 0 || (MODE == PROD_DZ_PAIR && it == it1);
+                    const bool first = it == 0 || (MODE == PROD_DZ_TWO && it == it1);
 #pragma unroll
                     for (int kk = 0; kk < BK / 16; ++kk) {
                         const uint64_t da = A_MN ? mat_desc(sa + kk * 2048, BOX, 1024) : mat_desc(sa + kk * 32, 16, 1024);
                         const uint64_t db =
                             B_MN || second ? mat_desc(sb + kk * 2048, BOX, 1024) : mat_desc(sb + kk * 32, 16, 1024);
-                        mma(d, da, db, second ? idesc2 : idesc1, !(first && kk == 0));
+                        mma<PAIR>(d, da, db, second ? idesc2 : idesc1, !(first && kk == 0));
                     }
-                    mma_commit(&empty[stage]);
+                    mma_commit<PAIR>(&empty[stage]);
                     if (++stage == STAGES) {
                         stage = 0;
                         phase ^= 1u;
                     }
                 }
-                mma_commit(&acc_full[buf]);
+                mma_commit<PAIR>(&acc_full[buf]);
             }
             if (!ok) {  // instructions in flight read shared memory and write tensor memory
-                mma_commit(&drained);
+                mma_commit<PAIR>(&drained);
                 const long long t0 = clock64();
                 while (!bar_try(&drained, 0) && clock64() - t0 < WAIT_CYCLES) {}
             }
@@ -258,146 +313,214 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
         const int w = warp - 2, q = warp & 3, half = w >> 2;  // a warp may read the 32 lanes of its quarter only
         Stager s{staged + w * OUT_BYTES, lane, 0};
         int n_acc = 0;
-        for (int idx = blockIdx.x; idx < total; idx += gridDim.x, ++n_acc) {
-            const Tile t = tile_at<MODE>(p, idx, width);
+        for (int idx = first_tile; idx < total; idx += step, ++n_acc) {
+            const Tile t = tile_at<MODE, PAIR>(p, idx, width, rank);
             const int buf = BUFFERS == 2 ? n_acc & 1 : 0;
+            const uint32_t acc = tmem + (uint32_t)(buf * BN) + ((uint32_t)(32 * q) << 16);
+            const int row0 = t.row + 32 * q, row = row0 + lane;
+            const bool counts = row < t.live;
+            const float rw = p.row_weight && counts ? p.row_weight[row] : 1.f;
+            const uint16_t* bias = p.bias ? p.bias + (size_t)t.expert * p.bias_ld : nullptr;
+            const uint16_t* extra = p.extra ? p.extra + (size_t)row * p.ld_extra : nullptr;
+            const int each = width / 2;  // columns of this warp
+            const int batch = MODE == PROD_DW ? t.expert : 0;
             if (!bar_wait(&acc_full[buf], (uint32_t)(n_acc / BUFFERS) & 1u, gave_up)) break;
             __syncwarp();
             tc_fence_after();
-            const uint32_t acc = tmem + (uint32_t)(buf * BN) + ((uint32_t)(32 * q) << 16);
-            const int row0 = t.row + 32 * q, row = row0 + lane;
-            const bool inside = row < p.rows;
-            const bool counts = inside && (!p.row_slot || p.row_slot[row] >= 0);
-            const float rw = p.row_weight && inside ? p.row_weight[row] : 1.f;
-            const uint16_t* bias = p.bias ? p.bias + (size_t)t.expert * p.bias_ld : nullptr;
-
-            if (MODE == PROD_FWD || MODE == PROD_DX || MODE == PROD_DW) {
-                const int each = width / 2;  // columns of this warp
+            if (row0 < t.store) {
+                float dot = 0.f;
 #pragma unroll 1
                 for (int c = 0; c < each; c += 32) {
                     const int at = half * each + c, col = t.col + at;
-                    float v[32];
+                    Row32 add, b0, b1;
+                    if (MODE == PROD_FWD || MODE == PROD_DZ) add.fetch(extra, col, p.cols, extra && counts);
+                    if (MODE != PROD_DX && MODE != PROD_DW) {
+                        b0.fetch(bias, col, p.cols, bias != nullptr);
+                        b1.fetch(bias ? bias + p.gate_rows : bias, col, p.cols, bias && gated);
+                    }
+                    float v[32], u[32];
                     tmem_ld32(acc + at, v);
-                    if (MODE == PROD_FWD && gated) {
-                        float u[32];
-                        tmem_ld32(acc + BN / 2 + at, u);
-                        tmem_wait_ld();
-                        if (bias) {
-                            add_row(v, bias, col, p.cols, 1.f, p.bf16);
-                            add_row(u, bias + p.gate_rows, col, p.cols, 1.f, p.bf16);
-                        }
-#pragma unroll
-                        for (int j = 0; j < 32; ++j) v[j] = act_of(v[j], p.act) * u[j];
-                    } else {
+                    if (MODE == PROD_DX || MODE == PROD_DW) {
                         tmem_wait_ld();
                         if (MODE == PROD_DW && t.k == 0) {
 #pragma unroll
                             for (int j = 0; j < 32; ++j) v[j] = 0.f;  // an expert without a token: nothing was summed
                         }
-                        if (MODE == PROD_FWD) {
-                            if (bias) add_row(v, bias, col, p.cols, p.weigh == 2 ? rw : 1.f, p.bf16);
+                    } else if (MODE == PROD_FWD) {
+                        if (gated) {
+                            tmem_ld32(acc + BN / 2 + at, u);
+                            tmem_wait_ld();
+                            if (bias) {
+                                b0.add(v, 1.f, p.bf16);
+                                b1.add(u, 1.f, p.bf16);
+                            }
+                            with_act(p.act, [&](auto tag) {
 #pragma unroll
-                            for (int j = 0; j < 32; ++j) v[j] = act_of(v[j], p.act);
+                                for (int j = 0; j < 32; ++j) v[j] = act_of<decltype(tag)::value>(v[j]) * u[j];
+                            });
+                        } else {
+                            tmem_wait_ld();
+                            if (bias) b0.add(v, p.weigh == 2 ? rw : 1.f, p.bf16);
+                            if (p.act != SOM_ACT_NONE)
+                                with_act(p.act, [&](auto tag) {
+#pragma unroll
+                                    for (int j = 0; j < 32; ++j) v[j] = act_of<decltype(tag)::value>(v[j]);
+                                });
                         }
-                    }
-                    if (MODE == PROD_FWD) {
-                        if (p.extra && inside) add_row(v, p.extra + (size_t)row * p.ld_extra, col, p.cols, 1.f, p.bf16);
+                        if (extra) add.add(v, 1.f, p.bf16);
                         if (p.weigh == 1) {
 #pragma unroll
-                            for (int j = 0; j < 32; ++j) v[j] = counts ? v[j] * rw : 0.f;
+                            for (int j = 0; j < 32; ++j) v[j] *= rw;
+                        }
+                    } else {
+                        // PROD_DZ, PROD_DZ_TWO: v = z (or the gate's z) becomes dz, u = the gated half's
+                        float g[32];
+                        if (gated) tmem_ld32(acc + BN / 2 + at, u);
+                        if (MODE == PROD_DZ_TWO) tmem_ld32(acc + BN + at, g);
+                        tmem_wait_ld();
+                        if (bias) {
+                            b0.add(v, 1.f, p.bf16);
+                            if (gated) b1.add(u, 1.f, p.bf16);
+                        }
+                        if (MODE == PROD_DZ) {
+#pragma unroll
+                            for (int j = 0; j < 32; ++j) g[j] = 0.f;
+                            add.add(g, 1.f, p.bf16);
+                        }
+                        float hid[32];
+                        with_act(p.act, [&](auto tag) {
+#pragma unroll
+                            for (int j = 0; j < 32; ++j) {
+                                float a, da;
+                                act_both<decltype(tag)::value>(v[j], a, da);
+                                if (gated) {
+                                    hid[j] = a * u[j];
+                                    v[j] = u[j] * da;
+                                    u[j] = a;
+                                } else {
+                                    hid[j] = a;
+                                    v[j] = da;
+                                }
+                            }
+                        });
+                        if (MODE == PROD_DZ_TWO) {
+#pragma unroll
+                            for (int j = 0; j < 32; ++j) {
+                                if (col + j < p.cols) dot = fmaf(hid[j], g[j], dot);
+                                hid[j] = counts ? hid[j] * rw : 0.f;
+                                g[j] *= rw;
+                            }
+                        }
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) {
+                            v[j] = counts ? v[j] * g[j] : 0.f;
+                            if (gated) u[j] = counts ? u[j] * g[j] : 0.f;
+                        }
+                        if (MODE == PROD_DZ_TWO) s.put16(&p.o2, hid, col, row0, 0, p);
+                        if (gated) s.put16(&p.o1, u, col, row0, 0, p);
+                    }
+                    if (p.out32) s.put32(&p.o0, v, col, row0, batch, p);
+                    else s.put16(&p.o0, v, col, row0, batch, p);
+                    if ((MODE == PROD_DZ || MODE == PROD_DZ_TWO) && p.column_sums) {
+                        // (outputs were rounded; the sums are over the unrounded values)
+                        float* to = p.column_sums + (size_t)(row0 / 32) * (p.cols + p.gate_rows);
+                        const float sv = column_sum(v, lane);
+                        if (col + lane < p.cols) to[col + lane] = sv;
+                        if (gated) {
+                            const float su = column_sum(u, lane);
+                            if (col + lane < p.cols) to[p.gate_rows + col + lane] = su;
                         }
                     }
-                    if (p.out32) s.put32(&p.o0, v, col, row0, MODE == PROD_DW ? t.expert : 0, p);
-                    else s.put16(&p.o0, v, col, row0, MODE == PROD_DW ? t.expert : 0, p);
                 }
-            } else {
-                // PROD_DZ, PROD_DZ_PAIR.  dh = the gradient that reaches the activation's output.
-                const int each = width / 2;
-                float dot = 0.f;
-#pragma unroll 1
-                for (int c = 0; c < each; c += 32) {
-                    const int at = half * each + c, col = t.col + at;
-                    float v[32], u[32], g[32];
-                    tmem_ld32(acc + at, v);
-                    if (gated) tmem_ld32(acc + BN / 2 + at, u);
-                    if (MODE == PROD_DZ_PAIR) tmem_ld32(acc + BN + at, g);
-                    tmem_wait_ld();
-                    if (bias) {
-                        add_row(v, bias, col, p.cols, 1.f, p.bf16);
-                        if (gated) add_row(u, bias + p.gate_rows, col, p.cols, 1.f, p.bf16);
-                    }
-                    if (MODE == PROD_DZ) {
-#pragma unroll
-                        for (int j = 0; j < 32; ++j) g[j] = 0.f;
-                        if (inside) add_row(g, p.extra + (size_t)row * p.ld_extra, col, p.cols, 1.f, p.bf16);
-                    }
-                    // v: z (or the gate) -> dz of it; u: the gated half -> dz of it; hidden values on the way
-                    float hid[32];
-#pragma unroll
-                    for (int j = 0; j < 32; ++j) {
-                        float a, da;
-                        act_both(v[j], p.act, a, da);
-                        const float other = gated ? u[j] : 1.f;
-                        const float hj = a * other;
-                        if (MODE == PROD_DZ_PAIR) {
-                            if (col + j < p.cols) dot = fmaf(hj, g[j], dot);
-                            hid[j] = counts ? hj * rw : 0.f;
-                            g[j] = counts ? g[j] * rw : 0.f;
-                        }
-                        v[j] = counts ? g[j] * other * da : 0.f;
-                        if (gated) u[j] = counts ? g[j] * a : 0.f;
-                    }
-                    s.put16(&p.o0, v, col, row0, 0, p);
-                    if (gated) s.put16(&p.o1, u, col, row0, 0, p);
-                    if (MODE == PROD_DZ_PAIR) s.put16(&p.o2, hid, col, row0, 0, p);
-                }
-                if (MODE == PROD_DZ_PAIR && inside)
-                    p.dot[(size_t)row * (2 * p.col_tiles) + 2 * (t.col / width) + half] = dot;
+                if (MODE == PROD_DZ_TWO && counts) p.dot[(size_t)row * (2 * p.col_tiles) + 2 * (t.col / width) + half] = dot;
             }
             tc_fence_before();
             __syncwarp();
-            if (lane == 0) bar_arrive(&acc_empty[buf]);
+            if (lane == 0) {
+                if (PAIR) bar_arrive_remote(cluster_addr(smem_addr(&acc_empty[buf]), 0));
+                else bar_arrive(&acc_empty[buf]);
+            }
         }
         if (lane == 0) store_wait_all();
     }
     __syncthreads();
     if (threadIdx.x == 0 && gave_up_sh) atomicOr(p.flags, LAY_FLAG_GAVE_UP);
+    __syncwarp();
+    if (PAIR) cluster_sync();  // no block leaves while the other may still reach its memory
     if (warp == 1) {
-        __syncwarp();
         tc_fence_after();
-        tmem_free(tmem, 512);
+        tmem_free<PAIR>(tmem, TMEM_COLUMNS);
     }
 }
 
-template <int MODE>
-int launch_mode(som_layers* l, const ProdArgs& args, cudaStream_t st)
+template <int MODE, bool PAIR>
+cudaError_t launch_mode(som_layers* l, const ProdArgs& args, cudaStream_t st)
 {
-    cudaError_t e = cudaFuncSetAttribute(k_product<MODE>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM);
-    if (e == cudaSuccess) {
-        int64_t most = (int64_t)args.row_tiles * args.col_tiles * (MODE == PROD_DW ? args.experts : 1);
-        const int grid = (int)(most < l->sm_count ? most : l->sm_count);
-        k_product<MODE><<<grid, THREADS, SMEM, st>>>(args);
-        ++l->launches;
-        e = cudaGetLastError();
-    }
-    if (e != cudaSuccess) {
-        l->last_cuda_error = (int)e;
-        return SOM_ERR_CUDA;
-    }
-    return SOM_OK;
+    const int64_t tiles = (int64_t)args.row_tiles * args.col_tiles * (MODE == PROD_DW ? args.experts : 1);
+    const int most = PAIR ? l->pairs : l->sm_count;
+    cudaLaunchConfig_t c = {};
+    c.gridDim = dim3((unsigned)(tiles < most ? tiles : most) * (PAIR ? 2 : 1));
+    c.blockDim = dim3(THREADS);
+    c.dynamicSmemBytes = SMEM;
+    c.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = 2;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    c.attrs = attr;
+    c.numAttrs = PAIR ? 1 : 0;
+    return cudaLaunchKernelEx(&c, k_product<MODE, PAIR>, args);
+}
+
+template <int MODE>
+cudaError_t prepare_mode(int* pairs)
+{
+    cudaError_t e = cudaFuncSetAttribute(k_product<MODE, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(k_product<MODE, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM);
+    if (e != cudaSuccess) return e;
+    cudaLaunchConfig_t c = {};
+    c.gridDim = dim3(2);
+    c.blockDim = dim3(THREADS);
+    c.dynamicSmemBytes = SMEM;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = 2;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    c.attrs = attr;
+    c.numAttrs = 1;
+    int n = 0;
+    e = cudaOccupancyMaxActiveClusters(&n, k_product<MODE, true>, &c);
+    if (n < *pairs) *pairs = n;
+    return e;
 }
 
 }  // namespace
 
-int launch_product(som_layers* l, ProdMode mode, const ProdArgs& args, cudaStream_t st)
+cudaError_t prepare_product(som_layers* l)
 {
+    l->pairs = l->sm_count / 2;
+    cudaError_t e = prepare_mode<PROD_FWD>(&l->pairs);
+    if (e == cudaSuccess) e = prepare_mode<PROD_DZ>(&l->pairs);
+    if (e == cudaSuccess) e = prepare_mode<PROD_DZ_TWO>(&l->pairs);
+    if (e == cudaSuccess) e = prepare_mode<PROD_DX>(&l->pairs);
+    if (e == cudaSuccess) e = prepare_mode<PROD_DW>(&l->pairs);
+    return l->pairs > 0 ? e : cudaErrorNotSupported;
+}
+
+int launch_product(som_layers* l, ProdMode mode, const ProdArgs& a, cudaStream_t st)
+{
+    cudaError_t e;
     switch (mode) {
-        case PROD_FWD: return launch_mode<PROD_FWD>(l, args, st);
-        case PROD_DZ: return launch_mode<PROD_DZ>(l, args, st);
-        case PROD_DZ_PAIR: return launch_mode<PROD_DZ_PAIR>(l, args, st);
-        case PROD_DX: return launch_mode<PROD_DX>(l, args, st);
-        default: return launch_mode<PROD_DW>(l, args, st);
+        case PROD_FWD: e = a.pair ? launch_mode<PROD_FWD, true>(l, a, st) : launch_mode<PROD_FWD, false>(l, a, st); break;
+        case PROD_DZ: e = a.pair ? launch_mode<PROD_DZ, true>(l, a, st) : launch_mode<PROD_DZ, false>(l, a, st); break;
+        case PROD_DZ_TWO: e = a.pair ? launch_mode<PROD_DZ_TWO, true>(l, a, st) : launch_mode<PROD_DZ_TWO, false>(l, a, st); break;
+        case PROD_DX: e = a.pair ? launch_mode<PROD_DX, true>(l, a, st) : launch_mode<PROD_DX, false>(l, a, st); break;
+        default: e = a.pair ? launch_mode<PROD_DW, true>(l, a, st) : launch_mode<PROD_DW, false>(l, a, st); break;
     }
+    ++l->launches;
+    if (e == cudaSuccess) return SOM_OK;
+    l->last_cuda_error = (int)e;
+    return SOM_ERR_CUDA;
 }
 
 }  // namespace lay

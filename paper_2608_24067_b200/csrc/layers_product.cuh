@@ -6,27 +6,32 @@
 namespace lay {
 
 enum ProdMode {
-    PROD_FWD = 0,      // out[row, n] = epilogue(sum_k A[row, k] B[n, k])
-    PROD_DZ = 1,       // the same product, epilogue multiplies dy by the activation's derivative
-    PROD_DZ_PAIR = 2,  // two products over the same rows: z = x W1^T and g = dy W2; epilogue of the experts' gradient
-    PROD_DX = 3,       // out[row, n] = sum_k A[row, k] B[k, n]
-    PROD_DW = 4        // out[e][m, n] = sum_rows A[row, m] B[row, n] over the rows of expert e
+    PROD_FWD = 0,     // out[row, n] = epilogue(sum_k A[row, k] B[n, k])
+    PROD_DZ = 1,      // the same product, epilogue multiplies dy by the activation's derivative
+    PROD_DZ_TWO = 2,  // two products over the same rows: z = x W1^T and g = dy W2; epilogue of the experts' gradient
+    PROD_DX = 3,      // out[row, n] = sum_k A[row, k] B[k, n]
+    PROD_DW = 4       // out[e][m, n] = sum_rows A[row, m] B[row, n] over the rows of expert e
 };
 
+// Output tiles: `pair` = 256 x 256 by two blocks of a cluster, else 128 x 128 by one block.
+constexpr int PAIR_ROWS = 256, PAIR_COLS = 256, SINGLE_ROWS = 128, SINGLE_COLS = 128;
+
 struct ProdArgs {
-    CUtensorMap a, b;        // operands (of the first product)
-    CUtensorMap a2, b2;      // second product of PROD_DZ_PAIR
-    CUtensorMap o0, o1, o2;  // outputs
-    const int* tiles;        // grouped rows: number of row tiles on the device; nullptr = row_tiles
-    const int* tile_expert;  // grouped rows: expert of a row tile; nullptr = 0
-    const int* seg;          // PROD_DW: rows [seg[e], seg[e + 1]) of expert e; nullptr = [0, k1)
-    const uint16_t* bias;    // [experts][bias_ld] or nullptr
-    const uint16_t* extra;   // residual (PROD_FWD) or dy (PROD_DZ), [rows][ld_extra], or nullptr
-    const float* row_weight; // [rows] or nullptr
-    const int* row_slot;     // [rows] -1 = padding; nullptr = every row counts
-    float* dot;              // PROD_DZ_PAIR: [rows][2 * col_tiles] partial sums of h * g
+    CUtensorMap a, b;         // operands (of the first product)
+    CUtensorMap a2, b2;       // second product of PROD_DZ_TWO
+    CUtensorMap o0, o1, o2;   // outputs
+    const int* tiles;         // grouped rows: number of row tiles on the device; nullptr = row_tiles
+    const int* tile_expert;   // grouped rows: expert of a row tile; nullptr = 0
+    const int* seg;           // grouped rows: first row of every expert
+    const int* count;         // and its rows in use; nullptr = one group of `rows` rows (PROD_DW: k1)
+    const uint16_t* bias;     // [experts][bias_ld] or nullptr
+    const uint16_t* extra;    // residual (PROD_FWD) or dy (PROD_DZ), [rows][ld_extra], or nullptr
+    const float* row_weight;  // [rows] or nullptr
+    float* dot;               // PROD_DZ_TWO: [rows][2 * col_tiles] partial sums of h * g
+    float* column_sums;       // PROD_DZ, PROD_DZ_TWO: [rows / 32][2 cols or cols] sums of dz over 32 rows, or nullptr
     int64_t ld_extra;
     int bias_ld;
+    int pair;
     int row_tiles, col_tiles, experts;
     int rows, cols;  // extent of the outputs (PROD_DW: of one expert's)
     int gate_rows;   // gated: rows of B between a feature's gate row and its other row; 0 = not gated

@@ -1,9 +1,15 @@
-// som_route and som_route_backward: one warp a token, the row's logits in registers (lane l holds experts l, l + 32, ...).
+// som_route and som_route_backward: one warp a token, the row's logits in registers.  Lane l holds the V experts from l * V,
+// so that a lane's order and the lanes' order are the experts' order and a tie goes to the lowest lane.
 //
-// The choice is k rounds of a warp-wide maximum of (key, lowest index): the keys as order-preserving 32-bit integers, so
-// that a round is two integer warp reductions.  Scores that the choice goes by are computed in fp64 and rounded to fp32
-// (an expert's rank then does not depend on the last bits of one exponential); where the logits order the experts
-// themselves only the chosen experts' scores are computed, in fp32.
+// The choice is k rounds of a warp-wide maximum over the keys as order-preserving 32-bit integers: one integer warp
+// reduction, one ballot, one shuffle a round; the lane that gave the maximum looks for its next one.
+//
+// Where the choice goes by scores (not by the logits themselves), it is that of the scores rounded from 64 bits, so that it
+// does not hang on the last bits of one exponential.  Computing every score in fp64 took 61 us for 16384 tokens of 256
+// experts, four fifths of it fp64 arithmetic.  So the scores are first computed in fp32, off by less than 2^-19, and the
+// rounds also look at the gaps between consecutive choices (the first one not taken among them) and between the last group
+// kept and the first one dropped: a gap beyond twice the errors cannot change sign.  Only a token with a smaller gap, about
+// one in a hundred, goes through the fp64 scores.
 #include "layers_math.cuh"
 #include "layers_slots.cuh"
 
@@ -42,6 +48,10 @@ __device__ __forceinline__ double warp_sum(double v)
 // exp(x - top), with the limit 1 where both are infinite
 __device__ __forceinline__ float exp_from(float x, float top) { return x == top ? 1.f : expf(x - top); }
 
+// the rare path's arithmetic, out of line: unrolled into the kernel it would take the registers of the common path
+__device__ __noinline__ double exp64(float x, float top) { return x == top ? 1.0 : exp((double)x - (double)top); }
+__device__ __noinline__ float sigmoid64(float x) { return (float)(1.0 / (1.0 + exp(-(double)x))); }
+
 struct RouteArgs {
     const void* logits;
     int64_t ld, T;
@@ -53,112 +63,202 @@ struct RouteArgs {
     float scale;
 };
 
+// The V logits from `at` on (-inf beyond the row's end); `whole`: rows and their pieces lie on the vector loads' grid.
+template <int TYPE, int V>
+__device__ __forceinline__ void load_row(const void* p, int64_t row, int at, int E, bool whole, float (&x)[V])
+{
+    constexpr int SIZE = TYPE == SOM_F32 ? 4 : 2, WORDS = V * SIZE / 4;
+    if (WORDS >= 1 && whole && at + V <= E) {
+        uint32_t w[WORDS ? WORDS : 1];
+        const char* q = static_cast<const char*>(p) + (row + at) * SIZE;
+        if (WORDS >= 4) {
+#pragma unroll
+            for (int i = 0; i < WORDS / 4; ++i) {
+                const uint4 u = __ldg(reinterpret_cast<const uint4*>(q) + i);
+                w[4 * i] = u.x, w[4 * i + 1] = u.y, w[4 * i + 2] = u.z, w[4 * i + 3] = u.w;
+            }
+        } else if (WORDS == 2) {
+            const uint2 u = __ldg(reinterpret_cast<const uint2*>(q));
+            w[0] = u.x, w[WORDS > 1 ? 1 : 0] = u.y;
+        } else {
+            w[0] = __ldg(reinterpret_cast<const uint32_t*>(q));
+        }
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            if (SIZE == 4) {
+                x[v] = __uint_as_float(w[v]);
+            } else {
+                const float2 f = unpack2(w[v / 2], TYPE == SOM_BF16);
+                x[v] = v & 1 ? f.y : f.x;
+            }
+        }
+    } else {
+#pragma unroll
+        for (int v = 0; v < V; ++v) x[v] = at + v < E ? logit_at<TYPE>(p, row + at + v) : -INFINITY;
+    }
+}
+
+// whether load_row may use vector loads on this matrix
+template <int TYPE, int V>
+__device__ __forceinline__ bool whole_rows(const void* p, int64_t ld)
+{
+    constexpr int SIZE = TYPE == SOM_F32 ? 4 : 2, BYTES = V * SIZE < 16 ? V * SIZE : 16;
+    return (reinterpret_cast<uintptr_t>(p) % BYTES) == 0 && (ld * SIZE) % BYTES == 0;
+}
+
+// the two largest keys of (m1 >= m2) and (o1 >= o2)
+__device__ __forceinline__ void merge2(uint32_t& m1, uint32_t& m2, uint32_t o1, uint32_t o2)
+{
+    m2 = max(min(m1, o1), max(m2, o2));
+    m1 = max(m1, o1);
+}
+
+__device__ __forceinline__ uint32_t group_key(uint32_t b1, uint32_t b2, int best)
+{
+    if (best == 1 || b2 == 0) return b1;
+    const float s = from_ordered(b1) + from_ordered(b2);
+    return s == s ? som_ordered_bits(s + 0.f) : 0u;
+}
+
+// Whether two keys from fp32 scores may be ordered otherwise by the exact ones; `errors`: scores in each of them.
+__device__ __forceinline__ bool too_near(uint32_t above, uint32_t below, int errors)
+{
+    if (above == 0 || below == 0) return false;  // nothing left below: no order to mistake
+    const float f = from_ordered(above), g = from_ordered(below);
+    return !(f - g > errors * 0x1p-18f * (1.f + fabsf(f)));
+}
+
 template <int TYPE, int V>
 __global__ void __launch_bounds__(32 * ROUTE_WARPS) k_route(const RouteArgs a)
 {
     extern __shared__ int hist[];  // [E] when counts are wanted
-    const int lane = threadIdx.x & 31;
+    const int lane = threadIdx.x & 31, first = lane * V;
     if (a.counts) {
         for (int i = threadIdx.x; i < a.E; i += 32 * ROUTE_WARPS) hist[i] = 0;
         __syncthreads();
     }
+    const bool whole = whole_rows<TYPE, V>(a.logits, a.ld);
+    const bool by_groups = a.groups > 1 && a.top_groups < a.groups;
     const bool by_score = a.bias || (a.groups > 1 && a.group_best == 2);
+    const int size = a.E / a.groups;
+    const int lanes = size % V == 0 ? size / V : 0;  // lanes of a group, where no lane spans two
+    const int my_group = lanes ? lane / lanes : 0, my_place = lanes ? lane - my_group * lanes : 0;
+    float bias[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) bias[v] = a.bias && first + v < a.E ? __ldg(a.bias + first + v) : 0.f;
+
     for (int64_t t = (int64_t)blockIdx.x * ROUTE_WARPS + (threadIdx.x >> 5); t < a.T; t += (int64_t)gridDim.x * ROUTE_WARPS) {
         const int64_t row = t * a.ld;
         float x[V];
-        uint32_t key[V];  // 0 = masked out or taken
+        load_row<TYPE, V>(a.logits, row, first, a.E, whole, x);
         uint32_t top_u = 0;
 #pragma unroll
-        for (int v = 0; v < V; ++v) {
-            const int i = v * 32 + lane;
-            x[v] = i < a.E ? logit_at<TYPE>(a.logits, row + i) : -INFINITY;
-            const bool live = x[v] > -INFINITY;  // (false for NaN)
-            key[v] = live ? som_ordered_bits(x[v] + 0.f) : 0u;  // + 0: the two zeros tie
-            top_u = max(top_u, key[v]);
-        }
+        for (int v = 0; v < V; ++v) top_u = max(top_u, x[v] > -INFINITY ? som_ordered_bits(x[v]) : 0u);  // (a NaN is not)
         top_u = __reduce_max_sync(ALL, top_u);
         const float top = top_u ? from_ordered(top_u) : 0.f;
         float total = 1.f;  // softmax: sum of exp(x - top)
-        if (by_score) {
-            double e[V], sum = 0.0;
-            if (a.score == SOM_SCORE_SOFTMAX) {
-#pragma unroll
-                for (int v = 0; v < V; ++v) {
-                    e[v] = key[v] ? (x[v] == top ? 1.0 : exp((double)x[v] - (double)top)) : 0.0;
-                    sum += e[v];
-                }
-                sum = warp_sum(sum);
-                total = (float)sum;
-            }
-#pragma unroll
-            for (int v = 0; v < V; ++v) {
-                if (!key[v]) continue;
-                float s = a.score == SOM_SCORE_SOFTMAX ? (float)(e[v] / sum) : (float)(1.0 / (1.0 + exp(-(double)x[v])));
-                if (a.bias) s += __ldg(a.bias + v * 32 + lane);
-                key[v] = s == s ? som_ordered_bits(s + 0.f) : 0u;
-            }
-        } else if (a.score == SOM_SCORE_SOFTMAX && !a.renorm) {
+        if (a.score == SOM_SCORE_SOFTMAX && (by_score || !a.renorm)) {
             float sum = 0.f;
 #pragma unroll
-            for (int v = 0; v < V; ++v) sum += key[v] ? exp_from(x[v], top) : 0.f;
+            for (int v = 0; v < V; ++v) sum += x[v] > -INFINITY ? exp_from(x[v], top) : 0.f;
             total = warp_sum(sum);
         }
-        if (a.groups > 1 && a.top_groups < a.groups) {
-            const int size = a.E / a.groups;
-            uint32_t mine = 0;  // lane g: key of group g
-            for (int g = 0; g < a.groups; ++g) {
-                uint32_t m1 = 0, m2 = 0;
+        int at;  // lane j: the j-th choice
+#pragma unroll 1
+        for (int exact = 0;; exact = 1) {
+            uint32_t key[V];  // 0 = masked out or taken
+            if (!by_score) {
+#pragma unroll
+                for (int v = 0; v < V; ++v) key[v] = x[v] > -INFINITY ? som_ordered_bits(x[v] + 0.f) : 0u;  // + 0: the two zeros tie
+            } else {
+                double sum = 1.0;
+                if (exact && a.score == SOM_SCORE_SOFTMAX) {
+                    sum = 0.0;
+#pragma unroll
+                    for (int v = 0; v < V; ++v) sum += x[v] > -INFINITY ? exp64(x[v], top) : 0.0;
+                    sum = warp_sum(sum);
+                }
 #pragma unroll
                 for (int v = 0; v < V; ++v) {
-                    const int i = v * 32 + lane - g * size;
-                    if (i >= 0 && i < size) {
-                        m2 = max(m2, min(m1, key[v]));
-                        m1 = max(m1, key[v]);
-                    }
+                    float s;
+                    if (a.score == SOM_SCORE_SOFTMAX) s = exact ? (float)(exp64(x[v], top) / sum) : __fdividef(exp_from(x[v], top), total);
+                    else s = exact ? sigmoid64(x[v]) : __fdividef(1.f, 1.f + __expf(-x[v]));
+                    s += bias[v];
+                    key[v] = x[v] > -INFINITY && s == s ? som_ordered_bits(s + 0.f) : 0u;
                 }
-                const uint32_t b1 = __reduce_max_sync(ALL, m1);
-                uint32_t gk = b1;
-                if (a.group_best == 2 && b1) {
-                    const int owner = __ffs(__ballot_sync(ALL, m1 == b1)) - 1;
-                    const uint32_t b2 = __reduce_max_sync(ALL, lane == owner ? m2 : m1);
-                    if (b2) {
-                        const float s = from_ordered(b1) + from_ordered(b2);
-                        gk = s == s ? som_ordered_bits(s + 0.f) : 0u;
-                    }
-                }
-                if (lane == g) mine = gk;
             }
-            int rank = 0;
-            for (int g = 0; g < a.groups; ++g) {
-                const uint32_t other = __shfl_sync(ALL, mine, g);
-                rank += other > mine || (other == mine && g < lane);
-            }
-            const unsigned kept = __ballot_sync(ALL, lane < a.groups && rank < a.top_groups);
+            bool unsure = false;
+            if (by_groups) {
+                uint32_t mine = 0;  // lane g: key of group g
+                if (lanes) {
+                    uint32_t m1 = 0, m2 = 0;
 #pragma unroll
-            for (int v = 0; v < V; ++v) {
-                const int i = v * 32 + lane;
-                if (i < a.E && !((kept >> (i / size)) & 1u)) key[v] = 0u;
+                    for (int v = 0; v < V; ++v) merge2(m1, m2, key[v], 0u);
+                    for (int d = 1; d < lanes; d <<= 1) {
+                        const uint32_t o1 = __shfl_down_sync(ALL, m1, d), o2 = __shfl_down_sync(ALL, m2, d);
+                        if (my_place + d < lanes) merge2(m1, m2, o1, o2);
+                    }
+                    m1 = group_key(m1, m2, a.group_best);
+                    mine = __shfl_sync(ALL, m1, lane * lanes & 31);
+                    if (lane >= a.groups) mine = 0;
+                } else {
+                    for (int g = 0; g < a.groups; ++g) {
+                        uint32_t m1 = 0, m2 = 0;
+#pragma unroll
+                        for (int v = 0; v < V; ++v) {
+                            const int i = first + v - g * size;
+                            if (i >= 0 && i < size) merge2(m1, m2, key[v], 0u);
+                        }
+                        const uint32_t b1 = __reduce_max_sync(ALL, m1);
+                        const int owner = __ffs(__ballot_sync(ALL, m1 == b1)) - 1;
+                        const uint32_t b2 = __reduce_max_sync(ALL, lane == owner ? m2 : m1);
+                        if (lane == g) mine = group_key(b1, b2, a.group_best);
+                    }
+                }
+                int rank = 0;
+                for (int g = 0; g < a.groups; ++g) {
+                    const uint32_t other = __shfl_sync(ALL, mine, g);
+                    rank += other > mine || (other == mine && g < lane);
+                }
+                const bool keep = lane < a.groups && rank < a.top_groups;
+                const unsigned kept = __ballot_sync(ALL, keep);
+                if (by_score && !exact) {
+                    const uint32_t low = __reduce_min_sync(ALL, keep ? mine : 0xffffffffu);
+                    const uint32_t next = __reduce_max_sync(ALL, !keep && lane < a.groups ? mine : 0u);
+                    unsure = too_near(low, next, 2);
+                }
+#pragma unroll
+                for (int v = 0; v < V; ++v) {
+                    const int g = lanes ? my_group : min((first + v) / size, 31);
+                    if (!((kept >> g) & 1u)) key[v] = 0u;
+                }
             }
-        }
-        int at = -1;  // lane j: the j-th choice
-        for (int j = 0; j < a.k; ++j) {
-            uint32_t best = 0;
-            int bi = 0x7fffffff;
+            at = -1;
+            uint32_t best = 0, last = 0;
+            int bv = 0;
 #pragma unroll
             for (int v = 0; v < V; ++v)
-                if (key[v] > best) {
-                    best = key[v];
-                    bi = v * 32 + lane;
-                }
-            const uint32_t m = __reduce_max_sync(ALL, best);
-            if (m == 0) break;
-            const int i = (int)__reduce_min_sync(ALL, (unsigned)(best == m ? bi : 0x7fffffff));
-            if (lane == j) at = i;
-            if ((i & 31) == lane) {
+                if (key[v] > best) best = key[v], bv = v;
+            const int rounds = by_score && !exact && a.k < a.E ? a.k + 1 : a.k;  // (the first one not taken is looked at)
+            for (int j = 0; j < rounds && !unsure; ++j) {
+                const uint32_t m = __reduce_max_sync(ALL, best);
+                if (m == 0) break;
+                if (by_score && !exact && j > 0 && too_near(last, m, 1)) unsure = true;
+                last = m;
+                const int owner = __ffs(__ballot_sync(ALL, best == m)) - 1;
+                const int i = owner * V + __shfl_sync(ALL, bv, owner);
+                if (lane == j && j < a.k) at = i;
+                if (lane == owner) {
+                    const int gone = bv;
+                    best = 0;
 #pragma unroll
-                for (int v = 0; v < V; ++v)
-                    if (v == (i >> 5)) key[v] = 0u;
+                    for (int v = 0; v < V; ++v) {
+                        if (v == gone) key[v] = 0u;
+                        if (key[v] > best) best = key[v], bv = v;
+                    }
+                }
             }
+            if (!unsure) break;
         }
         float s = 0.f;
         const float xj = at >= 0 ? logit_at<TYPE>(a.logits, row + at) : -INFINITY;

@@ -62,10 +62,6 @@ __global__ void __launch_bounds__(PLAN_THREADS) k_slot_plan(SlotPlan p, const in
         p.seg[e] = before * p.tile;
         p.count[e] = count;
         for (int i = 0; i < tiles; ++i) p.tile_expert[before + i] = e;
-        for (int r = before * p.tile + count; r < (before + tiles) * p.tile; ++r) {
-            p.row_slot[r] = -1;
-            p.row_weight[r] = 0.f;
-        }
         if (e == E - 1) {
             p.seg[E] = (before + tiles) * p.tile;
             *p.tiles = before + tiles;
@@ -94,20 +90,32 @@ __global__ void __launch_bounds__(PLAN_THREADS) k_slot_plan(SlotPlan p, const in
     }
 }
 
-// rows of x (blockIdx.y == 0) and of dy (1) in the slots' order; zeros in padding rows
-__global__ void __launch_bounds__(256) k_gather(SlotPlan p, int E, int k, int D, const uint16_t* x, int64_t ldx, uint16_t* xp,
+// Rows of x (blockIdx.z == 0) and of dy (1) in the slots' order, up to whole steps of 64 rows of an expert with zeros (the
+// sums over an expert's rows run in such steps).  A warp a row.
+__global__ void __launch_bounds__(256) k_gather(SlotPlan p, int k, int D, const uint16_t* x, int64_t ldx, uint16_t* xp,
                                                 const uint16_t* dy, int64_t lddy, uint16_t* dyp)
 {
-    const int rows = p.seg[E], chunks = D / 8;
-    const uint16_t* from = blockIdx.y ? dy : x;
-    const int64_t ld = blockIdx.y ? lddy : ldx;
-    uint16_t* to = blockIdx.y ? dyp : xp;
-    for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < (int64_t)rows * chunks; i += (int64_t)gridDim.x * blockDim.x) {
-        const int row = (int)(i / chunks), c = (int)(i % chunks);
-        const int slot = p.row_slot[row];
-        uint4 v = make_uint4(0u, 0u, 0u, 0u);
-        if (slot >= 0) v = __ldg(reinterpret_cast<const uint4*>(from + (size_t)(slot / k) * ld) + c);
-        *(reinterpret_cast<uint4*>(to + (size_t)row * D) + c) = v;
+    const int lane = threadIdx.x & 31, chunks = D / 8, rows = *p.tiles * p.tile;
+    const uint16_t* from = blockIdx.z ? dy : x;
+    const int64_t ld = blockIdx.z ? lddy : ldx;
+    uint16_t* to = blockIdx.z ? dyp : xp;
+    for (int row = blockIdx.x * 8 + (threadIdx.x >> 5); row < rows; row += gridDim.x * 8) {
+        const int e = p.tile_expert[row / p.tile], place = row - p.seg[e], n = p.count[e];
+        uint4* out = reinterpret_cast<uint4*>(to + (size_t)row * D);
+        if (place < n) {
+            const uint4* in = reinterpret_cast<const uint4*>(from + (size_t)(p.row_slot[row] / k) * ld);
+            int c = lane;
+            for (; c + 96 < chunks; c += 128) {
+                const uint4 u0 = __ldg(in + c), u1 = __ldg(in + c + 32), u2 = __ldg(in + c + 64), u3 = __ldg(in + c + 96);
+                out[c] = u0;
+                out[c + 32] = u1;
+                out[c + 64] = u2;
+                out[c + 96] = u3;
+            }
+            for (; c < chunks; c += 32) out[c] = __ldg(in + c);
+        } else if (place < ((n + 63) & ~63)) {
+            for (int c = lane; c < chunks; c += 32) out[c] = make_uint4(0u, 0u, 0u, 0u);
+        }
     }
 }
 
@@ -177,18 +185,17 @@ __global__ void __launch_bounds__(256) k_dweights(const int* pos, const int32_t*
 
 // out[e][c] = sum over the rows of expert e of weight[row] * v[row][c]; a block sums 64 columns of one expert, 32 rows at
 // a time, in a fixed order
-__global__ void __launch_bounds__(256) k_column_sums(const int* seg, int64_t rows, const uint16_t* v, int64_t ld, const float* weight,
-                                                     int cols, uint16_t* out, int bf16)
+__global__ void __launch_bounds__(256) k_column_sums(SlotPlan p, int64_t rows, const uint16_t* v, int64_t ld, int cols, uint16_t* out, int bf16)
 {
     __shared__ float part[32][65];
     const int e = blockIdx.y, c = blockIdx.x * 64 + (threadIdx.x & 7) * 8, r = threadIdx.x >> 3;
-    const int64_t lo = seg ? seg[e] : 0, hi = seg ? seg[e + 1] : rows;
+    const int64_t lo = p.seg ? p.seg[e] : 0, hi = p.seg ? lo + p.count[e] : rows;
     float a[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
     if (c < cols)
         for (int64_t i = lo + r; i < hi; i += 32) {
             float u[8];
             load8(v + (size_t)i * ld + c, u, bf16);
-            const float w = weight ? weight[i] : 1.f;
+            const float w = p.seg ? p.row_weight[i] : 1.f;
 #pragma unroll
             for (int j = 0; j < 8; ++j) a[j] = fmaf(w, u[j], a[j]);
         }
@@ -199,6 +206,24 @@ __global__ void __launch_bounds__(256) k_column_sums(const int* seg, int64_t row
         float s = 0.f;
         for (int i = 0; i < 32; ++i) s += part[i][threadIdx.x];
         out[(size_t)e * cols + blockIdx.x * 64 + threadIdx.x] = (uint16_t)pack2(s, 0.f, bf16);
+    }
+}
+
+// out[e][c] = sum of part[g][c] over the expert's groups of 32 rows (of 32-row sums); 32 columns a block, 8 groups at a time
+__global__ void __launch_bounds__(256) k_join_sums(SlotPlan p, int64_t rows, const float* part, int cols, uint16_t* out, int bf16)
+{
+    __shared__ float sums[8][33];
+    const int e = blockIdx.y, c = blockIdx.x * 32 + (threadIdx.x & 31), r = threadIdx.x >> 5;
+    const int64_t lo = p.seg ? p.seg[e] / 32 : 0, hi = p.seg ? lo + (p.count[e] + 31) / 32 : (rows + 31) / 32;
+    float a = 0.f;
+    if (c < cols)
+        for (int64_t i = lo + r; i < hi; i += 8) a += part[(size_t)i * cols + c];
+    sums[r][threadIdx.x & 31] = a;
+    __syncthreads();
+    if (r == 0 && c < cols) {
+#pragma unroll
+        for (int i = 1; i < 8; ++i) a += sums[i][threadIdx.x & 31];
+        out[(size_t)e * cols + c] = (uint16_t)pack2(a, 0.f, bf16);
     }
 }
 
@@ -233,11 +258,11 @@ int launch_plan(som_layers* l, const SlotPlan& p, const int32_t* indices, const 
     return done(l);
 }
 
-int launch_gather(som_layers* l, const SlotPlan& p, int E, int k, int64_t D, const void* x, int64_t ldx, void* xp, const void* dy,
+int launch_gather(som_layers* l, const SlotPlan& p, int k, int64_t D, const void* x, int64_t ldx, void* xp, const void* dy,
                   int64_t lddy, void* dyp, cudaStream_t st)
 {
-    const dim3 grid(grid_for(l, (int64_t)p.max_rows * (D / 8), 256 * 4), dy ? 2 : 1);
-    k_gather<<<grid, 256, 0, st>>>(p, E, k, (int)D, static_cast<const uint16_t*>(x), ldx, static_cast<uint16_t*>(xp),
+    const dim3 grid(grid_for(l, p.max_rows, 8), 1, dy ? 2 : 1);
+    k_gather<<<grid, 256, 0, st>>>(p, k, (int)D, static_cast<const uint16_t*>(x), ldx, static_cast<uint16_t*>(xp),
                                    static_cast<const uint16_t*>(dy), lddy, static_cast<uint16_t*>(dyp));
     return done(l);
 }
@@ -258,11 +283,18 @@ int launch_dweights(som_layers* l, const SlotPlan& p, const int32_t* indices, in
     return done(l);
 }
 
-int launch_column_sums(som_layers* l, const int* seg, int E, int64_t rows, const void* v, int64_t ld, const float* weight, int64_t cols,
-                       void* out, int bf16, cudaStream_t st)
+int launch_column_sums(som_layers* l, const SlotPlan& p, int E, int64_t rows, const void* v, int64_t ld, int64_t cols, void* out,
+                       int bf16, cudaStream_t st)
 {
     const dim3 grid((unsigned)((cols + 63) / 64), (unsigned)E);
-    k_column_sums<<<grid, 256, 0, st>>>(seg, rows, static_cast<const uint16_t*>(v), ld, weight, (int)cols, static_cast<uint16_t*>(out), bf16);
+    k_column_sums<<<grid, 256, 0, st>>>(p, rows, static_cast<const uint16_t*>(v), ld, (int)cols, static_cast<uint16_t*>(out), bf16);
+    return done(l);
+}
+
+int launch_join_sums(som_layers* l, const SlotPlan& p, int E, int64_t rows, const float* part, int64_t cols, void* out, int bf16, cudaStream_t st)
+{
+    const dim3 grid((unsigned)((cols + 31) / 32), (unsigned)E);
+    k_join_sums<<<grid, 256, 0, st>>>(p, rows, part, (int)cols, static_cast<uint16_t*>(out), bf16);
     return done(l);
 }
 

@@ -12,6 +12,9 @@ import torch
 
 from .som import SOM_OK, SomError, load_library
 
+# the current stream's address without building a Stream object (2 us a call)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
 _TYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
 _ACTS = {"none": 0, "relu": 1, "gelu": 2, "silu": 3}
 _SCORES = {"softmax": 0, "sigmoid": 1}
@@ -66,10 +69,11 @@ class Layers:
             raise SomError(rc, where, self._lib.som_layers_last_cuda_error(self._h))
 
     def _stream(self, stream) -> int:
-        return (torch.cuda.current_stream(self.device) if stream is None else stream).cuda_stream
-
-    def _empty(self, shape, dtype):
-        return torch.empty(shape, dtype=dtype, device=self.device)
+        if stream is not None:
+            return stream.cuda_stream
+        if _raw_stream is not None:
+            return _raw_stream(self.device.index)
+        return torch.cuda.current_stream(self.device).cuda_stream
 
     def _half(self, x, name="x"):
         if not isinstance(x, torch.Tensor) or x.dtype not in (torch.float16, torch.bfloat16) or x.dim() != 2:
@@ -91,7 +95,7 @@ class Layers:
         F = rows // 2 if gated else rows
         xp, ldx = _matrix(x, (T, D), x.dtype, "x")
         if out is None:
-            out = self._empty((T, F), x.dtype)
+            out = x.new_empty((T, F))
         yp, ldy = _matrix(out, (T, F), x.dtype, "out")
         rp, ldr = (0, 0) if residual is None else _matrix(residual, (T, F), x.dtype, "residual")
         rc = self._lib.som_linear(self._h, kind, _code(_ACTS, act, "act"), int(gated), T, D, F, xp, ldx,
@@ -113,9 +117,9 @@ class Layers:
         xp, ldx = _matrix(x, (T, D), x.dtype, "x")
         gp, ldg = _matrix(dy, (T, F), x.dtype, "dy")
         wp = _whole(weight, (rows, D), x.dtype, "weight")
-        out = {"dx": self._empty((T, D), x.dtype), "dweight": self._empty((rows, D), x.dtype)}
+        out = {"dx": x.new_empty((T, D)), "dweight": x.new_empty((rows, D))}
         if bias is not None:
-            out["dbias"] = self._empty((rows,), x.dtype)
+            out["dbias"] = x.new_empty((rows,))
         rc = self._lib.som_linear_backward(self._h, kind, _code(_ACTS, act, "act"), int(gated), T, D, F, xp, ldx, wp,
                                            _whole(bias, (rows,), x.dtype, "bias"), gp, ldg, out["dx"].data_ptr(),
                                            out["dweight"].data_ptr(), out["dbias"].data_ptr() if bias is not None else 0,
@@ -131,8 +135,8 @@ class Layers:
         T, E = logits.shape
         lp, ld = _matrix(logits, (T, E), logits.dtype, "logits")
         kind = _code(_TYPES, logits.dtype, "logits' type")
-        out = {"weights": self._empty((T, k), torch.float32), "indices": self._empty((T, k), torch.int32),
-               "counts": self._empty((E,), torch.int32)}
+        out = {"weights": logits.new_empty((T, k), dtype=torch.float32), "indices": logits.new_empty((T, k), dtype=torch.int32),
+               "counts": logits.new_empty((E,), dtype=torch.int32)}
         rc = self._lib.som_route(self._h, kind, _code(_SCORES, score, "score"), T, E, k, lp, ld,
                                  _whole(bias, (E,), torch.float32, "bias"), groups, top_groups, group_best, int(renorm), scale,
                                  out["weights"].data_ptr(), out["indices"].data_ptr(), out["counts"].data_ptr(),
@@ -148,7 +152,7 @@ class Layers:
         lp, ld = _matrix(logits, (T, E), logits.dtype, "logits")
         kind = _code(_TYPES, logits.dtype, "logits' type")
         k = indices.shape[-1]
-        out = self._empty((T, E), logits.dtype)
+        out = logits.new_empty((T, E))
         rc = self._lib.som_route_backward(self._h, kind, _code(_SCORES, score, "score"), T, E, k, lp, ld,
                                           _whole(indices, (T, k), torch.int32, "indices"),
                                           _whole(dweights, (T, k), torch.float32, "dweights"), int(renorm), scale,
@@ -178,7 +182,7 @@ class Layers:
         """som_experts: residual + sum over a token's experts of weight * (w2 act(w1 x + b1) + b2).  Returns [T, D]."""
         kind, T, E, k, D, I, rows, p = self._experts(x, indices, weights, w1, w2, b1, b2, gated)
         if out is None:
-            out = self._empty((T, D), x.dtype)
+            out = x.new_empty((T, D))
         yp, ldy = _matrix(out, (T, D), x.dtype, "out")
         rp, ldr = (0, 0) if residual is None else _matrix(residual, (T, D), x.dtype, "residual")
         rc = self._lib.som_experts(self._h, kind, _code(_ACTS, act, "act"), int(gated), T, E, k, D, I, *p, rp, ldr, yp, ldy,
@@ -190,12 +194,12 @@ class Layers:
         """som_experts_backward: {"dx", "dweights", "dw1", "dw2"} and, with biases, "db1", "db2"."""
         kind, T, E, k, D, I, rows, p = self._experts(x, indices, weights, w1, w2, b1, b2, gated)
         gp, ldg = _matrix(dy, (T, D), x.dtype, "dy")
-        out = {"dx": self._empty((T, D), x.dtype), "dweights": self._empty((T, k), weights.dtype),
-               "dw1": self._empty((E, rows, D), x.dtype), "dw2": self._empty((E, D, I), x.dtype)}
+        out = {"dx": x.new_empty((T, D)), "dweights": weights.new_empty((T, k)),
+               "dw1": x.new_empty((E, rows, D)), "dw2": x.new_empty((E, D, I))}
         if b1 is not None:
-            out["db1"] = self._empty((E, rows), x.dtype)
+            out["db1"] = x.new_empty((E, rows))
         if b2 is not None:
-            out["db2"] = self._empty((E, D), x.dtype)
+            out["db2"] = x.new_empty((E, D))
         at = lambda n: out[n].data_ptr() if n in out else 0  # noqa: E731
         rc = self._lib.som_experts_backward(self._h, kind, _code(_ACTS, act, "act"), int(gated), T, E, k, D, I, *p, gp, ldg,
                                             at("dx"), at("dweights"), at("dw1"), at("db1"), at("dw2"), at("db2"),
