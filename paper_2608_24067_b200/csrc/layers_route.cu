@@ -1,15 +1,16 @@
 // som_route and som_route_backward: one warp a token, the row's logits in registers.  Lane l holds the V experts from l * V,
-// so that a lane's order and the lanes' order are the experts' order and a tie goes to the lowest lane.
+// so that a lane's order and the lanes' order are the experts' order.
 //
-// The choice is k rounds of a warp-wide maximum over the keys as order-preserving 32-bit integers: one integer warp
-// reduction, one ballot, one shuffle a round; the lane that gave the maximum looks for its next one.
-//
-// Where the choice goes by scores (not by the logits themselves), it is that of the scores rounded from 64 bits, so that it
-// does not hang on the last bits of one exponential.  Computing every score in fp64 took 61 us for 16384 tokens of 256
-// experts, four fifths of it fp64 arithmetic.  So the scores are first computed in fp32, off by less than 2^-19, and the
-// rounds also look at the gaps between consecutive choices (the first one not taken among them) and between the last group
-// kept and the first one dropped: a gap beyond twice the errors cannot change sign.  Only a token with a smaller gap, about
-// one in a hundred, goes through the fp64 scores.
+// The choice takes k rounds of a warp-wide maximum.  What bounds it is instructions, not bytes (16384 tokens x 256 experts
+// are 17 MB, 2.6 us), so a round has to be short.  A key and its expert are packed into 32 bits, 22 of key and 10 of index,
+// so that one integer reduction finds the winner with ties to the lowest index; each lane's keys are sorted beforehand
+// (minima and maxima only), so that the winner's lane just moves up its list.  16-bit logits fit such a key exactly.  Others
+// become fixed-point distances from an upper bound, and scores come from fast fp32 exponentials; so the gaps between
+// consecutive choices (the first one not taken among them) and between the last group kept and the first dropped are
+// compared with the errors of both keys.  Only a token with a smaller gap, one in fifty or fewer, is done again from exact
+// keys: logits as order-preserving integers, scores in fp64 rounded to fp32, so that the choice does not hang on the last bits
+// of one exponential.  16384 tokens x 256 experts with bias and groups: 61 us with every score in fp64, 46 us with fp32 scores
+// and unsorted exact keys.
 #include "layers_math.cuh"
 #include "layers_slots.cuh"
 
@@ -48,9 +49,7 @@ __device__ __forceinline__ double warp_sum(double v)
 // exp(x - top), with the limit 1 where both are infinite
 __device__ __forceinline__ float exp_from(float x, float top) { return x == top ? 1.f : expf(x - top); }
 
-// the rare path's arithmetic, out of line: unrolled into the kernel it would take the registers of the common path
-__device__ __noinline__ double exp64(float x, float top) { return x == top ? 1.0 : exp((double)x - (double)top); }
-__device__ __noinline__ float sigmoid64(float x) { return (float)(1.0 / (1.0 + exp(-(double)x))); }
+__device__ __forceinline__ double exp64(float x, float top) { return x == top ? 1.0 : exp((double)x - (double)top); }
 
 struct RouteArgs {
     const void* logits;
@@ -120,12 +119,99 @@ __device__ __forceinline__ uint32_t group_key(uint32_t b1, uint32_t b2, int best
     return s == s ? som_ordered_bits(s + 0.f) : 0u;
 }
 
-// Whether two keys from fp32 scores may be ordered otherwise by the exact ones; `errors`: scores in each of them.
-__device__ __forceinline__ bool too_near(uint32_t above, uint32_t below, int errors)
+// The choice from exact keys: lane j returns the j-th.
+template <int V>
+__device__ __noinline__ int choose_exact(const RouteArgs& a, const float (&x)[V], const float (&bias)[V], float top, bool by_score,
+                                         bool by_groups, int lane)
 {
-    if (above == 0 || below == 0) return false;  // nothing left below: no order to mistake
-    const float f = from_ordered(above), g = from_ordered(below);
-    return !(f - g > errors * 0x1p-18f * (1.f + fabsf(f)));
+    const int first = lane * V, size = a.E / a.groups;
+    uint32_t key[V];  // 0 = masked out or taken
+    double sum = 1.0;
+    if (by_score && a.score == SOM_SCORE_SOFTMAX) {
+        sum = 0.0;
+        for (int v = 0; v < V; ++v) sum += x[v] > -INFINITY ? exp64(x[v], top) : 0.0;
+        sum = warp_sum(sum);
+    }
+    for (int v = 0; v < V; ++v) {
+        float s = x[v];
+        if (by_score) s = (a.score == SOM_SCORE_SOFTMAX ? (float)(exp64(x[v], top) / sum) : (float)(1.0 / (1.0 + exp(-(double)x[v])))) + bias[v];
+        key[v] = x[v] > -INFINITY && s == s ? som_ordered_bits(s + 0.f) : 0u;  // + 0: the two zeros tie
+    }
+    if (by_groups) {
+        uint32_t mine = 0;  // lane g: key of group g
+        for (int g = 0; g < a.groups; ++g) {
+            uint32_t m1 = 0, m2 = 0;
+            for (int v = 0; v < V; ++v) {
+                const int i = first + v - g * size;
+                if (i >= 0 && i < size) merge2(m1, m2, key[v], 0u);
+            }
+            const uint32_t b1 = __reduce_max_sync(ALL, m1);
+            const int owner = __ffs(__ballot_sync(ALL, m1 == b1)) - 1;
+            const uint32_t b2 = __reduce_max_sync(ALL, lane == owner ? m2 : m1);
+            if (lane == g) mine = group_key(b1, b2, a.group_best);
+        }
+        int rank = 0;
+        for (int g = 0; g < a.groups; ++g) {
+            const uint32_t other = __shfl_sync(ALL, mine, g);
+            rank += other > mine || (other == mine && g < lane);
+        }
+        const unsigned kept = __ballot_sync(ALL, lane < a.groups && rank < a.top_groups);
+        for (int v = 0; v < V; ++v)
+            if (!((kept >> min((first + v) / size, 31)) & 1u)) key[v] = 0u;
+    }
+    int at = -1;
+    for (int j = 0; j < a.k; ++j) {
+        uint32_t best = 0;
+        int bv = 0;
+        for (int v = 0; v < V; ++v)
+            if (key[v] > best) best = key[v], bv = v;
+        const uint32_t m = __reduce_max_sync(ALL, best);
+        if (m == 0) break;
+        const int owner = __ffs(__ballot_sync(ALL, best == m)) - 1;  // the lowest lane holds the lowest index
+        const int i = owner * V + __shfl_sync(ALL, bv, owner);
+        if (lane == j) at = i;
+        if (lane == owner) key[bv] = 0u;
+    }
+    return at;
+}
+
+constexpr int KEY_BITS = 22, INDEX_BITS = 10;
+constexpr uint32_t KEY_MOST = (1u << KEY_BITS) - 1u, INDEX_MASK = (1u << INDEX_BITS) - 1u;
+
+__device__ __forceinline__ void order2(uint32_t& a, uint32_t& b)
+{
+    const uint32_t hi = max(a, b), lo = min(a, b);
+    a = hi;
+    b = lo;
+}
+
+// descending: Batcher's odd-even merge sort, unrolled
+template <int V>
+__device__ __forceinline__ void sort_down(uint32_t (&k)[V])
+{
+#pragma unroll
+    for (int p = 1; p < V; p <<= 1)
+#pragma unroll
+        for (int q = p; q >= 1; q >>= 1)
+#pragma unroll
+            for (int j = q % p; j + q < V; j += 2 * q)
+#pragma unroll
+                for (int i = 0; i < q; ++i)
+                    if (i + j + q < V && (i + j) / (2 * p) == (i + j + q) / (2 * p)) order2(k[i + j], k[i + j + q]);
+}
+
+// 16-bit logits (exact as floats) as order-preserving 16-bit integers
+template <int TYPE>
+__device__ __forceinline__ uint32_t ordered16(float x)
+{
+    uint32_t u;
+    if (TYPE == SOM_BF16) {
+        u = __float_as_uint(x) >> 16;
+    } else {
+        const __half h = __float2half_rn(x);
+        u = *reinterpret_cast<const uint16_t*>(&h);
+    }
+    return u & 0x8000u ? ~u & 0xffffu : u | 0x8000u;
 }
 
 template <int TYPE, int V>
@@ -140,22 +226,42 @@ __global__ void __launch_bounds__(32 * ROUTE_WARPS) k_route(const RouteArgs a)
     const bool whole = whole_rows<TYPE, V>(a.logits, a.ld);
     const bool by_groups = a.groups > 1 && a.top_groups < a.groups;
     const bool by_score = a.bias || (a.groups > 1 && a.group_best == 2);
+    const bool exact16 = TYPE != SOM_F32 && !by_score;
     const int size = a.E / a.groups;
     const int lanes = size % V == 0 ? size / V : 0;  // lanes of a group, where no lane spans two
     const int my_group = lanes ? lane / lanes : 0, my_place = lanes ? lane - my_group * lanes : 0;
     float bias[V];
+    float high = 0.f, low = 0.f;  // of the biases, with 0 among them
 #pragma unroll
-    for (int v = 0; v < V; ++v) bias[v] = a.bias && first + v < a.E ? __ldg(a.bias + first + v) : 0.f;
+    for (int v = 0; v < V; ++v) {
+        bias[v] = a.bias && first + v < a.E ? __ldg(a.bias + first + v) : 0.f;
+        high = fmaxf(high, bias[v]);
+        low = fminf(low, bias[v]);
+    }
+    // packed keys: scores lie in [low, 1 + high]; logits up to 64 below the row's largest are told apart
+    float ceiling = 0.f, scale = (float)KEY_MOST / 64.f;
+    uint32_t margin = 3;  // key units: rounding of the distances (and the scores' errors, 2^-18 for two of them)
+    if (by_score) {
+#pragma unroll
+        for (int d = 16; d > 0; d >>= 1) {
+            high = fmaxf(high, __shfl_xor_sync(ALL, high, d));
+            low = fminf(low, __shfl_xor_sync(ALL, low, d));
+        }
+        ceiling = 1.f + high;
+        scale = (float)KEY_MOST / (ceiling - low);
+        margin = 3 + (uint32_t)(scale * 0x1p-18f * (1.f + fmaxf(ceiling, -low)));
+    }
+    const bool packs = (!by_groups || lanes) && a.k < 32 && scale > 16.f;  // (not with huge or infinite biases)
 
     for (int64_t t = (int64_t)blockIdx.x * ROUTE_WARPS + (threadIdx.x >> 5); t < a.T; t += (int64_t)gridDim.x * ROUTE_WARPS) {
         const int64_t row = t * a.ld;
         float x[V];
         load_row<TYPE, V>(a.logits, row, first, a.E, whole, x);
-        uint32_t top_u = 0;
+        float top = -INFINITY;
 #pragma unroll
-        for (int v = 0; v < V; ++v) top_u = max(top_u, x[v] > -INFINITY ? som_ordered_bits(x[v]) : 0u);  // (a NaN is not)
-        top_u = __reduce_max_sync(ALL, top_u);
-        const float top = top_u ? from_ordered(top_u) : 0.f;
+        for (int v = 0; v < V; ++v) top = fmaxf(top, x[v]);  // (a NaN is left out)
+        const uint32_t top_u = __reduce_max_sync(ALL, top > -INFINITY ? som_ordered_bits(top) : 0u);
+        top = top_u ? from_ordered(top_u) : 0.f;
         float total = 1.f;  // softmax: sum of exp(x - top)
         if (a.score == SOM_SCORE_SOFTMAX && (by_score || !a.renorm)) {
             float sum = 0.f;
@@ -163,103 +269,91 @@ __global__ void __launch_bounds__(32 * ROUTE_WARPS) k_route(const RouteArgs a)
             for (int v = 0; v < V; ++v) sum += x[v] > -INFINITY ? exp_from(x[v], top) : 0.f;
             total = warp_sum(sum);
         }
-        int at;  // lane j: the j-th choice
-#pragma unroll 1
-        for (int exact = 0;; exact = 1) {
+        int at = -1;  // lane j: the j-th choice
+        bool sure = packs && top < INFINITY;
+        if (sure) {
             uint32_t key[V];  // 0 = masked out or taken
-            if (!by_score) {
+            if (exact16) {
 #pragma unroll
-                for (int v = 0; v < V; ++v) key[v] = x[v] > -INFINITY ? som_ordered_bits(x[v] + 0.f) : 0u;  // + 0: the two zeros tie
+                for (int v = 0; v < V; ++v)
+                    key[v] = x[v] > -INFINITY ? ordered16<TYPE>(x[v] + 0.f) << 16 | (INDEX_MASK - first - v) : 0u;  // + 0: the two zeros tie
             } else {
-                double sum = 1.0;
-                if (exact && a.score == SOM_SCORE_SOFTMAX) {
-                    sum = 0.0;
-#pragma unroll
-                    for (int v = 0; v < V; ++v) sum += x[v] > -INFINITY ? exp64(x[v], top) : 0.0;
-                    sum = warp_sum(sum);
-                }
 #pragma unroll
                 for (int v = 0; v < V; ++v) {
-                    float s;
-                    if (a.score == SOM_SCORE_SOFTMAX) s = exact ? (float)(exp64(x[v], top) / sum) : __fdividef(exp_from(x[v], top), total);
-                    else s = exact ? sigmoid64(x[v]) : __fdividef(1.f, 1.f + __expf(-x[v]));
-                    s += bias[v];
-                    key[v] = x[v] > -INFINITY && s == s ? som_ordered_bits(s + 0.f) : 0u;
+                    float d;  // distance from the upper bound
+                    if (!by_score) d = top - x[v];
+                    else if (a.score == SOM_SCORE_SOFTMAX) d = ceiling - (__fdividef(exp_from(x[v], top), total) + bias[v]);
+                    else d = ceiling - (__fdividef(1.f, 1.f + __expf(-x[v])) + bias[v]);
+                    const uint32_t u = KEY_MOST - min((uint32_t)(d * scale), KEY_MOST - 1u);
+                    key[v] = x[v] > -INFINITY && d == d ? u << INDEX_BITS | (INDEX_MASK - first - v) : 0u;
                 }
             }
-            bool unsure = false;
             if (by_groups) {
-                uint32_t mine = 0;  // lane g: key of group g
-                if (lanes) {
-                    uint32_t m1 = 0, m2 = 0;
-#pragma unroll
-                    for (int v = 0; v < V; ++v) merge2(m1, m2, key[v], 0u);
-                    for (int d = 1; d < lanes; d <<= 1) {
-                        const uint32_t o1 = __shfl_down_sync(ALL, m1, d), o2 = __shfl_down_sync(ALL, m2, d);
-                        if (my_place + d < lanes) merge2(m1, m2, o1, o2);
-                    }
-                    m1 = group_key(m1, m2, a.group_best);
-                    mine = __shfl_sync(ALL, m1, lane * lanes & 31);
-                    if (lane >= a.groups) mine = 0;
-                } else {
-                    for (int g = 0; g < a.groups; ++g) {
-                        uint32_t m1 = 0, m2 = 0;
-#pragma unroll
-                        for (int v = 0; v < V; ++v) {
-                            const int i = first + v - g * size;
-                            if (i >= 0 && i < size) merge2(m1, m2, key[v], 0u);
-                        }
-                        const uint32_t b1 = __reduce_max_sync(ALL, m1);
-                        const int owner = __ffs(__ballot_sync(ALL, m1 == b1)) - 1;
-                        const uint32_t b2 = __reduce_max_sync(ALL, lane == owner ? m2 : m1);
-                        if (lane == g) mine = group_key(b1, b2, a.group_best);
-                    }
-                }
-                int rank = 0;
-                for (int g = 0; g < a.groups; ++g) {
-                    const uint32_t other = __shfl_sync(ALL, mine, g);
-                    rank += other > mine || (other == mine && g < lane);
-                }
-                const bool keep = lane < a.groups && rank < a.top_groups;
-                const unsigned kept = __ballot_sync(ALL, keep);
-                if (by_score && !exact) {
-                    const uint32_t low = __reduce_min_sync(ALL, keep ? mine : 0xffffffffu);
-                    const uint32_t next = __reduce_max_sync(ALL, !keep && lane < a.groups ? mine : 0u);
-                    unsure = too_near(low, next, 2);
-                }
+                uint32_t m1 = 0, m2 = 0;
 #pragma unroll
                 for (int v = 0; v < V; ++v) {
-                    const int g = lanes ? my_group : min((first + v) / size, 31);
-                    if (!((kept >> g) & 1u)) key[v] = 0u;
+                    m2 = max(m2, min(m1, key[v]));
+                    m1 = max(m1, key[v]);
+                }
+                for (int d = 1; d < lanes; d <<= 1) {
+                    const uint32_t o1 = __shfl_down_sync(ALL, m1, d), o2 = __shfl_down_sync(ALL, m2, d);
+                    if (my_place + d < lanes) merge2(m1, m2, o1, o2);
+                }
+                // a lone expert's distance is not comparable with the sum of two
+                if (a.group_best == 2 && __any_sync(ALL, my_place == 0 && m1 && !m2)) sure = false;
+                const uint32_t gk = a.group_best == 2 ? (m1 >> INDEX_BITS) + (m2 >> INDEX_BITS) : m1;
+                uint32_t mine = __shfl_sync(ALL, gk, lane * lanes & 31);  // lane g: group g
+                if (lane >= a.groups) mine = 0;
+                unsigned kept = 0;
+                uint32_t last = 0;
+                for (int r = 0; r < a.top_groups; ++r) {
+                    last = __reduce_max_sync(ALL, mine);
+                    if (last == 0) break;
+                    const int g = __ffs(__ballot_sync(ALL, mine == last)) - 1;
+                    kept |= 1u << g;
+                    if (lane == g) mine = 0;
+                }
+                const uint32_t next = last ? __reduce_max_sync(ALL, mine) : 0u;
+                if (!exact16 && next) {
+                    if (a.group_best == 2) sure = sure && last - next >= 2 * margin;
+                    else sure = sure && (last >> INDEX_BITS) - (next >> INDEX_BITS) >= margin;
+                }
+                if (!((kept >> my_group) & 1u)) {
+#pragma unroll
+                    for (int v = 0; v < V; ++v) key[v] = 0u;
                 }
             }
-            at = -1;
-            uint32_t best = 0, last = 0;
-            int bv = 0;
+            if (sure) {
+                sort_down<V>(key);
+                uint32_t won = 0;
+                const int rounds = exact16 ? a.k : a.k + 1;  // (the first one not taken is looked at)
+                for (int j = 0; j < rounds; ++j) {
+                    const uint32_t m = __reduce_max_sync(ALL, key[0]);
+                    if (m == 0) break;
+                    if (lane == j) won = m;
+                    if (key[0] == m) {
 #pragma unroll
-            for (int v = 0; v < V; ++v)
-                if (key[v] > best) best = key[v], bv = v;
-            const int rounds = by_score && !exact && a.k < a.E ? a.k + 1 : a.k;  // (the first one not taken is looked at)
-            for (int j = 0; j < rounds && !unsure; ++j) {
-                const uint32_t m = __reduce_max_sync(ALL, best);
-                if (m == 0) break;
-                if (by_score && !exact && j > 0 && too_near(last, m, 1)) unsure = true;
-                last = m;
-                const int owner = __ffs(__ballot_sync(ALL, best == m)) - 1;
-                const int i = owner * V + __shfl_sync(ALL, bv, owner);
-                if (lane == j && j < a.k) at = i;
-                if (lane == owner) {
-                    const int gone = bv;
-                    best = 0;
-#pragma unroll
-                    for (int v = 0; v < V; ++v) {
-                        if (v == gone) key[v] = 0u;
-                        if (key[v] > best) best = key[v], bv = v;
+                        for (int v = 0; v + 1 < V; ++v) key[v] = key[v + 1];
+                        key[V - 1] = 0u;
                     }
                 }
+                at = won ? (int)(INDEX_MASK - (won & INDEX_MASK)) : -1;
+                if (!exact16) {
+                    const float mx = at >= 0 ? logit_at<TYPE>(a.logits, row + at) + 0.f : 0.f;
+                    const float mb = at >= 0 && a.bias ? __ldg(a.bias + at) : 0.f;
+                    const uint32_t above = __shfl_up_sync(ALL, won, 1);
+                    const float ax = __shfl_up_sync(ALL, mx, 1), ab = __shfl_up_sync(ALL, mb, 1);
+                    // Equal logits and biases tie exactly, and the index decided.  (Not between the last one taken and the
+                    // first one left: what comes after that one has not been looked at.)
+                    bool near = won && lane > 0 && (above >> INDEX_BITS) - (won >> INDEX_BITS) < margin &&
+                                !(lane < a.k && ax == mx && ab == mb);
+                    near |= won && lane < a.k && (won >> INDEX_BITS) <= 1u;  // beyond the keys' range
+                    if (__any_sync(ALL, near)) sure = false;
+                }
+                if (lane >= a.k) at = -1;
             }
-            if (!unsure) break;
         }
+        if (!sure) at = choose_exact<V>(a, x, bias, top, by_score, by_groups, lane);
         float s = 0.f;
         const float xj = at >= 0 ? logit_at<TYPE>(a.logits, row + at) : -INFINITY;
         if (a.score == SOM_SCORE_SIGMOID) {
