@@ -119,28 +119,38 @@ __device__ __forceinline__ uint32_t group_key(uint32_t b1, uint32_t b2, int best
     return s == s ? som_ordered_bits(s + 0.f) : 0u;
 }
 
-// The choice from exact keys: lane j returns the j-th.
-template <int V>
-__device__ __noinline__ int choose_exact(const RouteArgs& a, const float (&x)[V], const float (&bias)[V], float top, bool by_score,
-                                         bool by_groups, int lane)
+// The choice from exact keys: lane j returns the j-th.  Reads the row again: the common path's registers stay its own.
+template <int TYPE, int V>
+__device__ __noinline__ int choose_exact(const RouteArgs& a, int64_t row, float top, bool by_score, bool by_groups, int lane)
 {
-    const int first = lane * V, size = a.E / a.groups;
+    const int first = lane * V;
     uint32_t key[V];  // 0 = masked out or taken
     double sum = 1.0;
     if (by_score && a.score == SOM_SCORE_SOFTMAX) {
         sum = 0.0;
-        for (int v = 0; v < V; ++v) sum += x[v] > -INFINITY ? exp64(x[v], top) : 0.0;
+#pragma unroll 4
+        for (int v = 0; v < V; ++v) {
+            const float x = first + v < a.E ? logit_at<TYPE>(a.logits, row + first + v) : -INFINITY;
+            sum += x > -INFINITY ? exp64(x, top) : 0.0;
+        }
         sum = warp_sum(sum);
     }
+#pragma unroll
     for (int v = 0; v < V; ++v) {
-        float s = x[v];
-        if (by_score) s = (a.score == SOM_SCORE_SOFTMAX ? (float)(exp64(x[v], top) / sum) : (float)(1.0 / (1.0 + exp(-(double)x[v])))) + bias[v];
-        key[v] = x[v] > -INFINITY && s == s ? som_ordered_bits(s + 0.f) : 0u;  // + 0: the two zeros tie
+        const float x = first + v < a.E ? logit_at<TYPE>(a.logits, row + first + v) : -INFINITY;
+        float s = x;
+        if (by_score) {
+            s = a.score == SOM_SCORE_SOFTMAX ? (float)(exp64(x, top) / sum) : (float)(1.0 / (1.0 + exp(-(double)x)));
+            if (a.bias && first + v < a.E) s += __ldg(a.bias + first + v);
+        }
+        key[v] = x > -INFINITY && s == s ? som_ordered_bits(s + 0.f) : 0u;  // + 0: the two zeros tie
     }
     if (by_groups) {
+        const int size = a.E / a.groups;
         uint32_t mine = 0;  // lane g: key of group g
         for (int g = 0; g < a.groups; ++g) {
             uint32_t m1 = 0, m2 = 0;
+#pragma unroll
             for (int v = 0; v < V; ++v) {
                 const int i = first + v - g * size;
                 if (i >= 0 && i < size) merge2(m1, m2, key[v], 0u);
@@ -156,6 +166,7 @@ __device__ __noinline__ int choose_exact(const RouteArgs& a, const float (&x)[V]
             rank += other > mine || (other == mine && g < lane);
         }
         const unsigned kept = __ballot_sync(ALL, lane < a.groups && rank < a.top_groups);
+#pragma unroll
         for (int v = 0; v < V; ++v)
             if (!((kept >> min((first + v) / size, 31)) & 1u)) key[v] = 0u;
     }
@@ -163,6 +174,7 @@ __device__ __noinline__ int choose_exact(const RouteArgs& a, const float (&x)[V]
     for (int j = 0; j < a.k; ++j) {
         uint32_t best = 0;
         int bv = 0;
+#pragma unroll
         for (int v = 0; v < V; ++v)
             if (key[v] > best) best = key[v], bv = v;
         const uint32_t m = __reduce_max_sync(ALL, best);
@@ -170,7 +182,11 @@ __device__ __noinline__ int choose_exact(const RouteArgs& a, const float (&x)[V]
         const int owner = __ffs(__ballot_sync(ALL, best == m)) - 1;  // the lowest lane holds the lowest index
         const int i = owner * V + __shfl_sync(ALL, bv, owner);
         if (lane == j) at = i;
-        if (lane == owner) key[bv] = 0u;
+        if (lane == owner) {
+#pragma unroll
+            for (int v = 0; v < V; ++v)
+                if (v == bv) key[v] = 0u;
+        }
     }
     return at;
 }
@@ -215,7 +231,7 @@ __device__ __forceinline__ uint32_t ordered16(float x)
 }
 
 template <int TYPE, int V>
-__global__ void __launch_bounds__(32 * ROUTE_WARPS) k_route(const RouteArgs a)
+__global__ void __launch_bounds__(32 * ROUTE_WARPS, V <= 8 ? 4 : 2) k_route(const RouteArgs a)
 {
     extern __shared__ int hist[];  // [E] when counts are wanted
     const int lane = threadIdx.x & 31, first = lane * V;
@@ -227,9 +243,13 @@ __global__ void __launch_bounds__(32 * ROUTE_WARPS) k_route(const RouteArgs a)
     const bool by_groups = a.groups > 1 && a.top_groups < a.groups;
     const bool by_score = a.bias || (a.groups > 1 && a.group_best == 2);
     const bool exact16 = TYPE != SOM_F32 && !by_score;
-    const int size = a.E / a.groups;
-    const int lanes = size % V == 0 ? size / V : 0;  // lanes of a group, where no lane spans two
-    const int my_group = lanes ? lane / lanes : 0, my_place = lanes ? lane - my_group * lanes : 0;
+    int lanes = 0, my_group = 0, my_place = 0;  // lanes of a group, where no lane spans two
+    if (by_groups) {
+        const int size = a.E / a.groups;
+        lanes = size % V == 0 ? size / V : 0;
+        my_group = lanes ? lane / lanes : 0;
+        my_place = lane - my_group * lanes;
+    }
     float bias[V];
     float high = 0.f, low = 0.f;  // of the biases, with 0 among them
 #pragma unroll
@@ -353,7 +373,7 @@ __global__ void __launch_bounds__(32 * ROUTE_WARPS) k_route(const RouteArgs a)
                 if (lane >= a.k) at = -1;
             }
         }
-        if (!sure) at = choose_exact<V>(a, x, bias, top, by_score, by_groups, lane);
+        if (!sure) at = choose_exact<TYPE, V>(a, row, top, by_score, by_groups, lane);
         float s = 0.f;
         const float xj = at >= 0 ? logit_at<TYPE>(a.logits, row + at) : -INFINITY;
         if (a.score == SOM_SCORE_SIGMOID) {
@@ -532,9 +552,10 @@ struct RouteGrad {
     }
 };
 
-int route_grid(const som_layers* l, int64_t T)
+// What a warp sets up (biases, groups, the block's counts) is shared by its tokens: no more blocks than are resident.
+int route_grid(const som_layers* l, int64_t T, int per_sm)
 {
-    const int64_t want = (T + ROUTE_WARPS - 1) / ROUTE_WARPS, most = (int64_t)l->sm_count * 8;
+    const int64_t want = (T + ROUTE_WARPS - 1) / ROUTE_WARPS, most = (int64_t)l->sm_count * per_sm;
     return (int)(want < most ? want : most);
 }
 
@@ -544,7 +565,7 @@ int launch_route(som_layers* l, int type, int score, int64_t T, int E, int k, co
                  int groups, int top_groups, int group_best, int renorm, float scale, float* weights, int32_t* indices,
                  int32_t* counts, cudaStream_t st)
 {
-    const int grid = T > 0 ? route_grid(l, T) : 0;
+    const int grid = T > 0 ? route_grid(l, T, E <= 256 ? 4 : 2) : 0;
     cudaError_t e = cudaSuccess;
     if (counts && grid != 1) e = cudaMemsetAsync(counts, 0, (size_t)E * sizeof(int32_t), st);  // one block writes its counts itself
     if (e == cudaSuccess && grid) {
@@ -560,7 +581,7 @@ int launch_route_backward(som_layers* l, int type, int score, int64_t T, int E, 
 {
     if (T == 0) return SOM_OK;
     const RouteGradArgs a{logits, ld, T, indices, dweights, dlogits, E, k, score, renorm, scale, l->flags};
-    const cudaError_t e = by_type<RouteGrad>(type, E, a, route_grid(l, T), 0, st);
+    const cudaError_t e = by_type<RouteGrad>(type, E, a, route_grid(l, T, 8), 0, st);
     ++l->launches;
     return done(l, e);
 }
