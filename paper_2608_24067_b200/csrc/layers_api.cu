@@ -1,6 +1,7 @@
 // Host side of the dense operators declared in include/som.h: handle, argument checks, workspace, tensor maps, launches.
 #include <new>
 
+#include "layers_few.cuh"
 #include "layers_product.cuh"
 #include "layers_slots.cuh"
 
@@ -158,6 +159,8 @@ int som_layers_create(som_layers** out)
     cudaError_t e = cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &l->encode, cudaEnableDefault, &found);
     if (e == cudaSuccess && (found != cudaDriverEntryPointSuccess || !l->encode)) e = cudaErrorNotSupported;
     if (e == cudaSuccess) e = prepare_product(l);
+    if (e == cudaSuccess) e = prepare_few();
+    if (e == cudaSuccess) e = prepare_plan();
     if (e == cudaSuccess) e = cudaMalloc(reinterpret_cast<void**>(&l->flags), 256);
     if (e == cudaSuccess) e = cudaMemset(l->flags, 0, 256);
     if (e != cudaSuccess) {
@@ -208,6 +211,24 @@ int som_linear(som_layers* l, int type, int act, int gated, int64_t T, int64_t D
     Guard g(l->device);
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
     const int64_t rows = gated ? 2 * F : F;
+    if (T <= FEW_ROWS && T * D * 2 <= FEW_SMEM / 2) {
+        FewArgs f = {};
+        f.x = static_cast<const uint16_t*>(x);
+        f.ldx = ldx;
+        f.w = static_cast<const uint16_t*>(w);
+        f.bias = static_cast<const uint16_t*>(bias);
+        f.residual = static_cast<const uint16_t*>(residual);
+        f.ldr = ldr;
+        f.y = static_cast<uint16_t*>(y);
+        f.ldy = ldy;
+        f.rows = (int)T;
+        f.D = (int)D;
+        f.F = (int)F;
+        f.act = act;
+        f.bf16 = type == SOM_BF16;
+        f.flags = l->flags;
+        return launch_few(l, f, 1, gated, st);
+    }
     ProdArgs a = {};
     LAY_TRY(map_left(l, &a.a, x, D, T, ldx));
     LAY_TRY(map_64(l, &a.b, w, D, rows, D));
@@ -365,8 +386,13 @@ static SlotPlan carve_plan(Carver& c, int64_t T, int E, int k, int tile)
     p.pos = c.take<int>(slots);
     p.row_slot = c.take<int>(p.max_rows);
     p.row_weight = c.take<float>(p.max_rows);
+    p.block_counts = c.take<int>((int64_t)plan_blocks(slots) * E);
     return p;
 }
+
+// So few slots that most experts in use have one: each slot reads its expert's weights by itself (a weight that two slots
+// read comes from L2 the second time).
+static bool few_slots(int64_t T, int E, int k) { return T * k <= 16 || (T * k <= 64 && T * k <= E); }
 
 // Pairs of blocks once the experts have rows enough for their tiles (256 rows); with fewer, a pair would mostly multiply
 // padding, and the weights' bytes bound the product, not the tensor cores.
@@ -402,6 +428,44 @@ int som_experts(som_layers* l, int type, int act, int gated, int64_t T, int32_t 
     Guard g(l->device);
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
     const int64_t rows1 = gated ? 2 * I : I;
+    if (few_slots(T, E, k) && D * 2 <= FEW_SMEM && k * I * 4 <= FEW_SMEM) {
+        LAY_TRY(ensure(l, (size_t)(T * k * I) * sizeof(float)));
+        FewArgs f = {};
+        f.x = static_cast<const uint16_t*>(x);
+        f.ldx = ldx;
+        f.w = static_cast<const uint16_t*>(w1);
+        f.bias = static_cast<const uint16_t*>(b1);
+        f.hidden = static_cast<float*>(l->ws);
+        f.indices = indices;
+        f.weights = weights;
+        f.weights_type = weights_type;
+        f.k = k;
+        f.E = E;
+        f.rows = 1;
+        f.D = (int)D;
+        f.F = (int)I;
+        f.act = act;
+        f.bf16 = type == SOM_BF16;
+        f.flags = l->flags;
+        LAY_TRY(launch_few(l, f, (int)(T * k), gated, st));
+        FewDownArgs d = {};
+        d.hidden = f.hidden;
+        d.indices = indices;
+        d.weights = weights;
+        d.w2 = static_cast<const uint16_t*>(w2);
+        d.b2 = static_cast<const uint16_t*>(b2);
+        d.residual = static_cast<const uint16_t*>(residual);
+        d.y = static_cast<uint16_t*>(y);
+        d.ldr = ldr;
+        d.ldy = ldy;
+        d.weights_type = weights_type;
+        d.k = k;
+        d.E = E;
+        d.D = (int)D;
+        d.I = (int)I;
+        d.bf16 = f.bf16;
+        return launch_few_down(l, d, T, st);
+    }
     SlotPlan p;
     uint16_t *xp, *h;
     float* part;

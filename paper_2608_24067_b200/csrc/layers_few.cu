@@ -1,0 +1,307 @@
+// The linear unit for a handful of rows, on the CUDA cores: single tokens while decoding.
+//
+// With so few rows a weight is used once or a few times, so the weights' bytes are all that counts and the tensor cores'
+// tiles would be almost empty.  A warp owns one output feature (its gate row and its other row together) and reads those
+// weight rows once, 16 bytes a lane and several loads in flight, against the tokens' rows in shared memory; a few warps
+// share a feature where there are too few features to keep the memory busy.  k_few computes act(x W^T + b) (+ residual),
+// for one group of rows (som_linear) or for every slot with its expert's weights (som_experts, first product); k_few_down
+// the experts' second product, one warp an output of one token over all of the token's experts, so that neither a join nor a
+// second pass over y follows.  The experts' hidden values stay in fp32 between the two.
+#include "layers_few.cuh"
+#include "layers_math.cuh"
+
+namespace lay {
+namespace {
+
+constexpr int FEW_WARPS = 8, FEW_THREADS = 32 * FEW_WARPS;
+
+// v[8] of an fp32 or 16-bit row in shared memory
+__device__ __forceinline__ void smem8(const uint16_t* p, float (&v)[8], int bf16)
+{
+    const uint4 w = *reinterpret_cast<const uint4*>(p);
+    const float2 a = unpack2(w.x, bf16), b = unpack2(w.y, bf16), c = unpack2(w.z, bf16), d = unpack2(w.w, bf16);
+    v[0] = a.x, v[1] = a.y, v[2] = b.x, v[3] = b.y, v[4] = c.x, v[5] = c.y, v[6] = d.x, v[7] = d.y;
+}
+
+__device__ __forceinline__ void widen8(const uint4& w, float (&v)[8], int bf16)
+{
+    const float2 a = unpack2(w.x, bf16), b = unpack2(w.y, bf16), c = unpack2(w.z, bf16), d = unpack2(w.w, bf16);
+    v[0] = a.x, v[1] = a.y, v[2] = b.x, v[3] = b.y, v[4] = c.x, v[5] = c.y, v[6] = d.x, v[7] = d.y;
+}
+
+// weights are read once: past L1
+__device__ __forceinline__ uint4 stream16(const uint16_t* p)
+{
+    uint4 v;
+    asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];"
+                 : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
+                 : "l"(p));
+    return v;
+}
+
+__device__ __forceinline__ float lanes_sum(float v)
+{
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
+    return v;
+}
+
+// ROWS rows of x against one feature; HALVES = 2 when gated.  `share` warps of the block split the sum over D.
+template <int ROWS, int HALVES>
+__global__ void __launch_bounds__(FEW_THREADS) k_few(const FewArgs a)
+{
+    extern __shared__ __align__(16) uint16_t xs[];  // [ROWS][D]
+    __shared__ float part[FEW_WARPS][ROWS * HALVES];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    int64_t first = 0;  // first row of x and of the output
+    const uint16_t *w = a.w, *bias = a.bias;
+    float weight = 1.f;
+    if (a.indices) {  // one slot a block column
+        const int e = a.indices[blockIdx.y];
+        if (e < 0 || e >= a.E) {
+            if (e < -1 || e >= a.E) {
+                if (threadIdx.x == 0) atomicOr(a.flags, LAY_FLAG_BAD_EXPERT);
+            }
+            return;
+        }
+        first = blockIdx.y / a.k;
+        w += (size_t)e * (HALVES * a.F) * a.D;
+        if (bias) bias += (size_t)e * HALVES * a.F;
+        weight = a.weights_type == SOM_F32 ? static_cast<const float*>(a.weights)[blockIdx.y]
+                                           : unpack1(static_cast<const uint16_t*>(a.weights)[blockIdx.y], a.weights_type == SOM_BF16);
+    }
+    const int share = a.share, features = FEW_WARPS / share;
+    const int f = blockIdx.x * features + warp / share, part_of = warp % share;
+    const uint16_t* row[HALVES];
+#pragma unroll
+    for (int h = 0; h < HALVES; ++h) row[h] = w + (size_t)((f < a.F ? f : 0) + h * a.F) * a.D;
+    float acc[ROWS][HALVES];
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r)
+#pragma unroll
+        for (int h = 0; h < HALVES; ++h) acc[r][h] = 0.f;
+
+    constexpr int DEEP = 8 / HALVES;  // eight 16-byte loads in flight
+    const int step = 256 * share;
+    int c = part_of * 256 + lane * 8;
+    uint4 next[DEEP][HALVES];
+    // the first weights travel while the rows of x are brought in
+#pragma unroll
+    for (int i = 0; i < DEEP; ++i)
+#pragma unroll
+        for (int h = 0; h < HALVES; ++h) next[i][h] = c + i * step < a.D ? stream16(row[h] + c + i * step) : make_uint4(0u, 0u, 0u, 0u);
+    for (int i = threadIdx.x; i < ROWS * (a.D / 8); i += FEW_THREADS) {
+        const int r = ROWS == 1 ? 0 : i / (a.D / 8), q = ROWS == 1 ? i : i % (a.D / 8);
+        *reinterpret_cast<uint4*>(xs + (size_t)i * 8) = r < a.rows ? __ldg(reinterpret_cast<const uint4*>(a.x + (size_t)(first + r) * a.ldx) + q) : make_uint4(0u, 0u, 0u, 0u);
+    }
+    __syncthreads();
+    while (c < a.D) {
+        uint4 now[DEEP][HALVES];
+        const int at = c;
+#pragma unroll
+        for (int i = 0; i < DEEP; ++i)
+#pragma unroll
+            for (int h = 0; h < HALVES; ++h) now[i][h] = next[i][h];
+        c += DEEP * step;
+#pragma unroll
+        for (int i = 0; i < DEEP; ++i)
+#pragma unroll
+            for (int h = 0; h < HALVES; ++h)
+                next[i][h] = c + i * step < a.D ? stream16(row[h] + c + i * step) : make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+        for (int i = 0; i < DEEP; ++i) {
+            if (at + i * step >= a.D) break;
+            float wv[HALVES][8];
+#pragma unroll
+            for (int h = 0; h < HALVES; ++h) widen8(now[i][h], wv[h], a.bf16);
+#pragma unroll
+            for (int r = 0; r < ROWS; ++r) {
+                float xv[8];
+                smem8(xs + (size_t)r * a.D + at + i * step, xv, a.bf16);
+#pragma unroll
+                for (int h = 0; h < HALVES; ++h)
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) acc[r][h] = fmaf(wv[h][j], xv[j], acc[r][h]);
+            }
+        }
+    }
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r)
+#pragma unroll
+        for (int h = 0; h < HALVES; ++h) acc[r][h] = lanes_sum(acc[r][h]);
+    if (share > 1) {  // the warps' parts, added in their order
+        if (lane == 0) {
+#pragma unroll
+            for (int r = 0; r < ROWS; ++r)
+#pragma unroll
+                for (int h = 0; h < HALVES; ++h) part[warp][r * HALVES + h] = acc[r][h];
+        }
+        __syncthreads();
+        if (part_of) return;
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r)
+#pragma unroll
+            for (int h = 0; h < HALVES; ++h) {
+                float s = part[warp][r * HALVES + h];
+                for (int i = 1; i < share; ++i) s += part[warp + i][r * HALVES + h];
+                acc[r][h] = s;
+            }
+    }
+    if (f >= a.F || lane >= a.rows) return;
+    float z = acc[0][0], u = HALVES == 2 ? acc[0][HALVES - 1] : 1.f;  // lane r: row r
+#pragma unroll
+    for (int r = 1; r < ROWS; ++r)
+        if (lane == r) {
+            z = acc[r][0];
+            if (HALVES == 2) u = acc[r][HALVES - 1];
+        }
+    if (bias) {
+        z += unpack1(__ldg(bias + f), a.bf16);
+        if (HALVES == 2) u += unpack1(__ldg(bias + a.F + f), a.bf16);
+    }
+    float y = 0.f;
+    with_act(a.act, [&](auto tag) { y = act_of<decltype(tag)::value>(z); });
+    if (HALVES == 2) y *= u;
+    if (a.hidden) {
+        a.hidden[(size_t)blockIdx.y * a.F + f] = y * weight;
+    } else {
+        if (a.residual) y += unpack1(__ldg(a.residual + (size_t)lane * a.ldr + f), a.bf16);
+        a.y[(size_t)lane * a.ldy + f] = (uint16_t)pack2(y, 0.f, a.bf16);
+    }
+}
+
+// y[t][d] = residual + sum_j (<w2[e_j][d], hidden[t, j]> + weight_j b2[e_j][d]); `share` warps of the block share an output,
+// each a part of the k * I products.
+__global__ void __launch_bounds__(FEW_THREADS) k_few_down(const FewDownArgs a)
+{
+    extern __shared__ __align__(16) float hs[];  // [k][I]
+    __shared__ float part[FEW_WARPS];
+    __shared__ int experts[32];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int64_t t = blockIdx.y;
+    if (threadIdx.x < a.k) {
+        const int e = a.indices[t * a.k + threadIdx.x];
+        experts[threadIdx.x] = e >= 0 && e < a.E ? e : -1;
+    }
+    __syncthreads();
+    const int share = a.share, outputs = FEW_WARPS / share;
+    const int d = blockIdx.x * outputs + warp / share, part_of = warp % share;
+    const int chunks = (a.I + 255) / 256, all = a.k * chunks;  // pieces of 256 products, a piece within one expert
+    constexpr int DEEP = 8;
+    float acc = 0.f;
+    uint4 next[DEEP];
+    const int row = d < a.D ? d : 0;
+    auto fetch = [&](int i) {
+        const int j = i / chunks, c = (i - j * chunks) * 256 + lane * 8;
+        return i < all && c < a.I && experts[j] >= 0 ? stream16(a.w2 + ((size_t)experts[j] * a.D + row) * a.I + c) : make_uint4(0u, 0u, 0u, 0u);
+    };
+#pragma unroll
+    for (int i = 0; i < DEEP; ++i) next[i] = fetch(part_of + i * share);
+    for (int i = threadIdx.x; i < a.k * a.I / 4; i += FEW_THREADS) {
+        const int j = i / (a.I / 4);
+        reinterpret_cast<float4*>(hs)[i] = experts[j] >= 0 ? __ldcg(reinterpret_cast<const float4*>(a.hidden + t * a.k * a.I) + i) : make_float4(0.f, 0.f, 0.f, 0.f);
+    }
+    __syncthreads();
+    for (int i0 = part_of; i0 < all; i0 += DEEP * share) {
+        uint4 now[DEEP];
+#pragma unroll
+        for (int i = 0; i < DEEP; ++i) now[i] = next[i];
+#pragma unroll
+        for (int i = 0; i < DEEP; ++i) next[i] = fetch(i0 + (DEEP + i) * share);
+#pragma unroll
+        for (int i = 0; i < DEEP; ++i) {
+            const int p = i0 + i * share;
+            if (p >= all) break;
+            const int j = p / chunks, c = (p - j * chunks) * 256 + lane * 8;
+            if (c >= a.I || experts[j] < 0) continue;
+            float wv[8];
+            widen8(now[i], wv, a.bf16);
+            const float4 h0 = *reinterpret_cast<const float4*>(hs + (size_t)j * a.I + c), h1 = *reinterpret_cast<const float4*>(hs + (size_t)j * a.I + c + 4);
+            acc = fmaf(wv[0], h0.x, acc), acc = fmaf(wv[1], h0.y, acc), acc = fmaf(wv[2], h0.z, acc), acc = fmaf(wv[3], h0.w, acc);
+            acc = fmaf(wv[4], h1.x, acc), acc = fmaf(wv[5], h1.y, acc), acc = fmaf(wv[6], h1.z, acc), acc = fmaf(wv[7], h1.w, acc);
+        }
+    }
+    acc = lanes_sum(acc);
+    if (share > 1) {
+        if (lane == 0) part[warp] = acc;
+        __syncthreads();
+        if (part_of) return;
+        acc = part[warp];
+        for (int i = 1; i < share; ++i) acc += part[warp + i];
+    }
+    if (d >= a.D || lane) return;
+    if (a.b2)
+        for (int j = 0; j < a.k; ++j) {
+            if (experts[j] < 0) continue;
+            const float wt = a.weights_type == SOM_F32 ? static_cast<const float*>(a.weights)[t * a.k + j]
+                                                       : unpack1(static_cast<const uint16_t*>(a.weights)[t * a.k + j], a.weights_type == SOM_BF16);
+            acc = fmaf(wt, unpack1(__ldg(a.b2 + (size_t)experts[j] * a.D + d), a.bf16), acc);
+        }
+    if (a.residual) acc += unpack1(__ldg(a.residual + (size_t)t * a.ldr + d), a.bf16);
+    a.y[(size_t)t * a.ldy + d] = (uint16_t)pack2(acc, 0.f, a.bf16);
+}
+
+template <int HALVES>
+cudaError_t go(const FewArgs& a, dim3 grid, size_t smem, cudaStream_t st)
+{
+    if (a.rows == 1) k_few<1, HALVES><<<grid, FEW_THREADS, smem, st>>>(a);
+    else if (a.rows == 2) k_few<2, HALVES><<<grid, FEW_THREADS, 2 * smem, st>>>(a);
+    else if (a.rows <= 4) k_few<4, HALVES><<<grid, FEW_THREADS, 4 * smem, st>>>(a);
+    else k_few<8, HALVES><<<grid, FEW_THREADS, 8 * smem, st>>>(a);
+    return cudaGetLastError();
+}
+
+template <int HALVES>
+cudaError_t allow()
+{
+    cudaError_t e = cudaFuncSetAttribute(k_few<1, HALVES>, cudaFuncAttributeMaxDynamicSharedMemorySize, FEW_SMEM);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(k_few<2, HALVES>, cudaFuncAttributeMaxDynamicSharedMemorySize, FEW_SMEM);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(k_few<4, HALVES>, cudaFuncAttributeMaxDynamicSharedMemorySize, FEW_SMEM);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(k_few<8, HALVES>, cudaFuncAttributeMaxDynamicSharedMemorySize, FEW_SMEM);
+    return e;
+}
+
+// Warps that share an output: as many as it takes for 32 warps on every SM, each with at least 512 products.
+int share_of(const som_layers* l, int64_t outputs, int64_t length)
+{
+    int s = 1;
+    while (s < FEW_WARPS && outputs * s < (int64_t)l->sm_count * 32 && length / (2 * s) >= 512) s *= 2;
+    return s;
+}
+
+}  // namespace
+
+cudaError_t prepare_few()
+{
+    cudaError_t e = allow<1>();
+    if (e == cudaSuccess) e = allow<2>();
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(k_few_down, cudaFuncAttributeMaxDynamicSharedMemorySize, FEW_SMEM);
+    return e;
+}
+
+int launch_few(som_layers* l, FewArgs a, int groups, bool gated, cudaStream_t st)
+{
+    a.share = share_of(l, (int64_t)a.F * groups, (int64_t)a.D);
+    const int features = FEW_WARPS / a.share;
+    const dim3 grid((unsigned)((a.F + features - 1) / features), (unsigned)groups);
+    const cudaError_t e = gated ? go<2>(a, grid, (size_t)a.D * 2, st) : go<1>(a, grid, (size_t)a.D * 2, st);
+    ++l->launches;
+    if (e == cudaSuccess) return SOM_OK;
+    l->last_cuda_error = (int)e;
+    return SOM_ERR_CUDA;
+}
+
+int launch_few_down(som_layers* l, FewDownArgs a, int64_t T, cudaStream_t st)
+{
+    a.share = share_of(l, a.D * T, (int64_t)a.k * a.I);
+    const int outputs = FEW_WARPS / a.share;
+    const dim3 grid((unsigned)((a.D + outputs - 1) / outputs), (unsigned)T);
+    k_few_down<<<grid, FEW_THREADS, (size_t)a.k * a.I * sizeof(float), st>>>(a);
+    ++l->launches;
+    const cudaError_t e = cudaGetLastError();
+    if (e == cudaSuccess) return SOM_OK;
+    l->last_cuda_error = (int)e;
+    return SOM_ERR_CUDA;
+}
+
+}  // namespace lay

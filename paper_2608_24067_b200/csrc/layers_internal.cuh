@@ -36,12 +36,15 @@ struct SlotPlan {
     int* pos;          // [T * k] row of a slot, -1 = none
     int* row_slot;     // [max rows] slot of a row in use
     float* row_weight; // [max rows] the slot's routing weight
+    int* block_counts; // [plan_blocks][E] scratch of the plan
     int max_rows;      // upper bound that the host sizes buffers and grids by
     int tile;          // rows of a tile
 };
 
 cudaError_t prepare_product(som_layers* l);  // once per handle
 
+cudaError_t prepare_plan();  // once per handle
+int plan_blocks(int64_t slots);  // rows of SlotPlan::block_counts
 int launch_plan(som_layers* l, const SlotPlan& p, const int32_t* indices, const void* weights, int weights_type, int64_t T,
                 int k, int E, cudaStream_t st);
 

@@ -90,6 +90,117 @@ __global__ void __launch_bounds__(PLAN_THREADS) k_slot_plan(SlotPlan p, const in
     }
 }
 
+// The same for many slots, in three launches over blocks of PLACE_SLOTS consecutive slots: every block counts its slots by
+// expert, one block turns the counts into segments and the blocks' starting places, every block places its slots.  (One
+// block alone took 60 us for 32768 slots.)
+constexpr int PLACE_SLOTS = 1024, PLACE_WARPS = 8;
+
+__global__ void __launch_bounds__(32 * PLACE_WARPS) k_slot_count(const int32_t* indices, int64_t slots, int E, int* counts, int* flags)
+{
+    extern __shared__ int hist[];  // [E]
+    for (int i = threadIdx.x; i < E; i += 32 * PLACE_WARPS) hist[i] = 0;
+    __syncthreads();
+    const int64_t lo = (int64_t)blockIdx.x * PLACE_SLOTS, hi = lo + PLACE_SLOTS < slots ? lo + PLACE_SLOTS : slots;
+    bool bad = false;
+    for (int64_t s = lo + threadIdx.x; s < hi; s += 32 * PLACE_WARPS) {
+        const int e = indices[s];
+        if (e >= 0 && e < E) atomicAdd(&hist[e], 1);
+        bad |= e < -1 || e >= E;
+    }
+    som_raise(flags, bad, LAY_FLAG_BAD_EXPERT);
+    __syncthreads();
+    for (int i = threadIdx.x; i < E; i += 32 * PLACE_WARPS) counts[(size_t)blockIdx.x * E + i] = hist[i];
+}
+
+// counts[block][e] -> first place of the block's slots within expert e; the segments
+__global__ void __launch_bounds__(PLAN_THREADS) k_slot_segments(SlotPlan p, int E, int blocks, int* counts)
+{
+    __shared__ int warp_sum[PLAN_WARPS];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, e = threadIdx.x;
+    int count = 0;
+    if (e < E)
+        for (int b0 = 0; b0 < blocks; b0 += 8) {
+            int c[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) c[i] = b0 + i < blocks ? counts[(size_t)(b0 + i) * E + e] : 0;
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (b0 + i < blocks) {
+                    counts[(size_t)(b0 + i) * E + e] = count;
+                    count += c[i];
+                }
+        }
+    const int tiles = (count + p.tile - 1) / p.tile;
+    int sum = tiles;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+        const int v = __shfl_up_sync(0xffffffffu, sum, d);
+        if (lane >= d) sum += v;
+    }
+    if (lane == 31) warp_sum[warp] = sum;
+    __syncthreads();
+    int before = sum - tiles;
+    for (int w = 0; w < warp; ++w) before += warp_sum[w];
+    if (e < E) {
+        p.seg[e] = before * p.tile;
+        p.count[e] = count;
+        for (int i = 0; i < tiles; ++i) p.tile_expert[before + i] = e;
+        if (e == E - 1) {
+            p.seg[E] = (before + tiles) * p.tile;
+            *p.tiles = before + tiles;
+        }
+    }
+}
+
+__global__ void __launch_bounds__(32 * PLACE_WARPS) k_slot_place(SlotPlan p, const int32_t* indices, const void* weights, int weights_type,
+                                                                int64_t slots, int E, const int* places)
+{
+    extern __shared__ int hist[];  // [PLACE_WARPS][E]
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    for (int i = threadIdx.x; i < PLACE_WARPS * E; i += 32 * PLACE_WARPS) hist[i] = 0;
+    __syncthreads();
+    constexpr int RUN = PLACE_SLOTS / PLACE_WARPS;
+    const int64_t lo = (int64_t)blockIdx.x * PLACE_SLOTS + warp * RUN;
+    int* mine = hist + warp * E;
+    int x[RUN / 32], same[RUN / 32];
+#pragma unroll
+    for (int i = 0; i < RUN / 32; ++i) {
+        const int64_t s = lo + i * 32 + lane;
+        x[i] = s < slots ? indices[s] : -1;
+        if (x[i] < 0 || x[i] >= E) x[i] = -1;
+        same[i] = (int)__match_any_sync(0xffffffffu, x[i]);
+        if (x[i] >= 0 && (same[i] & ((1 << lane) - 1)) == 0) mine[x[i]] += __popc(same[i]);
+        __syncwarp();
+    }
+    __syncthreads();
+    for (int e = threadIdx.x; e < E; e += 32 * PLACE_WARPS) {
+        int at = p.seg[e] + places[(size_t)blockIdx.x * E + e];
+        for (int w = 0; w < PLACE_WARPS; ++w) {
+            const int c = hist[w * E + e];
+            hist[w * E + e] = at;
+            at += c;
+        }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < RUN / 32; ++i) {
+        const int64_t s = lo + i * 32 + lane;
+        const int rank = __popc(same[i] & ((1 << lane) - 1));
+        int row = -1;
+        if (x[i] >= 0) row = mine[x[i]] + rank;
+        __syncwarp();
+        if (x[i] >= 0 && rank == 0) mine[x[i]] += __popc(same[i]);
+        __syncwarp();
+        if (s < slots) {
+            p.pos[s] = row;
+            if (row >= 0) {
+                p.row_slot[row] = (int)s;
+                p.row_weight[row] = load_weight(weights, weights_type, s);
+            }
+        }
+    }
+}
+
 // Rows of x (blockIdx.z == 0) and of dy (1) in the slots' order, up to whole steps of 64 rows of an expert with zeros (the
 // sums over an expert's rows run in such steps).  A warp a row.
 __global__ void __launch_bounds__(256) k_gather(SlotPlan p, int k, int D, const uint16_t* x, int64_t ldx, uint16_t* xp,
@@ -245,16 +356,28 @@ int grid_for(const som_layers* l, int64_t items, int per)
 
 }  // namespace
 
+cudaError_t prepare_plan()
+{
+    return cudaFuncSetAttribute(k_slot_plan, cudaFuncAttributeMaxDynamicSharedMemorySize, (PLAN_WARPS + 1) * 1024 * (int)sizeof(int));
+}
+
+// One block for up to 2048 slots (5 to 7 us; three launches take about as long), blocks of PLACE_SLOTS beyond.
+int plan_blocks(int64_t slots) { return slots <= 2048 ? 0 : (int)((slots + PLACE_SLOTS - 1) / PLACE_SLOTS); }
+
 int launch_plan(som_layers* l, const SlotPlan& p, const int32_t* indices, const void* weights, int weights_type, int64_t T,
                 int k, int E, cudaStream_t st)
 {
-    const size_t smem = (size_t)(PLAN_WARPS + 1) * E * sizeof(int);
-    const cudaError_t e = cudaFuncSetAttribute(k_slot_plan, cudaFuncAttributeMaxDynamicSharedMemorySize, (PLAN_WARPS + 1) * 1024 * (int)sizeof(int));
-    if (e != cudaSuccess) {
-        l->last_cuda_error = (int)e;
-        return SOM_ERR_CUDA;
+    const int blocks = plan_blocks(T * k);
+    if (blocks == 0) {
+        const size_t smem = (size_t)(PLAN_WARPS + 1) * E * sizeof(int);
+        k_slot_plan<<<1, PLAN_THREADS, smem, st>>>(p, indices, weights, weights_type, T * k, E, l->flags);
+        return done(l);
     }
-    k_slot_plan<<<1, PLAN_THREADS, smem, st>>>(p, indices, weights, weights_type, T * k, E, l->flags);
+    k_slot_count<<<blocks, 32 * PLACE_WARPS, (size_t)E * sizeof(int), st>>>(indices, T * k, E, p.block_counts, l->flags);
+    k_slot_segments<<<1, PLAN_THREADS, 0, st>>>(p, E, blocks, p.block_counts);
+    k_slot_place<<<blocks, 32 * PLACE_WARPS, (size_t)PLACE_WARPS * E * sizeof(int), st>>>(p, indices, weights, weights_type, T * k, E,
+                                                                                        p.block_counts);
+    l->launches += 2;
     return done(l);
 }
 
