@@ -46,9 +46,11 @@ __device__ __forceinline__ float lanes_sum(float v)
     return v;
 }
 
-// ROWS rows of x against one feature; HALVES = 2 when gated.  `share` warps of the block split the sum over D.
+// ROWS rows of x against one feature a warp; HALVES = 2 when gated.  `share` warps of the block split the sum over D.
+// Blocks stay and walk the features, and a weight's place in the registers is loaded again as soon as it has been used, with
+// the next feature's weights at the end of a row: the loads never drain.
 template <int ROWS, int HALVES>
-__global__ void __launch_bounds__(FEW_THREADS) k_few(const FewArgs a)
+__global__ void __launch_bounds__(FEW_THREADS, ROWS <= 2 ? 3 : 2) k_few(const FewArgs a)
 {
     extern __shared__ __align__(16) uint16_t xs[];  // [ROWS][D]
     __shared__ float part[FEW_WARPS][ROWS * HALVES];
@@ -59,9 +61,7 @@ __global__ void __launch_bounds__(FEW_THREADS) k_few(const FewArgs a)
     if (a.indices) {  // one slot a block column
         const int e = a.indices[blockIdx.y];
         if (e < 0 || e >= a.E) {
-            if (e < -1 || e >= a.E) {
-                if (threadIdx.x == 0) atomicOr(a.flags, LAY_FLAG_BAD_EXPERT);
-            }
+            if ((e < -1 || e >= a.E) && threadIdx.x == 0 && blockIdx.x == 0) atomicOr(a.flags, LAY_FLAG_BAD_EXPERT);
             return;
         }
         first = blockIdx.y / a.k;
@@ -70,175 +70,197 @@ __global__ void __launch_bounds__(FEW_THREADS) k_few(const FewArgs a)
         weight = a.weights_type == SOM_F32 ? static_cast<const float*>(a.weights)[blockIdx.y]
                                            : unpack1(static_cast<const uint16_t*>(a.weights)[blockIdx.y], a.weights_type == SOM_BF16);
     }
-    const int share = a.share, features = FEW_WARPS / share;
-    const int f = blockIdx.x * features + warp / share, part_of = warp % share;
-    const uint16_t* row[HALVES];
-#pragma unroll
-    for (int h = 0; h < HALVES; ++h) row[h] = w + (size_t)((f < a.F ? f : 0) + h * a.F) * a.D;
-    float acc[ROWS][HALVES];
-#pragma unroll
-    for (int r = 0; r < ROWS; ++r)
-#pragma unroll
-        for (int h = 0; h < HALVES; ++h) acc[r][h] = 0.f;
-
     constexpr int DEEP = 8 / HALVES;  // eight 16-byte loads in flight
-    const int step = 256 * share;
-    int c = part_of * 256 + lane * 8;
-    uint4 next[DEEP][HALVES];
-    // the first weights travel while the rows of x are brought in
+    const int share = a.share, features = FEW_WARPS / share, part_of = warp % share;
+    const int step = 256 * share, rounds = (a.D + DEEP * step - 1) / (DEEP * step);
+    const int c0 = part_of * 256 + lane * 8, stride = gridDim.x * features;
+    uint4 buf[DEEP][HALVES];
+    auto fetch = [&](int f, int round, int i) {
+        const int c = c0 + (round * DEEP + i) * step;
 #pragma unroll
-    for (int i = 0; i < DEEP; ++i)
+        for (int h = 0; h < HALVES; ++h)
+            buf[i][h] = f < a.F && c < a.D ? stream16(w + (size_t)(f + h * a.F) * a.D + c) : make_uint4(0u, 0u, 0u, 0u);
+    };
+    int f = blockIdx.x * features + warp / share;
 #pragma unroll
-        for (int h = 0; h < HALVES; ++h) next[i][h] = c + i * step < a.D ? stream16(row[h] + c + i * step) : make_uint4(0u, 0u, 0u, 0u);
+    for (int i = 0; i < DEEP; ++i) fetch(f, 0, i);  // the first weights travel while the rows of x are brought in
     for (int i = threadIdx.x; i < ROWS * (a.D / 8); i += FEW_THREADS) {
         const int r = ROWS == 1 ? 0 : i / (a.D / 8), q = ROWS == 1 ? i : i % (a.D / 8);
-        *reinterpret_cast<uint4*>(xs + (size_t)i * 8) = r < a.rows ? __ldg(reinterpret_cast<const uint4*>(a.x + (size_t)(first + r) * a.ldx) + q) : make_uint4(0u, 0u, 0u, 0u);
+        *reinterpret_cast<uint4*>(xs + (size_t)i * 8) =
+            r < a.rows ? __ldg(reinterpret_cast<const uint4*>(a.x + (size_t)(first + r) * a.ldx) + q) : make_uint4(0u, 0u, 0u, 0u);
     }
     __syncthreads();
-    while (c < a.D) {
-        uint4 now[DEEP][HALVES];
-        const int at = c;
-#pragma unroll
-        for (int i = 0; i < DEEP; ++i)
-#pragma unroll
-            for (int h = 0; h < HALVES; ++h) now[i][h] = next[i][h];
-        c += DEEP * step;
-#pragma unroll
-        for (int i = 0; i < DEEP; ++i)
-#pragma unroll
-            for (int h = 0; h < HALVES; ++h)
-                next[i][h] = c + i * step < a.D ? stream16(row[h] + c + i * step) : make_uint4(0u, 0u, 0u, 0u);
-#pragma unroll
-        for (int i = 0; i < DEEP; ++i) {
-            if (at + i * step >= a.D) break;
-            float wv[HALVES][8];
-#pragma unroll
-            for (int h = 0; h < HALVES; ++h) widen8(now[i][h], wv[h], a.bf16);
-#pragma unroll
-            for (int r = 0; r < ROWS; ++r) {
-                float xv[8];
-                smem8(xs + (size_t)r * a.D + at + i * step, xv, a.bf16);
-#pragma unroll
-                for (int h = 0; h < HALVES; ++h)
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) acc[r][h] = fmaf(wv[h][j], xv[j], acc[r][h]);
-            }
-        }
-    }
-#pragma unroll
-    for (int r = 0; r < ROWS; ++r)
-#pragma unroll
-        for (int h = 0; h < HALVES; ++h) acc[r][h] = lanes_sum(acc[r][h]);
-    if (share > 1) {  // the warps' parts, added in their order
-        if (lane == 0) {
-#pragma unroll
-            for (int r = 0; r < ROWS; ++r)
-#pragma unroll
-                for (int h = 0; h < HALVES; ++h) part[warp][r * HALVES + h] = acc[r][h];
-        }
-        __syncthreads();
-        if (part_of) return;
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    for (int f_block = blockIdx.x * features; f_block < a.F; f_block += stride, f += stride) {
+        float acc[ROWS][HALVES];
 #pragma unroll
         for (int r = 0; r < ROWS; ++r)
 #pragma unroll
-            for (int h = 0; h < HALVES; ++h) {
-                float s = part[warp][r * HALVES + h];
-                for (int i = 1; i < share; ++i) s += part[warp + i][r * HALVES + h];
-                acc[r][h] = s;
-            }
-    }
-    if (f >= a.F || lane >= a.rows) return;
-    float z = acc[0][0], u = HALVES == 2 ? acc[0][HALVES - 1] : 1.f;  // lane r: row r
+            for (int h = 0; h < HALVES; ++h) acc[r][h] = 0.f;
+        for (int round = 0; round < rounds; ++round) {
+            const bool last = round + 1 == rounds;
+            const int next_f = last ? f + stride : f, next_round = last ? 0 : round + 1;
 #pragma unroll
-    for (int r = 1; r < ROWS; ++r)
-        if (lane == r) {
-            z = acc[r][0];
-            if (HALVES == 2) u = acc[r][HALVES - 1];
+            for (int i = 0; i < DEEP; ++i) {
+                const int c = c0 + (round * DEEP + i) * step;
+                float wv[HALVES][8];
+#pragma unroll
+                for (int h = 0; h < HALVES; ++h) widen8(buf[i][h], wv[h], a.bf16);
+                fetch(next_f, next_round, i);
+                if (c < a.D) {
+#pragma unroll
+                    for (int r = 0; r < ROWS; ++r) {
+                        float xv[8];
+                        smem8(xs + (size_t)r * a.D + c, xv, a.bf16);
+#pragma unroll
+                        for (int h = 0; h < HALVES; ++h)
+#pragma unroll
+                            for (int j = 0; j < 8; ++j) acc[r][h] = fmaf(wv[h][j], xv[j], acc[r][h]);
+                    }
+                }
+            }
         }
-    if (bias) {
-        z += unpack1(__ldg(bias + f), a.bf16);
-        if (HALVES == 2) u += unpack1(__ldg(bias + a.F + f), a.bf16);
-    }
-    float y = 0.f;
-    with_act(a.act, [&](auto tag) { y = act_of<decltype(tag)::value>(z); });
-    if (HALVES == 2) y *= u;
-    if (a.hidden) {
-        a.hidden[(size_t)blockIdx.y * a.F + f] = y * weight;
-    } else {
-        if (a.residual) y += unpack1(__ldg(a.residual + (size_t)lane * a.ldr + f), a.bf16);
-        a.y[(size_t)lane * a.ldy + f] = (uint16_t)pack2(y, 0.f, a.bf16);
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r)
+#pragma unroll
+            for (int h = 0; h < HALVES; ++h) acc[r][h] = lanes_sum(acc[r][h]);
+        if (share > 1) {  // the warps' parts, added in their order
+            __syncthreads();  // the last feature's parts have been read
+            if (lane == 0) {
+#pragma unroll
+                for (int r = 0; r < ROWS; ++r)
+#pragma unroll
+                    for (int h = 0; h < HALVES; ++h) part[warp][r * HALVES + h] = acc[r][h];
+            }
+            __syncthreads();
+            if (part_of) continue;
+#pragma unroll
+            for (int r = 0; r < ROWS; ++r)
+#pragma unroll
+                for (int h = 0; h < HALVES; ++h) {
+                    float s = part[warp][r * HALVES + h];
+                    for (int i = 1; i < share; ++i) s += part[warp + i][r * HALVES + h];
+                    acc[r][h] = s;
+                }
+        }
+        if (f >= a.F || lane >= a.rows) continue;
+        float z = acc[0][0], u = HALVES == 2 ? acc[0][HALVES - 1] : 1.f;  // lane r: row r
+#pragma unroll
+        for (int r = 1; r < ROWS; ++r)
+            if (lane == r) {
+                z = acc[r][0];
+                if (HALVES == 2) u = acc[r][HALVES - 1];
+            }
+        if (bias) {
+            z += unpack1(__ldg(bias + f), a.bf16);
+            if (HALVES == 2) u += unpack1(__ldg(bias + a.F + f), a.bf16);
+        }
+        float y = 0.f;
+        with_act(a.act, [&](auto tag) { y = act_of<decltype(tag)::value>(z); });
+        if (HALVES == 2) y *= u;
+        if (a.hidden) {
+            a.hidden[(size_t)blockIdx.y * a.F + f] = y * weight;
+        } else {
+            if (a.residual) y += unpack1(__ldg(a.residual + (size_t)lane * a.ldr + f), a.bf16);
+            a.y[(size_t)lane * a.ldy + f] = (uint16_t)pack2(y, 0.f, a.bf16);
+        }
     }
 }
 
 // y[t][d] = residual + sum_j (<w2[e_j][d], hidden[t, j]> + weight_j b2[e_j][d]); `share` warps of the block share an output,
-// each a part of the k * I products.
-__global__ void __launch_bounds__(FEW_THREADS) k_few_down(const FewDownArgs a)
+// each a part of the k * I products.  Blocks stay, as above: the token's hidden values are brought in once a block.  The
+// first weights are read while the kernel before, which writes the hidden values, still runs.
+__global__ void __launch_bounds__(FEW_THREADS, 3) k_few_down(const FewDownArgs a)
 {
-    extern __shared__ __align__(16) float hs[];  // [k][I]
+    extern __shared__ __align__(16) float hs[];  // [k][2][I / 2]: of every eight values the first four, then the other four
     __shared__ float part[FEW_WARPS];
-    __shared__ int experts[32];
+    __shared__ int64_t base[32];  // the experts' weights, -1 = none
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int64_t t = blockIdx.y;
     if (threadIdx.x < a.k) {
         const int e = a.indices[t * a.k + threadIdx.x];
-        experts[threadIdx.x] = e >= 0 && e < a.E ? e : -1;
+        base[threadIdx.x] = e >= 0 && e < a.E ? (int64_t)e * a.D * a.I : -1;
     }
     __syncthreads();
-    const int share = a.share, outputs = FEW_WARPS / share;
-    const int d = blockIdx.x * outputs + warp / share, part_of = warp % share;
-    const int chunks = (a.I + 255) / 256, all = a.k * chunks;  // pieces of 256 products, a piece within one expert
     constexpr int DEEP = 8;
-    float acc = 0.f;
-    uint4 next[DEEP];
-    const int row = d < a.D ? d : 0;
-    auto fetch = [&](int i) {
-        const int j = i / chunks, c = (i - j * chunks) * 256 + lane * 8;
-        return i < all && c < a.I && experts[j] >= 0 ? stream16(a.w2 + ((size_t)experts[j] * a.D + row) * a.I + c) : make_uint4(0u, 0u, 0u, 0u);
+    const int share = a.share, outputs = FEW_WARPS / share, part_of = warp % share;
+    const int span = (a.I + 255) / 256 * 256, all = a.k * (span / 256);  // pieces of 256 products, a piece within one expert
+    const int rounds = (all + DEEP * share - 1) / (DEEP * share), stride = gridDim.x * outputs;
+    // a warp's pieces are part_of, part_of + share, ...: place (j, c) of the next one to read and of the next one to use
+    struct Place {
+        int j, c;
+        __device__ __forceinline__ void settle(int span)
+        {
+            while (c >= span) c -= span, ++j;
+        }
     };
+    Place from{0, part_of * 256};
+    from.settle(span);
+    const Place start = from;
+    uint4 buf[DEEP];
+    auto fetch = [&](int d, uint4& to) {
+        const int c = from.c + lane * 8;
+        to = make_uint4(0u, 0u, 0u, 0u);
+        if (d < a.D && from.j < a.k && c < a.I) {
+            const int64_t b = base[from.j];
+            if (b >= 0) to = stream16(a.w2 + b + (int64_t)d * a.I + c);
+        }
+        from.c += 256 * share;
+        from.settle(span);
+    };
+    int d = blockIdx.x * outputs + warp / share;
 #pragma unroll
-    for (int i = 0; i < DEEP; ++i) next[i] = fetch(part_of + i * share);
-    for (int i = threadIdx.x; i < a.k * a.I / 4; i += FEW_THREADS) {
-        const int j = i / (a.I / 4);
-        reinterpret_cast<float4*>(hs)[i] = experts[j] >= 0 ? __ldcg(reinterpret_cast<const float4*>(a.hidden + t * a.k * a.I) + i) : make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int i = 0; i < DEEP; ++i) fetch(d, buf[i]);
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    for (int i = threadIdx.x; i < a.k * (a.I / 4); i += FEW_THREADS) {
+        const int j = i / (a.I / 4), q = i - j * (a.I / 4);
+        reinterpret_cast<float4*>(hs)[j * (a.I / 4) + (q & 1) * (a.I / 8) + (q >> 1)] =
+            base[j] >= 0 ? __ldcg(reinterpret_cast<const float4*>(a.hidden + t * a.k * a.I) + i) : make_float4(0.f, 0.f, 0.f, 0.f);
     }
     __syncthreads();
-    for (int i0 = part_of; i0 < all; i0 += DEEP * share) {
-        uint4 now[DEEP];
+    for (int d_block = blockIdx.x * outputs; d_block < a.D; d_block += stride, d += stride) {
+        float acc = 0.f;
+        Place use = start;
+        for (int round = 0; round < rounds; ++round) {
+            const bool last = round + 1 == rounds;
+            if (last) from = start;
+            const int next_d = last ? d + stride : d;
 #pragma unroll
-        for (int i = 0; i < DEEP; ++i) now[i] = next[i];
-#pragma unroll
-        for (int i = 0; i < DEEP; ++i) next[i] = fetch(i0 + (DEEP + i) * share);
-#pragma unroll
-        for (int i = 0; i < DEEP; ++i) {
-            const int p = i0 + i * share;
-            if (p >= all) break;
-            const int j = p / chunks, c = (p - j * chunks) * 256 + lane * 8;
-            if (c >= a.I || experts[j] < 0) continue;
-            float wv[8];
-            widen8(now[i], wv, a.bf16);
-            const float4 h0 = *reinterpret_cast<const float4*>(hs + (size_t)j * a.I + c), h1 = *reinterpret_cast<const float4*>(hs + (size_t)j * a.I + c + 4);
-            acc = fmaf(wv[0], h0.x, acc), acc = fmaf(wv[1], h0.y, acc), acc = fmaf(wv[2], h0.z, acc), acc = fmaf(wv[3], h0.w, acc);
-            acc = fmaf(wv[4], h1.x, acc), acc = fmaf(wv[5], h1.y, acc), acc = fmaf(wv[6], h1.z, acc), acc = fmaf(wv[7], h1.w, acc);
+            for (int i = 0; i < DEEP; ++i) {
+                float wv[8];
+                widen8(buf[i], wv, a.bf16);
+                fetch(next_d, buf[i]);
+                const int c = use.c + lane * 8;
+                if (use.j < a.k && c < a.I) {
+                    const float* h = hs + (size_t)use.j * a.I + c / 2;
+                    const float4 h0 = *reinterpret_cast<const float4*>(h), h1 = *reinterpret_cast<const float4*>(h + a.I / 2);
+                    acc = fmaf(wv[0], h0.x, acc), acc = fmaf(wv[1], h0.y, acc), acc = fmaf(wv[2], h0.z, acc), acc = fmaf(wv[3], h0.w, acc);
+                    acc = fmaf(wv[4], h1.x, acc), acc = fmaf(wv[5], h1.y, acc), acc = fmaf(wv[6], h1.z, acc), acc = fmaf(wv[7], h1.w, acc);
+                }
+                use.c += 256 * share;
+                use.settle(span);
+            }
         }
-    }
-    acc = lanes_sum(acc);
-    if (share > 1) {
-        if (lane == 0) part[warp] = acc;
-        __syncthreads();
-        if (part_of) return;
-        acc = part[warp];
-        for (int i = 1; i < share; ++i) acc += part[warp + i];
-    }
-    if (d >= a.D || lane) return;
-    if (a.b2)
-        for (int j = 0; j < a.k; ++j) {
-            if (experts[j] < 0) continue;
-            const float wt = a.weights_type == SOM_F32 ? static_cast<const float*>(a.weights)[t * a.k + j]
-                                                       : unpack1(static_cast<const uint16_t*>(a.weights)[t * a.k + j], a.weights_type == SOM_BF16);
-            acc = fmaf(wt, unpack1(__ldg(a.b2 + (size_t)experts[j] * a.D + d), a.bf16), acc);
+        acc = lanes_sum(acc);
+        if (share > 1) {
+            __syncthreads();
+            if (lane == 0) part[warp] = acc;
+            __syncthreads();
+            if (part_of) continue;
+            acc = part[warp];
+            for (int i = 1; i < share; ++i) acc += part[warp + i];
         }
-    if (a.residual) acc += unpack1(__ldg(a.residual + (size_t)t * a.ldr + d), a.bf16);
-    a.y[(size_t)t * a.ldy + d] = (uint16_t)pack2(acc, 0.f, a.bf16);
+        if (d >= a.D || lane) continue;
+        if (a.b2)
+            for (int j = 0; j < a.k; ++j) {
+                if (base[j] < 0) continue;
+                const float wt = a.weights_type == SOM_F32 ? static_cast<const float*>(a.weights)[t * a.k + j]
+                                                           : unpack1(static_cast<const uint16_t*>(a.weights)[t * a.k + j], a.weights_type == SOM_BF16);
+                acc = fmaf(wt, unpack1(__ldg(a.b2 + (size_t)a.indices[t * a.k + j] * a.D + d), a.bf16), acc);
+            }
+        if (a.residual) acc += unpack1(__ldg(a.residual + (size_t)t * a.ldr + d), a.bf16);
+        a.y[(size_t)t * a.ldy + d] = (uint16_t)pack2(acc, 0.f, a.bf16);
+    }
 }
 
 template <int HALVES>
@@ -261,12 +283,20 @@ cudaError_t allow()
     return e;
 }
 
-// Warps that share an output: as many as it takes for 32 warps on every SM, each with at least 512 products.
-int share_of(const som_layers* l, int64_t outputs, int64_t length)
+// Warps that share an output: as many as it takes for three outputs' parts to every resident warp (24 on an SM), so that
+// the last ones do not leave the others idle for long, each part no shorter than the loads that a warp has in flight.
+int share_of(const som_layers* l, int64_t outputs, int64_t length, int in_flight)
 {
     int s = 1;
-    while (s < FEW_WARPS && outputs * s < (int64_t)l->sm_count * 32 && length / (2 * s) >= 512) s *= 2;
+    while (s < FEW_WARPS && outputs * s < (int64_t)l->sm_count * 24 * 3 && length / (2 * s) >= in_flight) s *= 2;
     return s;
+}
+
+// Blocks for `outputs` of them, `each` a block at a time, in `groups` columns: no more than are resident.
+dim3 few_grid(const som_layers* l, int64_t outputs, int each, int64_t groups)
+{
+    const int64_t want = (outputs + each - 1) / each, most = (int64_t)l->sm_count * 3 / groups;
+    return dim3((unsigned)(want < most ? want : most > 0 ? most : 1), (unsigned)groups);
 }
 
 }  // namespace
@@ -281,9 +311,8 @@ cudaError_t prepare_few()
 
 int launch_few(som_layers* l, FewArgs a, int groups, bool gated, cudaStream_t st)
 {
-    a.share = share_of(l, (int64_t)a.F * groups, (int64_t)a.D);
-    const int features = FEW_WARPS / a.share;
-    const dim3 grid((unsigned)((a.F + features - 1) / features), (unsigned)groups);
+    a.share = share_of(l, (int64_t)a.F * groups, (int64_t)a.D, gated ? 1024 : 2048);
+    const dim3 grid = few_grid(l, a.F, FEW_WARPS / a.share, groups);
     const cudaError_t e = gated ? go<2>(a, grid, (size_t)a.D * 2, st) : go<1>(a, grid, (size_t)a.D * 2, st);
     ++l->launches;
     if (e == cudaSuccess) return SOM_OK;
@@ -293,12 +322,19 @@ int launch_few(som_layers* l, FewArgs a, int groups, bool gated, cudaStream_t st
 
 int launch_few_down(som_layers* l, FewDownArgs a, int64_t T, cudaStream_t st)
 {
-    a.share = share_of(l, a.D * T, (int64_t)a.k * a.I);
-    const int outputs = FEW_WARPS / a.share;
-    const dim3 grid((unsigned)((a.D + outputs - 1) / outputs), (unsigned)T);
-    k_few_down<<<grid, FEW_THREADS, (size_t)a.k * a.I * sizeof(float), st>>>(a);
+    a.share = share_of(l, a.D * T, (int64_t)a.k * a.I, 2048);
+    cudaLaunchConfig_t c = {};
+    c.gridDim = few_grid(l, a.D, FEW_WARPS / a.share, T);
+    c.blockDim = dim3(FEW_THREADS);
+    c.dynamicSmemBytes = (size_t)a.k * a.I * sizeof(float);
+    c.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    c.attrs = attr;
+    c.numAttrs = 1;
+    const cudaError_t e = cudaLaunchKernelEx(&c, k_few_down, a);
     ++l->launches;
-    const cudaError_t e = cudaGetLastError();
     if (e == cudaSuccess) return SOM_OK;
     l->last_cuda_error = (int)e;
     return SOM_ERR_CUDA;
