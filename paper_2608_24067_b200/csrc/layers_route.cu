@@ -406,6 +406,267 @@ __global__ void __launch_bounds__(32 * ROUTE_WARPS, V <= 8 ? 4 : 2) k_route(cons
     }
 }
 
+// ---- many tokens ----------------------------------------------------------------------------------------------
+//
+// Four lanes a token, eight tokens a warp: the rounds of the warp-wide choice cost the same instructions for one token as
+// this form spends on eight.  A lane takes the row's experts in pieces of eight (its eight of every 32), sorts a piece and
+// merges it into its list of the L largest keys; two exchanges make the four lanes' lists one.  The largest key that fell out
+// is kept for the certificate.  With groups the first walk finds the groups' keys and the second one walks only the chosen
+// groups.  Tokens that the certificate cannot settle are done by the whole warp from exact keys, as above.
+
+// a (descending) becomes the L largest of a and b (descending), descending; `rest`: the largest of those left out
+template <int L>
+__device__ __forceinline__ void merge_down(uint32_t (&a)[L], const uint32_t (&b)[L], uint32_t& rest)
+{
+#pragma unroll
+    for (int i = 0; i < L; ++i) {
+        rest = max(rest, min(a[i], b[L - 1 - i]));
+        a[i] = max(a[i], b[L - 1 - i]);
+    }
+#pragma unroll
+    for (int h = L / 2; h >= 1; h >>= 1)
+#pragma unroll
+        for (int i = 0; i < L; ++i)
+            if (!(i & h)) order2(a[i], a[i + h]);
+}
+
+constexpr int ROUTE_MANY = 1024;  // tokens from which on k_route_many is used
+constexpr int QUAD_WARPS = 8, QUAD_ROWS = 8 * QUAD_WARPS;
+
+template <int TYPE, int L, int V>
+__global__ void __launch_bounds__(32 * QUAD_WARPS) k_route_many(const RouteArgs a)
+{
+    extern __shared__ int hist[];  // [E] when counts are wanted
+    __shared__ uint32_t group_keys[QUAD_ROWS][33];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, quad = lane >> 2, part = lane & 3;
+    if (a.counts) {
+        for (int i = threadIdx.x; i < a.E; i += 32 * QUAD_WARPS) hist[i] = 0;
+        __syncthreads();
+    }
+    const bool whole = whole_rows<TYPE, 8>(a.logits, a.ld) && (reinterpret_cast<uintptr_t>(a.bias) & 15u) == 0;
+    const bool by_groups = a.groups > 1 && a.top_groups < a.groups;
+    const bool by_score = a.bias || (a.groups > 1 && a.group_best == 2);
+    const bool exact16 = TYPE != SOM_F32 && !by_score;
+    const int pieces = (a.E + 31) / 32, size = a.E / a.groups, per_group = size / 32;
+    float ceiling = 0.f, scale = (float)KEY_MOST / 64.f;
+    uint32_t margin = 3;
+    if (a.bias) {
+        float high = 0.f, low = 0.f;
+        for (int i = lane; i < a.E; i += 32) {
+            const float b = __ldg(a.bias + i);
+            high = fmaxf(high, b);
+            low = fminf(low, b);
+        }
+#pragma unroll
+        for (int d = 16; d > 0; d >>= 1) {
+            high = fmaxf(high, __shfl_xor_sync(ALL, high, d));
+            low = fminf(low, __shfl_xor_sync(ALL, low, d));
+        }
+        ceiling = 1.f + high;
+        scale = (float)KEY_MOST / (ceiling - low);
+        margin = 3 + (uint32_t)(scale * 0x1p-18f * (1.f + fmaxf(ceiling, -low)));
+    } else if (by_score) {
+        ceiling = 1.f;
+        scale = (float)KEY_MOST;
+        margin = 3 + (uint32_t)(scale * 0x1p-17f);
+    }
+    const bool packs = scale > 16.f;
+
+    for (int64_t t0 = ((int64_t)blockIdx.x * QUAD_WARPS + warp) * 8; t0 < a.T; t0 += (int64_t)gridDim.x * QUAD_ROWS) {
+        const int64_t t = t0 + quad < a.T ? t0 + quad : a.T - 1, row = t * a.ld;  // (past the end: the last row again, not written)
+        float top = 0.f, total = 1.f;
+        if (a.score == SOM_SCORE_SOFTMAX ? by_score || !a.renorm || !exact16 || by_groups : !by_score && !exact16) {
+            top = -INFINITY;
+            for (int b = 0; b < pieces; ++b) {
+                float x[8];
+                load_row<TYPE, 8>(a.logits, row, b * 32 + part * 8, a.E, whole, x);
+#pragma unroll
+                for (int v = 0; v < 8; ++v) top = fmaxf(top, x[v]);
+            }
+            top = fmaxf(top, __shfl_xor_sync(ALL, top, 1));
+            top = fmaxf(top, __shfl_xor_sync(ALL, top, 2));
+            if (!(top > -INFINITY)) top = 0.f;
+        }
+        if (a.score == SOM_SCORE_SOFTMAX && (by_score || !a.renorm)) {
+            total = 0.f;
+            for (int b = 0; b < pieces; ++b) {
+                float x[8];
+                load_row<TYPE, 8>(a.logits, row, b * 32 + part * 8, a.E, whole, x);
+#pragma unroll
+                for (int v = 0; v < 8; ++v) total += x[v] > -INFINITY ? exp_from(x[v], top) : 0.f;
+            }
+            total += __shfl_xor_sync(ALL, total, 1);
+            total += __shfl_xor_sync(ALL, total, 2);
+        }
+        bool sure = packs && top < INFINITY;
+        auto keys_of = [&](int piece, uint32_t (&key)[8]) {
+            const int at = piece * 32 + part * 8;
+            float x[8];
+            load_row<TYPE, 8>(a.logits, row, at, a.E, whole, x);
+            if (exact16) {
+#pragma unroll
+                for (int v = 0; v < 8; ++v) key[v] = x[v] > -INFINITY ? ordered16<TYPE>(x[v] + 0.f) << 16 | (INDEX_MASK - at - v) : 0u;
+                return;
+            }
+            float bias[8];
+#pragma unroll
+            for (int v = 0; v < 8; ++v) bias[v] = 0.f;
+            if (a.bias) load_row<SOM_F32, 8>(a.bias, 0, at, a.E, whole, bias);
+#pragma unroll
+            for (int v = 0; v < 8; ++v) {
+                float d;
+                if (!by_score) d = top - x[v];
+                else if (a.score == SOM_SCORE_SOFTMAX) d = ceiling - (__fdividef(exp_from(x[v], top), total) + bias[v]);
+                else d = ceiling - (__fdividef(1.f, 1.f + __expf(-x[v])) + bias[v]);
+                const uint32_t u = KEY_MOST - min((uint32_t)(d * scale), KEY_MOST - 1u);
+                key[v] = x[v] > -INFINITY && d == d ? u << INDEX_BITS | (INDEX_MASK - at - v) : 0u;
+            }
+        };
+        unsigned kept = 0;
+        if (by_groups) {
+            uint32_t* mine = group_keys[warp * 8 + quad];
+            bool lone = false;
+            for (int g = 0; g < a.groups; ++g) {
+                uint32_t m1 = 0, m2 = 0;
+                for (int b = 0; b < per_group; ++b) {
+                    uint32_t key[8];
+                    keys_of(g * per_group + b, key);
+#pragma unroll
+                    for (int v = 0; v < 8; ++v) {
+                        m2 = max(m2, min(m1, key[v]));
+                        m1 = max(m1, key[v]);
+                    }
+                }
+#pragma unroll
+                for (int d = 1; d <= 2; d <<= 1) {
+                    const uint32_t o1 = __shfl_xor_sync(ALL, m1, d), o2 = __shfl_xor_sync(ALL, m2, d);
+                    merge2(m1, m2, o1, o2);
+                }
+                lone |= m1 && !m2;  // a lone expert's distance is not comparable with the sum of two
+                if (part == 0) mine[g] = a.group_best == 2 ? (m1 >> INDEX_BITS) + (m2 >> INDEX_BITS) : m1;
+            }
+            if (a.group_best == 2 && lone) sure = false;
+            __syncwarp();
+            uint32_t low = 0xffffffffu, next = 0u;  // of the groups kept and of the others, this lane's quarter
+            for (int g = part; g < a.groups; g += 4) {
+                const uint32_t k = mine[g];
+                int rank = 0;
+                for (int o = 0; o < a.groups; ++o) rank += mine[o] > k || (mine[o] == k && o < g);
+                if (rank < a.top_groups) {
+                    kept |= 1u << g;
+                    low = min(low, k);
+                } else {
+                    next = max(next, k);
+                }
+            }
+#pragma unroll
+            for (int d = 1; d <= 2; d <<= 1) {
+                kept |= __shfl_xor_sync(ALL, kept, d);
+                low = min(low, __shfl_xor_sync(ALL, low, d));
+                next = max(next, __shfl_xor_sync(ALL, next, d));
+            }
+            __syncwarp();  // the keys have been read: the next token may write its own
+            if (!exact16 && low && next) {
+                if (a.group_best == 2) sure = sure && low - next >= 2 * margin;
+                else sure = sure && (low >> INDEX_BITS) - (next >> INDEX_BITS) >= margin;
+            }
+        }
+        uint32_t list[L], rest = 0;
+#pragma unroll
+        for (int i = 0; i < L; ++i) list[i] = 0u;
+        const int walk = by_groups ? a.top_groups * per_group : pieces;
+        unsigned left = kept;
+        int within = 0;
+        for (int b = 0; b < walk; ++b) {
+            int piece = b;
+            if (by_groups) {  // (each token walks its own groups)
+                piece = (__ffs(left) - 1) * per_group + within;
+                if (++within == per_group) within = 0, left &= left - 1;
+            }
+            uint32_t key[8], more[L];
+            keys_of(piece, key);
+            sort_down<8>(key);
+#pragma unroll
+            for (int i = 0; i < L; ++i) more[i] = i < 8 ? key[i] : 0u;
+            merge_down<L>(list, more, rest);
+        }
+#pragma unroll
+        for (int d = 1; d <= 2; d <<= 1) {
+            uint32_t more[L];
+#pragma unroll
+            for (int i = 0; i < L; ++i) more[i] = __shfl_xor_sync(ALL, list[i], d);
+            rest = max(rest, __shfl_xor_sync(ALL, rest, d));
+            merge_down<L>(list, more, rest);
+        }
+        if (!exact16) {
+#pragma unroll
+            for (int i = 0; i < L; ++i) {
+                const uint32_t next = i + 1 < L ? list[i + 1 < L ? i + 1 : i] : rest;
+                if (i < a.k && list[i])
+                    sure = sure && (list[i] >> INDEX_BITS) > 1u && (!next || (list[i] >> INDEX_BITS) - (next >> INDEX_BITS) >= margin);
+            }
+        }
+        int at[L];
+#pragma unroll
+        for (int i = 0; i < L; ++i) at[i] = i < a.k && list[i] ? (int)(INDEX_MASK - (list[i] & INDEX_MASK)) : -1;
+        unsigned redo = __ballot_sync(ALL, !sure && part == 0 && t0 + quad < a.T);
+        while (redo) {
+            const int who = __ffs(redo) - 1;
+            redo &= redo - 1;
+            const int64_t its_row = (t0 + (who >> 2)) * a.ld;
+            const int got = choose_exact<TYPE, V>(a, its_row, __shfl_sync(ALL, top, who), by_score, by_groups, lane);
+#pragma unroll
+            for (int i = 0; i < L; ++i) {
+                const int v = __shfl_sync(ALL, got, i);
+                if (quad == who >> 2) at[i] = i < a.k ? v : -1;
+            }
+        }
+        // lane `part` writes choices part, part + 4, ...
+        float s[L / 4], x[L / 4], most = -INFINITY;
+        int mine[L / 4];
+#pragma unroll
+        for (int i = 0; i < L; ++i)
+            if ((i & 3) == part) mine[i >> 2] = at[i];
+#pragma unroll
+        for (int i = 0; i < L / 4; ++i) {
+            x[i] = mine[i] >= 0 ? logit_at<TYPE>(a.logits, row + mine[i]) : -INFINITY;
+            most = fmaxf(most, x[i]);
+        }
+        most = fmaxf(most, __shfl_xor_sync(ALL, most, 1));
+        most = fmaxf(most, __shfl_xor_sync(ALL, most, 2));
+        float sum = 0.f;
+#pragma unroll
+        for (int i = 0; i < L / 4; ++i) {
+            s[i] = 0.f;
+            if (mine[i] >= 0) {
+                if (a.score == SOM_SCORE_SIGMOID) s[i] = 1.f / (1.f + expf(-x[i]));
+                else if (!a.renorm) s[i] = exp_from(x[i], top) / total;
+                else if (most == top || top < INFINITY) s[i] = exp_from(x[i], most);  // only ratios count
+            }
+            sum += s[i];
+        }
+        sum += __shfl_xor_sync(ALL, sum, 1);
+        sum += __shfl_xor_sync(ALL, sum, 2);
+        if (t0 + quad < a.T) {
+#pragma unroll
+            for (int i = 0; i < L / 4; ++i) {
+                const int j = 4 * i + part;
+                if (j < a.k) {
+                    const float v = a.renorm ? (sum > 0.f ? s[i] / sum : 0.f) : s[i];
+                    a.weights[t * a.k + j] = v * a.scale;
+                    a.indices[t * a.k + j] = mine[i];
+                    if (a.counts && mine[i] >= 0) atomicAdd(&hist[mine[i]], 1);
+                }
+            }
+        }
+    }
+    if (a.counts) {
+        __syncthreads();
+        for (int i = threadIdx.x; i < a.E; i += 32 * QUAD_WARPS)
+            if (hist[i]) atomicAdd(&a.counts[i], hist[i]);
+    }
+}
+
 struct RouteGradArgs {
     const void* logits;
     int64_t ld, T;
@@ -561,6 +822,20 @@ int route_grid(const som_layers* l, int64_t T, int per_sm)
 
 }  // namespace
 
+template <int TYPE, int L>
+cudaError_t go_many(const RouteArgs& a, int grid, size_t smem, cudaStream_t st)
+{
+    if (a.E <= 256) k_route_many<TYPE, L, 8><<<grid, 32 * QUAD_WARPS, smem, st>>>(a);
+    else k_route_many<TYPE, L, 32><<<grid, 32 * QUAD_WARPS, smem, st>>>(a);
+    return cudaGetLastError();
+}
+
+template <int TYPE>
+cudaError_t route_many(const RouteArgs& a, int grid, size_t smem, cudaStream_t st)
+{
+    return a.k <= 8 ? go_many<TYPE, 8>(a, grid, smem, st) : go_many<TYPE, 16>(a, grid, smem, st);
+}
+
 int launch_route(som_layers* l, int type, int score, int64_t T, int E, int k, const void* logits, int64_t ld, const float* bias,
                  int groups, int top_groups, int group_best, int renorm, float scale, float* weights, int32_t* indices,
                  int32_t* counts, cudaStream_t st)
@@ -570,7 +845,18 @@ int launch_route(som_layers* l, int type, int score, int64_t T, int E, int k, co
     if (counts && grid != 1) e = cudaMemsetAsync(counts, 0, (size_t)E * sizeof(int32_t), st);  // one block writes its counts itself
     if (e == cudaSuccess && grid) {
         const RouteArgs a{logits, ld, T, bias, weights, indices, counts, E, k, score, groups, top_groups, group_best, renorm, scale};
-        e = by_type<Route>(type, E, a, grid, counts ? (size_t)E * sizeof(int) : 0, st);
+        const size_t smem = counts ? (size_t)E * sizeof(int) : 0;
+        const bool by_groups = groups > 1 && top_groups < groups;
+        // Four lanes a token from ROUTE_MANY tokens on, where they fill the SMs.  Not where pieces of 32 experts span groups, and
+        // not where scores of 16-bit logits without a bias decide: equal logits are common there, and only the other form
+        // settles them without exact keys.
+        if (T >= ROUTE_MANY && k <= 16 && (!by_groups || E / groups % 32 == 0) && (type == SOM_F32 || bias || groups == 1 || group_best == 1)) {
+            const int64_t want = (T + QUAD_ROWS - 1) / QUAD_ROWS, most = (int64_t)l->sm_count * 4;
+            const int blocks = (int)(want < most ? want : most);
+            e = type == SOM_F32 ? route_many<SOM_F32>(a, blocks, smem, st) : type == SOM_F16 ? route_many<SOM_F16>(a, blocks, smem, st) : route_many<SOM_BF16>(a, blocks, smem, st);
+        } else {
+            e = by_type<Route>(type, E, a, grid, smem, st);
+        }
         ++l->launches;
     }
     return done(l, e);

@@ -192,6 +192,36 @@ def test_route(L, T, E, k, opt, dtype, kind):
     assert all(torch.equal(got[n], again[n]) for n in got)
 
 
+@pytest.mark.parametrize("E,k,opt", [
+    (64, 8, dict(score="softmax", renorm=True)), (100, 6, dict(score="softmax", renorm=False)), (8, 8, dict(score="sigmoid", renorm=True)),
+    (256, 8, dict(score="sigmoid", renorm=True, bias=True, groups=8, top_groups=4, group_best=2)), (300, 16, dict(score="softmax", renorm=True, bias=True)),
+    (128, 12, dict(score="softmax", renorm=True, groups=4, top_groups=2)), (1024, 9, dict(score="sigmoid", renorm=False, bias=True, groups=32, top_groups=3, group_best=1)),
+    (36, 2, dict(score="sigmoid", renorm=True, groups=2, top_groups=1)), (64, 20, dict(score="softmax", renorm=True)), (1, 1, dict(score="softmax", renorm=True))])
+@pytest.mark.parametrize("dtype,kind", [(FP32, "normal"), (BF16, "normal"), (FP16, "masked"), (FP32, "ties")])
+def test_route_many_tokens(L, E, k, opt, dtype, kind):
+    """Many tokens take another form of the kernel: the choice is that of the same tokens a few at a time, and of the definition."""
+    T = 1301
+    gen = torch.Generator().manual_seed(E + k)
+    z = torch.randn(T, E, generator=gen) * 2
+    if kind == "ties":
+        z = (z * 2).round() / 2
+    if kind == "masked":
+        z[torch.rand(z.shape, generator=gen) < 0.3] = -math.inf
+        z[::7] = -math.inf
+    logits = z.to(dtype).cuda()
+    bias = (torch.randn(E, generator=gen) * 0.1).cuda() if opt.get("bias") else None
+    got = L.route(logits, k, bias=bias, **{n: v for n, v in opt.items() if n != "bias"})
+    at = torch.cat([L.route(logits[i:i + 200], k, bias=bias, **{n: v for n, v in opt.items() if n != "bias"})["indices"] for i in range(0, T, 200)])
+    assert torch.equal(got["indices"], at)
+    assert torch.equal(got["counts"].long(), torch.bincount(at[at >= 0].long(), minlength=E))
+    some = torch.arange(3, T, 61)
+    _, (w, want, _, _) = _route(logits[some], k, opt, bias)
+    assert torch.equal(got["indices"][some].cpu().long(), want)
+    assert ((got["weights"][some].double().cpu() - w).abs() <= (E + 16) * 2.0 ** -24 * w.abs() + 1e-37).all()
+    again = L.route(logits, k, bias=bias, **{n: v for n, v in opt.items() if n != "bias"})
+    assert all(torch.equal(got[n], again[n]) for n in got)
+
+
 def test_route_order_of_near_scores(L):
     """Scores that differ by less than one fp32 exponential's error are ordered as their fp32 roundings from 64 bits are."""
     gen = torch.Generator().manual_seed(0)
