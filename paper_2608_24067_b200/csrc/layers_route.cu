@@ -49,7 +49,6 @@ __device__ __forceinline__ double warp_sum(double v)
 // exp(x - top), with the limit 1 where both are infinite
 __device__ __forceinline__ float exp_from(float x, float top) { return x == top ? 1.f : expf(x - top); }
 
-__device__ __forceinline__ double exp64(float x, float top) { return x == top ? 1.0 : exp((double)x - (double)top); }
 
 struct RouteArgs {
     const void* logits;
@@ -119,77 +118,83 @@ __device__ __forceinline__ uint32_t group_key(uint32_t b1, uint32_t b2, int best
     return s == s ? som_ordered_bits(s + 0.f) : 0u;
 }
 
-// The choice from exact keys: lane j returns the j-th.  Reads the row again: the common path's registers stay its own.
-template <int TYPE, int V>
+// The choice from exact keys: lane j returns the j-th.  Rare, so what it costs is fetching its code: loops, nothing unrolled,
+// the keys in local memory.  (Unrolled, it added 17 us to 20 us for 16384 tokens of which one in a hundred came here.)
+template <int TYPE>
 __device__ __noinline__ int choose_exact(const RouteArgs& a, int64_t row, float top, bool by_score, bool by_groups, int lane)
 {
-    const int first = lane * V;
-    uint32_t key[V];  // 0 = masked out or taken
+    const int n = (a.E + 31) / 32, first = lane * n;
+    uint32_t key[32];  // 0 = masked out or taken
     double sum = 1.0;
-    if (by_score && a.score == SOM_SCORE_SOFTMAX) {
-        sum = 0.0;
-#pragma unroll 4
-        for (int v = 0; v < V; ++v) {
+#pragma unroll 1
+    for (int pass = by_score && a.score == SOM_SCORE_SOFTMAX ? 0 : 1; pass < 2; ++pass) {  // the scores' sum, the keys
+        if (pass == 0) sum = 0.0;
+#pragma unroll 1
+        for (int v = 0; v < n; ++v) {
             const float x = first + v < a.E ? logit_at<TYPE>(a.logits, row + first + v) : -INFINITY;
-            sum += x > -INFINITY ? exp64(x, top) : 0.0;
+            const bool live = x > -INFINITY;
+            float s = x;
+            if (by_score) {
+                const bool soft = a.score == SOM_SCORE_SOFTMAX;
+                const double e = soft && x == top ? 1.0 : exp(soft ? (double)x - (double)top : -(double)x);
+                if (pass == 0) {
+                    if (live) sum += e;
+                    continue;
+                }
+                s = (float)((soft ? e : 1.0) / (soft ? sum : 1.0 + e));
+                if (a.bias && first + v < a.E) s += __ldg(a.bias + first + v);
+            }
+            key[v] = live && s == s ? som_ordered_bits(s + 0.f) : 0u;  // + 0: the two zeros tie
         }
-        sum = warp_sum(sum);
-    }
-#pragma unroll
-    for (int v = 0; v < V; ++v) {
-        const float x = first + v < a.E ? logit_at<TYPE>(a.logits, row + first + v) : -INFINITY;
-        float s = x;
-        if (by_score) {
-            s = a.score == SOM_SCORE_SOFTMAX ? (float)(exp64(x, top) / sum) : (float)(1.0 / (1.0 + exp(-(double)x)));
-            if (a.bias && first + v < a.E) s += __ldg(a.bias + first + v);
-        }
-        key[v] = x > -INFINITY && s == s ? som_ordered_bits(s + 0.f) : 0u;  // + 0: the two zeros tie
+        if (pass == 0) sum = warp_sum(sum);
     }
     if (by_groups) {
         const int size = a.E / a.groups;
         uint32_t mine = 0;  // lane g: key of group g
+#pragma unroll 1
         for (int g = 0; g < a.groups; ++g) {
             uint32_t m1 = 0, m2 = 0;
-#pragma unroll
-            for (int v = 0; v < V; ++v) {
-                const int i = first + v - g * size;
-                if (i >= 0 && i < size) merge2(m1, m2, key[v], 0u);
-            }
+#pragma unroll 1
+            for (int v = max(0, g * size - first); v < min(n, (g + 1) * size - first); ++v) merge2(m1, m2, key[v], 0u);
             const uint32_t b1 = __reduce_max_sync(ALL, m1);
             const int owner = __ffs(__ballot_sync(ALL, m1 == b1)) - 1;
             const uint32_t b2 = __reduce_max_sync(ALL, lane == owner ? m2 : m1);
             if (lane == g) mine = group_key(b1, b2, a.group_best);
         }
         int rank = 0;
+#pragma unroll 1
         for (int g = 0; g < a.groups; ++g) {
             const uint32_t other = __shfl_sync(ALL, mine, g);
             rank += other > mine || (other == mine && g < lane);
         }
         const unsigned kept = __ballot_sync(ALL, lane < a.groups && rank < a.top_groups);
-#pragma unroll
-        for (int v = 0; v < V; ++v)
+#pragma unroll 1
+        for (int v = 0; v < n; ++v)
             if (!((kept >> min((first + v) / size, 31)) & 1u)) key[v] = 0u;
     }
     int at = -1;
+#pragma unroll 1
     for (int j = 0; j < a.k; ++j) {
         uint32_t best = 0;
         int bv = 0;
-#pragma unroll
-        for (int v = 0; v < V; ++v)
+#pragma unroll 1
+        for (int v = 0; v < n; ++v)
             if (key[v] > best) best = key[v], bv = v;
         const uint32_t m = __reduce_max_sync(ALL, best);
         if (m == 0) break;
         const int owner = __ffs(__ballot_sync(ALL, best == m)) - 1;  // the lowest lane holds the lowest index
-        const int i = owner * V + __shfl_sync(ALL, bv, owner);
+        const int i = owner * n + __shfl_sync(ALL, bv, owner);
         if (lane == j) at = i;
-        if (lane == owner) {
-#pragma unroll
-            for (int v = 0; v < V; ++v)
-                if (v == bv) key[v] = 0u;
-        }
+        if (lane == owner) key[bv] = 0u;
     }
     return at;
 }
+
+// Errors of two fp32 keys together, per unit of 1 + |bias|.  Sigmoid: 2^-22 of the exponential times s (1 - s), 2^-22.5 of the
+// division, 2^-24 each for the bias and for the exact key's own two roundings: below 2^-21 a key.  Softmax: the sum of up
+// to 1024 exponentials (37 additions in a row at most) and the exponential are off by 2^-18.5 of a score, and the scores of two
+// experts are at most 1 together.
+__device__ __forceinline__ float key_errors(int score) { return score == SOM_SCORE_SOFTMAX ? 0x1p-18f : 0x1p-20f; }
 
 constexpr int KEY_BITS = 22, INDEX_BITS = 10;
 constexpr uint32_t KEY_MOST = (1u << KEY_BITS) - 1u, INDEX_MASK = (1u << INDEX_BITS) - 1u;
@@ -260,7 +265,7 @@ __global__ void __launch_bounds__(32 * ROUTE_WARPS, V <= 8 ? 4 : 2) k_route(cons
     }
     // packed keys: scores lie in [low, 1 + high]; logits up to 64 below the row's largest are told apart
     float ceiling = 0.f, scale = (float)KEY_MOST / 64.f;
-    uint32_t margin = 3;  // key units: rounding of the distances (and the scores' errors, 2^-18 for two of them)
+    uint32_t margin = 3;  // key units: rounding of the distances (and the scores' errors)
     if (by_score) {
 #pragma unroll
         for (int d = 16; d > 0; d >>= 1) {
@@ -269,7 +274,7 @@ __global__ void __launch_bounds__(32 * ROUTE_WARPS, V <= 8 ? 4 : 2) k_route(cons
         }
         ceiling = 1.f + high;
         scale = (float)KEY_MOST / (ceiling - low);
-        margin = 3 + (uint32_t)(scale * 0x1p-18f * (1.f + fmaxf(ceiling, -low)));
+        margin = 3 + (uint32_t)(scale * key_errors(a.score) * fmaxf(ceiling, 1.f - low));
     }
     const bool packs = (!by_groups || lanes) && a.k < 32 && scale > 16.f;  // (not with huge or infinite biases)
 
@@ -373,7 +378,7 @@ __global__ void __launch_bounds__(32 * ROUTE_WARPS, V <= 8 ? 4 : 2) k_route(cons
                 if (lane >= a.k) at = -1;
             }
         }
-        if (!sure) at = choose_exact<TYPE, V>(a, row, top, by_score, by_groups, lane);
+        if (!sure) at = choose_exact<TYPE>(a, row, top, by_score, by_groups, lane);
         float s = 0.f;
         const float xj = at >= 0 ? logit_at<TYPE>(a.logits, row + at) : -INFINITY;
         if (a.score == SOM_SCORE_SIGMOID) {
@@ -433,7 +438,7 @@ __device__ __forceinline__ void merge_down(uint32_t (&a)[L], const uint32_t (&b)
 constexpr int ROUTE_MANY = 1024;  // tokens from which on k_route_many is used
 constexpr int QUAD_WARPS = 8, QUAD_ROWS = 8 * QUAD_WARPS;
 
-template <int TYPE, int L, int V>
+template <int TYPE, int L>
 __global__ void __launch_bounds__(32 * QUAD_WARPS) k_route_many(const RouteArgs a)
 {
     extern __shared__ int hist[];  // [E] when counts are wanted
@@ -464,11 +469,11 @@ __global__ void __launch_bounds__(32 * QUAD_WARPS) k_route_many(const RouteArgs 
         }
         ceiling = 1.f + high;
         scale = (float)KEY_MOST / (ceiling - low);
-        margin = 3 + (uint32_t)(scale * 0x1p-18f * (1.f + fmaxf(ceiling, -low)));
+        margin = 3 + (uint32_t)(scale * key_errors(a.score) * fmaxf(ceiling, 1.f - low));
     } else if (by_score) {
         ceiling = 1.f;
         scale = (float)KEY_MOST;
-        margin = 3 + (uint32_t)(scale * 0x1p-17f);
+        margin = 3 + (uint32_t)(scale * key_errors(a.score));
     }
     const bool packs = scale > 16.f;
 
@@ -493,7 +498,8 @@ __global__ void __launch_bounds__(32 * QUAD_WARPS) k_route_many(const RouteArgs 
                 float x[8];
                 load_row<TYPE, 8>(a.logits, row, b * 32 + part * 8, a.E, whole, x);
 #pragma unroll
-                for (int v = 0; v < 8; ++v) total += x[v] > -INFINITY ? exp_from(x[v], top) : 0.f;
+                for (int v = 0; v < 8; ++v) x[v] = x[v] > -INFINITY ? exp_from(x[v], top) : 0.f;
+                total += ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
             }
             total += __shfl_xor_sync(ALL, total, 1);
             total += __shfl_xor_sync(ALL, total, 2);
@@ -614,7 +620,7 @@ __global__ void __launch_bounds__(32 * QUAD_WARPS) k_route_many(const RouteArgs 
             const int who = __ffs(redo) - 1;
             redo &= redo - 1;
             const int64_t its_row = (t0 + (who >> 2)) * a.ld;
-            const int got = choose_exact<TYPE, V>(a, its_row, __shfl_sync(ALL, top, who), by_score, by_groups, lane);
+            const int got = choose_exact<TYPE>(a, its_row, __shfl_sync(ALL, top, who), by_score, by_groups, lane);
 #pragma unroll
             for (int i = 0; i < L; ++i) {
                 const int v = __shfl_sync(ALL, got, i);
@@ -825,8 +831,7 @@ int route_grid(const som_layers* l, int64_t T, int per_sm)
 template <int TYPE, int L>
 cudaError_t go_many(const RouteArgs& a, int grid, size_t smem, cudaStream_t st)
 {
-    if (a.E <= 256) k_route_many<TYPE, L, 8><<<grid, 32 * QUAD_WARPS, smem, st>>>(a);
-    else k_route_many<TYPE, L, 32><<<grid, 32 * QUAD_WARPS, smem, st>>>(a);
+    k_route_many<TYPE, L><<<grid, 32 * QUAD_WARPS, smem, st>>>(a);
     return cudaGetLastError();
 }
 
