@@ -8,20 +8,19 @@
 namespace lay {
 
 int make_map(som_layers* l, CUtensorMap* map, const void* base, int bytes, int64_t cols, int64_t rows, int64_t batch, int64_t ld,
-             int64_t batch_stride, int box_cols, int box_rows)
+             int64_t batch_stride, int box_bytes, int box_rows)
 {
     using Encode = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
                                 const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
                                 CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
     const cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)batch};
     const cuuint64_t strides[2] = {(cuuint64_t)(ld * bytes), (cuuint64_t)(batch_stride * bytes)};
-    const cuuint32_t box[3] = {(cuuint32_t)box_cols, (cuuint32_t)box_rows, 1u};
+    const cuuint32_t box[3] = {(cuuint32_t)(box_bytes / bytes), (cuuint32_t)box_rows, 1u};
     const cuuint32_t step[3] = {1u, 1u, 1u};
     const CUresult r = reinterpret_cast<Encode>(l->encode)(
         map, bytes == 4 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims,
-        strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
-        box_cols * bytes == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-        CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+        strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, box_bytes == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B,
+        CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     if (r == CUDA_SUCCESS) return SOM_OK;
     l->last_cuda_error = (int)cudaErrorInvalidValue;
     return SOM_ERR_CUDA;
@@ -112,15 +111,15 @@ int tiles_of(int64_t n, int64_t width) { return (int)((n + width - 1) / width); 
 // 16-bit operands of the products: the left one K-major in boxes of 128 rows; the right one, and M/N-major ones, of 64
 int map_left(som_layers* l, CUtensorMap* m, const void* p, int64_t cols, int64_t rows, int64_t ld)
 {
-    return make_map(l, m, p, 2, cols, rows, 1, ld, rows * ld, 64, 128);
+    return make_map(l, m, p, 2, cols, rows, 1, ld, rows * ld, 128, 128);
 }
 int map_64(som_layers* l, CUtensorMap* m, const void* p, int64_t cols, int64_t rows, int64_t ld, int64_t batch = 1)
 {
-    return make_map(l, m, p, 2, cols, rows, batch, ld, rows * ld, 64, 64);
+    return make_map(l, m, p, 2, cols, rows, batch, ld, rows * ld, 128, 64);
 }
 int map_out(som_layers* l, CUtensorMap* m, void* p, int bytes, int64_t cols, int64_t rows, int64_t ld, int64_t batch = 1)
 {
-    return make_map(l, m, p, bytes, cols, rows, batch, ld, rows * ld, 32, 32);
+    return make_map(l, m, p, bytes, cols, rows, batch, ld, rows * ld, 64, 32);
 }
 
 // The tiles of a product of `rows` x `cols` outputs (`batch` of them).  Pairs of blocks do twice a single block's work per
@@ -232,7 +231,7 @@ int som_linear(som_layers* l, int type, int act, int gated, int64_t T, int64_t D
     ProdArgs a = {};
     LAY_TRY(map_left(l, &a.a, x, D, T, ldx));
     LAY_TRY(map_64(l, &a.b, w, D, rows, D));
-    LAY_TRY(map_out(l, &a.o0, y, 2, F, T, ldy));
+    LAY_TRY(map_out(l, &a.o, y, 2, F, T, ldy));
     a.bias = static_cast<const uint16_t*>(bias);
     a.extra = static_cast<const uint16_t*>(residual);
     a.ld_extra = ldr;
@@ -290,8 +289,8 @@ int som_linear_backward(som_layers* l, int type, int act, int gated, int64_t T, 
         ProdArgs z = a;
         LAY_TRY(map_left(l, &z.a, x, D, T, ldx));
         LAY_TRY(map_64(l, &z.b, w, D, rows, D));
-        LAY_TRY(map_out(l, &z.o0, z_grad, 2, F, T, rows));
-        if (gated) LAY_TRY(map_out(l, &z.o1, z_grad + F, 2, F, T, rows));
+        z.o0 = z_grad;
+        z.ld0 = rows;
         z.bias = static_cast<const uint16_t*>(bias);
         z.extra = static_cast<const uint16_t*>(dy);
         z.ld_extra = lddy;
@@ -308,7 +307,7 @@ int som_linear_backward(som_layers* l, int type, int act, int gated, int64_t T, 
         ProdArgs p = a;
         LAY_TRY(map_left(l, &p.a, dz, rows, T, lddz));
         LAY_TRY(map_64(l, &p.b, w, D, rows, D));
-        LAY_TRY(map_out(l, &p.o0, dx, 2, D, T, D));
+        LAY_TRY(map_out(l, &p.o, dx, 2, D, T, D));
         set_tiles(l, &p, T, D, false);
         p.k1 = (int)rows;
         LAY_TRY(launch_product(l, PROD_DX, p, st));
@@ -317,7 +316,7 @@ int som_linear_backward(som_layers* l, int type, int act, int gated, int64_t T, 
         ProdArgs p = a;
         LAY_TRY(map_64(l, &p.a, dz, rows, T, lddz));
         LAY_TRY(map_64(l, &p.b, x, D, T, ldx));
-        LAY_TRY(map_out(l, &p.o0, dw, 2, D, rows, D));
+        LAY_TRY(map_out(l, &p.o, dw, 2, D, rows, D));
         set_tiles(l, &p, rows, D, false);
         p.k1 = (int)T;
         LAY_TRY(launch_product(l, PROD_DW, p, st));
@@ -486,7 +485,7 @@ int som_experts(som_layers* l, int type, int act, int gated, int64_t T, int32_t 
     ProdArgs a = grouped(l, p, type, I, gated);
     LAY_TRY(map_left(l, &a.a, xp, D, p.max_rows, D));
     LAY_TRY(map_64(l, &a.b, w1, D, rows1, D, E));
-    LAY_TRY(map_out(l, &a.o0, h, 2, I, p.max_rows, I));
+    LAY_TRY(map_out(l, &a.o, h, 2, I, p.max_rows, I));
     a.bias = static_cast<const uint16_t*>(b1);
     a.bias_ld = (int)rows1;
     a.gate_rows = gated ? (int)I : 0;
@@ -497,7 +496,7 @@ int som_experts(som_layers* l, int type, int act, int gated, int64_t T, int32_t 
     a = grouped(l, p, type, D, false);
     LAY_TRY(map_left(l, &a.a, h, I, p.max_rows, I));
     LAY_TRY(map_64(l, &a.b, w2, I, D, I, E));
-    LAY_TRY(map_out(l, &a.o0, part, 4, D, p.max_rows, D));
+    LAY_TRY(map_out(l, &a.o, part, 4, D, p.max_rows, D));
     a.bias = static_cast<const uint16_t*>(b2);
     a.bias_ld = (int)D;
     a.k1 = (int)I;
@@ -530,7 +529,7 @@ int som_experts_backward(som_layers* l, int type, int act, int gated, int64_t T,
     uint16_t *xp, *dyp, *h, *dz;
     float *part, *dot, *sums;
     const bool pair = pair_rows(T, E, k);
-    const int col_tiles = tiles_of(I, (pair ? PAIR_COLS : SINGLE_COLS) / (gated ? 2 : 1));
+    const int width = (pair ? PAIR_COLS : SINGLE_COLS) / 2, dots = tiles_of(I, width) * (width / 32);
     Carver c{nullptr, 0};
     for (int pass = 0; pass < 2; ++pass) {
         c.used = 0;
@@ -540,7 +539,7 @@ int som_experts_backward(som_layers* l, int type, int act, int gated, int64_t T,
         h = c.take<uint16_t>((int64_t)p.max_rows * I);
         dz = c.take<uint16_t>((int64_t)p.max_rows * rows1);
         part = c.take<float>((int64_t)p.max_rows * D);
-        dot = c.take<float>((int64_t)p.max_rows * 2 * col_tiles);
+        dot = c.take<float>((int64_t)p.max_rows * dots);
         sums = c.take<float>(db1 ? p.max_rows / 32 * rows1 : 0);
         if (pass == 0) {
             LAY_TRY(ensure(l, c.used));
@@ -549,31 +548,33 @@ int som_experts_backward(som_layers* l, int type, int act, int gated, int64_t T,
     }
     LAY_TRY(launch_plan(l, p, indices, weights, weights_type, T, k, E, st));
     LAY_TRY(launch_gather(l, p, k, D, x, ldx, xp, dy, lddy, dyp, st));
-    // z and g = W2^T dy side by side -> dz, the weighted h, partial sums of <h, g>
-    ProdArgs a = grouped(l, p, type, I, gated);
+    // z and g = W2^T dy side by side (half-width tiles) -> dz, the weighted h, partial sums of <h, g>
+    ProdArgs a = grouped(l, p, type, I, true);
     LAY_TRY(map_left(l, &a.a, xp, D, p.max_rows, D));
     LAY_TRY(map_64(l, &a.b, w1, D, rows1, D, E));
     LAY_TRY(map_left(l, &a.a2, dyp, D, p.max_rows, D));
     LAY_TRY(map_64(l, &a.b2, w2, I, D, I, E));
-    LAY_TRY(map_out(l, &a.o0, dz, 2, I, p.max_rows, rows1));
-    if (gated) LAY_TRY(map_out(l, &a.o1, dz + I, 2, I, p.max_rows, rows1));
-    LAY_TRY(map_out(l, &a.o2, h, 2, I, p.max_rows, I));
+    a.o0 = dz;
+    a.ld0 = rows1;
+    a.o2 = h;
+    a.ld2 = I;
     a.bias = static_cast<const uint16_t*>(b1);
     a.bias_ld = (int)rows1;
     a.dot = dot;
+    a.dots = dots;
     a.column_sums = db1 ? sums : nullptr;
     a.gate_rows = gated ? (int)I : 0;
     a.k1 = a.k2 = (int)D;
     a.act = act;
     LAY_TRY(launch_product(l, PROD_DZ_TWO, a, st));
-    LAY_TRY(launch_dweights(l, p, indices, T, k, D, dot, 2 * col_tiles, b2, dy, lddy, dweights, weights_type, a.bf16, st));
+    LAY_TRY(launch_dweights(l, p, indices, T, k, D, dot, dots, b2, dy, lddy, dweights, weights_type, a.bf16, st));
     if (db1) LAY_TRY(launch_join_sums(l, p, E, 0, sums, rows1, db1, a.bf16, st));
     if (db2) LAY_TRY(launch_column_sums(l, p, E, 0, dyp, D, D, db2, a.bf16, st));
     // dx
     a = grouped(l, p, type, D, false);
     LAY_TRY(map_left(l, &a.a, dz, rows1, p.max_rows, rows1));
     LAY_TRY(map_64(l, &a.b, w1, D, rows1, D, E));
-    LAY_TRY(map_out(l, &a.o0, part, 4, D, p.max_rows, D));
+    LAY_TRY(map_out(l, &a.o, part, 4, D, p.max_rows, D));
     a.k1 = (int)rows1;
     a.out32 = 1;
     LAY_TRY(launch_product(l, PROD_DX, a, st));
@@ -588,12 +589,12 @@ int som_experts_backward(som_layers* l, int type, int act, int gated, int64_t T,
     ProdArgs b = a;
     LAY_TRY(map_64(l, &a.a, dz, rows1, p.max_rows, rows1));
     LAY_TRY(map_64(l, &a.b, xp, D, p.max_rows, D));
-    LAY_TRY(map_out(l, &a.o0, dw1, 2, D, rows1, D, E));
+    LAY_TRY(map_out(l, &a.o, dw1, 2, D, rows1, D, E));
     set_tiles(l, &a, rows1, D, false, E);
     LAY_TRY(launch_product(l, PROD_DW, a, st));
     LAY_TRY(map_64(l, &b.a, dyp, D, p.max_rows, D));
     LAY_TRY(map_64(l, &b.b, h, I, p.max_rows, I));
-    LAY_TRY(map_out(l, &b.o0, dw2, 2, I, D, I, E));
+    LAY_TRY(map_out(l, &b.o, dw2, 2, I, D, I, E));
     set_tiles(l, &b, D, I, false, E);
     return launch_product(l, PROD_DW, b, st);
 }

@@ -40,22 +40,40 @@ __device__ __forceinline__ void load8(const uint16_t* p, float (&v)[8], int bf16
     v[0] = a.x, v[1] = a.y, v[2] = b.x, v[3] = b.y, v[4] = c.x, v[5] = c.y, v[6] = d.x, v[7] = d.y;
 }
 
-// P(N <= z), and exp(-z^2 / 2) that its computation needs: Abramowitz and Stegun 7.1.26 for 1 - erf(|z| / sqrt 2), off by
-// at most 1.5e-7, one exponential and one division for both.  erff and its branch took more time in the epilogues than the
-// products left for them (linear_backward of 4093 x 2048 x 4096 with gelu: first product 118 us with it, 72 us without).
+// one instruction each, subnormal results flushed to zero: 2^x off by 2 units, 1 / x by 1 unit in the last place
+__device__ __forceinline__ float fast_exp2(float x)
+{
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+__device__ __forceinline__ float fast_rcp(float x)
+{
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+// P(N <= z), and e = exp(-z^2 / 2) that its computation needs: Abramowitz and Stegun 7.1.26 for 1 - erf(|z| / sqrt 2), off by
+// at most 1.5e-7, one exponential and one reciprocal for both.  erff and its branch took more time in the epilogues than the
+// products left for them.
 __device__ __forceinline__ float normal_cdf(float z, float& e)
 {
-    const float t = __fdividef(1.f, fmaf(0.3275911f * 0.70710678f, fabsf(z), 1.f));
-    e = __expf(-0.5f * z * z);
-    const float q = t * fmaf(t, fmaf(t, fmaf(t, fmaf(t, 1.061405429f, -1.453152027f), 1.421413741f), -0.284496736f), 0.254829592f);
-    const float tail = 0.5f * q * e;  // P(N <= -|z|)
+    const float t = fast_rcp(fmaf(0.3275911f * 0.70710678f, fabsf(z), 1.f));
+    e = fast_exp2(z * (z * -0.72134752f));
+    // (the polynomial's coefficients halved)
+    const float q = t * fmaf(t, fmaf(t, fmaf(t, fmaf(t, 0.5307027145f, -0.7265760135f), 0.7107068705f), -0.142248368f), 0.127414796f);
+    const float tail = q * e;  // P(N <= -|z|)
     return z < 0.f ? tail : 1.f - tail;
 }
+
+__device__ __forceinline__ float sigmoid_of(float z) { return fast_rcp(1.f + fast_exp2(z * -1.44269504f)); }
 
 template <int ACT>
 __device__ __forceinline__ float act_of(float z)
 {
-    if (ACT == SOM_ACT_SILU) return __fdividef(z, 1.f + __expf(-z));
+    if (ACT == SOM_ACT_SILU) return z * sigmoid_of(z);
     if (ACT == SOM_ACT_GELU) {
         float e;
         return z * normal_cdf(z, e);
@@ -69,9 +87,9 @@ template <int ACT>
 __device__ __forceinline__ void act_both(float z, float& a, float& da)
 {
     if (ACT == SOM_ACT_SILU) {
-        const float s = __fdividef(1.f, 1.f + __expf(-z));
+        const float s = sigmoid_of(z);
         a = z * s;
-        da = s * fmaf(z, 1.f - s, 1.f);
+        da = fmaf(a, 1.f - s, s);
     } else if (ACT == SOM_ACT_GELU) {
         float e;
         const float c = normal_cdf(z, e);

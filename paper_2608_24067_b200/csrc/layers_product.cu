@@ -2,8 +2,11 @@
 //
 // Persistent blocks, one per SM, walk the output tiles.  Warp 0 issues the TMA copies of a six-stage ring (64 k of both
 // operands a stage, 32 KB, 128-byte swizzle), warp 1 issues the matrix instructions (tcgen05.mma, fp32 accumulators in
-// tensor memory), eight warps run the epilogue.  The accumulator is double-buffered, so that the epilogue of a tile runs
-// under the products of the next; PROD_DZ_TWO keeps two products of a tile side by side and has one buffer.  Operands enter
+// tensor memory), sixteen warps run the epilogue (with eight, two on a scheduler, the epilogues with an exponential
+// outlasted the products: 84 us against 56 for the first product of linear_backward at 4093 x 2048 x 4096, gelu).  The accumulator is double-buffered, so that the epilogue of a tile runs
+// under the products of the next.  PROD_DZ_TWO keeps two products of a tile side by side, z with one buffer and g with two: the
+// next tile's g is multiplied while the epilogue reads this tile's z and g (with one buffer for both the 206 GFLOP of 4096
+// tokens x 4 experts of 2048 x 1024 took 301 us).  Operands enter
 // K-major (a row holds consecutive k) or M/N-major (a row holds consecutive rows of the product), as they lie in memory: no
 // operand is transposed beforehand.  Every wait is bounded.
 //
@@ -23,8 +26,8 @@ constexpr int BM = 128, BK = 64, STAGES = 6;
 constexpr int HALF = 128 * BK * 2;  // bytes of a block's share of an operand in a stage
 constexpr int STAGE_BYTES = 2 * HALF;
 constexpr int BOX = 64 * 128;  // bytes of a box of 64 rows
-constexpr int EPI_WARPS = 8, THREADS = 32 * (2 + EPI_WARPS);
-constexpr int OUT_BYTES = 32 * 128;  // an epilogue warp's staged output: 32 rows of 128 bytes
+constexpr int EPI_WARPS = 16, THREADS = 32 * (2 + EPI_WARPS);
+constexpr int OUT_BYTES = 32 * 64;  // an epilogue warp's staged output: 32 rows of 64 bytes
 constexpr int SMEM = 1024 + STAGES * STAGE_BYTES + EPI_WARPS * OUT_BYTES;
 
 struct Tile {
@@ -74,80 +77,84 @@ __device__ __forceinline__ Tile tile_at(const ProdArgs& p, int idx, int width, i
     return t;
 }
 
-// An epilogue warp's way out: 32 rows (lane l holds row l) of 32 columns are staged in shared memory and stored by TMA,
-// which leaves out what lies outside the tensor.  16-bit pieces (64-byte rows, 64-byte swizzle) alternate between the
-// two halves of the buffer, so that a piece is staged while the one before is read; fp32 pieces (128-byte rows) fill it.
+// Ways out of the epilogue.  Staged: 32 rows (lane l holds row l) of 32 16-bit or 16 fp32 columns go through shared memory
+// (64-byte rows, 64-byte swizzle) to a TMA store, which leaves out what lies outside the tensor.  Direct: a lane writes its 16
+// columns.  Direct stores take the load/store pipe 32 cycles an instruction: too much where a tile's products are short
+// (PROD_DW at 512 rows an expert: 134 us staged, 178 us direct), but no waits, and no shared memory for up to three outputs
+// at once (PROD_DZ, PROD_DZ_TWO).
 struct Stager {
     unsigned char* buf;
-    int lane, turn;
-    __device__ __forceinline__ void put16(const CUtensorMap* map, const float (&v)[32], int col, int row, int batch, const ProdArgs& p)
-    {
-        unsigned char* to = buf + turn * (OUT_BYTES / 2);
-        turn ^= 1;
-        if (lane == 0) store_wait_read<1>();
-        __syncwarp();
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            uint4 u;
-            u.x = pack2(v[8 * j], v[8 * j + 1], p.bf16);
-            u.y = pack2(v[8 * j + 2], v[8 * j + 3], p.bf16);
-            u.z = pack2(v[8 * j + 4], v[8 * j + 5], p.bf16);
-            u.w = pack2(v[8 * j + 6], v[8 * j + 7], p.bf16);
-            *reinterpret_cast<uint4*>(to + lane * 64 + ((j ^ ((lane >> 1) & 3)) << 4)) = u;
-        }
-        send(map, to, col, row, batch, p);
-    }
-    __device__ __forceinline__ void put32(const CUtensorMap* map, const float (&v)[32], int col, int row, int batch, const ProdArgs& p)
+    int lane;
+    // the last store has read the buffer
+    __device__ __forceinline__ void begin()
     {
         if (lane == 0) store_wait_read<0>();
         __syncwarp();
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-            *reinterpret_cast<float4*>(buf + lane * 128 + ((j ^ (lane & 7)) << 4)) =
-                make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
-        send(map, buf, col, row, batch, p);
     }
-    __device__ __forceinline__ void send(const CUtensorMap* map, const unsigned char* from, int col, int row, int batch, const ProdArgs& p)
+    __device__ __forceinline__ void put(int chunk, uint4 v) { *reinterpret_cast<uint4*>(buf + lane * 64 + ((chunk ^ ((lane >> 1) & 3)) << 4)) = v; }
+    __device__ __forceinline__ void send(const CUtensorMap* map, int col, int row, int batch, const ProdArgs& p)
     {
         fence_async_smem();
         __syncwarp();
         if (lane == 0) {
-            if (col < p.cols && row < p.rows) tma_store(map, from, col, row, batch);
+            if (col < p.cols && row < p.rows) tma_store(map, buf, col, row, batch);
             store_commit();
         }
     }
 };
 
-// 32 values of a row of a 16-bit matrix, fetched before they are needed; zeros beyond `cols` (a multiple of 8)
-struct Row32 {
-    uint4 w[4];
+template <bool BF16>
+__device__ __forceinline__ uint4 pack8(const float* v)
+{
+    return make_uint4(pack2(v[0], v[1], BF16), pack2(v[2], v[3], BF16), pack2(v[4], v[5], BF16), pack2(v[6], v[7], BF16));
+}
+
+template <bool BF16>
+__device__ __forceinline__ void store16(uint16_t* to, const float (&v)[16], int col, int cols)
+{
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+        if (col + 8 * j < cols) *reinterpret_cast<uint4*>(to + col + 8 * j) = pack8<BF16>(v + 8 * j);
+}
+
+// 16 values of a row of a 16-bit matrix, fetched before they are needed; zeros beyond `cols` (a multiple of 8)
+struct Row16 {
+    uint4 w[2];
     __device__ __forceinline__ void fetch(const uint16_t* row, int col, int cols, bool want)
     {
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
+        for (int j = 0; j < 2; ++j)
             w[j] = want && col + 8 * j < cols ? __ldg(reinterpret_cast<const uint4*>(row + col) + j) : make_uint4(0u, 0u, 0u, 0u);
     }
-    // v += s * values
-    __device__ __forceinline__ void add(float (&v)[32], float s, int bf16) const
+    template <bool BF16>
+    __device__ __forceinline__ void get(float (&v)[16]) const
     {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
+        for (int j = 0; j < 2; ++j) {
             const uint32_t u[4] = {w[j].x, w[j].y, w[j].z, w[j].w};
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const float2 f = unpack2(u[i], bf16);
-                v[8 * j + 2 * i] = fmaf(f.x, s, v[8 * j + 2 * i]);
-                v[8 * j + 2 * i + 1] = fmaf(f.y, s, v[8 * j + 2 * i + 1]);
+                const float2 f = unpack2(u[i], BF16);
+                v[8 * j + 2 * i] = f.x;
+                v[8 * j + 2 * i + 1] = f.y;
             }
         }
     }
+    template <bool BF16>
+    __device__ __forceinline__ void add(float (&v)[16]) const
+    {
+        float f[16];
+        get<BF16>(f);
+#pragma unroll
+        for (int j = 0; j < 16; ++j) v[j] += f[j];
+    }
 };
 
-// Lane l holds v[0..31] of row l; returns to lane l the sum of column l over the 32 rows (31 exchanges, fixed order).
-__device__ __forceinline__ float column_sum(float (&v)[32], int lane)
+// Lane l holds v[0..15] of row l; returns to lanes l and l + 16 the sum of column l over the 32 rows (fixed order).
+__device__ __forceinline__ float column_sum(float (&v)[16], int lane)
 {
 #pragma unroll
-    for (int h = 16; h >= 1; h >>= 1) {
+    for (int h = 8; h >= 1; h >>= 1) {
         const bool up = lane & h;
 #pragma unroll
         for (int j = 0; j < h; ++j) {
@@ -155,14 +162,14 @@ __device__ __forceinline__ float column_sum(float (&v)[32], int lane)
             v[j] = keep + __shfl_xor_sync(0xffffffffu, give, h);
         }
     }
-    return v[0];
+    return v[0] + __shfl_xor_sync(0xffffffffu, v[0], 16);
 }
 
-template <int MODE, bool PAIR>
+template <int MODE, bool PAIR, bool BF16>
 __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ ProdArgs p)
 {
     constexpr bool A_MN = MODE == PROD_DW, B_MN = MODE == PROD_DX || MODE == PROD_DW;
-    constexpr int BUFFERS = MODE == PROD_DZ_TWO ? 1 : 2;
+    constexpr int BUFFERS = MODE == PROD_DZ_TWO ? 1 : 2;  // of the first product
     constexpr int BN = PAIR ? PAIR_COLS : SINGLE_COLS;
     constexpr uint32_t TMEM_COLUMNS = 2 * BN;
     extern __shared__ unsigned char smem_raw[];
@@ -170,6 +177,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
     __shared__ uint32_t tmem_sh;
     __shared__ int gave_up_sh;
     unsigned char* ring = smem_raw + ((1024u - (smem_addr(smem_raw) & 1023u)) & 1023u);
+
     unsigned char* staged = ring + STAGES * STAGE_BYTES;
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -196,12 +204,13 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
     volatile int* gave_up = &gave_up_sh;
 
     const bool gated = p.gate_rows != 0;
-    // output columns of a tile: a gated product spends half of the accumulator's columns on the other half of its rows
-    const int width = gated && (MODE == PROD_FWD || MODE == PROD_DZ || MODE == PROD_DZ_TWO) ? BN / 2 : BN;
+    // Output columns of a tile: a gated product spends half of the accumulator's columns on the other half of its rows.
+    // PROD_DZ_TWO: half in any case; the second product takes the other BN columns of tensor memory in turns of BN / 2.
+    const int width = MODE == PROD_DZ_TWO || (gated && (MODE == PROD_FWD || MODE == PROD_DZ)) ? BN / 2 : BN;
+    const int n1 = MODE == PROD_DZ_TWO && !gated ? BN / 2 : BN;  // accumulator columns of the first product
     const int total = tile_count<MODE>(p);
-    const int n2 = width;  // columns of the second product of PROD_DZ_TWO
+    constexpr int N2 = BN / 2, SHARE2 = PAIR ? N2 / 2 : N2;  // columns of the second product, and of its B in this block
     const int step = PAIR ? gridDim.x >> 1 : gridDim.x, first_tile = PAIR ? blockIdx.x >> 1 : blockIdx.x;
-    const int share2 = PAIR ? n2 / 2 : n2;  // columns of the second product's B in this block
 
     if (warp == 0) {
         if (lane == 0) {
@@ -212,8 +221,9 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
             for (int idx = first_tile; ok && idx < total; idx += step) {
                 const Tile t = tile_at<MODE, PAIR>(p, idx, width, rank);
                 // first row (K-major) or column of this block's 128 columns of B
-                const int b0 = !PAIR ? t.col : gated && !B_MN ? t.col + rank * p.gate_rows : t.col + rank * 128;
+                const int b0 = !PAIR ? t.col : gated && !B_MN ? t.col + rank * p.gate_rows : t.col + rank * (n1 / 2);
                 const int b1 = !PAIR && gated && !B_MN ? t.col + p.gate_rows : b0 + 64;
+                const bool two = n1 == BN;  // 128 columns of B, not 64
                 const int it1 = (t.k + BK - 1) / BK, it2 = MODE == PROD_DZ_TWO ? (p.k2 + BK - 1) / BK : 0;
                 for (int it = 0; it < it1 + it2; ++it) {
                     if (!bar_wait(&empty[stage], phase ^ 1u, gave_up)) {
@@ -224,14 +234,14 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
                     unsigned char* sb = sa + HALF;
                     // the leader's barrier counts both blocks' bytes
                     const uint32_t bar = PAIR ? cluster_addr(smem_addr(&full[stage]), 0) : smem_addr(&full[stage]);
-                    if (MODE == PROD_DZ_TWO && it >= it1) {
-                        const int k = (it - it1) * BK;
-                        if (rank == 0) bar_expect(&full[stage], (PAIR ? 2 : 1) * (HALF + share2 * BK * 2));
+                    if (MODE == PROD_DZ_TWO && it < it2) {
+                        const int k = it * BK;
+                        if (rank == 0) bar_expect(&full[stage], (PAIR ? 2 : 1) * (HALF + SHARE2 * BK * 2));
                         tma_load<PAIR>(sa, &p.a2, bar, k, t.row, 0);
-                        for (int j = 0; j < share2; j += 64) tma_load<PAIR>(sb + j * 128, &p.b2, bar, t.col + rank * share2 + j, k, t.expert);
+                        tma_load<PAIR>(sb, &p.b2, bar, t.col + rank * SHARE2, k, t.expert);
                     } else {
-                        const int k = t.k0 + it * BK;
-                        if (rank == 0) bar_expect(&full[stage], (PAIR ? 2 : 1) * STAGE_BYTES);
+                        const int k = t.k0 + (it - it2) * BK;
+                        if (rank == 0) bar_expect(&full[stage], (PAIR ? 2 : 1) * (two ? STAGE_BYTES : STAGE_BYTES - BOX));
                         if (A_MN) {
                             tma_load<PAIR>(sa, &p.a, bar, t.row, k, 0);
                             tma_load<PAIR>(sa + BOX, &p.a, bar, t.row + 64, k, 0);
@@ -243,7 +253,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
                             tma_load<PAIR>(sb + BOX, &p.b, bar, b1, k, MODE == PROD_DW ? 0 : t.expert);
                         } else {
                             tma_load<PAIR>(sb, &p.b, bar, k, b0, t.expert);
-                            tma_load<PAIR>(sb + BOX, &p.b, bar, k, b1, t.expert);
+                            if (two) tma_load<PAIR>(sb + BOX, &p.b, bar, k, b1, t.expert);
                         }
                     }
                     ++issued;
@@ -266,28 +276,28 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
             int stage = 0, n_acc = 0;
             uint32_t phase = 0;
             bool ok = true;
-            const uint32_t idesc1 = mma_desc(p.bf16, A_MN, B_MN, PAIR ? 256 : 128, BN);
-            const uint32_t idesc2 = mma_desc(p.bf16, 0, 1, PAIR ? 256 : 128, n2);
+            const uint32_t idesc1 = mma_desc(BF16, A_MN, B_MN, PAIR ? 256 : 128, n1);
+            const uint32_t idesc2 = mma_desc(BF16, 0, 1, PAIR ? 256 : 128, N2);
             for (int idx = first_tile; ok && idx < total; idx += step, ++n_acc) {
                 const Tile t = tile_at<MODE, PAIR>(p, idx, width, rank);
                 const int buf = BUFFERS == 2 ? n_acc & 1 : 0;
                 const uint32_t use = (uint32_t)(n_acc / BUFFERS) & 1u;
-                if (!bar_wait(&acc_empty[buf], use ^ 1u, gave_up)) {
-                    ok = false;
-                    break;
-                }
-                tc_fence_after();
                 const int it1 = (t.k + BK - 1) / BK, it2 = MODE == PROD_DZ_TWO ? (p.k2 + BK - 1) / BK : 0;
+                // (the second product's turn was read by the epilogue of the tile before the last, which is over)
                 for (int it = 0; it < it1 + it2; ++it) {
-                    if (!bar_wait(&full[stage], phase, gave_up)) {
+                    if (it == it2) {  // the first product's columns have been read
+                        ok = bar_wait(&acc_empty[buf], use ^ 1u, gave_up);
+                        tc_fence_after();
+                    }
+                    if (!ok || !bar_wait(&full[stage], phase, gave_up)) {
                         ok = false;
                         break;
                     }
                     tc_fence_after();
                     const uint32_t sa = smem_addr(ring + stage * STAGE_BYTES), sb = sa + HALF;
-                    const bool second = MODE == PROD_DZ_TWO && it >= it1;
-                    const uint32_t d = tmem + (uint32_t)(buf * BN) + (second ? (uint32_t)BN : 0u);
-                    const bool first = it == 0 || (MODE == PROD_DZ_TWO && it == it1);
+                    const bool second = MODE == PROD_DZ_TWO && it < it2;
+                    const uint32_t d = second ? tmem + (uint32_t)(BN + (n_acc & 1) * N2) : tmem + (uint32_t)(buf * BN);
+                    const bool first = it == 0 || it == it2;
 #pragma unroll
                     for (int kk = 0; kk < BK / 16; ++kk) {
                         const uint64_t da = A_MN ? mat_desc(sa + kk * 2048, BOX, 1024) : mat_desc(sa + kk * 32, 16, 1024);
@@ -301,6 +311,11 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
                         phase ^= 1u;
                     }
                 }
+                if (!ok) break;
+                if (it1 + it2 == 0 && !bar_wait(&acc_empty[buf], use ^ 1u, gave_up)) {  // nothing to sum
+                    ok = false;
+                    break;
+                }
                 mma_commit<PAIR>(&acc_full[buf]);
             }
             if (!ok) {  // instructions in flight read shared memory and write tensor memory
@@ -310,129 +325,156 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
             }
         }
     } else {
-        const int w = warp - 2, q = warp & 3, half = w >> 2;  // a warp may read the 32 lanes of its quarter only
-        Stager s{staged + w * OUT_BYTES, lane, 0};
+        // A warp may read the 32 lanes of its quarter only; the four warps of a quarter take the tile's pieces of 32 columns
+        // in turn, a piece in two steps of 16 columns.
+        const int q = warp & 3, turn = (warp - 2) >> 2;
+        Stager s{staged + (warp - 2) * OUT_BYTES, lane};
         int n_acc = 0;
         for (int idx = first_tile; idx < total; idx += step, ++n_acc) {
             const Tile t = tile_at<MODE, PAIR>(p, idx, width, rank);
             const int buf = BUFFERS == 2 ? n_acc & 1 : 0;
             const uint32_t acc = tmem + (uint32_t)(buf * BN) + ((uint32_t)(32 * q) << 16);
+            const uint32_t acc2 = tmem + (uint32_t)(BN + (n_acc & 1) * N2) + ((uint32_t)(32 * q) << 16);
             const int row0 = t.row + 32 * q, row = row0 + lane;
             const bool counts = row < t.live;
-            const float rw = p.row_weight && counts ? p.row_weight[row] : 1.f;
+            // padding rows weigh nothing (what they hold is zeros, or the bias's image of them)
+            const float rw = !p.row_weight ? 1.f : counts ? p.row_weight[row] : 0.f;
             const uint16_t* bias = p.bias ? p.bias + (size_t)t.expert * p.bias_ld : nullptr;
             const uint16_t* extra = p.extra ? p.extra + (size_t)row * p.ld_extra : nullptr;
-            const int each = width / 2;  // columns of this warp
-            const int batch = MODE == PROD_DW ? t.expert : 0;
+            const bool writes = row < t.store;
+            const bool any = row0 < t.store && turn * 32 < width;
+            // what the epilogue reads from memory is fetched ahead: the first step's before the products are done
+            Row16 add, b0, b1;
+            auto fetch = [&](int at) {
+                const int col = t.col + at;
+                if (MODE == PROD_FWD || MODE == PROD_DZ) add.fetch(extra, col, p.cols, extra && counts && at < width);
+                if (MODE != PROD_DX && MODE != PROD_DW) {
+                    b0.fetch(bias, col, p.cols, bias && at < width);
+                    b1.fetch(bias ? bias + p.gate_rows : bias, col, p.cols, bias && gated && at < width);
+                }
+            };
+            if (any) fetch(turn * 32);
             if (!bar_wait(&acc_full[buf], (uint32_t)(n_acc / BUFFERS) & 1u, gave_up)) break;
             __syncwarp();
             tc_fence_after();
-            if (row0 < t.store) {
+            if (any) {
                 float dot = 0.f;
 #pragma unroll 1
-                for (int c = 0; c < each; c += 32) {
-                    const int at = half * each + c, col = t.col + at;
-                    Row32 add, b0, b1;
-                    if (MODE == PROD_FWD || MODE == PROD_DZ) add.fetch(extra, col, p.cols, extra && counts);
-                    if (MODE != PROD_DX && MODE != PROD_DW) {
-                        b0.fetch(bias, col, p.cols, bias != nullptr);
-                        b1.fetch(bias ? bias + p.gate_rows : bias, col, p.cols, bias && gated);
-                    }
-                    float v[32], u[32];
-                    tmem_ld32(acc + at, v);
+                for (int at = turn * 32; at < width; at += at & 16 ? 112 : 16) {
+                    const int col = t.col + at, next = at + (at & 16 ? 112 : 16);
+                    float v[16], u[16];
+                    tmem_ld16(acc + at, v);
                     if (MODE == PROD_DX || MODE == PROD_DW) {
                         tmem_wait_ld();
                         if (MODE == PROD_DW && t.k == 0) {
 #pragma unroll
-                            for (int j = 0; j < 32; ++j) v[j] = 0.f;  // an expert without a token: nothing was summed
+                            for (int j = 0; j < 16; ++j) v[j] = 0.f;  // an expert without a token: nothing was summed
                         }
                     } else if (MODE == PROD_FWD) {
-                        if (gated) {
-                            tmem_ld32(acc + BN / 2 + at, u);
-                            tmem_wait_ld();
-                            if (bias) {
-                                b0.add(v, 1.f, p.bf16);
-                                b1.add(u, 1.f, p.bf16);
-                            }
+                        if (gated) tmem_ld16(acc + BN / 2 + at, u);
+                        tmem_wait_ld();
+                        if (bias) {
+                            float f[16];
+                            b0.template get<BF16>(f);
+                            const float by = p.weigh == 2 ? rw : 1.f;
+#pragma unroll
+                            for (int j = 0; j < 16; ++j) v[j] = fmaf(f[j], by, v[j]);
+                            if (gated) b1.template add<BF16>(u);
+                        }
+                        if (p.act != SOM_ACT_NONE)
                             with_act(p.act, [&](auto tag) {
 #pragma unroll
-                                for (int j = 0; j < 32; ++j) v[j] = act_of<decltype(tag)::value>(v[j]) * u[j];
+                                for (int j = 0; j < 16; ++j) v[j] = act_of<decltype(tag)::value>(v[j]);
                             });
-                        } else {
-                            tmem_wait_ld();
-                            if (bias) b0.add(v, p.weigh == 2 ? rw : 1.f, p.bf16);
-                            if (p.act != SOM_ACT_NONE)
-                                with_act(p.act, [&](auto tag) {
+                        if (gated) {
 #pragma unroll
-                                    for (int j = 0; j < 32; ++j) v[j] = act_of<decltype(tag)::value>(v[j]);
-                                });
+                            for (int j = 0; j < 16; ++j) v[j] *= u[j];
                         }
-                        if (extra) add.add(v, 1.f, p.bf16);
+                        if (extra) add.template add<BF16>(v);
+                        fetch(next);
                         if (p.weigh == 1) {
 #pragma unroll
-                            for (int j = 0; j < 32; ++j) v[j] *= rw;
+                            for (int j = 0; j < 16; ++j) v[j] *= rw;
                         }
                     } else {
                         // PROD_DZ, PROD_DZ_TWO: v = z (or the gate's z) becomes dz, u = the gated half's
-                        float g[32];
-                        if (gated) tmem_ld32(acc + BN / 2 + at, u);
-                        if (MODE == PROD_DZ_TWO) tmem_ld32(acc + BN + at, g);
+                        float g[16], hid[16];
+                        if (gated) tmem_ld16(acc + BN / 2 + at, u);
+                        if (MODE == PROD_DZ_TWO) tmem_ld16(acc2 + at, g);
                         tmem_wait_ld();
                         if (bias) {
-                            b0.add(v, 1.f, p.bf16);
-                            if (gated) b1.add(u, 1.f, p.bf16);
+                            b0.template add<BF16>(v);
+                            if (gated) b1.template add<BF16>(u);
                         }
-                        if (MODE == PROD_DZ) {
-#pragma unroll
-                            for (int j = 0; j < 32; ++j) g[j] = 0.f;
-                            add.add(g, 1.f, p.bf16);
-                        }
-                        float hid[32];
+                        if (MODE == PROD_DZ) add.template get<BF16>(g);
+                        fetch(next);
                         with_act(p.act, [&](auto tag) {
 #pragma unroll
-                            for (int j = 0; j < 32; ++j) {
+                            for (int j = 0; j < 16; ++j) {
                                 float a, da;
                                 act_both<decltype(tag)::value>(v[j], a, da);
-                                if (gated) {
-                                    hid[j] = a * u[j];
-                                    v[j] = u[j] * da;
-                                    u[j] = a;
-                                } else {
-                                    hid[j] = a;
-                                    v[j] = da;
-                                }
+                                hid[j] = a;
+                                v[j] = da;
                             }
                         });
-                        if (MODE == PROD_DZ_TWO) {
+                        if (gated) {
 #pragma unroll
-                            for (int j = 0; j < 32; ++j) {
-                                if (col + j < p.cols) dot = fmaf(hid[j], g[j], dot);
-                                hid[j] = counts ? hid[j] * rw : 0.f;
+                            for (int j = 0; j < 16; ++j) {
+                                const float a = hid[j];
+                                hid[j] = a * u[j];
+                                v[j] *= u[j];
+                                u[j] = a;
+                            }
+                        }
+                        if (MODE == PROD_DZ_TWO) {
+                            // (columns beyond the last have g = 0: W2 is filled with zeros there)
+#pragma unroll
+                            for (int j = 0; j < 16; ++j) {
+                                dot = fmaf(hid[j], g[j], dot);
                                 g[j] *= rw;
+                                hid[j] *= rw;
                             }
                         }
 #pragma unroll
-                        for (int j = 0; j < 32; ++j) {
-                            v[j] = counts ? v[j] * g[j] : 0.f;
-                            if (gated) u[j] = counts ? u[j] * g[j] : 0.f;
+                        for (int j = 0; j < 16; ++j) {
+                            v[j] *= g[j];
+                            if (gated) u[j] *= g[j];
                         }
-                        if (MODE == PROD_DZ_TWO) s.put16(&p.o2, hid, col, row0, 0, p);
-                        if (gated) s.put16(&p.o1, u, col, row0, 0, p);
+                        if (writes) {
+                            uint16_t* to = static_cast<uint16_t*>(p.o0) + (size_t)row * p.ld0;
+                            store16<BF16>(to, v, col, p.cols);
+                            if (gated) store16<BF16>(to + p.gate_rows, u, col, p.cols);
+                            if (MODE == PROD_DZ_TWO) store16<BF16>(static_cast<uint16_t*>(p.o2) + (size_t)row * p.ld2, hid, col, p.cols);
+                        }
                     }
-                    if (p.out32) s.put32(&p.o0, v, col, row0, batch, p);
-                    else s.put16(&p.o0, v, col, row0, batch, p);
+                    if (MODE == PROD_FWD || MODE == PROD_DX || MODE == PROD_DW) {
+                        const int batch = MODE == PROD_DW ? t.expert : 0;
+                        if (p.out32) {
+                            s.begin();
+#pragma unroll
+                            for (int j = 0; j < 4; ++j)
+                                s.put(j, make_uint4(__float_as_uint(v[4 * j]), __float_as_uint(v[4 * j + 1]), __float_as_uint(v[4 * j + 2]), __float_as_uint(v[4 * j + 3])));
+                            s.send(&p.o, col, row0, batch, p);
+                        } else {
+                            const int half = (at >> 4) & 1;
+                            if (half == 0) s.begin();
+                            s.put(2 * half, pack8<BF16>(v));
+                            s.put(2 * half + 1, pack8<BF16>(v + 8));
+                            if (half == 1) s.send(&p.o, col - 16, row0, batch, p);
+                        }
+                    }
                     if ((MODE == PROD_DZ || MODE == PROD_DZ_TWO) && p.column_sums) {
-                        // (outputs were rounded; the sums are over the unrounded values)
-                        float* to = p.column_sums + (size_t)(row0 / 32) * (p.cols + p.gate_rows);
+                        // (outputs were rounded; the sums are over the unrounded values; rows that do not count hold zeros)
+                        float* to = p.column_sums + (size_t)(row0 / 32) * (p.cols + p.gate_rows) + col;
                         const float sv = column_sum(v, lane);
-                        if (col + lane < p.cols) to[col + lane] = sv;
+                        if (lane < 16 && col + lane < p.cols) to[lane] = sv;
                         if (gated) {
                             const float su = column_sum(u, lane);
-                            if (col + lane < p.cols) to[p.gate_rows + col + lane] = su;
+                            if (lane < 16 && col + lane < p.cols) to[p.gate_rows + lane] = su;
                         }
                     }
                 }
-                if (MODE == PROD_DZ_TWO && counts) p.dot[(size_t)row * (2 * p.col_tiles) + 2 * (t.col / width) + half] = dot;
+                if (MODE == PROD_DZ_TWO && counts) p.dot[(size_t)row * p.dots + (t.col / width) * (width / 32) + turn] = dot;
             }
             tc_fence_before();
             __syncwarp();
@@ -441,8 +483,8 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
                 else bar_arrive(&acc_empty[buf]);
             }
         }
-        if (lane == 0) store_wait_all();
     }
+    if (warp >= 2 && lane == 0) store_wait_all();
     __syncthreads();
     if (threadIdx.x == 0 && gave_up_sh) atomicOr(p.flags, LAY_FLAG_GAVE_UP);
     __syncwarp();
@@ -453,45 +495,59 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
     }
 }
 
-template <int MODE, bool PAIR>
-cudaError_t launch_mode(som_layers* l, const ProdArgs& args, cudaStream_t st)
+template <bool PAIR>
+void set_cluster(cudaLaunchConfig_t* c, cudaLaunchAttribute* attr)
+{
+    attr->id = cudaLaunchAttributeClusterDimension;
+    attr->val.clusterDim.x = 2;
+    attr->val.clusterDim.y = attr->val.clusterDim.z = 1;
+    c->attrs = attr;
+    c->numAttrs = PAIR ? 1 : 0;
+    c->blockDim = dim3(THREADS);
+    c->dynamicSmemBytes = SMEM;
+}
+
+template <int MODE, bool PAIR, bool BF16>
+cudaError_t launch_as(som_layers* l, const ProdArgs& args, cudaStream_t st)
 {
     const int64_t tiles = (int64_t)args.row_tiles * args.col_tiles * (MODE == PROD_DW ? args.experts : 1);
     const int most = PAIR ? l->pairs : l->sm_count;
     cudaLaunchConfig_t c = {};
-    c.gridDim = dim3((unsigned)(tiles < most ? tiles : most) * (PAIR ? 2 : 1));
-    c.blockDim = dim3(THREADS);
-    c.dynamicSmemBytes = SMEM;
-    c.stream = st;
     cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = 2;
-    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-    c.attrs = attr;
-    c.numAttrs = PAIR ? 1 : 0;
-    return cudaLaunchKernelEx(&c, k_product<MODE, PAIR>, args);
+    set_cluster<PAIR>(&c, attr);
+    c.gridDim = dim3((unsigned)(tiles < most ? tiles : most) * (PAIR ? 2 : 1));
+    c.stream = st;
+    return cudaLaunchKernelEx(&c, k_product<MODE, PAIR, BF16>, args);
+}
+
+template <int MODE>
+cudaError_t launch_mode(som_layers* l, const ProdArgs& a, cudaStream_t st)
+{
+    if (a.pair) return a.bf16 ? launch_as<MODE, true, true>(l, a, st) : launch_as<MODE, true, false>(l, a, st);
+    return a.bf16 ? launch_as<MODE, false, true>(l, a, st) : launch_as<MODE, false, false>(l, a, st);
+}
+
+template <int MODE, bool BF16>
+cudaError_t prepare_as(int* pairs)
+{
+    cudaError_t e = cudaFuncSetAttribute(k_product<MODE, false, BF16>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(k_product<MODE, true, BF16>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM);
+    if (e != cudaSuccess) return e;
+    cudaLaunchConfig_t c = {};
+    cudaLaunchAttribute attr[1];
+    set_cluster<true>(&c, attr);
+    c.gridDim = dim3(2);
+    int n = 0;
+    e = cudaOccupancyMaxActiveClusters(&n, k_product<MODE, true, BF16>, &c);
+    if (n < *pairs) *pairs = n;
+    return e;
 }
 
 template <int MODE>
 cudaError_t prepare_mode(int* pairs)
 {
-    cudaError_t e = cudaFuncSetAttribute(k_product<MODE, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM);
-    if (e == cudaSuccess) e = cudaFuncSetAttribute(k_product<MODE, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM);
-    if (e != cudaSuccess) return e;
-    cudaLaunchConfig_t c = {};
-    c.gridDim = dim3(2);
-    c.blockDim = dim3(THREADS);
-    c.dynamicSmemBytes = SMEM;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = 2;
-    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-    c.attrs = attr;
-    c.numAttrs = 1;
-    int n = 0;
-    e = cudaOccupancyMaxActiveClusters(&n, k_product<MODE, true>, &c);
-    if (n < *pairs) *pairs = n;
-    return e;
+    const cudaError_t e = prepare_as<MODE, true>(pairs);
+    return e == cudaSuccess ? prepare_as<MODE, false>(pairs) : e;
 }
 
 }  // namespace
@@ -511,11 +567,11 @@ int launch_product(som_layers* l, ProdMode mode, const ProdArgs& a, cudaStream_t
 {
     cudaError_t e;
     switch (mode) {
-        case PROD_FWD: e = a.pair ? launch_mode<PROD_FWD, true>(l, a, st) : launch_mode<PROD_FWD, false>(l, a, st); break;
-        case PROD_DZ: e = a.pair ? launch_mode<PROD_DZ, true>(l, a, st) : launch_mode<PROD_DZ, false>(l, a, st); break;
-        case PROD_DZ_TWO: e = a.pair ? launch_mode<PROD_DZ_TWO, true>(l, a, st) : launch_mode<PROD_DZ_TWO, false>(l, a, st); break;
-        case PROD_DX: e = a.pair ? launch_mode<PROD_DX, true>(l, a, st) : launch_mode<PROD_DX, false>(l, a, st); break;
-        default: e = a.pair ? launch_mode<PROD_DW, true>(l, a, st) : launch_mode<PROD_DW, false>(l, a, st); break;
+        case PROD_FWD: e = launch_mode<PROD_FWD>(l, a, st); break;
+        case PROD_DZ: e = launch_mode<PROD_DZ>(l, a, st); break;
+        case PROD_DZ_TWO: e = launch_mode<PROD_DZ_TWO>(l, a, st); break;
+        case PROD_DX: e = launch_mode<PROD_DX>(l, a, st); break;
+        default: e = launch_mode<PROD_DW>(l, a, st); break;
     }
     ++l->launches;
     if (e == cudaSuccess) return SOM_OK;

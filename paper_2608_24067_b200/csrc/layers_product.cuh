@@ -19,7 +19,10 @@ constexpr int PAIR_ROWS = 256, PAIR_COLS = 256, SINGLE_ROWS = 128, SINGLE_COLS =
 struct ProdArgs {
     CUtensorMap a, b;         // operands (of the first product)
     CUtensorMap a2, b2;       // second product of PROD_DZ_TWO
-    CUtensorMap o0, o1, o2;   // outputs
+    CUtensorMap o;            // output of PROD_FWD, PROD_DX, PROD_DW
+    void* o0;                 // PROD_DZ, PROD_DZ_TWO: dz [rows][ld0], the gated half gate_rows columns on
+    void* o2;                 // PROD_DZ_TWO: weighted hidden values [rows][ld2]
+    int64_t ld0, ld2;
     const int* tiles;         // grouped rows: number of row tiles on the device; nullptr = row_tiles
     const int* tile_expert;   // grouped rows: expert of a row tile; nullptr = 0
     const int* seg;           // grouped rows: first row of every expert
@@ -27,10 +30,10 @@ struct ProdArgs {
     const uint16_t* bias;     // [experts][bias_ld] or nullptr
     const uint16_t* extra;    // residual (PROD_FWD) or dy (PROD_DZ), [rows][ld_extra], or nullptr
     const float* row_weight;  // [rows] or nullptr
-    float* dot;               // PROD_DZ_TWO: [rows][2 * col_tiles] partial sums of h * g
+    float* dot;               // PROD_DZ_TWO: [rows][dots] partial sums of h * g over 32 columns
     float* column_sums;       // PROD_DZ, PROD_DZ_TWO: [rows / 32][2 cols or cols] sums of dz over 32 rows, or nullptr
     int64_t ld_extra;
-    int bias_ld;
+    int bias_ld, dots;
     int pair;
     int row_tiles, col_tiles, experts;
     int rows, cols;  // extent of the outputs (PROD_DW: of one expert's)
@@ -43,9 +46,9 @@ struct ProdArgs {
 
 int launch_product(som_layers* l, ProdMode mode, const ProdArgs& args, cudaStream_t st);
 
-// 3-d tensor map over [batch][rows][cols] of 16-bit (bytes = 2) or fp32 (4) elements in boxes of [1][box_rows][box_cols],
-// box_cols * bytes = 64 or 128 (the swizzle)
+// 3-d tensor map over [batch][rows][cols] of 16-bit (bytes = 2) or fp32 (4) elements in boxes of [1][box_rows] rows of
+// box_bytes, 64 or 128 (the swizzle)
 int make_map(som_layers* l, CUtensorMap* map, const void* base, int bytes, int64_t cols, int64_t rows, int64_t batch,
-             int64_t ld, int64_t batch_stride, int box_cols, int box_rows);
+             int64_t ld, int64_t batch_stride, int box_bytes, int box_rows);
 
 }  // namespace lay
