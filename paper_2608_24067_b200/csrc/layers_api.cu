@@ -529,7 +529,7 @@ int som_experts_backward(som_layers* l, int type, int act, int gated, int64_t T,
     uint16_t *xp, *dyp, *h, *dz;
     float *part, *dot, *sums;
     const bool pair = pair_rows(T, E, k);
-    const int width = (pair ? PAIR_COLS : SINGLE_COLS) / 2, dots = tiles_of(I, width) * (width / 32);
+    const int dots = tiles_of(I, (pair ? PAIR_COLS : SINGLE_COLS) / 2) * tile_dots(pair);
     Carver c{nullptr, 0};
     for (int pass = 0; pass < 2; ++pass) {
         c.used = 0;

@@ -26,7 +26,8 @@ constexpr int BM = 128, BK = 64, STAGES = 6;
 constexpr int HALF = 128 * BK * 2;  // bytes of a block's share of an operand in a stage
 constexpr int STAGE_BYTES = 2 * HALF;
 constexpr int BOX = 64 * 128;  // bytes of a box of 64 rows
-constexpr int EPI_WARPS = 16, THREADS = 32 * (2 + EPI_WARPS);
+constexpr int EPI_WARPS = 4 * EPI_TURNS, THREADS = 32 * (2 + EPI_WARPS);
+constexpr int ROUND = EPI_TURNS * 32;  // columns that the epilogue's warps take in a round
 constexpr int OUT_BYTES = 32 * 64;  // an epilogue warp's staged output: 32 rows of 64 bytes
 constexpr int SMEM = 1024 + STAGES * STAGE_BYTES + EPI_WARPS * OUT_BYTES;
 
@@ -354,14 +355,15 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
                 }
             };
             if (any) fetch(turn * 32);
-            if (!bar_wait(&acc_full[buf], (uint32_t)(n_acc / BUFFERS) & 1u, gave_up)) break;
-            __syncwarp();
+            bool ok = true;
+            if (lane == 0) ok = bar_wait(&acc_full[buf], (uint32_t)(n_acc / BUFFERS) & 1u, gave_up);
+            if (!__shfl_sync(0xffffffffu, ok, 0)) break;
             tc_fence_after();
             if (any) {
                 float dot = 0.f;
 #pragma unroll 1
-                for (int at = turn * 32; at < width; at += at & 16 ? 112 : 16) {
-                    const int col = t.col + at, next = at + (at & 16 ? 112 : 16);
+                for (int at = turn * 32; at < width; at += at & 16 ? ROUND - 16 : 16) {
+                    const int col = t.col + at, next = at + (at & 16 ? ROUND - 16 : 16);
                     float v[16], u[16];
                     tmem_ld16(acc + at, v);
                     if (MODE == PROD_DX || MODE == PROD_DW) {
@@ -474,7 +476,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
                         }
                     }
                 }
-                if (MODE == PROD_DZ_TWO && counts) p.dot[(size_t)row * p.dots + (t.col / width) * (width / 32) + turn] = dot;
+                if (MODE == PROD_DZ_TWO && counts) p.dot[(size_t)row * p.dots + (t.col / width) * tile_dots(PAIR) + turn] = dot;
             }
             tc_fence_before();
             __syncwarp();

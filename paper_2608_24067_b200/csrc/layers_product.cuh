@@ -16,6 +16,15 @@ enum ProdMode {
 // Output tiles: `pair` = 256 x 256 by two blocks of a cluster, else 128 x 128 by one block.
 constexpr int PAIR_ROWS = 256, PAIR_COLS = 256, SINGLE_ROWS = 128, SINGLE_COLS = 128;
 
+constexpr int EPI_TURNS = 2;  // epilogue warps per 32 rows of a block's tile; they take its pieces of 32 columns in turn
+
+// partial sums of h * g that a tile of PROD_DZ_TWO (half as wide as others) leaves for a row
+__host__ __device__ constexpr int tile_dots(bool pair)
+{
+    const int pieces = (pair ? PAIR_COLS : SINGLE_COLS) / 2 / 32;
+    return pieces < EPI_TURNS ? pieces : EPI_TURNS;
+}
+
 struct ProdArgs {
     CUtensorMap a, b;         // operands (of the first product)
     CUtensorMap a2, b2;       // second product of PROD_DZ_TWO
@@ -30,7 +39,7 @@ struct ProdArgs {
     const uint16_t* bias;     // [experts][bias_ld] or nullptr
     const uint16_t* extra;    // residual (PROD_FWD) or dy (PROD_DZ), [rows][ld_extra], or nullptr
     const float* row_weight;  // [rows] or nullptr
-    float* dot;               // PROD_DZ_TWO: [rows][dots] partial sums of h * g over 32 columns
+    float* dot;               // PROD_DZ_TWO: [rows][dots] partial sums of h * g, tile_dots a tile
     float* column_sums;       // PROD_DZ, PROD_DZ_TWO: [rows / 32][2 cols or cols] sums of dz over 32 rows, or nullptr
     int64_t ld_extra;
     int bias_ld, dots;
