@@ -55,6 +55,7 @@ __global__ void __launch_bounds__(FEW_THREADS, ROWS <= 2 ? 3 : 2) k_few(const Fe
     extern __shared__ __align__(16) uint16_t xs[];  // [ROWS][D]
     __shared__ float part[FEW_WARPS][ROWS * HALVES];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    enter();
     int64_t first = 0;  // first row of x and of the output
     const uint16_t *w = a.w, *bias = a.bias;
     float weight = 1.f;
@@ -90,7 +91,6 @@ __global__ void __launch_bounds__(FEW_THREADS, ROWS <= 2 ? 3 : 2) k_few(const Fe
             r < a.rows ? __ldg(reinterpret_cast<const uint4*>(a.x + (size_t)(first + r) * a.ldx) + q) : make_uint4(0u, 0u, 0u, 0u);
     }
     __syncthreads();
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     for (int f_block = blockIdx.x * features; f_block < a.F; f_block += stride, f += stride) {
         float acc[ROWS][HALVES];
 #pragma unroll
@@ -177,6 +177,7 @@ __global__ void __launch_bounds__(FEW_THREADS, 3) k_few_down(const FewDownArgs a
     __shared__ int64_t base[32];  // the experts' weights, -1 = none
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int64_t t = blockIdx.y;
+    // (The kernel before, k_few, was let in only after all earlier work: indices and weights are there.  It does not write them.)
     if (threadIdx.x < a.k) {
         const int e = a.indices[t * a.k + threadIdx.x];
         base[threadIdx.x] = e >= 0 && e < a.E ? (int64_t)e * a.D * a.I : -1;
@@ -211,7 +212,7 @@ __global__ void __launch_bounds__(FEW_THREADS, 3) k_few_down(const FewDownArgs a
     int d = blockIdx.x * outputs + warp / share;
 #pragma unroll
     for (int i = 0; i < DEEP; ++i) fetch(d, buf[i]);
-    asm volatile("griddepcontrol.wait;" ::: "memory");
+    enter();
     for (int i = threadIdx.x; i < a.k * (a.I / 4); i += FEW_THREADS) {
         const int j = i / (a.I / 4), q = i - j * (a.I / 4);
         reinterpret_cast<float4*>(hs)[j * (a.I / 4) + (q & 1) * (a.I / 8) + (q >> 1)] =
@@ -264,13 +265,12 @@ __global__ void __launch_bounds__(FEW_THREADS, 3) k_few_down(const FewDownArgs a
 }
 
 template <int HALVES>
-cudaError_t go(const FewArgs& a, dim3 grid, size_t smem, cudaStream_t st)
+cudaError_t go(som_layers* l, const FewArgs& a, dim3 grid, size_t smem, cudaStream_t st)
 {
-    if (a.rows == 1) k_few<1, HALVES><<<grid, FEW_THREADS, smem, st>>>(a);
-    else if (a.rows == 2) k_few<2, HALVES><<<grid, FEW_THREADS, 2 * smem, st>>>(a);
-    else if (a.rows <= 4) k_few<4, HALVES><<<grid, FEW_THREADS, 4 * smem, st>>>(a);
-    else k_few<8, HALVES><<<grid, FEW_THREADS, 8 * smem, st>>>(a);
-    return cudaGetLastError();
+    if (a.rows == 1) return launch(l, k_few<1, HALVES>, grid, FEW_THREADS, smem, st, 1, a);
+    if (a.rows == 2) return launch(l, k_few<2, HALVES>, grid, FEW_THREADS, 2 * smem, st, 1, a);
+    if (a.rows <= 4) return launch(l, k_few<4, HALVES>, grid, FEW_THREADS, 4 * smem, st, 1, a);
+    return launch(l, k_few<8, HALVES>, grid, FEW_THREADS, 8 * smem, st, 1, a);
 }
 
 template <int HALVES>
@@ -313,31 +313,13 @@ int launch_few(som_layers* l, FewArgs a, int groups, bool gated, cudaStream_t st
 {
     a.share = share_of(l, (int64_t)a.F * groups, (int64_t)a.D, gated ? 1024 : 2048);
     const dim3 grid = few_grid(l, a.F, FEW_WARPS / a.share, groups);
-    const cudaError_t e = gated ? go<2>(a, grid, (size_t)a.D * 2, st) : go<1>(a, grid, (size_t)a.D * 2, st);
-    ++l->launches;
-    if (e == cudaSuccess) return SOM_OK;
-    l->last_cuda_error = (int)e;
-    return SOM_ERR_CUDA;
+    return outcome(l, gated ? go<2>(l, a, grid, (size_t)a.D * 2, st) : go<1>(l, a, grid, (size_t)a.D * 2, st));
 }
 
 int launch_few_down(som_layers* l, FewDownArgs a, int64_t T, cudaStream_t st)
 {
     a.share = share_of(l, a.D * T, (int64_t)a.k * a.I, 2048);
-    cudaLaunchConfig_t c = {};
-    c.gridDim = few_grid(l, a.D, FEW_WARPS / a.share, T);
-    c.blockDim = dim3(FEW_THREADS);
-    c.dynamicSmemBytes = (size_t)a.k * a.I * sizeof(float);
-    c.stream = st;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    c.attrs = attr;
-    c.numAttrs = 1;
-    const cudaError_t e = cudaLaunchKernelEx(&c, k_few_down, a);
-    ++l->launches;
-    if (e == cudaSuccess) return SOM_OK;
-    l->last_cuda_error = (int)e;
-    return SOM_ERR_CUDA;
+    return outcome(l, launch(l, k_few_down, few_grid(l, a.D, FEW_WARPS / a.share, T), FEW_THREADS, (size_t)a.k * a.I * sizeof(float), st, 1, a));
 }
 
 }  // namespace lay

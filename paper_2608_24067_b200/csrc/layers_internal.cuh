@@ -26,6 +26,43 @@ struct som_layers {
 
 namespace lay {
 
+// Every kernel of the dense operators is launched so that its blocks may come in while the kernel before it ends
+// (programmatic stream serialization), and begins with enter(): nothing is read or written before all earlier work in the
+// stream is complete, and the next kernel's launch is let through only after that.
+__device__ __forceinline__ void enter()
+{
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+}
+
+template <class... P, class... A>
+cudaError_t launch(som_layers* l, void (*kernel)(P...), dim3 grid, int threads, size_t smem, cudaStream_t st, int cluster, const A&... args)
+{
+    cudaLaunchConfig_t c = {};
+    c.gridDim = grid;
+    c.blockDim = dim3((unsigned)threads);
+    c.dynamicSmemBytes = smem;
+    c.stream = st;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = (unsigned)cluster;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    c.attrs = attr;
+    c.numAttrs = cluster > 1 ? 2 : 1;
+    ++l->launches;
+    return cudaLaunchKernelEx(&c, kernel, P(args)...);
+}
+
+// a launch's outcome as a status, the error kept on the handle
+inline int outcome(som_layers* l, cudaError_t e)
+{
+    if (e == cudaSuccess) return SOM_OK;
+    l->last_cuda_error = (int)e;
+    return SOM_ERR_CUDA;
+}
+
 // Rows of the experts' work ("slots" = (token, place) pairs with an expert) in the experts' order, every expert's
 // segment padded to whole row tiles.  All on the device, written by launch_plan.
 struct SlotPlan {

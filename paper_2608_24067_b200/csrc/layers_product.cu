@@ -28,8 +28,8 @@ constexpr int STAGE_BYTES = 2 * HALF;
 constexpr int BOX = 64 * 128;  // bytes of a box of 64 rows
 constexpr int EPI_WARPS = 4 * EPI_TURNS, THREADS = 32 * (2 + EPI_WARPS);
 constexpr int ROUND = EPI_TURNS * 32;  // columns that the epilogue's warps take in a round
-constexpr int OUT_BYTES = 32 * 64;  // an epilogue warp's staged output: 32 rows of 64 bytes
-constexpr int SMEM = 1024 + STAGES * STAGE_BYTES + EPI_WARPS * OUT_BYTES;
+constexpr int OUT_BYTES = 32 * 64;  // an epilogue warp's staged output: 32 rows of 64 bytes, two of them
+constexpr int SMEM = 1024 + STAGES * STAGE_BYTES + EPI_WARPS * 2 * OUT_BYTES;
 
 struct Tile {
     int row, col, expert;  // this block's first row and the tile's first column of the output, expert
@@ -85,11 +85,13 @@ __device__ __forceinline__ Tile tile_at(const ProdArgs& p, int idx, int width, i
 // at once (PROD_DZ, PROD_DZ_TWO).
 struct Stager {
     unsigned char* buf;
-    int lane;
-    // the last store has read the buffer
+    int lane, other;  // other: distance to the other buffer
+    // the store before the last has read its buffer
     __device__ __forceinline__ void begin()
     {
-        if (lane == 0) store_wait_read<0>();
+        buf += other;
+        other = -other;
+        if (lane == 0) store_wait_read<1>();
         __syncwarp();
     }
     __device__ __forceinline__ void put(int chunk, uint4 v) { *reinterpret_cast<uint4*>(buf + lane * 64 + ((chunk ^ ((lane >> 1) & 3)) << 4)) = v; }
@@ -197,10 +199,15 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 1) tmem_alloc<PAIR>(&tmem_sh, TMEM_COLUMNS);
+    if (threadIdx.x == 0) {
+        prefetch_map(&p.a);
+        prefetch_map(&p.b);
+    }
     tc_fence_before();
     __syncthreads();
     if (PAIR) cluster_sync();  // the other block's barriers are ready
     tc_fence_after();
+    enter();
     const uint32_t tmem = tmem_sh;
     volatile int* gave_up = &gave_up_sh;
 
@@ -329,7 +336,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
         // A warp may read the 32 lanes of its quarter only; the four warps of a quarter take the tile's pieces of 32 columns
         // in turn, a piece in two steps of 16 columns.
         const int q = warp & 3, turn = (warp - 2) >> 2;
-        Stager s{staged + (warp - 2) * OUT_BYTES, lane};
+        Stager s{staged + (warp - 2) * 2 * OUT_BYTES, lane, OUT_BYTES};
         int n_acc = 0;
         for (int idx = first_tile; idx < total; idx += step, ++n_acc) {
             const Tile t = tile_at<MODE, PAIR>(p, idx, width, rank);
@@ -354,7 +361,11 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
                     b1.fetch(bias ? bias + p.gate_rows : bias, col, p.cols, bias && gated && at < width);
                 }
             };
-            if (any) fetch(turn * 32);
+            if (any) {
+                fetch(turn * 32);
+                if ((MODE == PROD_FWD || MODE == PROD_DZ) && extra && counts)  // the rest on its way to L2
+                    for (int at = turn * 32 + ROUND; at < width && t.col + at < p.cols; at += ROUND) prefetch_l2(extra + t.col + at);
+            }
             bool ok = true;
             if (lane == 0) ok = bar_wait(&acc_full[buf], (uint32_t)(n_acc / BUFFERS) & 1u, gave_up);
             if (!__shfl_sync(0xffffffffu, ok, 0)) break;
@@ -497,29 +508,13 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
     }
 }
 
-template <bool PAIR>
-void set_cluster(cudaLaunchConfig_t* c, cudaLaunchAttribute* attr)
-{
-    attr->id = cudaLaunchAttributeClusterDimension;
-    attr->val.clusterDim.x = 2;
-    attr->val.clusterDim.y = attr->val.clusterDim.z = 1;
-    c->attrs = attr;
-    c->numAttrs = PAIR ? 1 : 0;
-    c->blockDim = dim3(THREADS);
-    c->dynamicSmemBytes = SMEM;
-}
-
 template <int MODE, bool PAIR, bool BF16>
 cudaError_t launch_as(som_layers* l, const ProdArgs& args, cudaStream_t st)
 {
     const int64_t tiles = (int64_t)args.row_tiles * args.col_tiles * (MODE == PROD_DW ? args.experts : 1);
     const int most = PAIR ? l->pairs : l->sm_count;
-    cudaLaunchConfig_t c = {};
-    cudaLaunchAttribute attr[1];
-    set_cluster<PAIR>(&c, attr);
-    c.gridDim = dim3((unsigned)(tiles < most ? tiles : most) * (PAIR ? 2 : 1));
-    c.stream = st;
-    return cudaLaunchKernelEx(&c, k_product<MODE, PAIR, BF16>, args);
+    return launch(l, k_product<MODE, PAIR, BF16>, dim3((unsigned)(tiles < most ? tiles : most) * (PAIR ? 2 : 1)), THREADS, SMEM, st,
+                  PAIR ? 2 : 1, args);
 }
 
 template <int MODE>
@@ -536,9 +531,15 @@ cudaError_t prepare_as(int* pairs)
     if (e == cudaSuccess) e = cudaFuncSetAttribute(k_product<MODE, true, BF16>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t c = {};
-    cudaLaunchAttribute attr[1];
-    set_cluster<true>(&c, attr);
     c.gridDim = dim3(2);
+    c.blockDim = dim3(THREADS);
+    c.dynamicSmemBytes = SMEM;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = 2;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    c.attrs = attr;
+    c.numAttrs = 1;
     int n = 0;
     e = cudaOccupancyMaxActiveClusters(&n, k_product<MODE, true, BF16>, &c);
     if (n < *pairs) *pairs = n;
@@ -575,10 +576,7 @@ int launch_product(som_layers* l, ProdMode mode, const ProdArgs& a, cudaStream_t
         case PROD_DX: e = launch_mode<PROD_DX>(l, a, st); break;
         default: e = launch_mode<PROD_DW>(l, a, st); break;
     }
-    ++l->launches;
-    if (e == cudaSuccess) return SOM_OK;
-    l->last_cuda_error = (int)e;
-    return SOM_ERR_CUDA;
+    return outcome(l, e);
 }
 
 }  // namespace lay

@@ -238,6 +238,7 @@ __device__ __forceinline__ uint32_t ordered16(float x)
 template <int TYPE, int V>
 __global__ void __launch_bounds__(32 * ROUTE_WARPS, V <= 8 ? 4 : 2) k_route(const RouteArgs a)
 {
+    enter();
     extern __shared__ int hist[];  // [E] when counts are wanted
     const int lane = threadIdx.x & 31, first = lane * V;
     if (a.counts) {
@@ -441,6 +442,7 @@ constexpr int QUAD_WARPS = 8, QUAD_ROWS = 8 * QUAD_WARPS;
 template <int TYPE, int L>
 __global__ void __launch_bounds__(32 * QUAD_WARPS) k_route_many(const RouteArgs a)
 {
+    enter();
     extern __shared__ int hist[];  // [E] when counts are wanted
     __shared__ uint32_t group_keys[QUAD_ROWS][33];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, quad = lane >> 2, part = lane & 3;
@@ -695,6 +697,7 @@ __device__ __forceinline__ void put_logit(void* p, int64_t i, float v)
 template <int TYPE, int V>
 __global__ void __launch_bounds__(32 * ROUTE_WARPS) k_route_backward(const RouteGradArgs a)
 {
+    enter();
     const int lane = threadIdx.x & 31;
     for (int64_t t = (int64_t)blockIdx.x * ROUTE_WARPS + (threadIdx.x >> 5); t < a.T; t += (int64_t)gridDim.x * ROUTE_WARPS) {
         const int64_t row = t * a.ld, out = t * a.E;
@@ -773,49 +776,39 @@ __global__ void __launch_bounds__(32 * ROUTE_WARPS) k_route_backward(const Route
     }
 }
 
-int done(som_layers* l, cudaError_t e)
-{
-    if (e == cudaSuccess) e = cudaGetLastError();
-    if (e == cudaSuccess) return SOM_OK;
-    l->last_cuda_error = (int)e;
-    return SOM_ERR_CUDA;
-}
-
 // the warp's registers for a row: the smallest power of two of 32 experts that holds it
 template <template <int, int> class K, int TYPE, class A>
-cudaError_t by_size(int E, const A& a, int grid, size_t smem, cudaStream_t st)
+cudaError_t by_size(som_layers* l, int E, const A& a, int grid, size_t smem, cudaStream_t st)
 {
-    if (E <= 32) return K<TYPE, 1>::go(a, grid, smem, st);
-    if (E <= 64) return K<TYPE, 2>::go(a, grid, smem, st);
-    if (E <= 128) return K<TYPE, 4>::go(a, grid, smem, st);
-    if (E <= 256) return K<TYPE, 8>::go(a, grid, smem, st);
-    if (E <= 512) return K<TYPE, 16>::go(a, grid, smem, st);
-    return K<TYPE, 32>::go(a, grid, smem, st);
+    if (E <= 32) return K<TYPE, 1>::go(l, a, grid, smem, st);
+    if (E <= 64) return K<TYPE, 2>::go(l, a, grid, smem, st);
+    if (E <= 128) return K<TYPE, 4>::go(l, a, grid, smem, st);
+    if (E <= 256) return K<TYPE, 8>::go(l, a, grid, smem, st);
+    if (E <= 512) return K<TYPE, 16>::go(l, a, grid, smem, st);
+    return K<TYPE, 32>::go(l, a, grid, smem, st);
 }
 
 template <template <int, int> class K, class A>
-cudaError_t by_type(int type, int E, const A& a, int grid, size_t smem, cudaStream_t st)
+cudaError_t by_type(som_layers* l, int type, int E, const A& a, int grid, size_t smem, cudaStream_t st)
 {
-    if (type == SOM_F32) return by_size<K, SOM_F32>(E, a, grid, smem, st);
-    if (type == SOM_F16) return by_size<K, SOM_F16>(E, a, grid, smem, st);
-    return by_size<K, SOM_BF16>(E, a, grid, smem, st);
+    if (type == SOM_F32) return by_size<K, SOM_F32>(l, E, a, grid, smem, st);
+    if (type == SOM_F16) return by_size<K, SOM_F16>(l, E, a, grid, smem, st);
+    return by_size<K, SOM_BF16>(l, E, a, grid, smem, st);
 }
 
 template <int TYPE, int V>
 struct Route {
-    static cudaError_t go(const RouteArgs& a, int grid, size_t smem, cudaStream_t st)
+    static cudaError_t go(som_layers* l, const RouteArgs& a, int grid, size_t smem, cudaStream_t st)
     {
-        k_route<TYPE, V><<<grid, 32 * ROUTE_WARPS, smem, st>>>(a);
-        return cudaGetLastError();
+        return launch(l, k_route<TYPE, V>, dim3(grid), 32 * ROUTE_WARPS, smem, st, 1, a);
     }
 };
 
 template <int TYPE, int V>
 struct RouteGrad {
-    static cudaError_t go(const RouteGradArgs& a, int grid, size_t smem, cudaStream_t st)
+    static cudaError_t go(som_layers* l, const RouteGradArgs& a, int grid, size_t smem, cudaStream_t st)
     {
-        k_route_backward<TYPE, V><<<grid, 32 * ROUTE_WARPS, smem, st>>>(a);
-        return cudaGetLastError();
+        return launch(l, k_route_backward<TYPE, V>, dim3(grid), 32 * ROUTE_WARPS, smem, st, 1, a);
     }
 };
 
@@ -829,16 +822,15 @@ int route_grid(const som_layers* l, int64_t T, int per_sm)
 }  // namespace
 
 template <int TYPE, int L>
-cudaError_t go_many(const RouteArgs& a, int grid, size_t smem, cudaStream_t st)
+cudaError_t go_many(som_layers* l, const RouteArgs& a, int grid, size_t smem, cudaStream_t st)
 {
-    k_route_many<TYPE, L><<<grid, 32 * QUAD_WARPS, smem, st>>>(a);
-    return cudaGetLastError();
+    return launch(l, k_route_many<TYPE, L>, dim3(grid), 32 * QUAD_WARPS, smem, st, 1, a);
 }
 
 template <int TYPE>
-cudaError_t route_many(const RouteArgs& a, int grid, size_t smem, cudaStream_t st)
+cudaError_t route_many(som_layers* l, const RouteArgs& a, int grid, size_t smem, cudaStream_t st)
 {
-    return a.k <= 8 ? go_many<TYPE, 8>(a, grid, smem, st) : go_many<TYPE, 16>(a, grid, smem, st);
+    return a.k <= 8 ? go_many<TYPE, 8>(l, a, grid, smem, st) : go_many<TYPE, 16>(l, a, grid, smem, st);
 }
 
 int launch_route(som_layers* l, int type, int score, int64_t T, int E, int k, const void* logits, int64_t ld, const float* bias,
@@ -858,13 +850,12 @@ int launch_route(som_layers* l, int type, int score, int64_t T, int E, int k, co
         if (T >= ROUTE_MANY && k <= 16 && (!by_groups || E / groups % 32 == 0) && (type == SOM_F32 || bias || groups == 1 || group_best == 1)) {
             const int64_t want = (T + QUAD_ROWS - 1) / QUAD_ROWS, most = (int64_t)l->sm_count * 4;
             const int blocks = (int)(want < most ? want : most);
-            e = type == SOM_F32 ? route_many<SOM_F32>(a, blocks, smem, st) : type == SOM_F16 ? route_many<SOM_F16>(a, blocks, smem, st) : route_many<SOM_BF16>(a, blocks, smem, st);
+            e = type == SOM_F32 ? route_many<SOM_F32>(l, a, blocks, smem, st) : type == SOM_F16 ? route_many<SOM_F16>(l, a, blocks, smem, st) : route_many<SOM_BF16>(l, a, blocks, smem, st);
         } else {
-            e = by_type<Route>(type, E, a, grid, smem, st);
+            e = by_type<Route>(l, type, E, a, grid, smem, st);
         }
-        ++l->launches;
     }
-    return done(l, e);
+    return outcome(l, e);
 }
 
 int launch_route_backward(som_layers* l, int type, int score, int64_t T, int E, int k, const void* logits, int64_t ld,
@@ -872,9 +863,8 @@ int launch_route_backward(som_layers* l, int type, int score, int64_t T, int E, 
 {
     if (T == 0) return SOM_OK;
     const RouteGradArgs a{logits, ld, T, indices, dweights, dlogits, E, k, score, renorm, scale, l->flags};
-    const cudaError_t e = by_type<RouteGrad>(type, E, a, route_grid(l, T, 8), 0, st);
-    ++l->launches;
-    return done(l, e);
+    const cudaError_t e = by_type<RouteGrad>(l, type, E, a, route_grid(l, T, 8), 0, st);
+    return outcome(l, e);
 }
 
 }  // namespace lay

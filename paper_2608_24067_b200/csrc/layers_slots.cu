@@ -20,6 +20,7 @@ __device__ __forceinline__ float load_weight(const void* w, int type, int64_t i)
 __global__ void __launch_bounds__(PLAN_THREADS) k_slot_plan(SlotPlan p, const int32_t* indices, const void* weights,
                                                            int weights_type, int64_t slots, int E, int* flags)
 {
+    enter();
     extern __shared__ int hist[];  // [PLAN_WARPS][E], then [E] segment starts
     __shared__ int warp_sum[PLAN_WARPS];
     int* start = hist + PLAN_WARPS * E;
@@ -97,6 +98,7 @@ constexpr int PLACE_SLOTS = 1024, PLACE_WARPS = 8;
 
 __global__ void __launch_bounds__(32 * PLACE_WARPS) k_slot_count(const int32_t* indices, int64_t slots, int E, int* counts, int* flags)
 {
+    enter();
     extern __shared__ int hist[];  // [E]
     for (int i = threadIdx.x; i < E; i += 32 * PLACE_WARPS) hist[i] = 0;
     __syncthreads();
@@ -115,6 +117,7 @@ __global__ void __launch_bounds__(32 * PLACE_WARPS) k_slot_count(const int32_t* 
 // counts[block][e] -> first place of the block's slots within expert e; the segments
 __global__ void __launch_bounds__(PLAN_THREADS) k_slot_segments(SlotPlan p, int E, int blocks, int* counts)
 {
+    enter();
     __shared__ int warp_sum[PLAN_WARPS];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, e = threadIdx.x;
     int count = 0;
@@ -155,6 +158,7 @@ __global__ void __launch_bounds__(PLAN_THREADS) k_slot_segments(SlotPlan p, int 
 __global__ void __launch_bounds__(32 * PLACE_WARPS) k_slot_place(SlotPlan p, const int32_t* indices, const void* weights, int weights_type,
                                                                 int64_t slots, int E, const int* places)
 {
+    enter();
     extern __shared__ int hist[];  // [PLACE_WARPS][E]
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     for (int i = threadIdx.x; i < PLACE_WARPS * E; i += 32 * PLACE_WARPS) hist[i] = 0;
@@ -206,6 +210,7 @@ __global__ void __launch_bounds__(32 * PLACE_WARPS) k_slot_place(SlotPlan p, con
 __global__ void __launch_bounds__(256) k_gather(SlotPlan p, int k, int D, const uint16_t* x, int64_t ldx, uint16_t* xp,
                                                 const uint16_t* dy, int64_t lddy, uint16_t* dyp)
 {
+    enter();
     const int lane = threadIdx.x & 31, chunks = D / 8, rows = *p.tiles * p.tile;
     const uint16_t* from = blockIdx.z ? dy : x;
     const int64_t ld = blockIdx.z ? lddy : ldx;
@@ -234,6 +239,7 @@ __global__ void __launch_bounds__(256) k_gather(SlotPlan p, int k, int D, const 
 __global__ void __launch_bounds__(256) k_join(const int* pos, int64_t T, int k, int D, const float* part, const uint16_t* residual,
                                               int64_t ldr, uint16_t* y, int64_t ldy, int bf16)
 {
+    enter();
     const int chunks = D / 8;
     for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < T * chunks; i += (int64_t)gridDim.x * blockDim.x) {
         const int64_t t = i / chunks;
@@ -267,6 +273,7 @@ __global__ void __launch_bounds__(256) k_dweights(const int* pos, const int32_t*
                                                   const float* dot, int parts, const uint16_t* b2, const uint16_t* dy,
                                                   int64_t lddy, void* dweights, int weights_type, int bf16)
 {
+    enter();
     const int lane = threadIdx.x & 31;
     for (int64_t s = ((int64_t)blockIdx.x * blockDim.x + threadIdx.x) >> 5; s < slots; s += ((int64_t)gridDim.x * blockDim.x) >> 5) {
         const int row = pos[s];
@@ -298,6 +305,7 @@ __global__ void __launch_bounds__(256) k_dweights(const int* pos, const int32_t*
 // a time, in a fixed order
 __global__ void __launch_bounds__(256) k_column_sums(SlotPlan p, int64_t rows, const uint16_t* v, int64_t ld, int cols, uint16_t* out, int bf16)
 {
+    enter();
     __shared__ float part[32][65];
     const int e = blockIdx.y, c = blockIdx.x * 64 + (threadIdx.x & 7) * 8, r = threadIdx.x >> 3;
     const int64_t lo = p.seg ? p.seg[e] : 0, hi = p.seg ? lo + p.count[e] : rows;
@@ -323,6 +331,7 @@ __global__ void __launch_bounds__(256) k_column_sums(SlotPlan p, int64_t rows, c
 // out[e][c] = sum of part[g][c] over the expert's groups of 32 rows (of 32-row sums); 32 columns a block, 8 groups at a time
 __global__ void __launch_bounds__(256) k_join_sums(SlotPlan p, int64_t rows, const float* part, int cols, uint16_t* out, int bf16)
 {
+    enter();
     __shared__ float sums[8][33];
     const int e = blockIdx.y, c = blockIdx.x * 32 + (threadIdx.x & 31), r = threadIdx.x >> 5;
     const int64_t lo = p.seg ? p.seg[e] / 32 : 0, hi = p.seg ? lo + (p.count[e] + 31) / 32 : (rows + 31) / 32;
@@ -336,15 +345,6 @@ __global__ void __launch_bounds__(256) k_join_sums(SlotPlan p, int64_t rows, con
         for (int i = 1; i < 8; ++i) a += sums[i][threadIdx.x & 31];
         out[(size_t)e * cols + c] = (uint16_t)pack2(a, 0.f, bf16);
     }
-}
-
-int done(som_layers* l)
-{
-    ++l->launches;
-    const cudaError_t e = cudaGetLastError();
-    if (e == cudaSuccess) return SOM_OK;
-    l->last_cuda_error = (int)e;
-    return SOM_ERR_CUDA;
 }
 
 // blocks of `per` items each, at most eight per SM: the kernels walk the rest
@@ -370,55 +370,50 @@ int launch_plan(som_layers* l, const SlotPlan& p, const int32_t* indices, const 
     const int blocks = plan_blocks(T * k);
     if (blocks == 0) {
         const size_t smem = (size_t)(PLAN_WARPS + 1) * E * sizeof(int);
-        k_slot_plan<<<1, PLAN_THREADS, smem, st>>>(p, indices, weights, weights_type, T * k, E, l->flags);
-        return done(l);
+        return outcome(l, launch(l, k_slot_plan, dim3(1), PLAN_THREADS, smem, st, 1, p, indices, weights, weights_type, T * k, E, l->flags));
     }
-    k_slot_count<<<blocks, 32 * PLACE_WARPS, (size_t)E * sizeof(int), st>>>(indices, T * k, E, p.block_counts, l->flags);
-    k_slot_segments<<<1, PLAN_THREADS, 0, st>>>(p, E, blocks, p.block_counts);
-    k_slot_place<<<blocks, 32 * PLACE_WARPS, (size_t)PLACE_WARPS * E * sizeof(int), st>>>(p, indices, weights, weights_type, T * k, E,
-                                                                                        p.block_counts);
-    l->launches += 2;
-    return done(l);
+    cudaError_t e = launch(l, k_slot_count, dim3(blocks), 32 * PLACE_WARPS, (size_t)E * sizeof(int), st, 1, indices, T * k, E, p.block_counts, l->flags);
+    if (e == cudaSuccess) e = launch(l, k_slot_segments, dim3(1), PLAN_THREADS, 0, st, 1, p, E, blocks, p.block_counts);
+    if (e == cudaSuccess)
+        e = launch(l, k_slot_place, dim3(blocks), 32 * PLACE_WARPS, (size_t)PLACE_WARPS * E * sizeof(int), st, 1, p, indices, weights, weights_type,
+                   T * k, E, p.block_counts);
+    return outcome(l, e);
 }
 
 int launch_gather(som_layers* l, const SlotPlan& p, int k, int64_t D, const void* x, int64_t ldx, void* xp, const void* dy,
                   int64_t lddy, void* dyp, cudaStream_t st)
 {
     const dim3 grid(grid_for(l, p.max_rows, 8), 1, dy ? 2 : 1);
-    k_gather<<<grid, 256, 0, st>>>(p, k, (int)D, static_cast<const uint16_t*>(x), ldx, static_cast<uint16_t*>(xp),
-                                   static_cast<const uint16_t*>(dy), lddy, static_cast<uint16_t*>(dyp));
-    return done(l);
+    return outcome(l, launch(l, k_gather, grid, 256, 0, st, 1, p, k, (int)D, static_cast<const uint16_t*>(x), ldx, static_cast<uint16_t*>(xp),
+                             static_cast<const uint16_t*>(dy), lddy, static_cast<uint16_t*>(dyp)));
 }
 
 int launch_join(som_layers* l, const SlotPlan& p, int64_t T, int k, int64_t D, const float* part, const void* residual, int64_t ldr,
                 void* y, int64_t ldy, int bf16, cudaStream_t st)
 {
-    k_join<<<grid_for(l, T * (D / 8), 256), 256, 0, st>>>(p.pos, T, k, (int)D, part, static_cast<const uint16_t*>(residual), ldr,
-                                                         static_cast<uint16_t*>(y), ldy, bf16);
-    return done(l);
+    return outcome(l, launch(l, k_join, dim3(grid_for(l, T * (D / 8), 256)), 256, 0, st, 1, p.pos, T, k, (int)D, part,
+                             static_cast<const uint16_t*>(residual), ldr, static_cast<uint16_t*>(y), ldy, bf16));
 }
 
 int launch_dweights(som_layers* l, const SlotPlan& p, const int32_t* indices, int64_t T, int k, int64_t D, const float* dot, int parts,
                     const void* b2, const void* dy, int64_t lddy, void* dweights, int weights_type, int bf16, cudaStream_t st)
 {
-    k_dweights<<<grid_for(l, T * k, 8), 256, 0, st>>>(p.pos, indices, T * k, k, (int)D, dot, parts, static_cast<const uint16_t*>(b2),
-                                                     static_cast<const uint16_t*>(dy), lddy, dweights, weights_type, bf16);
-    return done(l);
+    return outcome(l, launch(l, k_dweights, dim3(grid_for(l, T * k, 8)), 256, 0, st, 1, p.pos, indices, T * k, k, (int)D, dot, parts,
+                             static_cast<const uint16_t*>(b2), static_cast<const uint16_t*>(dy), lddy, dweights, weights_type, bf16));
 }
 
 int launch_column_sums(som_layers* l, const SlotPlan& p, int E, int64_t rows, const void* v, int64_t ld, int64_t cols, void* out,
                        int bf16, cudaStream_t st)
 {
     const dim3 grid((unsigned)((cols + 63) / 64), (unsigned)E);
-    k_column_sums<<<grid, 256, 0, st>>>(p, rows, static_cast<const uint16_t*>(v), ld, (int)cols, static_cast<uint16_t*>(out), bf16);
-    return done(l);
+    return outcome(l, launch(l, k_column_sums, grid, 256, 0, st, 1, p, rows, static_cast<const uint16_t*>(v), ld, (int)cols,
+                             static_cast<uint16_t*>(out), bf16));
 }
 
 int launch_join_sums(som_layers* l, const SlotPlan& p, int E, int64_t rows, const float* part, int64_t cols, void* out, int bf16, cudaStream_t st)
 {
     const dim3 grid((unsigned)((cols + 31) / 32), (unsigned)E);
-    k_join_sums<<<grid, 256, 0, st>>>(p, rows, part, (int)cols, static_cast<uint16_t*>(out), bf16);
-    return done(l);
+    return outcome(l, launch(l, k_join_sums, grid, 256, 0, st, 1, p, rows, part, (int)cols, static_cast<uint16_t*>(out), bf16));
 }
 
 }  // namespace lay
