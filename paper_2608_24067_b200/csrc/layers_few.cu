@@ -33,7 +33,7 @@ __device__ __forceinline__ void widen8(const uint4& w, float (&v)[8], int bf16)
 __device__ __forceinline__ uint4 stream16(const uint16_t* p)
 {
     uint4 v;
-    asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];"
+    asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];"
                  : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
                  : "l"(p));
     return v;
@@ -88,7 +88,7 @@ __global__ void __launch_bounds__(FEW_THREADS, ROWS <= 2 ? 3 : 2) k_few(const Fe
     for (int i = threadIdx.x; i < ROWS * (a.D / 8); i += FEW_THREADS) {
         const int r = ROWS == 1 ? 0 : i / (a.D / 8), q = ROWS == 1 ? i : i % (a.D / 8);
         *reinterpret_cast<uint4*>(xs + (size_t)i * 8) =
-            r < a.rows ? __ldg(reinterpret_cast<const uint4*>(a.x + (size_t)(first + r) * a.ldx) + q) : make_uint4(0u, 0u, 0u, 0u);
+            r < a.rows ? *(reinterpret_cast<const uint4*>(a.x + (size_t)(first + r) * a.ldx) + q) : make_uint4(0u, 0u, 0u, 0u);
     }
     __syncthreads();
     for (int f_block = blockIdx.x * features; f_block < a.F; f_block += stride, f += stride) {
@@ -152,8 +152,8 @@ __global__ void __launch_bounds__(FEW_THREADS, ROWS <= 2 ? 3 : 2) k_few(const Fe
                 if (HALVES == 2) u = acc[r][HALVES - 1];
             }
         if (bias) {
-            z += unpack1(__ldg(bias + f), a.bf16);
-            if (HALVES == 2) u += unpack1(__ldg(bias + a.F + f), a.bf16);
+            z += unpack1(*(bias + f), a.bf16);
+            if (HALVES == 2) u += unpack1(*(bias + a.F + f), a.bf16);
         }
         float y = 0.f;
         with_act(a.act, [&](auto tag) { y = act_of<decltype(tag)::value>(z); });
@@ -161,7 +161,7 @@ __global__ void __launch_bounds__(FEW_THREADS, ROWS <= 2 ? 3 : 2) k_few(const Fe
         if (a.hidden) {
             a.hidden[(size_t)blockIdx.y * a.F + f] = y * weight;
         } else {
-            if (a.residual) y += unpack1(__ldg(a.residual + (size_t)lane * a.ldr + f), a.bf16);
+            if (a.residual) y += unpack1(*(a.residual + (size_t)lane * a.ldr + f), a.bf16);
             a.y[(size_t)lane * a.ldy + f] = (uint16_t)pack2(y, 0.f, a.bf16);
         }
     }
@@ -257,9 +257,9 @@ __global__ void __launch_bounds__(FEW_THREADS, 3) k_few_down(const FewDownArgs a
                 if (base[j] < 0) continue;
                 const float wt = a.weights_type == SOM_F32 ? static_cast<const float*>(a.weights)[t * a.k + j]
                                                            : unpack1(static_cast<const uint16_t*>(a.weights)[t * a.k + j], a.weights_type == SOM_BF16);
-                acc = fmaf(wt, unpack1(__ldg(a.b2 + (size_t)a.indices[t * a.k + j] * a.D + d), a.bf16), acc);
+                acc = fmaf(wt, unpack1(*(a.b2 + (size_t)a.indices[t * a.k + j] * a.D + d), a.bf16), acc);
             }
-        if (a.residual) acc += unpack1(__ldg(a.residual + (size_t)t * a.ldr + d), a.bf16);
+        if (a.residual) acc += unpack1(*(a.residual + (size_t)t * a.ldr + d), a.bf16);
         a.y[(size_t)t * a.ldy + d] = (uint16_t)pack2(acc, 0.f, a.bf16);
     }
 }

@@ -28,7 +28,8 @@ namespace lay {
 
 // Every kernel of the dense operators is launched so that its blocks may come in while the kernel before it ends
 // (programmatic stream serialization), and begins with enter(): nothing is read or written before all earlier work in the
-// stream is complete, and the next kernel's launch is let through only after that.
+// stream is complete, and the next kernel's launch is let through only after that.  What such a kernel reads may have been
+// written while it was already resident, so none of them uses the read-only data path.
 __device__ __forceinline__ void enter()
 {
     asm volatile("griddepcontrol.wait;" ::: "memory");

@@ -35,7 +35,7 @@ __device__ __forceinline__ float unpack1(uint16_t v, int bf16)
 // eight consecutive 16-bit values, 16-byte aligned
 __device__ __forceinline__ void load8(const uint16_t* p, float (&v)[8], int bf16)
 {
-    const uint4 w = __ldg(reinterpret_cast<const uint4*>(p));
+    const uint4 w = *(reinterpret_cast<const uint4*>(p));
     const float2 a = unpack2(w.x, bf16), b = unpack2(w.y, bf16), c = unpack2(w.z, bf16), d = unpack2(w.w, bf16);
     v[0] = a.x, v[1] = a.y, v[2] = b.x, v[3] = b.y, v[4] = c.x, v[5] = c.y, v[6] = d.x, v[7] = d.y;
 }

@@ -127,7 +127,7 @@ struct Row16 {
     {
 #pragma unroll
         for (int j = 0; j < 2; ++j)
-            w[j] = want && col + 8 * j < cols ? __ldg(reinterpret_cast<const uint4*>(row + col) + j) : make_uint4(0u, 0u, 0u, 0u);
+            w[j] = want && col + 8 * j < cols ? *(reinterpret_cast<const uint4*>(row + col) + j) : make_uint4(0u, 0u, 0u, 0u);
     }
     template <bool BF16>
     __device__ __forceinline__ void get(float (&v)[16]) const

@@ -23,8 +23,8 @@ constexpr int ROUTE_WARPS = 8;
 template <int TYPE>
 __device__ __forceinline__ float logit_at(const void* p, int64_t i)
 {
-    if (TYPE == SOM_F32) return __ldg(static_cast<const float*>(p) + i);
-    return unpack1(__ldg(static_cast<const uint16_t*>(p) + i), TYPE == SOM_BF16);
+    if (TYPE == SOM_F32) return static_cast<const float*>(p)[i];
+    return unpack1(static_cast<const uint16_t*>(p)[i], TYPE == SOM_BF16);
 }
 
 __device__ __forceinline__ float from_ordered(uint32_t u)
@@ -72,14 +72,14 @@ __device__ __forceinline__ void load_row(const void* p, int64_t row, int at, int
         if (WORDS >= 4) {
 #pragma unroll
             for (int i = 0; i < WORDS / 4; ++i) {
-                const uint4 u = __ldg(reinterpret_cast<const uint4*>(q) + i);
+                const uint4 u = *(reinterpret_cast<const uint4*>(q) + i);
                 w[4 * i] = u.x, w[4 * i + 1] = u.y, w[4 * i + 2] = u.z, w[4 * i + 3] = u.w;
             }
         } else if (WORDS == 2) {
-            const uint2 u = __ldg(reinterpret_cast<const uint2*>(q));
+            const uint2 u = *(reinterpret_cast<const uint2*>(q));
             w[0] = u.x, w[WORDS > 1 ? 1 : 0] = u.y;
         } else {
-            w[0] = __ldg(reinterpret_cast<const uint32_t*>(q));
+            w[0] = *(reinterpret_cast<const uint32_t*>(q));
         }
 #pragma unroll
         for (int v = 0; v < V; ++v) {
@@ -142,7 +142,7 @@ __device__ __noinline__ int choose_exact(const RouteArgs& a, int64_t row, float 
                     continue;
                 }
                 s = (float)((soft ? e : 1.0) / (soft ? sum : 1.0 + e));
-                if (a.bias && first + v < a.E) s += __ldg(a.bias + first + v);
+                if (a.bias && first + v < a.E) s += *(a.bias + first + v);
             }
             key[v] = live && s == s ? som_ordered_bits(s + 0.f) : 0u;  // + 0: the two zeros tie
         }
@@ -260,7 +260,7 @@ __global__ void __launch_bounds__(32 * ROUTE_WARPS, V <= 8 ? 4 : 2) k_route(cons
     float high = 0.f, low = 0.f;  // of the biases, with 0 among them
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-        bias[v] = a.bias && first + v < a.E ? __ldg(a.bias + first + v) : 0.f;
+        bias[v] = a.bias && first + v < a.E ? *(a.bias + first + v) : 0.f;
         high = fmaxf(high, bias[v]);
         low = fminf(low, bias[v]);
     }
@@ -366,7 +366,7 @@ __global__ void __launch_bounds__(32 * ROUTE_WARPS, V <= 8 ? 4 : 2) k_route(cons
                 at = won ? (int)(INDEX_MASK - (won & INDEX_MASK)) : -1;
                 if (!exact16) {
                     const float mx = at >= 0 ? logit_at<TYPE>(a.logits, row + at) + 0.f : 0.f;
-                    const float mb = at >= 0 && a.bias ? __ldg(a.bias + at) : 0.f;
+                    const float mb = at >= 0 && a.bias ? *(a.bias + at) : 0.f;
                     const uint32_t above = __shfl_up_sync(ALL, won, 1);
                     const float ax = __shfl_up_sync(ALL, mx, 1), ab = __shfl_up_sync(ALL, mb, 1);
                     // Equal logits and biases tie exactly, and the index decided.  (Not between the last one taken and the
@@ -460,7 +460,7 @@ __global__ void __launch_bounds__(32 * QUAD_WARPS) k_route_many(const RouteArgs 
     if (a.bias) {
         float high = 0.f, low = 0.f;
         for (int i = lane; i < a.E; i += 32) {
-            const float b = __ldg(a.bias + i);
+            const float b = *(a.bias + i);
             high = fmaxf(high, b);
             low = fminf(low, b);
         }

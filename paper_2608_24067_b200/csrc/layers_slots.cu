@@ -10,8 +10,8 @@ constexpr int PLAN_THREADS = 1024, PLAN_WARPS = PLAN_THREADS / 32;
 
 __device__ __forceinline__ float load_weight(const void* w, int type, int64_t i)
 {
-    if (type == SOM_F32) return __ldg(static_cast<const float*>(w) + i);
-    return unpack1(__ldg(static_cast<const uint16_t*>(w) + i), type == SOM_BF16);
+    if (type == SOM_F32) return static_cast<const float*>(w)[i];
+    return unpack1(static_cast<const uint16_t*>(w)[i], type == SOM_BF16);
 }
 
 // A stable counting sort of the slots by expert in one block: every warp owns a contiguous run of slots, counts it into a
@@ -222,13 +222,13 @@ __global__ void __launch_bounds__(256) k_gather(SlotPlan p, int k, int D, const 
             const uint4* in = reinterpret_cast<const uint4*>(from + (size_t)(p.row_slot[row] / k) * ld);
             int c = lane;
             for (; c + 96 < chunks; c += 128) {
-                const uint4 u0 = __ldg(in + c), u1 = __ldg(in + c + 32), u2 = __ldg(in + c + 64), u3 = __ldg(in + c + 96);
+                const uint4 u0 = *(in + c), u1 = *(in + c + 32), u2 = *(in + c + 64), u3 = *(in + c + 96);
                 out[c] = u0;
                 out[c + 32] = u1;
                 out[c + 64] = u2;
                 out[c + 96] = u3;
             }
-            for (; c < chunks; c += 32) out[c] = __ldg(in + c);
+            for (; c < chunks; c += 32) out[c] = *(in + c);
         } else if (place < ((n + 63) & ~63)) {
             for (int c = lane; c < chunks; c += 32) out[c] = make_uint4(0u, 0u, 0u, 0u);
         }
