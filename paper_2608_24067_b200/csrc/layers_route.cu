@@ -416,17 +416,21 @@ __global__ void __launch_bounds__(32 * ROUTE_WARPS, V <= 8 ? 4 : 2) k_route(cons
 //
 // Four lanes a token, eight tokens a warp: the rounds of the warp-wide choice cost the same instructions for one token as
 // this form spends on eight.  A lane takes the row's experts in pieces of eight (its eight of every 32), sorts a piece and
-// merges it into its list of the L largest keys; two exchanges make the four lanes' lists one.  The largest key that fell out
-// is kept for the certificate.  With groups the first walk finds the groups' keys and the second one walks only the chosen
-// groups.  Tokens that the certificate cannot settle are done by the whole warp from exact keys, as above.
+// merges it into its list of the L largest keys; two exchanges make the four lanes' lists one.  The two largest keys that fell
+// out are kept for the certificate.  With groups the first walk finds the groups' keys and the second one walks only the chosen
+// groups.  What the certificate leaves open, the whole warp settles for one token at a time: contested groups by their exact
+// keys, and contested places by the exact keys of the list, one candidate a lane.  Only where the contest reaches beyond the
+// list, or scores need a sum over all experts, are all keys of the token computed exactly.
 
-// a (descending) becomes the L largest of a and b (descending), descending; `rest`: the largest of those left out
+// a (descending) becomes the L largest of a and b (descending), descending; rest >= rest2: the largest of those left out
 template <int L>
-__device__ __forceinline__ void merge_down(uint32_t (&a)[L], const uint32_t (&b)[L], uint32_t& rest)
+__device__ __forceinline__ void merge_down(uint32_t (&a)[L], const uint32_t (&b)[L], uint32_t& rest, uint32_t& rest2)
 {
 #pragma unroll
     for (int i = 0; i < L; ++i) {
-        rest = max(rest, min(a[i], b[L - 1 - i]));
+        const uint32_t out = min(a[i], b[L - 1 - i]);
+        rest2 = max(rest2, min(rest, out));
+        rest = max(rest, out);
         a[i] = max(a[i], b[L - 1 - i]);
     }
 #pragma unroll
@@ -434,6 +438,49 @@ __device__ __forceinline__ void merge_down(uint32_t (&a)[L], const uint32_t (&b)
 #pragma unroll
         for (int i = 0; i < L; ++i)
             if (!(i & h)) order2(a[i], a[i + h]);
+}
+
+// The exact key of one expert as an order-preserving integer, where it needs no other expert: a logit, or sigmoid + bias.
+template <int TYPE>
+__device__ __noinline__ uint32_t exact_key(const RouteArgs& a, int64_t row, int i, bool by_score)
+{
+    const float x = logit_at<TYPE>(a.logits, row + i);
+    float s = x;
+    if (by_score) {
+        s = (float)(1.0 / (1.0 + exp(-(double)x)));
+        if (a.bias) s += a.bias[i];
+    }
+    return x > -INFINITY && s == s ? som_ordered_bits(s + 0.f) : 0u;
+}
+
+// Which groups are kept, by one warp for one token: lane g holds the key of group g; `low` and `next` are the smallest key
+// kept and the largest one dropped, nearer than `margin`.  Groups beyond the margin on either side stay where they are.
+template <int TYPE>
+__device__ __noinline__ unsigned settle_groups(const RouteArgs& a, int64_t row, uint32_t key, uint32_t low, uint32_t next, uint32_t margin, int lane)
+{
+    const bool there = lane < a.groups && key;
+    const bool above = there && key >= next + margin, open = there && !above && key + margin > low;
+    unsigned kept = __ballot_sync(ALL, above), todo = __ballot_sync(ALL, open);
+    const int size = a.E / a.groups;
+    uint32_t mine = 0;
+    for (unsigned left = todo; left; left &= left - 1) {
+        const int g = __ffs(left) - 1;
+        uint32_t m1 = 0, m2 = 0;
+#pragma unroll 1
+        for (int i = lane; i < size; i += 32) merge2(m1, m2, exact_key<TYPE>(a, row, g * size + i, true), 0u);
+        const uint32_t b1 = __reduce_max_sync(ALL, m1);
+        const int owner = __ffs(__ballot_sync(ALL, m1 == b1)) - 1;
+        const uint32_t b2 = __reduce_max_sync(ALL, lane == owner ? m2 : m1);
+        if (lane == g) mine = group_key(b1, b2, a.group_best);
+    }
+    for (int n = a.top_groups - __popc(kept); n > 0; --n) {
+        const uint32_t m = __reduce_max_sync(ALL, open ? mine : 0u);
+        if (m == 0) break;
+        const int g = __ffs(__ballot_sync(ALL, open && mine == m)) - 1;
+        kept |= 1u << g;
+        if (lane == g) mine = 0;
+    }
+    return kept;
 }
 
 constexpr int ROUTE_MANY = 1024;  // tokens from which on k_route_many is used
@@ -506,7 +553,7 @@ __global__ void __launch_bounds__(32 * QUAD_WARPS) k_route_many(const RouteArgs 
             total += __shfl_xor_sync(ALL, total, 1);
             total += __shfl_xor_sync(ALL, total, 2);
         }
-        bool sure = packs && top < INFINITY;
+        bool full = !(packs && top < INFINITY);  // all keys have to be computed exactly
         auto keys_of = [&](int piece, uint32_t (&key)[8]) {
             const int at = piece * 32 + part * 8;
             float x[8];
@@ -553,7 +600,7 @@ __global__ void __launch_bounds__(32 * QUAD_WARPS) k_route_many(const RouteArgs 
                 lone |= m1 && !m2;  // a lone expert's distance is not comparable with the sum of two
                 if (part == 0) mine[g] = a.group_best == 2 ? (m1 >> INDEX_BITS) + (m2 >> INDEX_BITS) : m1;
             }
-            if (a.group_best == 2 && lone) sure = false;
+            if (a.group_best == 2 && lone) full = true;
             __syncwarp();
             uint32_t low = 0xffffffffu, next = 0u;  // of the groups kept and of the others, this lane's quarter
             for (int g = part; g < a.groups; g += 4) {
@@ -573,13 +620,26 @@ __global__ void __launch_bounds__(32 * QUAD_WARPS) k_route_many(const RouteArgs 
                 low = min(low, __shfl_xor_sync(ALL, low, d));
                 next = max(next, __shfl_xor_sync(ALL, next, d));
             }
-            __syncwarp();  // the keys have been read: the next token may write its own
-            if (!exact16 && low && next) {
-                if (a.group_best == 2) sure = sure && low - next >= 2 * margin;
-                else sure = sure && (low >> INDEX_BITS) - (next >> INDEX_BITS) >= margin;
+            if (!exact16) {
+                const uint32_t apart = a.group_best == 2 ? 2 * margin : margin;
+                const int shift = a.group_best == 2 ? 0 : INDEX_BITS;
+                const bool open = !full && low != 0xffffffffu && low && next && (low >> shift) - (next >> shift) < apart;
+                if (a.score == SOM_SCORE_SOFTMAX || !by_score) {
+                    full |= open;
+                } else {
+                    for (unsigned todo = __ballot_sync(ALL, open && part == 0); todo; todo &= todo - 1) {
+                        const int who = __ffs(todo) - 1;
+                        const int64_t its_row = __shfl_sync(ALL, row, who);
+                        const uint32_t its_low = __shfl_sync(ALL, low, who) >> shift, its_next = __shfl_sync(ALL, next, who) >> shift;
+                        const unsigned got = settle_groups<TYPE>(a, its_row, lane < a.groups ? group_keys[warp * 8 + (who >> 2)][lane] >> shift : 0u,
+                                                                 its_low, its_next, apart, lane);
+                        if (quad == who >> 2) kept = got;
+                    }
+                }
             }
+            __syncwarp();  // the keys have been read: the next token may write its own
         }
-        uint32_t list[L], rest = 0;
+        uint32_t list[L], rest = 0, rest2 = 0;
 #pragma unroll
         for (int i = 0; i < L; ++i) list[i] = 0u;
         const int walk = by_groups ? a.top_groups * per_group : pieces;
@@ -588,7 +648,7 @@ __global__ void __launch_bounds__(32 * QUAD_WARPS) k_route_many(const RouteArgs 
         for (int b = 0; b < walk; ++b) {
             int piece = b;
             if (by_groups) {  // (each token walks its own groups)
-                piece = (__ffs(left) - 1) * per_group + within;
+                piece = left ? (__ffs(left) - 1) * per_group + within : pieces;  // (beyond the row: no experts)
                 if (++within == per_group) within = 0, left &= left - 1;
             }
             uint32_t key[8], more[L];
@@ -596,33 +656,70 @@ __global__ void __launch_bounds__(32 * QUAD_WARPS) k_route_many(const RouteArgs 
             sort_down<8>(key);
 #pragma unroll
             for (int i = 0; i < L; ++i) more[i] = i < 8 ? key[i] : 0u;
-            merge_down<L>(list, more, rest);
+            merge_down<L>(list, more, rest, rest2);
         }
 #pragma unroll
         for (int d = 1; d <= 2; d <<= 1) {
             uint32_t more[L];
 #pragma unroll
             for (int i = 0; i < L; ++i) more[i] = __shfl_xor_sync(ALL, list[i], d);
-            rest = max(rest, __shfl_xor_sync(ALL, rest, d));
-            merge_down<L>(list, more, rest);
-        }
-        if (!exact16) {
-#pragma unroll
-            for (int i = 0; i < L; ++i) {
-                const uint32_t next = i + 1 < L ? list[i + 1 < L ? i + 1 : i] : rest;
-                if (i < a.k && list[i])
-                    sure = sure && (list[i] >> INDEX_BITS) > 1u && (!next || (list[i] >> INDEX_BITS) - (next >> INDEX_BITS) >= margin);
-            }
+            const uint32_t r1 = __shfl_xor_sync(ALL, rest, d), r2 = __shfl_xor_sync(ALL, rest2, d);
+            merge2(rest, rest2, r1, r2);
+            merge_down<L>(list, more, rest, rest2);
         }
         int at[L];
 #pragma unroll
         for (int i = 0; i < L; ++i) at[i] = i < a.k && list[i] ? (int)(INDEX_MASK - (list[i] & INDEX_MASK)) : -1;
-        unsigned redo = __ballot_sync(ALL, !sure && part == 0 && t0 + quad < a.T);
-        while (redo) {
-            const int who = __ffs(redo) - 1;
-            redo &= redo - 1;
-            const int64_t its_row = (t0 + (who >> 2)) * a.ld;
-            const int got = choose_exact<TYPE>(a, its_row, __shfl_sync(ALL, top, who), by_score, by_groups, lane);
+        const bool there = t0 + quad < a.T;
+        if (!exact16) {
+            bool near = false;
+#pragma unroll
+            for (int i = 0; i < L; ++i) {
+                const uint32_t next = i + 1 < L ? list[i + 1 < L ? i + 1 : i] : rest;
+                if (i < a.k && list[i]) {
+                    near |= next && (list[i] >> INDEX_BITS) - (next >> INDEX_BITS) < margin;
+                    full |= (list[i] >> INDEX_BITS) <= 1u;  // beyond the keys' range
+                }
+            }
+            if (by_score && a.score == SOM_SCORE_SOFTMAX) full |= near;
+            for (unsigned todo = __ballot_sync(ALL, near && !full && there && part == 0); todo; todo &= todo - 1) {
+                const int who = __ffs(todo) - 1;
+                uint32_t mine = __shfl_sync(ALL, rest, who), next = __shfl_sync(ALL, rest2, who);  // lanes 0 to L: the candidates
+#pragma unroll
+                for (int i = 0; i < L; ++i) {
+                    const uint32_t v = __shfl_sync(ALL, list[i], who);
+                    if (lane == i) mine = v;
+                }
+                const uint32_t below = __shfl_down_sync(ALL, mine, 1);
+                if (lane < L) next = below;
+                // the contest for the last place has to end within the list
+                const unsigned clear = __ballot_sync(ALL, lane <= L && (!next || (mine >> INDEX_BITS) - (next >> INDEX_BITS) >= margin));
+                if (!(clear >> (a.k - 1))) {
+                    if (quad == who >> 2) full = true;
+                    continue;
+                }
+                const int index = (int)(INDEX_MASK - (mine & INDEX_MASK));
+                const int64_t its_row = __shfl_sync(ALL, row, who);
+                uint32_t key = 0;
+                if (lane <= L && mine) key = exact_key<TYPE>(a, its_row, index, by_score);
+                __syncwarp();
+                int rank = 0;
+                for (int i = 0; i <= L; ++i) {
+                    const uint32_t k = __shfl_sync(ALL, key, i);
+                    const int o = __shfl_sync(ALL, index, i);
+                    rank += k > key || (k == key && k && o < index);
+                }
+#pragma unroll
+                for (int i = 0; i < L; ++i) {
+                    const unsigned is = __ballot_sync(ALL, key && rank == i);
+                    const int v = __shfl_sync(ALL, index, is ? __ffs(is) - 1 : 0);
+                    if (quad == who >> 2) at[i] = i < a.k && is ? v : -1;
+                }
+            }
+        }
+        for (unsigned todo = __ballot_sync(ALL, full && part == 0 && there); todo; todo &= todo - 1) {
+            const int who = __ffs(todo) - 1;
+            const int got = choose_exact<TYPE>(a, __shfl_sync(ALL, row, who), __shfl_sync(ALL, top, who), by_score, by_groups, lane);
 #pragma unroll
             for (int i = 0; i < L; ++i) {
                 const int v = __shfl_sync(ALL, got, i);

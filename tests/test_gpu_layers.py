@@ -234,6 +234,21 @@ def test_route_order_of_near_scores(L):
         assert torch.equal(L.route(z.cuda(), 5, score=score, bias=bias.cuda())["indices"].cpu().long(), at)
 
 
+@pytest.mark.parametrize("groups,top_groups,group_best", [(1, 1, 1), (4, 2, 2), (4, 3, 1)])
+@pytest.mark.parametrize("score,spread", [("sigmoid", 2.0 ** -22), ("sigmoid", 2.0 ** -18), ("softmax", 2.0 ** -20)])
+def test_route_many_near_scores(L, score, spread, groups, top_groups, group_best):
+    """The same for many tokens: values from a coarse grid plus noise far below it, so that choices, boundaries and groups are
+    contested in every token, some by two experts and some by many."""
+    gen = torch.Generator().manual_seed(7)
+    T, E, k = 1040, 128, 8
+    z = (torch.randn(T, E, generator=gen) * 4).round() / 4 + torch.randn(T, E, generator=gen) * spread
+    bias = (torch.randn(E, generator=gen) * 4).round() / 64
+    got = L.route(z.cuda(), k, score=score, bias=bias.cuda(), groups=groups, top_groups=top_groups, group_best=group_best)
+    some = torch.arange(0, T, 3)
+    _, at, _, _ = ref.route(z[some], k, score, bias, groups, top_groups, group_best, True, 1.0)
+    assert torch.equal(got["indices"][some].cpu().long(), at)
+
+
 @pytest.mark.parametrize("T,E,k", [(1, 4, 2), (33, 36, 4), (70, 100, 6), (9, 256, 12), (4, 1024, 32), (2, 1, 1)])
 @pytest.mark.parametrize("score", ["softmax", "sigmoid"])
 @pytest.mark.parametrize("renorm", [True, False])
