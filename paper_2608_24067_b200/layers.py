@@ -20,22 +20,25 @@ _ACTS = {"none": 0, "relu": 1, "gelu": 2, "silu": 3}
 _SCORES = {"softmax": 0, "sigmoid": 1}
 
 
-def _matrix(t, shape, dtype, name):
+def _matrix(t, rows, cols, dtype, name):
     """(address, distance of rows) of a [rows][cols] tensor."""
-    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype != dtype or t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+    if t.dtype is not dtype or not t.is_cuda:
         raise TypeError("%s must be a 2-d CUDA tensor of %s with contiguous rows" % (name, dtype))
-    if tuple(t.shape) != shape:
-        raise ValueError("%s must have shape %s, not %s" % (name, shape, tuple(t.shape)))
-    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else t.shape[1]
+    if t.shape != (rows, cols):
+        raise ValueError("%s must have shape %s, not %s" % (name, (rows, cols), tuple(t.shape)))
+    far, near = t.stride()
+    if near != 1 and cols > 1:
+        raise TypeError("%s must be a 2-d CUDA tensor of %s with contiguous rows" % (name, dtype))
+    return t.data_ptr(), far if rows > 1 else cols
 
 
 def _whole(t, shape, dtype, name):
     """Address of a contiguous tensor; 0 for None."""
     if t is None:
         return 0
-    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype != dtype or not t.is_contiguous():
+    if t.dtype is not dtype or not t.is_cuda or not t.is_contiguous():
         raise TypeError("%s must be a contiguous CUDA tensor of %s" % (name, dtype))
-    if tuple(t.shape) != shape:
+    if t.shape != shape:
         raise ValueError("%s must have shape %s, not %s" % (name, shape, tuple(t.shape)))
     return t.data_ptr()
 
@@ -75,89 +78,91 @@ class Layers:
             return _raw_stream(self.device.index)
         return torch.cuda.current_stream(self.device).cuda_stream
 
-    def _half(self, x, name="x"):
+    def _half(self, x):
+        """The type code of x, which has to be a 16-bit matrix on the handle's device."""
         if not isinstance(x, torch.Tensor) or x.dtype not in (torch.float16, torch.bfloat16) or x.dim() != 2:
-            raise TypeError("%s must be a 2-d float16 or bfloat16 CUDA tensor" % name)
+            raise TypeError("x must be a 2-d float16 or bfloat16 CUDA tensor")
         if x.device != self.device:
-            raise ValueError("%s is on %s, the handle on %s" % (name, x.device, self.device))
+            raise ValueError("x is on %s, the handle on %s" % (x.device, self.device))
         return _TYPES[x.dtype]
+
+    def _unit(self, x, weight, bias, gated):
+        """What linear and its gradient share: type, T, D, F and the rows of weight, addresses."""
+        kind = self._half(x)
+        T, D = x.shape
+        if weight.dim() != 2:
+            raise ValueError("weight must be 2-d")
+        rows = weight.shape[0]
+        if gated and rows % 2:
+            raise ValueError("a gated weight has an even number of rows")
+        xp, ldx = _matrix(x, T, D, x.dtype, "x")
+        return (kind, T, D, rows // 2 if gated else rows, rows, xp, ldx, _whole(weight, (rows, D), x.dtype, "weight"),
+                0 if bias is None else _whole(bias, (rows,), x.dtype, "bias"))
 
     def linear(self, x, weight, bias=None, residual=None, act="none", gated=False, out=None, stream=None):
         """som_linear: act(x weight^T + bias) + residual; gated: weight's first half of rows is activated and multiplies
         the products of the second.  Returns [T, F]."""
-        kind = self._half(x)
-        if weight.dim() != 2:
-            raise ValueError("weight must be 2-d")
-        T, D = x.shape
-        rows = weight.shape[0]
-        if gated and rows % 2:
-            raise ValueError("a gated weight has an even number of rows")
-        F = rows // 2 if gated else rows
-        xp, ldx = _matrix(x, (T, D), x.dtype, "x")
+        kind, T, D, F, rows, xp, ldx, wp, bp = self._unit(x, weight, bias, gated)
         if out is None:
             out = x.new_empty((T, F))
-        yp, ldy = _matrix(out, (T, F), x.dtype, "out")
-        rp, ldr = (0, 0) if residual is None else _matrix(residual, (T, F), x.dtype, "residual")
-        rc = self._lib.som_linear(self._h, kind, _code(_ACTS, act, "act"), int(gated), T, D, F, xp, ldx,
-                                  _whole(weight, (rows, D), x.dtype, "weight"), _whole(bias, (rows,), x.dtype, "bias"),
-                                  rp, ldr, yp, ldy, self._stream(stream))
-        self._check(rc, "som_linear")
+            yp, ldy = out.data_ptr(), F
+        else:
+            yp, ldy = _matrix(out, T, F, x.dtype, "out")
+        rp, ldr = (0, 0) if residual is None else _matrix(residual, T, F, x.dtype, "residual")
+        rc = self._lib.som_linear(self._h, kind, _code(_ACTS, act, "act"), bool(gated), T, D, F, xp, ldx, wp, bp, rp, ldr, yp, ldy,
+                                  self._stream(stream))
+        if rc:
+            self._check(rc, "som_linear")
         return out
 
     def linear_backward(self, x, weight, dy, bias=None, act="none", gated=False, stream=None):
         """som_linear_backward: {"dx", "dweight"} and, with a bias, "dbias" (the residual's gradient is dy)."""
-        kind = self._half(x)
-        if weight.dim() != 2:
-            raise ValueError("weight must be 2-d")
-        T, D = x.shape
-        rows = weight.shape[0]
-        if gated and rows % 2:
-            raise ValueError("a gated weight has an even number of rows")
-        F = rows // 2 if gated else rows
-        xp, ldx = _matrix(x, (T, D), x.dtype, "x")
-        gp, ldg = _matrix(dy, (T, F), x.dtype, "dy")
-        wp = _whole(weight, (rows, D), x.dtype, "weight")
+        kind, T, D, F, rows, xp, ldx, wp, bp = self._unit(x, weight, bias, gated)
+        gp, ldg = _matrix(dy, T, F, x.dtype, "dy")
         out = {"dx": x.new_empty((T, D)), "dweight": x.new_empty((rows, D))}
         if bias is not None:
             out["dbias"] = x.new_empty((rows,))
-        rc = self._lib.som_linear_backward(self._h, kind, _code(_ACTS, act, "act"), int(gated), T, D, F, xp, ldx, wp,
-                                           _whole(bias, (rows,), x.dtype, "bias"), gp, ldg, out["dx"].data_ptr(),
-                                           out["dweight"].data_ptr(), out["dbias"].data_ptr() if bias is not None else 0,
-                                           self._stream(stream))
-        self._check(rc, "som_linear_backward")
+        rc = self._lib.som_linear_backward(self._h, kind, _code(_ACTS, act, "act"), bool(gated), T, D, F, xp, ldx, wp, bp, gp, ldg,
+                                           out["dx"].data_ptr(), out["dweight"].data_ptr(),
+                                           out["dbias"].data_ptr() if bias is not None else 0, self._stream(stream))
+        if rc:
+            self._check(rc, "som_linear_backward")
         return out
+
+    def _logits(self, logits):
+        """Type code, T, E, address and distance of rows."""
+        if not isinstance(logits, torch.Tensor) or logits.dim() != 2:
+            raise TypeError("logits must be a 2-d CUDA tensor")
+        kind = _code(_TYPES, logits.dtype, "logits' type")
+        if logits.device != self.device:
+            raise ValueError("logits are on %s, the handle on %s" % (logits.device, self.device))
+        T, E = logits.shape
+        return (kind, T, E, *_matrix(logits, T, E, logits.dtype, "logits"))
 
     def route(self, logits, k, score="softmax", bias=None, groups=1, top_groups=1, group_best=1, renorm=True, scale=1.0,
               stream=None):
         """som_route: {"weights" fp32 [T, k], "indices" int32 [T, k], "counts" int32 [E]}."""
-        if not isinstance(logits, torch.Tensor) or logits.dim() != 2:
-            raise TypeError("logits must be a 2-d CUDA tensor")
-        T, E = logits.shape
-        lp, ld = _matrix(logits, (T, E), logits.dtype, "logits")
-        kind = _code(_TYPES, logits.dtype, "logits' type")
-        out = {"weights": logits.new_empty((T, k), dtype=torch.float32), "indices": logits.new_empty((T, k), dtype=torch.int32),
-               "counts": logits.new_empty((E,), dtype=torch.int32)}
+        kind, T, E, lp, ld = self._logits(logits)
+        new = logits.new_empty
+        weights, indices, counts = new((T, k), dtype=torch.float32), new((T, k), dtype=torch.int32), new((E,), dtype=torch.int32)
         rc = self._lib.som_route(self._h, kind, _code(_SCORES, score, "score"), T, E, k, lp, ld,
-                                 _whole(bias, (E,), torch.float32, "bias"), groups, top_groups, group_best, int(renorm), scale,
-                                 out["weights"].data_ptr(), out["indices"].data_ptr(), out["counts"].data_ptr(),
-                                 self._stream(stream))
-        self._check(rc, "som_route")
-        return out
+                                 0 if bias is None else _whole(bias, (E,), torch.float32, "bias"), groups, top_groups, group_best,
+                                 bool(renorm), scale, weights.data_ptr(), indices.data_ptr(), counts.data_ptr(), self._stream(stream))
+        if rc:
+            self._check(rc, "som_route")
+        return {"weights": weights, "indices": indices, "counts": counts}
 
     def route_backward(self, logits, indices, dweights, score="softmax", renorm=True, scale=1.0, stream=None):
         """som_route_backward: the logits' gradient [T, E]."""
-        if not isinstance(logits, torch.Tensor) or logits.dim() != 2:
-            raise TypeError("logits must be a 2-d CUDA tensor")
-        T, E = logits.shape
-        lp, ld = _matrix(logits, (T, E), logits.dtype, "logits")
-        kind = _code(_TYPES, logits.dtype, "logits' type")
+        kind, T, E, lp, ld = self._logits(logits)
         k = indices.shape[-1]
         out = logits.new_empty((T, E))
         rc = self._lib.som_route_backward(self._h, kind, _code(_SCORES, score, "score"), T, E, k, lp, ld,
                                           _whole(indices, (T, k), torch.int32, "indices"),
-                                          _whole(dweights, (T, k), torch.float32, "dweights"), int(renorm), scale,
+                                          _whole(dweights, (T, k), torch.float32, "dweights"), bool(renorm), scale,
                                           out.data_ptr(), self._stream(stream))
-        self._check(rc, "som_route_backward")
+        if rc:
+            self._check(rc, "som_route_backward")
         return out
 
     def _experts(self, x, indices, weights, w1, w2, b1, b2, gated):
@@ -170,41 +175,46 @@ class Layers:
             raise ValueError("a gated w1 has an even number of rows")
         I = rows // 2 if gated else rows
         k = indices.shape[1]
-        if weights.dtype not in (torch.float32, x.dtype):
+        t, wt = x.dtype, weights.dtype
+        if wt is not torch.float32 and wt is not t:
             raise TypeError("weights must be float32 or of x's type")
-        xp, ldx = _matrix(x, (T, D), x.dtype, "x")
+        xp, ldx = _matrix(x, T, D, t, "x")
         return kind, T, E, k, D, I, rows, (xp, ldx, _whole(indices, (T, k), torch.int32, "indices"),
-                                           _whole(weights, (T, k), weights.dtype, "weights"), _TYPES[weights.dtype],
-                                           _whole(w1, (E, rows, D), x.dtype, "w1"), _whole(b1, (E, rows), x.dtype, "b1"),
-                                           _whole(w2, (E, D, I), x.dtype, "w2"), _whole(b2, (E, D), x.dtype, "b2"))
+                                           _whole(weights, (T, k), wt, "weights"), _TYPES[wt],
+                                           _whole(w1, (E, rows, D), t, "w1"), _whole(b1, (E, rows), t, "b1"),
+                                           _whole(w2, (E, D, I), t, "w2"), _whole(b2, (E, D), t, "b2"))
 
     def experts(self, x, indices, weights, w1, w2, b1=None, b2=None, residual=None, act="silu", gated=True, out=None, stream=None):
         """som_experts: residual + sum over a token's experts of weight * (w2 act(w1 x + b1) + b2).  Returns [T, D]."""
         kind, T, E, k, D, I, rows, p = self._experts(x, indices, weights, w1, w2, b1, b2, gated)
         if out is None:
             out = x.new_empty((T, D))
-        yp, ldy = _matrix(out, (T, D), x.dtype, "out")
-        rp, ldr = (0, 0) if residual is None else _matrix(residual, (T, D), x.dtype, "residual")
-        rc = self._lib.som_experts(self._h, kind, _code(_ACTS, act, "act"), int(gated), T, E, k, D, I, *p, rp, ldr, yp, ldy,
+            yp, ldy = out.data_ptr(), D
+        else:
+            yp, ldy = _matrix(out, T, D, x.dtype, "out")
+        rp, ldr = (0, 0) if residual is None else _matrix(residual, T, D, x.dtype, "residual")
+        rc = self._lib.som_experts(self._h, kind, _code(_ACTS, act, "act"), bool(gated), T, E, k, D, I, *p, rp, ldr, yp, ldy,
                                    self._stream(stream))
-        self._check(rc, "som_experts")
+        if rc:
+            self._check(rc, "som_experts")
         return out
 
     def experts_backward(self, x, indices, weights, w1, w2, dy, b1=None, b2=None, act="silu", gated=True, stream=None):
         """som_experts_backward: {"dx", "dweights", "dw1", "dw2"} and, with biases, "db1", "db2"."""
         kind, T, E, k, D, I, rows, p = self._experts(x, indices, weights, w1, w2, b1, b2, gated)
-        gp, ldg = _matrix(dy, (T, D), x.dtype, "dy")
-        out = {"dx": x.new_empty((T, D)), "dweights": weights.new_empty((T, k)),
-               "dw1": x.new_empty((E, rows, D)), "dw2": x.new_empty((E, D, I))}
+        gp, ldg = _matrix(dy, T, D, x.dtype, "dy")
+        new = x.new_empty
+        out = {"dx": new((T, D)), "dweights": weights.new_empty((T, k)), "dw1": new((E, rows, D)), "dw2": new((E, D, I))}
         if b1 is not None:
-            out["db1"] = x.new_empty((E, rows))
+            out["db1"] = new((E, rows))
         if b2 is not None:
-            out["db2"] = x.new_empty((E, D))
-        at = lambda n: out[n].data_ptr() if n in out else 0  # noqa: E731
-        rc = self._lib.som_experts_backward(self._h, kind, _code(_ACTS, act, "act"), int(gated), T, E, k, D, I, *p, gp, ldg,
-                                            at("dx"), at("dweights"), at("dw1"), at("db1"), at("dw2"), at("db2"),
-                                            self._stream(stream))
-        self._check(rc, "som_experts_backward")
+            out["db2"] = new((E, D))
+        rc = self._lib.som_experts_backward(self._h, kind, _code(_ACTS, act, "act"), bool(gated), T, E, k, D, I, *p, gp, ldg,
+                                            out["dx"].data_ptr(), out["dweights"].data_ptr(), out["dw1"].data_ptr(),
+                                            out["db1"].data_ptr() if b1 is not None else 0, out["dw2"].data_ptr(),
+                                            out["db2"].data_ptr() if b2 is not None else 0, self._stream(stream))
+        if rc:
+            self._check(rc, "som_experts_backward")
         return out
 
     def device_flags(self, stream=None) -> int:
