@@ -13,7 +13,8 @@
 namespace lay {
 namespace {
 
-constexpr int FEW_WARPS = 8, FEW_THREADS = 32 * FEW_WARPS;
+constexpr int FEW_WARPS = 8, FEW_THREADS = 32 * FEW_WARPS;  // k_few: three blocks an SM
+constexpr int DOWN_WARPS = 24, DOWN_THREADS = 32 * DOWN_WARPS;  // k_few_down: one block an SM shares the token's hidden values
 
 // v[8] of an fp32 or 16-bit row in shared memory
 __device__ __forceinline__ void smem8(const uint16_t* p, float (&v)[8], int bf16)
@@ -170,10 +171,10 @@ __global__ void __launch_bounds__(FEW_THREADS, ROWS <= 2 ? 3 : 2) k_few(const Fe
 // y[t][d] = residual + sum_j (<w2[e_j][d], hidden[t, j]> + weight_j b2[e_j][d]); `share` warps of the block share an output,
 // each a part of the k * I products.  Blocks stay, as above: the token's hidden values are brought in once a block.  The
 // first weights are read while the kernel before, which writes the hidden values, still runs.
-__global__ void __launch_bounds__(FEW_THREADS, 3) k_few_down(const FewDownArgs a)
+__global__ void __launch_bounds__(DOWN_THREADS, 1) k_few_down(const FewDownArgs a)
 {
     extern __shared__ __align__(16) float hs[];  // [k][2][I / 2]: of every eight values the first four, then the other four
-    __shared__ float part[FEW_WARPS];
+    __shared__ float part[DOWN_WARPS];
     __shared__ int64_t base[32];  // the experts' weights, -1 = none
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int64_t t = blockIdx.y;
@@ -184,7 +185,7 @@ __global__ void __launch_bounds__(FEW_THREADS, 3) k_few_down(const FewDownArgs a
     }
     __syncthreads();
     constexpr int DEEP = 8;
-    const int share = a.share, outputs = FEW_WARPS / share, part_of = warp % share;
+    const int share = a.share, outputs = DOWN_WARPS / share, part_of = warp % share;
     const int span = (a.I + 255) / 256 * 256, all = a.k * (span / 256);  // pieces of 256 products, a piece within one expert
     const int rounds = (all + DEEP * share - 1) / (DEEP * share), stride = gridDim.x * outputs;
     // a warp's pieces are part_of, part_of + share, ...: place (j, c) of the next one to read and of the next one to use
@@ -213,7 +214,7 @@ __global__ void __launch_bounds__(FEW_THREADS, 3) k_few_down(const FewDownArgs a
 #pragma unroll
     for (int i = 0; i < DEEP; ++i) fetch(d, buf[i]);
     enter();
-    for (int i = threadIdx.x; i < a.k * (a.I / 4); i += FEW_THREADS) {
+    for (int i = threadIdx.x; i < a.k * (a.I / 4); i += DOWN_THREADS) {
         const int j = i / (a.I / 4), q = i - j * (a.I / 4);
         reinterpret_cast<float4*>(hs)[j * (a.I / 4) + (q & 1) * (a.I / 8) + (q >> 1)] =
             base[j] >= 0 ? __ldcg(reinterpret_cast<const float4*>(a.hidden + t * a.k * a.I) + i) : make_float4(0.f, 0.f, 0.f, 0.f);
@@ -293,9 +294,9 @@ int share_of(const som_layers* l, int64_t outputs, int64_t length, int in_flight
 }
 
 // Blocks for `outputs` of them, `each` a block at a time, in `groups` columns: no more than are resident.
-dim3 few_grid(const som_layers* l, int64_t outputs, int each, int64_t groups)
+dim3 few_grid(const som_layers* l, int64_t outputs, int each, int64_t groups, int per_sm)
 {
-    const int64_t want = (outputs + each - 1) / each, most = (int64_t)l->sm_count * 3 / groups;
+    const int64_t want = (outputs + each - 1) / each, most = (int64_t)l->sm_count * per_sm / groups;
     return dim3((unsigned)(want < most ? want : most > 0 ? most : 1), (unsigned)groups);
 }
 
@@ -312,14 +313,14 @@ cudaError_t prepare_few()
 int launch_few(som_layers* l, FewArgs a, int groups, bool gated, cudaStream_t st)
 {
     a.share = share_of(l, (int64_t)a.F * groups, (int64_t)a.D, gated ? 1024 : 2048);
-    const dim3 grid = few_grid(l, a.F, FEW_WARPS / a.share, groups);
+    const dim3 grid = few_grid(l, a.F, FEW_WARPS / a.share, groups, 3);
     return outcome(l, gated ? go<2>(l, a, grid, (size_t)a.D * 2, st) : go<1>(l, a, grid, (size_t)a.D * 2, st));
 }
 
 int launch_few_down(som_layers* l, FewDownArgs a, int64_t T, cudaStream_t st)
 {
     a.share = share_of(l, a.D * T, (int64_t)a.k * a.I, 2048);
-    return outcome(l, launch(l, k_few_down, few_grid(l, a.D, FEW_WARPS / a.share, T), FEW_THREADS, (size_t)a.k * a.I * sizeof(float), st, 1, a));
+    return outcome(l, launch(l, k_few_down, few_grid(l, a.D, DOWN_WARPS / a.share, T, 1), DOWN_THREADS, (size_t)a.k * a.I * sizeof(float), st, 1, a));
 }
 
 }  // namespace lay
