@@ -2,8 +2,7 @@
 //
 // Persistent blocks, one per SM, walk the output tiles.  Warp 0 issues the TMA copies of a six-stage ring (64 k of both
 // operands a stage, 32 KB, 128-byte swizzle), warp 1 issues the matrix instructions (tcgen05.mma, fp32 accumulators in
-// tensor memory), sixteen warps run the epilogue (with eight, two on a scheduler, the epilogues with an exponential
-// outlasted the products: 84 us against 56 for the first product of linear_backward at 4093 x 2048 x 4096, gelu).  The accumulator is double-buffered, so that the epilogue of a tile runs
+// tensor memory), eight warps run the epilogue (sixteen were no faster where the epilogue counts, and slower elsewhere).  The accumulator is double-buffered, so that the epilogue of a tile runs
 // under the products of the next.  PROD_DZ_TWO keeps two products of a tile side by side, z with one buffer and g with two: the
 // next tile's g is multiplied while the epilogue reads this tile's z and g (with one buffer for both the 206 GFLOP of 4096
 // tokens x 4 experts of 2048 x 1024 took 301 us).  Operands enter
@@ -28,8 +27,8 @@ constexpr int STAGE_BYTES = 2 * HALF;
 constexpr int BOX = 64 * 128;  // bytes of a box of 64 rows
 constexpr int EPI_WARPS = 4 * EPI_TURNS, THREADS = 32 * (2 + EPI_WARPS);
 constexpr int ROUND = EPI_TURNS * 32;  // columns that the epilogue's warps take in a round
-constexpr int OUT_BYTES = 32 * 64;  // an epilogue warp's staged output: 32 rows of 64 bytes, two of them
-constexpr int SMEM = 1024 + STAGES * STAGE_BYTES + EPI_WARPS * 2 * OUT_BYTES;
+constexpr int OUT_BYTES = 32 * 64;  // an epilogue warp's staged output: 32 rows of 64 bytes
+constexpr int SMEM = 1024 + STAGES * STAGE_BYTES + EPI_WARPS * OUT_BYTES;
 
 struct Tile {
     int row, col, expert;  // this block's first row and the tile's first column of the output, expert
@@ -85,13 +84,11 @@ __device__ __forceinline__ Tile tile_at(const ProdArgs& p, int idx, int width, i
 // at once (PROD_DZ, PROD_DZ_TWO).
 struct Stager {
     unsigned char* buf;
-    int lane, other;  // other: distance to the other buffer
-    // the store before the last has read its buffer
+    int lane;
+    // the last store has read the buffer
     __device__ __forceinline__ void begin()
     {
-        buf += other;
-        other = -other;
-        if (lane == 0) store_wait_read<1>();
+        if (lane == 0) store_wait_read<0>();
         __syncwarp();
     }
     __device__ __forceinline__ void put(int chunk, uint4 v) { *reinterpret_cast<uint4*>(buf + lane * 64 + ((chunk ^ ((lane >> 1) & 3)) << 4)) = v; }
@@ -104,6 +101,13 @@ struct Stager {
             store_commit();
         }
     }
+    // N = 16 fp32 columns
+    __device__ __forceinline__ void put32(const float* v)
+    {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            put(j, make_uint4(__float_as_uint(v[4 * j]), __float_as_uint(v[4 * j + 1]), __float_as_uint(v[4 * j + 2]), __float_as_uint(v[4 * j + 3])));
+    }
 };
 
 template <bool BF16>
@@ -112,28 +116,28 @@ __device__ __forceinline__ uint4 pack8(const float* v)
     return make_uint4(pack2(v[0], v[1], BF16), pack2(v[2], v[3], BF16), pack2(v[4], v[5], BF16), pack2(v[6], v[7], BF16));
 }
 
+// 8 consecutive values of a lane's row -> global memory
 template <bool BF16>
-__device__ __forceinline__ void store16(uint16_t* to, const float (&v)[16], int col, int cols)
+__device__ __forceinline__ void store8(uint16_t* to, const float (&v)[8])
 {
-#pragma unroll
-    for (int j = 0; j < 2; ++j)
-        if (col + 8 * j < cols) *reinterpret_cast<uint4*>(to + col + 8 * j) = pack8<BF16>(v + 8 * j);
+    *reinterpret_cast<uint4*>(to) = pack8<BF16>(v);
 }
 
-// 16 values of a row of a 16-bit matrix, fetched before they are needed; zeros beyond `cols` (a multiple of 8)
-struct Row16 {
-    uint4 w[2];
+// N values of a row of a 16-bit matrix, fetched before they are needed; zeros beyond `cols` (a multiple of 8)
+template <int N>
+struct RowPart {
+    uint4 w[N / 8];
     __device__ __forceinline__ void fetch(const uint16_t* row, int col, int cols, bool want)
     {
 #pragma unroll
-        for (int j = 0; j < 2; ++j)
+        for (int j = 0; j < N / 8; ++j)
             w[j] = want && col + 8 * j < cols ? *(reinterpret_cast<const uint4*>(row + col) + j) : make_uint4(0u, 0u, 0u, 0u);
     }
     template <bool BF16>
-    __device__ __forceinline__ void get(float (&v)[16]) const
+    __device__ __forceinline__ void get(float (&v)[N]) const
     {
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
+        for (int j = 0; j < N / 8; ++j) {
             const uint32_t u[4] = {w[j].x, w[j].y, w[j].z, w[j].w};
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
@@ -144,20 +148,20 @@ struct Row16 {
         }
     }
     template <bool BF16>
-    __device__ __forceinline__ void add(float (&v)[16]) const
+    __device__ __forceinline__ void add(float (&v)[N]) const
     {
-        float f[16];
+        float f[N];
         get<BF16>(f);
 #pragma unroll
-        for (int j = 0; j < 16; ++j) v[j] += f[j];
+        for (int j = 0; j < N; ++j) v[j] += f[j];
     }
 };
 
-// Lane l holds v[0..15] of row l; returns to lanes l and l + 16 the sum of column l over the 32 rows (fixed order).
-__device__ __forceinline__ float column_sum(float (&v)[16], int lane)
+// Lane l holds v[0..7] of row l; returns to the lanes with l % 8 = c the sum of column c over the 32 rows (fixed order).
+__device__ __forceinline__ float column_sum(float (&v)[8], int lane)
 {
 #pragma unroll
-    for (int h = 8; h >= 1; h >>= 1) {
+    for (int h = 4; h >= 1; h >>= 1) {
         const bool up = lane & h;
 #pragma unroll
         for (int j = 0; j < h; ++j) {
@@ -165,6 +169,7 @@ __device__ __forceinline__ float column_sum(float (&v)[16], int lane)
             v[j] = keep + __shfl_xor_sync(0xffffffffu, give, h);
         }
     }
+    v[0] += __shfl_xor_sync(0xffffffffu, v[0], 8);
     return v[0] + __shfl_xor_sync(0xffffffffu, v[0], 16);
 }
 
@@ -334,9 +339,10 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
         }
     } else {
         // A warp may read the 32 lanes of its quarter only; the four warps of a quarter take the tile's pieces of 32 columns
-        // in turn, a piece in two steps of 16 columns.
+        // in turn, a piece in steps of as many columns as the registers hold.
+        constexpr int STEP = MODE == PROD_FWD ? 16 : 8;
         const int q = warp & 3, turn = (warp - 2) >> 2;
-        Stager s{staged + (warp - 2) * 2 * OUT_BYTES, lane, OUT_BYTES};
+        Stager s{staged + (warp - 2) * OUT_BYTES, lane};
         int n_acc = 0;
         for (int idx = first_tile; idx < total; idx += step, ++n_acc) {
             const Tile t = tile_at<MODE, PAIR>(p, idx, width, rank);
@@ -349,10 +355,9 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
             const float rw = !p.row_weight ? 1.f : counts ? p.row_weight[row] : 0.f;
             const uint16_t* bias = p.bias ? p.bias + (size_t)t.expert * p.bias_ld : nullptr;
             const uint16_t* extra = p.extra ? p.extra + (size_t)row * p.ld_extra : nullptr;
-            const bool writes = row < t.store;
             const bool any = row0 < t.store && turn * 32 < width;
             // what the epilogue reads from memory is fetched ahead: the first step's before the products are done
-            Row16 add, b0, b1;
+            RowPart<STEP> add, b0, b1;
             auto fetch = [&](int at) {
                 const int col = t.col + at;
                 if (MODE == PROD_FWD || MODE == PROD_DZ) add.fetch(extra, col, p.cols, extra && counts && at < width);
@@ -366,124 +371,145 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
                 if ((MODE == PROD_FWD || MODE == PROD_DZ) && extra && counts)  // the rest on its way to L2
                     for (int at = turn * 32 + ROUND; at < width && t.col + at < p.cols; at += ROUND) prefetch_l2(extra + t.col + at);
             }
-            bool ok = true;
-            if (lane == 0) ok = bar_wait(&acc_full[buf], (uint32_t)(n_acc / BUFFERS) & 1u, gave_up);
-            if (!__shfl_sync(0xffffffffu, ok, 0)) break;
+            // One lane waits for the products, the other warps for that lane at a hardware barrier: trying the mbarrier
+            // takes shared-memory cycles (sixteen warps that did slowed the products by 5 %).
+            if (warp == 2 && lane == 0) bar_wait(&acc_full[buf], (uint32_t)(n_acc / BUFFERS) & 1u, gave_up);
+            asm volatile("bar.sync 1, %0;" ::"n"(32 * EPI_WARPS) : "memory");
+            if (*gave_up) break;
             tc_fence_after();
-            if (any) {
-                float dot = 0.f;
+            if (!any) {
+                // none of this warp's rows or columns
+            } else if constexpr (MODE == PROD_DX || MODE == PROD_DW) {
+                const int batch = MODE == PROD_DW ? t.expert : 0;
+                float next[32];
+                tmem_ld(acc + turn * 32, next);
+                for (int at = turn * 32; at < width; at += ROUND) {
+                    float v[32];
+                    tmem_wait_ld();
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) v[j] = MODE == PROD_DW && t.k == 0 ? 0.f : next[j];  // (no token: nothing was summed)
+                    if (at + ROUND < width) tmem_ld(acc + at + ROUND, next);
+                    s.begin();
+                    if (p.out32) {
+                        s.put32(v);
+                        s.send(&p.o, t.col + at, row0, batch, p);
+                        s.begin();
+                        s.put32(v + 16);
+                        s.send(&p.o, t.col + at + 16, row0, batch, p);
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) s.put(j, pack8<BF16>(v + 8 * j));
+                        s.send(&p.o, t.col + at, row0, batch, p);
+                    }
+                }
+            } else if constexpr (MODE == PROD_FWD) {
 #pragma unroll 1
                 for (int at = turn * 32; at < width; at += at & 16 ? ROUND - 16 : 16) {
-                    const int col = t.col + at, next = at + (at & 16 ? ROUND - 16 : 16);
-                    float v[16], u[16];
-                    tmem_ld16(acc + at, v);
-                    if (MODE == PROD_DX || MODE == PROD_DW) {
-                        tmem_wait_ld();
-                        if (MODE == PROD_DW && t.k == 0) {
+                    const int col = t.col + at;
+                    float v[STEP], u[STEP];
+                    tmem_ld(acc + at, v);
+                    if (gated) tmem_ld(acc + BN / 2 + at, u);
+                    tmem_wait_ld();
+                    if (bias) {
+                        float f[STEP];
+                        b0.template get<BF16>(f);
+                        const float by = p.weigh == 2 ? rw : 1.f;
 #pragma unroll
-                            for (int j = 0; j < 16; ++j) v[j] = 0.f;  // an expert without a token: nothing was summed
-                        }
-                    } else if (MODE == PROD_FWD) {
-                        if (gated) tmem_ld16(acc + BN / 2 + at, u);
-                        tmem_wait_ld();
-                        if (bias) {
-                            float f[16];
-                            b0.template get<BF16>(f);
-                            const float by = p.weigh == 2 ? rw : 1.f;
-#pragma unroll
-                            for (int j = 0; j < 16; ++j) v[j] = fmaf(f[j], by, v[j]);
-                            if (gated) b1.template add<BF16>(u);
-                        }
-                        if (p.act != SOM_ACT_NONE)
-                            with_act(p.act, [&](auto tag) {
-#pragma unroll
-                                for (int j = 0; j < 16; ++j) v[j] = act_of<decltype(tag)::value>(v[j]);
-                            });
-                        if (gated) {
-#pragma unroll
-                            for (int j = 0; j < 16; ++j) v[j] *= u[j];
-                        }
-                        if (extra) add.template add<BF16>(v);
-                        fetch(next);
-                        if (p.weigh == 1) {
-#pragma unroll
-                            for (int j = 0; j < 16; ++j) v[j] *= rw;
-                        }
-                    } else {
-                        // PROD_DZ, PROD_DZ_TWO: v = z (or the gate's z) becomes dz, u = the gated half's
-                        float g[16], hid[16];
-                        if (gated) tmem_ld16(acc + BN / 2 + at, u);
-                        if (MODE == PROD_DZ_TWO) tmem_ld16(acc2 + at, g);
-                        tmem_wait_ld();
-                        if (bias) {
-                            b0.template add<BF16>(v);
-                            if (gated) b1.template add<BF16>(u);
-                        }
-                        if (MODE == PROD_DZ) add.template get<BF16>(g);
-                        fetch(next);
+                        for (int j = 0; j < STEP; ++j) v[j] = fmaf(f[j], by, v[j]);
+                        if (gated) b1.template add<BF16>(u);
+                    }
+                    if (p.act != SOM_ACT_NONE)
                         with_act(p.act, [&](auto tag) {
 #pragma unroll
-                            for (int j = 0; j < 16; ++j) {
-                                float a, da;
-                                act_both<decltype(tag)::value>(v[j], a, da);
-                                hid[j] = a;
-                                v[j] = da;
-                            }
+                            for (int j = 0; j < STEP; ++j) v[j] = act_of<decltype(tag)::value>(v[j]);
                         });
-                        if (gated) {
+                    if (gated) {
 #pragma unroll
-                            for (int j = 0; j < 16; ++j) {
-                                const float a = hid[j];
-                                hid[j] = a * u[j];
-                                v[j] *= u[j];
-                                u[j] = a;
-                            }
-                        }
-                        if (MODE == PROD_DZ_TWO) {
-                            // (columns beyond the last have g = 0: W2 is filled with zeros there)
+                        for (int j = 0; j < STEP; ++j) v[j] *= u[j];
+                    }
+                    if (extra) add.template add<BF16>(v);
+                    fetch(at + (at & 16 ? ROUND - 16 : 16));
+                    if (p.weigh == 1) {
 #pragma unroll
-                            for (int j = 0; j < 16; ++j) {
-                                dot = fmaf(hid[j], g[j], dot);
-                                g[j] *= rw;
-                                hid[j] *= rw;
-                            }
-                        }
+                        for (int j = 0; j < STEP; ++j) v[j] *= rw;
+                    }
+                    if (p.out32) {
+                        s.begin();
+                        s.put32(v);
+                        s.send(&p.o, col, row0, 0, p);
+                    } else {
+                        const int half = (at >> 4) & 1;
+                        if (half == 0) s.begin();
+                        s.put(2 * half, pack8<BF16>(v));
+                        s.put(2 * half + 1, pack8<BF16>(v + 8));
+                        if (half == 1) s.send(&p.o, col - 16, row0, 0, p);
+                    }
+                }
+            } else {
+                // PROD_DZ, PROD_DZ_TWO: v = z (or the gate's z) becomes dz, u = the gated half's
+                const bool writes = row < t.store;
+                uint16_t* out = static_cast<uint16_t*>(p.o0) + (size_t)row * p.ld0;
+                uint16_t* out2 = static_cast<uint16_t*>(p.o2) + (size_t)row * p.ld2;
+                float dot = 0.f;
+#pragma unroll 1
+                for (int at = turn * 32; at < width; at += (at & 24) == 24 ? ROUND - 24 : 8) {
+                    const int col = t.col + at;
+                    float v[8], u[8], g[8], hid[8];
+                    tmem_ld(acc + at, v);
+                    if (gated) tmem_ld(acc + BN / 2 + at, u);
+                    if (MODE == PROD_DZ_TWO) tmem_ld(acc2 + at, g);
+                    tmem_wait_ld();
+                    if (bias) {
+                        b0.template add<BF16>(v);
+                        if (gated) b1.template add<BF16>(u);
+                    }
+                    if (MODE == PROD_DZ) add.template get<BF16>(g);
+                    fetch(at + ((at & 24) == 24 ? ROUND - 24 : 8));
+                    with_act(p.act, [&](auto tag) {
 #pragma unroll
-                        for (int j = 0; j < 16; ++j) {
-                            v[j] *= g[j];
-                            if (gated) u[j] *= g[j];
+                        for (int j = 0; j < 8; ++j) {
+                            float a, da;
+                            act_both<decltype(tag)::value>(v[j], a, da);
+                            hid[j] = a;
+                            v[j] = da;
                         }
-                        if (writes) {
-                            uint16_t* to = static_cast<uint16_t*>(p.o0) + (size_t)row * p.ld0;
-                            store16<BF16>(to, v, col, p.cols);
-                            if (gated) store16<BF16>(to + p.gate_rows, u, col, p.cols);
-                            if (MODE == PROD_DZ_TWO) store16<BF16>(static_cast<uint16_t*>(p.o2) + (size_t)row * p.ld2, hid, col, p.cols);
+                    });
+                    if (gated) {
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) {
+                            const float a = hid[j];
+                            hid[j] = a * u[j];
+                            v[j] *= u[j];
+                            u[j] = a;
                         }
                     }
-                    if (MODE == PROD_FWD || MODE == PROD_DX || MODE == PROD_DW) {
-                        const int batch = MODE == PROD_DW ? t.expert : 0;
-                        if (p.out32) {
-                            s.begin();
+                    if (MODE == PROD_DZ_TWO) {
+                        // (columns beyond the last have g = 0: W2 is filled with zeros there)
 #pragma unroll
-                            for (int j = 0; j < 4; ++j)
-                                s.put(j, make_uint4(__float_as_uint(v[4 * j]), __float_as_uint(v[4 * j + 1]), __float_as_uint(v[4 * j + 2]), __float_as_uint(v[4 * j + 3])));
-                            s.send(&p.o, col, row0, batch, p);
-                        } else {
-                            const int half = (at >> 4) & 1;
-                            if (half == 0) s.begin();
-                            s.put(2 * half, pack8<BF16>(v));
-                            s.put(2 * half + 1, pack8<BF16>(v + 8));
-                            if (half == 1) s.send(&p.o, col - 16, row0, batch, p);
+                        for (int j = 0; j < 8; ++j) {
+                            dot = fmaf(hid[j], g[j], dot);
+                            g[j] *= rw;
+                            hid[j] *= rw;
                         }
                     }
-                    if ((MODE == PROD_DZ || MODE == PROD_DZ_TWO) && p.column_sums) {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        v[j] *= g[j];
+                        if (gated) u[j] *= g[j];
+                    }
+                    if (writes && col < p.cols) {
+                        store8<BF16>(out + col, v);
+                        if (gated) store8<BF16>(out + p.gate_rows + col, u);
+                        if (MODE == PROD_DZ_TWO) store8<BF16>(out2 + col, hid);
+                    }
+                    if (p.column_sums) {
                         // (outputs were rounded; the sums are over the unrounded values; rows that do not count hold zeros)
                         float* to = p.column_sums + (size_t)(row0 / 32) * (p.cols + p.gate_rows) + col;
                         const float sv = column_sum(v, lane);
-                        if (lane < 16 && col + lane < p.cols) to[lane] = sv;
+                        if (lane < 8 && col < p.cols) to[lane] = sv;
                         if (gated) {
                             const float su = column_sum(u, lane);
-                            if (lane < 16 && col + lane < p.cols) to[p.gate_rows + lane] = su;
+                            if (lane < 8 && col < p.cols) to[p.gate_rows + lane] = su;
                         }
                     }
                 }

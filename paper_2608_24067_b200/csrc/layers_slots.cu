@@ -311,6 +311,7 @@ __global__ void __launch_bounds__(256) k_column_sums(SlotPlan p, int64_t rows, c
     const int64_t lo = p.seg ? p.seg[e] : 0, hi = p.seg ? lo + p.count[e] : rows;
     float a[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
     if (c < cols)
+#pragma unroll 4
         for (int64_t i = lo + r; i < hi; i += 32) {
             float u[8];
             load8(v + (size_t)i * ld + c, u, bf16);
@@ -361,8 +362,8 @@ cudaError_t prepare_plan()
     return cudaFuncSetAttribute(k_slot_plan, cudaFuncAttributeMaxDynamicSharedMemorySize, (PLAN_WARPS + 1) * 1024 * (int)sizeof(int));
 }
 
-// One block for up to 2048 slots (5 to 7 us; three launches take about as long), blocks of PLACE_SLOTS beyond.
-int plan_blocks(int64_t slots) { return slots <= 2048 ? 0 : (int)((slots + PLACE_SLOTS - 1) / PLACE_SLOTS); }
+// One block for up to 4096 slots (5 to 12 us; three launches take about 14), blocks of PLACE_SLOTS beyond.
+int plan_blocks(int64_t slots) { return slots <= 4096 ? 0 : (int)((slots + PLACE_SLOTS - 1) / PLACE_SLOTS); }
 
 int launch_plan(som_layers* l, const SlotPlan& p, const int32_t* indices, const void* weights, int weights_type, int64_t T,
                 int k, int E, cudaStream_t st)
