@@ -2,6 +2,7 @@
 #include <new>
 
 #include "layers_few.cuh"
+#include "layers_finish.cuh"
 #include "layers_product.cuh"
 #include "layers_slots.cuh"
 
@@ -132,6 +133,32 @@ void set_tiles(const som_layers* l, ProdArgs* a, int64_t rows, int64_t cols, boo
     a->col_tiles = a->pair ? (int)pc : tiles_of(cols, gated ? SINGLE_COLS / 2 : SINGLE_COLS);
     a->rows = (int)rows;
     a->cols = (int)cols;
+    a->splits = 1;
+}
+
+// Blocks that share each tile's sum, for products whose tiles leave SMs idle: worth its second launch (about 3 us, with a
+// step of 64 k at about 0.3 us) where it takes at least 14 steps off the longest sum.
+int splits_of(const som_layers* l, const ProdArgs& a, int64_t k)
+{
+    if (a.pair) return 1;
+    const int64_t tiles = (int64_t)a.row_tiles * a.col_tiles, steps = tiles_of(k, 64);
+    int64_t s = l->sm_count / tiles;
+    if (s > steps / 4) s = steps / 4;
+    if (s > 16) s = 16;
+    return s > 1 && steps - steps / s >= 14 ? (int)s : 1;
+}
+
+// Runs a product in a.splits parts of [rows][n] fp32 at `parts` and joins them by `f`.
+int run_split(som_layers* l, ProdMode mode, ProdArgs a, FinishArgs f, unsigned char* parts, cudaStream_t st)
+{
+    const int rc = make_map(l, &a.o, parts, 4, f.n, f.rows, a.splits, f.n, f.rows * f.n, 64, 32);
+    if (rc != SOM_OK) return rc;
+    a.out32 = 1;
+    f.part = reinterpret_cast<const float*>(parts);
+    f.splits = a.splits;
+    f.bf16 = a.bf16;
+    const int done = launch_product(l, mode, a, st);
+    return done != SOM_OK ? done : launch_finish(l, f, st);
 }
 
 }  // namespace
@@ -231,17 +258,35 @@ int som_linear(som_layers* l, int type, int act, int gated, int64_t T, int64_t D
     ProdArgs a = {};
     LAY_TRY(map_left(l, &a.a, x, D, T, ldx));
     LAY_TRY(map_64(l, &a.b, w, D, rows, D));
+    a.bf16 = type == SOM_BF16;
+    a.flags = l->flags;
+    a.experts = 1;
+    a.k1 = (int)D;
+    set_tiles(l, &a, T, rows, false);
+    a.splits = splits_of(l, a, D);
+    if (a.splits > 1) {
+        LAY_TRY(ensure(l, (size_t)a.splits * T * rows * sizeof(float)));
+        FinishArgs f = {};
+        f.rows = T;
+        f.n = (int)rows;
+        f.cols = (int)F;
+        f.bias = static_cast<const uint16_t*>(bias);
+        f.extra = static_cast<const uint16_t*>(residual);
+        f.ld_extra = ldr;
+        f.out = static_cast<uint16_t*>(y);
+        f.ld = ldy;
+        f.mode = FINISH_FWD;
+        f.act = act;
+        f.gated = gated;
+        return run_split(l, PROD_FWD, a, f, static_cast<unsigned char*>(l->ws), st);
+    }
     LAY_TRY(map_out(l, &a.o, y, 2, F, T, ldy));
     a.bias = static_cast<const uint16_t*>(bias);
     a.extra = static_cast<const uint16_t*>(residual);
     a.ld_extra = ldr;
     set_tiles(l, &a, T, F, gated);
-    a.experts = 1;
     a.gate_rows = gated ? (int)F : 0;
-    a.k1 = (int)D;
     a.act = act;
-    a.bf16 = type == SOM_BF16;
-    a.flags = l->flags;
     return launch_product(l, PROD_FWD, a, st);
 }
 
@@ -271,55 +316,100 @@ int som_linear_backward(som_layers* l, int type, int act, int gated, int64_t T, 
     a.act = act;
     a.bf16 = type == SOM_BF16;
     a.flags = l->flags;
-    if (again) {
-        uint16_t* z_grad;
-        float* sums;
-        Carver c{nullptr, 0};
-        for (int pass = 0; pass < 2; ++pass) {
-            c.used = 0;
-            z_grad = c.take<uint16_t>(T * rows);
-            sums = c.take<float>(dbias ? tiles_of(T, 32) * rows : 0);
-            if (pass == 0) {
-                LAY_TRY(ensure(l, c.used));
-                c.base = static_cast<unsigned char*>(l->ws);
-            }
+    // the three products and the blocks that share their tiles' sums
+    ProdArgs z = a, px = a, pw = a;
+    z.k1 = (int)D;
+    set_tiles(l, &z, T, rows, false);
+    z.splits = splits_of(l, z, D);
+    px.k1 = (int)rows;
+    set_tiles(l, &px, T, D, false);
+    px.splits = splits_of(l, px, rows);
+    pw.k1 = (int)T;
+    set_tiles(l, &pw, rows, D, false);
+    pw.splits = splits_of(l, pw, T);
+    uint16_t* z_grad;
+    float* sums;
+    unsigned char* parts;
+    Carver c{nullptr, 0};
+    for (int pass = 0; pass < 2; ++pass) {
+        c.used = 0;
+        z_grad = c.take<uint16_t>(again ? T * rows : 0);
+        sums = c.take<float>(again && dbias && z.splits == 1 ? tiles_of(T, 32) * rows : 0);
+        int64_t most = again && z.splits > 1 ? (int64_t)z.splits * T * rows : 0;
+        if (dx && px.splits > 1 && (int64_t)px.splits * T * D > most) most = (int64_t)px.splits * T * D;
+        if (dw && pw.splits > 1 && (int64_t)pw.splits * rows * D > most) most = (int64_t)pw.splits * rows * D;
+        parts = reinterpret_cast<unsigned char*>(c.take<float>(most));
+        if (pass == 0) {
+            LAY_TRY(ensure(l, c.used));
+            c.base = static_cast<unsigned char*>(l->ws);
         }
+    }
+    FinishArgs f = {};
+    if (again) {
         dz = z_grad;
         lddz = rows;
-        ProdArgs z = a;
         LAY_TRY(map_left(l, &z.a, x, D, T, ldx));
         LAY_TRY(map_64(l, &z.b, w, D, rows, D));
-        z.o0 = z_grad;
-        z.ld0 = rows;
-        z.bias = static_cast<const uint16_t*>(bias);
-        z.extra = static_cast<const uint16_t*>(dy);
-        z.ld_extra = lddy;
-        z.column_sums = dbias ? sums : nullptr;
-        set_tiles(l, &z, T, F, gated);
-        z.gate_rows = gated ? (int)F : 0;
-        z.k1 = (int)D;
-        LAY_TRY(launch_product(l, PROD_DZ, z, st));
-        if (dbias) LAY_TRY(launch_join_sums(l, SlotPlan(), 1, T, sums, rows, dbias, a.bf16, st));
-    } else if (dbias) {
-        LAY_TRY(launch_column_sums(l, SlotPlan(), 1, T, dy, lddy, rows, dbias, a.bf16, st));
+        if (z.splits > 1) {
+            f.rows = T;
+            f.n = (int)rows;
+            f.cols = (int)F;
+            f.bias = static_cast<const uint16_t*>(bias);
+            f.extra = static_cast<const uint16_t*>(dy);
+            f.ld_extra = lddy;
+            f.out = z_grad;
+            f.ld = rows;
+            f.mode = FINISH_DZ;
+            f.act = act;
+            f.gated = gated;
+            z.act = SOM_ACT_NONE;
+            LAY_TRY(run_split(l, PROD_FWD, z, f, parts, st));
+        } else {
+            z.o0 = z_grad;
+            z.ld0 = rows;
+            z.bias = static_cast<const uint16_t*>(bias);
+            z.extra = static_cast<const uint16_t*>(dy);
+            z.ld_extra = lddy;
+            z.column_sums = dbias ? sums : nullptr;
+            set_tiles(l, &z, T, F, gated);
+            z.gate_rows = gated ? (int)F : 0;
+            LAY_TRY(launch_product(l, PROD_DZ, z, st));
+        }
     }
+    if (dbias) {
+        if (again && z.splits == 1) LAY_TRY(launch_join_sums(l, SlotPlan(), 1, T, sums, rows, dbias, a.bf16, st));
+        else LAY_TRY(launch_column_sums(l, SlotPlan(), 1, T, dz, lddz, rows, dbias, a.bf16, st));
+    }
+    f = FinishArgs();
+    f.mode = FINISH_SUM;
+    px.act = pw.act = SOM_ACT_NONE;
     if (dx) {
-        ProdArgs p = a;
-        LAY_TRY(map_left(l, &p.a, dz, rows, T, lddz));
-        LAY_TRY(map_64(l, &p.b, w, D, rows, D));
-        LAY_TRY(map_out(l, &p.o, dx, 2, D, T, D));
-        set_tiles(l, &p, T, D, false);
-        p.k1 = (int)rows;
-        LAY_TRY(launch_product(l, PROD_DX, p, st));
+        LAY_TRY(map_left(l, &px.a, dz, rows, T, lddz));
+        LAY_TRY(map_64(l, &px.b, w, D, rows, D));
+        if (px.splits > 1) {
+            f.rows = T;
+            f.n = f.cols = (int)D;
+            f.out = static_cast<uint16_t*>(dx);
+            f.ld = D;
+            LAY_TRY(run_split(l, PROD_DX, px, f, parts, st));
+        } else {
+            LAY_TRY(map_out(l, &px.o, dx, 2, D, T, D));
+            LAY_TRY(launch_product(l, PROD_DX, px, st));
+        }
     }
     if (dw) {
-        ProdArgs p = a;
-        LAY_TRY(map_64(l, &p.a, dz, rows, T, lddz));
-        LAY_TRY(map_64(l, &p.b, x, D, T, ldx));
-        LAY_TRY(map_out(l, &p.o, dw, 2, D, rows, D));
-        set_tiles(l, &p, rows, D, false);
-        p.k1 = (int)T;
-        LAY_TRY(launch_product(l, PROD_DW, p, st));
+        LAY_TRY(map_64(l, &pw.a, dz, rows, T, lddz));
+        LAY_TRY(map_64(l, &pw.b, x, D, T, ldx));
+        if (pw.splits > 1) {
+            f.rows = rows;
+            f.n = f.cols = (int)D;
+            f.out = static_cast<uint16_t*>(dw);
+            f.ld = D;
+            LAY_TRY(run_split(l, PROD_DW, pw, f, parts, st));
+        } else {
+            LAY_TRY(map_out(l, &pw.o, dw, 2, D, rows, D));
+            LAY_TRY(launch_product(l, PROD_DW, pw, st));
+        }
     }
     return SOM_OK;
 }
@@ -410,6 +500,7 @@ static ProdArgs grouped(const som_layers* l, const SlotPlan& p, int type, int64_
     a.col_tiles = tiles_of(cols, (a.pair ? PAIR_COLS : SINGLE_COLS) / (gated ? 2 : 1));
     a.rows = p.max_rows;
     a.cols = (int)cols;
+    a.splits = 1;
     a.bf16 = type == SOM_BF16;
     a.flags = l->flags;
     return a;

@@ -33,6 +33,7 @@ constexpr int SMEM = 1024 + STAGES * STAGE_BYTES + EPI_WARPS * OUT_BYTES;
 struct Tile {
     int row, col, expert;  // this block's first row and the tile's first column of the output, expert
     int k0, k;             // PROD_DW: first row of the sum; length of the first product's sum
+    int split;             // part of the sum
     int live, store;       // rows below `live` are in use, rows below `store` are written (zeros from `live` on)
 };
 
@@ -41,8 +42,8 @@ __device__ __forceinline__ int round64(int n) { return (n + 63) & ~63; }
 template <int MODE>
 __device__ __forceinline__ int tile_count(const ProdArgs& p)
 {
-    if (MODE == PROD_DW) return p.experts * p.row_tiles * p.col_tiles;
-    return (p.tiles ? *p.tiles : p.row_tiles) * p.col_tiles;
+    if (MODE == PROD_DW) return p.experts * p.row_tiles * p.col_tiles * p.splits;
+    return (p.tiles ? *p.tiles : p.row_tiles) * p.col_tiles * p.splits;
 }
 
 template <int MODE, bool PAIR>
@@ -50,6 +51,11 @@ __device__ __forceinline__ Tile tile_at(const ProdArgs& p, int idx, int width, i
 {
     constexpr int ROWS = PAIR ? PAIR_ROWS : SINGLE_ROWS;
     Tile t;
+    t.split = 0;
+    if (p.splits > 1) {
+        t.split = idx % p.splits;
+        idx /= p.splits;
+    }
     if (MODE == PROD_DW) {
         const int per = p.row_tiles * p.col_tiles;
         t.expert = idx / per;
@@ -73,6 +79,11 @@ __device__ __forceinline__ Tile tile_at(const ProdArgs& p, int idx, int width, i
             // the sums over an expert's rows (PROD_DW) run over whole steps of 64 rows
             t.store = MODE == PROD_DZ_TWO ? s + round64(n) : t.live;
         }
+    }
+    if (p.splits > 1) {
+        const int steps = (p.k1 + BK - 1) / BK, from = steps * t.split / p.splits, to = steps * (t.split + 1) / p.splits;
+        t.k0 = from * BK;
+        t.k = (to - from) * BK;
     }
     return t;
 }
@@ -380,7 +391,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
             if (!any) {
                 // none of this warp's rows or columns
             } else if constexpr (MODE == PROD_DX || MODE == PROD_DW) {
-                const int batch = MODE == PROD_DW ? t.expert : 0;
+                const int batch = MODE == PROD_DW ? t.expert + t.split : t.split;
                 float next[32];
                 tmem_ld(acc + turn * 32, next);
                 for (int at = turn * 32; at < width; at += ROUND) {
@@ -436,7 +447,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
                     if (p.out32) {
                         s.begin();
                         s.put32(v);
-                        s.send(&p.o, col, row0, 0, p);
+                        s.send(&p.o, col, row0, t.split, p);
                     } else {
                         const int half = (at >> 4) & 1;
                         if (half == 0) s.begin();
@@ -537,7 +548,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
 template <int MODE, bool PAIR, bool BF16>
 cudaError_t launch_as(som_layers* l, const ProdArgs& args, cudaStream_t st)
 {
-    const int64_t tiles = (int64_t)args.row_tiles * args.col_tiles * (MODE == PROD_DW ? args.experts : 1);
+    const int64_t tiles = (int64_t)args.row_tiles * args.col_tiles * (MODE == PROD_DW ? args.experts : 1) * args.splits;
     const int most = PAIR ? l->pairs : l->sm_count;
     return launch(l, k_product<MODE, PAIR, BF16>, dim3((unsigned)(tiles < most ? tiles : most) * (PAIR ? 2 : 1)), THREADS, SMEM, st,
                   PAIR ? 2 : 1, args);

@@ -45,6 +45,7 @@ struct ProdArgs {
     int bias_ld, dots;
     int pair;
     int row_tiles, col_tiles, experts;
+    int splits;      // blocks that share a tile's sum (PROD_FWD, PROD_DX, PROD_DW; not grouped): part s goes to batch s of the output
     int rows, cols;  // extent of the outputs (PROD_DW: of one expert's)
     int gate_rows;   // gated: rows of B between a feature's gate row and its other row; 0 = not gated
     int k1, k2;      // length of the products' sums

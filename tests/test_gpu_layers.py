@@ -35,7 +35,8 @@ def _wide(t):
 
 
 SIZES = [(1, 8, 8), (1, 64, 128), (2, 72, 40), (5, 2048, 264), (16, 136, 520), (17, 200, 256), (64, 64, 64), (127, 136, 264),
-         (128, 256, 256), (129, 264, 136), (300, 520, 1000)]
+         (128, 256, 256), (129, 264, 136), (300, 520, 1000),
+         (40, 2048, 264), (200, 3000, 72), (3000, 72, 72), (9, 1000, 4096)]  # (sums split over blocks)
 
 
 @pytest.mark.parametrize("T,D,F", SIZES)
