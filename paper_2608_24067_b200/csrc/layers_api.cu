@@ -9,18 +9,18 @@
 namespace lay {
 
 int make_map(som_layers* l, CUtensorMap* map, const void* base, int bytes, int64_t cols, int64_t rows, int64_t batch, int64_t ld,
-             int64_t batch_stride, int box_bytes, int box_rows)
+             int64_t batch_stride, int box_rows)
 {
     using Encode = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
                                 const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
                                 CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
     const cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)batch};
     const cuuint64_t strides[2] = {(cuuint64_t)(ld * bytes), (cuuint64_t)(batch_stride * bytes)};
-    const cuuint32_t box[3] = {(cuuint32_t)(box_bytes / bytes), (cuuint32_t)box_rows, 1u};
+    const cuuint32_t box[3] = {(cuuint32_t)(128 / bytes), (cuuint32_t)box_rows, 1u};
     const cuuint32_t step[3] = {1u, 1u, 1u};
     const CUresult r = reinterpret_cast<Encode>(l->encode)(
         map, bytes == 4 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims,
-        strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, box_bytes == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B,
+        strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
         CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     if (r == CUDA_SUCCESS) return SOM_OK;
     l->last_cuda_error = (int)cudaErrorInvalidValue;
@@ -107,30 +107,30 @@ int check_sizes(int64_t a, int64_t b)
     return SOM_OK;
 }
 
-int tiles_of(int64_t n, int64_t width) { return (int)((n + width - 1) / width); }
+int64_t tiles_of(int64_t n, int64_t width) { return (n + width - 1) / width; }
 
 // 16-bit operands of the products: the left one K-major in boxes of 128 rows; the right one, and M/N-major ones, of 64
 int map_left(som_layers* l, CUtensorMap* m, const void* p, int64_t cols, int64_t rows, int64_t ld)
 {
-    return make_map(l, m, p, 2, cols, rows, 1, ld, rows * ld, 128, 128);
+    return make_map(l, m, p, 2, cols, rows, 1, ld, rows * ld, 128);
 }
 int map_64(som_layers* l, CUtensorMap* m, const void* p, int64_t cols, int64_t rows, int64_t ld, int64_t batch = 1)
 {
-    return make_map(l, m, p, 2, cols, rows, batch, ld, rows * ld, 128, 64);
+    return make_map(l, m, p, 2, cols, rows, batch, ld, rows * ld, 64);
 }
 int map_out(som_layers* l, CUtensorMap* m, void* p, int bytes, int64_t cols, int64_t rows, int64_t ld, int64_t batch = 1)
 {
-    return make_map(l, m, p, bytes, cols, rows, batch, ld, rows * ld, 64, 32);
+    return make_map(l, m, p, bytes, cols, rows, batch, ld, rows * ld, 32);
 }
 
 // The tiles of a product of `rows` x `cols` outputs (`batch` of them).  Pairs of blocks do twice a single block's work per
-// byte that they load, but need tiles enough for every SM: singles where pairs would leave more than a third of them idle.
+// byte that they load, but need tiles enough for every SM: narrow single tiles where pairs would leave a third of them idle.
 void set_tiles(const som_layers* l, ProdArgs* a, int64_t rows, int64_t cols, bool gated, int64_t batch = 1)
 {
-    const int64_t pr = tiles_of(rows, PAIR_ROWS), pc = tiles_of(cols, gated ? PAIR_COLS / 2 : PAIR_COLS);
-    a->pair = 3 * pr * pc * batch >= 2 * l->pairs;
-    a->row_tiles = a->pair ? (int)pr : tiles_of(rows, SINGLE_ROWS);
-    a->col_tiles = a->pair ? (int)pc : tiles_of(cols, gated ? SINGLE_COLS / 2 : SINGLE_COLS);
+    const int halves = gated ? 2 : 1;
+    a->shape = 3 * tiles_of(rows, 256) * tiles_of(cols, 256 / halves) * batch >= 2 * l->pairs ? PAIR : NARROW;
+    a->row_tiles = tiles_of(rows, shape_rows(a->shape));
+    a->col_tiles = tiles_of(cols, shape_cols(a->shape) / halves);
     a->rows = (int)rows;
     a->cols = (int)cols;
     a->splits = 1;
@@ -140,7 +140,7 @@ void set_tiles(const som_layers* l, ProdArgs* a, int64_t rows, int64_t cols, boo
 // step of 64 k at about 0.3 us) where it takes at least 14 steps off the longest sum.
 int splits_of(const som_layers* l, const ProdArgs& a, int64_t k)
 {
-    if (a.pair) return 1;
+    if (a.shape != NARROW) return 1;
     const int64_t tiles = (int64_t)a.row_tiles * a.col_tiles, steps = tiles_of(k, 64);
     int64_t s = l->sm_count / tiles;
     if (s > steps / 4) s = steps / 4;
@@ -151,7 +151,7 @@ int splits_of(const som_layers* l, const ProdArgs& a, int64_t k)
 // Runs a product in a.splits parts of [rows][n] fp32 at `parts` and joins them by `f`.
 int run_split(som_layers* l, ProdMode mode, ProdArgs a, FinishArgs f, unsigned char* parts, cudaStream_t st)
 {
-    const int rc = make_map(l, &a.o, parts, 4, f.n, f.rows, a.splits, f.n, f.rows * f.n, 64, 32);
+    const int rc = make_map(l, &a.o, parts, 4, f.n, f.rows, a.splits, f.n, f.rows * f.n, 32);
     if (rc != SOM_OK) return rc;
     a.out32 = 1;
     f.part = reinterpret_cast<const float*>(parts);
@@ -483,11 +483,12 @@ static SlotPlan carve_plan(Carver& c, int64_t T, int E, int k, int tile)
 // read comes from L2 the second time).
 static bool few_slots(int64_t T, int E, int k) { return T * k <= 16 || (T * k <= 64 && T * k <= E); }
 
-// Pairs of blocks once the experts have rows enough for their tiles (256 rows); with fewer, a pair would mostly multiply
-// padding, and the weights' bytes bound the product, not the tensor cores.
-static bool pair_rows(int64_t T, int E, int k) { return T * k >= (int64_t)128 * E; }
+// Rows of an expert's tiles: a pair's once the experts have rows enough; with fewer, a pair would mostly multiply padding, and
+// the weights' bytes bound the product, not the tensor cores.
+static int tile_rows(int64_t T, int E, int k) { return T * k >= (int64_t)128 * E ? shape_rows(PAIR) : shape_rows(WIDE); }
 
-static ProdArgs grouped(const som_layers* l, const SlotPlan& p, int type, int64_t cols, bool gated)
+// A product over the slots' rows.  Single blocks are wide where that leaves a tile for every SM, by the tiles to expect.
+static ProdArgs grouped(const som_layers* l, const SlotPlan& p, int64_t slots, int E, int type, int64_t cols, bool gated)
 {
     ProdArgs a = {};
     a.tiles = p.tiles;
@@ -495,9 +496,11 @@ static ProdArgs grouped(const som_layers* l, const SlotPlan& p, int type, int64_
     a.seg = p.seg;
     a.count = p.count;
     a.row_weight = p.row_weight;
-    a.pair = p.tile == PAIR_ROWS;
+    const int64_t expected = (slots < E ? slots : E) + slots / 256;
+    const int halves = gated ? 2 : 1;
+    a.shape = p.tile == shape_rows(PAIR) ? PAIR : expected * tiles_of(cols, shape_cols(WIDE) / halves) >= l->sm_count ? WIDE : NARROW;
     a.row_tiles = p.max_rows / p.tile;
-    a.col_tiles = tiles_of(cols, (a.pair ? PAIR_COLS : SINGLE_COLS) / (gated ? 2 : 1));
+    a.col_tiles = tiles_of(cols, shape_cols(a.shape) / halves);
     a.rows = p.max_rows;
     a.cols = (int)cols;
     a.splits = 1;
@@ -562,7 +565,7 @@ int som_experts(som_layers* l, int type, int act, int gated, int64_t T, int32_t 
     Carver c{nullptr, 0};
     for (int pass = 0; pass < 2; ++pass) {
         c.used = 0;
-        p = carve_plan(c, T, E, k, pair_rows(T, E, k) ? PAIR_ROWS : SINGLE_ROWS);
+        p = carve_plan(c, T, E, k, tile_rows(T, E, k));
         xp = c.take<uint16_t>((int64_t)p.max_rows * D);
         h = c.take<uint16_t>((int64_t)p.max_rows * I);
         part = c.take<float>((int64_t)p.max_rows * D);
@@ -573,7 +576,7 @@ int som_experts(som_layers* l, int type, int act, int gated, int64_t T, int32_t 
     }
     LAY_TRY(launch_plan(l, p, indices, weights, weights_type, T, k, E, st));
     LAY_TRY(launch_gather(l, p, k, D, x, ldx, xp, nullptr, 0, nullptr, st));
-    ProdArgs a = grouped(l, p, type, I, gated);
+    ProdArgs a = grouped(l, p, T * k, E, type, I, gated);
     LAY_TRY(map_left(l, &a.a, xp, D, p.max_rows, D));
     LAY_TRY(map_64(l, &a.b, w1, D, rows1, D, E));
     LAY_TRY(map_out(l, &a.o, h, 2, I, p.max_rows, I));
@@ -584,7 +587,7 @@ int som_experts(som_layers* l, int type, int act, int gated, int64_t T, int32_t 
     a.act = act;
     a.weigh = 1;
     LAY_TRY(launch_product(l, PROD_FWD, a, st));
-    a = grouped(l, p, type, D, false);
+    a = grouped(l, p, T * k, E, type, D, false);
     LAY_TRY(map_left(l, &a.a, h, I, p.max_rows, I));
     LAY_TRY(map_64(l, &a.b, w2, I, D, I, E));
     LAY_TRY(map_out(l, &a.o, part, 4, D, p.max_rows, D));
@@ -619,18 +622,19 @@ int som_experts_backward(som_layers* l, int type, int act, int gated, int64_t T,
     SlotPlan p;
     uint16_t *xp, *dyp, *h, *dz;
     float *part, *dot, *sums;
-    const bool pair = pair_rows(T, E, k);
-    const int dots = tiles_of(I, (pair ? PAIR_COLS : SINGLE_COLS) / 2) * tile_dots(pair);
+    ProdArgs z;  // z and g = W2^T dy side by side, in tiles of half the width
     Carver c{nullptr, 0};
     for (int pass = 0; pass < 2; ++pass) {
         c.used = 0;
-        p = carve_plan(c, T, E, k, pair ? PAIR_ROWS : SINGLE_ROWS);
+        p = carve_plan(c, T, E, k, tile_rows(T, E, k));
+        z = grouped(l, p, T * k, E, type, I, true);
+        z.dots = z.col_tiles * tile_dots(z.shape);
         xp = c.take<uint16_t>((int64_t)p.max_rows * D);
         dyp = c.take<uint16_t>((int64_t)p.max_rows * D);
         h = c.take<uint16_t>((int64_t)p.max_rows * I);
         dz = c.take<uint16_t>((int64_t)p.max_rows * rows1);
         part = c.take<float>((int64_t)p.max_rows * D);
-        dot = c.take<float>((int64_t)p.max_rows * dots);
+        dot = c.take<float>((int64_t)p.max_rows * z.dots);
         sums = c.take<float>(db1 ? p.max_rows / 32 * rows1 : 0);
         if (pass == 0) {
             LAY_TRY(ensure(l, c.used));
@@ -639,8 +643,8 @@ int som_experts_backward(som_layers* l, int type, int act, int gated, int64_t T,
     }
     LAY_TRY(launch_plan(l, p, indices, weights, weights_type, T, k, E, st));
     LAY_TRY(launch_gather(l, p, k, D, x, ldx, xp, dy, lddy, dyp, st));
-    // z and g = W2^T dy side by side (half-width tiles) -> dz, the weighted h, partial sums of <h, g>
-    ProdArgs a = grouped(l, p, type, I, true);
+    // -> dz, the weighted h, partial sums of <h, g>
+    ProdArgs a = z;
     LAY_TRY(map_left(l, &a.a, xp, D, p.max_rows, D));
     LAY_TRY(map_64(l, &a.b, w1, D, rows1, D, E));
     LAY_TRY(map_left(l, &a.a2, dyp, D, p.max_rows, D));
@@ -652,17 +656,16 @@ int som_experts_backward(som_layers* l, int type, int act, int gated, int64_t T,
     a.bias = static_cast<const uint16_t*>(b1);
     a.bias_ld = (int)rows1;
     a.dot = dot;
-    a.dots = dots;
     a.column_sums = db1 ? sums : nullptr;
     a.gate_rows = gated ? (int)I : 0;
     a.k1 = a.k2 = (int)D;
     a.act = act;
     LAY_TRY(launch_product(l, PROD_DZ_TWO, a, st));
-    LAY_TRY(launch_dweights(l, p, indices, T, k, D, dot, dots, b2, dy, lddy, dweights, weights_type, a.bf16, st));
+    LAY_TRY(launch_dweights(l, p, indices, T, k, D, dot, a.dots, b2, dy, lddy, dweights, weights_type, a.bf16, st));
     if (db1) LAY_TRY(launch_join_sums(l, p, E, 0, sums, rows1, db1, a.bf16, st));
     if (db2) LAY_TRY(launch_column_sums(l, p, E, 0, dyp, D, D, db2, a.bf16, st));
     // dx
-    a = grouped(l, p, type, D, false);
+    a = grouped(l, p, T * k, E, type, D, false);
     LAY_TRY(map_left(l, &a.a, dz, rows1, p.max_rows, rows1));
     LAY_TRY(map_64(l, &a.b, w1, D, rows1, D, E));
     LAY_TRY(map_out(l, &a.o, part, 4, D, p.max_rows, D));

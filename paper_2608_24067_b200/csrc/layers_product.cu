@@ -1,7 +1,7 @@
 // Matrix products of the dense operators on the 5th-generation tensor cores.
 //
-// Persistent blocks, one per SM, walk the output tiles.  Warp 0 issues the TMA copies of a six-stage ring (64 k of both
-// operands a stage, 32 KB, 128-byte swizzle), warp 1 issues the matrix instructions (tcgen05.mma, fp32 accumulators in
+// Persistent blocks, one per SM, walk the output tiles.  Warp 0 issues the TMA copies of a ring (64 k of both
+// operands a stage, 128-byte swizzle; six stages of 32 KB, or four of 48), warp 1 issues the matrix instructions (tcgen05.mma, fp32 accumulators in
 // tensor memory), eight warps run the epilogue (sixteen were no faster where the epilogue counts, and slower elsewhere).  The accumulator is double-buffered, so that the epilogue of a tile runs
 // under the products of the next.  PROD_DZ_TWO keeps two products of a tile side by side, z with one buffer and g with two: the
 // next tile's g is multiplied while the epilogue reads this tile's z and g (with one buffer for both the 206 GFLOP of 4096
@@ -9,11 +9,11 @@
 // K-major (a row holds consecutive k) or M/N-major (a row holds consecutive rows of the product), as they lie in memory: no
 // operand is transposed beforehand.  Every wait is bounded.
 //
-// Two tile shapes.  PAIR: two blocks of a cluster share a tile of 256 x 256; each loads its own 128 rows of A and one half of
+// Three tile shapes.  PAIR: two blocks of a cluster share a tile of 256 x 256; each loads its own 128 rows of A and one half of
 // B, and the matrix instruction reads both halves (cta_group::2).  A single block on 128 x 256 moves 48 KB into and 48 KB out
 // of its shared memory for 512 clocks of matrix work, 192 bytes a clock where shared memory gives 128: 4096 x 4096 x 4096
-// took 134 us so.  With the pair it is 32 KB each way, 128 bytes a clock.  SINGLE: 128 x 128 by one block, for products
-// that have too few tiles to fill the SMs with pairs or too few rows per expert.
+// took 134 us so.  With the pair it is 32 KB each way, 128 bytes a clock.  WIDE: that single block, for experts with fewer rows
+// than a pair's tile, where the weights' bytes count.  NARROW: 128 x 128 by one block, for products with few tiles.
 #include "layers_math.cuh"
 #include "layers_product.cuh"
 #include "layers_ptx.cuh"
@@ -21,14 +21,13 @@
 namespace lay {
 namespace {
 
-constexpr int BM = 128, BK = 64, STAGES = 6;
-constexpr int HALF = 128 * BK * 2;  // bytes of a block's share of an operand in a stage
-constexpr int STAGE_BYTES = 2 * HALF;
-constexpr int BOX = 64 * 128;  // bytes of a box of 64 rows
+constexpr int BM = 128, BK = 64;
+constexpr int BOX = 64 * 128;      // bytes of a box of 64 rows
+constexpr int A_BYTES = 2 * BOX;   // a block's rows of A in a stage
+constexpr int MOST_STAGES = 6, RING_BYTES = MOST_STAGES * 2 * A_BYTES;
 constexpr int EPI_WARPS = 4 * EPI_TURNS, THREADS = 32 * (2 + EPI_WARPS);
-constexpr int ROUND = EPI_TURNS * 32;  // columns that the epilogue's warps take in a round
-constexpr int OUT_BYTES = 32 * 64;  // an epilogue warp's staged output: 32 rows of 64 bytes
-constexpr int SMEM = 1024 + STAGES * STAGE_BYTES + EPI_WARPS * OUT_BYTES;
+constexpr int OUT_BYTES = 32 * 128;  // an epilogue warp's staged output: 32 rows of 128 bytes
+constexpr int SMEM = 1024 + RING_BYTES + EPI_WARPS * OUT_BYTES;
 
 struct Tile {
     int row, col, expert;  // this block's first row and the tile's first column of the output, expert
@@ -46,10 +45,10 @@ __device__ __forceinline__ int tile_count(const ProdArgs& p)
     return (p.tiles ? *p.tiles : p.row_tiles) * p.col_tiles * p.splits;
 }
 
-template <int MODE, bool PAIR>
+template <int MODE, int SHAPE>
 __device__ __forceinline__ Tile tile_at(const ProdArgs& p, int idx, int width, int rank)
 {
-    constexpr int ROWS = PAIR ? PAIR_ROWS : SINGLE_ROWS;
+    constexpr int ROWS = shape_rows(SHAPE);
     Tile t;
     t.split = 0;
     if (p.splits > 1) {
@@ -88,8 +87,8 @@ __device__ __forceinline__ Tile tile_at(const ProdArgs& p, int idx, int width, i
     return t;
 }
 
-// Ways out of the epilogue.  Staged: 32 rows (lane l holds row l) of 32 16-bit or 16 fp32 columns go through shared memory
-// (64-byte rows, 64-byte swizzle) to a TMA store, which leaves out what lies outside the tensor.  Direct: a lane writes its 16
+// Ways out of the epilogue.  Staged: 32 rows (lane l holds row l) of 64 16-bit or 32 fp32 columns go through shared memory
+// (128-byte rows, 128-byte swizzle) to a TMA store, which leaves out what lies outside the tensor.  Direct: a lane writes its 16
 // columns.  Direct stores take the load/store pipe 32 cycles an instruction: too much where a tile's products are short
 // (PROD_DW at 512 rows an expert: 134 us staged, 178 us direct), but no waits, and no shared memory for up to three outputs
 // at once (PROD_DZ, PROD_DZ_TWO).
@@ -102,7 +101,12 @@ struct Stager {
         if (lane == 0) store_wait_read<0>();
         __syncwarp();
     }
-    __device__ __forceinline__ void put(int chunk, uint4 v) { *reinterpret_cast<uint4*>(buf + lane * 64 + ((chunk ^ ((lane >> 1) & 3)) << 4)) = v; }
+    // 16 bytes of this lane's row
+    __device__ __forceinline__ void put(int chunk, uint4 v) { *reinterpret_cast<uint4*>(buf + lane * 128 + ((chunk ^ (lane & 7)) << 4)) = v; }
+    __device__ __forceinline__ void put(int chunk, const float* v)
+    {
+        put(chunk, make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])));
+    }
     __device__ __forceinline__ void send(const CUtensorMap* map, int col, int row, int batch, const ProdArgs& p)
     {
         fence_async_smem();
@@ -111,13 +115,6 @@ struct Stager {
             if (col < p.cols && row < p.rows) tma_store(map, buf, col, row, batch);
             store_commit();
         }
-    }
-    // N = 16 fp32 columns
-    __device__ __forceinline__ void put32(const float* v)
-    {
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-            put(j, make_uint4(__float_as_uint(v[4 * j]), __float_as_uint(v[4 * j + 1]), __float_as_uint(v[4 * j + 2]), __float_as_uint(v[4 * j + 3])));
     }
 };
 
@@ -184,12 +181,15 @@ __device__ __forceinline__ float column_sum(float (&v)[8], int lane)
     return v[0] + __shfl_xor_sync(0xffffffffu, v[0], 16);
 }
 
-template <int MODE, bool PAIR, bool BF16>
+template <int MODE, int SHAPE, bool BF16>
 __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ ProdArgs p)
 {
     constexpr bool A_MN = MODE == PROD_DW, B_MN = MODE == PROD_DX || MODE == PROD_DW;
     constexpr int BUFFERS = MODE == PROD_DZ_TWO ? 1 : 2;  // of the first product
-    constexpr int BN = PAIR ? PAIR_COLS : SINGLE_COLS;
+    constexpr bool PAIRED = SHAPE == PAIR;
+    constexpr int BN = shape_cols(SHAPE);
+    constexpr int SHARE = PAIRED ? BN / 2 : BN;  // columns of B in this block
+    constexpr int STAGE_BYTES = A_BYTES + SHARE * 128, STAGES = RING_BYTES / STAGE_BYTES;
     constexpr uint32_t TMEM_COLUMNS = 2 * BN;
     extern __shared__ unsigned char smem_raw[];
     __shared__ __align__(8) uint64_t full[STAGES], empty[STAGES], acc_full[2], acc_empty[2], drained;
@@ -197,10 +197,10 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
     __shared__ int gave_up_sh;
     unsigned char* ring = smem_raw + ((1024u - (smem_addr(smem_raw) & 1023u)) & 1023u);
 
-    unsigned char* staged = ring + STAGES * STAGE_BYTES;
+    unsigned char* staged = ring + RING_BYTES;
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int rank = PAIR ? (int)cluster_rank() : 0;
+    const int rank = PAIRED ? (int)cluster_rank() : 0;
     if (threadIdx.x == 0) {
         for (int i = 0; i < STAGES; ++i) {
             bar_init(&full[i], 1);
@@ -208,20 +208,20 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
         }
         for (int i = 0; i < 2; ++i) {
             bar_init(&acc_full[i], 1);
-            bar_init(&acc_empty[i], EPI_WARPS * (PAIR ? 2 : 1));
+            bar_init(&acc_empty[i], EPI_WARPS * (PAIRED ? 2 : 1));
         }
         bar_init(&drained, 1);
         gave_up_sh = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    if (warp == 1) tmem_alloc<PAIR>(&tmem_sh, TMEM_COLUMNS);
+    if (warp == 1) tmem_alloc<PAIRED>(&tmem_sh, TMEM_COLUMNS);
     if (threadIdx.x == 0) {
         prefetch_map(&p.a);
         prefetch_map(&p.b);
     }
     tc_fence_before();
     __syncthreads();
-    if (PAIR) cluster_sync();  // the other block's barriers are ready
+    if (PAIRED) cluster_sync();  // the other block's barriers are ready
     tc_fence_after();
     enter();
     const uint32_t tmem = tmem_sh;
@@ -233,8 +233,8 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
     const int width = MODE == PROD_DZ_TWO || (gated && (MODE == PROD_FWD || MODE == PROD_DZ)) ? BN / 2 : BN;
     const int n1 = MODE == PROD_DZ_TWO && !gated ? BN / 2 : BN;  // accumulator columns of the first product
     const int total = tile_count<MODE>(p);
-    constexpr int N2 = BN / 2, SHARE2 = PAIR ? N2 / 2 : N2;  // columns of the second product, and of its B in this block
-    const int step = PAIR ? gridDim.x >> 1 : gridDim.x, first_tile = PAIR ? blockIdx.x >> 1 : blockIdx.x;
+    constexpr int N2 = BN / 2, SHARE2 = PAIRED ? N2 / 2 : N2;  // columns of the second product, and of its B in this block
+    const int step = PAIRED ? gridDim.x >> 1 : gridDim.x, first_tile = PAIRED ? blockIdx.x >> 1 : blockIdx.x;
 
     if (warp == 0) {
         if (lane == 0) {
@@ -243,11 +243,11 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
             int64_t issued = 0;
             bool ok = true;
             for (int idx = first_tile; ok && idx < total; idx += step) {
-                const Tile t = tile_at<MODE, PAIR>(p, idx, width, rank);
-                // first row (K-major) or column of this block's 128 columns of B
-                const int b0 = !PAIR ? t.col : gated && !B_MN ? t.col + rank * p.gate_rows : t.col + rank * (n1 / 2);
-                const int b1 = !PAIR && gated && !B_MN ? t.col + p.gate_rows : b0 + 64;
-                const bool two = n1 == BN;  // 128 columns of B, not 64
+                const Tile t = tile_at<MODE, SHAPE>(p, idx, width, rank);
+                // First row (K-major) or column of this block's columns of B, in boxes of 64.  Gated: a pair's second block has
+                // the other half of the rows, in a single block they follow the gate's boxes.
+                const int b0 = !PAIRED ? t.col : gated && !B_MN ? t.col + rank * p.gate_rows : t.col + rank * (n1 / 2);
+                const int boxes = (PAIRED ? n1 / 2 : n1) / 64, gates = !PAIRED && gated && !B_MN ? boxes / 2 : boxes;
                 const int it1 = (t.k + BK - 1) / BK, it2 = MODE == PROD_DZ_TWO ? (p.k2 + BK - 1) / BK : 0;
                 for (int it = 0; it < it1 + it2; ++it) {
                     if (!bar_wait(&empty[stage], phase ^ 1u, gave_up)) {
@@ -255,29 +255,28 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
                         break;
                     }
                     unsigned char* sa = ring + stage * STAGE_BYTES;
-                    unsigned char* sb = sa + HALF;
+                    unsigned char* sb = sa + A_BYTES;
                     // the leader's barrier counts both blocks' bytes
-                    const uint32_t bar = PAIR ? cluster_addr(smem_addr(&full[stage]), 0) : smem_addr(&full[stage]);
+                    const uint32_t bar = PAIRED ? cluster_addr(smem_addr(&full[stage]), 0) : smem_addr(&full[stage]);
                     if (MODE == PROD_DZ_TWO && it < it2) {
                         const int k = it * BK;
-                        if (rank == 0) bar_expect(&full[stage], (PAIR ? 2 : 1) * (HALF + SHARE2 * BK * 2));
-                        tma_load<PAIR>(sa, &p.a2, bar, k, t.row, 0);
-                        tma_load<PAIR>(sb, &p.b2, bar, t.col + rank * SHARE2, k, t.expert);
+                        if (rank == 0) bar_expect(&full[stage], (PAIRED ? 2 : 1) * (A_BYTES + SHARE2 * 128));
+                        tma_load<PAIRED>(sa, &p.a2, bar, k, t.row, 0);
+                        for (int j = 0; j < SHARE2; j += 64) tma_load<PAIRED>(sb + j * 128, &p.b2, bar, t.col + rank * SHARE2 + j, k, t.expert);
                     } else {
                         const int k = t.k0 + (it - it2) * BK;
-                        if (rank == 0) bar_expect(&full[stage], (PAIR ? 2 : 1) * (two ? STAGE_BYTES : STAGE_BYTES - BOX));
+                        if (rank == 0) bar_expect(&full[stage], (PAIRED ? 2 : 1) * (A_BYTES + boxes * BOX));
                         if (A_MN) {
-                            tma_load<PAIR>(sa, &p.a, bar, t.row, k, 0);
-                            tma_load<PAIR>(sa + BOX, &p.a, bar, t.row + 64, k, 0);
+                            tma_load<PAIRED>(sa, &p.a, bar, t.row, k, 0);
+                            tma_load<PAIRED>(sa + BOX, &p.a, bar, t.row + 64, k, 0);
                         } else {
-                            tma_load<PAIR>(sa, &p.a, bar, k, t.row, 0);
+                            tma_load<PAIRED>(sa, &p.a, bar, k, t.row, 0);
                         }
-                        if (B_MN) {
-                            tma_load<PAIR>(sb, &p.b, bar, b0, k, MODE == PROD_DW ? 0 : t.expert);
-                            tma_load<PAIR>(sb + BOX, &p.b, bar, b1, k, MODE == PROD_DW ? 0 : t.expert);
-                        } else {
-                            tma_load<PAIR>(sb, &p.b, bar, k, b0, t.expert);
-                            if (two) tma_load<PAIR>(sb + BOX, &p.b, bar, k, b1, t.expert);
+#pragma unroll
+                        for (int j = 0; j < SHARE / 64; ++j) {
+                            if (j >= boxes) break;
+                            if (B_MN) tma_load<PAIRED>(sb + j * BOX, &p.b, bar, b0 + 64 * j, k, MODE == PROD_DW ? 0 : t.expert);
+                            else tma_load<PAIRED>(sb + j * BOX, &p.b, bar, k, j < gates ? b0 + 64 * j : b0 + 64 * (j - gates) + p.gate_rows, t.expert);
                         }
                     }
                     ++issued;
@@ -300,10 +299,10 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
             int stage = 0, n_acc = 0;
             uint32_t phase = 0;
             bool ok = true;
-            const uint32_t idesc1 = mma_desc(BF16, A_MN, B_MN, PAIR ? 256 : 128, n1);
-            const uint32_t idesc2 = mma_desc(BF16, 0, 1, PAIR ? 256 : 128, N2);
+            const uint32_t idesc1 = mma_desc(BF16, A_MN, B_MN, PAIRED ? 256 : 128, n1);
+            const uint32_t idesc2 = mma_desc(BF16, 0, 1, PAIRED ? 256 : 128, N2);
             for (int idx = first_tile; ok && idx < total; idx += step, ++n_acc) {
-                const Tile t = tile_at<MODE, PAIR>(p, idx, width, rank);
+                const Tile t = tile_at<MODE, SHAPE>(p, idx, width, rank);
                 const int buf = BUFFERS == 2 ? n_acc & 1 : 0;
                 const uint32_t use = (uint32_t)(n_acc / BUFFERS) & 1u;
                 const int it1 = (t.k + BK - 1) / BK, it2 = MODE == PROD_DZ_TWO ? (p.k2 + BK - 1) / BK : 0;
@@ -318,7 +317,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
                         break;
                     }
                     tc_fence_after();
-                    const uint32_t sa = smem_addr(ring + stage * STAGE_BYTES), sb = sa + HALF;
+                    const uint32_t sa = smem_addr(ring + stage * STAGE_BYTES), sb = sa + A_BYTES;
                     const bool second = MODE == PROD_DZ_TWO && it < it2;
                     const uint32_t d = second ? tmem + (uint32_t)(BN + (n_acc & 1) * N2) : tmem + (uint32_t)(buf * BN);
                     const bool first = it == 0 || it == it2;
@@ -327,9 +326,9 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
                         const uint64_t da = A_MN ? mat_desc(sa + kk * 2048, BOX, 1024) : mat_desc(sa + kk * 32, 16, 1024);
                         const uint64_t db =
                             B_MN || second ? mat_desc(sb + kk * 2048, BOX, 1024) : mat_desc(sb + kk * 32, 16, 1024);
-                        mma<PAIR>(d, da, db, second ? idesc2 : idesc1, !(first && kk == 0));
+                        mma<PAIRED>(d, da, db, second ? idesc2 : idesc1, !(first && kk == 0));
                     }
-                    mma_commit<PAIR>(&empty[stage]);
+                    mma_commit<PAIRED>(&empty[stage]);
                     if (++stage == STAGES) {
                         stage = 0;
                         phase ^= 1u;
@@ -340,23 +339,24 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
                     ok = false;
                     break;
                 }
-                mma_commit<PAIR>(&acc_full[buf]);
+                mma_commit<PAIRED>(&acc_full[buf]);
             }
             if (!ok) {  // instructions in flight read shared memory and write tensor memory
-                mma_commit<PAIR>(&drained);
+                mma_commit<PAIRED>(&drained);
                 const long long t0 = clock64();
                 while (!bar_try(&drained, 0) && clock64() - t0 < WAIT_CYCLES) {}
             }
         }
     } else {
-        // A warp may read the 32 lanes of its quarter only; the four warps of a quarter take the tile's pieces of 32 columns
-        // in turn, a piece in steps of as many columns as the registers hold.
+        // A warp may read the 32 lanes of its quarter only; the warps of a quarter take the tile's pieces in turn: 128 bytes
+        // of staged outputs, or 32 columns of direct ones, in steps of as many columns as the registers hold.
         constexpr int STEP = MODE == PROD_FWD ? 16 : 8;
+        const int piece = MODE == PROD_DZ || MODE == PROD_DZ_TWO || p.out32 ? 32 : 64, round = EPI_TURNS * piece;
         const int q = warp & 3, turn = (warp - 2) >> 2;
         Stager s{staged + (warp - 2) * OUT_BYTES, lane};
         int n_acc = 0;
         for (int idx = first_tile; idx < total; idx += step, ++n_acc) {
-            const Tile t = tile_at<MODE, PAIR>(p, idx, width, rank);
+            const Tile t = tile_at<MODE, SHAPE>(p, idx, width, rank);
             const int buf = BUFFERS == 2 ? n_acc & 1 : 0;
             const uint32_t acc = tmem + (uint32_t)(buf * BN) + ((uint32_t)(32 * q) << 16);
             const uint32_t acc2 = tmem + (uint32_t)(BN + (n_acc & 1) * N2) + ((uint32_t)(32 * q) << 16);
@@ -366,7 +366,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
             const float rw = !p.row_weight ? 1.f : counts ? p.row_weight[row] : 0.f;
             const uint16_t* bias = p.bias ? p.bias + (size_t)t.expert * p.bias_ld : nullptr;
             const uint16_t* extra = p.extra ? p.extra + (size_t)row * p.ld_extra : nullptr;
-            const bool any = row0 < t.store && turn * 32 < width;
+            const bool any = row0 < t.store && turn * piece < width;
             // what the epilogue reads from memory is fetched ahead: the first step's before the products are done
             RowPart<STEP> add, b0, b1;
             auto fetch = [&](int at) {
@@ -378,9 +378,9 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
                 }
             };
             if (any) {
-                fetch(turn * 32);
+                fetch(turn * piece);
                 if ((MODE == PROD_FWD || MODE == PROD_DZ) && extra && counts)  // the rest on its way to L2
-                    for (int at = turn * 32 + ROUND; at < width && t.col + at < p.cols; at += ROUND) prefetch_l2(extra + t.col + at);
+                    for (int at = turn * piece + round; at < width && t.col + at < p.cols; at += round) prefetch_l2(extra + t.col + at);
             }
             // One lane waits for the products, the other warps for that lane at a hardware barrier: trying the mbarrier
             // takes shared-memory cycles (sixteen warps that did slowed the products by 5 %).
@@ -393,30 +393,31 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
             } else if constexpr (MODE == PROD_DX || MODE == PROD_DW) {
                 const int batch = MODE == PROD_DW ? t.expert + t.split : t.split;
                 float next[32];
-                tmem_ld(acc + turn * 32, next);
-                for (int at = turn * 32; at < width; at += ROUND) {
+                tmem_ld(acc + turn * piece, next);
+                for (int at = turn * piece; at < width;) {
                     float v[32];
+                    const int half = p.out32 ? 0 : (at >> 5) & 1, step_on = !p.out32 && half == 0 ? 32 : round - 32 * half;
                     tmem_wait_ld();
 #pragma unroll
                     for (int j = 0; j < 32; ++j) v[j] = MODE == PROD_DW && t.k == 0 ? 0.f : next[j];  // (no token: nothing was summed)
-                    if (at + ROUND < width) tmem_ld(acc + at + ROUND, next);
-                    s.begin();
+                    if (at + step_on < width) tmem_ld(acc + at + step_on, next);
+                    if (half == 0) s.begin();
                     if (p.out32) {
-                        s.put32(v);
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) s.put(j, v + 4 * j);
                         s.send(&p.o, t.col + at, row0, batch, p);
-                        s.begin();
-                        s.put32(v + 16);
-                        s.send(&p.o, t.col + at + 16, row0, batch, p);
                     } else {
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) s.put(j, pack8<BF16>(v + 8 * j));
-                        s.send(&p.o, t.col + at, row0, batch, p);
+                        for (int j = 0; j < 4; ++j) s.put(4 * half + j, pack8<BF16>(v + 8 * j));
+                        if (half == 1) s.send(&p.o, t.col + at - 32, row0, batch, p);
                     }
+                    at += step_on;
                 }
             } else if constexpr (MODE == PROD_FWD) {
 #pragma unroll 1
-                for (int at = turn * 32; at < width; at += at & 16 ? ROUND - 16 : 16) {
-                    const int col = t.col + at;
+                for (int at = turn * piece; at < width;) {
+                    const int col = t.col + at, done = (at & (piece - 1)) + 16;  // columns of the piece after this step
+                    const int step_on = done == piece ? round - piece + 16 : 16;
                     float v[STEP], u[STEP];
                     tmem_ld(acc + at, v);
                     if (gated) tmem_ld(acc + BN / 2 + at, u);
@@ -439,22 +440,21 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
                         for (int j = 0; j < STEP; ++j) v[j] *= u[j];
                     }
                     if (extra) add.template add<BF16>(v);
-                    fetch(at + (at & 16 ? ROUND - 16 : 16));
+                    fetch(at + step_on);
                     if (p.weigh == 1) {
 #pragma unroll
                         for (int j = 0; j < STEP; ++j) v[j] *= rw;
                     }
+                    if (done == 16) s.begin();
                     if (p.out32) {
-                        s.begin();
-                        s.put32(v);
-                        s.send(&p.o, col, row0, t.split, p);
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) s.put((done - 16) / 4 + j, v + 4 * j);
                     } else {
-                        const int half = (at >> 4) & 1;
-                        if (half == 0) s.begin();
-                        s.put(2 * half, pack8<BF16>(v));
-                        s.put(2 * half + 1, pack8<BF16>(v + 8));
-                        if (half == 1) s.send(&p.o, col - 16, row0, 0, p);
+                        s.put((done - 16) / 8, pack8<BF16>(v));
+                        s.put((done - 16) / 8 + 1, pack8<BF16>(v + 8));
                     }
+                    if (done == piece) s.send(&p.o, col + 16 - piece, row0, t.split, p);
+                    at += step_on;
                 }
             } else {
                 // PROD_DZ, PROD_DZ_TWO: v = z (or the gate's z) becomes dz, u = the gated half's
@@ -463,7 +463,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
                 uint16_t* out2 = static_cast<uint16_t*>(p.o2) + (size_t)row * p.ld2;
                 float dot = 0.f;
 #pragma unroll 1
-                for (int at = turn * 32; at < width; at += (at & 24) == 24 ? ROUND - 24 : 8) {
+                for (int at = turn * 32; at < width; at += (at & 24) == 24 ? round - 24 : 8) {
                     const int col = t.col + at;
                     float v[8], u[8], g[8], hid[8];
                     tmem_ld(acc + at, v);
@@ -475,7 +475,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
                         if (gated) b1.template add<BF16>(u);
                     }
                     if (MODE == PROD_DZ) add.template get<BF16>(g);
-                    fetch(at + ((at & 24) == 24 ? ROUND - 24 : 8));
+                    fetch(at + ((at & 24) == 24 ? round - 24 : 8));
                     with_act(p.act, [&](auto tag) {
 #pragma unroll
                         for (int j = 0; j < 8; ++j) {
@@ -524,12 +524,12 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
                         }
                     }
                 }
-                if (MODE == PROD_DZ_TWO && counts) p.dot[(size_t)row * p.dots + (t.col / width) * tile_dots(PAIR) + turn] = dot;
+                if (MODE == PROD_DZ_TWO && counts) p.dot[(size_t)row * p.dots + (t.col / width) * tile_dots(SHAPE) + turn] = dot;
             }
             tc_fence_before();
             __syncwarp();
             if (lane == 0) {
-                if (PAIR) bar_arrive_remote(cluster_addr(smem_addr(&acc_empty[buf]), 0));
+                if (PAIRED) bar_arrive_remote(cluster_addr(smem_addr(&acc_empty[buf]), 0));
                 else bar_arrive(&acc_empty[buf]);
             }
         }
@@ -538,34 +538,37 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
     __syncthreads();
     if (threadIdx.x == 0 && gave_up_sh) atomicOr(p.flags, LAY_FLAG_GAVE_UP);
     __syncwarp();
-    if (PAIR) cluster_sync();  // no block leaves while the other may still reach its memory
+    if (PAIRED) cluster_sync();  // no block leaves while the other may still reach its memory
     if (warp == 1) {
         tc_fence_after();
-        tmem_free<PAIR>(tmem, TMEM_COLUMNS);
+        tmem_free<PAIRED>(tmem, TMEM_COLUMNS);
     }
 }
 
-template <int MODE, bool PAIR, bool BF16>
+template <int MODE, int SHAPE, bool BF16>
 cudaError_t launch_as(som_layers* l, const ProdArgs& args, cudaStream_t st)
 {
     const int64_t tiles = (int64_t)args.row_tiles * args.col_tiles * (MODE == PROD_DW ? args.experts : 1) * args.splits;
-    const int most = PAIR ? l->pairs : l->sm_count;
-    return launch(l, k_product<MODE, PAIR, BF16>, dim3((unsigned)(tiles < most ? tiles : most) * (PAIR ? 2 : 1)), THREADS, SMEM, st,
-                  PAIR ? 2 : 1, args);
+    const int most = SHAPE == PAIR ? l->pairs : l->sm_count, blocks = SHAPE == PAIR ? 2 : 1;
+    return launch(l, k_product<MODE, SHAPE, BF16>, dim3((unsigned)(tiles < most ? tiles : most) * blocks), THREADS, SMEM, st, blocks, args);
 }
 
 template <int MODE>
 cudaError_t launch_mode(som_layers* l, const ProdArgs& a, cudaStream_t st)
 {
-    if (a.pair) return a.bf16 ? launch_as<MODE, true, true>(l, a, st) : launch_as<MODE, true, false>(l, a, st);
-    return a.bf16 ? launch_as<MODE, false, true>(l, a, st) : launch_as<MODE, false, false>(l, a, st);
+    switch (a.shape) {
+        case NARROW: return a.bf16 ? launch_as<MODE, NARROW, true>(l, a, st) : launch_as<MODE, NARROW, false>(l, a, st);
+        case WIDE: return a.bf16 ? launch_as<MODE, WIDE, true>(l, a, st) : launch_as<MODE, WIDE, false>(l, a, st);
+        default: return a.bf16 ? launch_as<MODE, PAIR, true>(l, a, st) : launch_as<MODE, PAIR, false>(l, a, st);
+    }
 }
 
 template <int MODE, bool BF16>
 cudaError_t prepare_as(int* pairs)
 {
-    cudaError_t e = cudaFuncSetAttribute(k_product<MODE, false, BF16>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM);
-    if (e == cudaSuccess) e = cudaFuncSetAttribute(k_product<MODE, true, BF16>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM);
+    cudaError_t e = cudaFuncSetAttribute(k_product<MODE, NARROW, BF16>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(k_product<MODE, WIDE, BF16>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(k_product<MODE, PAIR, BF16>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t c = {};
     c.gridDim = dim3(2);
@@ -578,7 +581,7 @@ cudaError_t prepare_as(int* pairs)
     c.attrs = attr;
     c.numAttrs = 1;
     int n = 0;
-    e = cudaOccupancyMaxActiveClusters(&n, k_product<MODE, true, BF16>, &c);
+    e = cudaOccupancyMaxActiveClusters(&n, k_product<MODE, PAIR, BF16>, &c);
     if (n < *pairs) *pairs = n;
     return e;
 }

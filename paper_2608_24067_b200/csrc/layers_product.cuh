@@ -13,16 +13,17 @@ enum ProdMode {
     PROD_DW = 4       // out[e][m, n] = sum_rows A[row, m] B[row, n] over the rows of expert e
 };
 
-// Output tiles: `pair` = 256 x 256 by two blocks of a cluster, else 128 x 128 by one block.
-constexpr int PAIR_ROWS = 256, PAIR_COLS = 256, SINGLE_ROWS = 128, SINGLE_COLS = 128;
+// Output tiles: NARROW 128 x 128 and WIDE 128 x 256 by one block, PAIR 256 x 256 by two blocks of a cluster.
+enum ProdShape { NARROW = 0, WIDE = 1, PAIR = 2 };
+__host__ __device__ constexpr int shape_rows(int shape) { return shape == PAIR ? 256 : 128; }
+__host__ __device__ constexpr int shape_cols(int shape) { return shape == NARROW ? 128 : 256; }
 
 constexpr int EPI_TURNS = 2;  // epilogue warps per 32 rows of a block's tile; they take its pieces of 32 columns in turn
 
 // partial sums of h * g that a tile of PROD_DZ_TWO (half as wide as others) leaves for a row
-__host__ __device__ constexpr int tile_dots(bool pair)
+__host__ __device__ constexpr int tile_dots(int shape)
 {
-    const int pieces = (pair ? PAIR_COLS : SINGLE_COLS) / 2 / 32;
-    return pieces < EPI_TURNS ? pieces : EPI_TURNS;
+    return shape_cols(shape) / 2 / 32 < EPI_TURNS ? shape_cols(shape) / 2 / 32 : EPI_TURNS;
 }
 
 struct ProdArgs {
@@ -43,7 +44,7 @@ struct ProdArgs {
     float* column_sums;       // PROD_DZ, PROD_DZ_TWO: [rows / 32][2 cols or cols] sums of dz over 32 rows, or nullptr
     int64_t ld_extra;
     int bias_ld, dots;
-    int pair;
+    int shape;
     int row_tiles, col_tiles, experts;
     int splits;      // blocks that share a tile's sum (PROD_FWD, PROD_DX, PROD_DW; not grouped): part s goes to batch s of the output
     int rows, cols;  // extent of the outputs (PROD_DW: of one expert's)
@@ -56,9 +57,8 @@ struct ProdArgs {
 
 int launch_product(som_layers* l, ProdMode mode, const ProdArgs& args, cudaStream_t st);
 
-// 3-d tensor map over [batch][rows][cols] of 16-bit (bytes = 2) or fp32 (4) elements in boxes of [1][box_rows] rows of
-// box_bytes, 64 or 128 (the swizzle)
-int make_map(som_layers* l, CUtensorMap* map, const void* base, int bytes, int64_t cols, int64_t rows, int64_t batch,
-             int64_t ld, int64_t batch_stride, int box_bytes, int box_rows);
+// 3-d tensor map over [batch][rows][cols] of 16-bit (bytes = 2) or fp32 (4) elements in boxes of [1][box_rows] rows of 128 bytes
+int make_map(som_layers* l, CUtensorMap* map, const void* base, int bytes, int64_t cols, int64_t rows, int64_t batch, int64_t ld,
+             int64_t batch_stride, int box_rows);
 
 }  // namespace lay
