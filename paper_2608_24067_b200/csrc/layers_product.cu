@@ -1,7 +1,7 @@
 // Matrix products of the dense operators on the 5th-generation tensor cores.
 //
 // Persistent blocks, one per SM, walk the output tiles.  Warp 0 issues the TMA copies of a ring (64 k of both
-// operands a stage, 128-byte swizzle; six stages of 32 KB, or four of 48), warp 1 issues the matrix instructions (tcgen05.mma, fp32 accumulators in
+// operands a stage, 128-byte swizzle: 32 KB, or 48 for wide tiles), warp 1 issues the matrix instructions (tcgen05.mma, fp32 accumulators in
 // tensor memory), eight warps run the epilogue (sixteen were no faster where the epilogue counts, and slower elsewhere).  The accumulator is double-buffered, so that the epilogue of a tile runs
 // under the products of the next.  PROD_DZ_TWO keeps two products of a tile side by side, z with one buffer and g with two: the
 // next tile's g is multiplied while the epilogue reads this tile's z and g (with one buffer for both the 206 GFLOP of 4096
@@ -24,10 +24,14 @@ namespace {
 constexpr int BM = 128, BK = 64;
 constexpr int BOX = 64 * 128;      // bytes of a box of 64 rows
 constexpr int A_BYTES = 2 * BOX;   // a block's rows of A in a stage
-constexpr int MOST_STAGES = 6, RING_BYTES = MOST_STAGES * 2 * A_BYTES;
+// Bytes of the ring and buffers of an epilogue warp.  PROD_DW, whose sums may be short (an expert's rows), gives a stage of its
+// ring for a second buffer, so that a piece is staged while the one before is read.
+__host__ __device__ constexpr int ring_bytes(int mode) { return (mode == PROD_DW ? 5 : 6) * 2 * A_BYTES; }
+__host__ __device__ constexpr int out_buffers(int mode) { return mode == PROD_DW ? 2 : 1; }
 constexpr int EPI_WARPS = 4 * EPI_TURNS, THREADS = 32 * (2 + EPI_WARPS);
 constexpr int OUT_BYTES = 32 * 128;  // an epilogue warp's staged output: 32 rows of 128 bytes
-constexpr int SMEM = 1024 + RING_BYTES + EPI_WARPS * OUT_BYTES;
+constexpr int SMEM = 1024 + ring_bytes(PROD_FWD) + EPI_WARPS * OUT_BYTES;
+static_assert(SMEM == 1024 + ring_bytes(PROD_DW) + EPI_WARPS * 2 * OUT_BYTES, "one size for all modes");
 
 struct Tile {
     int row, col, expert;  // this block's first row and the tile's first column of the output, expert
@@ -92,13 +96,18 @@ __device__ __forceinline__ Tile tile_at(const ProdArgs& p, int idx, int width, i
 // columns.  Direct stores take the load/store pipe 32 cycles an instruction: too much where a tile's products are short
 // (PROD_DW at 512 rows an expert: 134 us staged, 178 us direct), but no waits, and no shared memory for up to three outputs
 // at once (PROD_DZ, PROD_DZ_TWO).
+template <int BUFFERS>
 struct Stager {
     unsigned char* buf;
-    int lane;
-    // the last store has read the buffer
+    int lane, other;  // other: distance to the other buffer
+    // the last store from this buffer has read it
     __device__ __forceinline__ void begin()
     {
-        if (lane == 0) store_wait_read<0>();
+        if (BUFFERS == 2) {
+            buf += other;
+            other = -other;
+        }
+        if (lane == 0) store_wait_read<BUFFERS - 1>();
         __syncwarp();
     }
     // 16 bytes of this lane's row
@@ -189,7 +198,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
     constexpr bool PAIRED = SHAPE == PAIR;
     constexpr int BN = shape_cols(SHAPE);
     constexpr int SHARE = PAIRED ? BN / 2 : BN;  // columns of B in this block
-    constexpr int STAGE_BYTES = A_BYTES + SHARE * 128, STAGES = RING_BYTES / STAGE_BYTES;
+    constexpr int STAGE_BYTES = A_BYTES + SHARE * 128, STAGES = ring_bytes(MODE) / STAGE_BYTES;
     constexpr uint32_t TMEM_COLUMNS = 2 * BN;
     extern __shared__ unsigned char smem_raw[];
     __shared__ __align__(8) uint64_t full[STAGES], empty[STAGES], acc_full[2], acc_empty[2], drained;
@@ -197,7 +206,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
     __shared__ int gave_up_sh;
     unsigned char* ring = smem_raw + ((1024u - (smem_addr(smem_raw) & 1023u)) & 1023u);
 
-    unsigned char* staged = ring + RING_BYTES;
+    unsigned char* staged = ring + ring_bytes(MODE);
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int rank = PAIRED ? (int)cluster_rank() : 0;
@@ -353,7 +362,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
         constexpr int STEP = MODE == PROD_FWD ? 16 : 8;
         const int piece = MODE == PROD_DZ || MODE == PROD_DZ_TWO || p.out32 ? 32 : 64, round = EPI_TURNS * piece;
         const int q = warp & 3, turn = (warp - 2) >> 2;
-        Stager s{staged + (warp - 2) * OUT_BYTES, lane};
+        Stager<out_buffers(MODE)> s{staged + (warp - 2) * out_buffers(MODE) * OUT_BYTES, lane, OUT_BYTES};
         int n_acc = 0;
         for (int idx = first_tile; idx < total; idx += step, ++n_acc) {
             const Tile t = tile_at<MODE, SHAPE>(p, idx, width, rank);
@@ -553,21 +562,25 @@ cudaError_t launch_as(som_layers* l, const ProdArgs& args, cudaStream_t st)
     return launch(l, k_product<MODE, SHAPE, BF16>, dim3((unsigned)(tiles < most ? tiles : most) * blocks), THREADS, SMEM, st, blocks, args);
 }
 
+// wide tiles are for grouped rows
+template <int MODE>
+constexpr bool HAS_WIDE = MODE == PROD_FWD || MODE == PROD_DZ_TWO || MODE == PROD_DX;
+
 template <int MODE>
 cudaError_t launch_mode(som_layers* l, const ProdArgs& a, cudaStream_t st)
 {
-    switch (a.shape) {
-        case NARROW: return a.bf16 ? launch_as<MODE, NARROW, true>(l, a, st) : launch_as<MODE, NARROW, false>(l, a, st);
-        case WIDE: return a.bf16 ? launch_as<MODE, WIDE, true>(l, a, st) : launch_as<MODE, WIDE, false>(l, a, st);
-        default: return a.bf16 ? launch_as<MODE, PAIR, true>(l, a, st) : launch_as<MODE, PAIR, false>(l, a, st);
-    }
+    if constexpr (HAS_WIDE<MODE>)
+        if (a.shape == WIDE) return a.bf16 ? launch_as<MODE, WIDE, true>(l, a, st) : launch_as<MODE, WIDE, false>(l, a, st);
+    if (a.shape == PAIR) return a.bf16 ? launch_as<MODE, PAIR, true>(l, a, st) : launch_as<MODE, PAIR, false>(l, a, st);
+    return a.bf16 ? launch_as<MODE, NARROW, true>(l, a, st) : launch_as<MODE, NARROW, false>(l, a, st);
 }
 
 template <int MODE, bool BF16>
 cudaError_t prepare_as(int* pairs)
 {
     cudaError_t e = cudaFuncSetAttribute(k_product<MODE, NARROW, BF16>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM);
-    if (e == cudaSuccess) e = cudaFuncSetAttribute(k_product<MODE, WIDE, BF16>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM);
+    if constexpr (HAS_WIDE<MODE>)
+        if (e == cudaSuccess) e = cudaFuncSetAttribute(k_product<MODE, WIDE, BF16>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM);
     if (e == cudaSuccess) e = cudaFuncSetAttribute(k_product<MODE, PAIR, BF16>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t c = {};
