@@ -257,6 +257,10 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
                 // the other half of the rows, in a single block they follow the gate's boxes.
                 const int b0 = !PAIRED ? t.col : gated && !B_MN ? t.col + rank * p.gate_rows : t.col + rank * (n1 / 2);
                 const int boxes = (PAIRED ? n1 / 2 : n1) / 64, gates = !PAIRED && gated && !B_MN ? boxes / 2 : boxes;
+                // a pair's second block has no rows in use at the end of an expert with few: it leaves A as it is (what its half of the
+                // product then holds is not read)
+                const bool rows_here = MODE == PROD_DW || t.row < t.live;
+                const uint32_t a_bytes = A_BYTES * (PAIRED && (MODE == PROD_DW || t.row + BM < t.live) ? 2 : 1);
                 const int it1 = (t.k + BK - 1) / BK, it2 = MODE == PROD_DZ_TWO ? (p.k2 + BK - 1) / BK : 0;
                 for (int it = 0; it < it1 + it2; ++it) {
                     if (!bar_wait(&empty[stage], phase ^ 1u, gave_up)) {
@@ -269,16 +273,16 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
                     const uint32_t bar = PAIRED ? cluster_addr(smem_addr(&full[stage]), 0) : smem_addr(&full[stage]);
                     if (MODE == PROD_DZ_TWO && it < it2) {
                         const int k = it * BK;
-                        if (rank == 0) bar_expect(&full[stage], (PAIRED ? 2 : 1) * (A_BYTES + SHARE2 * 128));
-                        tma_load<PAIRED>(sa, &p.a2, bar, k, t.row, 0);
+                        if (rank == 0) bar_expect(&full[stage], a_bytes + (PAIRED ? 2 : 1) * SHARE2 * 128);
+                        if (rows_here) tma_load<PAIRED>(sa, &p.a2, bar, k, t.row, 0);
                         for (int j = 0; j < SHARE2; j += 64) tma_load<PAIRED>(sb + j * 128, &p.b2, bar, t.col + rank * SHARE2 + j, k, t.expert);
                     } else {
                         const int k = t.k0 + (it - it2) * BK;
-                        if (rank == 0) bar_expect(&full[stage], (PAIRED ? 2 : 1) * (A_BYTES + boxes * BOX));
+                        if (rank == 0) bar_expect(&full[stage], a_bytes + (PAIRED ? 2 : 1) * boxes * BOX);
                         if (A_MN) {
                             tma_load<PAIRED>(sa, &p.a, bar, t.row, k, 0);
                             tma_load<PAIRED>(sa + BOX, &p.a, bar, t.row + 64, k, 0);
-                        } else {
+                        } else if (rows_here) {
                             tma_load<PAIRED>(sa, &p.a, bar, k, t.row, 0);
                         }
 #pragma unroll
