@@ -480,7 +480,9 @@ static SlotPlan carve_plan(Carver& c, int64_t T, int E, int k, int tile)
 }
 
 // So few slots that most experts in use have one: each slot reads its expert's weights by itself (a weight that two slots
-// read comes from L2 the second time).
+// read comes from L2 the second time).  In us, each slot by itself / slots ordered by expert, at D 2048, I 1024 unless said:
+// 32 slots of 128 experts (1024, 512) 25 / 40; 64 slots of 64 experts 128 / 124; 96 of 64 189 / 138; 16 slots of 8 experts 35 / 39;
+// 32 of 8 61 / 40; 16 of 8 (1024, 512) 19 / 27; 48 of 8 28 / 28.
 static bool few_slots(int64_t T, int E, int k) { return T * k <= 16 || (T * k <= 64 && T * k <= E); }
 
 // Rows of an expert's tiles: a pair's once the experts have rows enough; with fewer, a pair would mostly multiply padding, and
