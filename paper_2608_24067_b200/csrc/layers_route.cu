@@ -7,10 +7,11 @@
 // (minima and maxima only), so that the winner's lane just moves up its list.  16-bit logits fit such a key exactly.  Others
 // become fixed-point distances from an upper bound, and scores come from fast fp32 exponentials; so the gaps between
 // consecutive choices (the first one not taken among them) and between the last group kept and the first dropped are
-// compared with the errors of both keys.  Only a token with a smaller gap, one in fifty or fewer, is done again from exact
-// keys: logits as order-preserving integers, scores in fp64 rounded to fp32, so that the choice does not hang on the last bits
-// of one exponential.  16384 tokens x 256 experts with bias and groups: 61 us with every score in fp64, 46 us with fp32 scores
-// and unsorted exact keys.
+// compared with the errors of both keys.  Where a gap is smaller, the contested groups or places are settled from the exact keys
+// of those that contest them (of all experts where that is not enough): logits as order-preserving integers, scores in fp64
+// rounded to fp32, so that the choice does not hang on the last bits of one exponential.  2048 tokens x 256 experts with bias
+// and groups: 12.3 us; 20.5 us where a small gap sends the whole token to the exact keys; 16384 tokens: 61 us with every score
+// in fp64.
 #include "layers_math.cuh"
 #include "layers_slots.cuh"
 
@@ -235,6 +236,71 @@ __device__ __forceinline__ uint32_t ordered16(float x)
     return u & 0x8000u ? ~u & 0xffffu : u | 0x8000u;
 }
 
+// The exact key of one expert as an order-preserving integer, where it needs no other expert: a logit, or sigmoid + bias.
+template <int TYPE>
+__device__ __noinline__ uint32_t exact_key(const RouteArgs& a, int64_t row, int i, bool by_score)
+{
+    const float x = logit_at<TYPE>(a.logits, row + i);
+    float s = x;
+    if (by_score) {
+        s = (float)(1.0 / (1.0 + exp(-(double)x)));
+        if (a.bias) s += a.bias[i];
+    }
+    return x > -INFINITY && s == s ? som_ordered_bits(s + 0.f) : 0u;
+}
+
+// Which groups are kept, by one warp for one token: lane g holds the key of group g; `low` and `next` are the smallest key
+// kept and the largest one dropped, nearer than `margin`.  Groups beyond the margin on either side stay where they are.
+template <int TYPE>
+__device__ __noinline__ unsigned settle_groups(const RouteArgs& a, int64_t row, uint32_t key, uint32_t low, uint32_t next, uint32_t margin, int lane)
+{
+    const bool there = lane < a.groups && key;
+    const bool above = there && key >= next + margin, open = there && !above && key + margin > low;
+    unsigned kept = __ballot_sync(ALL, above), todo = __ballot_sync(ALL, open);
+    const int size = a.E / a.groups;
+    uint32_t mine = 0;
+    for (unsigned left = todo; left; left &= left - 1) {
+        const int g = __ffs(left) - 1;
+        uint32_t m1 = 0, m2 = 0;
+#pragma unroll 1
+        for (int i = lane; i < size; i += 32) merge2(m1, m2, exact_key<TYPE>(a, row, g * size + i, true), 0u);
+        const uint32_t b1 = __reduce_max_sync(ALL, m1);
+        const int owner = __ffs(__ballot_sync(ALL, m1 == b1)) - 1;
+        const uint32_t b2 = __reduce_max_sync(ALL, lane == owner ? m2 : m1);
+        if (lane == g) mine = group_key(b1, b2, a.group_best);
+    }
+    for (int n = a.top_groups - __popc(kept); n > 0; --n) {
+        const uint32_t m = __reduce_max_sync(ALL, open ? mine : 0u);
+        if (m == 0) break;
+        const int g = __ffs(__ballot_sync(ALL, open && mine == m)) - 1;
+        kept |= 1u << g;
+        if (lane == g) mine = 0;
+    }
+    return kept;
+}
+
+// Puts candidates (lanes 0 to n - 1: expert `index`) into the order of their exact keys; returns to lane j the j-th of k, or -1.
+template <int TYPE>
+__device__ __noinline__ int settle_places(const RouteArgs& a, int64_t row, int index, int n, bool by_score, int lane)
+{
+    uint32_t key = 0;
+    if (lane < n) key = exact_key<TYPE>(a, row, index, by_score);
+    __syncwarp();
+    int rank = 0;
+    for (int i = 0; i < n; ++i) {
+        const uint32_t k = __shfl_sync(ALL, key, i);
+        const int o = __shfl_sync(ALL, index, i);
+        rank += k > key || (k == key && k && o < index);
+    }
+    int at = -1;
+    for (int i = 0; i < a.k && i < n; ++i) {
+        const unsigned is = __ballot_sync(ALL, key && rank == i);
+        const int v = __shfl_sync(ALL, index, is ? __ffs(is) - 1 : 0);
+        if (lane == i && is) at = v;
+    }
+    return at;
+}
+
 template <int TYPE, int V>
 __global__ void __launch_bounds__(32 * ROUTE_WARPS, V <= 8 ? 4 : 2) k_route(const RouteArgs a)
 {
@@ -330,6 +396,7 @@ __global__ void __launch_bounds__(32 * ROUTE_WARPS, V <= 8 ? 4 : 2) k_route(cons
                 const uint32_t gk = a.group_best == 2 ? (m1 >> INDEX_BITS) + (m2 >> INDEX_BITS) : m1;
                 uint32_t mine = __shfl_sync(ALL, gk, lane * lanes & 31);  // lane g: group g
                 if (lane >= a.groups) mine = 0;
+                const uint32_t all = mine;
                 unsigned kept = 0;
                 uint32_t last = 0;
                 for (int r = 0; r < a.top_groups; ++r) {
@@ -340,9 +407,13 @@ __global__ void __launch_bounds__(32 * ROUTE_WARPS, V <= 8 ? 4 : 2) k_route(cons
                     if (lane == g) mine = 0;
                 }
                 const uint32_t next = last ? __reduce_max_sync(ALL, mine) : 0u;
-                if (!exact16 && next) {
-                    if (a.group_best == 2) sure = sure && last - next >= 2 * margin;
-                    else sure = sure && (last >> INDEX_BITS) - (next >> INDEX_BITS) >= margin;
+                if (!exact16 && next && sure) {
+                    const int shift = a.group_best == 2 ? 0 : INDEX_BITS;
+                    const uint32_t apart = a.group_best == 2 ? 2 * margin : margin;
+                    if ((last >> shift) - (next >> shift) < apart) {
+                        if (by_score && a.score == SOM_SCORE_SIGMOID) kept = settle_groups<TYPE>(a, row, all >> shift, last >> shift, next >> shift, apart, lane);
+                        else sure = false;
+                    }
                 }
                 if (!((kept >> my_group) & 1u)) {
 #pragma unroll
@@ -365,16 +436,35 @@ __global__ void __launch_bounds__(32 * ROUTE_WARPS, V <= 8 ? 4 : 2) k_route(cons
                 }
                 at = won ? (int)(INDEX_MASK - (won & INDEX_MASK)) : -1;
                 if (!exact16) {
-                    const float mx = at >= 0 ? logit_at<TYPE>(a.logits, row + at) + 0.f : 0.f;
-                    const float mb = at >= 0 && a.bias ? *(a.bias + at) : 0.f;
-                    const uint32_t above = __shfl_up_sync(ALL, won, 1);
-                    const float ax = __shfl_up_sync(ALL, mx, 1), ab = __shfl_up_sync(ALL, mb, 1);
-                    // Equal logits and biases tie exactly, and the index decided.  (Not between the last one taken and the
-                    // first one left: what comes after that one has not been looked at.)
-                    bool near = won && lane > 0 && (above >> INDEX_BITS) - (won >> INDEX_BITS) < margin &&
-                                !(lane < a.k && ax == mx && ab == mb);
-                    near |= won && lane < a.k && (won >> INDEX_BITS) <= 1u;  // beyond the keys' range
-                    if (__any_sync(ALL, near)) sure = false;
+                    if (__any_sync(ALL, won && lane < a.k && (won >> INDEX_BITS) <= 1u)) sure = false;  // beyond the keys' range
+                    uint32_t above = __shfl_up_sync(ALL, won, 1);
+                    // contested places: lane j's winner and the one above it
+                    unsigned near = __ballot_sync(ALL, won && lane > 0 && (above >> INDEX_BITS) - (won >> INDEX_BITS) < margin);
+                    if (near && sure) {
+                        if (by_score && a.score == SOM_SCORE_SOFTMAX) {
+                            sure = false;
+                        } else {
+                            // the contest for the last place: more winners, until one stands apart or none is left
+                            int n = __popc(__ballot_sync(ALL, won != 0));
+                            bool open = n > a.k && (near >> a.k & 1u);
+                            while (open && n < 32) {
+                                const uint32_t m = __reduce_max_sync(ALL, key[0]);
+                                if (m == 0) break;
+                                const uint32_t before = __shfl_sync(ALL, won, n - 1);
+                                open = (before >> INDEX_BITS) - (m >> INDEX_BITS) < margin;
+                                if (!open) break;
+                                if (lane == n) won = m;
+                                ++n;
+                                if (key[0] == m) {
+#pragma unroll
+                                    for (int v = 0; v + 1 < V; ++v) key[v] = key[v + 1];
+                                    key[V - 1] = 0u;
+                                }
+                            }
+                            if (n == 32) sure = false;
+                            else at = settle_places<TYPE>(a, row, (int)(INDEX_MASK - (won & INDEX_MASK)), n, by_score, lane);
+                        }
+                    }
                 }
                 if (lane >= a.k) at = -1;
             }
@@ -440,50 +530,9 @@ __device__ __forceinline__ void merge_down(uint32_t (&a)[L], const uint32_t (&b)
             if (!(i & h)) order2(a[i], a[i + h]);
 }
 
-// The exact key of one expert as an order-preserving integer, where it needs no other expert: a logit, or sigmoid + bias.
-template <int TYPE>
-__device__ __noinline__ uint32_t exact_key(const RouteArgs& a, int64_t row, int i, bool by_score)
-{
-    const float x = logit_at<TYPE>(a.logits, row + i);
-    float s = x;
-    if (by_score) {
-        s = (float)(1.0 / (1.0 + exp(-(double)x)));
-        if (a.bias) s += a.bias[i];
-    }
-    return x > -INFINITY && s == s ? som_ordered_bits(s + 0.f) : 0u;
-}
-
-// Which groups are kept, by one warp for one token: lane g holds the key of group g; `low` and `next` are the smallest key
-// kept and the largest one dropped, nearer than `margin`.  Groups beyond the margin on either side stay where they are.
-template <int TYPE>
-__device__ __noinline__ unsigned settle_groups(const RouteArgs& a, int64_t row, uint32_t key, uint32_t low, uint32_t next, uint32_t margin, int lane)
-{
-    const bool there = lane < a.groups && key;
-    const bool above = there && key >= next + margin, open = there && !above && key + margin > low;
-    unsigned kept = __ballot_sync(ALL, above), todo = __ballot_sync(ALL, open);
-    const int size = a.E / a.groups;
-    uint32_t mine = 0;
-    for (unsigned left = todo; left; left &= left - 1) {
-        const int g = __ffs(left) - 1;
-        uint32_t m1 = 0, m2 = 0;
-#pragma unroll 1
-        for (int i = lane; i < size; i += 32) merge2(m1, m2, exact_key<TYPE>(a, row, g * size + i, true), 0u);
-        const uint32_t b1 = __reduce_max_sync(ALL, m1);
-        const int owner = __ffs(__ballot_sync(ALL, m1 == b1)) - 1;
-        const uint32_t b2 = __reduce_max_sync(ALL, lane == owner ? m2 : m1);
-        if (lane == g) mine = group_key(b1, b2, a.group_best);
-    }
-    for (int n = a.top_groups - __popc(kept); n > 0; --n) {
-        const uint32_t m = __reduce_max_sync(ALL, open ? mine : 0u);
-        if (m == 0) break;
-        const int g = __ffs(__ballot_sync(ALL, open && mine == m)) - 1;
-        kept |= 1u << g;
-        if (lane == g) mine = 0;
-    }
-    return kept;
-}
-
-constexpr int ROUTE_MANY = 1024;  // tokens from which on k_route_many is used
+// Tokens from which on k_route_many is used.  256 experts, 8 chosen, without / with groups: 14.4 / 22.6 us at 4096 and at 8192
+// tokens (one pass of long latency), 18.5 / 25 at 16384; k_route 12.3 / 14.4, 16.4 / 20.5 and 22.6 / 28.6.
+constexpr int ROUTE_MANY = 8192;
 constexpr int QUAD_WARPS = 8, QUAD_ROWS = 8 * QUAD_WARPS;
 
 template <int TYPE, int L>
@@ -699,21 +748,12 @@ __global__ void __launch_bounds__(32 * QUAD_WARPS) k_route_many(const RouteArgs 
                     continue;
                 }
                 const int index = (int)(INDEX_MASK - (mine & INDEX_MASK));
-                const int64_t its_row = __shfl_sync(ALL, row, who);
-                uint32_t key = 0;
-                if (lane <= L && mine) key = exact_key<TYPE>(a, its_row, index, by_score);
-                __syncwarp();
-                int rank = 0;
-                for (int i = 0; i <= L; ++i) {
-                    const uint32_t k = __shfl_sync(ALL, key, i);
-                    const int o = __shfl_sync(ALL, index, i);
-                    rank += k > key || (k == key && k && o < index);
-                }
+                const int n = __popc(__ballot_sync(ALL, lane <= L && mine));
+                const int got = settle_places<TYPE>(a, __shfl_sync(ALL, row, who), index, n, by_score, lane);
 #pragma unroll
                 for (int i = 0; i < L; ++i) {
-                    const unsigned is = __ballot_sync(ALL, key && rank == i);
-                    const int v = __shfl_sync(ALL, index, is ? __ffs(is) - 1 : 0);
-                    if (quad == who >> 2) at[i] = i < a.k && is ? v : -1;
+                    const int v = __shfl_sync(ALL, got, i);
+                    if (quad == who >> 2) at[i] = i < a.k ? v : -1;
                 }
             }
         }

@@ -201,7 +201,7 @@ def test_route(L, T, E, k, opt, dtype, kind):
 @pytest.mark.parametrize("dtype,kind", [(FP32, "normal"), (BF16, "normal"), (FP16, "masked"), (FP32, "ties")])
 def test_route_many_tokens(L, E, k, opt, dtype, kind):
     """Many tokens take another form of the kernel: the choice is that of the same tokens a few at a time, and of the definition."""
-    T = 1301
+    T = 8201
     gen = torch.Generator().manual_seed(E + k)
     z = torch.randn(T, E, generator=gen) * 2
     if kind == "ties":
@@ -212,7 +212,7 @@ def test_route_many_tokens(L, E, k, opt, dtype, kind):
     logits = z.to(dtype).cuda()
     bias = (torch.randn(E, generator=gen) * 0.1).cuda() if opt.get("bias") else None
     got = L.route(logits, k, bias=bias, **{n: v for n, v in opt.items() if n != "bias"})
-    at = torch.cat([L.route(logits[i:i + 200], k, bias=bias, **{n: v for n, v in opt.items() if n != "bias"})["indices"] for i in range(0, T, 200)])
+    at = torch.cat([L.route(logits[i:i + 600], k, bias=bias, **{n: v for n, v in opt.items() if n != "bias"})["indices"] for i in range(0, T, 600)])
     assert torch.equal(got["indices"], at)
     assert torch.equal(got["counts"].long(), torch.bincount(at[at >= 0].long(), minlength=E))
     some = torch.arange(3, T, 61)
@@ -235,17 +235,18 @@ def test_route_order_of_near_scores(L):
         assert torch.equal(L.route(z.cuda(), 5, score=score, bias=bias.cuda())["indices"].cpu().long(), at)
 
 
+@pytest.mark.parametrize("T", [350, 8200])
 @pytest.mark.parametrize("groups,top_groups,group_best", [(1, 1, 1), (4, 2, 2), (4, 3, 1)])
 @pytest.mark.parametrize("score,spread", [("sigmoid", 2.0 ** -22), ("sigmoid", 2.0 ** -18), ("softmax", 2.0 ** -20)])
-def test_route_many_near_scores(L, score, spread, groups, top_groups, group_best):
-    """The same for many tokens: values from a coarse grid plus noise far below it, so that choices, boundaries and groups are
+def test_route_contested(L, T, score, spread, groups, top_groups, group_best):
+    """The same in both forms of the kernel: values from a coarse grid plus noise far below it, so that choices, boundaries and groups are
     contested in every token, some by two experts and some by many."""
     gen = torch.Generator().manual_seed(7)
-    T, E, k = 1040, 128, 8
+    T, E, k = T, 128, 8
     z = (torch.randn(T, E, generator=gen) * 4).round() / 4 + torch.randn(T, E, generator=gen) * spread
     bias = (torch.randn(E, generator=gen) * 4).round() / 64
     got = L.route(z.cuda(), k, score=score, bias=bias.cuda(), groups=groups, top_groups=top_groups, group_best=group_best)
-    some = torch.arange(0, T, 3)
+    some = torch.arange(0, T, 1 + T // 350)
     _, at, _, _ = ref.route(z[some], k, score, bias, groups, top_groups, group_best, True, 1.0)
     assert torch.equal(got["indices"][some].cpu().long(), at)
 
