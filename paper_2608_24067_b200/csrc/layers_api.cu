@@ -109,10 +109,11 @@ int check_sizes(int64_t a, int64_t b)
 
 int64_t tiles_of(int64_t n, int64_t width) { return (n + width - 1) / width; }
 
-// 16-bit operands of the products: the left one K-major in boxes of 128 rows; the right one, and M/N-major ones, of 64
-int map_left(som_layers* l, CUtensorMap* m, const void* p, int64_t cols, int64_t rows, int64_t ld)
+// 16-bit operands of the products: the left one K-major in boxes of 128 rows (LEFT_BOX where they are the experts'); the right
+// one, and M/N-major ones, of 64
+int map_left(som_layers* l, CUtensorMap* m, const void* p, int64_t cols, int64_t rows, int64_t ld, int box = 128)
 {
-    return make_map(l, m, p, 2, cols, rows, 1, ld, rows * ld, 128);
+    return make_map(l, m, p, 2, cols, rows, 1, ld, rows * ld, box);
 }
 int map_64(som_layers* l, CUtensorMap* m, const void* p, int64_t cols, int64_t rows, int64_t ld, int64_t batch = 1)
 {
@@ -579,7 +580,7 @@ int som_experts(som_layers* l, int type, int act, int gated, int64_t T, int32_t 
     LAY_TRY(launch_plan(l, p, indices, weights, weights_type, T, k, E, st));
     LAY_TRY(launch_gather(l, p, k, D, x, ldx, xp, nullptr, 0, nullptr, st));
     ProdArgs a = grouped(l, p, T * k, E, type, I, gated);
-    LAY_TRY(map_left(l, &a.a, xp, D, p.max_rows, D));
+    LAY_TRY(map_left(l, &a.a, xp, D, p.max_rows, D, LEFT_BOX));
     LAY_TRY(map_64(l, &a.b, w1, D, rows1, D, E));
     LAY_TRY(map_out(l, &a.o, h, 2, I, p.max_rows, I));
     a.bias = static_cast<const uint16_t*>(b1);
@@ -590,7 +591,7 @@ int som_experts(som_layers* l, int type, int act, int gated, int64_t T, int32_t 
     a.weigh = 1;
     LAY_TRY(launch_product(l, PROD_FWD, a, st));
     a = grouped(l, p, T * k, E, type, D, false);
-    LAY_TRY(map_left(l, &a.a, h, I, p.max_rows, I));
+    LAY_TRY(map_left(l, &a.a, h, I, p.max_rows, I, LEFT_BOX));
     LAY_TRY(map_64(l, &a.b, w2, I, D, I, E));
     LAY_TRY(map_out(l, &a.o, part, 4, D, p.max_rows, D));
     a.bias = static_cast<const uint16_t*>(b2);
@@ -647,9 +648,9 @@ int som_experts_backward(som_layers* l, int type, int act, int gated, int64_t T,
     LAY_TRY(launch_gather(l, p, k, D, x, ldx, xp, dy, lddy, dyp, st));
     // -> dz, the weighted h, partial sums of <h, g>
     ProdArgs a = z;
-    LAY_TRY(map_left(l, &a.a, xp, D, p.max_rows, D));
+    LAY_TRY(map_left(l, &a.a, xp, D, p.max_rows, D, LEFT_BOX));
     LAY_TRY(map_64(l, &a.b, w1, D, rows1, D, E));
-    LAY_TRY(map_left(l, &a.a2, dyp, D, p.max_rows, D));
+    LAY_TRY(map_left(l, &a.a2, dyp, D, p.max_rows, D, LEFT_BOX));
     LAY_TRY(map_64(l, &a.b2, w2, I, D, I, E));
     a.o0 = dz;
     a.ld0 = rows1;
@@ -668,7 +669,7 @@ int som_experts_backward(som_layers* l, int type, int act, int gated, int64_t T,
     if (db2) LAY_TRY(launch_column_sums(l, p, E, 0, dyp, D, D, db2, a.bf16, st));
     // dx
     a = grouped(l, p, T * k, E, type, D, false);
-    LAY_TRY(map_left(l, &a.a, dz, rows1, p.max_rows, rows1));
+    LAY_TRY(map_left(l, &a.a, dz, rows1, p.max_rows, rows1, LEFT_BOX));
     LAY_TRY(map_64(l, &a.b, w1, D, rows1, D, E));
     LAY_TRY(map_out(l, &a.o, part, 4, D, p.max_rows, D));
     a.k1 = (int)rows1;

@@ -257,10 +257,18 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
                 // the other half of the rows, in a single block they follow the gate's boxes.
                 const int b0 = !PAIRED ? t.col : gated && !B_MN ? t.col + rank * p.gate_rows : t.col + rank * (n1 / 2);
                 const int boxes = (PAIRED ? n1 / 2 : n1) / 64, gates = !PAIRED && gated && !B_MN ? boxes / 2 : boxes;
-                // a pair's second block has no rows in use at the end of an expert with few: it leaves A as it is (what its half of the
-                // product then holds is not read)
-                const bool rows_here = MODE == PROD_DW || t.row < t.live;
-                const uint32_t a_bytes = A_BYTES * (PAIRED && (MODE == PROD_DW || t.row + BM < t.live) ? 2 : 1);
+                // Experts' rows of A come in boxes of LEFT_BOX; where none of a box is in use it is read from beyond the matrix, which
+                // gives zeros without traffic (and multiplying zeros takes less power).
+                const bool grouped = MODE != PROD_DW && p.seg;
+                auto load_rows = [&](unsigned char* to, const CUtensorMap* map, uint32_t bar, int k) {
+                    if (!grouped) {
+                        tma_load<PAIRED>(to, map, bar, k, t.row, 0);
+                        return;
+                    }
+#pragma unroll
+                    for (int r = 0; r < BM; r += LEFT_BOX) tma_load<PAIRED>(to + r * 128, map, bar, k, t.row + r < t.live ? t.row + r : p.rows, 0);
+                };
+                constexpr uint32_t a_bytes = A_BYTES * (PAIRED ? 2 : 1);
                 const int it1 = (t.k + BK - 1) / BK, it2 = MODE == PROD_DZ_TWO ? (p.k2 + BK - 1) / BK : 0;
                 for (int it = 0; it < it1 + it2; ++it) {
                     if (!bar_wait(&empty[stage], phase ^ 1u, gave_up)) {
@@ -274,7 +282,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
                     if (MODE == PROD_DZ_TWO && it < it2) {
                         const int k = it * BK;
                         if (rank == 0) bar_expect(&full[stage], a_bytes + (PAIRED ? 2 : 1) * SHARE2 * 128);
-                        if (rows_here) tma_load<PAIRED>(sa, &p.a2, bar, k, t.row, 0);
+                        load_rows(sa, &p.a2, bar, k);
                         for (int j = 0; j < SHARE2; j += 64) tma_load<PAIRED>(sb + j * 128, &p.b2, bar, t.col + rank * SHARE2 + j, k, t.expert);
                     } else {
                         const int k = t.k0 + (it - it2) * BK;
@@ -282,8 +290,8 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
                         if (A_MN) {
                             tma_load<PAIRED>(sa, &p.a, bar, t.row, k, 0);
                             tma_load<PAIRED>(sa + BOX, &p.a, bar, t.row + 64, k, 0);
-                        } else if (rows_here) {
-                            tma_load<PAIRED>(sa, &p.a, bar, k, t.row, 0);
+                        } else {
+                            load_rows(sa, &p.a, bar, k);
                         }
 #pragma unroll
                         for (int j = 0; j < SHARE / 64; ++j) {
