@@ -115,6 +115,11 @@ int map_left(som_layers* l, CUtensorMap* m, const void* p, int64_t cols, int64_t
 {
     return make_map(l, m, p, 2, cols, rows, 1, ld, rows * ld, box);
 }
+int map_right(som_layers* l, ProdArgs* a, ProdMode mode, bool gated, const void* p, int64_t cols, int64_t rows, int64_t batch = 1)
+{
+    a->right_box = right_box(mode, a->shape, gated);
+    return make_map(l, &a->b, p, 2, cols, rows, batch, cols, rows * cols, a->right_box);
+}
 int map_64(som_layers* l, CUtensorMap* m, const void* p, int64_t cols, int64_t rows, int64_t ld, int64_t batch = 1)
 {
     return make_map(l, m, p, 2, cols, rows, batch, ld, rows * ld, 64);
@@ -258,7 +263,6 @@ int som_linear(som_layers* l, int type, int act, int gated, int64_t T, int64_t D
     }
     ProdArgs a = {};
     LAY_TRY(map_left(l, &a.a, x, D, T, ldx));
-    LAY_TRY(map_64(l, &a.b, w, D, rows, D));
     a.bf16 = type == SOM_BF16;
     a.flags = l->flags;
     a.experts = 1;
@@ -267,6 +271,7 @@ int som_linear(som_layers* l, int type, int act, int gated, int64_t T, int64_t D
     a.splits = splits_of(l, a, D);
     if (a.splits > 1) {
         LAY_TRY(ensure(l, (size_t)a.splits * T * rows * sizeof(float)));
+        LAY_TRY(map_right(l, &a, PROD_FWD, false, w, D, rows));
         FinishArgs f = {};
         f.rows = T;
         f.n = (int)rows;
@@ -286,6 +291,7 @@ int som_linear(som_layers* l, int type, int act, int gated, int64_t T, int64_t D
     a.extra = static_cast<const uint16_t*>(residual);
     a.ld_extra = ldr;
     set_tiles(l, &a, T, F, gated);
+    LAY_TRY(map_right(l, &a, PROD_FWD, gated, w, D, rows));
     a.gate_rows = gated ? (int)F : 0;
     a.act = act;
     return launch_product(l, PROD_FWD, a, st);
@@ -350,8 +356,8 @@ int som_linear_backward(som_layers* l, int type, int act, int gated, int64_t T, 
         dz = z_grad;
         lddz = rows;
         LAY_TRY(map_left(l, &z.a, x, D, T, ldx));
-        LAY_TRY(map_64(l, &z.b, w, D, rows, D));
         if (z.splits > 1) {
+            LAY_TRY(map_right(l, &z, PROD_FWD, false, w, D, rows));
             f.rows = T;
             f.n = (int)rows;
             f.cols = (int)F;
@@ -373,6 +379,7 @@ int som_linear_backward(som_layers* l, int type, int act, int gated, int64_t T, 
             z.ld_extra = lddy;
             z.column_sums = dbias ? sums : nullptr;
             set_tiles(l, &z, T, F, gated);
+            LAY_TRY(map_right(l, &z, PROD_DZ, gated, w, D, rows));
             z.gate_rows = gated ? (int)F : 0;
             LAY_TRY(launch_product(l, PROD_DZ, z, st));
         }
@@ -507,6 +514,7 @@ static ProdArgs grouped(const som_layers* l, const SlotPlan& p, int64_t slots, i
     a.rows = p.max_rows;
     a.cols = (int)cols;
     a.splits = 1;
+    a.columns_first = 1;  // (all its products follow the gather or a later kernel)
     a.bf16 = type == SOM_BF16;
     a.flags = l->flags;
     return a;
@@ -581,7 +589,7 @@ int som_experts(som_layers* l, int type, int act, int gated, int64_t T, int32_t 
     LAY_TRY(launch_gather(l, p, k, D, x, ldx, xp, nullptr, 0, nullptr, st));
     ProdArgs a = grouped(l, p, T * k, E, type, I, gated);
     LAY_TRY(map_left(l, &a.a, xp, D, p.max_rows, D, LEFT_BOX));
-    LAY_TRY(map_64(l, &a.b, w1, D, rows1, D, E));
+    LAY_TRY(map_right(l, &a, PROD_FWD, gated, w1, D, rows1, E));
     LAY_TRY(map_out(l, &a.o, h, 2, I, p.max_rows, I));
     a.bias = static_cast<const uint16_t*>(b1);
     a.bias_ld = (int)rows1;
@@ -592,7 +600,7 @@ int som_experts(som_layers* l, int type, int act, int gated, int64_t T, int32_t 
     LAY_TRY(launch_product(l, PROD_FWD, a, st));
     a = grouped(l, p, T * k, E, type, D, false);
     LAY_TRY(map_left(l, &a.a, h, I, p.max_rows, I, LEFT_BOX));
-    LAY_TRY(map_64(l, &a.b, w2, I, D, I, E));
+    LAY_TRY(map_right(l, &a, PROD_FWD, false, w2, I, D, E));
     LAY_TRY(map_out(l, &a.o, part, 4, D, p.max_rows, D));
     a.bias = static_cast<const uint16_t*>(b2);
     a.bias_ld = (int)D;
@@ -649,7 +657,7 @@ int som_experts_backward(som_layers* l, int type, int act, int gated, int64_t T,
     // -> dz, the weighted h, partial sums of <h, g>
     ProdArgs a = z;
     LAY_TRY(map_left(l, &a.a, xp, D, p.max_rows, D, LEFT_BOX));
-    LAY_TRY(map_64(l, &a.b, w1, D, rows1, D, E));
+    LAY_TRY(map_right(l, &a, PROD_DZ_TWO, gated, w1, D, rows1, E));
     LAY_TRY(map_left(l, &a.a2, dyp, D, p.max_rows, D, LEFT_BOX));
     LAY_TRY(map_64(l, &a.b2, w2, I, D, I, E));
     a.o0 = dz;
@@ -681,6 +689,7 @@ int som_experts_backward(som_layers* l, int type, int act, int gated, int64_t T,
     a.seg = p.seg;
     a.count = p.count;
     a.experts = E;
+    a.columns_first = 1;
     a.bf16 = type == SOM_BF16;
     a.flags = l->flags;
     ProdArgs b = a;

@@ -42,14 +42,21 @@ struct Tile {
 
 __device__ __forceinline__ int round64(int n) { return (n + 63) & ~63; }
 
-template <int MODE>
+// EARLY: the plan is read before the kernel in front is over, past what this SM's L1 holds
+template <bool EARLY>
+__device__ __forceinline__ int plan_at(const int* p)
+{
+    return EARLY ? __ldcg(p) : *p;
+}
+
+template <int MODE, bool EARLY = false>
 __device__ __forceinline__ int tile_count(const ProdArgs& p)
 {
     if (MODE == PROD_DW) return p.experts * p.row_tiles * p.col_tiles * p.splits;
-    return (p.tiles ? *p.tiles : p.row_tiles) * p.col_tiles * p.splits;
+    return (p.tiles ? plan_at<EARLY>(p.tiles) : p.row_tiles) * p.col_tiles * p.splits;
 }
 
-template <int MODE, int SHAPE>
+template <int MODE, int SHAPE, bool EARLY = false>
 __device__ __forceinline__ Tile tile_at(const ProdArgs& p, int idx, int width, int rank)
 {
     constexpr int ROWS = shape_rows(SHAPE);
@@ -65,19 +72,19 @@ __device__ __forceinline__ Tile tile_at(const ProdArgs& p, int idx, int width, i
         const int rest = idx - t.expert * per, rt = rest / p.col_tiles;
         t.row = rt * ROWS + rank * BM;
         t.col = (rest - rt * p.col_tiles) * width;
-        t.k0 = p.seg ? p.seg[t.expert] : 0;
-        t.k = p.seg ? round64(p.count[t.expert]) : p.k1;
+        t.k0 = p.seg ? plan_at<EARLY>(p.seg + t.expert) : 0;
+        t.k = p.seg ? round64(plan_at<EARLY>(p.count + t.expert)) : p.k1;
         t.live = t.store = p.rows;
     } else {
         const int rt = idx / p.col_tiles;
         t.row = rt * ROWS + rank * BM;
         t.col = (idx - rt * p.col_tiles) * width;
-        t.expert = p.tile_expert ? p.tile_expert[rt] : 0;
+        t.expert = p.tile_expert ? plan_at<EARLY>(p.tile_expert + rt) : 0;
         t.k0 = 0;
         t.k = p.k1;
         t.live = t.store = p.rows;
         if (p.seg) {
-            const int s = p.seg[t.expert], n = p.count[t.expert];
+            const int s = plan_at<EARLY>(p.seg + t.expert), n = plan_at<EARLY>(p.count + t.expert);
             t.live = s + n;
             // the sums over an expert's rows (PROD_DW) run over whole steps of 64 rows
             t.store = MODE == PROD_DZ_TWO ? s + round64(n) : t.live;
@@ -232,7 +239,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
     __syncthreads();
     if (PAIRED) cluster_sync();  // the other block's barriers are ready
     tc_fence_after();
-    enter();
+    if (warp > 0) enter();
     const uint32_t tmem = tmem_sh;
     volatile int* gave_up = &gave_up_sh;
 
@@ -241,7 +248,6 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
     // PROD_DZ_TWO: half in any case; the second product takes the other BN columns of tensor memory in turns of BN / 2.
     const int width = MODE == PROD_DZ_TWO || (gated && (MODE == PROD_FWD || MODE == PROD_DZ)) ? BN / 2 : BN;
     const int n1 = MODE == PROD_DZ_TWO && !gated ? BN / 2 : BN;  // accumulator columns of the first product
-    const int total = tile_count<MODE>(p);
     constexpr int N2 = BN / 2, SHARE2 = PAIRED ? N2 / 2 : N2;  // columns of the second product, and of its B in this block
     const int step = PAIRED ? gridDim.x >> 1 : gridDim.x, first_tile = PAIRED ? blockIdx.x >> 1 : blockIdx.x;
 
@@ -251,55 +257,66 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
             uint32_t phase = 0;
             int64_t issued = 0;
             bool ok = true;
+            constexpr int A_ALL = A_BYTES * (PAIRED ? 2 : 1);
+            // the same for all tiles: steps of the second product (which comes first); columns of the first product's B in this block,
+            // and how many of them are the gate's (gated: a pair's second block has the other half, in a single block they follow)
+            const int it2 = MODE == PROD_DZ_TWO ? (p.k2 + BK - 1) / BK : 0;
+            const int share = PAIRED ? n1 / 2 : n1, gates = !PAIRED && gated && !B_MN ? share / 2 : share;
+            const int from = !PAIRED ? 0 : gated && !B_MN ? p.gate_rows : share;
+            const int box = B_MN ? 64 : p.right_box, all1 = A_ALL + (PAIRED ? 2 : 1) * share * 128, all2 = A_ALL + N2 * 128;
+            // the leader's barrier counts both blocks' bytes
+            const uint32_t full0 = PAIRED ? cluster_addr(smem_addr(&full[0]), 0) : smem_addr(&full[0]);
+            auto load_columns = [&](const Tile& t, int it, int s) {
+                unsigned char* sb = ring + s * STAGE_BYTES + A_BYTES;
+                const uint32_t bar = full0 + 8 * s;
+                if (MODE == PROD_DZ_TWO && it < it2) {
+                    if (rank == 0) bar_expect(&full[s], all2);
+                    for (int j = 0; j < SHARE2; j += 64) tma_load<PAIRED>(sb + j * 128, &p.b2, bar, t.col + rank * SHARE2 + j, it * BK, t.expert);
+                    return;
+                }
+                const int b0 = t.col + rank * from, k = t.k0 + (it - it2) * BK;
+                if (rank == 0) bar_expect(&full[s], all1);
+                for (int j = 0; j < share; j += box) {
+                    if (B_MN) tma_load<PAIRED>(sb + j * 128, &p.b, bar, b0 + j, k, MODE == PROD_DW ? 0 : t.expert);
+                    else tma_load<PAIRED>(sb + j * 128, &p.b, bar, k, j < gates ? b0 + j : b0 + j - gates + p.gate_rows, t.expert);
+                }
+            };
+            auto load_rows = [&](const Tile& t, int it, int s) {
+                unsigned char* sa = ring + s * STAGE_BYTES;
+                const uint32_t bar = full0 + 8 * s;
+                const bool second = MODE == PROD_DZ_TWO && it < it2;
+                const CUtensorMap* map = second ? &p.a2 : &p.a;
+                const int k = second ? it * BK : t.k0 + (it - it2) * BK;
+                if (A_MN) {
+                    tma_load<PAIRED>(sa, map, bar, t.row, k, 0);
+                    tma_load<PAIRED>(sa + BOX, map, bar, t.row + 64, k, 0);
+                } else if (p.seg) {
+                    // Experts' rows come in boxes of LEFT_BOX; where none of a box is in use it is read from beyond the matrix, which
+                    // gives zeros without traffic (and multiplying zeros takes less power).
+#pragma unroll
+                    for (int r = 0; r < BM; r += LEFT_BOX) tma_load<PAIRED>(sa + r * 128, map, bar, k, t.row + r < t.live ? t.row + r : p.rows, 0);
+                } else {
+                    tma_load<PAIRED>(sa, map, bar, k, t.row, 0);
+                }
+            };
+            int ahead = 0;  // stages of the first tile whose columns are on their way
+            if (p.columns_first && first_tile < tile_count<MODE, true>(p)) {
+                const Tile t = tile_at<MODE, SHAPE, true>(p, first_tile, width, rank);
+                const int n = (t.k + BK - 1) / BK + it2;
+                for (; ahead < STAGES && ahead < n; ++ahead) load_columns(t, ahead, ahead);
+            }
+            enter();
+            const int total = tile_count<MODE>(p);
             for (int idx = first_tile; ok && idx < total; idx += step) {
                 const Tile t = tile_at<MODE, SHAPE>(p, idx, width, rank);
-                // First row (K-major) or column of this block's columns of B, in boxes of 64.  Gated: a pair's second block has
-                // the other half of the rows, in a single block they follow the gate's boxes.
-                const int b0 = !PAIRED ? t.col : gated && !B_MN ? t.col + rank * p.gate_rows : t.col + rank * (n1 / 2);
-                const int boxes = (PAIRED ? n1 / 2 : n1) / 64, gates = !PAIRED && gated && !B_MN ? boxes / 2 : boxes;
-                // Experts' rows of A come in boxes of LEFT_BOX; where none of a box is in use it is read from beyond the matrix, which
-                // gives zeros without traffic (and multiplying zeros takes less power).
-                const bool grouped = MODE != PROD_DW && p.seg;
-                auto load_rows = [&](unsigned char* to, const CUtensorMap* map, uint32_t bar, int k) {
-                    if (!grouped) {
-                        tma_load<PAIRED>(to, map, bar, k, t.row, 0);
-                        return;
-                    }
-#pragma unroll
-                    for (int r = 0; r < BM; r += LEFT_BOX) tma_load<PAIRED>(to + r * 128, map, bar, k, t.row + r < t.live ? t.row + r : p.rows, 0);
-                };
-                constexpr uint32_t a_bytes = A_BYTES * (PAIRED ? 2 : 1);
-                const int it1 = (t.k + BK - 1) / BK, it2 = MODE == PROD_DZ_TWO ? (p.k2 + BK - 1) / BK : 0;
-                for (int it = 0; it < it1 + it2; ++it) {
+                const int n = (t.k + BK - 1) / BK + it2;
+                for (int it = 0; it < n; ++it) {
                     if (!bar_wait(&empty[stage], phase ^ 1u, gave_up)) {
                         ok = false;
                         break;
                     }
-                    unsigned char* sa = ring + stage * STAGE_BYTES;
-                    unsigned char* sb = sa + A_BYTES;
-                    // the leader's barrier counts both blocks' bytes
-                    const uint32_t bar = PAIRED ? cluster_addr(smem_addr(&full[stage]), 0) : smem_addr(&full[stage]);
-                    if (MODE == PROD_DZ_TWO && it < it2) {
-                        const int k = it * BK;
-                        if (rank == 0) bar_expect(&full[stage], a_bytes + (PAIRED ? 2 : 1) * SHARE2 * 128);
-                        load_rows(sa, &p.a2, bar, k);
-                        for (int j = 0; j < SHARE2; j += 64) tma_load<PAIRED>(sb + j * 128, &p.b2, bar, t.col + rank * SHARE2 + j, k, t.expert);
-                    } else {
-                        const int k = t.k0 + (it - it2) * BK;
-                        if (rank == 0) bar_expect(&full[stage], a_bytes + (PAIRED ? 2 : 1) * boxes * BOX);
-                        if (A_MN) {
-                            tma_load<PAIRED>(sa, &p.a, bar, t.row, k, 0);
-                            tma_load<PAIRED>(sa + BOX, &p.a, bar, t.row + 64, k, 0);
-                        } else {
-                            load_rows(sa, &p.a, bar, k);
-                        }
-#pragma unroll
-                        for (int j = 0; j < SHARE / 64; ++j) {
-                            if (j >= boxes) break;
-                            if (B_MN) tma_load<PAIRED>(sb + j * BOX, &p.b, bar, b0 + 64 * j, k, MODE == PROD_DW ? 0 : t.expert);
-                            else tma_load<PAIRED>(sb + j * BOX, &p.b, bar, k, j < gates ? b0 + 64 * j : b0 + 64 * (j - gates) + p.gate_rows, t.expert);
-                        }
-                    }
+                    load_rows(t, it, stage);
+                    if (issued >= ahead) load_columns(t, it, stage);
                     ++issued;
                     if (++stage == STAGES) {
                         stage = 0;
@@ -307,6 +324,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
                     }
                 }
             }
+            if (issued < ahead) issued = ahead;
             if (!ok && rank == 0) {  // copies still in flight write shared memory: let them land before the block leaves
                 const long long t0 = clock64();
                 for (int s = 0; s < STAGES; ++s) {
@@ -320,6 +338,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
             int stage = 0, n_acc = 0;
             uint32_t phase = 0;
             bool ok = true;
+            const int total = tile_count<MODE>(p);
             const uint32_t idesc1 = mma_desc(BF16, A_MN, B_MN, PAIRED ? 256 : 128, n1);
             const uint32_t idesc2 = mma_desc(BF16, 0, 1, PAIRED ? 256 : 128, N2);
             for (int idx = first_tile; ok && idx < total; idx += step, ++n_acc) {
@@ -373,7 +392,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
         // of staged outputs, or 32 columns of direct ones, in steps of as many columns as the registers hold.
         constexpr int STEP = MODE == PROD_FWD ? 16 : 8;
         const int piece = MODE == PROD_DZ || MODE == PROD_DZ_TWO || p.out32 ? 32 : 64, round = EPI_TURNS * piece;
-        const int q = warp & 3, turn = (warp - 2) >> 2;
+        const int q = warp & 3, turn = (warp - 2) >> 2, total = tile_count<MODE>(p);
         Stager<out_buffers(MODE)> s{staged + (warp - 2) * out_buffers(MODE) * OUT_BYTES, lane, OUT_BYTES};
         int n_acc = 0;
         for (int idx = first_tile; idx < total; idx += step, ++n_acc) {
