@@ -385,8 +385,21 @@ int som_linear_backward(som_layers* l, int type, int act, int gated, int64_t T, 
         }
     }
     if (dbias) {
-        if (again && z.splits == 1) LAY_TRY(launch_join_sums(l, SlotPlan(), 1, T, sums, rows, dbias, a.bf16, st));
-        else LAY_TRY(launch_column_sums(l, SlotPlan(), 1, T, dz, lddz, rows, dbias, a.bf16, st));
+        EndArgs s = {};
+        s.rows = T;
+        s.E = 1;
+        s.bf16 = a.bf16;
+        if (again && z.splits == 1) {
+            s.sums = sums;
+            s.sums_cols = (int)rows;
+            s.sums_out = static_cast<uint16_t*>(dbias);
+        } else {
+            s.v = static_cast<const uint16_t*>(dz);
+            s.ldv = lddz;
+            s.v_cols = (int)rows;
+            s.v_sums = static_cast<uint16_t*>(dbias);
+        }
+        LAY_TRY(launch_ends(l, s, st));
     }
     f = FinishArgs();
     f.mode = FINISH_SUM;
@@ -608,7 +621,18 @@ int som_experts(som_layers* l, int type, int act, int gated, int64_t T, int32_t 
     a.weigh = 2;
     a.out32 = 1;
     LAY_TRY(launch_product(l, PROD_FWD, a, st));
-    return launch_join(l, p, T, k, D, part, residual, ldr, y, ldy, a.bf16, st);
+    EndArgs s = {};
+    s.p = p;
+    s.T = T;
+    s.k = k;
+    s.D = (int)D;
+    s.bf16 = a.bf16;
+    s.part = part;
+    s.residual = static_cast<const uint16_t*>(residual);
+    s.ldr = ldr;
+    s.y = static_cast<uint16_t*>(y);
+    s.ldy = ldy;
+    return launch_ends(l, s, st);
 }
 
 int som_experts_backward(som_layers* l, int type, int act, int gated, int64_t T, int32_t E, int32_t k, int64_t D, int64_t I,
@@ -672,10 +696,7 @@ int som_experts_backward(som_layers* l, int type, int act, int gated, int64_t T,
     a.k1 = a.k2 = (int)D;
     a.act = act;
     LAY_TRY(launch_product(l, PROD_DZ_TWO, a, st));
-    LAY_TRY(launch_dweights(l, p, indices, T, k, D, dot, a.dots, b2, dy, lddy, dweights, weights_type, a.bf16, st));
-    if (db1) LAY_TRY(launch_join_sums(l, p, E, 0, sums, rows1, db1, a.bf16, st));
-    if (db2) LAY_TRY(launch_column_sums(l, p, E, 0, dyp, D, D, db2, a.bf16, st));
-    // dx
+    // dx; with its join all other sums
     a = grouped(l, p, T * k, E, type, D, false);
     LAY_TRY(map_left(l, &a.a, dz, rows1, p.max_rows, rows1, LEFT_BOX));
     LAY_TRY(map_64(l, &a.b, w1, D, rows1, D, E));
@@ -683,7 +704,32 @@ int som_experts_backward(som_layers* l, int type, int act, int gated, int64_t T,
     a.k1 = (int)rows1;
     a.out32 = 1;
     LAY_TRY(launch_product(l, PROD_DX, a, st));
-    LAY_TRY(launch_join(l, p, T, k, D, part, nullptr, 0, dx, D, a.bf16, st));
+    EndArgs s = {};
+    s.p = p;
+    s.T = T;
+    s.k = k;
+    s.D = (int)D;
+    s.E = E;
+    s.bf16 = a.bf16;
+    s.part = part;
+    s.y = static_cast<uint16_t*>(dx);
+    s.ldy = D;
+    s.dot = dot;
+    s.dots = z.dots;
+    s.indices = indices;
+    s.b2 = static_cast<const uint16_t*>(b2);
+    s.dy = static_cast<const uint16_t*>(dy);
+    s.lddy = lddy;
+    s.dweights = dweights;
+    s.weights_type = weights_type;
+    s.sums = sums;
+    s.sums_cols = (int)rows1;
+    s.sums_out = static_cast<uint16_t*>(db1);
+    s.v = dyp;
+    s.ldv = D;
+    s.v_cols = (int)D;
+    s.v_sums = static_cast<uint16_t*>(db2);
+    LAY_TRY(launch_ends(l, s, st));
     // dw1 = dz^T x, dw2 = dy^T (weighted h)
     a = ProdArgs();
     a.seg = p.seg;

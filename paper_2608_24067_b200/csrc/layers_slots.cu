@@ -236,57 +236,52 @@ __global__ void __launch_bounds__(256) k_gather(SlotPlan p, int k, int D, const 
 }
 
 // y[t] = residual[t] + sum over j of part[pos[t][j]], in the order of j
-__global__ void __launch_bounds__(256) k_join(const int* pos, int64_t T, int k, int D, const float* part, const uint16_t* residual,
-                                              int64_t ldr, uint16_t* y, int64_t ldy, int bf16)
+__device__ __forceinline__ void join_rows(const EndArgs& a, int block)
 {
-    enter();
-    const int chunks = D / 8;
-    for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < T * chunks; i += (int64_t)gridDim.x * blockDim.x) {
+    const int chunks = a.D / 8;
+    for (int64_t i = (int64_t)block * blockDim.x + threadIdx.x; i < a.T * chunks; i += (int64_t)a.join_blocks * blockDim.x) {
         const int64_t t = i / chunks;
         const int c = (int)(i % chunks);
         float v[8];
-        if (residual) {
-            load8(residual + (size_t)t * ldr + 8 * c, v, bf16);
+        if (a.residual) {
+            load8(a.residual + (size_t)t * a.ldr + 8 * c, v, a.bf16);
         } else {
 #pragma unroll
             for (int j = 0; j < 8; ++j) v[j] = 0.f;
         }
-        for (int j = 0; j < k; ++j) {
-            const int row = pos[t * k + j];
+        for (int j = 0; j < a.k; ++j) {
+            const int row = a.p.pos[t * a.k + j];
             if (row < 0) continue;
-            const float4* q = reinterpret_cast<const float4*>(part + (size_t)row * D + 8 * c);
-            const float4 a = q[0], b = q[1];
-            v[0] += a.x, v[1] += a.y, v[2] += a.z, v[3] += a.w;
-            v[4] += b.x, v[5] += b.y, v[6] += b.z, v[7] += b.w;
+            const float4* q = reinterpret_cast<const float4*>(a.part + (size_t)row * a.D + 8 * c);
+            const float4 x = q[0], y = q[1];
+            v[0] += x.x, v[1] += x.y, v[2] += x.z, v[3] += x.w;
+            v[4] += y.x, v[5] += y.y, v[6] += y.z, v[7] += y.w;
         }
         uint4 u;
-        u.x = pack2(v[0], v[1], bf16);
-        u.y = pack2(v[2], v[3], bf16);
-        u.z = pack2(v[4], v[5], bf16);
-        u.w = pack2(v[6], v[7], bf16);
-        *reinterpret_cast<uint4*>(y + (size_t)t * ldy + 8 * c) = u;
+        u.x = pack2(v[0], v[1], a.bf16);
+        u.y = pack2(v[2], v[3], a.bf16);
+        u.z = pack2(v[4], v[5], a.bf16);
+        u.w = pack2(v[6], v[7], a.bf16);
+        *reinterpret_cast<uint4*>(a.y + (size_t)t * a.ldy + 8 * c) = u;
     }
 }
 
 // dweights[slot] = sum of the slot's partial <h, W2^T dy> + <b2, dy>; one warp a slot
-__global__ void __launch_bounds__(256) k_dweights(const int* pos, const int32_t* indices, int64_t slots, int k, int D,
-                                                  const float* dot, int parts, const uint16_t* b2, const uint16_t* dy,
-                                                  int64_t lddy, void* dweights, int weights_type, int bf16)
+__device__ __forceinline__ void slot_dweights(const EndArgs& a, int block)
 {
-    enter();
     const int lane = threadIdx.x & 31;
-    for (int64_t s = ((int64_t)blockIdx.x * blockDim.x + threadIdx.x) >> 5; s < slots; s += ((int64_t)gridDim.x * blockDim.x) >> 5) {
-        const int row = pos[s];
+    for (int64_t s = ((int64_t)block * blockDim.x + threadIdx.x) >> 5; s < a.T * a.k; s += ((int64_t)a.dweights_blocks * blockDim.x) >> 5) {
+        const int row = a.p.pos[s];
         float v = 0.f;
         if (row >= 0) {
-            for (int i = lane; i < parts; i += 32) v += dot[(size_t)row * parts + i];
-            if (b2) {
-                const uint16_t* b = b2 + (size_t)indices[s] * D;
-                const uint16_t* g = dy + (size_t)(s / k) * lddy;
-                for (int i = lane * 8; i < D; i += 256) {
+            for (int i = lane; i < a.dots; i += 32) v += a.dot[(size_t)row * a.dots + i];
+            if (a.b2) {
+                const uint16_t* b = a.b2 + (size_t)a.indices[s] * a.D;
+                const uint16_t* g = a.dy + (size_t)(s / a.k) * a.lddy;
+                for (int i = lane * 8; i < a.D; i += 256) {
                     float u[8], w[8];
-                    load8(b + i, u, bf16);
-                    load8(g + i, w, bf16);
+                    load8(b + i, u, a.bf16);
+                    load8(g + i, w, a.bf16);
 #pragma unroll
                     for (int j = 0; j < 8; ++j) v = fmaf(u[j], w[j], v);
                 }
@@ -295,57 +290,69 @@ __global__ void __launch_bounds__(256) k_dweights(const int* pos, const int32_t*
 #pragma unroll
         for (int d = 16; d > 0; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
         if (lane == 0) {
-            if (weights_type == SOM_F32) static_cast<float*>(dweights)[s] = v;
-            else static_cast<uint16_t*>(dweights)[s] = (uint16_t)pack2(v, 0.f, bf16);
+            if (a.weights_type == SOM_F32) static_cast<float*>(a.dweights)[s] = v;
+            else static_cast<uint16_t*>(a.dweights)[s] = (uint16_t)pack2(v, 0.f, a.bf16);
         }
     }
 }
 
 // out[e][c] = sum over the rows of expert e of weight[row] * v[row][c]; a block sums 64 columns of one expert, 32 rows at
 // a time, in a fixed order
-__global__ void __launch_bounds__(256) k_column_sums(SlotPlan p, int64_t rows, const uint16_t* v, int64_t ld, int cols, uint16_t* out, int bf16)
+__device__ __forceinline__ void column_sums(const EndArgs& a, int block, float* part)
 {
-    enter();
-    __shared__ float part[32][65];
-    const int e = blockIdx.y, c = blockIdx.x * 64 + (threadIdx.x & 7) * 8, r = threadIdx.x >> 3;
-    const int64_t lo = p.seg ? p.seg[e] : 0, hi = p.seg ? lo + p.count[e] : rows;
-    float a[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    if (c < cols)
+    const int across = (a.v_cols + 63) / 64, e = block / across, c0 = (block - e * across) * 64;
+    const int c = c0 + (threadIdx.x & 7) * 8, r = threadIdx.x >> 3;
+    const int64_t lo = a.p.seg ? a.p.seg[e] : 0, hi = a.p.seg ? lo + a.p.count[e] : a.rows;
+    float s[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    if (c < a.v_cols)
 #pragma unroll 4
         for (int64_t i = lo + r; i < hi; i += 32) {
             float u[8];
-            load8(v + (size_t)i * ld + c, u, bf16);
-            const float w = p.seg ? p.row_weight[i] : 1.f;
+            load8(a.v + (size_t)i * a.ldv + c, u, a.bf16);
+            const float w = a.p.seg ? a.p.row_weight[i] : 1.f;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) a[j] = fmaf(w, u[j], a[j]);
+            for (int j = 0; j < 8; ++j) s[j] = fmaf(w, u[j], s[j]);
         }
 #pragma unroll
-    for (int j = 0; j < 8; ++j) part[r][(threadIdx.x & 7) * 8 + j] = a[j];
+    for (int j = 0; j < 8; ++j) part[r * 65 + (threadIdx.x & 7) * 8 + j] = s[j];
     __syncthreads();
-    if (threadIdx.x < 64 && blockIdx.x * 64 + threadIdx.x < cols) {
-        float s = 0.f;
-        for (int i = 0; i < 32; ++i) s += part[i][threadIdx.x];
-        out[(size_t)e * cols + blockIdx.x * 64 + threadIdx.x] = (uint16_t)pack2(s, 0.f, bf16);
+    if (threadIdx.x < 64 && c0 + threadIdx.x < a.v_cols) {
+        float sum = 0.f;
+        for (int i = 0; i < 32; ++i) sum += part[i * 65 + threadIdx.x];
+        a.v_sums[(size_t)e * a.v_cols + c0 + threadIdx.x] = (uint16_t)pack2(sum, 0.f, a.bf16);
     }
 }
 
 // out[e][c] = sum of part[g][c] over the expert's groups of 32 rows (of 32-row sums); 32 columns a block, 8 groups at a time
-__global__ void __launch_bounds__(256) k_join_sums(SlotPlan p, int64_t rows, const float* part, int cols, uint16_t* out, int bf16)
+__device__ __forceinline__ void join_sums(const EndArgs& a, int block, float* sums)
+{
+    const int across = (a.sums_cols + 31) / 32, e = block / across;
+    const int c = (block - e * across) * 32 + (threadIdx.x & 31), r = threadIdx.x >> 5;
+    const int64_t lo = a.p.seg ? a.p.seg[e] / 32 : 0, hi = a.p.seg ? lo + (a.p.count[e] + 31) / 32 : (a.rows + 31) / 32;
+    float s = 0.f;
+    if (c < a.sums_cols)
+        for (int64_t i = lo + r; i < hi; i += 8) s += a.sums[(size_t)i * a.sums_cols + c];
+    sums[r * 33 + (threadIdx.x & 31)] = s;
+    __syncthreads();
+    if (r == 0 && c < a.sums_cols) {
+#pragma unroll
+        for (int i = 1; i < 8; ++i) s += sums[i * 33 + threadIdx.x];
+        a.sums_out[(size_t)e * a.sums_cols + c] = (uint16_t)pack2(s, 0.f, a.bf16);
+    }
+}
+
+// What nothing follows, in one launch, each part by blocks of its own: the parts that take longest a block come first.
+__global__ void __launch_bounds__(256) k_ends(const __grid_constant__ EndArgs a)
 {
     enter();
-    __shared__ float sums[8][33];
-    const int e = blockIdx.y, c = blockIdx.x * 32 + (threadIdx.x & 31), r = threadIdx.x >> 5;
-    const int64_t lo = p.seg ? p.seg[e] / 32 : 0, hi = p.seg ? lo + (p.count[e] + 31) / 32 : (rows + 31) / 32;
-    float a = 0.f;
-    if (c < cols)
-        for (int64_t i = lo + r; i < hi; i += 8) a += part[(size_t)i * cols + c];
-    sums[r][threadIdx.x & 31] = a;
-    __syncthreads();
-    if (r == 0 && c < cols) {
-#pragma unroll
-        for (int i = 1; i < 8; ++i) a += sums[i][threadIdx.x & 31];
-        out[(size_t)e * cols + c] = (uint16_t)pack2(a, 0.f, bf16);
-    }
+    extern __shared__ float shared[];
+    int block = blockIdx.x;
+    if (block < a.v_blocks) return column_sums(a, block, shared);
+    block -= a.v_blocks;
+    if (block < a.sums_blocks) return join_sums(a, block, shared);
+    block -= a.sums_blocks;
+    if (block < a.dweights_blocks) return slot_dweights(a, block);
+    join_rows(a, block - a.dweights_blocks);
 }
 
 // blocks of `per` items each, at most eight per SM: the kernels walk the rest
@@ -389,32 +396,16 @@ int launch_gather(som_layers* l, const SlotPlan& p, int k, int64_t D, const void
                              static_cast<const uint16_t*>(dy), lddy, static_cast<uint16_t*>(dyp)));
 }
 
-int launch_join(som_layers* l, const SlotPlan& p, int64_t T, int k, int64_t D, const float* part, const void* residual, int64_t ldr,
-                void* y, int64_t ldy, int bf16, cudaStream_t st)
+int launch_ends(som_layers* l, EndArgs a, cudaStream_t st)
 {
-    return outcome(l, launch(l, k_join, dim3(grid_for(l, T * (D / 8), 256)), 256, 0, st, 1, p.pos, T, k, (int)D, part,
-                             static_cast<const uint16_t*>(residual), ldr, static_cast<uint16_t*>(y), ldy, bf16));
-}
-
-int launch_dweights(som_layers* l, const SlotPlan& p, const int32_t* indices, int64_t T, int k, int64_t D, const float* dot, int parts,
-                    const void* b2, const void* dy, int64_t lddy, void* dweights, int weights_type, int bf16, cudaStream_t st)
-{
-    return outcome(l, launch(l, k_dweights, dim3(grid_for(l, T * k, 8)), 256, 0, st, 1, p.pos, indices, T * k, k, (int)D, dot, parts,
-                             static_cast<const uint16_t*>(b2), static_cast<const uint16_t*>(dy), lddy, dweights, weights_type, bf16));
-}
-
-int launch_column_sums(som_layers* l, const SlotPlan& p, int E, int64_t rows, const void* v, int64_t ld, int64_t cols, void* out,
-                       int bf16, cudaStream_t st)
-{
-    const dim3 grid((unsigned)((cols + 63) / 64), (unsigned)E);
-    return outcome(l, launch(l, k_column_sums, grid, 256, 0, st, 1, p, rows, static_cast<const uint16_t*>(v), ld, (int)cols,
-                             static_cast<uint16_t*>(out), bf16));
-}
-
-int launch_join_sums(som_layers* l, const SlotPlan& p, int E, int64_t rows, const float* part, int64_t cols, void* out, int bf16, cudaStream_t st)
-{
-    const dim3 grid((unsigned)((cols + 31) / 32), (unsigned)E);
-    return outcome(l, launch(l, k_join_sums, grid, 256, 0, st, 1, p, rows, part, (int)cols, static_cast<uint16_t*>(out), bf16));
+    a.join_blocks = a.y ? grid_for(l, a.T * (a.D / 8), 256) : 0;
+    a.dweights_blocks = a.dweights ? grid_for(l, a.T * a.k, 8) : 0;
+    a.sums_blocks = a.sums_out ? a.E * ((a.sums_cols + 31) / 32) : 0;
+    a.v_blocks = a.v_sums ? a.E * ((a.v_cols + 63) / 64) : 0;
+    const int64_t blocks = (int64_t)a.join_blocks + a.dweights_blocks + a.sums_blocks + a.v_blocks;
+    // (blocks without shared memory are brought in while the products still have theirs: 3 us of a join after products)
+    const size_t smem = a.v_blocks ? 32 * 65 * sizeof(float) : a.sums_blocks ? 8 * 33 * sizeof(float) : 0;
+    return outcome(l, launch(l, k_ends, dim3((unsigned)blocks), 256, smem, st, 1, a));
 }
 
 }  // namespace lay

@@ -8,16 +8,35 @@ namespace lay {
 // xp[row] = x[token of row's slot], the same of dy unless it is NULL; zeros up to whole steps of 64 rows
 int launch_gather(som_layers* l, const SlotPlan& p, int k, int64_t D, const void* x, int64_t ldx, void* xp, const void* dy,
                   int64_t lddy, void* dyp, cudaStream_t st);
-int launch_join(som_layers* l, const SlotPlan& p, int64_t T, int k, int64_t D, const float* part, const void* residual, int64_t ldr,
-                void* y, int64_t ldy, int bf16, cudaStream_t st);
-int launch_dweights(som_layers* l, const SlotPlan& p, const int32_t* indices, int64_t T, int k, int64_t D, const float* dot, int parts,
-                    const void* b2, const void* dy, int64_t lddy, void* dweights, int weights_type, int bf16, cudaStream_t st);
-// out[e][c] = sum of row weight * v[row][c] over the rows of expert e; without p.seg the sum over [0, rows)
-int launch_column_sums(som_layers* l, const SlotPlan& p, int E, int64_t rows, const void* v, int64_t ld, int64_t cols, void* out,
-                       int bf16, cudaStream_t st);
-// the same from the products' sums over 32 rows
-int launch_join_sums(som_layers* l, const SlotPlan& p, int E, int64_t rows, const float* part, int64_t cols, void* out, int bf16,
-                     cudaStream_t st);
+// Sums that end an operator.  Parts whose output is NULL are left out.
+struct EndArgs {
+    SlotPlan p;  // without p.seg: one group of `rows` rows
+    int64_t T, rows;
+    int k, D, E, bf16;
+    // y[t] = residual[t] + the sum of part over token t's rows
+    const float* part;
+    const uint16_t* residual;
+    uint16_t* y;
+    int64_t ldr, ldy;
+    // dweights[slot] = the sum of dot over the slot's row + <b2[expert], dy[t]>
+    const float* dot;
+    const int32_t* indices;
+    const uint16_t *b2, *dy;
+    void* dweights;
+    int64_t lddy;
+    int dots, weights_type;
+    // v_sums[e][c] = sum of row weight * v[row][c] over the rows of expert e
+    const uint16_t* v;
+    uint16_t* v_sums;
+    int64_t ldv;
+    int v_cols;
+    // the same from the products' sums over 32 rows
+    const float* sums;
+    uint16_t* sums_out;
+    int sums_cols;
+    int join_blocks, dweights_blocks, v_blocks, sums_blocks;  // set by launch_ends
+};
+int launch_ends(som_layers* l, EndArgs a, cudaStream_t st);
 
 int launch_route(som_layers* l, int type, int score, int64_t T, int E, int k, const void* logits, int64_t ld, const float* bias,
                  int groups, int top_groups, int group_best, int renorm, float scale, float* weights, int32_t* indices,
