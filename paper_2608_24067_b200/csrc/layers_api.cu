@@ -730,7 +730,7 @@ int som_experts_backward(som_layers* l, int type, int act, int gated, int64_t T,
     s.v_cols = (int)D;
     s.v_sums = static_cast<uint16_t*>(db2);
     LAY_TRY(launch_ends(l, s, st));
-    // dw1 = dz^T x, dw2 = dy^T (weighted h)
+    // dw1 = dz^T x and dw2 = dy^T (weighted h), in one launch
     a = ProdArgs();
     a.seg = p.seg;
     a.count = p.count;
@@ -738,17 +738,18 @@ int som_experts_backward(som_layers* l, int type, int act, int gated, int64_t T,
     a.columns_first = 1;
     a.bf16 = type == SOM_BF16;
     a.flags = l->flags;
-    ProdArgs b = a;
     LAY_TRY(map_64(l, &a.a, dz, rows1, p.max_rows, rows1));
     LAY_TRY(map_64(l, &a.b, xp, D, p.max_rows, D));
     LAY_TRY(map_out(l, &a.o, dw1, 2, D, rows1, D, E));
     set_tiles(l, &a, rows1, D, false, E);
-    LAY_TRY(launch_product(l, PROD_DW, a, st));
-    LAY_TRY(map_64(l, &b.a, dyp, D, p.max_rows, D));
-    LAY_TRY(map_64(l, &b.b, h, I, p.max_rows, I));
-    LAY_TRY(map_out(l, &b.o, dw2, 2, I, D, I, E));
-    set_tiles(l, &b, D, I, false, E);
-    return launch_product(l, PROD_DW, b, st);
+    LAY_TRY(map_64(l, &a.a2, dyp, D, p.max_rows, D));
+    LAY_TRY(map_64(l, &a.b2, h, I, p.max_rows, I));
+    LAY_TRY(map_out(l, &a.o2map, dw2, 2, I, D, I, E));
+    a.rows2 = (int)D;
+    a.cols2 = (int)I;
+    a.row_tiles2 = tiles_of(D, shape_rows(a.shape));
+    a.col_tiles2 = tiles_of(I, shape_cols(a.shape));
+    return launch_product(l, PROD_DW, a, st);
 }
 
 }  // extern "C"

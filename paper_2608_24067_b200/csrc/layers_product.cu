@@ -37,6 +37,7 @@ struct Tile {
     int row, col, expert;  // this block's first row and the tile's first column of the output, expert
     int k0, k;             // PROD_DW: first row of the sum; length of the first product's sum
     int split;             // part of the sum
+    bool second;           // PROD_DW: a tile of the second product
     int live, store;       // rows below `live` are in use, rows below `store` are written (zeros from `live` on)
 };
 
@@ -52,7 +53,7 @@ __device__ __forceinline__ int plan_at(const int* p)
 template <int MODE, bool EARLY = false>
 __device__ __forceinline__ int tile_count(const ProdArgs& p)
 {
-    if (MODE == PROD_DW) return p.experts * p.row_tiles * p.col_tiles * p.splits;
+    if (MODE == PROD_DW) return p.experts * (p.row_tiles * p.col_tiles + p.row_tiles2 * p.col_tiles2) * p.splits;
     return (p.tiles ? plan_at<EARLY>(p.tiles) : p.row_tiles) * p.col_tiles * p.splits;
 }
 
@@ -62,19 +63,23 @@ __device__ __forceinline__ Tile tile_at(const ProdArgs& p, int idx, int width, i
     constexpr int ROWS = shape_rows(SHAPE);
     Tile t;
     t.split = 0;
+    t.second = false;
     if (p.splits > 1) {
         t.split = idx % p.splits;
         idx /= p.splits;
     }
     if (MODE == PROD_DW) {
-        const int per = p.row_tiles * p.col_tiles;
+        const int all = p.experts * p.row_tiles * p.col_tiles;
+        t.second = idx >= all;
+        if (t.second) idx -= all;
+        const int col_tiles = t.second ? p.col_tiles2 : p.col_tiles, per = (t.second ? p.row_tiles2 : p.row_tiles) * col_tiles;
         t.expert = idx / per;
-        const int rest = idx - t.expert * per, rt = rest / p.col_tiles;
+        const int rest = idx - t.expert * per, rt = rest / col_tiles;
         t.row = rt * ROWS + rank * BM;
-        t.col = (rest - rt * p.col_tiles) * width;
+        t.col = (rest - rt * col_tiles) * width;
         t.k0 = p.seg ? plan_at<EARLY>(p.seg + t.expert) : 0;
         t.k = p.seg ? round64(plan_at<EARLY>(p.count + t.expert)) : p.k1;
-        t.live = t.store = p.rows;
+        t.live = t.store = t.second ? p.rows2 : p.rows;
     } else {
         const int rt = idx / p.col_tiles;
         t.row = rt * ROWS + rank * BM;
@@ -123,12 +128,12 @@ struct Stager {
     {
         put(chunk, make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])));
     }
-    __device__ __forceinline__ void send(const CUtensorMap* map, int col, int row, int batch, const ProdArgs& p)
+    __device__ __forceinline__ void send(const CUtensorMap* map, int col, int row, int batch, int rows, int cols)
     {
         fence_async_smem();
         __syncwarp();
         if (lane == 0) {
-            if (col < p.cols && row < p.rows) tma_store(map, buf, col, row, batch);
+            if (col < cols && row < rows) tma_store(map, buf, col, row, batch);
             store_commit();
         }
     }
@@ -277,7 +282,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
                 const int b0 = t.col + rank * from, k = t.k0 + (it - it2) * BK;
                 if (rank == 0) bar_expect(&full[s], all1);
                 for (int j = 0; j < share; j += box) {
-                    if (B_MN) tma_load<PAIRED>(sb + j * 128, &p.b, bar, b0 + j, k, MODE == PROD_DW ? 0 : t.expert);
+                    if (B_MN) tma_load<PAIRED>(sb + j * 128, t.second ? &p.b2 : &p.b, bar, b0 + j, k, MODE == PROD_DW ? 0 : t.expert);
                     else tma_load<PAIRED>(sb + j * 128, &p.b, bar, k, j < gates ? b0 + j : b0 + j - gates + p.gate_rows, t.expert);
                 }
             };
@@ -285,7 +290,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
                 unsigned char* sa = ring + s * STAGE_BYTES;
                 const uint32_t bar = full0 + 8 * s;
                 const bool second = MODE == PROD_DZ_TWO && it < it2;
-                const CUtensorMap* map = second ? &p.a2 : &p.a;
+                const CUtensorMap* map = second || t.second ? &p.a2 : &p.a;
                 const int k = second ? it * BK : t.k0 + (it - it2) * BK;
                 if (A_MN) {
                     tma_load<PAIRED>(sa, map, bar, t.row, k, 0);
@@ -431,7 +436,8 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
             if (!any) {
                 // none of this warp's rows or columns
             } else if constexpr (MODE == PROD_DX || MODE == PROD_DW) {
-                const int batch = MODE == PROD_DW ? t.expert + t.split : t.split;
+                const int batch = MODE == PROD_DW ? t.expert + t.split : t.split, cols = t.second ? p.cols2 : p.cols;
+                const CUtensorMap* map = t.second ? &p.o2map : &p.o;
                 float next[32];
                 tmem_ld(acc + turn * piece, next);
                 for (int at = turn * piece; at < width;) {
@@ -445,11 +451,11 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
                     if (p.out32) {
 #pragma unroll
                         for (int j = 0; j < 8; ++j) s.put(j, v + 4 * j);
-                        s.send(&p.o, t.col + at, row0, batch, p);
+                        s.send(map, t.col + at, row0, batch, t.second ? p.rows2 : p.rows, cols);
                     } else {
 #pragma unroll
                         for (int j = 0; j < 4; ++j) s.put(4 * half + j, pack8<BF16>(v + 8 * j));
-                        if (half == 1) s.send(&p.o, t.col + at - 32, row0, batch, p);
+                        if (half == 1) s.send(map, t.col + at - 32, row0, batch, t.second ? p.rows2 : p.rows, cols);
                     }
                     at += step_on;
                 }
@@ -493,7 +499,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
                         s.put((done - 16) / 8, pack8<BF16>(v));
                         s.put((done - 16) / 8 + 1, pack8<BF16>(v + 8));
                     }
-                    if (done == piece) s.send(&p.o, col + 16 - piece, row0, t.split, p);
+                    if (done == piece) s.send(&p.o, col + 16 - piece, row0, t.split, p.rows, p.cols);
                     at += step_on;
                 }
             } else {
@@ -588,7 +594,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
 template <int MODE, int SHAPE, bool BF16>
 cudaError_t launch_as(som_layers* l, const ProdArgs& args, cudaStream_t st)
 {
-    const int64_t tiles = (int64_t)args.row_tiles * args.col_tiles * (MODE == PROD_DW ? args.experts : 1) * args.splits;
+    const int64_t tiles = ((int64_t)args.row_tiles * args.col_tiles + (int64_t)args.row_tiles2 * args.col_tiles2) * (MODE == PROD_DW ? args.experts : 1) * args.splits;
     const int most = SHAPE == PAIR ? l->pairs : l->sm_count, blocks = SHAPE == PAIR ? 2 : 1;
     return launch(l, k_product<MODE, SHAPE, BF16>, dim3((unsigned)(tiles < most ? tiles : most) * blocks), THREADS, SMEM, st, blocks, args);
 }

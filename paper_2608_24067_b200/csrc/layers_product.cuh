@@ -39,8 +39,10 @@ __host__ __device__ constexpr int tile_dots(int shape)
 
 struct ProdArgs {
     CUtensorMap a, b;         // operands (of the first product)
-    CUtensorMap a2, b2;       // second product of PROD_DZ_TWO
+    CUtensorMap a2, b2;       // second product of PROD_DZ_TWO, or a second one of PROD_DW over the same experts' rows
     CUtensorMap o;            // output of PROD_FWD, PROD_DX, PROD_DW
+    CUtensorMap o2map;        // output of PROD_DW's second product, of rows2 x cols2
+    int row_tiles2, col_tiles2, rows2, cols2;
     void* o0;                 // PROD_DZ, PROD_DZ_TWO: dz [rows][ld0], the gated half gate_rows columns on
     void* o2;                 // PROD_DZ_TWO: weighted hidden values [rows][ld2]
     int64_t ld0, ld2;
