@@ -507,8 +507,14 @@ static SlotPlan carve_plan(Carver& c, int64_t T, int E, int k, int tile)
 static bool few_slots(int64_t T, int E, int k) { return T * k <= 16 || (T * k <= 64 && T * k <= E); }
 
 // Rows of an expert's tiles: a pair's once the experts have rows enough; with fewer, a pair would mostly multiply padding, and
-// the weights' bytes bound the product, not the tensor cores.
-static int tile_rows(int64_t T, int E, int k) { return T * k >= (int64_t)128 * E ? shape_rows(PAIR) : shape_rows(WIDE); }
+// the weights' bytes bound the product, not the tensor cores.  In us, single blocks / pairs, gated, D 2048 and I 1024 unless said:
+//   rows an expert                  64           128          192          256          512
+//   64 experts                   189 / 222    254 / 263    308 / 305    357 / 359    620 / 602
+//   12 experts (1000, 712)        39 / 39      43 / 45      51 / 48      57 / 50      80 / 68
+//   64 experts, gradient         507 / 585    654 / 683    792 / 812    938 / 947   1533 / 1508
+//   16 experts, gradient         144 / 163    192 / 186    216 / 231    272 / 258    406 / 410
+//   12 experts, gradient          77 / 69      79 / 86      94 / 93     114 / 101    171 / 156
+static int tile_rows(int64_t T, int E, int k) { return T * k >= (int64_t)256 * E ? shape_rows(PAIR) : shape_rows(WIDE); }
 
 // A product over the slots' rows.  Single blocks are wide where that leaves a tile for every SM, by the tiles to expect.
 static ProdArgs grouped(const som_layers* l, const SlotPlan& p, int64_t slots, int E, int type, int64_t cols, bool gated)

@@ -320,7 +320,8 @@ def test_route_backward_bad_and_repeated_indices(L):
 
 CASES = [  # T, E, k, D, I
     (1, 4, 2, 64, 64), (1, 64, 8, 256, 136), (2, 5, 5, 72, 40), (7, 3, 1, 520, 264), (40, 16, 4, 264, 136), (130, 1, 1, 136, 200),
-    (200, 5, 2, 264, 72), (300, 40, 8, 64, 128), (513, 6, 2, 256, 256)]
+    (200, 5, 2, 264, 72), (300, 40, 8, 64, 128), (513, 6, 2, 256, 256),
+    (1100, 7, 2, 264, 136)]
 
 
 def _expert_inputs(T, E, k, D, I, dtype, gated, bias, residual, gen, wtype, pad=0.1):
