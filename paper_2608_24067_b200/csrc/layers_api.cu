@@ -130,11 +130,12 @@ int map_out(som_layers* l, CUtensorMap* m, void* p, int bytes, int64_t cols, int
 }
 
 // The tiles of a product of `rows` x `cols` outputs (`batch` of them).  Pairs of blocks do twice a single block's work per
-// byte that they load, but need tiles enough for every SM: narrow single tiles where pairs would leave a third of them idle.
+// byte that they load, but need tiles enough for every SM: narrow single tiles where every SM has one at most.  1024 rows, sums of
+// 2048, narrow tiles / pairs: 1024 columns 13.6 / 16.2 us, 2048 (128 narrow tiles) 15.2 / 16.4, 2560 (160) 25.3 / 17.7.
 void set_tiles(const som_layers* l, ProdArgs* a, int64_t rows, int64_t cols, bool gated, int64_t batch = 1)
 {
     const int halves = gated ? 2 : 1;
-    a->shape = 3 * tiles_of(rows, 256) * tiles_of(cols, 256 / halves) * batch >= 2 * l->pairs ? PAIR : NARROW;
+    a->shape = tiles_of(rows, 128) * tiles_of(cols, 128 / halves) * batch > l->sm_count ? PAIR : NARROW;
     a->row_tiles = tiles_of(rows, shape_rows(a->shape));
     a->col_tiles = tiles_of(cols, shape_cols(a->shape) / halves);
     a->rows = (int)rows;
@@ -143,7 +144,8 @@ void set_tiles(const som_layers* l, ProdArgs* a, int64_t rows, int64_t cols, boo
 }
 
 // Blocks that share each tile's sum, for products whose tiles leave SMs idle: worth its second launch (about 3 us, with a
-// step of 64 k at about 0.3 us) where it takes at least 14 steps off the longest sum.
+// step of 64 k at about 0.3 us) where it takes at least 14 steps off the longest sum.  In parts / in one: 32 x 4096 outputs, sums of
+// 4096, 13.5 / 24.1 us; 64 x 8192, 4096, 19.3 / 24.9; 256 x 1024, 2048, 11.6 / 14.2; 128 x 1024, 1024 (not split) 11.8 / 9.3.
 int splits_of(const som_layers* l, const ProdArgs& a, int64_t k)
 {
     if (a.shape != NARROW) return 1;
@@ -527,7 +529,10 @@ static ProdArgs grouped(const som_layers* l, const SlotPlan& p, int64_t slots, i
     a.row_weight = p.row_weight;
     const int64_t expected = (slots < E ? slots : E) + slots / 256;
     const int halves = gated ? 2 : 1;
-    a.shape = p.tile == shape_rows(PAIR) ? PAIR : expected * tiles_of(cols, shape_cols(WIDE) / halves) >= l->sm_count ? WIDE : NARROW;
+    // Wide tiles once they are two thirds of the SMs.  Gated, D 2048 and I 1024 unless said, wide / narrow: 8 experts with 8 or 16 rows
+    // (64 wide tiles) 45 / 39 us, 12 with 33 (1000, 712; 78) 38 / 33, 16 with 8 (128) 54.8 / 57.8, 32 with 4 (256) 82.4 / 83.6, 64 with 9
+    // (512) 159.4 / 164
+    a.shape = p.tile == shape_rows(PAIR) ? PAIR : 3 * expected * tiles_of(cols, shape_cols(WIDE) / halves) >= 2 * l->sm_count ? WIDE : NARROW;
     a.row_tiles = p.max_rows / p.tile;
     a.col_tiles = tiles_of(cols, shape_cols(a.shape) / halves);
     a.rows = p.max_rows;
