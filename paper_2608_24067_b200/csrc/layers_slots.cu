@@ -16,7 +16,7 @@ __device__ __forceinline__ float load_weight(const void* w, int type, int64_t i)
 
 // A stable counting sort of the slots by expert in one block: every warp owns a contiguous run of slots, counts it into a
 // row of its own in shared memory, the rows are turned into starting places, and the warp walks its run again.
-// Stable, so that the rows of an expert (and the sums over them) have one order.
+// Stable, so that the rows of an expert (and the sums over them) have one order.  Latency: 6 us for 576 slots of 64 experts.
 __global__ void __launch_bounds__(PLAN_THREADS) k_slot_plan(SlotPlan p, const int32_t* indices, const void* weights,
                                                            int weights_type, int64_t slots, int E, int* flags)
 {
@@ -93,7 +93,7 @@ __global__ void __launch_bounds__(PLAN_THREADS) k_slot_plan(SlotPlan p, const in
 
 // The same for many slots, in three launches over blocks of PLACE_SLOTS consecutive slots: every block counts its slots by
 // expert, one block turns the counts into segments and the blocks' starting places, every block places its slots.  (One
-// block alone took 60 us for 32768 slots.)
+// block alone took 60 us for 32768 slots; these take 3 + 5 + 9.)
 constexpr int PLACE_SLOTS = 1024, PLACE_WARPS = 8;
 
 __global__ void __launch_bounds__(32 * PLACE_WARPS) k_slot_count(const int32_t* indices, int64_t slots, int E, int* counts, int* flags)
@@ -206,7 +206,8 @@ __global__ void __launch_bounds__(32 * PLACE_WARPS) k_slot_place(SlotPlan p, con
 }
 
 // Rows of x (blockIdx.z == 0) and of dy (1) in the slots' order, up to whole steps of 64 rows of an expert with zeros (the
-// sums over an expert's rows run in such steps).  A warp a row.
+// sums over an expert's rows run in such steps).  A warp a row.  Bound by the writes: 32768 rows of 2048 in 31 us, 134 MB written
+// and 17 read (4.9 TB/s).  (Rows fetched one by one by the products' copies instead took longer than both.)
 __global__ void __launch_bounds__(256) k_gather(SlotPlan p, int k, int D, const uint16_t* x, int64_t ldx, uint16_t* xp,
                                                 const uint16_t* dy, int64_t lddy, uint16_t* dyp)
 {
@@ -235,7 +236,8 @@ __global__ void __launch_bounds__(256) k_gather(SlotPlan p, int k, int D, const 
     }
 }
 
-// y[t] = residual[t] + sum over j of part[pos[t][j]], in the order of j
+// y[t] = residual[t] + sum over j of part[pos[t][j]], in the order of j.  The parts are fp32 so that a token's result is rounded
+// once.  Bound by HBM: 4096 tokens x 8 x 2048 in 48 us, 285 MB (5.9 TB/s).
 __device__ __forceinline__ void join_rows(const EndArgs& a, int block)
 {
     const int chunks = a.D / 8;
