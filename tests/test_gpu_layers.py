@@ -486,3 +486,31 @@ def test_refusals(L):
     raises(ValueError, L.experts, ok, at, wt, w1, w2, b1=w1[0])
     raises(SomError, L.experts, ok, at, wt, torch.zeros(3, 24, 64, dtype=BF16, device="cuda"), torch.zeros(3, 64, 12, dtype=BF16, device="cuda"), status=3)
     raises(ValueError, L.experts_backward, ok, at, wt, w1, w2, ok[:2])
+
+
+def test_captured(L):
+    """Routing, experts and their gradient replayed from a graph, with other inputs in the same tensors."""
+    gen = torch.Generator().manual_seed(5)
+    T, E, k, D, I = 70, 9, 3, 136, 72
+    s, _ = _expert_inputs(T, E, k, D, I, BF16, True, True, False, gen, FP32)
+    logits, dy = torch.randn(T, E, generator=gen).cuda(), _normal(gen, T, D, dtype=BF16)
+
+    def step():
+        r = L.route(logits, k, score="sigmoid", renorm=True)
+        y = L.experts(s["x"], r["indices"], r["weights"], s["w1"], s["w2"], s["b1"], s["b2"], act="silu", gated=True)
+        g = L.experts_backward(s["x"], r["indices"], r["weights"], s["w1"], s["w2"], dy, s["b1"], s["b2"], act="silu", gated=True)
+        z = L.linear(y, s["w1"][0], act="gelu")
+        return [r["indices"], r["weights"], y, z] + [g[n] for n in sorted(g)]
+
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        kept = step()
+    for turn in range(2):
+        logits.copy_(torch.randn(T, E, generator=gen))
+        dy.copy_(torch.randn(T, D, generator=gen))
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(kept, step()):
+            assert torch.equal(a, b)
