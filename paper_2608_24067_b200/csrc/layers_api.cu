@@ -496,7 +496,6 @@ static SlotPlan carve_plan(Carver& c, int64_t T, int E, int k, int tile)
     p.tiles = c.take<int>(1);
     p.tile_expert = c.take<int>(p.max_rows / tile);
     p.pos = c.take<int>(slots);
-    p.row_slot = c.take<int>(p.max_rows);
     p.row_weight = c.take<float>(p.max_rows);
     p.block_counts = c.take<int>((int64_t)plan_blocks(slots) * E);
     return p;
@@ -610,7 +609,7 @@ int som_experts(som_layers* l, int type, int act, int gated, int64_t T, int32_t 
         }
     }
     LAY_TRY(launch_plan(l, p, indices, weights, weights_type, T, k, E, st));
-    LAY_TRY(launch_gather(l, p, k, D, x, ldx, xp, nullptr, 0, nullptr, st));
+    LAY_TRY(launch_gather(l, p, T * k, E, k, D, x, ldx, xp, nullptr, 0, nullptr, st));
     ProdArgs a = grouped(l, p, T * k, E, type, I, gated);
     LAY_TRY(map_left(l, &a.a, xp, D, p.max_rows, D, LEFT_BOX));
     LAY_TRY(map_right(l, &a, PROD_FWD, gated, w1, D, rows1, E));
@@ -688,7 +687,7 @@ int som_experts_backward(som_layers* l, int type, int act, int gated, int64_t T,
         }
     }
     LAY_TRY(launch_plan(l, p, indices, weights, weights_type, T, k, E, st));
-    LAY_TRY(launch_gather(l, p, k, D, x, ldx, xp, dy, lddy, dyp, st));
+    LAY_TRY(launch_gather(l, p, T * k, E, k, D, x, ldx, xp, dy, lddy, dyp, st));
     // -> dz, the weighted h, partial sums of <h, g>
     ProdArgs a = z;
     LAY_TRY(map_left(l, &a.a, xp, D, p.max_rows, D, LEFT_BOX));

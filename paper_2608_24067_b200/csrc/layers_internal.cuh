@@ -72,7 +72,6 @@ struct SlotPlan {
     int* tiles;        // [1] row tiles in use
     int* tile_expert;  // [max tiles]
     int* pos;          // [T * k] row of a slot, -1 = none
-    int* row_slot;     // [max rows] slot of a row in use
     float* row_weight; // [max rows] the slot's routing weight
     int* block_counts; // [plan_blocks][E] scratch of the plan
     int max_rows;      // upper bound that the host sizes buffers and grids by

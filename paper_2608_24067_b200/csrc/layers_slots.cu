@@ -83,10 +83,7 @@ __global__ void __launch_bounds__(PLAN_THREADS) k_slot_plan(SlotPlan p, const in
         if (s < hi) {
             const int row = x >= 0 ? start[x] + at + rank : -1;
             p.pos[s] = row;
-            if (row >= 0) {
-                p.row_slot[row] = (int)s;
-                p.row_weight[row] = load_weight(weights, weights_type, s);
-            }
+            if (row >= 0) p.row_weight[row] = load_weight(weights, weights_type, s);
         }
     }
 }
@@ -197,40 +194,43 @@ __global__ void __launch_bounds__(32 * PLACE_WARPS) k_slot_place(SlotPlan p, con
         __syncwarp();
         if (s < slots) {
             p.pos[s] = row;
-            if (row >= 0) {
-                p.row_slot[row] = (int)s;
-                p.row_weight[row] = load_weight(weights, weights_type, s);
-            }
+            if (row >= 0) p.row_weight[row] = load_weight(weights, weights_type, s);
         }
     }
 }
 
-// Rows of x (blockIdx.z == 0) and of dy (1) in the slots' order, up to whole steps of 64 rows of an expert with zeros (the
-// sums over an expert's rows run in such steps).  A warp a row.  Bound by the writes: 32768 rows of 2048 in 31 us, 134 MB written
-// and 17 read (4.9 TB/s).  (Rows fetched one by one by the products' copies instead took longer than both.)
-__global__ void __launch_bounds__(256) k_gather(SlotPlan p, int k, int D, const uint16_t* x, int64_t ldx, uint16_t* xp,
-                                                const uint16_t* dy, int64_t lddy, uint16_t* dyp)
+// Rows of x (blockIdx.z == 0) and of dy (1) in the slots' order, a warp a slot: what it reads does not wait for where it goes.  With
+// `zeros` up to whole steps of 64 rows of an expert are zeros (the sums over an expert's rows run in such steps; rows of products
+// do not mix).  Bound by the writes: 32768 rows of 2048 in 28 us, 134 MB
+// written and 17 read (5.4 TB/s); by rows, each asking for its slot, 31.  (Rows fetched one by one by the products' copies instead took
+// longer than both.)
+__global__ void __launch_bounds__(256) k_gather(SlotPlan p, int64_t slots, int E, int k, int D, const uint16_t* x, int64_t ldx, uint16_t* xp,
+                                                const uint16_t* dy, int64_t lddy, uint16_t* dyp, int zeros)
 {
     enter();
-    const int lane = threadIdx.x & 31, chunks = D / 8, rows = *p.tiles * p.tile;
+    const int lane = threadIdx.x & 31, chunks = D / 8;
     const uint16_t* from = blockIdx.z ? dy : x;
-    const int64_t ld = blockIdx.z ? lddy : ldx;
+    const int64_t ld = blockIdx.z ? lddy : ldx, all = slots + (zeros ? (int64_t)E * 64 : 0);
     uint16_t* to = blockIdx.z ? dyp : xp;
-    for (int row = blockIdx.x * 8 + (threadIdx.x >> 5); row < rows; row += gridDim.x * 8) {
-        const int e = p.tile_expert[row / p.tile], place = row - p.seg[e], n = p.count[e];
-        uint4* out = reinterpret_cast<uint4*>(to + (size_t)row * D);
-        if (place < n) {
-            const uint4* in = reinterpret_cast<const uint4*>(from + (size_t)(p.row_slot[row] / k) * ld);
-            int c = lane;
-            for (; c + 96 < chunks; c += 128) {
-                const uint4 u0 = *(in + c), u1 = *(in + c + 32), u2 = *(in + c + 64), u3 = *(in + c + 96);
-                out[c] = u0;
-                out[c + 32] = u1;
-                out[c + 64] = u2;
-                out[c + 96] = u3;
+    for (int64_t i = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); i < all; i += (int64_t)gridDim.x * 8) {
+        if (i < slots) {
+            const uint4* in = reinterpret_cast<const uint4*>(from + (size_t)(i / k) * ld);
+            const int row = p.pos[i];
+            for (int c = lane; c < chunks; c += 128) {
+                uint4 u[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (c + 32 * j < chunks) u[j] = *(in + c + 32 * j);
+                if (row < 0) break;
+                uint4* out = reinterpret_cast<uint4*>(to + (size_t)row * D);
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (c + 32 * j < chunks) out[c + 32 * j] = u[j];
             }
-            for (; c < chunks; c += 32) out[c] = *(in + c);
-        } else if (place < ((n + 63) & ~63)) {
+        } else {
+            const int e = (int)((i - slots) >> 6), n = p.count[e], r = n + (int)((i - slots) & 63);
+            if (r >= ((n + 63) & ~63)) continue;
+            uint4* out = reinterpret_cast<uint4*>(to + (size_t)(p.seg[e] + r) * D);
             for (int c = lane; c < chunks; c += 32) out[c] = make_uint4(0u, 0u, 0u, 0u);
         }
     }
@@ -390,12 +390,13 @@ int launch_plan(som_layers* l, const SlotPlan& p, const int32_t* indices, const 
     return outcome(l, e);
 }
 
-int launch_gather(som_layers* l, const SlotPlan& p, int k, int64_t D, const void* x, int64_t ldx, void* xp, const void* dy,
-                  int64_t lddy, void* dyp, cudaStream_t st)
+int launch_gather(som_layers* l, const SlotPlan& p, int64_t slots, int E, int k, int64_t D, const void* x, int64_t ldx, void* xp,
+                  const void* dy, int64_t lddy, void* dyp, cudaStream_t st)
 {
-    const dim3 grid(grid_for(l, p.max_rows, 8), 1, dy ? 2 : 1);
-    return outcome(l, launch(l, k_gather, grid, 256, 0, st, 1, p, k, (int)D, static_cast<const uint16_t*>(x), ldx, static_cast<uint16_t*>(xp),
-                             static_cast<const uint16_t*>(dy), lddy, static_cast<uint16_t*>(dyp)));
+    const int zeros = dy != nullptr;
+    const dim3 grid(grid_for(l, slots + (zeros ? (int64_t)E * 64 : 0), 8), 1, dy ? 2 : 1);
+    return outcome(l, launch(l, k_gather, grid, 256, 0, st, 1, p, slots, E, k, (int)D, static_cast<const uint16_t*>(x), ldx,
+                             static_cast<uint16_t*>(xp), static_cast<const uint16_t*>(dy), lddy, static_cast<uint16_t*>(dyp), zeros));
 }
 
 int launch_ends(som_layers* l, EndArgs a, cudaStream_t st)

@@ -5,9 +5,9 @@
 
 namespace lay {
 
-// xp[row] = x[token of row's slot], the same of dy unless it is NULL; zeros up to whole steps of 64 rows
-int launch_gather(som_layers* l, const SlotPlan& p, int k, int64_t D, const void* x, int64_t ldx, void* xp, const void* dy,
-                  int64_t lddy, void* dyp, cudaStream_t st);
+// xp[row] = x[token of row's slot]; unless dy is NULL the same of dy, and zeros in both up to whole steps of 64 rows
+int launch_gather(som_layers* l, const SlotPlan& p, int64_t slots, int E, int k, int64_t D, const void* x, int64_t ldx, void* xp,
+                  const void* dy, int64_t lddy, void* dyp, cudaStream_t st);
 // Sums that end an operator.  Parts whose output is NULL are left out.
 struct EndArgs {
     SlotPlan p;  // without p.seg: one group of `rows` rows
