@@ -221,7 +221,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
     extern __shared__ unsigned char smem_raw[];
     __shared__ __align__(8) uint64_t full[STAGES], empty[STAGES], acc_full[2], acc_empty[2], drained;
     __shared__ uint32_t tmem_sh;
-    __shared__ int gave_up_sh;
+    __shared__ int gave_up_sh, summed[2];  // summed: whether a tile's products came, for the epilogue
     unsigned char* ring = smem_raw + ((1024u - (smem_addr(smem_raw) & 1023u)) & 1023u);
 
     unsigned char* staged = ring + ring_bytes(MODE);
@@ -434,10 +434,12 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
                     for (int at = turn * piece + round; at < width && t.col + at < p.cols; at += round) prefetch_l2(extra + t.col + at);
             }
             // One lane waits for the products, the other warps for that lane at a hardware barrier: trying the mbarrier
-            // takes shared-memory cycles (sixteen warps that did slowed the products by 5 %).
-            if (warp == 2 && lane == 0) bar_wait(&acc_full[buf], (uint32_t)(n_acc / BUFFERS) & 1u, gave_up);
+            // takes shared-memory cycles (sixteen warps that did slowed the products by 5 %).  All go on or all leave, by that lane's
+            // word: *gave_up may be raised between two warps' looks at it, and one that had left would be missing at the next barrier.
+            // (Two words in turn: a word is written again only after every warp has passed the other tile's barrier.)
+            if (warp == 2 && lane == 0) summed[n_acc & 1] = bar_wait(&acc_full[buf], (uint32_t)(n_acc / BUFFERS) & 1u, gave_up);
             asm volatile("bar.sync 1, %0;" ::"n"(32 * EPI_WARPS) : "memory");
-            if (*gave_up) break;
+            if (!summed[n_acc & 1]) break;
             tc_fence_after();
             if (!any) {
                 // none of this warp's rows or columns

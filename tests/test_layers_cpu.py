@@ -1,5 +1,7 @@
 """The dense operators' C entries without a GPU: null handles and arguments are refused before anything touches a device."""
 import ctypes
+import os
+import re
 
 import pytest
 import torch
@@ -28,3 +30,23 @@ def test_no_device():
     lib = som.load_library()
     out = ctypes.c_void_p()
     assert lib.som_layers_create(ctypes.byref(out)) == 6 and not out.value
+
+
+def _source(name):
+    return open(os.path.join(os.path.dirname(som.__file__), "csrc", name)).read()
+
+
+def test_epilogue_gives_up_as_one():
+    """The epilogue's warps meet at a hardware barrier in every tile, so they have to leave together: whether a wait ran out is read
+    from a word that only the waiting lane writes, before the barrier, never from the flag that other warps may raise at any time."""
+    text = re.sub(r"//[^\n]*", "", _source("layers_product.cu"))
+    loop = text[text.index("Stager<out_buffers(MODE)> s{"):]
+    loop = loop[:loop.index("if (warp >= 2 && lane == 0) store_wait_all()")]
+    assert loop.count("bar.sync 1") == 1
+    before, after = loop.split("bar.sync 1")
+    word = re.search(r"(\w+)\[n_acc & 1\] = bar_wait\(&acc_full\[buf\],", before)
+    assert word and "*gave_up" not in loop
+    assert re.match(r'[^\n]*"memory"\);\s*if \(!%s\[n_acc & 1\]\) break;' % word.group(1), after)
+    # (the other word is in use until every warp has passed the next tile's barrier: two take turns)
+    assert re.search(r"__shared__ int[^;]*\b%s\[2\]" % word.group(1), text)
+    assert len(re.findall(r"\b%s\[" % word.group(1), loop)) == 2  # written once, read once
