@@ -360,7 +360,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
                 // (the second product's turn was read by the epilogue of the tile before the last, which is over)
                 for (int it = 0; it < it1 + it2; ++it) {
                     if (it == it2) {  // the first product's columns have been read
-                        ok = bar_wait(&acc_empty[buf], use ^ 1u, gave_up);
+                        ok = bar_wait<PAIRED>(&acc_empty[buf], use ^ 1u, gave_up);
                         tc_fence_after();
                     }
                     if (!ok || !bar_wait(&full[stage], phase, gave_up)) {
@@ -386,7 +386,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
                     }
                 }
                 if (!ok) break;
-                if (it1 + it2 == 0 && !bar_wait(&acc_empty[buf], use ^ 1u, gave_up)) {  // nothing to sum
+                if (it1 + it2 == 0 && !bar_wait<PAIRED>(&acc_empty[buf], use ^ 1u, gave_up)) {  // nothing to sum
                     ok = false;
                     break;
                 }

@@ -45,28 +45,39 @@ __device__ __forceinline__ bool bar_try(uint64_t* bar, uint32_t parity)
 }
 
 // The same, suspended for up to a millisecond: polling would take shared-memory cycles that the matrix instructions'
-// operands need.
+// operands need.  CLUSTER: for arrivals from the other block of a pair (bar_arrive_remote).
+template <bool CLUSTER>
 __device__ __forceinline__ bool bar_try_long(uint64_t* bar, uint32_t parity)
 {
     uint32_t done;
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\t"
-        "selp.u32 %0, 1, 0, p;\n\t}"
-        : "=r"(done)
-        : "r"(smem_addr(bar)), "r"(parity), "r"(1000000u)
-        : "memory");
+    if (CLUSTER)
+        asm volatile(
+            "{\n\t.reg .pred p;\n\t"
+            "mbarrier.try_wait.parity.relaxed.cluster.shared::cta.b64 p, [%1], %2, %3;\n\t"
+            "selp.u32 %0, 1, 0, p;\n\t}"
+            : "=r"(done)
+            : "r"(smem_addr(bar)), "r"(parity), "r"(1000000u)
+            : "memory");
+    else
+        asm volatile(
+            "{\n\t.reg .pred p;\n\t"
+            "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\t"
+            "selp.u32 %0, 1, 0, p;\n\t}"
+            : "=r"(done)
+            : "r"(smem_addr(bar)), "r"(parity), "r"(1000000u)
+            : "memory");
     return done != 0;
 }
 
 // Waits for the phase with this parity; gives up (false) after WAIT_CYCLES or when another role of the block has
 // given up, so that no role waits for one that has left.
+template <bool CLUSTER = false>
 __device__ __forceinline__ bool bar_wait(uint64_t* bar, uint32_t parity, volatile int* gave_up)
 {
-    if (bar_try_long(bar, parity)) return true;
+    if (bar_try_long<CLUSTER>(bar, parity)) return true;
     const long long t0 = clock64();
     for (;;) {
-        if (bar_try_long(bar, parity)) return true;
+        if (bar_try_long<CLUSTER>(bar, parity)) return true;
         if (*gave_up) return false;
         if (clock64() - t0 > WAIT_CYCLES) {
             *gave_up = 1;
@@ -99,8 +110,11 @@ __device__ __forceinline__ void cluster_sync()
 }
 
 // Arrive at a barrier of another block of the cluster (address from cluster_addr).  Nothing but the order of tensor-memory
-// reads hangs on it, which tc_fence_before gives; a release at cluster scope waited for all outstanding stores, 3000 clocks of
-// the 7000 that the epilogue of a 256 x 256 tile with plain outputs took.
+// accesses hangs on it: the reader's tcgen05.wait::ld, tcgen05.fence::before_thread_sync and this arrival, the writer's wait
+// and tcgen05.fence::after_thread_sync before its next tcgen05.mma.  In the PTX memory model those two fences order the
+// asynchronous tensor-memory accesses on either side of a synchronisation that itself may be relaxed, as long as the arrival
+// and the wait are at one scope that holds both threads: bar_wait<true>.  (A release at cluster scope waited for all outstanding
+// stores, 3000 clocks of the 7000 that the epilogue of a 256 x 256 tile with plain outputs took.)
 __device__ __forceinline__ void bar_arrive_remote(uint32_t addr)
 {
     asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(addr) : "memory");

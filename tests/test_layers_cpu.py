@@ -50,3 +50,12 @@ def test_epilogue_gives_up_as_one():
     # (the other word is in use until every warp has passed the next tile's barrier: two take turns)
     assert re.search(r"__shared__ int[^;]*\b%s\[2\]" % word.group(1), text)
     assert len(re.findall(r"\b%s\[" % word.group(1), loop)) == 2  # written once, read once
+
+
+def test_pair_waits_at_the_scope_it_arrives_at():
+    """A pair's accumulator is freed by arrivals from both blocks: they are made, and have to be waited for, at cluster scope."""
+    ptx, product = _source("layers_ptx.cuh"), _source("layers_product.cu")
+    assert "mbarrier.arrive.relaxed.cluster.shared::cluster.b64" in ptx
+    assert "mbarrier.try_wait.parity.relaxed.cluster.shared::cta.b64" in ptx
+    waits = re.findall(r"bar_wait(<\w+>)?\(&acc_empty", product)
+    assert waits and set(waits) == {"<PAIRED>"}
