@@ -20,9 +20,18 @@ _ACTS = {"none": 0, "relu": 1, "gelu": 2, "silu": 3}
 _SCORES = {"softmax": 0, "sigmoid": 1}
 
 
-def _matrix(t, rows, cols, dtype, name):
-    """(address, distance of rows) of a [rows][cols] tensor."""
-    if t.dtype is not dtype or not t.is_cuda:
+def _elsewhere(t, index, name):
+    """Raises: t is not on the handle's device, GPU `index`."""
+    if not t.is_cuda:
+        raise TypeError("%s must be a CUDA tensor" % name)
+    raise ValueError("%s is on %s, the handle on cuda:%d" % (name, t.device, index))
+
+
+def _matrix(t, rows, cols, dtype, index, name):
+    """(address, distance of rows) of a [rows][cols] tensor on GPU `index`."""
+    if t.get_device() != index:
+        _elsewhere(t, index, name)
+    if t.dtype is not dtype:
         raise TypeError("%s must be a 2-d CUDA tensor of %s with contiguous rows" % (name, dtype))
     if t.shape != (rows, cols):
         raise ValueError("%s must have shape %s, not %s" % (name, (rows, cols), tuple(t.shape)))
@@ -32,11 +41,13 @@ def _matrix(t, rows, cols, dtype, name):
     return t.data_ptr(), far if rows > 1 else cols
 
 
-def _whole(t, shape, dtype, name):
-    """Address of a contiguous tensor; 0 for None."""
+def _whole(t, shape, dtype, index, name):
+    """Address of a contiguous tensor on GPU `index`; 0 for None."""
     if t is None:
         return 0
-    if t.dtype is not dtype or not t.is_cuda or not t.is_contiguous():
+    if t.get_device() != index:
+        _elsewhere(t, index, name)
+    if t.dtype is not dtype or not t.is_contiguous():
         raise TypeError("%s must be a contiguous CUDA tensor of %s" % (name, dtype))
     if t.shape != shape:
         raise ValueError("%s must have shape %s, not %s" % (name, shape, tuple(t.shape)))
@@ -92,12 +103,12 @@ class Layers:
         T, D = x.shape
         if weight.dim() != 2:
             raise ValueError("weight must be 2-d")
-        rows = weight.shape[0]
+        rows, on = weight.shape[0], self.device.index
         if gated and rows % 2:
             raise ValueError("a gated weight has an even number of rows")
-        xp, ldx = _matrix(x, T, D, x.dtype, "x")
-        return (kind, T, D, rows // 2 if gated else rows, rows, xp, ldx, _whole(weight, (rows, D), x.dtype, "weight"),
-                0 if bias is None else _whole(bias, (rows,), x.dtype, "bias"))
+        xp, ldx = _matrix(x, T, D, x.dtype, on, "x")
+        return (kind, T, D, rows // 2 if gated else rows, rows, xp, ldx, _whole(weight, (rows, D), x.dtype, on, "weight"),
+                0 if bias is None else _whole(bias, (rows,), x.dtype, on, "bias"))
 
     def linear(self, x, weight, bias=None, residual=None, act="none", gated=False, out=None, stream=None):
         """som_linear: act(x weight^T + bias) + residual; gated: weight's first half of rows is activated and multiplies
@@ -107,8 +118,8 @@ class Layers:
             out = x.new_empty((T, F))
             yp, ldy = out.data_ptr(), F
         else:
-            yp, ldy = _matrix(out, T, F, x.dtype, "out")
-        rp, ldr = (0, 0) if residual is None else _matrix(residual, T, F, x.dtype, "residual")
+            yp, ldy = _matrix(out, T, F, x.dtype, self.device.index, "out")
+        rp, ldr = (0, 0) if residual is None else _matrix(residual, T, F, x.dtype, self.device.index, "residual")
         rc = self._lib.som_linear(self._h, kind, _code(_ACTS, act, "act"), bool(gated), T, D, F, xp, ldx, wp, bp, rp, ldr, yp, ldy,
                                   self._stream(stream))
         if rc:
@@ -118,7 +129,7 @@ class Layers:
     def linear_backward(self, x, weight, dy, bias=None, act="none", gated=False, stream=None):
         """som_linear_backward: {"dx", "dweight"} and, with a bias, "dbias" (the residual's gradient is dy)."""
         kind, T, D, F, rows, xp, ldx, wp, bp = self._unit(x, weight, bias, gated)
-        gp, ldg = _matrix(dy, T, F, x.dtype, "dy")
+        gp, ldg = _matrix(dy, T, F, x.dtype, self.device.index, "dy")
         out = {"dx": x.new_empty((T, D)), "dweight": x.new_empty((rows, D))}
         if bias is not None:
             out["dbias"] = x.new_empty((rows,))
@@ -137,7 +148,7 @@ class Layers:
         if logits.device != self.device:
             raise ValueError("logits are on %s, the handle on %s" % (logits.device, self.device))
         T, E = logits.shape
-        return (kind, T, E, *_matrix(logits, T, E, logits.dtype, "logits"))
+        return (kind, T, E, *_matrix(logits, T, E, logits.dtype, self.device.index, "logits"))
 
     def route(self, logits, k, score="softmax", bias=None, groups=1, top_groups=1, group_best=1, renorm=True, scale=1.0,
               stream=None):
@@ -146,7 +157,7 @@ class Layers:
         new = logits.new_empty
         weights, indices, counts = new((T, k), dtype=torch.float32), new((T, k), dtype=torch.int32), new((E,), dtype=torch.int32)
         rc = self._lib.som_route(self._h, kind, _code(_SCORES, score, "score"), T, E, k, lp, ld,
-                                 0 if bias is None else _whole(bias, (E,), torch.float32, "bias"), groups, top_groups, group_best,
+                                 0 if bias is None else _whole(bias, (E,), torch.float32, self.device.index, "bias"), groups, top_groups, group_best,
                                  bool(renorm), scale, weights.data_ptr(), indices.data_ptr(), counts.data_ptr(), self._stream(stream))
         if rc:
             self._check(rc, "som_route")
@@ -158,8 +169,8 @@ class Layers:
         k = indices.shape[-1]
         out = logits.new_empty((T, E))
         rc = self._lib.som_route_backward(self._h, kind, _code(_SCORES, score, "score"), T, E, k, lp, ld,
-                                          _whole(indices, (T, k), torch.int32, "indices"),
-                                          _whole(dweights, (T, k), torch.float32, "dweights"), bool(renorm), scale,
+                                          _whole(indices, (T, k), torch.int32, self.device.index, "indices"),
+                                          _whole(dweights, (T, k), torch.float32, self.device.index, "dweights"), bool(renorm), scale,
                                           out.data_ptr(), self._stream(stream))
         if rc:
             self._check(rc, "som_route_backward")
@@ -175,14 +186,14 @@ class Layers:
             raise ValueError("a gated w1 has an even number of rows")
         I = rows // 2 if gated else rows
         k = indices.shape[1]
-        t, wt = x.dtype, weights.dtype
+        t, wt, on = x.dtype, weights.dtype, self.device.index
         if wt is not torch.float32 and wt is not t:
             raise TypeError("weights must be float32 or of x's type")
-        xp, ldx = _matrix(x, T, D, t, "x")
-        return kind, T, E, k, D, I, rows, (xp, ldx, _whole(indices, (T, k), torch.int32, "indices"),
-                                           _whole(weights, (T, k), wt, "weights"), _TYPES[wt],
-                                           _whole(w1, (E, rows, D), t, "w1"), _whole(b1, (E, rows), t, "b1"),
-                                           _whole(w2, (E, D, I), t, "w2"), _whole(b2, (E, D), t, "b2"))
+        xp, ldx = _matrix(x, T, D, t, on, "x")
+        return kind, T, E, k, D, I, rows, (xp, ldx, _whole(indices, (T, k), torch.int32, on, "indices"),
+                                           _whole(weights, (T, k), wt, on, "weights"), _TYPES[wt],
+                                           _whole(w1, (E, rows, D), t, on, "w1"), _whole(b1, (E, rows), t, on, "b1"),
+                                           _whole(w2, (E, D, I), t, on, "w2"), _whole(b2, (E, D), t, on, "b2"))
 
     def experts(self, x, indices, weights, w1, w2, b1=None, b2=None, residual=None, act="silu", gated=True, out=None, stream=None):
         """som_experts: residual + sum over a token's experts of weight * (w2 act(w1 x + b1) + b2).  Returns [T, D]."""
@@ -191,8 +202,8 @@ class Layers:
             out = x.new_empty((T, D))
             yp, ldy = out.data_ptr(), D
         else:
-            yp, ldy = _matrix(out, T, D, x.dtype, "out")
-        rp, ldr = (0, 0) if residual is None else _matrix(residual, T, D, x.dtype, "residual")
+            yp, ldy = _matrix(out, T, D, x.dtype, self.device.index, "out")
+        rp, ldr = (0, 0) if residual is None else _matrix(residual, T, D, x.dtype, self.device.index, "residual")
         rc = self._lib.som_experts(self._h, kind, _code(_ACTS, act, "act"), bool(gated), T, E, k, D, I, *p, rp, ldr, yp, ldy,
                                    self._stream(stream))
         if rc:
@@ -202,7 +213,7 @@ class Layers:
     def experts_backward(self, x, indices, weights, w1, w2, dy, b1=None, b2=None, act="silu", gated=True, stream=None):
         """som_experts_backward: {"dx", "dweights", "dw1", "dw2"} and, with biases, "db1", "db2"."""
         kind, T, E, k, D, I, rows, p = self._experts(x, indices, weights, w1, w2, b1, b2, gated)
-        gp, ldg = _matrix(dy, T, D, x.dtype, "dy")
+        gp, ldg = _matrix(dy, T, D, x.dtype, self.device.index, "dy")
         new = x.new_empty
         out = {"dx": new((T, D)), "dweights": weights.new_empty((T, k)), "dw1": new((E, rows, D)), "dw2": new((E, D, I))}
         if b1 is not None:

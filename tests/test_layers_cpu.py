@@ -6,7 +6,7 @@ import re
 import pytest
 import torch
 
-from paper_2608_24067_b200 import som
+from paper_2608_24067_b200 import layers, som
 
 
 def test_null_handles():
@@ -59,3 +59,68 @@ def test_pair_waits_at_the_scope_it_arrives_at():
     assert "mbarrier.try_wait.parity.relaxed.cluster.shared::cta.b64" in ptx
     waits = re.findall(r"bar_wait(<\w+>)?\(&acc_empty", product)
     assert waits and set(waits) == {"<PAIRED>"}
+
+
+class _On(torch.Tensor):
+    """A CPU tensor that says that it lies on GPU `index`."""
+
+    index = 0
+    is_cuda = property(lambda self: True)
+    device = property(lambda self: torch.device("cuda", self.index))
+    get_device = lambda self: self.index  # noqa: E731
+
+
+class _Refused(AssertionError):
+    pass
+
+
+class _Library:
+    """Stands for the compiled library: no call may get this far."""
+
+    def __getattr__(self, name):
+        def call(*a):
+            raise _Refused(name)
+        return call
+
+
+def _handle():
+    h = layers.Layers.__new__(layers.Layers)
+    h._lib, h._h, h.device = _Library(), ctypes.c_void_p(), torch.device("cuda", 0)
+    h._stream = lambda stream: 0
+    return h
+
+
+T, E, K, D, I = 4, 3, 2, 64, 16
+BF16 = torch.bfloat16
+TENSORS = {
+    "linear": {"x": ((T, D), BF16), "weight": ((32, D), BF16), "bias": ((32,), BF16), "residual": ((T, 32), BF16), "out": ((T, 32), BF16)},
+    "linear_backward": {"x": ((T, D), BF16), "weight": ((32, D), BF16), "dy": ((T, 32), BF16), "bias": ((32,), BF16)},
+    "route": {"logits": ((T, E), torch.float32), "bias": ((E,), torch.float32)},
+    "route_backward": {"logits": ((T, E), torch.float32), "indices": ((T, K), torch.int32), "dweights": ((T, K), torch.float32)},
+    "experts": {"x": ((T, D), BF16), "indices": ((T, K), torch.int32), "weights": ((T, K), torch.float32), "w1": ((E, 2 * I, D), BF16),
+                "w2": ((E, D, I), BF16), "b1": ((E, 2 * I), BF16), "b2": ((E, D), BF16), "residual": ((T, D), BF16), "out": ((T, D), BF16)},
+    "experts_backward": {"x": ((T, D), BF16), "indices": ((T, K), torch.int32), "weights": ((T, K), torch.float32), "w1": ((E, 2 * I, D), BF16),
+                         "w2": ((E, D, I), BF16), "dy": ((T, D), BF16), "b1": ((E, 2 * I), BF16), "b2": ((E, D), BF16)},
+}
+
+
+def _call(name, elsewhere=None, where=1):
+    args = {n: torch.zeros(shape, dtype=dtype).as_subclass(_On) for n, (shape, dtype) in TENSORS[name].items()}
+    if elsewhere:
+        shape, dtype = TENSORS[name][elsewhere]
+        args[elsewhere] = torch.zeros(shape, dtype=dtype)  # where < 0: on the host
+        if where >= 0:
+            args[elsewhere] = args[elsewhere].as_subclass(type("_Other", (_On,), {"index": where}))
+    return getattr(_handle(), name)(**args, **({"k": 2} if name == "route" else {}))
+
+
+@pytest.mark.parametrize("name", TENSORS)
+def test_tensors_of_another_device_are_refused(name):
+    """Every tensor of a call has to lie on the handle's device: the address of one that does not would be an illegal access."""
+    with pytest.raises(_Refused):  # all on the handle's device: the call goes through to the library
+        _call(name)
+    for n in TENSORS[name]:
+        with pytest.raises(ValueError):
+            _call(name, n, 1)
+        with pytest.raises((TypeError, ValueError)):
+            _call(name, n, -1)
