@@ -64,7 +64,8 @@ def _code(table, key, name):
 class Layers:
     """Handle of the dense operators on one device (``som_layers_create``): workspace and status.
 
-    Calls on one handle must not overlap on the GPU: issue them on one stream or order the streams."""
+    Calls on one handle must not overlap on the GPU: issue them on one stream or order the streams.  Calls run on the current
+    stream, or on ``stream``: the caller orders that stream behind what writes the inputs, and what reads the outputs behind it."""
 
     def __init__(self, device=None):
         self._lib = load_library()
@@ -82,7 +83,23 @@ class Layers:
         if rc != SOM_OK:
             raise SomError(rc, where, self._lib.som_layers_last_cuda_error(self._h))
 
-    def _stream(self, stream) -> int:
+    def _on(self, stream, call, *args, **kw):
+        """call(*args, **kw) on `stream`.  Its outputs are that stream's memory: memory of the current stream may have work before it
+        that was queued when it belonged to another tensor.  And neither what the call is given nor what it returns is handed
+        out again before both streams are done with it."""
+        if stream.device != self.device:
+            raise ValueError("the stream is on %s, the handle on %s" % (stream.device, self.device))
+        before = torch.cuda.current_stream(self.device)
+        with torch.cuda.stream(stream):
+            out = call(*args, **kw)
+        for t in (*args, *kw.values()):
+            if isinstance(t, torch.Tensor):
+                t.record_stream(stream)
+        for t in out.values() if isinstance(out, dict) else (out,):
+            t.record_stream(before)
+        return out
+
+    def _stream(self, stream=None) -> int:
         if stream is not None:
             return stream.cuda_stream
         if _raw_stream is not None:
@@ -113,6 +130,8 @@ class Layers:
     def linear(self, x, weight, bias=None, residual=None, act="none", gated=False, out=None, stream=None):
         """som_linear: act(x weight^T + bias) + residual; gated: weight's first half of rows is activated and multiplies
         the products of the second.  Returns [T, F]."""
+        if stream is not None:
+            return self._on(stream, self.linear, x, weight, bias, residual, act, gated, out)
         kind, T, D, F, rows, xp, ldx, wp, bp = self._unit(x, weight, bias, gated)
         if out is None:
             out = x.new_empty((T, F))
@@ -121,13 +140,15 @@ class Layers:
             yp, ldy = _matrix(out, T, F, x.dtype, self.device.index, "out")
         rp, ldr = (0, 0) if residual is None else _matrix(residual, T, F, x.dtype, self.device.index, "residual")
         rc = self._lib.som_linear(self._h, kind, _code(_ACTS, act, "act"), bool(gated), T, D, F, xp, ldx, wp, bp, rp, ldr, yp, ldy,
-                                  self._stream(stream))
+                                  self._stream())
         if rc:
             self._check(rc, "som_linear")
         return out
 
     def linear_backward(self, x, weight, dy, bias=None, act="none", gated=False, stream=None):
         """som_linear_backward: {"dx", "dweight"} and, with a bias, "dbias" (the residual's gradient is dy)."""
+        if stream is not None:
+            return self._on(stream, self.linear_backward, x, weight, dy, bias, act, gated)
         kind, T, D, F, rows, xp, ldx, wp, bp = self._unit(x, weight, bias, gated)
         gp, ldg = _matrix(dy, T, F, x.dtype, self.device.index, "dy")
         out = {"dx": x.new_empty((T, D)), "dweight": x.new_empty((rows, D))}
@@ -135,7 +156,7 @@ class Layers:
             out["dbias"] = x.new_empty((rows,))
         rc = self._lib.som_linear_backward(self._h, kind, _code(_ACTS, act, "act"), bool(gated), T, D, F, xp, ldx, wp, bp, gp, ldg,
                                            out["dx"].data_ptr(), out["dweight"].data_ptr(),
-                                           out["dbias"].data_ptr() if bias is not None else 0, self._stream(stream))
+                                           out["dbias"].data_ptr() if bias is not None else 0, self._stream())
         if rc:
             self._check(rc, "som_linear_backward")
         return out
@@ -153,25 +174,29 @@ class Layers:
     def route(self, logits, k, score="softmax", bias=None, groups=1, top_groups=1, group_best=1, renorm=True, scale=1.0,
               stream=None):
         """som_route: {"weights" fp32 [T, k], "indices" int32 [T, k], "counts" int32 [E]}."""
+        if stream is not None:
+            return self._on(stream, self.route, logits, k, score, bias, groups, top_groups, group_best, renorm, scale)
         kind, T, E, lp, ld = self._logits(logits)
         new = logits.new_empty
         weights, indices, counts = new((T, k), dtype=torch.float32), new((T, k), dtype=torch.int32), new((E,), dtype=torch.int32)
         rc = self._lib.som_route(self._h, kind, _code(_SCORES, score, "score"), T, E, k, lp, ld,
                                  0 if bias is None else _whole(bias, (E,), torch.float32, self.device.index, "bias"), groups, top_groups, group_best,
-                                 bool(renorm), scale, weights.data_ptr(), indices.data_ptr(), counts.data_ptr(), self._stream(stream))
+                                 bool(renorm), scale, weights.data_ptr(), indices.data_ptr(), counts.data_ptr(), self._stream())
         if rc:
             self._check(rc, "som_route")
         return {"weights": weights, "indices": indices, "counts": counts}
 
     def route_backward(self, logits, indices, dweights, score="softmax", renorm=True, scale=1.0, stream=None):
         """som_route_backward: the logits' gradient [T, E]."""
+        if stream is not None:
+            return self._on(stream, self.route_backward, logits, indices, dweights, score, renorm, scale)
         kind, T, E, lp, ld = self._logits(logits)
         k = indices.shape[-1]
         out = logits.new_empty((T, E))
         rc = self._lib.som_route_backward(self._h, kind, _code(_SCORES, score, "score"), T, E, k, lp, ld,
                                           _whole(indices, (T, k), torch.int32, self.device.index, "indices"),
                                           _whole(dweights, (T, k), torch.float32, self.device.index, "dweights"), bool(renorm), scale,
-                                          out.data_ptr(), self._stream(stream))
+                                          out.data_ptr(), self._stream())
         if rc:
             self._check(rc, "som_route_backward")
         return out
@@ -197,6 +222,8 @@ class Layers:
 
     def experts(self, x, indices, weights, w1, w2, b1=None, b2=None, residual=None, act="silu", gated=True, out=None, stream=None):
         """som_experts: residual + sum over a token's experts of weight * (w2 act(w1 x + b1) + b2).  Returns [T, D]."""
+        if stream is not None:
+            return self._on(stream, self.experts, x, indices, weights, w1, w2, b1, b2, residual, act, gated, out)
         kind, T, E, k, D, I, rows, p = self._experts(x, indices, weights, w1, w2, b1, b2, gated)
         if out is None:
             out = x.new_empty((T, D))
@@ -205,13 +232,15 @@ class Layers:
             yp, ldy = _matrix(out, T, D, x.dtype, self.device.index, "out")
         rp, ldr = (0, 0) if residual is None else _matrix(residual, T, D, x.dtype, self.device.index, "residual")
         rc = self._lib.som_experts(self._h, kind, _code(_ACTS, act, "act"), bool(gated), T, E, k, D, I, *p, rp, ldr, yp, ldy,
-                                   self._stream(stream))
+                                   self._stream())
         if rc:
             self._check(rc, "som_experts")
         return out
 
     def experts_backward(self, x, indices, weights, w1, w2, dy, b1=None, b2=None, act="silu", gated=True, stream=None):
         """som_experts_backward: {"dx", "dweights", "dw1", "dw2"} and, with biases, "db1", "db2"."""
+        if stream is not None:
+            return self._on(stream, self.experts_backward, x, indices, weights, w1, w2, dy, b1, b2, act, gated)
         kind, T, E, k, D, I, rows, p = self._experts(x, indices, weights, w1, w2, b1, b2, gated)
         gp, ldg = _matrix(dy, T, D, x.dtype, self.device.index, "dy")
         new = x.new_empty
@@ -223,7 +252,7 @@ class Layers:
         rc = self._lib.som_experts_backward(self._h, kind, _code(_ACTS, act, "act"), bool(gated), T, E, k, D, I, *p, gp, ldg,
                                             out["dx"].data_ptr(), out["dweights"].data_ptr(), out["dw1"].data_ptr(),
                                             out["db1"].data_ptr() if b1 is not None else 0, out["dw2"].data_ptr(),
-                                            out["db2"].data_ptr() if b2 is not None else 0, self._stream(stream))
+                                            out["db2"].data_ptr() if b2 is not None else 0, self._stream())
         if rc:
             self._check(rc, "som_experts_backward")
         return out

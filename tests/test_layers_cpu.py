@@ -86,7 +86,7 @@ class _Library:
 def _handle():
     h = layers.Layers.__new__(layers.Layers)
     h._lib, h._h, h.device = _Library(), ctypes.c_void_p(), torch.device("cuda", 0)
-    h._stream = lambda stream: 0
+    h._stream = lambda stream=None: 0
     return h
 
 
@@ -124,3 +124,53 @@ def test_tensors_of_another_device_are_refused(name):
             _call(name, n, 1)
         with pytest.raises((TypeError, ValueError)):
             _call(name, n, -1)
+
+
+@pytest.mark.parametrize("name", TENSORS)
+def test_memory_follows_the_stream(name, monkeypatch):
+    """With `stream=` the outputs are that stream's memory (another stream may still have work in memory of its own that was
+    freed), and what the call is given and returns is not handed out again while either stream uses it."""
+    import contextlib
+    now, log = ["main"], []
+
+    class Stream:
+        def __init__(self, name):
+            self.name, self.cuda_stream, self.device = name, len(name), torch.device("cuda", 0)
+
+    main, side = Stream("main"), Stream("side")
+
+    @contextlib.contextmanager
+    def as_current(stream):
+        before, now[0] = now[0], stream.name
+        yield
+        now[0] = before
+
+    monkeypatch.setattr(torch.cuda, "stream", as_current)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: {"main": main, "side": side}[now[0]])
+
+    class Seen(_On):
+        def new_empty(self, *a, **kw):
+            log.append(("made", now[0]))
+            return super().new_empty(*a, **kw).as_subclass(Seen)
+
+        def record_stream(self, stream):
+            log.append((self.what if hasattr(self, "what") else "output", stream.name))
+
+    h = _handle()
+    h._lib = type("Library", (), {"__getattr__": lambda self, n: lambda *a: log.append(("called", now[0])) or 0})()
+    args = {n: torch.zeros(shape, dtype=dtype).as_subclass(Seen) for n, (shape, dtype) in TENSORS[name].items() if n != "out"}
+    for n in args:
+        args[n].what = n
+    kw = {"k": 2} if name == "route" else {}
+    getattr(h, name)(**args, **kw)
+    assert {w for what, w in log if what in ("made", "called")} == {"main"} and not any(what in args for what, _ in log)
+    log.clear()
+    out = getattr(h, name)(**args, **kw, stream=side)
+    count = len(out) if isinstance(out, dict) else 1
+    assert [w for what, w in log if what in ("made", "called")] == ["side"] * (count + 1)
+    assert sorted(what for what, w in log if what in args and w == "side") == sorted(args)
+    assert log.count(("output", "main")) == count
+    other = Stream("far")
+    other.device = torch.device("cuda", 1)
+    with pytest.raises(ValueError):
+        getattr(h, name)(**args, **kw, stream=other)
