@@ -460,10 +460,12 @@ int som_linear_backward(som_layers* l, int type, int act, int gated, int64_t T, 
  *   keys     what the choice goes by: s + bias (bias fp32 [E] or NULL), both in fp32, s rounded from 64 bits so that the
  *            order of two near scores is that of their exact values; without a bias (and with groups == 1 or group_best == 1)
  *            the logits themselves, which order the experts the same way without a rounding.
+ *            A bias of -inf or NaN switches an expert off: it is not chosen, however few others are left, and has no part in its
+ *            group's key (its score stays in the softmax's sum).
  *   groups   E / groups consecutive experts form a group (E % groups == 0); a group's key is the sum of its group_best
  *            (1 or 2) largest keys, and only experts of the top_groups best groups can be chosen.
  *   choice   the k largest keys, best first; ties go to the lowest index, among groups too.
- *   indices  int32 [T][k], -1 where fewer than k experts are left.
+ *   indices  int32 [T][k], -1 where fewer than k experts are left (unmasked, on, and in the groups kept).
  *   weights  fp32 [T][k]: scale * s of the chosen experts, divided by their sum if renorm (0 if the sum is 0); 0 beside
  *            an index of -1.  The bias does not enter the weights.
  *   counts   int32 [E] or NULL: tokens that chose each expert (the bias for balance is moved by them).

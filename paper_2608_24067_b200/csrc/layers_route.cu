@@ -145,7 +145,7 @@ __device__ __noinline__ int choose_exact(const RouteArgs& a, int64_t row, float 
                 s = (float)((soft ? e : 1.0) / (soft ? sum : 1.0 + e));
                 if (a.bias && first + v < a.E) s += *(a.bias + first + v);
             }
-            key[v] = live && s == s ? som_ordered_bits(s + 0.f) : 0u;  // + 0: the two zeros tie
+            key[v] = live && s > -INFINITY ? som_ordered_bits(s + 0.f) : 0u;  // + 0: the two zeros tie
         }
         if (pass == 0) sum = warp_sum(sum);
     }
@@ -246,7 +246,7 @@ __device__ __noinline__ uint32_t exact_key(const RouteArgs& a, int64_t row, int 
         s = (float)(1.0 / (1.0 + exp(-(double)x)));
         if (a.bias) s += a.bias[i];
     }
-    return x > -INFINITY && s == s ? som_ordered_bits(s + 0.f) : 0u;
+    return x > -INFINITY && s > -INFINITY ? som_ordered_bits(s + 0.f) : 0u;  // (a bias of -inf or NaN: never chosen)
 }
 
 // Which groups are kept, by one warp for one token: lane g holds the key of group g; `low` and `next` are the smallest key

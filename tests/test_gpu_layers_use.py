@@ -1,4 +1,4 @@
-"""GPU tests of how the dense operators are used: other streams."""
+"""GPU tests of how the dense operators are used: other streams, biases that switch experts off."""
 import math
 
 import pytest
@@ -62,3 +62,58 @@ def test_memory_of_another_stream(L):
     assert again.data_ptr() != at
     torch.cuda.synchronize()
     assert torch.equal(read, want)
+
+
+def _choice(z, bias, k, score, groups, top_groups, group_best):
+    """The k experts of the largest keys, best first, and their scores, from fp64; a key of -inf or NaN is never chosen and has no
+    part in its group's key."""
+    E = z.shape[1]
+    z = z.double()
+    s = torch.sigmoid(z) if score == "sigmoid" else torch.softmax(z, 1)
+    key = (s.float() + bias).masked_fill(z == -math.inf, -math.inf)
+    key = key.masked_fill(key.isnan(), -math.inf)
+    indices = torch.full((len(z), k), -1)
+    for t in range(len(z)):
+        row = key[t].tolist()
+        rank = []
+        for g in range(groups):
+            best = sorted((v for v in row[g * (E // groups):(g + 1) * (E // groups)] if v > -math.inf), reverse=True)[:group_best]
+            rank.append((-float(torch.tensor(best).sum()) if best else math.inf, g))
+        kept = {g for v, g in sorted(rank)[:top_groups] if v < math.inf}
+        of = sorted((i for i in range(E) if row[i] > -math.inf and i // (E // groups) in kept), key=lambda i: (-row[i], i))[:k]
+        indices[t, :len(of)] = torch.tensor(of, dtype=torch.int64)
+    return indices, s.gather(1, indices.clamp_min(0)) * (indices >= 0)
+
+
+SWITCHES = [(64, 6, 1, 1, 1), (128, 8, 4, 2, 2), (128, 8, 4, 2, 1), (256, 12, 8, 3, 2), (100, 9, 1, 1, 1)]
+
+
+@pytest.mark.parametrize("T", [1, 97, 12301])
+@pytest.mark.parametrize("E,k,groups,top_groups,group_best", SWITCHES)
+@pytest.mark.parametrize("score", ["sigmoid", "softmax"])
+@pytest.mark.parametrize("dtype", [FP32, BF16])
+@pytest.mark.parametrize("off", [-math.inf, math.nan])
+def test_route_bias_switches_off(L, T, E, k, groups, top_groups, group_best, score, dtype, off):
+    """An expert whose bias is -inf is never chosen, also where fewer than k others are left, and has no part in its group's key; NaN the
+    same.  An infinite bias of the other sign is chosen first."""
+    gen = torch.Generator().manual_seed(T + E)
+    z = (torch.randn(T, E, generator=gen) * 2).to(dtype)
+    bias = torch.randn(E, generator=gen) * 0.2
+    size = E // groups
+    bias[torch.rand(E, generator=gen) < 0.5] = off
+    bias[:size] = off
+    bias[2] = 0.9  # the first group: one expert on (group_best 2: its key is that one's)
+    if groups > 1:
+        bias[size:2 * size] = off  # a group without any
+    else:
+        bias[k - 2:] = off  # fewer than k on
+    bias[size - 1] = math.inf if T == 97 else bias[size - 1]
+    got = L.route(z.cuda(), k, score=score, bias=bias.cuda(), groups=groups, top_groups=top_groups, group_best=group_best)
+    some = torch.arange(0, T, 1 + T // 97)
+    at, s = _choice(z[some], bias, k, score, groups, top_groups, group_best)
+    assert torch.equal(got["indices"][some].cpu().long(), at)
+    # exponentials, a sum of up to E of them and two divisions in fp32: (E + 16) half units
+    w = s / s.sum(1, keepdim=True)
+    assert ((got["weights"][some].double().cpu() - w).abs() <= (E + 16) * 2.0 ** -24 * w).all()
+    every = got["indices"][got["indices"] >= 0].long()
+    assert torch.equal(got["counts"].long(), torch.bincount(every, minlength=E))
