@@ -200,6 +200,36 @@ __device__ __forceinline__ float key_errors(int score) { return score == SOM_SCO
 constexpr int KEY_BITS = 22, INDEX_BITS = 10;
 constexpr uint32_t KEY_MOST = (1u << KEY_BITS) - 1u, INDEX_MASK = (1u << INDEX_BITS) - 1u;
 
+// How scores and biases are packed.  Keys lie between the lowest bias and 1 + the highest, with 0 among them.  Biases below FAR_BIAS
+// (-1e9 switches an expert off) do not count for that range: such an expert's key is the lowest, 1, which no key within the range
+// gets, and where the choice, or a kept group's key, would hang on it, exact keys are taken.  (16384 tokens x 256 experts with groups,
+// one bias of -1e9: 27 us; 121 where it counts for the range, and so every token takes the exact keys.)
+struct Packing {
+    float ceiling, scale;
+    uint32_t margin;  // key units: rounding of the distances and the scores' errors
+    bool fits;        // (not with biases of 2.6e5 and more)
+};
+constexpr float FAR_BIAS = -64.f;
+
+// from a lane's lowest bias that counts and its highest
+__device__ __forceinline__ Packing packing_of(float low, float high, int score)
+{
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) {
+        high = fmaxf(high, __shfl_xor_sync(ALL, high, d));
+        low = fminf(low, __shfl_xor_sync(ALL, low, d));
+    }
+    Packing p;
+    p.ceiling = 1.f + high;
+    p.scale = (float)(KEY_MOST - 8u) / (p.ceiling - low);
+    p.margin = 3 + (uint32_t)(p.scale * key_errors(score) * fmaxf(p.ceiling, 1.f - low));
+    p.fits = p.scale > 16.f;
+    return p;
+}
+
+// beyond the keys' range
+__device__ __forceinline__ bool far_key(uint32_t packed) { return (packed >> INDEX_BITS) <= 1u; }
+
 __device__ __forceinline__ void order2(uint32_t& a, uint32_t& b)
 {
     const uint32_t hi = max(a, b), lo = min(a, b);
@@ -323,27 +353,19 @@ __global__ void __launch_bounds__(32 * ROUTE_WARPS, V <= 8 ? 4 : 2) k_route(cons
         my_place = lane - my_group * lanes;
     }
     float bias[V];
-    float high = 0.f, low = 0.f;  // of the biases, with 0 among them
+    float high = 0.f, low = 0.f;
 #pragma unroll
     for (int v = 0; v < V; ++v) {
         bias[v] = a.bias && first + v < a.E ? *(a.bias + first + v) : 0.f;
         high = fmaxf(high, bias[v]);
-        low = fminf(low, bias[v]);
+        if (bias[v] >= FAR_BIAS) low = fminf(low, bias[v]);
     }
-    // packed keys: scores lie in [low, 1 + high]; logits up to 64 below the row's largest are told apart
-    float ceiling = 0.f, scale = (float)KEY_MOST / 64.f;
-    uint32_t margin = 3;  // key units: rounding of the distances (and the scores' errors)
-    if (by_score) {
-#pragma unroll
-        for (int d = 16; d > 0; d >>= 1) {
-            high = fmaxf(high, __shfl_xor_sync(ALL, high, d));
-            low = fminf(low, __shfl_xor_sync(ALL, low, d));
-        }
-        ceiling = 1.f + high;
-        scale = (float)KEY_MOST / (ceiling - low);
-        margin = 3 + (uint32_t)(scale * key_errors(a.score) * fmaxf(ceiling, 1.f - low));
-    }
-    const bool packs = (!by_groups || lanes) && a.k < 32 && scale > 16.f;  // (not with huge or infinite biases)
+    // packed keys: scores and biases; or logits, of which those up to 64 below the row's largest are told apart
+    Packing pack{0.f, (float)KEY_MOST / 64.f, 3, true};
+    if (by_score) pack = packing_of(low, high, a.score);
+    const float ceiling = pack.ceiling, scale = pack.scale;
+    const uint32_t margin = pack.margin;
+    const bool packs = (!by_groups || lanes) && a.k < 32 && pack.fits;
 
     for (int64_t t = (int64_t)blockIdx.x * ROUTE_WARPS + (threadIdx.x >> 5); t < a.T; t += (int64_t)gridDim.x * ROUTE_WARPS) {
         const int64_t row = t * a.ld;
@@ -377,7 +399,7 @@ __global__ void __launch_bounds__(32 * ROUTE_WARPS, V <= 8 ? 4 : 2) k_route(cons
                     else if (a.score == SOM_SCORE_SOFTMAX) d = ceiling - (__fdividef(exp_from(x[v], top), total) + bias[v]);
                     else d = ceiling - (__fdividef(1.f, 1.f + __expf(-x[v])) + bias[v]);
                     const uint32_t u = KEY_MOST - min((uint32_t)(d * scale), KEY_MOST - 1u);
-                    key[v] = x[v] > -INFINITY && d == d ? u << INDEX_BITS | (INDEX_MASK - first - v) : 0u;
+                    key[v] = x[v] > -INFINITY && d < INFINITY ? u << INDEX_BITS | (INDEX_MASK - first - v) : 0u;
                 }
             }
             if (by_groups) {
@@ -406,6 +428,8 @@ __global__ void __launch_bounds__(32 * ROUTE_WARPS, V <= 8 ? 4 : 2) k_route(cons
                     kept |= 1u << g;
                     if (lane == g) mine = 0;
                 }
+                // (with the lowest key in it, a sum is an upper bound of the group's key: enough for a group that is not kept)
+                if (a.group_best == 2 && __any_sync(ALL, my_place == 0 && ((kept >> my_group) & 1u) && far_key(m2))) sure = false;
                 const uint32_t next = last ? __reduce_max_sync(ALL, mine) : 0u;
                 if (!exact16 && next && sure) {
                     const int shift = a.group_best == 2 ? 0 : INDEX_BITS;
@@ -436,7 +460,7 @@ __global__ void __launch_bounds__(32 * ROUTE_WARPS, V <= 8 ? 4 : 2) k_route(cons
                 }
                 at = won ? (int)(INDEX_MASK - (won & INDEX_MASK)) : -1;
                 if (!exact16) {
-                    if (__any_sync(ALL, won && lane < a.k && (won >> INDEX_BITS) <= 1u)) sure = false;  // beyond the keys' range
+                    if (__any_sync(ALL, won && lane < a.k && far_key(won))) sure = false;
                     uint32_t above = __shfl_up_sync(ALL, won, 1);
                     // contested places: lane j's winner and the one above it
                     unsigned near = __ballot_sync(ALL, won && lane > 0 && (above >> INDEX_BITS) - (won >> INDEX_BITS) < margin);
@@ -554,29 +578,19 @@ __global__ void __launch_bounds__(32 * QUAD_WARPS) k_route_many(const RouteArgs 
     const bool by_score = a.bias || (a.groups > 1 && a.group_best == 2);
     const bool exact16 = TYPE != SOM_F32 && !by_score;
     const int pieces = (a.E + 31) / 32, size = a.E / a.groups, per_group = size / 32;
-    float ceiling = 0.f, scale = (float)KEY_MOST / 64.f;
-    uint32_t margin = 3;
-    if (a.bias) {
+    Packing pack{0.f, (float)KEY_MOST / 64.f, 3, true};
+    if (by_score) {
         float high = 0.f, low = 0.f;
-        for (int i = lane; i < a.E; i += 32) {
-            const float b = *(a.bias + i);
-            high = fmaxf(high, b);
-            low = fminf(low, b);
-        }
-#pragma unroll
-        for (int d = 16; d > 0; d >>= 1) {
-            high = fmaxf(high, __shfl_xor_sync(ALL, high, d));
-            low = fminf(low, __shfl_xor_sync(ALL, low, d));
-        }
-        ceiling = 1.f + high;
-        scale = (float)KEY_MOST / (ceiling - low);
-        margin = 3 + (uint32_t)(scale * key_errors(a.score) * fmaxf(ceiling, 1.f - low));
-    } else if (by_score) {
-        ceiling = 1.f;
-        scale = (float)KEY_MOST;
-        margin = 3 + (uint32_t)(scale * key_errors(a.score));
+        if (a.bias)
+            for (int i = lane; i < a.E; i += 32) {
+                const float b = *(a.bias + i);
+                high = fmaxf(high, b);
+                if (b >= FAR_BIAS) low = fminf(low, b);
+            }
+        pack = packing_of(low, high, a.score);
     }
-    const bool packs = scale > 16.f;
+    const float ceiling = pack.ceiling, scale = pack.scale;
+    const uint32_t margin = pack.margin;
 
     for (int64_t t0 = ((int64_t)blockIdx.x * QUAD_WARPS + warp) * 8; t0 < a.T; t0 += (int64_t)gridDim.x * QUAD_ROWS) {
         const int64_t t = t0 + quad < a.T ? t0 + quad : a.T - 1, row = t * a.ld;  // (past the end: the last row again, not written)
@@ -605,7 +619,7 @@ __global__ void __launch_bounds__(32 * QUAD_WARPS) k_route_many(const RouteArgs 
             total += __shfl_xor_sync(ALL, total, 1);
             total += __shfl_xor_sync(ALL, total, 2);
         }
-        bool full = !(packs && top < INFINITY);  // all keys have to be computed exactly
+        bool full = !(pack.fits && top < INFINITY);  // all keys have to be computed exactly
         auto keys_of = [&](int piece, uint32_t (&key)[8]) {
             const int at = piece * 32 + part * 8;
             float x[8];
@@ -626,13 +640,14 @@ __global__ void __launch_bounds__(32 * QUAD_WARPS) k_route_many(const RouteArgs 
                 else if (a.score == SOM_SCORE_SOFTMAX) d = ceiling - (__fdividef(exp_from(x[v], top), total) + bias[v]);
                 else d = ceiling - (__fdividef(1.f, 1.f + __expf(-x[v])) + bias[v]);
                 const uint32_t u = KEY_MOST - min((uint32_t)(d * scale), KEY_MOST - 1u);
-                key[v] = x[v] > -INFINITY && d == d ? u << INDEX_BITS | (INDEX_MASK - at - v) : 0u;
+                key[v] = x[v] > -INFINITY && d < INFINITY ? u << INDEX_BITS | (INDEX_MASK - at - v) : 0u;
             }
         };
         unsigned kept = 0;
         if (by_groups) {
             uint32_t* mine = group_keys[warp * 8 + quad];
             bool lone = false;
+            unsigned bounds = 0;  // groups whose sum has the lowest key in it: an upper bound of the group's key
             for (int g = 0; g < a.groups; ++g) {
                 uint32_t m1 = 0, m2 = 0;
                 for (int b = 0; b < per_group; ++b) {
@@ -649,6 +664,7 @@ __global__ void __launch_bounds__(32 * QUAD_WARPS) k_route_many(const RouteArgs 
                     const uint32_t o1 = __shfl_xor_sync(ALL, m1, d), o2 = __shfl_xor_sync(ALL, m2, d);
                     merge2(m1, m2, o1, o2);
                 }
+                bounds |= (unsigned)(m1 && far_key(m2)) << g;
                 lone |= m1 && !m2;  // a lone expert's distance is not comparable with the sum of two
                 if (part == 0) mine[g] = a.group_best == 2 ? (m1 >> INDEX_BITS) + (m2 >> INDEX_BITS) : m1;
             }
@@ -672,6 +688,7 @@ __global__ void __launch_bounds__(32 * QUAD_WARPS) k_route_many(const RouteArgs 
                 low = min(low, __shfl_xor_sync(ALL, low, d));
                 next = max(next, __shfl_xor_sync(ALL, next, d));
             }
+            if (a.group_best == 2 && (kept & bounds)) full = true;
             if (!exact16) {
                 const uint32_t apart = a.group_best == 2 ? 2 * margin : margin;
                 const int shift = a.group_best == 2 ? 0 : INDEX_BITS;
@@ -730,7 +747,7 @@ __global__ void __launch_bounds__(32 * QUAD_WARPS) k_route_many(const RouteArgs 
                 const uint32_t next = i + 1 < L ? list[i + 1 < L ? i + 1 : i] : rest;
                 if (i < a.k && list[i]) {
                     near |= next && (list[i] >> INDEX_BITS) - (next >> INDEX_BITS) < margin;
-                    full |= (list[i] >> INDEX_BITS) <= 1u;  // beyond the keys' range
+                    full |= far_key(list[i]);
                 }
             }
             if (by_score && a.score == SOM_SCORE_SOFTMAX) full |= near;

@@ -1,4 +1,4 @@
-"""GPU tests of how the dense operators are used: other streams, biases that switch experts off."""
+"""GPU tests of how the dense operators are used: other streams, biases that switch experts off or are large."""
 import math
 
 import pytest
@@ -117,3 +117,30 @@ def test_route_bias_switches_off(L, T, E, k, groups, top_groups, group_best, sco
     assert ((got["weights"][some].double().cpu() - w).abs() <= (E + 16) * 2.0 ** -24 * w).all()
     every = got["indices"][got["indices"] >= 0].long()
     assert torch.equal(got["counts"].long(), torch.bincount(every, minlength=E))
+
+
+@pytest.mark.parametrize("T", [33, 12301])
+@pytest.mark.parametrize("E,k,groups,top_groups,group_best", SWITCHES + [(64, 12, 4, 4, 1), (256, 8, 8, 4, 2)])
+@pytest.mark.parametrize("score", ["sigmoid", "softmax"])
+@pytest.mark.parametrize("value", [-1e9, -3e38, -2.0 ** 18, -100.0, -64.5, -20.0, 40.0, 1000.0, 1e9])
+def test_route_large_biases(L, T, E, k, groups, top_groups, group_best, score, value):
+    """Finite biases far from the others: some experts of every group, all of one and all but one of another have one; the logits
+    come from a coarse grid, so that choices are contested."""
+    gen = torch.Generator().manual_seed(T + E)
+    z = (torch.randn(T, E, generator=gen) * 4).round() / 4 + torch.randn(T, E, generator=gen) * 2.0 ** -20
+    bias = torch.randn(E, generator=gen) * 0.2
+    size = E // groups
+    far = torch.rand(E, generator=gen) < 0.3
+    far[:size] = True
+    far[1] = False
+    if groups > 1:
+        far[size:2 * size] = True
+    else:
+        far[k - 2:] = True
+    if value > 0:
+        far = torch.rand(E, generator=gen) < 0.1
+    bias[far] += value
+    got = L.route(z.cuda(), k, score=score, bias=bias.cuda(), groups=groups, top_groups=top_groups, group_best=group_best)
+    some = torch.arange(0, T, 1 + T // 97)
+    at, _ = _choice(z[some], bias, k, score, groups, top_groups, group_best)
+    assert torch.equal(got["indices"][some].cpu().long(), at)
