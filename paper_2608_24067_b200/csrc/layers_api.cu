@@ -217,6 +217,10 @@ int som_layers_destroy(som_layers* l)
 
 int som_layers_last_cuda_error(const som_layers* l) { return l ? l->last_cuda_error : 0; }
 int64_t som_layers_launch_count(const som_layers* l) { return l ? l->launches : 0; }
+int64_t som_layers_rounds(const som_layers* l, int product, int tiles)
+{
+    return l && product >= PROD_FWD && product <= PROD_DW && tiles >= NARROW && tiles <= PAIR ? l->rounds[product][tiles] : -1;
+}
 
 int som_layers_device_flags(som_layers* l, void* stream)
 {

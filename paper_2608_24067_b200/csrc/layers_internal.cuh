@@ -21,6 +21,7 @@ struct som_layers {
     int* flags;  // device, sticky LAY_FLAG_* bits
     int last_cuda_error;
     int64_t launches;
+    int64_t rounds[5][3];  // most tiles a block walked, by ProdMode and ProdShape
     void* encode;  // cuTensorMapEncodeTiled
 };
 

@@ -604,7 +604,9 @@ cudaError_t launch_as(som_layers* l, const ProdArgs& args, cudaStream_t st)
 {
     const int64_t tiles = ((int64_t)args.row_tiles * args.col_tiles + (int64_t)args.row_tiles2 * args.col_tiles2) * (MODE == PROD_DW ? args.experts : 1) * args.splits;
     const int most = SHAPE == PAIR ? l->pairs : l->sm_count, blocks = SHAPE == PAIR ? 2 : 1;
-    return launch(l, k_product<MODE, SHAPE, BF16>, dim3((unsigned)(tiles < most ? tiles : most) * blocks), THREADS, SMEM, st, blocks, args);
+    const int64_t at_once = tiles < most ? tiles : most, rounds = (tiles + at_once - 1) / at_once;
+    if (rounds > l->rounds[MODE][SHAPE]) l->rounds[MODE][SHAPE] = rounds;
+    return launch(l, k_product<MODE, SHAPE, BF16>, dim3((unsigned)at_once * blocks), THREADS, SMEM, st, blocks, args);
 }
 
 // wide tiles are for grouped rows

@@ -27,7 +27,7 @@ EXPORTS = [
     "som_launch_count", "som_set_option", "som_norms_noalloc", "som_bmu2", "som_create_f16", "som_update", "som_last_uncertain", "som_bmu_values",
     "som_bmu_host_async", "som_host_sync", "som_plan_create", "som_bmu_planned", "som_plan_destroy",
     "som_device_flags", "som_measure_fadd_peak", "som_measure_operand_paths", "som_tc_probe",
-    "som_layers_create", "som_layers_destroy", "som_layers_last_cuda_error", "som_layers_launch_count",
+    "som_layers_create", "som_layers_destroy", "som_layers_last_cuda_error", "som_layers_launch_count", "som_layers_rounds",
     "som_layers_device_flags", "som_linear", "som_linear_backward", "som_route", "som_route_backward", "som_experts",
     "som_experts_backward",
 ]
@@ -108,6 +108,8 @@ def load_library():
     lib.som_layers_destroy.argtypes = [P]
     lib.som_layers_last_cuda_error.argtypes = [P]
     lib.som_layers_launch_count.argtypes = [P]
+    lib.som_layers_rounds.argtypes = [P, INT, INT]
+    lib.som_layers_rounds.restype = I64
     lib.som_layers_device_flags.argtypes = [P, P]
     lib.som_linear.argtypes = [P, INT, INT, INT, I64, I64, I64, P, I64, P, P, P, I64, P, I64, P]
     lib.som_linear_backward.argtypes = [P, INT, INT, INT, I64, I64, I64, P, I64, P, P, P, I64, P, P, P, P]

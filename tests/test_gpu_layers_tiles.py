@@ -1,0 +1,103 @@
+"""GPU tests of the dense operators at sizes that reach every tile shape of their products, with more than one tile a block: what long
+prompts, training steps and batches of single tokens run on.  Bounds as in layers_reference.py; sums are kept short, the outputs large."""
+import os
+import sys
+
+import pytest
+import torch
+
+sys.path.insert(0, os.path.dirname(os.path.abspath(__file__)))
+import layers_reference as ref  # noqa: E402
+from test_gpu_layers import _expert_inputs, _linear_grad, _normal, _wide  # noqa: E402
+
+pytestmark = pytest.mark.gpu
+
+BF16, FP16, FP32 = torch.bfloat16, torch.float16, torch.float32
+
+
+@pytest.fixture
+def L():
+    """A handle of the test's own: it has seen no other launches."""
+    if not torch.cuda.is_available():
+        pytest.skip("no CUDA device")
+    from paper_2608_24067_b200 import layers
+    return layers.Layers()
+
+
+def _linear_inputs(T, D, F, dtype, gated, wide):
+    gen = torch.Generator().manual_seed(T + D + F)
+    rows = 2 * F if gated else F
+    return (_normal(gen, T, D, dtype=dtype, wide=wide), _normal(gen, rows, D, scale=D ** -0.5, dtype=dtype), _normal(gen, rows, dtype=dtype),
+            _normal(gen, T, F, dtype=dtype, wide=wide))
+
+
+@pytest.mark.parametrize("dtype,act,gated,bias,residual,wide", [
+    (BF16, "gelu", False, True, True, 0), (FP16, "none", False, False, False, 8), (BF16, "silu", True, True, True, 16), (FP16, "relu", True, False, False, 0)])
+def test_linear_pairs(L, dtype, act, gated, bias, residual, wide):
+    T, D, F = 2605, 136, 1048 if gated else 2072
+    x, w, b, r = _linear_inputs(T, D, F, dtype, gated, wide)
+    b, r = b if bias else None, r if residual else None
+    out = torch.zeros(T, F + wide, dtype=dtype, device="cuda")
+    y = L.linear(x, w, b, r, act=act, gated=gated, out=out[:, :F])
+    assert L.rounds("forward", "256x256") >= 2
+    h, eh, _, _ = ref.hidden(_wide(x), _wide(w), _wide(b), act, gated)
+    if r is not None:
+        h, eh = h + _wide(r), eh + 2.0 ** -22 * (h.abs() + _wide(r).abs())
+    ref.close(y, h, ref.rounded(h, eh, dtype), "y")
+    assert not out[:, F:].any()
+    assert torch.equal(y, L.linear(x, w, b, r, act=act, gated=gated))
+    assert L.device_flags() == 0
+
+
+# (dz in pairs; dx in pairs; dw in pairs)
+@pytest.mark.parametrize("product,T,D,F", [("dz", 2605, 136, 2072), ("dx", 2605, 2072, 136), ("dw", 200, 2072, 2600)])
+@pytest.mark.parametrize("dtype,act,gated,bias,wide", [
+    (BF16, "gelu", False, True, 8), (FP16, "silu", False, False, 0), (BF16, "silu", True, True, 0), (FP16, "relu", True, True, 16)])
+def test_linear_backward_pairs(L, product, T, D, F, dtype, act, gated, bias, wide):
+    F = F // 16 * 8 if gated else F
+    x, w, b, dy = _linear_inputs(T, D, F, dtype, gated, wide)
+    b = b if bias else None
+    got = L.linear_backward(x, w, dy, b, act=act, gated=gated)
+    assert L.rounds(product, "256x256") >= 2
+    want = _linear_grad(_wide(x), _wide(w), _wide(b), _wide(dy), act, gated, dtype)
+    for n, v in got.items():
+        ref.close(v, *want[n], n)
+    again = L.linear_backward(x, w, dy, b, act=act, gated=gated)
+    assert all(torch.equal(got[n], again[n]) for n in got)
+    assert L.device_flags() == 0
+
+
+# a few rows an expert; rows enough for pairs; few experts with few rows
+EXPERTS = [("128x256", 96, 64, 6, 520, 264), ("256x256", 4000, 8, 2, 520, 520), ("128x128", 300, 40, 8, 512, 256)]
+
+
+@pytest.mark.parametrize("tiles,T,E,k,D,I", EXPERTS)
+@pytest.mark.parametrize("dtype,act,gated,bias,residual", [(BF16, "silu", True, False, True), (FP16, "gelu", False, True, False), (FP16, "silu", True, True, True)])
+def test_experts_tiles(L, tiles, T, E, k, D, I, dtype, act, gated, bias, residual):
+    gen = torch.Generator().manual_seed(T + E + D)
+    s, r = _expert_inputs(T, E, k, D, I, dtype, gated, bias, residual, gen, FP32, pad=0.05)
+    y = L.experts(s["x"], s["indices"], s["weights"], s["w1"], s["w2"], s["b1"], s["b2"], r, act=act, gated=gated)
+    assert L.rounds("forward", tiles) >= 2 and all(L.rounds("forward", t) == 0 for t in {"128x128", "128x256", "256x256"} - {tiles})
+    c = {n: _wide(v) for n, v in s.items()}
+    want, bound = ref.experts(c["x"], s["indices"].cpu(), c["weights"], c["w1"], c["w2"], c["b1"], c["b2"], _wide(r), act, gated, dtype)
+    ref.close(y, want, bound, "y")
+    assert torch.equal(y, L.experts(s["x"], s["indices"], s["weights"], s["w1"], s["w2"], s["b1"], s["b2"], r, act=act, gated=gated))
+    assert L.device_flags() == 0
+
+
+@pytest.mark.parametrize("tiles,T,E,k,D,I", EXPERTS)
+@pytest.mark.parametrize("dtype,act,gated,bias,wtype", [(BF16, "silu", True, True, FP32), (FP16, "gelu", False, True, FP16), (FP16, "silu", True, False, FP32)])
+def test_experts_backward_tiles(L, tiles, T, E, k, D, I, dtype, act, gated, bias, wtype):
+    gen = torch.Generator().manual_seed(T + E + D)
+    s, _ = _expert_inputs(T, E, k, D, I, dtype, gated, bias, False, gen, wtype, pad=0.05)
+    dy = _normal(gen, T, D, dtype=dtype, wide=8)
+    got = L.experts_backward(s["x"], s["indices"], s["weights"], s["w1"], s["w2"], dy, s["b1"], s["b2"], act=act, gated=gated)
+    assert L.rounds("dz of experts", tiles) >= 2 and L.rounds("dx", tiles) >= 2
+    assert max(L.rounds("dw", t) for t in ("128x128", "256x256")) >= 2
+    c = {n: _wide(v) for n, v in s.items()}
+    want = ref.experts_backward(c["x"], s["indices"].cpu(), c["weights"], c["w1"], c["w2"], c["b1"], c["b2"], _wide(dy), act, gated, dtype)
+    for n, v in got.items():
+        ref.close(v, want[n][0], ref.rounded(*want[n], wtype) if n == "dweights" else want[n][1], n)
+    again = L.experts_backward(s["x"], s["indices"], s["weights"], s["w1"], s["w2"], dy, s["b1"], s["b2"], act=act, gated=gated)
+    assert all(torch.equal(got[n], again[n]) for n in got)
+    assert L.device_flags() == 0

@@ -174,3 +174,7 @@ def test_memory_follows_the_stream(name, monkeypatch):
     other.device = torch.device("cuda", 1)
     with pytest.raises(ValueError):
         getattr(h, name)(**args, **kw, stream=other)
+
+
+def test_rounds_without_a_handle():
+    assert som.load_library().som_layers_rounds(None, 0, 0) == -1
