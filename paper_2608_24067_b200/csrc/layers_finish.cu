@@ -75,6 +75,7 @@ __global__ void __launch_bounds__(256) k_finish(const FinishArgs a)
             });
             if (a.gated) store8(a.out + row * a.ld + a.cols + col, u, a.bf16);
         }
+        // (FINISH_DZ: dz in 16 bits, as the next products' operand; see the products' own epilogue)
         store8(a.out + row * a.ld + col, v, a.bf16);
     }
 }

@@ -495,6 +495,9 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
                     }
                     if (extra) add.template add<BF16>(v);
                     fetch(at + step_on);
+                    // The experts' hidden values are rounded to 16 bits below: the next product's instructions take no wider operands (two
+                    // 16-bit terms a value would double its work).  Weighted before: a weight of at most 1 keeps large values in fp16's
+                    // range, and what a small one loses below that range, 2^-25, is what y's own rounding loses there.
                     if (p.weigh == 1) {
 #pragma unroll
                         for (int j = 0; j < STEP; ++j) v[j] *= rw;
@@ -562,6 +565,9 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
                         v[j] *= g[j];
                         if (gated) u[j] *= g[j];
                     }
+                    // dz and the weighted h are rounded to 16 bits here, as operands of the products that follow (those would take twice the
+                    // instructions for two terms a value): dx and dw are off by 2.3e-3 (bf16) and 2.9e-4 (fp16) against 64 bits in the
+                    // relative norm, where one rounding of exact results is off by 1.7e-3 and 2.1e-4.
                     if (writes && col < p.cols) {
                         store8<BF16>(out + col, v);
                         if (gated) store8<BF16>(out + p.gate_rows + col, u);

@@ -1,12 +1,18 @@
-"""GPU tests of how the dense operators are used: other streams, biases that switch experts off or are large."""
+"""GPU tests of how the dense operators are used: other streams, biases that switch experts off or are large,
+values near the ends of fp16."""
 import math
+import os
+import sys
 
 import pytest
 import torch
 
+sys.path.insert(0, os.path.dirname(os.path.abspath(__file__)))
+import layers_reference as ref  # noqa: E402
+
 pytestmark = pytest.mark.gpu
 
-BF16, FP32 = torch.bfloat16, torch.float32
+BF16, FP16, FP32 = torch.bfloat16, torch.float16, torch.float32
 
 
 @pytest.fixture(scope="module")
@@ -144,3 +150,47 @@ def test_route_large_biases(L, T, E, k, groups, top_groups, group_best, score, v
     some = torch.arange(0, T, 1 + T // 97)
     at, _ = _choice(z[some], bias, k, score, groups, top_groups, group_best)
     assert torch.equal(got["indices"][some].cpu().long(), at)
+
+
+def _wide(t):
+    return None if t is None else t.double().cpu()
+
+
+@pytest.mark.parametrize("T,E,k", [(1, 4, 3), (60, 6, 3)])  # each slot by itself; slots ordered by expert
+@pytest.mark.parametrize("least", [1e-3, 1e-6])
+def test_experts_small_weights(L, T, E, k, least):
+    """fp16, routing weights down to `least`: weighted hidden values and dz fall below fp16's normal range, and stay within the bounds
+    that say so (an absolute 2^-24 a rounding)."""
+    gen = torch.Generator().manual_seed(T)
+    D, I = 136, 72
+    x, dy = _normal(gen, T, D, dtype=FP16), _normal(gen, T, D, dtype=FP16)
+    w1, w2 = _normal(gen, E, 2 * I, D, scale=D ** -0.5, dtype=FP16), _normal(gen, E, D, I, scale=I ** -0.5, dtype=FP16)
+    b1, b2 = _normal(gen, E, 2 * I, scale=0.3, dtype=FP16), _normal(gen, E, D, scale=0.3, dtype=FP16)
+    at = torch.rand(T, E, generator=gen).topk(k, dim=1).indices.int()
+    weights = least ** torch.rand(T, k, generator=gen)
+    args = [_wide(x), at, weights.double(), _wide(w1), _wide(w2), _wide(b1), _wide(b2)]
+    y = L.experts(x, at.cuda(), weights.cuda(), w1, w2, b1, b2, act="silu", gated=True)
+    ref.close(y, *ref.experts(*args, None, "silu", True, FP16), "y")
+    got = L.experts_backward(x, at.cuda(), weights.cuda(), w1, w2, dy, b1, b2, act="silu", gated=True)
+    for n, (v, bound) in ref.experts_backward(*args, _wide(dy), "silu", True, FP16).items():
+        ref.close(got[n], v, ref.rounded(v, bound, FP32) if n == "dweights" else bound, n)
+
+
+@pytest.mark.parametrize("T,E,k", [(1, 4, 3), (60, 6, 3)])
+def test_experts_large_values(L, T, E, k):
+    """fp16, hidden values up to the upper end of its range: finite, and within the bounds."""
+    gen = torch.Generator().manual_seed(T)
+    D, I = 136, 72
+    w1 = _normal(gen, E, 2 * I, D, scale=D ** -0.5, dtype=FP16)
+    x = torch.randn(T, D, generator=gen)
+    at = torch.rand(T, E, generator=gen).topk(k, dim=1).indices.int()
+    most = lambda v: max(float(ref.hidden(v.half().double(), _wide(w1[e]), None, "silu", True)[0][(at == e).any(1)].abs().max()) for e in at.unique().tolist())  # noqa: E731
+    for _ in range(4):
+        x = x * (5e4 / most(x)) ** 0.5
+    assert 4e4 < most(x) < 6e4
+    x = x.half().cuda()
+    w2 = _normal(gen, E, D, I, scale=0.1 * I ** -0.5, dtype=FP16)
+    weights = torch.ones(T, k)
+    y = L.experts(x, at.cuda(), weights.cuda(), w1, w2, act="silu", gated=True)
+    assert y.isfinite().all()
+    ref.close(y, *ref.experts(_wide(x), at, weights.double(), _wide(w1), _wide(w2), None, None, None, "silu", True, FP16), "y")
