@@ -495,7 +495,8 @@ int som_route_backward(som_layers* l, int type, int score, int64_t T, int32_t E,
  *   residual [T][D] (ldr) or NULL, y [T][D] (ldy).
  * The hidden values, times their weight, are rounded to `type` once, as operands of the second product (in fp16 a weighted hidden
  * value beyond 65504 becomes infinite); where so few tokens come that each slot reads its weights by itself (up to 16 slots, or 64
- * of as many experts) they stay in fp32 and the weight as well.  The second product's results are kept in fp32, summed in the order of j and rounded once.  1 <= E <= 1024, 1 <= k <= 32, T * k + 128 E < 2^30.
+ * of as many experts) they stay in fp32.  The second product's results are kept in fp32, summed in the order of j and rounded once.
+ * 1 <= E <= 1024, 1 <= k <= 32, T * k + 128 E < 2^30.
  */
 int som_experts(som_layers* l, int type, int act, int gated, int64_t T, int32_t E, int32_t k, int64_t D, int64_t I,
                 const void* x, int64_t ldx, const int32_t* indices, const void* weights, int weights_type, const void* w1,
@@ -505,8 +506,8 @@ int som_experts(som_layers* l, int type, int act, int gated, int64_t T, int32_t 
 /*
  * som_experts_backward - the gradient of som_experts (r's is dy itself).  Nothing of the forward call is kept: z, h and
  * W2^T dy are computed again in fp32.  dz and the weighted h are rounded to `type` as operands of the remaining products: each
- * such rounding adds its 2^-9 (bf16; fp16 2^-12, or 2^-25 absolutely below its normal range) of an operand, so that dx, dw1 and dw2
- * are off by about sqrt(2) times what their own last rounding is.
+ * such rounding is off by up to 2^-8 (bf16) or 2^-11 (fp16; 2^-25 absolutely below its normal range) of the operand, so that dx, dw1
+ * and dw2 are off by about sqrt(2) times what their own last rounding is.
  *   dy [T][D] (lddy); dx [T][D], dweights [T][k] (weights_type), dw1, dw2 and, unless NULL, db1, db2: contiguous outputs
  *   of the shapes above, all elements written (zeros for experts without a token and for an index of -1).
  */
