@@ -1,5 +1,5 @@
 """GPU tests of the dense operators at sizes that reach every tile shape of their products, with more than one tile a block: what long
-prompts, training steps and batches of single tokens run on.  Bounds as in layers_reference.py; sums are kept short, the outputs large."""
+prompts, training steps and batches of single tokens run on; and of a few rows without tiles.  Bounds as in layers_reference.py; sums are kept short, the outputs large."""
 import os
 import sys
 
@@ -29,6 +29,22 @@ def _linear_inputs(T, D, F, dtype, gated, wide):
     rows = 2 * F if gated else F
     return (_normal(gen, T, D, dtype=dtype, wide=wide), _normal(gen, rows, D, scale=D ** -0.5, dtype=dtype), _normal(gen, rows, dtype=dtype),
             _normal(gen, T, F, dtype=dtype, wide=wide))
+
+
+@pytest.mark.parametrize("T,D,F", [(T, D, F) for T in (2, 3, 4, 6, 7, 8) for D, F in ((1032, 200), (72, 4104))] + [(3, 8200, 40), (5, 6552, 24)])
+@pytest.mark.parametrize("dtype,act,gated,bias,residual,wide", [(BF16, "silu", True, True, True, 8), (FP16, "gelu", False, True, False, 0)])
+def test_linear_few_rows(L, T, D, F, dtype, act, gated, bias, residual, wide):
+    """Every number of rows that shares a read of the weights, long rows (few blocks an SM), and many outputs a warp."""
+    x, w, b, r = _linear_inputs(T, D, F, dtype, gated, wide)
+    b, r = b if bias else None, r if residual else None
+    y = L.linear(x, w, b, r, act=act, gated=gated)
+    h, eh, _, _ = ref.hidden(_wide(x), _wide(w), _wide(b), act, gated)
+    if r is not None:
+        h, eh = h + _wide(r), eh + 2.0 ** -22 * (h.abs() + _wide(r).abs())
+    ref.close(y, h, ref.rounded(h, eh, dtype), "y")
+    assert torch.equal(y, L.linear(x, w, b, r, act=act, gated=gated))
+    assert all(L.rounds("forward", t) == 0 for t in ("128x128", "128x256", "256x256"))
+    assert L.device_flags() == 0
 
 
 @pytest.mark.parametrize("dtype,act,gated,bias,residual,wide", [
