@@ -169,6 +169,30 @@ int run_split(som_layers* l, ProdMode mode, ProdArgs a, FinishArgs f, unsigned c
     return done != SOM_OK ? done : launch_finish(l, f, st);
 }
 
+// Rows so few that the CUDA cores take them, a warp an output, and not the tensor cores' tiles.  One and two rows are bound by the
+// weights' bytes, unless the rows are short and the outputs many; with more a warp's instructions count, a reduction over its
+// lanes for each row and output among them, about as much as 1024 products.  In us, k_few / tiles, bf16, `*` where tiles are taken:
+//   D -> outputs            1 row         2 rows        3 or 4          5 to 8
+//   4096 -> 4096           9.8 / 14.5   11.6 / 14.4   17.1 / 14.6 *   30.2 / 14.6 *
+//   4096 -> 8192 (gated)  14.1 / 22.5   18.0 / 22.6   25.6 / 22.7 *   47.2 / 22.2 *
+//   4096 -> 32768         45.2 / 82.5   53.1 / 70.9   79.0 / 76.5 *    152 / 68.9 *
+//   4096 -> 2048           9.5 / 14.0    9.5 / 14.2   11.0 / 14.2     18.4 / 12.7 *
+//   2048 -> 4096           9.6 / 12.0    9.7 / 12.1    9.8 / 11.9     15.1 / 11.9 *
+//   2048 -> 2048          12.2 / 18.4   11.0 / 11.9    9.6 / 11.9      9.9 / 12.0
+//   4096 -> 1024           9.6 / 12.3    9.9 / 12.1    9.7 / 12.1     11.8 / 12.1
+//   8192 -> 1024           9.6 / 12.8    9.6 / 12.9   12.8 / 12.9     36.7 / 12.8 *
+//   1392 -> 3728 (gated)   9.9 / 12.5    9.7 / 12.3    9.9 / 12.3      9.9 / 12.3 *
+//   1024 -> 16384         11.2 / 13.7   13.1 / 13.7   17.1 / 13.7 *   26.4 / 13.4 *
+//   512 -> 16384           9.7 / 9.8    11.2 / 10.0   13.8 / 10.0 *   19.1 / 9.9 *
+//   256 -> 32768          15.0 / 12.3   17.2 / 12.1 * 21.6 / 12.3 *   28.0 / 11.7 *
+//   2048 -> 256, 512 -> 512: launches alone, 9.7 / 10 to 12 at 1 to 8 rows
+bool few_rows(int64_t T, int64_t D, int64_t outputs)
+{
+    if (T > FEW_ROWS || T * D * 2 > FEW_SMEM / 2) return false;  // (the rows lie in shared memory)
+    const int64_t rows = T <= 2 ? T : T <= 4 ? 4 : FEW_ROWS;
+    return (T <= 2 && D >= 1024) || rows * outputs * (D + 1024) <= (int64_t)48 << 20;
+}
+
 }  // namespace
 }  // namespace lay
 
@@ -249,7 +273,7 @@ int som_linear(som_layers* l, int type, int act, int gated, int64_t T, int64_t D
     Guard g(l->device);
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
     const int64_t rows = gated ? 2 * F : F;
-    if (T <= FEW_ROWS && T * D * 2 <= FEW_SMEM / 2) {
+    if (few_rows(T, D, rows)) {
         FewArgs f = {};
         f.x = static_cast<const uint16_t*>(x);
         f.ldx = ldx;

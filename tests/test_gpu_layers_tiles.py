@@ -31,7 +31,7 @@ def _linear_inputs(T, D, F, dtype, gated, wide):
             _normal(gen, T, F, dtype=dtype, wide=wide))
 
 
-@pytest.mark.parametrize("T,D,F", [(T, D, F) for T in (2, 3, 4, 6, 7, 8) for D, F in ((1032, 200), (72, 4104))] + [(3, 8200, 40), (5, 6552, 24)])
+@pytest.mark.parametrize("T,D,F", [(T, D, F) for T in (2, 3, 4, 6, 7, 8) for D, F in ((1032, 200), (72, 2504))] + [(3, 8200, 40), (5, 6552, 24)])
 @pytest.mark.parametrize("dtype,act,gated,bias,residual,wide", [(BF16, "silu", True, True, True, 8), (FP16, "gelu", False, True, False, 0)])
 def test_linear_few_rows(L, T, D, F, dtype, act, gated, bias, residual, wide):
     """Every number of rows that shares a read of the weights, long rows (few blocks an SM), and many outputs a warp."""
@@ -45,6 +45,18 @@ def test_linear_few_rows(L, T, D, F, dtype, act, gated, bias, residual, wide):
     assert torch.equal(y, L.linear(x, w, b, r, act=act, gated=gated))
     assert all(L.rounds("forward", t) == 0 for t in ("128x128", "128x256", "256x256"))
     assert L.device_flags() == 0
+
+
+@pytest.mark.parametrize("T,D,F,tiles", [(2, 1032, 8200, False), (2, 520, 20000, True), (4, 2048, 4096, False), (4, 2048, 8200, True),
+                                         (8, 2048, 1024, False), (8, 2048, 4096, True), (8, 8192, 64, True)])
+def test_linear_few_rows_or_tiles(L, T, D, F, tiles):
+    """A few rows against many weights are the tiles' work (4 rows of 4096 against 8192 outputs: 26 us by rows, 23 by tiles; 8 rows 47 and
+    22), against few weights the rows'."""
+    x, w, _, _ = _linear_inputs(T, D, F, BF16, False, 0)
+    y = L.linear(x, w)
+    assert any(L.rounds("forward", t) for t in ("128x128", "128x256", "256x256")) == tiles
+    z, ez = ref.product(_wide(x), torch.zeros_like(_wide(x)), _wide(w).t(), torch.zeros_like(_wide(w).t()))
+    ref.close(y, z, ref.rounded(z, ez, BF16), "y")
 
 
 @pytest.mark.parametrize("dtype,act,gated,bias,residual,wide", [
