@@ -429,9 +429,10 @@ int som_layers_create(som_layers** out);
 int som_layers_destroy(som_layers* l); /* NULL is accepted */
 int som_layers_last_cuda_error(const som_layers* l);
 int64_t som_layers_launch_count(const som_layers* l);
-/* Which kernels the calls' matrix products took: the most tiles that one block had to walk in a launch on this handle so far (rows
- * grouped by expert: at most, the device may use fewer), 0 = never launched.  product: 0 forward, 1 dz of som_linear, 2 dz of
- * som_experts, 3 dx, 4 dw; tiles: 0 128 x 128, 1 128 x 256, 2 256 x 256 by a pair of blocks.  -1 for other values. */
+/* Which kernels the calls took: the most rounds that a block had to make in a launch on this handle so far (tiles of a matrix
+ * product, rows grouped by expert counted at their most; batches of tokens), 0 = never launched.  product: 0 forward, 1 dz of
+ * som_linear, 2 dz of som_experts, 3 dx, 4 dw, with tiles: 0 128 x 128, 1 128 x 256, 2 256 x 256 by a pair of blocks; product 5:
+ * som_route, with tiles: 0 a warp a token, 1 four lanes a token.  -1 for other values. */
 int64_t som_layers_rounds(const som_layers* l, int product, int tiles);
 /* What earlier calls skipped on the device, like som_device_flags: SOM_ERR_INVALID_ARG if an expert index outside
  * [-1, E) was met (it was treated as -1), SOM_ERR_CUDA if a wait inside a kernel ran out (the outputs of that call are

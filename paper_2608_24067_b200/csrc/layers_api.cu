@@ -243,7 +243,7 @@ int som_layers_last_cuda_error(const som_layers* l) { return l ? l->last_cuda_er
 int64_t som_layers_launch_count(const som_layers* l) { return l ? l->launches : 0; }
 int64_t som_layers_rounds(const som_layers* l, int product, int tiles)
 {
-    return l && product >= PROD_FWD && product <= PROD_DW && tiles >= NARROW && tiles <= PAIR ? l->rounds[product][tiles] : -1;
+    return l && product >= 0 && product < 6 && tiles >= 0 && tiles < 3 ? l->rounds[product][tiles] : -1;
 }
 
 int som_layers_device_flags(som_layers* l, void* stream)

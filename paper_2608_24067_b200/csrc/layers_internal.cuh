@@ -21,7 +21,7 @@ struct som_layers {
     int* flags;  // device, sticky LAY_FLAG_* bits
     int last_cuda_error;
     int64_t launches;
-    int64_t rounds[5][3];  // most tiles a block walked, by ProdMode and ProdShape
+    int64_t rounds[6][3];  // most tiles a block walked, by ProdMode and ProdShape; most rounds of som_route's two forms
     void* encode;  // cuTensorMapEncodeTiled
 };
 

@@ -557,9 +557,6 @@ __device__ __forceinline__ void merge_down(uint32_t (&a)[L], const uint32_t (&b)
             if (!(i & h)) order2(a[i], a[i + h]);
 }
 
-// Tokens from which on k_route_many is used.  256 experts, 8 chosen, without / with groups: 14.4 / 22.6 us at 4096 and at 8192
-// tokens (one pass of long latency), 18.5 / 25 at 16384; k_route 12.3 / 14.4, 16.4 / 20.5 and 22.6 / 28.6.
-constexpr int ROUTE_MANY = 8192;
 constexpr int QUAD_WARPS = 8, QUAD_ROWS = 8 * QUAD_WARPS;
 
 template <int TYPE, int L>
@@ -971,6 +968,40 @@ struct RouteGrad {
     }
 };
 
+// Tokens from which on four lanes a token (k_route_many) are faster than a warp a token (k_route).  k_route_many takes one pass of
+// long latency, the longer the more it walks a row (groups: twice), k_route time by tokens x experts.  8 chosen, fp32, k_route_many
+// / k_route in us (`*` where k_route_many is taken; calls of up to about 15 us are the host's):
+//   experts, keys            6000 tokens      8192            12288           16384           32768
+//   64, logits               15 / 15          15 / 15 *       15 / 15 *       15 / 17 *       19 / 25 *
+//   128, sigmoid             16 / 16          16 / 16 *       16 / 17 *       17 / 19 *       26 / 29 *
+//   128, sigmoid, groups     17 / 16          17 / 16         19 / 19         19 / 22 *       31 / 36 *
+//   256, logits              17 / 15          17 / 17 *       19 / 21 *       20 / 23 *       32 / 34 *
+//   256, sigmoid             19 / 17          19 / 20 *       22 / 23 *       23 / 25 *       37 / 40 *
+//   256, sigmoid, groups     23 / 19          23 / 22         27 / 25         27 / 29 *       46 / 48 *
+//   384, sigmoid             24 / 27          24 / 34 *       29 / 42 *       29 / 51 *       50 / 89 *
+//   512, sigmoid, groups     35 / 31          35 / 37 *       41 / 48 *       41 / 58 *       78 / 103 *
+//   1024, sigmoid            48 / 65          48 / 80 *       57 / 108 *      58 / 139 *      123 / 260 *
+//   1024, sigmoid, groups    62 / 70          62 / 85 *       72 / 115 *      71 / 150 *      155 / 281 *
+// Softmax scores with a bias or groups by two walk a row up to four times, and near ties of them take all exact keys of a token,
+// which is the whole warp's work in either form:
+//   64                       16 / 16          16 / 16         18 / 19         17 / 21 *       27 / 33 *
+//   256                      40 / 25          40 / 27         44 / 32         44 / 41         67 / 65
+//   256, groups              41 / 29          54 / 33         57 / 39         58 / 54         81 / 70
+//   512                      54 / 61          69 / 66         66 / 77         82 / 88 *       126 / 148 *
+//   512, groups              90 / 57          91 / 81         91 / 91         104 / 108 *     158 / 163 *
+//   1024, groups             138 / 123        180 / 179       192 / 222       193 / 245 *     355 / 435 *
+// (256 experts, 65536 tokens: 111 / 104, with groups 141 / 125.)
+bool takes_many(int64_t T, int E, bool by_groups, bool softmax_keys)
+{
+    if (softmax_keys) return T >= 16384 && (E <= 128 || E >= 512);
+    return T >= (by_groups && E <= 256 ? 16384 : 8192);
+}
+
+void note_rounds(som_layers* l, int form, int64_t rounds)
+{
+    if (rounds > l->rounds[5][form]) l->rounds[5][form] = rounds;
+}
+
 // What a warp sets up (biases, groups, the block's counts) is shared by its tokens: no more blocks than are resident.
 int route_grid(const som_layers* l, int64_t T, int per_sm)
 {
@@ -1003,14 +1034,18 @@ int launch_route(som_layers* l, int type, int score, int64_t T, int E, int k, co
         const RouteArgs a{logits, ld, T, bias, weights, indices, counts, E, k, score, groups, top_groups, group_best, renorm, scale};
         const size_t smem = counts ? (size_t)E * sizeof(int) : 0;
         const bool by_groups = groups > 1 && top_groups < groups;
-        // Four lanes a token from ROUTE_MANY tokens on, where they fill the SMs.  Not where pieces of 32 experts span groups, and
-        // not where scores of 16-bit logits without a bias decide: equal logits are common there, and only the other form
-        // settles them without exact keys.
-        if (T >= ROUTE_MANY && k <= 16 && (!by_groups || E / groups % 32 == 0) && (type == SOM_F32 || bias || groups == 1 || group_best == 1)) {
+        const bool by_score = bias || (groups > 1 && group_best == 2);
+        // Not four lanes a token where pieces of 32 experts span groups, and not where scores of 16-bit logits without a bias decide: equal
+        // logits are common there, and only the other form settles them without exact keys.
+        if (takes_many(T, E, by_groups, by_score && score == SOM_SCORE_SOFTMAX) && k <= 16 && (!by_groups || E / groups % 32 == 0) &&
+            (type == SOM_F32 || bias || !by_score)) {
+            // (two blocks an SM are resident; with four an SM the last ones even out: 65536 tokens x 256 experts 60 us, 63 with two)
             const int64_t want = (T + QUAD_ROWS - 1) / QUAD_ROWS, most = (int64_t)l->sm_count * 4;
             const int blocks = (int)(want < most ? want : most);
+            note_rounds(l, 1, (want + blocks - 1) / blocks);
             e = type == SOM_F32 ? route_many<SOM_F32>(l, a, blocks, smem, st) : type == SOM_F16 ? route_many<SOM_F16>(l, a, blocks, smem, st) : route_many<SOM_BF16>(l, a, blocks, smem, st);
         } else {
+            note_rounds(l, 0, ((T + ROUTE_WARPS - 1) / ROUTE_WARPS + grid - 1) / grid);
             e = by_type<Route>(l, type, E, a, grid, smem, st);
         }
     }

@@ -18,8 +18,8 @@ _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 _TYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
 _ACTS = {"none": 0, "relu": 1, "gelu": 2, "silu": 3}
 _SCORES = {"softmax": 0, "sigmoid": 1}
-_PRODUCTS = {"forward": 0, "dz": 1, "dz of experts": 2, "dx": 3, "dw": 4}
-_TILES = {"128x128": 0, "128x256": 1, "256x256": 2}
+_PRODUCTS = {"forward": 0, "dz": 1, "dz of experts": 2, "dx": 3, "dw": 4, "route": 5}
+_TILES = {"128x128": 0, "128x256": 1, "256x256": 2, "warp a token": 0, "four lanes a token": 1}
 
 
 def _elsewhere(t, index, name):
@@ -267,7 +267,7 @@ class Layers:
         return int(self._lib.som_layers_launch_count(self._h))
 
     def rounds(self, product, tiles) -> int:
-        """som_layers_rounds: the most tiles of this size that a block walked for this product so far, 0 = none."""
+        """som_layers_rounds: the most rounds of this form that a block made for this product (or "route") so far, 0 = none."""
         return int(self._lib.som_layers_rounds(self._h, _code(_PRODUCTS, product, "product"), _code(_TILES, tiles, "tiles")))
 
     def destroy(self):

@@ -8,7 +8,7 @@ import torch
 
 sys.path.insert(0, os.path.dirname(os.path.abspath(__file__)))
 import layers_reference as ref  # noqa: E402
-from test_gpu_layers import _expert_inputs, _linear_grad, _normal, _wide  # noqa: E402
+from test_gpu_layers import _expert_inputs, _linear_grad, _normal, _route, _wide  # noqa: E402
 
 pytestmark = pytest.mark.gpu
 
@@ -129,3 +129,38 @@ def test_experts_backward_tiles(L, tiles, T, E, k, D, I, dtype, act, gated, bias
     again = L.experts_backward(s["x"], s["indices"], s["weights"], s["w1"], s["w2"], dy, s["b1"], s["b2"], act=act, gated=gated)
     assert all(torch.equal(got[n], again[n]) for n in got)
     assert L.device_flags() == 0
+
+
+@pytest.mark.parametrize("T,E,k,opt,form", [
+    (16400, 256, 8, dict(score="sigmoid", bias=True, groups=8, top_groups=4, group_best=2), "four lanes a token"),
+    (16400, 128, 12, dict(score="sigmoid", renorm=False, bias=True, groups=4, top_groups=1, group_best=1), "four lanes a token"),
+    (16400, 96, 5, dict(score="softmax", bias=True), "four lanes a token"),
+    (16400, 64, 16, dict(score="softmax", bias=True, groups=2, top_groups=1, group_best=2, scale=2.5), "four lanes a token"),
+    (16400, 512, 8, dict(score="softmax", renorm=False, bias=True, groups=8, top_groups=3, group_best=2), "four lanes a token"),
+    (16400, 256, 8, dict(score="softmax", bias=True, groups=8, top_groups=4, group_best=2), "warp a token"),
+    (8200, 512, 8, dict(score="sigmoid", bias=True, groups=16, top_groups=4, group_best=2), "four lanes a token"),
+    (8200, 256, 8, dict(score="sigmoid", bias=True, groups=8, top_groups=4, group_best=2), "warp a token"),
+    (8200, 200, 7, dict(score="softmax", renorm=False), "four lanes a token"),
+    (8191, 200, 7, dict(score="softmax", renorm=False), "warp a token")])
+@pytest.mark.parametrize("dtype,kind", [(FP32, "normal"), (BF16, "masked"), (FP32, "contested")])
+def test_route_forms(L, T, E, k, opt, form, dtype, kind):
+    """Both forms of the routing kernel on either side of the rule between them."""
+    gen = torch.Generator().manual_seed(T + E)
+    z = torch.randn(T, E, generator=gen) * 2
+    bias = torch.randn(E, generator=gen) * 0.1 if opt.get("bias") else None
+    if kind == "masked":
+        z[torch.rand(z.shape, generator=gen) < 0.3] = -float("inf")
+        z[::7] = -float("inf")
+    if kind == "contested":
+        z = z.round() / 2 + torch.randn(T, E, generator=gen) * 2.0 ** -20
+        bias = None if bias is None else (bias * 32).round() / 32
+    logits, opt = z.to(dtype).cuda(), {"renorm": True, **opt}
+    got = L.route(logits, k, bias=None if bias is None else bias.cuda(), **{n: v for n, v in opt.items() if n != "bias"})
+    assert L.rounds("route", form) >= 1 and sum(L.rounds("route", f) > 0 for f in ("warp a token", "four lanes a token")) == 1
+    some = torch.arange(3, T, 83)
+    _, (w, want, _, _) = _route(logits[some], k, opt, bias)
+    assert torch.equal(got["indices"][some].cpu().long(), want)
+    # exponentials, a sum of up to E of them and two divisions in fp32: (E + 16) half units
+    assert ((got["weights"][some].double().cpu() - w).abs() <= (E + 16) * 2.0 ** -24 * w.abs() + 1e-37).all()
+    at = got["indices"].long()
+    assert torch.equal(got["counts"].long(), torch.bincount(at[at >= 0], minlength=E))
