@@ -20,20 +20,6 @@ constexpr int FEW_WARPS = 8, FEW_THREADS = 32 * FEW_WARPS;
 __host__ __device__ constexpr int few_resident(int rows) { return rows <= 2 ? 3 : 2; }  // by its registers
 constexpr int DOWN_WARPS = 24, DOWN_THREADS = 32 * DOWN_WARPS;  // k_few_down: one block an SM shares the token's hidden values
 
-// v[8] of an fp32 or 16-bit row in shared memory
-__device__ __forceinline__ void smem8(const uint16_t* p, float (&v)[8], int bf16)
-{
-    const uint4 w = *reinterpret_cast<const uint4*>(p);
-    const float2 a = unpack2(w.x, bf16), b = unpack2(w.y, bf16), c = unpack2(w.z, bf16), d = unpack2(w.w, bf16);
-    v[0] = a.x, v[1] = a.y, v[2] = b.x, v[3] = b.y, v[4] = c.x, v[5] = c.y, v[6] = d.x, v[7] = d.y;
-}
-
-__device__ __forceinline__ void widen8(const uint4& w, float (&v)[8], int bf16)
-{
-    const float2 a = unpack2(w.x, bf16), b = unpack2(w.y, bf16), c = unpack2(w.z, bf16), d = unpack2(w.w, bf16);
-    v[0] = a.x, v[1] = a.y, v[2] = b.x, v[3] = b.y, v[4] = c.x, v[5] = c.y, v[6] = d.x, v[7] = d.y;
-}
-
 // weights are read once: past L1
 __device__ __forceinline__ uint4 stream16(const uint16_t* p)
 {
@@ -116,7 +102,7 @@ __global__ void __launch_bounds__(FEW_THREADS, few_resident(ROWS)) k_few(const F
 #pragma unroll
                     for (int r = 0; r < ROWS; ++r) {
                         float xv[8];
-                        smem8(xs + (size_t)r * a.D + c, xv, a.bf16);
+                        load8(xs + (size_t)r * a.D + c, xv, a.bf16);
 #pragma unroll
                         for (int h = 0; h < HALVES; ++h)
 #pragma unroll

@@ -32,12 +32,18 @@ __device__ __forceinline__ float unpack1(uint16_t v, int bf16)
     return __half2float(*reinterpret_cast<const __half*>(&v));
 }
 
-// eight consecutive 16-bit values, 16-byte aligned
-__device__ __forceinline__ void load8(const uint16_t* p, float (&v)[8], int bf16)
+// eight 16-bit values of a 16-byte word -> fp32
+__device__ __forceinline__ void widen8(const uint4& w, float (&v)[8], int bf16)
 {
-    const uint4 w = *(reinterpret_cast<const uint4*>(p));
     const float2 a = unpack2(w.x, bf16), b = unpack2(w.y, bf16), c = unpack2(w.z, bf16), d = unpack2(w.w, bf16);
     v[0] = a.x, v[1] = a.y, v[2] = b.x, v[3] = b.y, v[4] = c.x, v[5] = c.y, v[6] = d.x, v[7] = d.y;
+}
+
+// the same from memory, 16-byte aligned
+__device__ __forceinline__ void load8(const uint16_t* p, float (&v)[8], int bf16)
+{
+    const uint4 w = *reinterpret_cast<const uint4*>(p);
+    widen8(w, v, bf16);
 }
 
 // one instruction each, subnormal results flushed to zero: 2^x off by 2 units, 1 / x by 1 unit in the last place

@@ -172,15 +172,7 @@ struct RowPart {
     __device__ __forceinline__ void get(float (&v)[N]) const
     {
 #pragma unroll
-        for (int j = 0; j < N / 8; ++j) {
-            const uint32_t u[4] = {w[j].x, w[j].y, w[j].z, w[j].w};
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float2 f = unpack2(u[i], BF16);
-                v[8 * j + 2 * i] = f.x;
-                v[8 * j + 2 * i + 1] = f.y;
-            }
-        }
+        for (int j = 0; j < N / 8; ++j) widen8(w[j], reinterpret_cast<float(&)[8]>(v[8 * j]), BF16);
     }
     template <bool BF16>
     __device__ __forceinline__ void add(float (&v)[N]) const
