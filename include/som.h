@@ -413,7 +413,8 @@ int som_set_option(som_handle* h, int key, int64_t value);
  *     matrix starts on a 16-byte boundary and its ld, D, F and I are multiples of 8 (else SOM_ERR_UNSUPPORTED); weights
  *     and the gradients written are contiguous.
  *   - Calls only enqueue work on `stream`, except that the handle's workspace grows (with a device synchronisation) when
- *     a call needs more than any before.  Calls on one handle must not overlap on the GPU.  Outputs must not overlap inputs.
+ *     a call needs more than any before.  Calls on one handle must not overlap on the GPU, and one host thread at a time uses
+ *     it.  Outputs must not overlap inputs.
  *   - Calls can be captured into a CUDA graph once the workspace is large enough (after a call of the same sizes).  A graph keeps the
  *     workspace's address: no call on the handle may need a larger one while the graph is in use.
  *   - Results are bit-identical from run to run for the same inputs.

@@ -536,13 +536,18 @@ static SlotPlan carve_plan(Carver& c, int64_t T, int E, int k, int tile)
 static bool few_slots(int64_t T, int E, int k) { return T * k <= 16 || (T * k <= 64 && T * k <= E); }
 
 // Rows of an expert's tiles: a pair's once the experts have rows enough; with fewer, a pair would mostly multiply padding, and
-// the weights' bytes bound the product, not the tensor cores.  In us, single blocks / pairs, gated, D 2048 and I 1024 unless said:
-//   rows an expert                  64           128          192          256          512
-//   64 experts                   189 / 222    254 / 263    308 / 305    357 / 359    620 / 602
-//   12 experts (1000, 712)        39 / 39      43 / 45      51 / 48      57 / 50      80 / 68
-//   64 experts, gradient         507 / 585    654 / 683    792 / 812    938 / 947   1533 / 1508
-//   16 experts, gradient         144 / 163    192 / 186    216 / 231    272 / 258    406 / 410
-//   12 experts, gradient          77 / 69      79 / 86      94 / 93     114 / 101    171 / 156
+// the weights' bytes bound the product, not the tensor cores.  Where the two meet depends on how the experts' rows fall into tiles, so
+// no one number is right everywhere: 256 is within 15 % of the better shape in all of these.  In us, single blocks / pairs, D 2048
+// and I 1024, gated, unless said:
+//   rows an expert                  64           128          192          256          384          512
+//   64 experts                   181 / 202    219 / 219    268 / 278    315 / 337    438 / 448    552 / 540
+//   16 experts                    68 / 80      90 / 84      94 / 105    113 / 102    139 / 127    143 / 146
+//   8 experts (1024, 2048)        49 / 55      58 / 58      60 / 66      78 / 68      83 / 71      86 / 89
+//   12 experts (1000, 712)        44 / 43      48 / 55      66 / 58      70 / 67      84 / 74      91 / 75
+//   64 experts, gradient         496 / 557    602 / 641    737 / 792    869 / 911   1079 / 1068  1432 / 1362
+//   32 experts (1024, 512), grad. 90 / 103    116 / 111    128 / 141    158 / 151    178 / 186    228 / 242
+//   16 experts, gradient         138 / 155    175 / 162    189 / 214    243 / 225    273 / 313    355 / 386
+//   12 experts (1000, 712), grad. 73 / 68      84 / 86      90 / 94     113 / 99     130 / 131    163 / 145
 static int tile_rows(int64_t T, int E, int k) { return T * k >= (int64_t)256 * E ? shape_rows(PAIR) : shape_rows(WIDE); }
 
 // A product over the slots' rows.  Single blocks are wide where that leaves a tile for every SM, by the tiles to expect.

@@ -160,7 +160,8 @@ __global__ void __launch_bounds__(FEW_THREADS, few_resident(ROWS)) k_few(const F
 
 // y[t][d] = residual + sum_j (<w2[e_j][d], hidden[t, j]> + weight_j b2[e_j][d]); `share` warps of the block share an output,
 // each a part of the k * I products.  Blocks stay, as above: the token's hidden values are brought in once a block.  The
-// first weights are read while the kernel before, which writes the hidden values, still runs.
+// first weights are read before the kernel in front, which writes the hidden values, is waited for.  (What that overlaps is its end: a
+// block here takes 768 x 72 registers, and comes in on an SM when k_few's blocks there, 61440 registers together, have left.)
 __global__ void __launch_bounds__(DOWN_THREADS, 1) k_few_down(const FewDownArgs a)
 {
     extern __shared__ __align__(16) float hs[];  // [k][2][I / 2]: of every eight values the first four, then the other four

@@ -110,8 +110,8 @@ __device__ __forceinline__ Tile tile_at(const ProdArgs& p, int idx, int width, i
 }
 
 // Ways out of the epilogue.  Staged: 32 rows (lane l holds row l) of 64 16-bit or 32 fp32 columns go through shared memory
-// (128-byte rows, 128-byte swizzle) to a TMA store, which leaves out what lies outside the tensor.  Direct: a lane writes its 16
-// columns.  Direct stores take the load/store pipe 32 cycles an instruction: too much where a tile's products are short
+// (128-byte rows, 128-byte swizzle) to a TMA store, which leaves out what lies outside the tensor.  Direct: a lane writes 8
+// columns at a time.  Direct stores take the load/store pipe 32 cycles an instruction: too much where a tile's products are short
 // (PROD_DW at 512 rows an expert: 134 us staged, 178 us direct), but no waits, and no shared memory for up to three outputs
 // at once (PROD_DZ, PROD_DZ_TWO).
 template <int BUFFERS>

@@ -536,8 +536,9 @@ __global__ void __launch_bounds__(32 * ROUTE_WARPS, V <= 8 ? 4 : 2) k_route(cons
 // keys, and contested places by the exact keys of the list, one candidate a lane.  Only where the contest reaches beyond the
 // list, or scores need a sum over all experts, are all keys of the token computed exactly.
 //
-// 16384 tokens x 256 experts, 8 of 4 of 8 groups, bias: 25 us (0.7 TB/s).  10.8 million warp instructions, issued in 41 % of the
-// cycles: latency of the sorting networks with 14 warps an SM, whose lists fill the registers.
+// 16384 tokens x 256 experts, 8 of 4 of 8 groups, bias: 27 us (0.7 TB/s).  Latency of the sorting networks, the grid leaving too few
+// warps to cover it: 2048 warps are 256 blocks on 148 SMs, one on some and two on the others (two are resident by their registers),
+// which issue in 20 and 39 % of the cycles; and with groups a row is walked, and the kept experts' scores are computed, twice.
 
 // a (descending) becomes the L largest of a and b (descending), descending; rest >= rest2: the largest of those left out
 template <int L>
@@ -849,7 +850,8 @@ __device__ __forceinline__ void put_logit(void* p, int64_t i, float v)
 
 // ds = scale dw for the chosen, 0 for others; renormalised: scale (dw - sum of w dw) / (sum of the chosen s).  dlogit = s (1 - s) ds for
 // the sigmoid, s (ds - sum of s ds) for the softmax.  Lane j holds choice j.  The row is written as if nothing had been chosen, then
-// the chosen elements are written over it.  16381 tokens x 100 bf16 logits: 7.3 MB in 9.5 us a call, of which the launch is most.
+// the chosen elements are written over it.  16381 tokens x 100 bf16 logits: 7.3 MB, 9.0 us a call on the device (calls one after
+// the other in a graph; the host's call takes about as long).  Bound by instructions: issued in 75 % of the cycles that an SM is busy.
 template <int TYPE, int V>
 __global__ void __launch_bounds__(32 * ROUTE_WARPS) k_route_backward(const RouteGradArgs a)
 {

@@ -3,6 +3,10 @@ the experts' products, and their gradients.
 
 Argument marshalling only, like ``som``: the library computes, PyTorch supplies memory and streams, and there is no
 fallback.  Matrices are 2-d CUDA tensors whose rows are contiguous (``stride(1) == 1``); rows may lie further apart.
+
+The calls leave no autograd history, also where their inputs require a gradient: what they return is detached, and the gradients
+come from the ``*_backward`` calls (``examples/experts_on_map.py`` chains them; an ``autograd.Function`` around a pair of calls makes
+them part of a graph).
 """
 from __future__ import annotations
 
@@ -66,7 +70,8 @@ def _code(table, key, name):
 class Layers:
     """Handle of the dense operators on one device (``som_layers_create``): workspace and status.
 
-    Calls on one handle must not overlap on the GPU: issue them on one stream or order the streams.  Calls run on the current
+    Calls on one handle must not overlap, neither on the GPU (issue them on one stream or order the streams) nor on the host: one
+    thread at a time, as a call may grow the workspace.  Calls run on the current
     stream, or on ``stream``: the caller orders that stream behind what writes the inputs, and what reads the outputs behind it."""
 
     def __init__(self, device=None):
