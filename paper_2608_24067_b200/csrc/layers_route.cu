@@ -51,6 +51,21 @@ __device__ __forceinline__ double warp_sum(double v)
 __device__ __forceinline__ float exp_from(float x, float top) { return x == top ? 1.f : expf(x - top); }
 
 
+// Sigmoid scores below LOW_LOGIT leave fp32's range, but where they are renormalised only their ratios count: sigmoid(x) as a multiple
+// of exp(most), most <= 0 the largest chosen logit or 0.  (All below -700: scores of 0 in 64 bits as well, and so weights of 0.)
+constexpr float LOW_LOGIT = -80.f;
+__device__ __forceinline__ float sigmoid_from(float x, float most)
+{
+    return most < -700.f ? 0.f : expf(fminf(x, 0.f) - most) / (1.f + expf(-fabsf(x)));
+}
+
+__device__ __forceinline__ float warp_max(float v)
+{
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) v = fmaxf(v, __shfl_xor_sync(ALL, v, d));
+    return v;
+}
+
 struct RouteArgs {
     const void* logits;
     int64_t ld, T;
@@ -498,11 +513,13 @@ __global__ void __launch_bounds__(32 * ROUTE_WARPS, V <= 8 ? 4 : 2) k_route(cons
         const float xj = at >= 0 ? logit_at<TYPE>(a.logits, row + at) : -INFINITY;
         if (a.score == SOM_SCORE_SIGMOID) {
             if (at >= 0) s = 1.f / (1.f + expf(-xj));
+            if (a.renorm && __any_sync(ALL, at >= 0 && xj < LOW_LOGIT)) {
+                const float m = fminf(warp_max(xj), 0.f);
+                if (at >= 0) s = sigmoid_from(xj, m);
+            }
         } else if (a.renorm) {
             // only ratios of the chosen experts' scores count: taken from the largest of them
-            float m = xj;
-#pragma unroll
-            for (int d = 16; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor_sync(ALL, m, d));
+            const float m = warp_max(xj);
             if (at >= 0 && (m == top || top < INFINITY)) s = exp_from(xj, m);  // (beside an infinite logit all others score 0)
         } else if (at >= 0) {
             s = exp_from(xj, top) / total;
@@ -785,7 +802,7 @@ __global__ void __launch_bounds__(32 * QUAD_WARPS) k_route_many(const RouteArgs 
             }
         }
         // lane `part` writes choices part, part + 4, ...
-        float s[L / 4], x[L / 4], most = -INFINITY;
+        float s[L / 4], x[L / 4], most = -INFINITY, least = INFINITY;
         int mine[L / 4];
 #pragma unroll
         for (int i = 0; i < L; ++i)
@@ -794,15 +811,19 @@ __global__ void __launch_bounds__(32 * QUAD_WARPS) k_route_many(const RouteArgs 
         for (int i = 0; i < L / 4; ++i) {
             x[i] = mine[i] >= 0 ? logit_at<TYPE>(a.logits, row + mine[i]) : -INFINITY;
             most = fmaxf(most, x[i]);
+            if (mine[i] >= 0) least = fminf(least, x[i]);
         }
-        most = fmaxf(most, __shfl_xor_sync(ALL, most, 1));
-        most = fmaxf(most, __shfl_xor_sync(ALL, most, 2));
+#pragma unroll
+        for (int d = 1; d <= 2; d <<= 1) {
+            most = fmaxf(most, __shfl_xor_sync(ALL, most, d));
+            least = fminf(least, __shfl_xor_sync(ALL, least, d));
+        }
         float sum = 0.f;
 #pragma unroll
         for (int i = 0; i < L / 4; ++i) {
             s[i] = 0.f;
             if (mine[i] >= 0) {
-                if (a.score == SOM_SCORE_SIGMOID) s[i] = 1.f / (1.f + expf(-x[i]));
+                if (a.score == SOM_SCORE_SIGMOID) s[i] = a.renorm && least < LOW_LOGIT ? sigmoid_from(x[i], fminf(most, 0.f)) : 1.f / (1.f + expf(-x[i]));
                 else if (!a.renorm) s[i] = exp_from(x[i], top) / total;
                 else if (most == top || top < INFINITY) s[i] = exp_from(x[i], most);  // only ratios count
             }
@@ -900,14 +921,16 @@ __global__ void __launch_bounds__(32 * ROUTE_WARPS) k_route_backward(const Route
                 if (i < a.E) put_logit<TYPE>(a.dlogits, out + i, x[v] > 0.f ? -(x[v] * inv) * dot : 0.f);
             }
         } else {
-            float q = 0.f, top = 0.f;
+            float q = 0.f;  // (renormalised: any multiple of the scores will do)
             if (a.score == SOM_SCORE_SOFTMAX) {
-                top = xj;
-#pragma unroll
-                for (int m = 16; m > 0; m >>= 1) top = fmaxf(top, __shfl_xor_sync(ALL, top, m));
+                const float top = warp_max(xj);
                 if (live) q = exp_from(xj, top);
-            } else if (live) {
-                q = 1.f / (1.f + expf(-xj));
+            } else {
+                if (live) q = 1.f / (1.f + expf(-xj));
+                if (a.renorm && __any_sync(ALL, live && xj < LOW_LOGIT)) {
+                    const float m = fminf(warp_max(xj), 0.f);
+                    if (live) q = sigmoid_from(xj, m);
+                }
             }
             float e = d;
             if (a.renorm) {

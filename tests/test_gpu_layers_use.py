@@ -194,3 +194,30 @@ def test_experts_large_values(L, T, E, k):
     y = L.experts(x, at.cuda(), weights.cuda(), w1, w2, act="silu", gated=True)
     assert y.isfinite().all()
     ref.close(y, *ref.experts(_wide(x), at, weights.double(), _wide(w1), _wide(w2), None, None, None, "silu", True, FP16), "y")
+
+
+@pytest.mark.parametrize("T", [40, 16400])
+@pytest.mark.parametrize("base", [-60.0, -82.0, -87.0, -88.5, -95.0, -104.0, -200.0, -600.0])
+@pytest.mark.parametrize("k", [1, 6])
+def test_sigmoid_scores_below_fp32(L, T, base, k):
+    """Renormalised sigmoid scores of logits far below zero: the ratios count, also where the scores themselves are below fp32's range.
+    Exponents of up to 16 apart, rounded to fp32, are off by 16 half units, and the exponentials, sums and divisions by up to 64 more."""
+    gen = torch.Generator().manual_seed(3)
+    E = 64
+    z = (base + torch.randn(T, E, generator=gen) * 2).float()
+    z[::5, :3] += 70  # rows with a few scores in range
+    got = L.route(z.cuda(), k, score="sigmoid", renorm=True)
+    some = torch.arange(0, T, 1 + T // 97)
+    at = got["indices"][some].cpu().long()
+    x = z[some].double().requires_grad_()
+    assert torch.equal(at, x.detach().topk(k, dim=1).indices)
+    # sigmoid(x) = exp(x) / (1 + exp(x)), in logarithms
+    w = torch.softmax(torch.nn.functional.logsigmoid(x).gather(1, at), 1)
+    assert ((got["weights"][some].double().cpu() - w).abs() <= 80 * 2.0 ** -24 * w).all()
+    dw = torch.randn(T, k, generator=gen)
+    (w * dw[some].double()).sum().backward()
+    dz = L.route_backward(z.cuda(), got["indices"], dw.cuda(), score="sigmoid", renorm=True)[some].double().cpu()
+    # w (1 - s) (dw - mean): of each factor as above, relative to the largest difference
+    spread = (dw[some].double().abs().max(1, keepdim=True).values * 2).expand(-1, E)
+    size = torch.zeros_like(dz).scatter_(1, at, w.detach())
+    assert ((dz - x.grad).abs() <= 256 * 2.0 ** -24 * size * spread).all()
