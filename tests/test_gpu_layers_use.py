@@ -221,3 +221,27 @@ def test_sigmoid_scores_below_fp32(L, T, base, k):
     spread = (dw[some].double().abs().max(1, keepdim=True).values * 2).expand(-1, E)
     size = torch.zeros_like(dz).scatter_(1, at, w.detach())
     assert ((dz - x.grad).abs() <= 256 * 2.0 ** -24 * size * spread).all()
+
+
+def test_workspace_that_cannot_be_had(L):
+    """A call whose workspace does not fit the card (4.2 million rows of 8192 in fp32 and 16 bits: 206 GB) says so; neither the handle nor
+    what else runs in the process is affected."""
+    from paper_2608_24067_b200.som import SomError
+    gen = torch.Generator().manual_seed(2)
+    x, w = _normal(gen, 100, 256, dtype=BF16), _normal(gen, 512, 256, dtype=BF16)
+    want = L.linear(x, w, act="gelu")
+    T, E, k, D, I = 1 << 17, 32, 32, 8192, 8
+    assert T * k * D * 6 > torch.cuda.get_device_properties(0).total_memory
+    args = (torch.zeros(T, D, dtype=BF16, device="cuda"), torch.zeros(T, k, dtype=torch.int32, device="cuda"), torch.zeros(T, k, device="cuda"),
+            torch.zeros(E, 2 * I, D, dtype=BF16, device="cuda"), torch.zeros(E, D, I, dtype=BF16, device="cuda"))
+    with pytest.raises(SomError) as e:
+        L.experts(*args)
+    assert e.value.status == 4 and e.value.cuda_error == 2  # out of memory
+    del args, e
+    torch.cuda.empty_cache()
+    assert float((torch.ones(8, device="cuda") + 1).sum()) == 16  # (a check of the last CUDA error comes with every launch)
+    torch.cuda.synchronize()
+    assert torch.equal(L.linear(x, w, act="gelu"), want)
+    s = torch.rand(40, 8, generator=gen).topk(4, dim=1)
+    y = L.experts(_normal(gen, 40, 64, dtype=BF16), s.indices.int().cuda(), s.values.cuda(), _normal(gen, 8, 64, 64, dtype=BF16), _normal(gen, 8, 64, 32, dtype=BF16))
+    assert y.isfinite().all() and L.device_flags() == 0
