@@ -473,8 +473,9 @@ int som_linear_backward(som_layers* l, int type, int act, int gated, int64_t T, 
  *   choice   the k largest keys, best first; ties go to the lowest index, among groups too.
  *   indices  int32 [T][k], -1 where fewer than k experts are left (unmasked, on, and in the groups kept).
  *   weights  fp32 [T][k]: scale * s of the chosen experts, divided by their sum if renorm, and 0 beside an index of -1.  With renorm
- *            only the scores' ratios count, also where the scores themselves are below fp32's range (sigmoid: 0 where all chosen
- *            logits are below -700; an infinite logit that is not chosen: 0).  The bias does not enter the weights.
+ *            only the scores' ratios count, also where the scores themselves are below fp32's range; where all of them are below
+ *            exp(-700) (softmax: of the row's largest, as that of a mask by the type's lowest value) the weights are 0.  The bias does not
+ *            enter the weights.
  *   counts   int32 [E] or NULL: tokens that chose each expert (the bias for balance is moved by them).
  * 1 <= E <= 1024, 1 <= k <= min(32, E), 1 <= top_groups <= groups <= 32.
  */

@@ -51,12 +51,17 @@ __device__ __forceinline__ double warp_sum(double v)
 __device__ __forceinline__ float exp_from(float x, float top) { return x == top ? 1.f : expf(x - top); }
 
 
-// Sigmoid scores below LOW_LOGIT leave fp32's range, but where they are renormalised only their ratios count: sigmoid(x) as a multiple
-// of exp(most), most <= 0 the largest chosen logit or 0.  (All below -700: scores of 0 in 64 bits as well, and so weights of 0.)
+// Where scores are renormalised only the chosen ones' ratios count, also where the scores themselves are below fp32's range; but
+// scores that are 0 in 64 bits as well (a logit of the type's lowest value as a mask, chosen for its bias) weigh 0: those below
+// exp(NO_SCORE), against the row's largest logit for the softmax.
+constexpr float NO_SCORE = -700.f;
+__device__ __forceinline__ bool scores_at(float most, float top) { return most == top || most > top + NO_SCORE; }
+
+// sigmoid(x) as a multiple of exp(most), most <= 0 the largest chosen logit or 0; needed from LOW_LOGIT down
 constexpr float LOW_LOGIT = -80.f;
 __device__ __forceinline__ float sigmoid_from(float x, float most)
 {
-    return most < -700.f ? 0.f : expf(fminf(x, 0.f) - most) / (1.f + expf(-fabsf(x)));
+    return most < NO_SCORE ? 0.f : expf(fminf(x, 0.f) - most) / (1.f + expf(-fabsf(x)));
 }
 
 __device__ __forceinline__ float warp_max(float v)
@@ -520,7 +525,7 @@ __global__ void __launch_bounds__(32 * ROUTE_WARPS, V <= 8 ? 4 : 2) k_route(cons
         } else if (a.renorm) {
             // only ratios of the chosen experts' scores count: taken from the largest of them
             const float m = warp_max(xj);
-            if (at >= 0 && (m == top || top < INFINITY)) s = exp_from(xj, m);  // (beside an infinite logit all others score 0)
+            if (at >= 0 && scores_at(m, top)) s = exp_from(xj, m);  // (beside an infinite logit all others score 0)
         } else if (at >= 0) {
             s = exp_from(xj, top) / total;
         }
@@ -606,11 +611,13 @@ __global__ void __launch_bounds__(32 * QUAD_WARPS) k_route_many(const RouteArgs 
     }
     const float ceiling = pack.ceiling, scale = pack.scale;
     const uint32_t margin = pack.margin;
+    // whether the row's largest logit has to be found first (where not, the largest chosen one is that)
+    const bool has_top = a.score == SOM_SCORE_SOFTMAX ? by_score || !a.renorm || !exact16 || by_groups : !by_score && !exact16;
 
     for (int64_t t0 = ((int64_t)blockIdx.x * QUAD_WARPS + warp) * 8; t0 < a.T; t0 += (int64_t)gridDim.x * QUAD_ROWS) {
         const int64_t t = t0 + quad < a.T ? t0 + quad : a.T - 1, row = t * a.ld;  // (past the end: the last row again, not written)
         float top = 0.f, total = 1.f;
-        if (a.score == SOM_SCORE_SOFTMAX ? by_score || !a.renorm || !exact16 || by_groups : !by_score && !exact16) {
+        if (has_top) {
             top = -INFINITY;
             for (int b = 0; b < pieces; ++b) {
                 float x[8];
@@ -825,7 +832,7 @@ __global__ void __launch_bounds__(32 * QUAD_WARPS) k_route_many(const RouteArgs 
             if (mine[i] >= 0) {
                 if (a.score == SOM_SCORE_SIGMOID) s[i] = a.renorm && least < LOW_LOGIT ? sigmoid_from(x[i], fminf(most, 0.f)) : 1.f / (1.f + expf(-x[i]));
                 else if (!a.renorm) s[i] = exp_from(x[i], top) / total;
-                else if (most == top || top < INFINITY) s[i] = exp_from(x[i], most);  // only ratios count
+                else if (!has_top || scores_at(most, top)) s[i] = exp_from(x[i], most);  // only ratios count
             }
             sum += s[i];
         }
@@ -923,8 +930,14 @@ __global__ void __launch_bounds__(32 * ROUTE_WARPS) k_route_backward(const Route
         } else {
             float q = 0.f;  // (renormalised: any multiple of the scores will do)
             if (a.score == SOM_SCORE_SOFTMAX) {
-                const float top = warp_max(xj);
-                if (live) q = exp_from(xj, top);
+                const float most = warp_max(xj);
+                bool scores = true;
+                if (most < NO_SCORE + 100.f) {  // (above that only a row's largest logit beyond 100 could leave no score)
+                    float top = most;
+                    for (int i = lane; i < a.E; i += 32) top = fmaxf(top, logit_at<TYPE>(a.logits, row + i));
+                    scores = scores_at(most, warp_max(top));
+                }
+                if (live && scores) q = exp_from(xj, most);
             } else {
                 if (live) q = 1.f / (1.f + expf(-xj));
                 if (a.renorm && __any_sync(ALL, live && xj < LOW_LOGIT)) {

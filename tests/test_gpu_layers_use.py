@@ -245,3 +245,35 @@ def test_workspace_that_cannot_be_had(L):
     s = torch.rand(40, 8, generator=gen).topk(4, dim=1)
     y = L.experts(_normal(gen, 40, 64, dtype=BF16), s.indices.int().cuda(), s.values.cuda(), _normal(gen, 8, 64, 64, dtype=BF16), _normal(gen, 8, 64, 32, dtype=BF16))
     assert y.isfinite().all() and L.device_flags() == 0
+
+
+@pytest.mark.parametrize("T", [40, 16400])
+@pytest.mark.parametrize("dtype", [FP32, BF16, FP16])
+@pytest.mark.parametrize("k,groups", [(1, 1), (3, 1), (2, 4)])
+def test_softmax_masks_of_the_lowest_value(L, T, dtype, k, groups):
+    """Logits of the type's lowest value as a mask: such an expert's score is 0 in 64 bits.  Where the bias has only such experts chosen,
+    renormalised weights are 0 and not 1 / k, and nothing flows back; beside one that is not masked they weigh 0."""
+    gen = torch.Generator().manual_seed(T)
+    E = 64
+    z = (torch.randn(T, E, generator=gen) * 2).to(dtype)
+    low = torch.rand(T, E, generator=gen) < 0.6
+    low[:, 7] = False
+    z[low] = torch.finfo(dtype).min
+    bias = torch.randn(E, generator=gen) * 0.5  # (beyond the scores: it decides)
+    opt = dict(score="softmax", groups=groups, top_groups=1, group_best=1)
+    got = L.route(z.cuda(), k, bias=bias.cuda(), renorm=True, **opt)
+    at = got["indices"].cpu().long()
+    x = z.double().requires_grad_()
+    q = torch.softmax(x, 1).gather(1, at)
+    w = q / q.sum(1, keepdim=True).clamp_min(1e-300)
+    masked = low.gather(1, at)
+    assert masked.all(1).any() and (masked.any(1) & ~masked.all(1)).any() == (k > 1)
+    # (E + 16) half units for exponentials, sums and divisions, 16 for differences of exponents of up to 16
+    assert ((got["weights"].double().cpu() - w).abs() <= (E + 32) * 2.0 ** -24 * w).all()
+    assert not got["weights"].cpu()[masked].any()
+    dw = torch.randn(T, k, generator=gen)
+    (w * dw.double()).sum().backward()
+    dz = L.route_backward(z.cuda(), got["indices"], dw.cuda(), score="softmax", renorm=True).double().cpu()
+    bound = (E + 3 * k + 48) * 2.0 ** -23 * dw.double().abs().max(1, keepdim=True).values
+    assert ((dz - x.grad).abs() <= bound + (0 if dtype == FP32 else 2.0 ** -8 * x.grad.abs())).all()
+    assert not dz.gather(1, at)[masked].any()
