@@ -223,6 +223,7 @@ int som_layers_create(som_layers** out)
     if (e == cudaSuccess) e = cudaMemset(l->flags, 0, 256);
     if (e != cudaSuccess) {
         som_layers_destroy(l);
+        (void)cudaGetLastError();
         return SOM_ERR_CUDA;
     }
     *out = l;

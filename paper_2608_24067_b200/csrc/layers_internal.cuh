@@ -57,11 +57,12 @@ cudaError_t launch(som_layers* l, void (*kernel)(P...), dim3 grid, int threads, 
     return cudaLaunchKernelEx(&c, kernel, P(args)...);
 }
 
-// a launch's outcome as a status, the error kept on the handle
+// a launch's outcome as a status, the error kept on the handle (and not left for the check of another call's launch)
 inline int outcome(som_layers* l, cudaError_t e)
 {
     if (e == cudaSuccess) return SOM_OK;
     l->last_cuda_error = (int)e;
+    (void)cudaGetLastError();
     return SOM_ERR_CUDA;
 }
 

@@ -103,6 +103,7 @@ static int create_impl(som_handle** out, int32_t V, int64_t M, const void* d_cod
     if (e == cudaSuccess) e = cudaMemset(h->dev_flags, 0, 256);
     if (e != cudaSuccess) {
         som_destroy(h);
+        (void)cudaGetLastError();
         return SOM_ERR_CUDA;
     }
     *out = h;
@@ -577,7 +578,8 @@ int som_plan_create(som_handle* h, const int32_t* d_indptr, const int32_t* d_ind
                                       SOM_PLAN_MASK_FEATURES, geom.n_hot, st);
     }
     if (rc) {
-        if (rc == SOM_ERR_CUDA && !h->last_cuda_error) h->last_cuda_error = (int)cudaGetLastError();
+        const cudaError_t last = cudaGetLastError();  // (read in any case: the next launch's check must not find it)
+        if (rc == SOM_ERR_CUDA && !h->last_cuda_error) h->last_cuda_error = (int)last;
         som_plan_destroy(p);
         return rc;
     }

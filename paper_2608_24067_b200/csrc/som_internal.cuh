@@ -112,6 +112,7 @@ enum { EV_NORMS_BEGIN = 0, EV_NORMS_END, EV_BMU_BEGIN, EV_BMU_PLAN_END, EV_BMU_S
         cudaError_t e__ = (call);                         \
         if (e__ != cudaSuccess) {                         \
             (h)->last_cuda_error = (int)e__;              \
+            (void)cudaGetLastError(); /* the next launch's check must not find it */ \
             return SOM_ERR_CUDA;                          \
         }                                                 \
     } while (0)

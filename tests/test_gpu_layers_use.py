@@ -223,13 +223,9 @@ def test_sigmoid_scores_below_fp32(L, T, base, k):
     assert ((dz - x.grad).abs() <= 256 * 2.0 ** -24 * size * spread).all()
 
 
-def test_workspace_that_cannot_be_had(L):
-    """A call whose workspace does not fit the card (4.2 million rows of 8192 in fp32 and 16 bits: 206 GB) says so; neither the handle nor
-    what else runs in the process is affected."""
+def _too_much(L):
+    """A call that fails for want of memory."""
     from paper_2608_24067_b200.som import SomError
-    gen = torch.Generator().manual_seed(2)
-    x, w = _normal(gen, 100, 256, dtype=BF16), _normal(gen, 512, 256, dtype=BF16)
-    want = L.linear(x, w, act="gelu")
     T, E, k, D, I = 1 << 17, 32, 32, 8192, 8
     assert T * k * D * 6 > torch.cuda.get_device_properties(0).total_memory
     args = (torch.zeros(T, D, dtype=BF16, device="cuda"), torch.zeros(T, k, dtype=torch.int32, device="cuda"), torch.zeros(T, k, device="cuda"),
@@ -239,6 +235,15 @@ def test_workspace_that_cannot_be_had(L):
     assert e.value.status == 4 and e.value.cuda_error == 2  # out of memory
     del args, e
     torch.cuda.empty_cache()
+
+
+def test_workspace_that_cannot_be_had(L):
+    """A call whose workspace does not fit the card (4.2 million rows of 8192 in fp32 and 16 bits: 206 GB) says so; neither the handle nor
+    what else runs in the process is affected."""
+    gen = torch.Generator().manual_seed(2)
+    x, w = _normal(gen, 100, 256, dtype=BF16), _normal(gen, 512, 256, dtype=BF16)
+    want = L.linear(x, w, act="gelu")
+    _too_much(L)
     assert float((torch.ones(8, device="cuda") + 1).sum()) == 16  # (a check of the last CUDA error comes with every launch)
     torch.cuda.synchronize()
     assert torch.equal(L.linear(x, w, act="gelu"), want)
@@ -277,3 +282,18 @@ def test_softmax_masks_of_the_lowest_value(L, T, dtype, k, groups):
     bound = (E + 3 * k + 48) * 2.0 ** -23 * dw.double().abs().max(1, keepdim=True).values
     assert ((dz - x.grad).abs() <= bound + (0 if dtype == FP32 else 2.0 ** -8 * x.grad.abs())).all()
     assert not dz.gather(1, at)[masked].any()
+
+
+def test_search_after_a_failed_call(L):
+    """The error of a call that failed is that call's: the next one, of another handle of the library, does not find it."""
+    from paper_2608_24067_b200 import synth
+    from paper_2608_24067_b200.som import Som
+    V, M = 500, 256
+    batch = synth.sample_csr(1000, V, 5.0, 1, device="cuda")
+    som = Som(V, M, synth.fill_codebook(V, M, 1, device="cuda"))
+    som.norms()
+    want, _ = som.bmu(batch.indptr, batch.indices)
+    _too_much(L)
+    som.norms()
+    got, _ = som.bmu(batch.indptr, batch.indices)
+    assert torch.equal(got, want)
