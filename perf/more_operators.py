@@ -262,14 +262,15 @@ def _random_bits(n, seed, tensor, device):
 
 
 def _encode(x, signed, bits, nonzero):
-    """8-bit codes of fp32 values and the exponent of each block of 256: the code is the top of the fp32 number scaled so that the
-    block's largest exponent is 15 (signed: a sign, 4 bits of exponent and 3 of fraction) or 31 (5 and 3), rounded up where the
-    20 bits below, plus 20 random ones (16 drawn), pass 2^20.  nonzero: a positive value does not become 0."""
+    """8-bit codes of fp32 values and the exponent of each block of 256 (that of the largest magnitude, one more where its fraction is above the
+    codes' last, 7 / 8): the code is the top of the fp32 number scaled so that the block's exponent is 15 (signed: a sign, 4 bits of
+    exponent and 3 of fraction) or 31 (5 and 3), rounded up where the 20 bits below, plus 20 random ones (16 drawn), pass 2^20.
+    nonzero: a positive value does not become 0."""
     flat = x.reshape(-1)
     n, blocks = flat.numel(), -(-flat.numel() // BLOCK)
     a = flat.abs()
-    e = torch.zeros(blocks * BLOCK, dtype=torch.int32, device=x.device).index_copy_(0, torch.arange(n, device=x.device), a.view(torch.int32) >> 23)
-    e = e.view(blocks, BLOCK).amax(1)
+    e = torch.zeros(blocks * BLOCK, dtype=torch.int32, device=x.device).index_copy_(0, torch.arange(n, device=x.device), a.view(torch.int32))
+    e = (e.view(blocks, BLOCK).amax(1).clamp_max(0x7F800000) + 0x100000) >> 23
     up = torch.exp2((127 - e).double()).float()[torch.arange(n, device=x.device) // BLOCK]
     scaled = (a * up) * (2.0 ** -112 if signed else 2.0 ** -96)
     code = ((scaled.view(torch.int32) + (bits << 4)) >> 20).clamp_max(127 if signed else 255)
