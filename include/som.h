@@ -520,6 +520,101 @@ int som_experts_backward(som_layers* l, int type, int act, int gated, int64_t T,
                          const void* w1, const void* b1, const void* w2, const void* b2, const void* dy, int64_t lddy,
                          void* dx, void* dweights, void* dw1, void* db1, void* dw2, void* db2, void* stream);
 
+/*
+ * What stands around these layers when they are trained and served: a norm in front of them, the step that moves their weights by
+ * their gradients, and their weights in 4 bits.  What is said above of all the calls holds for these too.
+ */
+
+/*
+ * som_norm - layer norm of every row of h = x + residual:  y = (h - mean) / sqrt(variance + eps) * weight + bias, the mean and the
+ * variance (that of the D values, not of a sample) over the row.  h is rounded to `type` before anything else is computed from it, so that
+ * what a later call reads from `sum` is what was normed here.
+ *   type SOM_F32, SOM_F16 or SOM_BF16; x [T][D] (ldx), residual [T][D] (ldr) or NULL, weight, bias [D] of weights_type (SOM_F32 or
+ *   `type`), each NULL = 1 or 0; sum [T][D] (lds): h, or NULL = not wanted; y [T][D] (ldy).
+ * Any D up to 2^24, any ld, any alignment of elements (rows that lie on 16 bytes are faster).  T < 2^30.
+ */
+int som_norm(som_layers* l, int type, int64_t T, int64_t D, const void* x, int64_t ldx, const void* weight, const void* bias,
+             int weights_type, const void* residual, int64_t ldr, float eps, void* sum, int64_t lds, void* y, int64_t ldy, void* stream);
+
+/*
+ * som_norm_backward - the gradient of som_norm by h (x here; it is x's and the residual's gradient alike) from dy, plus dsum, what `sum` got
+ * from elsewhere (NULL = nothing).  The rows' statistics are computed again; the forward call keeps nothing.
+ *   dy [T][D] (lddy), dsum [T][D] (ldds) or NULL; dx [T][D], dweight, dbias [D] (weights_type): contiguous outputs, NULL = not wanted.
+ */
+int som_norm_backward(som_layers* l, int type, int64_t T, int64_t D, const void* x, int64_t ldx, const void* weight, int weights_type,
+                      const void* dy, int64_t lddy, const void* dsum, int64_t ldds, float eps, void* dx, void* dweight, void* dbias,
+                      void* stream);
+
+/* One tensor of som_adamw: n elements, contiguous, at addresses on device memory.  m and v: fp32, or 8-bit codes with
+ * exponents [2][(n + 255) / 256] (m's, then v's), all zeros before the first step.  number: which tensor it is, for the random bits.
+ * first_chunk is the library's own. */
+typedef struct som_adamw_tensor {
+    void* param;
+    const void* grad;
+    void* copy;
+    void *m, *v;
+    uint8_t* exponents;
+    int64_t n;
+    uint32_t number, first_chunk;
+} som_adamw_tensor;
+
+typedef struct som_adamw_step {
+    double rate, beta1, beta2, eps, decay;
+    int64_t step;            /* t, from 1 */
+    const float* rate_at;    /* device: in the place of rate, or NULL */
+    const int64_t* step_at;  /* device: in the place of step, and seed + *step_at in the place of seed, or NULL (for captured graphs) */
+    const float* scale;      /* device: multiplies the gradients; if it is an infinity or NaN nothing is changed; or NULL */
+    uint32_t seed;           /* 8-bit moments: of the random bits; another one each step */
+} som_adamw_step;
+
+/*
+ * som_adamw - one step over `count` tensors (a host array, read within the call; no two may share memory):
+ *   g = scale * grad, m = beta1 m + (1 - beta1) g, v = beta2 v + (1 - beta2) g^2,
+ *   param = param (1 - rate decay) - rate (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps)
+ * in fp32, param rounded once to param_type, copy (copy_type SOM_F16 or SOM_BF16 beside fp32 parameters, -1 = none) to its type.
+ * grad_type: SOM_F32, or 16 bits (beside 16-bit parameters their own type).
+ * bits 32: moments in fp32.  bits 8: 256 consecutive elements share a power of two 2^(e - 127), that of their largest magnitude, or the next
+ * where that is 1.875 times it or more (e = 255: it is not finite, and the block's values are infinities and NaN); an element is a code of 8 bits: m a sign, 4 bits of exponent E and 3 of fraction
+ * f, (1 + f / 8) 2^(E - 15), f / 8 2^-14 for E = 0; v the same with 5 bits and no sign, 2^(E - 31) and 2^-30.  A new value is rounded to one
+ * of its two neighbours by 16 random bits that are a function of (seed, number, element), so that the mean is right; v > 0 does not
+ * become 0.  The step itself uses the value before that rounding.
+ */
+int som_adamw(som_layers* l, int param_type, int grad_type, int copy_type, int bits, int32_t count, const som_adamw_tensor* tensors,
+              const som_adamw_step* step, void* stream);
+
+/* som_adamw_moments - the values of 8-bit moments, as bf16 (which holds them exactly): m[i], v[i] (host arrays of device addresses) get
+ * those of tensors[i].  (Only m, v, exponents and n are looked at.) */
+int som_adamw_moments(som_layers* l, int32_t count, const som_adamw_tensor* tensors, void* const* m, void* const* v, void* stream);
+
+/*
+ * Matrices in 4 bits: 32 consecutive values of a row share a power of two, each is one of 0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives.
+ *   codes   [rows][D / 2]: two a byte, the even column in the low half; sign, 2 bits of exponent, 1 of fraction.
+ *   scales  som_fp4_scale_bytes(rows, D) bytes: the byte e of a block stands for 2^(e - 127), 255 for NaN.  Block j of row r is byte
+ *           ((r / 128) ((D + 255) / 256) + j / 8) 1024 + (j / 4 % 2) 512 + (r % 32) 16 + (r / 32 % 4) 4 + j % 4, the
+ *           order in which the matrix instructions take them.  Blocks beyond the row's end are 0; rows beyond the last are not written.
+ * D is a multiple of 32; codes start on 16 bytes, scales on 128 (else SOM_ERR_UNSUPPORTED).
+ */
+int64_t som_fp4_scale_bytes(int64_t rows, int64_t D); /* -1 for sizes that are not supported */
+
+/*
+ * som_fp4_quantize - x [T][D] (ldx; SOM_F32, SOM_F16 or SOM_BF16, rows on 16 bytes) -> codes, scales.  A block's power of two is that of its
+ * largest magnitude over 4, and one more where that magnitude is 1.75 times its power of two or more (it would round to 8), at least 2^-127, at most 2^125;
+ * the quotients are rounded to the nearest value, ties to the even code.  A block that holds an infinity or NaN becomes NaN.
+ */
+int som_fp4_quantize(som_layers* l, int type, int64_t T, int64_t D, const void* x, int64_t ldx, void* codes, void* scales, void* stream);
+
+/* som_fp4_values - what they stand for, rounded to `type` (exact in fp32 and bf16): y [T][D] (ldy, rows on 16 bytes). */
+int som_fp4_values(som_layers* l, int type, int64_t T, int64_t D, const void* codes, const void* scales, void* y, int64_t ldy, void* stream);
+
+/*
+ * som_fp4_linear - som_linear with both operands in 4 bits: x is quantised within the call as som_fp4_quantize does it, the weights
+ * w_codes, w_scales [rows][D] with rows = gated ? 2 F : F were before.  z, act and the sum with the residual are fp32, y is rounded once.
+ * type, bias, residual, y, ld* and F as in som_linear; D a multiple of 32.
+ */
+int som_fp4_linear(som_layers* l, int type, int act, int gated, int64_t T, int64_t D, int64_t F, const void* x, int64_t ldx,
+                   const void* w_codes, const void* w_scales, const void* bias, const void* residual, int64_t ldr, void* y, int64_t ldy,
+                   void* stream);
+
 #ifdef __cplusplus
 }
 #endif

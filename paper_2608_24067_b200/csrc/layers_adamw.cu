@@ -1,0 +1,421 @@
+// A step of AdamW over many tensors in one launch, with its moments in 32 bits or in 8.
+//
+//   g = scale grad, m = b1 m + (1 - b1) g, v = b2 v + (1 - b2) g^2,
+//   p = p (1 - rate decay) - rate (m / (1 - b1^t)) / (sqrt(v / (1 - b2^t)) + eps); a 16-bit copy of p where one is wanted.
+//
+// Moments in 8 bits: 256 consecutive elements share a power of two, that of their largest magnitude (the next where it is above the
+// largest code, which could not be rounded up, and a growing moment would stay at it); an element's code is a
+// small floating-point number below it: m a sign, 4 bits of exponent and 3 of fraction, v 5 and 3 (it spans twice m's powers), both
+// with gradual underflow, 2^-17 and 2^-33 of the block's power at the least.  Rounding to the nearest would hold v still for ever: a
+// step moves it by a thousandth, a code is a sixteenth apart.  So a value is rounded up with the probability that makes the code
+// right in the mean, by 16 random bits that are a function of (seed, tensor, element): the same call gives the same codes.  A
+// positive v never becomes 0 (the quotient would lose its measure).  The fp32 value that a code is made from is the one that the step used.
+//
+// Products and sums that the codes come from are rounded one by one (no fused multiply-add): which code is taken is then a matter of
+// the definition, not of the compiler.
+//
+// Bound by HBM: 28 bytes an element with fp32 parameters, a bf16 copy and bf16 gradients, 10 with 8-bit moments and bf16
+// parameters.  A block takes 2048 elements of one tensor, a thread eight in a row, a warp the 256 that share a power; the tensors'
+// addresses are the kernel's own parameters (no table to copy, and a captured graph keeps them).
+#include "layers_host.cuh"
+#include "layers_math.cuh"
+
+namespace lay {
+namespace {
+
+constexpr int ADAM_THREADS = 256, ADAM_BLOCK = 256, ADAM_CHUNK = 8 * ADAM_THREADS;
+
+struct Hyper {
+    float keep, rate, b1, c1, b2, c2, k1, k2, eps;  // keep = 1 - rate decay; c = 1 - b; k = 1 / (1 - b^t)
+    uint32_t seed;
+};
+
+template <int CAP>
+struct AdamTable {
+    som_adamw_tensor item[CAP];  // first_chunk: the launch's chunks before the tensor
+    int count;
+    int param_bf16, grad_bf16, copy_bf16;
+    Hyper h;
+    const Hyper* h_at;  // in its place where the host does not know it
+    const float* scale;
+};
+
+template <int CAP>
+struct MomentTable {
+    som_adamw_tensor item[CAP];  // param, copy: where m and v go
+    int count;
+};
+
+struct HyperArgs {
+    Hyper* to;
+    double rate, b1, b2, eps, decay;
+    int64_t step;
+    const float* rate_at;
+    const int64_t* step_at;
+    uint32_t seed;
+};
+
+__host__ __device__ inline Hyper hyper_of(double rate, double b1, double b2, double eps, double decay, int64_t step, uint32_t seed)
+{
+    return {(float)(1.0 - rate * decay), (float)rate, (float)b1, (float)(1.0 - b1), (float)b2, (float)(1.0 - b2),
+            (float)(1.0 / (1.0 - pow(b1, (double)step))), (float)(1.0 / (1.0 - pow(b2, (double)step))), (float)eps, seed};
+}
+
+__global__ void k_adamw_hyper(const HyperArgs a)
+{
+    enter();
+    const int64_t step = a.step_at ? *a.step_at : a.step;
+    *a.to = hyper_of(a.rate_at ? (double)*a.rate_at : a.rate, a.b1, a.b2, a.eps, a.decay, step, a.step_at ? a.seed + (uint32_t)step : a.seed);
+}
+
+__device__ __forceinline__ uint32_t mix(uint32_t x)
+{
+    x ^= x >> 16;
+    x *= 0x9E3779B9u;
+    x ^= x >> 15;
+    x *= 0xBB67AE85u;
+    return x ^ (x >> 16);
+}
+
+// eight consecutive values as fp32; `left` of them exist (vector loads only where all do)
+__device__ __forceinline__ void read8(const float* p, float (&v)[8], bool whole, int left)
+{
+    if (whole) {
+        const float4 a = *reinterpret_cast<const float4*>(p), b = *(reinterpret_cast<const float4*>(p) + 1);
+        v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = i < left ? p[i] : 0.f;
+    }
+}
+__device__ __forceinline__ void read8(const uint16_t* p, float (&v)[8], bool whole, int left, int bf16)
+{
+    if (whole) {
+        load8(p, v, bf16);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = i < left ? unpack1(p[i], bf16) : 0.f;
+    }
+}
+__device__ __forceinline__ void write8(float* p, const float (&v)[8], bool whole, int left)
+{
+    if (whole) {
+        *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
+        *(reinterpret_cast<float4*>(p) + 1) = make_float4(v[4], v[5], v[6], v[7]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < left) p[i] = v[i];
+    }
+}
+__device__ __forceinline__ void write8(uint16_t* p, const float (&v)[8], bool whole, int left, int bf16)
+{
+    const uint4 w = make_uint4(pack2(v[0], v[1], bf16), pack2(v[2], v[3], bf16), pack2(v[4], v[5], bf16), pack2(v[6], v[7], bf16));
+    if (whole) {
+        *reinterpret_cast<uint4*>(p) = w;
+    } else {
+        const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < left) p[i] = (uint16_t)(u[i / 2] >> (16 * (i & 1)));
+    }
+}
+__device__ __forceinline__ uint2 read_codes(const uint8_t* p, bool whole, int left)
+{
+    if (whole) return *reinterpret_cast<const uint2*>(p);
+    uint32_t w[2] = {0u, 0u};
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        if (i < left) w[i / 4] |= (uint32_t)p[i] << (8 * (i & 3));
+    return make_uint2(w[0], w[1]);
+}
+__device__ __forceinline__ void write_codes(uint8_t* p, const uint32_t (&w)[2], bool whole, int left)
+{
+    if (whole) {
+        *reinterpret_cast<uint2*>(p) = make_uint2(w[0], w[1]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < left) p[i] = (uint8_t)(w[i / 4] >> (8 * (i & 3)));
+    }
+}
+
+// 2^(e - 127) of an exponent byte; 255 (a block that holds an infinity or NaN) gives infinity, and 0 times it NaN
+__device__ __forceinline__ float power_of(uint32_t e) { return __uint_as_float(e ? e << 23 : 0x00400000u); }
+// 2^(127 - e), e <= 255
+__device__ __forceinline__ float power_below(uint32_t e) { return __uint_as_float(e < 254u ? (254u - e) << 23 : e == 254u ? 0x00400000u : 0x00200000u); }
+
+// the values of eight codes: a code's bits are the top of a number of the smallest exponents, which TOP lifts to [0, 2)
+template <bool SIGNED>
+__device__ __forceinline__ void decode8(uint2 c, uint32_t e, float (&v)[8])
+{
+    const float by = power_of(e), top = SIGNED ? 0x1p112f : 0x1p96f;
+    const uint32_t w[2] = {c.x, c.y};
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const uint32_t code = (w[i / 4] >> (8 * (i & 3))) & 255u;
+        const float f = (__uint_as_float((SIGNED ? code & 127u : code) << 20) * top) * by;
+        v[i] = SIGNED && code > 127u ? -f : f;
+    }
+}
+
+// codes of eight values of a block of a warp's 256, and the block's exponent; h: 32 random bits for each, the lower half for m, the upper for v
+template <bool SIGNED>
+__device__ __forceinline__ uint32_t encode8(const float (&v)[8], const uint32_t (&h)[8], uint32_t (&w)[2])
+{
+    uint32_t most = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) most = max(most, __float_as_uint(v[i]) & 0x7fffffffu);
+    const uint32_t e = (min(__reduce_max_sync(0xffffffffu, most), 0x7f800000u) + 0x100000u) >> 23;  // (a fraction of 7 / 8 and more carries)
+    const float up = power_below(e);
+    w[0] = w[1] = 0u;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const float a = __fmul_rn(__fmul_rn(fabsf(v[i]), up), SIGNED ? 0x1p-112f : 0x1p-96f);
+        const uint32_t r = SIGNED ? (h[i] & 0xffffu) << 4 : (h[i] >> 16) << 4;
+        uint32_t code = min((__float_as_uint(a) + r) >> 20, SIGNED ? 127u : 255u);
+        if (SIGNED) code |= v[i] < 0.f ? 128u : 0u;
+        else if (v[i] > 0.f) code = max(code, 1u);
+        w[i / 4] |= code << (8 * (i & 3));
+    }
+    return e;
+}
+
+// the tensor that a chunk of the launch belongs to
+template <class TABLE>
+__device__ __forceinline__ int tensor_of(const TABLE& t, uint32_t chunk)
+{
+    int lo = 0, hi = t.count - 1;
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (t.item[mid].first_chunk <= chunk) lo = mid;
+        else hi = mid - 1;
+    }
+    return lo;
+}
+
+// P16, G16: 16-bit parameters, gradients; COPY: a 16-bit copy of fp32 parameters
+template <bool P16, bool G16, bool COPY, int BITS, int CAP>
+__global__ void __launch_bounds__(ADAM_THREADS) k_adamw(const __grid_constant__ AdamTable<CAP> t)
+{
+    enter();
+    const som_adamw_tensor& it = t.item[tensor_of(t, blockIdx.x)];
+    const int64_t at = (int64_t)(blockIdx.x - it.first_chunk) * ADAM_CHUNK + threadIdx.x * 8;
+    const float scale = t.scale ? *t.scale : 1.f;
+    if (!(fabsf(scale) <= 3.4028235e38f)) return;  // an infinity or NaN: the step is left out
+    if (at - (int)(threadIdx.x & 31) * 8 >= it.n) return;  // none of the warp's
+    const Hyper h = t.h_at ? *t.h_at : t.h;
+    const int left = it.n - at >= 8 ? 8 : it.n > at ? (int)(it.n - at) : 0;
+    const uintptr_t all = reinterpret_cast<uintptr_t>(it.param) | reinterpret_cast<uintptr_t>(it.grad) | reinterpret_cast<uintptr_t>(it.copy) |
+                          reinterpret_cast<uintptr_t>(it.m) | reinterpret_cast<uintptr_t>(it.v);
+    const bool whole = left == 8 && (all & 15u) == 0;
+
+    float p[8], g[8], m[8], v[8];
+    if (P16) read8(static_cast<const uint16_t*>(it.param) + at, p, whole, left, t.param_bf16);
+    else read8(static_cast<const float*>(it.param) + at, p, whole, left);
+    if (G16) read8(static_cast<const uint16_t*>(it.grad) + at, g, whole, left, t.grad_bf16);
+    else read8(static_cast<const float*>(it.grad) + at, g, whole, left);
+    const int64_t blocks = (it.n + ADAM_BLOCK - 1) / ADAM_BLOCK, block = at / ADAM_BLOCK;
+    if (BITS == 8) {
+        const uint2 mc = read_codes(static_cast<const uint8_t*>(it.m) + at, whole, left), vc = read_codes(static_cast<const uint8_t*>(it.v) + at, whole, left);
+        decode8<true>(mc, it.exponents[block], m);
+        decode8<false>(vc, it.exponents[blocks + block], v);
+    } else {
+        read8(static_cast<const float*>(it.m) + at, m, whole, left);
+        read8(static_cast<const float*>(it.v) + at, v, whole, left);
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        if (t.scale) g[i] = __fmul_rn(g[i], scale);
+        m[i] = __fadd_rn(__fmul_rn(m[i], h.b1), __fmul_rn(g[i], h.c1));
+        v[i] = __fadd_rn(__fmul_rn(v[i], h.b2), __fmul_rn(__fmul_rn(g[i], g[i]), h.c2));
+        const float change = m[i] * h.k1 / (sqrtf(v[i] * h.k2) + h.eps);
+        p[i] = p[i] * h.keep - change * h.rate;
+    }
+    if (P16) write8(static_cast<uint16_t*>(it.param) + at, p, whole, left, t.param_bf16);
+    else write8(static_cast<float*>(it.param) + at, p, whole, left);
+    if (COPY) write8(static_cast<uint16_t*>(it.copy) + at, p, whole, left, t.copy_bf16);
+    if (BITS == 8) {
+        const uint32_t key = mix(mix((uint32_t)block) ^ (h.seed + it.number * 0x9E3779B9u));
+        uint32_t r[8], w[2];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            r[i] = mix(key + ((threadIdx.x & 31) * 8 + i) * 0x6A09E667u);
+            if (i >= left) m[i] = v[i] = 0.f;  // (beyond the tensor's end)
+        }
+        const uint32_t em = encode8<true>(m, r, w);
+        write_codes(static_cast<uint8_t*>(it.m) + at, w, whole, left);
+        const uint32_t ev = encode8<false>(v, r, w);
+        write_codes(static_cast<uint8_t*>(it.v) + at, w, whole, left);
+        if ((threadIdx.x & 31) == 0) {
+            it.exponents[block] = (uint8_t)em;
+            it.exponents[blocks + block] = (uint8_t)ev;
+        }
+    } else {
+        write8(static_cast<float*>(it.m) + at, m, whole, left);
+        write8(static_cast<float*>(it.v) + at, v, whole, left);
+    }
+}
+
+// What the 8-bit moments stand for, as bf16 values, which hold them exactly.
+template <int CAP>
+__global__ void __launch_bounds__(ADAM_THREADS) k_adamw_moments(const __grid_constant__ MomentTable<CAP> t)
+{
+    enter();
+    const som_adamw_tensor& it = t.item[tensor_of(t, blockIdx.x)];
+    const int64_t at = (int64_t)(blockIdx.x - it.first_chunk) * ADAM_CHUNK + threadIdx.x * 8;
+    if (at >= it.n) return;
+    const int left = it.n - at >= 8 ? 8 : (int)(it.n - at);
+    const uintptr_t all = reinterpret_cast<uintptr_t>(it.param) | reinterpret_cast<uintptr_t>(it.copy) | reinterpret_cast<uintptr_t>(it.m) | reinterpret_cast<uintptr_t>(it.v);
+    const bool whole = left == 8 && (all & 15u) == 0;
+    const int64_t blocks = (it.n + ADAM_BLOCK - 1) / ADAM_BLOCK, block = at / ADAM_BLOCK;
+    float m[8], v[8];
+    decode8<true>(read_codes(static_cast<const uint8_t*>(it.m) + at, whole, left), it.exponents[block], m);
+    decode8<false>(read_codes(static_cast<const uint8_t*>(it.v) + at, whole, left), it.exponents[blocks + block], v);
+    write8(static_cast<uint16_t*>(it.param) + at, m, whole, left, 1);
+    write8(static_cast<uint16_t*>(it.copy) + at, v, whole, left, 1);
+}
+
+// Tensors a launch: what a kernel's parameters hold (32764 bytes), and fewer where there are few, since a launch copies them.
+constexpr int FEW_TENSORS = 24, MOST_TENSORS = 500;
+static_assert(sizeof(AdamTable<MOST_TENSORS>) <= 32764, "kernel parameters");
+
+template <bool P16, bool G16, bool COPY, int BITS>
+cudaError_t launch_adamw(som_layers* l, const AdamTable<MOST_TENSORS>& t, unsigned chunks, cudaStream_t st)
+{
+    if (t.count > FEW_TENSORS) return launch(l, k_adamw<P16, G16, COPY, BITS, MOST_TENSORS>, dim3(chunks), ADAM_THREADS, 0, st, 1, t);
+    AdamTable<FEW_TENSORS> s;
+    for (int i = 0; i < t.count; ++i) s.item[i] = t.item[i];
+    s.count = t.count;
+    s.param_bf16 = t.param_bf16, s.grad_bf16 = t.grad_bf16, s.copy_bf16 = t.copy_bf16;
+    s.h = t.h;
+    s.h_at = t.h_at;
+    s.scale = t.scale;
+    return launch(l, k_adamw<P16, G16, COPY, BITS, FEW_TENSORS>, dim3(chunks), ADAM_THREADS, 0, st, 1, s);
+}
+
+template <int BITS>
+cudaError_t launch_types(som_layers* l, const AdamTable<MOST_TENSORS>& t, bool p16, bool g16, bool copy, unsigned chunks, cudaStream_t st)
+{
+    if (p16) return g16 ? launch_adamw<true, true, false, BITS>(l, t, chunks, st) : launch_adamw<true, false, false, BITS>(l, t, chunks, st);
+    if (copy) return g16 ? launch_adamw<false, true, true, BITS>(l, t, chunks, st) : launch_adamw<false, false, true, BITS>(l, t, chunks, st);
+    return g16 ? launch_adamw<false, true, false, BITS>(l, t, chunks, st) : launch_adamw<false, false, false, BITS>(l, t, chunks, st);
+}
+
+constexpr int64_t MOST_CHUNKS = ((int64_t)1 << 31) - 1;
+
+bool off_by(const void* p, int bytes) { return (reinterpret_cast<uintptr_t>(p) & (uintptr_t)(bytes - 1)) != 0; }
+
+// Hands the tensors out to launches: run(first, count, chunks) with their first_chunk written to `to`
+template <class TABLE, class RUN>
+int in_launches(const som_adamw_tensor* tensors, int32_t count, TABLE& t, RUN&& run)
+{
+    int32_t i = 0;
+    while (i < count) {
+        int64_t chunks = 0;
+        t.count = 0;
+        for (; i < count && t.count < MOST_TENSORS; ++i) {
+            if (tensors[i].n == 0) continue;
+            const int64_t more = (tensors[i].n + ADAM_CHUNK - 1) / ADAM_CHUNK;
+            if (chunks + more > MOST_CHUNKS) break;
+            som_adamw_tensor& to = t.item[t.count++];
+            to = tensors[i];
+            to.first_chunk = (uint32_t)chunks;
+            chunks += more;
+        }
+        if (t.count) LAY_TRY(run((unsigned)chunks));
+    }
+    return SOM_OK;
+}
+
+int check_tensors(const som_adamw_tensor* t, int32_t count)
+{
+    if (count < 0 || (count > 0 && !t)) return SOM_ERR_INVALID_ARG;
+    for (int32_t i = 0; i < count; ++i) {
+        if (t[i].n < 0) return SOM_ERR_INVALID_ARG;
+        if (t[i].n > (int64_t)1 << 40) return SOM_ERR_UNSUPPORTED;
+    }
+    return SOM_OK;
+}
+
+}  // namespace
+}  // namespace lay
+
+using namespace lay;
+
+extern "C" {
+
+int som_adamw(som_layers* l, int param_type, int grad_type, int copy_type, int bits, int32_t count, const som_adamw_tensor* tensors,
+              const som_adamw_step* step, void* stream)
+{
+    if (!l || !step || param_type < SOM_F32 || param_type > SOM_BF16 || grad_type < SOM_F32 || grad_type > SOM_BF16 || copy_type > SOM_BF16)
+        return SOM_ERR_INVALID_ARG;
+    const bool copy = copy_type >= 0;
+    if ((bits != 8 && bits != 32) || copy_type == SOM_F32 || (copy && param_type != SOM_F32)) return SOM_ERR_INVALID_ARG;
+    if (half_type(param_type) && half_type(grad_type) && grad_type != param_type) return SOM_ERR_INVALID_ARG;
+    const double b1 = step->beta1, b2 = step->beta2;
+    if (!(b1 >= 0.0 && b1 < 1.0) || !(b2 >= 0.0 && b2 < 1.0) || !(step->eps >= 0.0) || !(step->decay >= 0.0) || (!step->step_at && step->step < 1))
+        return SOM_ERR_INVALID_ARG;
+    LAY_TRY(check_tensors(tensors, count));
+    const int param_bytes = param_type == SOM_F32 ? 4 : 2, grad_bytes = grad_type == SOM_F32 ? 4 : 2;
+    for (int32_t i = 0; i < count; ++i) {
+        const som_adamw_tensor& t = tensors[i];
+        if (t.n == 0) continue;
+        if (!t.param || !t.grad || !t.m || !t.v || (copy && !t.copy) || (bits == 8 && !t.exponents)) return SOM_ERR_INVALID_ARG;
+        if (off_by(t.param, param_bytes) || off_by(t.grad, grad_bytes) || off_by(copy ? t.copy : nullptr, 2) || off_by(t.m, bits / 8) || off_by(t.v, bits / 8))
+            return SOM_ERR_UNSUPPORTED;
+    }
+    Guard g(l->device);
+    cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+    AdamTable<MOST_TENSORS> t;
+    t.param_bf16 = param_type == SOM_BF16, t.grad_bf16 = grad_type == SOM_BF16, t.copy_bf16 = copy_type == SOM_BF16;
+    t.scale = step->scale;
+    t.h_at = nullptr;
+    if (step->rate_at || step->step_at) {
+        LAY_TRY(ensure(l, sizeof(Hyper)));
+        const HyperArgs a = {static_cast<Hyper*>(l->ws), step->rate, b1, b2, step->eps, step->decay, step->step, step->rate_at, step->step_at, step->seed};
+        LAY_TRY(outcome(l, launch(l, k_adamw_hyper, dim3(1), 1, 0, st, 1, a)));
+        t.h_at = a.to;
+    }
+    t.h = hyper_of(step->rate, b1, b2, step->eps, step->decay, step->step_at ? 1 : step->step, step->seed);
+    return in_launches(tensors, count, t, [&](unsigned chunks) {
+        for (int i = 0; i < t.count; ++i)
+            if (!copy) t.item[i].copy = nullptr;
+        return outcome(l, bits == 8 ? launch_types<8>(l, t, param_type != SOM_F32, grad_type != SOM_F32, copy, chunks, st)
+                                    : launch_types<32>(l, t, param_type != SOM_F32, grad_type != SOM_F32, copy, chunks, st));
+    });
+}
+
+int som_adamw_moments(som_layers* l, int32_t count, const som_adamw_tensor* tensors, void* const* m, void* const* v, void* stream)
+{
+    if (!l || (count > 0 && (!m || !v))) return SOM_ERR_INVALID_ARG;
+    LAY_TRY(check_tensors(tensors, count));
+    for (int32_t i = 0; i < count; ++i) {
+        if (tensors[i].n == 0) continue;
+        if (!tensors[i].m || !tensors[i].v || !tensors[i].exponents || !m[i] || !v[i]) return SOM_ERR_INVALID_ARG;
+        if (off_by(m[i], 2) || off_by(v[i], 2)) return SOM_ERR_UNSUPPORTED;
+    }
+    Guard g(l->device);
+    cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+    int32_t from = 0;
+    while (from < count) {  // (the outputs' addresses take the places of param and copy)
+        som_adamw_tensor some[FEW_TENSORS];
+        const int32_t n = count - from < FEW_TENSORS ? count - from : FEW_TENSORS;
+        for (int32_t i = 0; i < n; ++i) {
+            some[i] = tensors[from + i];
+            some[i].param = m[from + i];
+            some[i].copy = v[from + i];
+        }
+        MomentTable<MOST_TENSORS> t;
+        LAY_TRY(in_launches(some, n, t, [&](unsigned chunks) {
+            MomentTable<FEW_TENSORS> s;
+            for (int i = 0; i < t.count; ++i) s.item[i] = t.item[i];
+            s.count = t.count;
+            return outcome(l, launch(l, k_adamw_moments<FEW_TENSORS>, dim3(chunks), ADAM_THREADS, 0, st, 1, s));
+        }));
+        from += n;
+    }
+    return SOM_OK;
+}
+
+}  // extern "C"

@@ -29,7 +29,8 @@ EXPORTS = [
     "som_device_flags", "som_measure_fadd_peak", "som_measure_operand_paths", "som_tc_probe",
     "som_layers_create", "som_layers_destroy", "som_layers_last_cuda_error", "som_layers_launch_count", "som_layers_rounds",
     "som_layers_device_flags", "som_linear", "som_linear_backward", "som_route", "som_route_backward", "som_experts",
-    "som_experts_backward",
+    "som_experts_backward", "som_norm", "som_norm_backward", "som_adamw", "som_adamw_moments", "som_fp4_scale_bytes", "som_fp4_quantize",
+    "som_fp4_values", "som_fp4_linear",
 ]
 
 NOALLOC_MAX_M = 524288
@@ -118,6 +119,17 @@ def load_library():
     experts = [P, INT, INT, INT, I64, I32, I32, I64, I64, P, I64, P, P, INT, P, P, P, P, P, I64]
     lib.som_experts.argtypes = experts + [P, I64, P]
     lib.som_experts_backward.argtypes = experts + [P, P, P, P, P, P, P]
+    lib.som_norm.argtypes = [P, INT, I64, I64, P, I64, P, P, INT, P, I64, F32, P, I64, P, I64, P]
+    lib.som_norm_backward.argtypes = [P, INT, I64, I64, P, I64, P, INT, P, I64, P, I64, F32, P, P, P, P]
+    lib.som_adamw.argtypes = [P, INT, INT, INT, INT, I32, P, P, P]
+    lib.som_adamw_moments.argtypes = [P, I32, P, P, P, P]
+    lib.som_fp4_scale_bytes.argtypes = [I64, I64]
+    lib.som_fp4_scale_bytes.restype = I64
+    lib.som_fp4_quantize.argtypes = [P, INT, I64, I64, P, I64, P, P, P]
+    lib.som_fp4_values.argtypes = [P, INT, I64, I64, P, P, P, I64, P]
+    lib.som_fp4_linear.argtypes = [P, INT, INT, INT, I64, I64, I64, P, I64, P, P, P, P, I64, P, I64, P]
+    for name in ("som_norm", "som_norm_backward", "som_adamw", "som_adamw_moments", "som_fp4_quantize", "som_fp4_values", "som_fp4_linear"):
+        getattr(lib, name).restype = INT
     for name in ("som_layers_create", "som_layers_destroy", "som_layers_last_cuda_error", "som_layers_device_flags",
                  "som_linear", "som_linear_backward", "som_route", "som_route_backward", "som_experts",
                  "som_experts_backward"):
