@@ -3,6 +3,7 @@
 
 #include "layers_few.cuh"
 #include "layers_finish.cuh"
+#include "layers_fp4.cuh"
 #include "layers_host.cuh"
 #include "layers_product.cuh"
 #include "layers_slots.cuh"
@@ -138,6 +139,7 @@ int som_layers_create(som_layers** out)
     cudaError_t e = cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &l->encode, cudaEnableDefault, &found);
     if (e == cudaSuccess && (found != cudaDriverEntryPointSuccess || !l->encode)) e = cudaErrorNotSupported;
     if (e == cudaSuccess) e = prepare_product(l);
+    if (e == cudaSuccess) e = prepare_fp4_product(l);
     if (e == cudaSuccess) e = prepare_few();
     if (e == cudaSuccess) e = prepare_plan();
     if (e == cudaSuccess) e = cudaMalloc(reinterpret_cast<void**>(&l->flags), 256);

@@ -111,50 +111,6 @@ int check_quantized(const void* codes, const void* scales, int64_t rows)
     return aligned16(codes) && (reinterpret_cast<uintptr_t>(scales) & 127u) == 0 ? SOM_OK : SOM_ERR_UNSUPPORTED;
 }
 
-struct NaiveArgs {
-    const uint8_t *xc, *xs, *wc, *ws;
-    const uint16_t *bias, *residual;
-    uint16_t* y;
-    int64_t T, D, F, ldr, ldy;
-    int act, bf16, gated;
-};
-
-__device__ float naive_dot(const NaiveArgs& a, int64_t row, int64_t f, int lane)
-{
-    float s = 0.f;
-    const int64_t tiles = fp4_tiles(a.D);
-    for (int64_t j = lane; j < a.D / 32; j += 32) {
-        float d = 0.f;
-        for (int i = 0; i < 16; ++i) {
-            const uint32_t u = a.xc[(row * a.D + j * 32) / 2 + i], w = a.wc[(f * a.D + j * 32) / 2 + i];
-            d += fp4_value(u) * fp4_value(w) + fp4_value(u >> 4) * fp4_value(w >> 4);
-        }
-        s += d * fp4_power(a.xs[fp4_scale_at(row, j, tiles)]) * fp4_power(a.ws[fp4_scale_at(f, j, tiles)]);
-    }
-    for (int d = 16; d > 0; d >>= 1) s += __shfl_xor_sync(0xffffffffu, s, d);
-    return s;
-}
-
-// a warp an output
-__global__ void __launch_bounds__(256) k_fp4_naive(const NaiveArgs a)
-{
-    enter();
-    const int lane = threadIdx.x & 31;
-    for (int64_t i = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); i < a.T * a.F; i += (int64_t)gridDim.x * 8) {
-        const int64_t row = i / a.F, f = i - row * a.F;
-        float z = naive_dot(a, row, f, lane), u = a.gated ? naive_dot(a, row, a.F + f, lane) : 1.f;
-        if (a.bias) {
-            z += unpack1(a.bias[f], a.bf16);
-            if (a.gated) u += unpack1(a.bias[a.F + f], a.bf16);
-        }
-        float y = 0.f;
-        with_act(a.act, [&](auto tag) { y = act_of<decltype(tag)::value>(z); });
-        y *= u;
-        if (a.residual) y += unpack1(a.residual[row * a.ldr + f], a.bf16);
-        if (lane == 0) a.y[row * a.ldy + f] = (uint16_t)pack2(y, 0.f, a.bf16);
-    }
-}
-
 }  // namespace
 
 int launch_fp4_quantize(som_layers* l, int type, int64_t T, int64_t D, const void* x, int64_t ldx, uint8_t* codes, uint8_t* scales, cudaStream_t st)
@@ -213,18 +169,28 @@ int som_fp4_linear(som_layers* l, int type, int act, int gated, int64_t T, int64
     if (T == 0) return SOM_OK;
     Guard g(l->device);
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
-    Carver c{nullptr, 0};
-    c.take<uint8_t>(T * D / 2);
-    c.take<uint8_t>(fp4_scale_bytes(T, D));
-    LAY_TRY(ensure(l, c.used));
-    c = Carver{static_cast<unsigned char*>(l->ws), 0};
-    uint8_t* codes = c.take<uint8_t>(T * D / 2);
-    uint8_t* scales = c.take<uint8_t>(fp4_scale_bytes(T, D));
+    Fp4Product p = {};
+    p.w_codes = static_cast<const uint8_t*>(w_codes);
+    p.w_scales = static_cast<const uint8_t*>(w_scales);
+    p.bias = static_cast<const uint16_t*>(bias);
+    p.residual = static_cast<const uint16_t*>(residual);
+    p.y = static_cast<uint16_t*>(y);
+    p.T = T, p.D = D, p.F = F, p.ldr = ldr, p.ldy = ldy;
+    p.act = act, p.gated = gated != 0, p.bf16 = type == SOM_BF16;
+    uint8_t *codes = nullptr, *scales = nullptr;
+    unsigned char* parts = nullptr;
+    auto carve = [&](Carver c) {
+        codes = c.take<uint8_t>(T * D / 2);
+        scales = c.take<uint8_t>(fp4_scale_bytes(T, D));
+        parts = c.take<unsigned char>((int64_t)fp4_product_bytes(l, p));
+        return c.used;
+    };
+    LAY_TRY(ensure(l, carve(Carver{nullptr, 0})));
+    carve(Carver{static_cast<unsigned char*>(l->ws), 0});
     LAY_TRY(launch_fp4_quantize(l, type, T, D, x, ldx, codes, scales, st));
-    const NaiveArgs a = {codes, scales, static_cast<const uint8_t*>(w_codes), static_cast<const uint8_t*>(w_scales), static_cast<const uint16_t*>(bias),
-                         static_cast<const uint16_t*>(residual), static_cast<uint16_t*>(y), T, D, F, ldr, ldy, act, type == SOM_BF16, gated != 0};
-    const int64_t want = tiles_of(T * F, 8), most = (int64_t)l->sm_count * 64;
-    return outcome(l, launch(l, k_fp4_naive, dim3((unsigned)(want < most ? want : most)), 256, 0, st, 1, a));
+    p.x_codes = codes;
+    p.x_scales = scales;
+    return launch_fp4_product(l, p, parts, st);
 }
 
 }  // extern "C"

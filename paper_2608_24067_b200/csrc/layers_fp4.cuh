@@ -52,6 +52,19 @@ __device__ __forceinline__ uint32_t fp4_codes(const float (&v)[8])
 // smallest exponents, which 2^126 lifts to [0, 6].
 __device__ __forceinline__ float fp4_value(uint32_t code) { return __uint_as_float(((code & 7u) << 22) | ((code & 8u) << 28)) * 0x1p126f; }
 
+// A product of two matrices in 4 bits with som_linear's epilogue.
+struct Fp4Product {
+    const uint8_t *x_codes, *x_scales, *w_codes, *w_scales;
+    const uint16_t *bias, *residual;
+    uint16_t* y;
+    int64_t T, D, F, ldr, ldy;
+    int act, gated, bf16;
+};
+
+cudaError_t prepare_fp4_product(som_layers* l);  // once per handle
+size_t fp4_product_bytes(const som_layers* l, const Fp4Product& p);  // workspace
+int launch_fp4_product(som_layers* l, const Fp4Product& p, unsigned char* ws, cudaStream_t st);
+
 int launch_fp4_quantize(som_layers* l, int type, int64_t T, int64_t D, const void* x, int64_t ldx, uint8_t* codes, uint8_t* scales, cudaStream_t st);
 
 }  // namespace lay

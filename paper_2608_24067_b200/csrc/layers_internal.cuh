@@ -16,6 +16,7 @@ struct som_layers {
     int device;
     int sm_count;
     int pairs;  // pairs of blocks that the products' kernels can have resident
+    int fp4_pairs;  // the same of the 4-bit product
     void* ws;  // grow-only device workspace of all calls on the handle
     size_t ws_bytes;
     int* flags;  // device, sticky LAY_FLAG_* bits

@@ -195,6 +195,45 @@ __device__ __forceinline__ void mma(uint32_t d, uint64_t a, uint64_t b, uint32_t
             : "memory");
 }
 
+// The same for 4-bit operands with a power of two for each 32 k (kind::mxf4): 64 k.  The descriptor's `half` says which two of the four bytes in
+// a word of the scales in tensor memory are meant; word c of lane r is that of row r + 32 c (and so on in fours for rows from 128 on),
+// the same in all four quarters of the lanes.
+__host__ __device__ constexpr uint32_t mma_fp4_desc(int m, int n, int half)
+{
+    return ((uint32_t)(2 * half) << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(n >> 3) << 17) | (1u << 23) | ((uint32_t)(m >> 4) << 24) |
+           ((uint32_t)(2 * half) << 29);
+}
+
+template <bool PAIR>
+__device__ __forceinline__ void mma_fp4(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t scales_a, uint32_t scales_b, uint32_t accumulate)
+{
+    if (PAIR)
+        asm volatile(
+            "{\n\t.reg .pred p;\n\t"
+            "setp.ne.b32 p, %6, 0;\n\t"
+            "tcgen05.mma.cta_group::2.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}" ::"r"(d),
+            "l"(a), "l"(b), "r"(idesc), "r"(scales_a), "r"(scales_b), "r"(accumulate)
+            : "memory");
+    else
+        asm volatile(
+            "{\n\t.reg .pred p;\n\t"
+            "setp.ne.b32 p, %6, 0;\n\t"
+            "tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}" ::"r"(d),
+            "l"(a), "l"(b), "r"(idesc), "r"(scales_a), "r"(scales_b), "r"(accumulate)
+            : "memory");
+}
+
+// 512 bytes of scales, 16 of each of 32 lanes, from shared memory to four columns of tensor memory, in all four quarters of the lanes (with PAIR in
+// both blocks, each from its own shared memory at this address)
+template <bool PAIR>
+__device__ __forceinline__ void tmem_put_scales(uint32_t taddr, uint32_t addr)
+{
+    // rows of 16 bytes without a swizzle: groups of eight lie 128 bytes apart
+    const uint64_t desc = (uint64_t)((addr >> 4) & 0x3fffu) | (8ull << 32) | (1ull << 46);
+    if (PAIR) asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(desc) : "memory");
+    else asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(desc) : "memory");
+}
+
 // The barrier (with PAIR: of both blocks) gets an arrival when all earlier matrix instructions of this thread are done.
 template <bool PAIR>
 __device__ __forceinline__ void mma_commit(uint64_t* bar)

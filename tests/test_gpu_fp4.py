@@ -134,7 +134,14 @@ def test_activations_and_gates(L, T, D, F, act):
             check_layer(L, *layer(T, D, F, "bf16", gated, bias, residual), act=act, gated=gated)
 
 
-@pytest.mark.parametrize("T", [1, 7, 140])
+@pytest.mark.parametrize("kind", ["bf16", "fp16"])
+@pytest.mark.parametrize("T,D,F,gated", [(1500, 1056, 2056, False), (2900, 544, 3200, False), (1300, 512, 1024, True), (1409, 288, 1000, True), (5000, 256, 640, False), (2200, 2080, 2304, True)])
+def test_pairs_of_blocks(L, T, D, F, gated, kind):
+    """Tiles of 256 x 256, one to several rounds of them, with rows and columns that end inside a tile."""
+    check_layer(L, *layer(T, D, F, kind, gated, seed=T, wild=True), act="gelu" if T % 2 else "none", gated=gated)
+
+
+@pytest.mark.parametrize("T", [1, 7, 140, 6200])
 def test_no_column_of_the_weights_is_mixed_up(L, T):
     """Weights and rows with one block that counts: every block of every row meets its own scale."""
     D, F = 1088, 392
@@ -149,7 +156,7 @@ def test_no_column_of_the_weights_is_mixed_up(L, T):
     assert torch.equal(y, want.to(torch.bfloat16))
 
 
-@pytest.mark.parametrize("T", [1, 33, 300])
+@pytest.mark.parametrize("T", [1, 33, 300, 9700])
 def test_nan_stays_in_its_row(L, T):
     x, w, b, r = layer(T, 512, 256, "bf16")
     q = L.quantize_fp4(w)
@@ -170,7 +177,7 @@ def test_only_the_rows_are_written(L, T):
     assert bool((whole[:, :16] == 9).all()) and bool((whole[:, 280:] == 9).all()) and torch.equal(y, whole[:, 16:280])
 
 
-@pytest.mark.parametrize("T,D,F", [(1, 2048, 2048), (50, 2048, 512), (600, 1024, 1024)])
+@pytest.mark.parametrize("T,D,F", [(1, 2048, 2048), (50, 2048, 512), (600, 1024, 1024), (4000, 512, 2048)])
 def test_same_bits_every_time_and_in_a_graph(L, T, D, F):
     x, w, b, r = layer(T, D, F, "bf16")
     q = L.quantize_fp4(w)
