@@ -10,6 +10,7 @@ namespace {
 struct QuantArgs {
     const void* x;
     int64_t ldx, T, D;
+    uint32_t tiles, units;
     uint8_t *codes, *scales;
     int bf16;
 };
@@ -18,45 +19,78 @@ struct ValuesArgs {
     const uint8_t *codes, *scales;
     void* y;
     int64_t ldy, T, D;
+    uint32_t tiles, units;
     int bf16;
 };
 
-constexpr int Q_THREADS = 256;
+constexpr int Q_THREADS = 256, Q_ROWS = 4;
+
+// Unit u of the work: a tile of 256 columns of the rows row, row + 32, row + 64 and row + 96, whose bytes of scales lie next to each other.
+struct Unit {
+    int64_t row, tile;
+    __device__ __forceinline__ Unit(uint32_t u, uint32_t tiles)
+    {
+        const uint32_t r = u / tiles;
+        tile = u - r * tiles;
+        row = (int64_t)(r >> 5) * 128 + (r & 31);
+    }
+};
 
 template <bool WIDE>
 __global__ void __launch_bounds__(Q_THREADS) k_fp4_quantize(const QuantArgs a)
 {
     enter();
     const int lane = threadIdx.x & 31;
-    const int64_t tiles = fp4_tiles(a.D), warps = a.T * tiles;
-    for (int64_t i = ((int64_t)blockIdx.x * Q_THREADS + threadIdx.x) >> 5; i < warps; i += (int64_t)gridDim.x * (Q_THREADS / 32)) {
-        const int64_t row = i / tiles, tile = i - row * tiles, col = tile * 256 + lane * 8;
+    for (uint32_t u = (blockIdx.x * Q_THREADS + threadIdx.x) >> 5; u < a.units; u += gridDim.x * (Q_THREADS / 32)) {
+        const Unit at(u, a.tiles);
+        const int64_t col = at.tile * 256 + lane * 8;
         const bool in = col < a.D;
-        float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-        if (in) {
-            if (WIDE) {
-                const float4* p = reinterpret_cast<const float4*>(static_cast<const float*>(a.x) + row * a.ldx + col);
-                const float4 x0 = p[0], x1 = p[1];
-                v[0] = x0.x, v[1] = x0.y, v[2] = x0.z, v[3] = x0.w, v[4] = x1.x, v[5] = x1.y, v[6] = x1.z, v[7] = x1.w;
+        float v[Q_ROWS][8];
+#pragma unroll
+        for (int i = 0; i < Q_ROWS; ++i) {
+            const int64_t row = at.row + 32 * i;
+            if (in && row < a.T) {
+                if (WIDE) {
+                    const float4* p = reinterpret_cast<const float4*>(static_cast<const float*>(a.x) + row * a.ldx + col);
+                    const float4 x0 = p[0], x1 = p[1];
+                    v[i][0] = x0.x, v[i][1] = x0.y, v[i][2] = x0.z, v[i][3] = x0.w, v[i][4] = x1.x, v[i][5] = x1.y, v[i][6] = x1.z, v[i][7] = x1.w;
+                } else {
+                    load8(static_cast<const uint16_t*>(a.x) + row * a.ldx + col, v[i], a.bf16);
+                }
             } else {
-                load8(static_cast<const uint16_t*>(a.x) + row * a.ldx + col, v, a.bf16);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[i][j] = 0.f;
             }
         }
-        uint32_t most = 0;
+        uint32_t four[Q_ROWS];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) most = max(most, __float_as_uint(v[j]) & 0x7fffffffu);
-        most = max(most, __shfl_xor_sync(0xffffffffu, most, 1));
-        most = max(most, __shfl_xor_sync(0xffffffffu, most, 2));
-        const uint32_t e = fp4_scale_of(most);
-        const float by = fp4_inverse(e);
+        for (int i = 0; i < Q_ROWS; ++i) {
+            uint32_t most = 0;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] *= by;
-        if (in) *reinterpret_cast<uint32_t*>(a.codes + (row * a.D + col) / 2) = e == 255u ? 0u : fp4_codes(v);
-        // four blocks' bytes lie next to each other
-        uint32_t four = e << (8 * ((lane >> 2) & 3));
-        four |= __shfl_xor_sync(0xffffffffu, four, 4);
-        four |= __shfl_xor_sync(0xffffffffu, four, 8);
-        if ((lane & 15) == 0) *reinterpret_cast<uint32_t*>(a.scales + fp4_scale_at(row, tile * 8 + lane / 4, tiles)) = four;
+            for (int j = 0; j < 8; ++j) most = max(most, __float_as_uint(v[i][j]) & 0x7fffffffu);
+            most = max(most, __shfl_xor_sync(0xffffffffu, most, 1));
+            most = max(most, __shfl_xor_sync(0xffffffffu, most, 2));
+            const uint32_t e = fp4_scale_of(most);
+            const float by = fp4_inverse(e);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[i][j] *= by;
+            const int64_t row = at.row + 32 * i;
+            if (in && row < a.T) *reinterpret_cast<uint32_t*>(a.codes + (row * a.D + col) / 2) = e == 255u ? 0u : fp4_codes(v[i]);
+            // four blocks' bytes lie next to each other
+            four[i] = e << (8 * ((lane >> 2) & 3));
+            four[i] |= __shfl_xor_sync(0xffffffffu, four[i], 4);
+            four[i] |= __shfl_xor_sync(0xffffffffu, four[i], 8);
+        }
+        if ((lane & 15) == 0) {
+            uint32_t* to = reinterpret_cast<uint32_t*>(a.scales + fp4_scale_at(at.row, at.tile * 8 + lane / 4, a.tiles));
+            if (at.row + 96 < a.T) {
+                *reinterpret_cast<uint4*>(to) = make_uint4(four[0], four[1], four[2], four[3]);
+            } else {
+#pragma unroll
+                for (int i = 0; i < Q_ROWS; ++i)
+                    if (at.row + 32 * i < a.T) to[i] = four[i];
+            }
+        }
     }
 }
 
@@ -65,36 +99,54 @@ __global__ void __launch_bounds__(Q_THREADS) k_fp4_values(const ValuesArgs a)
 {
     enter();
     const int lane = threadIdx.x & 31;
-    const int64_t tiles = fp4_tiles(a.D), warps = a.T * tiles;
-    for (int64_t i = ((int64_t)blockIdx.x * Q_THREADS + threadIdx.x) >> 5; i < warps; i += (int64_t)gridDim.x * (Q_THREADS / 32)) {
-        const int64_t row = i / tiles, tile = i - row * tiles, col = tile * 256 + lane * 8;
+    for (uint32_t u = (blockIdx.x * Q_THREADS + threadIdx.x) >> 5; u < a.units; u += gridDim.x * (Q_THREADS / 32)) {
+        const Unit at(u, a.tiles);
+        const int64_t col = at.tile * 256 + lane * 8;
         if (col >= a.D) continue;
-        const uint32_t w = *reinterpret_cast<const uint32_t*>(a.codes + (row * a.D + col) / 2);
-        const float by = fp4_power(a.scales[fp4_scale_at(row, tile * 8 + lane / 4, tiles)]);
-        float v[8];
+        uint32_t w[Q_ROWS];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = fp4_value(w >> (4 * j)) * by;
-        if (WIDE) {
-            float4* p = reinterpret_cast<float4*>(static_cast<float*>(a.y) + row * a.ldy + col);
-            p[0] = make_float4(v[0], v[1], v[2], v[3]);
-            p[1] = make_float4(v[4], v[5], v[6], v[7]);
-        } else {
-            *reinterpret_cast<uint4*>(static_cast<uint16_t*>(a.y) + row * a.ldy + col) =
-                make_uint4(pack2(v[0], v[1], a.bf16), pack2(v[2], v[3], a.bf16), pack2(v[4], v[5], a.bf16), pack2(v[6], v[7], a.bf16));
+        for (int i = 0; i < Q_ROWS; ++i)
+            w[i] = at.row + 32 * i < a.T ? *reinterpret_cast<const uint32_t*>(a.codes + ((at.row + 32 * i) * a.D + col) / 2) : 0u;
+        // (the bytes of rows beyond the last are there, and not used)
+        const uint4 e = *reinterpret_cast<const uint4*>(a.scales + fp4_scale_at(at.row, (at.tile * 8 + lane / 4) & ~3, a.tiles));
+        const uint32_t es[Q_ROWS] = {e.x, e.y, e.z, e.w};
+#pragma unroll
+        for (int i = 0; i < Q_ROWS; ++i) {
+            const int64_t row = at.row + 32 * i;
+            if (row >= a.T) break;
+            const float by = fp4_power((es[i] >> (8 * ((lane >> 2) & 3))) & 255u);
+            float v[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = fp4_value(w[i] >> (4 * j)) * by;
+            if (WIDE) {
+                float4* p = reinterpret_cast<float4*>(static_cast<float*>(a.y) + row * a.ldy + col);
+                p[0] = make_float4(v[0], v[1], v[2], v[3]);
+                p[1] = make_float4(v[4], v[5], v[6], v[7]);
+            } else {
+                *reinterpret_cast<uint4*>(static_cast<uint16_t*>(a.y) + row * a.ldy + col) =
+                    make_uint4(pack2(v[0], v[1], a.bf16), pack2(v[2], v[3], a.bf16), pack2(v[4], v[5], a.bf16), pack2(v[6], v[7], a.bf16));
+            }
         }
     }
 }
 
-unsigned blocks_for(const som_layers* l, int64_t warps)
+// units of T rows: 32 of every 128 rows, or as many as there are
+uint32_t units_of(int64_t T, int64_t D)
 {
-    const int64_t want = tiles_of(warps, Q_THREADS / 32), most = (int64_t)l->sm_count * 64;
+    const int64_t rest = T % 128;
+    return (uint32_t)((T / 128 * 32 + (rest < 32 ? rest : 32)) * fp4_tiles(D));
+}
+
+unsigned blocks_for(const som_layers* l, uint32_t units)
+{
+    const int64_t want = tiles_of(units, Q_THREADS / 32), most = (int64_t)l->sm_count * 64;
     return (unsigned)(want < most ? want : most);
 }
 
 int check_fp4(const som_layers* l, int type, int64_t T, int64_t D)
 {
     if (!l || T < 0 || D <= 0 || type < SOM_F32 || type > SOM_BF16) return SOM_ERR_INVALID_ARG;
-    return T >= MOST_ROWS || D > MOST_COLS || D % FP4_BLOCK != 0 ? SOM_ERR_UNSUPPORTED : SOM_OK;
+    return T >= MOST_ROWS || D > MOST_COLS || D % FP4_BLOCK != 0 || T * fp4_tiles(D) >= (int64_t)1 << 33 ? SOM_ERR_UNSUPPORTED : SOM_OK;
 }
 
 int check_rows_of(int type, const void* p, int64_t ld, int64_t D, int64_t T)
@@ -115,8 +167,8 @@ int check_quantized(const void* codes, const void* scales, int64_t rows)
 
 int launch_fp4_quantize(som_layers* l, int type, int64_t T, int64_t D, const void* x, int64_t ldx, uint8_t* codes, uint8_t* scales, cudaStream_t st)
 {
-    const QuantArgs a = {x, ldx, T, D, codes, scales, type == SOM_BF16};
-    const dim3 grid(blocks_for(l, T * fp4_tiles(D)));
+    const QuantArgs a = {x, ldx, T, D, (uint32_t)fp4_tiles(D), units_of(T, D), codes, scales, type == SOM_BF16};
+    const dim3 grid(blocks_for(l, a.units));
     return outcome(l, type == SOM_F32 ? launch(l, k_fp4_quantize<true>, grid, Q_THREADS, 0, st, 1, a) : launch(l, k_fp4_quantize<false>, grid, Q_THREADS, 0, st, 1, a));
 }
 
@@ -149,8 +201,8 @@ int som_fp4_values(som_layers* l, int type, int64_t T, int64_t D, const void* co
     if (T == 0) return SOM_OK;
     Guard g(l->device);
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
-    const ValuesArgs a = {static_cast<const uint8_t*>(codes), static_cast<const uint8_t*>(scales), y, ldy, T, D, type == SOM_BF16};
-    const dim3 grid(blocks_for(l, T * fp4_tiles(D)));
+    const ValuesArgs a = {static_cast<const uint8_t*>(codes), static_cast<const uint8_t*>(scales), y, ldy, T, D, (uint32_t)fp4_tiles(D), units_of(T, D), type == SOM_BF16};
+    const dim3 grid(blocks_for(l, a.units));
     return outcome(l, type == SOM_F32 ? launch(l, k_fp4_values<true>, grid, Q_THREADS, 0, st, 1, a) : launch(l, k_fp4_values<false>, grid, Q_THREADS, 0, st, 1, a));
 }
 

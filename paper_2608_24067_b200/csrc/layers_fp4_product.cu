@@ -2,14 +2,14 @@
 //
 // Persistent blocks walk the output tiles as the 16-bit products do (layers_product.cu): warp 0 issues the TMA copies of a ring, warp 1 the
 // matrix instructions, eight warps run the epilogue; every wait is bounded.  A stage holds 256 k of both operands (rows of 128 bytes) and their
-// scales, 1 KB for 128 rows as they lie in memory; four copies of scales a stage from shared to tensor memory (tcgen05.cp)
-// go in front of the four instructions that use them, into two sets in turn, each free when the stage before the last is done.
+// scales, 1 KB for 128 rows as they lie in memory; copies from shared to tensor memory (tcgen05.cp) bring the scales in front of the
+// instructions that use them, a set of columns for each place of the ring.
 //
 // PAIR: 256 x 256 tiles by two blocks of a cluster (cta_group::2); each loads its own 128 rows of A, one half of B, and the scales of its rows of
 // A and of all of B.  A pair's instruction takes 4 bits four times as fast as 16, and a stage's bytes last as long as a
 // 16-bit stage's.  Two accumulators of 256 columns and the scales are more than the 512 columns of tensor memory, so the
-// second accumulator lies over the last columns of the first: the warps that own those read them into registers first, and the next
-// tile's products begin when they have.  NARROW: 128 x 128 by one block, for products with few tiles; where SMs still idle the sum is
+// second accumulator lies over the last 128 columns of the first: the epilogue reads those into registers first, and the next
+// tile's products begin when it has.  NARROW: 128 x 128 by one block, for products with few tiles; where SMs still idle the sum is
 // split over blocks, which leave fp32 parts for k_finish.
 #include "layers_epilogue.cuh"
 #include "layers_finish.cuh"
@@ -64,11 +64,10 @@ template <bool PAIRED, bool OUT32, bool BF16>
 __global__ void __launch_bounds__(THREADS, 1) k_fp4_product(const __grid_constant__ Fp4Args p)
 {
     constexpr int BN = PAIRED ? 256 : 128;
-    constexpr uint32_t SECOND = PAIRED ? 208 : 128;   // columns of the second accumulator
-    constexpr uint32_t SCALES = PAIRED ? 464 : 256, SCALES_A = 8, SCALES_SET = SCALES_A + BN / 16;  // and of the scales
-    constexpr uint32_t SHARED = PAIRED ? 256 - SECOND : 0;  // that both accumulators have
-    static_assert(SCALES + 2 * SCALES_SET <= 512 && SECOND + BN <= SCALES, "tensor memory");
-    static_assert(SHARED <= 64, "what lies over one another is in one piece");
+    constexpr uint32_t SECOND = 128;  // first column of the second accumulator: of a pair's 256 columns half lie over the first one's
+    constexpr uint32_t SCALES = SECOND + BN, SCALES_A = 8, SCALES_SET = SCALES_A + BN / 16;  // and of the stages' scales
+    static_assert(SCALES + STAGES * SCALES_SET <= 512, "tensor memory");
+    static_assert(!PAIRED || BN - SECOND <= EPI_TURNS * 64, "the epilogue's first pieces hold what lies over one another");
     extern __shared__ unsigned char smem_raw[];
     __shared__ __align__(8) uint64_t full[STAGES], empty[STAGES], acc_full[2], acc_free[2], drained;
     __shared__ uint32_t tmem_sh;
@@ -171,61 +170,63 @@ __global__ void __launch_bounds__(THREADS, 1) k_fp4_product(const __grid_constan
             }
         }
     } else if (warp == 1) {
-        if (lane == 0 && rank == 0) {
+        // The whole warp walks the stages and one lane issues: addresses and descriptors then stay in the warp's own registers.  With one
+        // lane alone in the loop an instruction took 60 to 70 clocks to issue, 940 a stage: 8192 x 16384 x 4096 took 239 us.
+        if (rank == 0) {
             int stage = 0, n_acc = 0;
             uint32_t phase = 0;
-            int64_t done = 0;  // stages so far
             bool ok = true;
+            const bool lead = elect_lane();
             constexpr uint32_t idesc[2] = {mma_fp4_desc(PAIRED ? 256 : 128, BN, 0), mma_fp4_desc(PAIRED ? 256 : 128, BN, 1)};
             for (int idx = first_tile; ok && idx < total; idx += step, ++n_acc) {
                 const Tile t = tile_at<PAIRED>(p, idx, width, rank);
                 const int buf = n_acc & 1;
                 const uint32_t d = tmem + (buf ? SECOND : 0u);
-                // PAIR: the tile before has left the columns that both have (and so the tile before that all of its own); else this buffer is read
+                // a pair's tile before has left the columns that both have (and the one before that all of its own); else this buffer has been read
                 if (PAIRED) {
                     if (n_acc > 0) ok = bar_wait<true>(&acc_free[buf ^ 1], (uint32_t)((n_acc - 1) >> 1) & 1u, gave_up);
                 } else if (n_acc > 1) {
                     ok = bar_wait(&acc_free[buf], (uint32_t)((n_acc >> 1) - 1) & 1u, gave_up);
                 }
+                ok = __all_sync(0xffffffffu, ok);  // all go on or all leave
                 tc_fence_after();
-                for (int it = 0; ok && it < t.n; ++it, ++done) {
-                    if (!bar_wait(&full[stage], phase, gave_up)) {
-                        ok = false;
-                        break;
-                    }
-                    // the set of scales was used two stages ago
-                    const int64_t last = done - 2;
-                    if (last >= 0 && !bar_wait(&empty[last % STAGES], (uint32_t)(last / STAGES) & 1u, gave_up)) {
-                        ok = false;
-                        break;
-                    }
+                for (int it = 0; ok && it < t.n; ++it) {
+                    ok = __all_sync(0xffffffffu, bar_wait(&full[stage], phase, gave_up));
+                    if (!ok) break;
                     tc_fence_after();
-                    const uint32_t sa = smem_addr(ring + stage * STAGE_BYTES), sb = sa + PART_BYTES, ss = smem_addr(scales + stage * SCALE_BYTES);
-                    const uint32_t ta = tmem + SCALES + (uint32_t)(done & 1) * SCALES_SET, tb = ta + SCALES_A;
+                    const uint32_t sa = smem_addr(ring) + stage * STAGE_BYTES, sb = sa + PART_BYTES, ss = smem_addr(scales) + stage * SCALE_BYTES;
+                    // A stage's scales have a set of columns for each place of the ring: what used it is done when the place is loaded again.
+                    // (The next stage's in front of this stage's instructions, where it is here, was slower.)
+                    const uint32_t ta = tmem + SCALES + stage * SCALES_SET, tb = ta + SCALES_A;
+                    if (lead) {
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        tmem_put_scales<PAIRED>(ta + 4 * h, ss + 512 * h);
+                        for (int h = 0; h < 2; ++h) {
+                            tmem_put_scales<PAIRED>(ta + 4 * h, ss + 512 * h);
 #pragma unroll
-                        for (int c = 0; c < BN / 128; ++c) tmem_put_scales<PAIRED>(tb + h * (BN / 32) + 4 * c, ss + FP4_SCALE_TILE * (1 + c) + 512 * h);
+                            for (int c = 0; c < BN / 128; ++c) tmem_put_scales<PAIRED>(tb + h * (BN / 32) + 4 * c, ss + FP4_SCALE_TILE * (1 + c) + 512 * h);
+                        }
+#pragma unroll
+                        for (int kk = 0; kk < STEPS; ++kk)
+                            mma_fp4<PAIRED>(d, mat_desc(sa + kk * 32, 16, 1024), mat_desc(sb + kk * 32, 16, 1024), idesc[kk & 1], ta + 4 * (kk >> 1), tb + (kk >> 1) * (BN / 32),
+                                            !(it == 0 && kk == 0));
+                        mma_commit<PAIRED>(&empty[stage]);
                     }
-#pragma unroll
-                    for (int kk = 0; kk < STEPS; ++kk)
-                        mma_fp4<PAIRED>(d, mat_desc(sa + kk * 32, 16, 1024), mat_desc(sb + kk * 32, 16, 1024), idesc[kk & 1], ta + 4 * (kk >> 1), tb + (kk >> 1) * (BN / 32),
-                                        !(it == 0 && kk == 0));
-                    mma_commit<PAIRED>(&empty[stage]);
+                    __syncwarp();
                     if (++stage == STAGES) {
                         stage = 0;
                         phase ^= 1u;
                     }
                 }
                 if (!ok) break;
-                mma_commit<PAIRED>(&acc_full[buf]);
+                if (lead) mma_commit<PAIRED>(&acc_full[buf]);
+                __syncwarp();
             }
-            if (!ok) {  // instructions in flight read shared memory and write tensor memory
+            if (!ok && lead) {  // instructions in flight read shared memory and write tensor memory
                 mma_commit<PAIRED>(&drained);
                 const long long t0 = clock64();
                 while (!bar_try(&drained, 0) && clock64() - t0 < WAIT_CYCLES) {}
             }
+            __syncwarp();
         }
     } else {
         // A warp may read the 32 lanes of its quarter only; the two warps of a quarter take pieces of 64 columns (fp32: 32) in turn.
@@ -280,7 +281,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_fp4_product(const __grid_constan
                         if (gated) tmem_ld(acc + BN / 2 + at + 32 * h, u[h]);
                     }
                     tmem_wait_ld();
-                    // Only the first piece holds shared columns.  (Gated, a warp has one piece.)
+                    // Only first pieces hold shared columns.  (Gated, a warp has one piece.)
                     if (PAIRED && !left) {
                         leave();
                         left = true;

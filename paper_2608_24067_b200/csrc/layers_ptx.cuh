@@ -16,6 +16,18 @@ __device__ __forceinline__ uint32_t smem_addr(const void* p)
     return (uint32_t)__cvta_generic_to_shared(p);
 }
 
+// One lane of a converged warp.
+__device__ __forceinline__ bool elect_lane()
+{
+    uint32_t mine;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "elect.sync _|p, 0xffffffff;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(mine));
+    return mine != 0;
+}
+
 __device__ __forceinline__ void bar_init(uint64_t* bar, uint32_t count)
 {
     asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(smem_addr(bar)), "r"(count));
