@@ -59,8 +59,10 @@ __device__ __forceinline__ Tile tile_at(const Fp4Args& p, int idx, int width, in
     return t;
 }
 
-// OUT32: fp32 parts without an epilogue (NARROW)
-template <bool PAIRED, bool OUT32, bool BF16>
+// What a kernel makes of the sums: outputs, outputs of features with a gate (pairs), fp32 parts without an epilogue (single blocks).
+enum Ends { PLAIN = 0, GATED = 1, PARTS = 2 };
+
+template <bool PAIRED, int ENDS, bool BF16>
 __global__ void __launch_bounds__(THREADS, 1) k_fp4_product(const __grid_constant__ Fp4Args p)
 {
     constexpr int BN = PAIRED ? 256 : 128;
@@ -104,8 +106,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_fp4_product(const __grid_constan
     const uint32_t tmem = tmem_sh;
     volatile int* gave_up = &gave_up_sh;
 
-    const bool gated = p.gate_rows != 0;
-    const int width = gated ? BN / 2 : BN;  // output columns of a tile
+    constexpr int WIDTH = ENDS == GATED ? BN / 2 : BN;  // output columns of a tile
     const int step = PAIRED ? gridDim.x >> 1 : gridDim.x, first_tile = PAIRED ? blockIdx.x >> 1 : blockIdx.x;
     const int total = p.row_tiles * p.col_tiles * p.splits;
 
@@ -120,10 +121,10 @@ __global__ void __launch_bounds__(THREADS, 1) k_fp4_product(const __grid_constan
                 const uint32_t bar = full0 + 8 * s;
                 const int k = (t.from + it) * (BK / 4);
                 if (rank == 0) bar_expect(&full[s], BYTES);
-                if (!gated) {
+                if (ENDS != GATED) {
                     tma_load<PAIRED>(sb, &p.b, bar, k, t.col + rank * SHARE, 0);
                     tma_load<PAIRED>(ss, &p.sb, bar, 0, t.from + it, t.col / 128);
-                } else if (PAIRED) {  // the first block has the gate's rows, the second the others
+                } else {  // the first block has the gate's rows, the second the others
                     tma_load<PAIRED>(sb, &p.b, bar, k, t.col + rank * p.gate_rows, 0);
                     tma_load<PAIRED>(ss, &p.sb, bar, 0, t.from + it, t.col / 128);
                     tma_load<PAIRED>(ss + FP4_SCALE_TILE, &p.sb, bar, 0, t.from + it, (t.col + p.gate_rows) / 128);
@@ -140,12 +141,12 @@ __global__ void __launch_bounds__(THREADS, 1) k_fp4_product(const __grid_constan
             bool ok = true;
             // The weights were complete before the kernel in front (x's quantisation, which the same call launched) began its work.
             if (first_tile < total) {
-                const Tile t = tile_at<PAIRED>(p, first_tile, width, rank);
+                const Tile t = tile_at<PAIRED>(p, first_tile, WIDTH, rank);
                 for (; ahead < STAGES && ahead < t.n; ++ahead) load_columns(t, ahead, ahead);
             }
             enter();
             for (int idx = first_tile; ok && idx < total; idx += step) {
-                const Tile t = tile_at<PAIRED>(p, idx, width, rank);
+                const Tile t = tile_at<PAIRED>(p, idx, WIDTH, rank);
                 for (int it = 0; it < t.n; ++it) {
                     if (!bar_wait(&empty[stage], phase ^ 1u, gave_up)) {
                         ok = false;
@@ -179,7 +180,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_fp4_product(const __grid_constan
             const bool lead = elect_lane();
             constexpr uint32_t idesc[2] = {mma_fp4_desc(PAIRED ? 256 : 128, BN, 0), mma_fp4_desc(PAIRED ? 256 : 128, BN, 1)};
             for (int idx = first_tile; ok && idx < total; idx += step, ++n_acc) {
-                const Tile t = tile_at<PAIRED>(p, idx, width, rank);
+                const Tile t = tile_at<PAIRED>(p, idx, WIDTH, rank);
                 const int buf = n_acc & 1;
                 const uint32_t d = tmem + (buf ? SECOND : 0u);
                 // a pair's tile before has left the columns that both have (and the one before that all of its own); else this buffer has been read
@@ -232,22 +233,31 @@ __global__ void __launch_bounds__(THREADS, 1) k_fp4_product(const __grid_constan
         // A warp may read the 32 lanes of its quarter only; the two warps of a quarter take pieces of 64 columns (fp32: 32) in turn.
         const int q = warp & 3, turn = (warp - 2) >> 2;
         Stager<1> s{staged + (warp - 2) * OUT_BYTES, lane, OUT_BYTES};
-        constexpr int PIECE = OUT32 ? 32 : 64;
+        constexpr int PIECE = ENDS == PARTS ? 32 : 64, PIECES = WIDTH / PIECE;
+        constexpr int AHEAD = ENDS == GATED ? 16 : 64;  // columns whose bias and residual are fetched at once (gated, the sums take twice the registers)
         int n_acc = 0;
         for (int idx = first_tile; idx < total; idx += step, ++n_acc) {
-            const Tile t = tile_at<PAIRED>(p, idx, width, rank);
+            const Tile t = tile_at<PAIRED>(p, idx, WIDTH, rank);
             const int buf = n_acc & 1;
             const uint32_t acc = tmem + (buf ? SECOND : 0u) + ((uint32_t)(32 * q) << 16);
             const int row0 = t.row + 32 * q, row = row0 + lane;
             const bool counts = row < p.rows;
-            const uint16_t* extra = p.residual ? p.residual + (size_t)row * p.ldr : nullptr;
-            const int pieces = width / PIECE;
+            const uint16_t* extra = ENDS != PARTS && p.residual ? p.residual + (size_t)row * p.ldr : nullptr;
             // The first accumulator shares its last columns, the second its first: the pieces run from there.
             const bool down = PAIRED && buf == 0;
-            auto piece_at = [&](int j) { return (down ? pieces - 1 - j : j) * PIECE; };
-            if (extra && counts && !OUT32)
-                for (int j = turn; j < pieces; j += EPI_TURNS)
-                    if (t.col + piece_at(j) < p.cols) prefetch_l2(extra + t.col + piece_at(j));
+            auto piece_at = [&](int j) { return (down ? PIECES - 1 - j : j) * PIECE; };
+            RowPart<AHEAD> add, b0, b1;
+            auto fetch = [&](int col) {
+                add.fetch(extra, col, p.cols, extra && counts);
+                b0.fetch(p.bias, col, p.cols, p.bias);
+                if (ENDS == GATED) b1.fetch(p.bias + p.gate_rows, col, p.cols, p.bias);
+            };
+            if (ENDS != PARTS) {  // the first piece's while the products still run, the others' on the way to L2
+                fetch(t.col + piece_at(turn));
+                if (extra && counts)
+                    for (int j = turn + EPI_TURNS; j < PIECES; j += EPI_TURNS)
+                        if (t.col + piece_at(j) < p.cols) prefetch_l2(extra + t.col + piece_at(j));
+            }
             // One lane waits, the others for it at a hardware barrier; all go on or all leave by the word that it writes (two words in turn).
             if (warp == 2 && lane == 0) summed[buf] = bar_wait(&acc_full[buf], (uint32_t)(n_acc >> 1) & 1u, gave_up);
             asm volatile("bar.sync 1, %0;" ::"n"(32 * EPI_WARPS) : "memory");
@@ -261,65 +271,59 @@ __global__ void __launch_bounds__(THREADS, 1) k_fp4_product(const __grid_constan
                     else bar_arrive(&acc_free[buf]);
                 }
             };
-            bool left = false;
-#pragma unroll 1
-            for (int j = turn; j < pieces; j += EPI_TURNS) {
-                const int at = piece_at(j), col = t.col + at;
-                if constexpr (OUT32) {
+            static_assert(PIECES % EPI_TURNS == 0, "every warp has pieces");
+#pragma unroll
+            for (int i = 0; i < PIECES / EPI_TURNS; ++i) {
+                const int at = piece_at(turn + i * EPI_TURNS), col = t.col + at;
+                const bool last = i + 1 == PIECES / EPI_TURNS;
+                if constexpr (ENDS == PARTS) {
                     float v[32];
                     tmem_ld(acc + at, v);
                     tmem_wait_ld();
+                    if (last) leave();
                     s.begin();
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) s.put(i, v + 4 * i);
+                    for (int c = 0; c < 8; ++c) s.put(c, v + 4 * c);
                     s.send(&p.o, col, row0, t.split, p.rows, p.cols);
                 } else {
                     float v[2][32], u[2][32];
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
                         tmem_ld(acc + at + 32 * h, v[h]);
-                        if (gated) tmem_ld(acc + BN / 2 + at + 32 * h, u[h]);
+                        if (ENDS == GATED) tmem_ld(acc + BN / 2 + at + 32 * h, u[h]);
                     }
+                    if (i > 0) fetch(col);
                     tmem_wait_ld();
-                    // Only first pieces hold shared columns.  (Gated, a warp has one piece.)
-                    if (PAIRED && !left) {
-                        leave();
-                        left = true;
-                    }
+                    if (PAIRED ? i == 0 : last) leave();  // (only first pieces hold shared columns; gated, a warp has one piece)
                     s.begin();
 #pragma unroll
                     for (int c = 0; c < 4; ++c) {
                         float(&z)[16] = reinterpret_cast<float(&)[16]>(v[c / 2][16 * (c & 1)]);
                         float(&w)[16] = reinterpret_cast<float(&)[16]>(u[c / 2][16 * (c & 1)]);
-                        RowPart<16> b;
+                        constexpr int OF = AHEAD / 16;  // steps of 16 columns that were fetched at once
+                        const RowPart<16>&add16 = reinterpret_cast<const RowPart<16>*>(&add)[c % OF], &b016 = reinterpret_cast<const RowPart<16>*>(&b0)[c % OF],
+                              &b116 = reinterpret_cast<const RowPart<16>*>(&b1)[c % OF];
                         if (p.bias) {
-                            b.fetch(p.bias, col + 16 * c, p.cols, true);
-                            b.template add<BF16>(z);
-                            if (gated) {
-                                b.fetch(p.bias + p.gate_rows, col + 16 * c, p.cols, true);
-                                b.template add<BF16>(w);
-                            }
+                            b016.template add<BF16>(z);
+                            if (ENDS == GATED) b116.template add<BF16>(w);
                         }
                         if (p.act != SOM_ACT_NONE)
                             with_act(p.act, [&](auto tag) {
 #pragma unroll
-                                for (int i = 0; i < 16; ++i) z[i] = act_of<decltype(tag)::value>(z[i]);
+                                for (int k = 0; k < 16; ++k) z[k] = act_of<decltype(tag)::value>(z[k]);
                             });
-                        if (gated) {
+                        if (ENDS == GATED) {
 #pragma unroll
-                            for (int i = 0; i < 16; ++i) z[i] *= w[i];
+                            for (int k = 0; k < 16; ++k) z[k] *= w[k];
                         }
-                        if (extra) {
-                            b.fetch(extra, col + 16 * c, p.cols, counts);
-                            b.template add<BF16>(z);
-                        }
+                        if (extra) add16.template add<BF16>(z);
+                        if (OF == 1 && c < 3) fetch(col + 16 * (c + 1));
                         s.put(2 * c, pack8<BF16>(z));
                         s.put(2 * c + 1, pack8<BF16>(z + 8));
                     }
                     s.send(&p.o, col, row0, 0, p.rows, p.cols);
                 }
             }
-            if (!left) leave();
         }
     }
     if (warp >= 2 && lane == 0) store_wait_all();
@@ -376,32 +380,26 @@ Cut cut_of(const som_layers* l, const Fp4Product& p)
     return c;
 }
 
-template <bool PAIRED, bool OUT32>
+dim3 grid_of(const som_layers* l, const Fp4Args& a, bool paired)
+{
+    const int64_t tiles = (int64_t)a.row_tiles * a.col_tiles * a.splits, most = paired ? l->fp4_pairs : l->sm_count;
+    return dim3((unsigned)((tiles < most ? tiles : most) * (paired ? 2 : 1)));
+}
+
+template <bool PAIRED, int ENDS>
 cudaError_t launch_as(som_layers* l, const Fp4Args& a, bool bf16, cudaStream_t st)
 {
-    const int64_t tiles = (int64_t)a.row_tiles * a.col_tiles * a.splits;
-    const int most = PAIRED ? l->fp4_pairs : l->sm_count, blocks = PAIRED ? 2 : 1;
-    const dim3 grid((unsigned)((tiles < most ? tiles : most) * blocks));
-    return bf16 ? launch(l, k_fp4_product<PAIRED, OUT32, true>, grid, THREADS, SMEM, st, blocks, a)
-                : launch(l, k_fp4_product<PAIRED, OUT32, false>, grid, THREADS, SMEM, st, blocks, a);
+    const dim3 grid = grid_of(l, a, PAIRED);
+    return bf16 ? launch(l, k_fp4_product<PAIRED, ENDS, true>, grid, THREADS, SMEM, st, PAIRED ? 2 : 1, a)
+                : launch(l, k_fp4_product<PAIRED, ENDS, false>, grid, THREADS, SMEM, st, PAIRED ? 2 : 1, a);
 }
 
-template <bool PAIRED, bool OUT32, bool BF16>
-cudaError_t prepare_as()
+// (and, of pairs, how many can be resident)
+template <bool PAIRED, int ENDS, bool BF16>
+cudaError_t prepare_as(int* pairs)
 {
-    return cudaFuncSetAttribute(k_fp4_product<PAIRED, OUT32, BF16>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM);
-}
-
-}  // namespace
-
-cudaError_t prepare_fp4_product(som_layers* l)
-{
-    cudaError_t e = prepare_as<false, false, true>();
-    if (e == cudaSuccess) e = prepare_as<false, false, false>();
-    if (e == cudaSuccess) e = prepare_as<false, true, true>();
-    if (e == cudaSuccess) e = prepare_as<true, false, true>();
-    if (e == cudaSuccess) e = prepare_as<true, false, false>();
-    if (e != cudaSuccess) return e;
+    const cudaError_t e = cudaFuncSetAttribute(k_fp4_product<PAIRED, ENDS, BF16>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM);
+    if (e != cudaSuccess || !PAIRED) return e;
     cudaLaunchConfig_t c = {};
     c.gridDim = dim3(2);
     c.blockDim = dim3(THREADS);
@@ -412,13 +410,26 @@ cudaError_t prepare_fp4_product(som_layers* l)
     attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
     c.attrs = attr;
     c.numAttrs = 1;
-    l->fp4_pairs = l->sm_count / 2;
     int n = 0;
-    e = cudaOccupancyMaxActiveClusters(&n, k_fp4_product<true, false, true>, &c);
-    if (n < l->fp4_pairs) l->fp4_pairs = n;
-    if (e == cudaSuccess) e = cudaOccupancyMaxActiveClusters(&n, k_fp4_product<true, false, false>, &c);
-    if (n < l->fp4_pairs) l->fp4_pairs = n;
-    return e == cudaSuccess && l->fp4_pairs < 1 ? cudaErrorNotSupported : e;
+    const cudaError_t f = cudaOccupancyMaxActiveClusters(&n, k_fp4_product<PAIRED, ENDS, BF16>, &c);
+    if (n < *pairs) *pairs = n;
+    return f;
+}
+
+}  // namespace
+
+cudaError_t prepare_fp4_product(som_layers* l)
+{
+    int n = l->sm_count / 2;
+    cudaError_t e = prepare_as<false, PLAIN, true>(&n);
+    if (e == cudaSuccess) e = prepare_as<false, PLAIN, false>(&n);
+    if (e == cudaSuccess) e = prepare_as<false, PARTS, true>(&n);
+    if (e == cudaSuccess) e = prepare_as<true, PLAIN, true>(&n);
+    if (e == cudaSuccess) e = prepare_as<true, PLAIN, false>(&n);
+    if (e == cudaSuccess) e = prepare_as<true, GATED, true>(&n);
+    if (e == cudaSuccess) e = prepare_as<true, GATED, false>(&n);
+    l->fp4_pairs = n;
+    return e == cudaSuccess && n < 1 ? cudaErrorNotSupported : e;
 }
 
 size_t fp4_product_bytes(const som_layers* l, const Fp4Product& p)
@@ -445,7 +456,7 @@ int launch_fp4_product(som_layers* l, const Fp4Product& p, unsigned char* ws, cu
     if (c.joined) {
         a.cols = (int)outputs;
         LAY_TRY(make_map(l, &a.o, ws, 4, outputs, p.T, c.splits, outputs, p.T * outputs, 32));
-        LAY_TRY(outcome(l, launch_as<false, true>(l, a, true, st)));
+        LAY_TRY(outcome(l, launch(l, k_fp4_product<false, PARTS, true>, grid_of(l, a, false), THREADS, SMEM, st, 1, a)));
         FinishArgs f = {};
         f.part = reinterpret_cast<const float*>(ws);
         f.rows = p.T;
@@ -470,7 +481,7 @@ int launch_fp4_product(som_layers* l, const Fp4Product& p, unsigned char* ws, cu
     a.residual = p.residual;
     a.ldr = p.ldr;
     LAY_TRY(make_map(l, &a.o, p.y, 2, p.F, p.T, 1, p.ldy, p.T * p.ldy, 32));
-    return outcome(l, c.paired ? launch_as<true, false>(l, a, p.bf16, st) : launch_as<false, false>(l, a, p.bf16, st));
+    return outcome(l, !c.paired ? launch_as<false, PLAIN>(l, a, p.bf16, st) : p.gated ? launch_as<true, GATED>(l, a, p.bf16, st) : launch_as<true, PLAIN>(l, a, p.bf16, st));
 }
 
 }  // namespace lay
