@@ -11,7 +11,8 @@ namespace lay {
 // columns at a time.  Direct stores take the load/store pipe 32 cycles an instruction: too much where a tile's products are short
 // (PROD_DW at 512 rows an expert: 134 us staged, 178 us direct), but no waits, and no shared memory for up to three outputs
 // at once (PROD_DZ, PROD_DZ_TWO).
-template <int BUFFERS>
+// ROW_BYTES 64: half as many columns, 64-byte rows under the 64-byte swizzle.
+template <int BUFFERS, int ROW_BYTES = 128>
 struct Stager {
     unsigned char* buf;
     int lane, other;  // other: distance to the other buffer
@@ -26,7 +27,10 @@ struct Stager {
         __syncwarp();
     }
     // 16 bytes of this lane's row
-    __device__ __forceinline__ void put(int chunk, uint4 v) { *reinterpret_cast<uint4*>(buf + lane * 128 + ((chunk ^ (lane & 7)) << 4)) = v; }
+    __device__ __forceinline__ void put(int chunk, uint4 v)
+    {
+        *reinterpret_cast<uint4*>(buf + lane * ROW_BYTES + ((chunk ^ (ROW_BYTES == 128 ? lane & 7 : (lane >> 1) & 3)) << 4)) = v;
+    }
     __device__ __forceinline__ void put(int chunk, const float* v)
     {
         put(chunk, make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])));

@@ -1,15 +1,12 @@
 // The product of two matrices in 4 bits on the 5th-generation tensor cores (tcgen05.mma kind::mxf4, fp32 accumulators).
 //
 // Persistent blocks walk the output tiles as the 16-bit products do (layers_product.cu): warp 0 issues the TMA copies of a ring, warp 1 the
-// matrix instructions, eight warps run the epilogue; every wait is bounded.  A stage holds 256 k of both operands (rows of 128 bytes) and their
+// matrix instructions, sixteen warps run the epilogue; every wait is bounded.  A stage holds 256 k of both operands (rows of 128 bytes) and their
 // scales, 1 KB for 128 rows as they lie in memory; copies from shared to tensor memory (tcgen05.cp) bring the scales in front of the
 // instructions that use them, a set of columns for each place of the ring.
 //
 // PAIR: 256 x 256 tiles by two blocks of a cluster (cta_group::2); each loads its own 128 rows of A, one half of B, and the scales of its rows of
-// A and of all of B.  A pair's instruction takes 4 bits four times as fast as 16, and a stage's bytes last as long as a
-// 16-bit stage's.  Two accumulators of 256 columns and the scales are more than the 512 columns of tensor memory, so the
-// second accumulator lies over the last 128 columns of the first: the epilogue reads those into registers first, and the next
-// tile's products begin when it has.  NARROW: 128 x 128 by one block, for products with few tiles; where SMs still idle the sum is
+// A and of all of B.  NARROW: 128 x 128 by one block, for products with few tiles; where SMs still idle the sum is
 // split over blocks, which leave fp32 parts for k_finish.
 #include "layers_epilogue.cuh"
 #include "layers_finish.cuh"
@@ -22,8 +19,8 @@ namespace {
 constexpr int BM = 128, BK = 256, STEPS = BK / 64;
 constexpr int PART_BYTES = BM * BK / 2;  // 128 rows of a stage
 constexpr int STAGES = 5, STAGE_BYTES = 2 * PART_BYTES, SCALE_BYTES = 3 * FP4_SCALE_TILE;
-constexpr int EPI_WARPS = 4 * EPI_TURNS, THREADS = 32 * (2 + EPI_WARPS);
-constexpr int OUT_BYTES = 32 * 128;
+constexpr int TURNS = 4, EPI_WARPS = 4 * TURNS, THREADS = 32 * (2 + EPI_WARPS);
+constexpr int ROW_BYTES = 64, OUT_BYTES = 32 * ROW_BYTES;  // an epilogue warp's staged output: 32 rows of 32 columns (fp32: 16)
 constexpr int SMEM = 1024 + STAGES * (STAGE_BYTES + SCALE_BYTES) + EPI_WARPS * OUT_BYTES;
 
 struct Fp4Args {
@@ -66,10 +63,9 @@ template <bool PAIRED, int ENDS, bool BF16>
 __global__ void __launch_bounds__(THREADS, 1) k_fp4_product(const __grid_constant__ Fp4Args p)
 {
     constexpr int BN = PAIRED ? 256 : 128;
-    constexpr uint32_t SECOND = 128;  // first column of the second accumulator: of a pair's 256 columns half lie over the first one's
-    constexpr uint32_t SCALES = SECOND + BN, SCALES_A = 8, SCALES_SET = SCALES_A + BN / 16;  // and of the stages' scales
+    constexpr int BUFFERS = PAIRED ? 1 : 2;  // accumulators
+    constexpr uint32_t SCALES = BUFFERS * BN, SCALES_A = 8, SCALES_SET = SCALES_A + BN / 16;  // first column of the stages' scales
     static_assert(SCALES + STAGES * SCALES_SET <= 512, "tensor memory");
-    static_assert(!PAIRED || BN - SECOND <= EPI_TURNS * 64, "the epilogue's first pieces hold what lies over one another");
     extern __shared__ unsigned char smem_raw[];
     __shared__ __align__(8) uint64_t full[STAGES], empty[STAGES], acc_full[2], acc_free[2], drained;
     __shared__ uint32_t tmem_sh;
@@ -181,15 +177,9 @@ __global__ void __launch_bounds__(THREADS, 1) k_fp4_product(const __grid_constan
             constexpr uint32_t idesc[2] = {mma_fp4_desc(PAIRED ? 256 : 128, BN, 0), mma_fp4_desc(PAIRED ? 256 : 128, BN, 1)};
             for (int idx = first_tile; ok && idx < total; idx += step, ++n_acc) {
                 const Tile t = tile_at<PAIRED>(p, idx, WIDTH, rank);
-                const int buf = n_acc & 1;
-                const uint32_t d = tmem + (buf ? SECOND : 0u);
-                // a pair's tile before has left the columns that both have (and the one before that all of its own); else this buffer has been read
-                if (PAIRED) {
-                    if (n_acc > 0) ok = bar_wait<true>(&acc_free[buf ^ 1], (uint32_t)((n_acc - 1) >> 1) & 1u, gave_up);
-                } else if (n_acc > 1) {
-                    ok = bar_wait(&acc_free[buf], (uint32_t)((n_acc >> 1) - 1) & 1u, gave_up);
-                }
-                ok = __all_sync(0xffffffffu, ok);  // all go on or all leave
+                const int buf = n_acc % BUFFERS;
+                const uint32_t d = tmem + buf * BN;
+                ok = __all_sync(0xffffffffu, bar_wait<PAIRED>(&acc_free[buf], (uint32_t)(n_acc / BUFFERS) & 1u ^ 1u, gave_up));  // all go on or all leave
                 tc_fence_after();
                 for (int it = 0; ok && it < t.n; ++it) {
                     ok = __all_sync(0xffffffffu, bar_wait(&full[stage], phase, gave_up));
@@ -230,99 +220,75 @@ __global__ void __launch_bounds__(THREADS, 1) k_fp4_product(const __grid_constan
             __syncwarp();
         }
     } else {
-        // A warp may read the 32 lanes of its quarter only; the two warps of a quarter take pieces of 64 columns (fp32: 32) in turn.
+        // A warp may read the 32 lanes of its quarter only; the four warps of a quarter take a fourth of the tile's columns each, into
+        // registers at once, so that the accumulator is free again before any of the epilogue's work.
+        constexpr int PIECE = WIDTH / TURNS, SENT = ENDS == PARTS ? 16 : 32;  // columns of a warp, and of what it stages at once
         const int q = warp & 3, turn = (warp - 2) >> 2;
-        Stager<1> s{staged + (warp - 2) * OUT_BYTES, lane, OUT_BYTES};
-        constexpr int PIECE = ENDS == PARTS ? 32 : 64, PIECES = WIDTH / PIECE;
-        constexpr int AHEAD = ENDS == GATED ? 16 : 64;  // columns whose bias and residual are fetched at once (gated, the sums take twice the registers)
+        Stager<1, ROW_BYTES> s{staged + (warp - 2) * OUT_BYTES, lane, 0};
         int n_acc = 0;
         for (int idx = first_tile; idx < total; idx += step, ++n_acc) {
             const Tile t = tile_at<PAIRED>(p, idx, WIDTH, rank);
-            const int buf = n_acc & 1;
-            const uint32_t acc = tmem + (buf ? SECOND : 0u) + ((uint32_t)(32 * q) << 16);
+            const int buf = n_acc % BUFFERS, at = turn * PIECE, col = t.col + at;
+            const uint32_t acc = tmem + buf * BN + ((uint32_t)(32 * q) << 16);
             const int row0 = t.row + 32 * q, row = row0 + lane;
             const bool counts = row < p.rows;
             const uint16_t* extra = ENDS != PARTS && p.residual ? p.residual + (size_t)row * p.ldr : nullptr;
-            // The first accumulator shares its last columns, the second its first: the pieces run from there.
-            const bool down = PAIRED && buf == 0;
-            auto piece_at = [&](int j) { return (down ? PIECES - 1 - j : j) * PIECE; };
-            RowPart<AHEAD> add, b0, b1;
+            RowPart<16> add, b0, b1;
             auto fetch = [&](int col) {
                 add.fetch(extra, col, p.cols, extra && counts);
                 b0.fetch(p.bias, col, p.cols, p.bias);
                 if (ENDS == GATED) b1.fetch(p.bias + p.gate_rows, col, p.cols, p.bias);
             };
-            if (ENDS != PARTS) {  // the first piece's while the products still run, the others' on the way to L2
-                fetch(t.col + piece_at(turn));
-                if (extra && counts)
-                    for (int j = turn + EPI_TURNS; j < PIECES; j += EPI_TURNS)
-                        if (t.col + piece_at(j) < p.cols) prefetch_l2(extra + t.col + piece_at(j));
+            if (ENDS != PARTS) {  // the first columns' while the products still run, the others on the way to L2
+                fetch(col);
+                if (extra && counts && col < p.cols) prefetch_l2(extra + col);
             }
             // One lane waits, the others for it at a hardware barrier; all go on or all leave by the word that it writes (two words in turn).
-            if (warp == 2 && lane == 0) summed[buf] = bar_wait(&acc_full[buf], (uint32_t)(n_acc >> 1) & 1u, gave_up);
+            if (warp == 2 && lane == 0) summed[n_acc & 1] = bar_wait(&acc_full[buf], (uint32_t)(n_acc / BUFFERS) & 1u, gave_up);
             asm volatile("bar.sync 1, %0;" ::"n"(32 * EPI_WARPS) : "memory");
-            if (!summed[buf]) break;
+            if (!summed[n_acc & 1]) break;
             tc_fence_after();
-            auto leave = [&] {  // what both accumulators share has been read (PAIR), or all of this one
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) {
-                    if (PAIRED) bar_arrive_remote(cluster_addr(smem_addr(&acc_free[buf]), 0));
-                    else bar_arrive(&acc_free[buf]);
-                }
-            };
-            static_assert(PIECES % EPI_TURNS == 0, "every warp has pieces");
+            float v[PIECE], u[ENDS == GATED ? PIECE : 16];
 #pragma unroll
-            for (int i = 0; i < PIECES / EPI_TURNS; ++i) {
-                const int at = piece_at(turn + i * EPI_TURNS), col = t.col + at;
-                const bool last = i + 1 == PIECES / EPI_TURNS;
+            for (int h = 0; h < PIECE; h += 32) {
+                tmem_ld(acc + at + h, reinterpret_cast<float(&)[32]>(v[h]));
+                if constexpr (ENDS == GATED) tmem_ld(acc + BN / 2 + at + h, reinterpret_cast<float(&)[32]>(u[h]));
+            }
+            tmem_wait_ld();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) {
+                if (PAIRED) bar_arrive_remote(cluster_addr(smem_addr(&acc_free[buf]), 0));
+                else bar_arrive(&acc_free[buf]);
+            }
+#pragma unroll
+            for (int c = 0; c < PIECE / 16; ++c) {
+                float(&z)[16] = reinterpret_cast<float(&)[16]>(v[16 * c]);
+                const bool first = c * 16 % SENT == 0, last = (c + 1) * 16 % SENT == 0;
+                if (first && (ENDS == PARTS || c == 0)) s.begin();
                 if constexpr (ENDS == PARTS) {
-                    float v[32];
-                    tmem_ld(acc + at, v);
-                    tmem_wait_ld();
-                    if (last) leave();
-                    s.begin();
 #pragma unroll
-                    for (int c = 0; c < 8; ++c) s.put(c, v + 4 * c);
-                    s.send(&p.o, col, row0, t.split, p.rows, p.cols);
+                    for (int k = 0; k < 4; ++k) s.put(k, z + 4 * k);
                 } else {
-                    float v[2][32], u[2][32];
+                    if (p.bias) b0.template add<BF16>(z);
+                    if (p.act != SOM_ACT_NONE)
+                        with_act(p.act, [&](auto tag) {
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        tmem_ld(acc + at + 32 * h, v[h]);
-                        if (ENDS == GATED) tmem_ld(acc + BN / 2 + at + 32 * h, u[h]);
+                            for (int k = 0; k < 16; ++k) z[k] = act_of<decltype(tag)::value>(z[k]);
+                        });
+                    if constexpr (ENDS == GATED) {
+                        float(&w)[16] = reinterpret_cast<float(&)[16]>(u[16 * c]);
+                        if (p.bias) b1.template add<BF16>(w);
+#pragma unroll
+                        for (int k = 0; k < 16; ++k) z[k] *= w[k];
                     }
-                    if (i > 0) fetch(col);
-                    tmem_wait_ld();
-                    if (PAIRED ? i == 0 : last) leave();  // (only first pieces hold shared columns; gated, a warp has one piece)
-                    s.begin();
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        float(&z)[16] = reinterpret_cast<float(&)[16]>(v[c / 2][16 * (c & 1)]);
-                        float(&w)[16] = reinterpret_cast<float(&)[16]>(u[c / 2][16 * (c & 1)]);
-                        constexpr int OF = AHEAD / 16;  // steps of 16 columns that were fetched at once
-                        const RowPart<16>&add16 = reinterpret_cast<const RowPart<16>*>(&add)[c % OF], &b016 = reinterpret_cast<const RowPart<16>*>(&b0)[c % OF],
-                              &b116 = reinterpret_cast<const RowPart<16>*>(&b1)[c % OF];
-                        if (p.bias) {
-                            b016.template add<BF16>(z);
-                            if (ENDS == GATED) b116.template add<BF16>(w);
-                        }
-                        if (p.act != SOM_ACT_NONE)
-                            with_act(p.act, [&](auto tag) {
-#pragma unroll
-                                for (int k = 0; k < 16; ++k) z[k] = act_of<decltype(tag)::value>(z[k]);
-                            });
-                        if (ENDS == GATED) {
-#pragma unroll
-                            for (int k = 0; k < 16; ++k) z[k] *= w[k];
-                        }
-                        if (extra) add16.template add<BF16>(z);
-                        if (OF == 1 && c < 3) fetch(col + 16 * (c + 1));
-                        s.put(2 * c, pack8<BF16>(z));
-                        s.put(2 * c + 1, pack8<BF16>(z + 8));
-                    }
-                    s.send(&p.o, col, row0, 0, p.rows, p.cols);
+                    if (extra) add.template add<BF16>(z);
+                    if (c + 1 < PIECE / 16) fetch(col + 16 * (c + 1));
+                    if (first && c > 0) s.begin();
+                    s.put(2 * (c & 1), pack8<BF16>(z));
+                    s.put(2 * (c & 1) + 1, pack8<BF16>(z + 8));
                 }
+                if (last) s.send(&p.o, col + 16 * (c + 1) - SENT, row0, t.split, p.rows, p.cols);
             }
         }
     }
@@ -455,7 +421,7 @@ int launch_fp4_product(som_layers* l, const Fp4Product& p, unsigned char* ws, cu
     a.flags = l->flags;
     if (c.joined) {
         a.cols = (int)outputs;
-        LAY_TRY(make_map(l, &a.o, ws, 4, outputs, p.T, c.splits, outputs, p.T * outputs, 32));
+        LAY_TRY(make_map(l, &a.o, ws, 4, outputs, p.T, c.splits, outputs, p.T * outputs, 32, ROW_BYTES));
         LAY_TRY(outcome(l, launch(l, k_fp4_product<false, PARTS, true>, grid_of(l, a, false), THREADS, SMEM, st, 1, a)));
         FinishArgs f = {};
         f.part = reinterpret_cast<const float*>(ws);
@@ -480,7 +446,7 @@ int launch_fp4_product(som_layers* l, const Fp4Product& p, unsigned char* ws, cu
     a.bias = p.bias;
     a.residual = p.residual;
     a.ldr = p.ldr;
-    LAY_TRY(make_map(l, &a.o, p.y, 2, p.F, p.T, 1, p.ldy, p.T * p.ldy, 32));
+    LAY_TRY(make_map(l, &a.o, p.y, 2, p.F, p.T, 1, p.ldy, p.T * p.ldy, 32, ROW_BYTES));
     return outcome(l, !c.paired ? launch_as<false, PLAIN>(l, a, p.bf16, st) : p.gated ? launch_as<true, GATED>(l, a, p.bf16, st) : launch_as<true, PLAIN>(l, a, p.bf16, st));
 }
 

@@ -74,8 +74,9 @@ struct ProdArgs {
 
 int launch_product(som_layers* l, ProdMode mode, const ProdArgs& args, cudaStream_t st);
 
-// 3-d tensor map over [batch][rows][cols] of 16-bit (bytes = 2) or fp32 (4) elements in boxes of [1][box_rows] rows of 128 bytes
+// 3-d tensor map over [batch][rows][cols] of 16-bit (bytes = 2) or fp32 (4) elements in boxes of [1][box_rows] rows of 128 or 64 bytes,
+// under the swizzle of that size
 int make_map(som_layers* l, CUtensorMap* map, const void* base, int bytes, int64_t cols, int64_t rows, int64_t batch, int64_t ld,
-             int64_t batch_stride, int box_rows);
+             int64_t batch_stride, int box_rows, int row_bytes = 128);
 
 }  // namespace lay
