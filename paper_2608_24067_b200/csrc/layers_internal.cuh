@@ -82,6 +82,7 @@ struct SlotPlan {
 };
 
 cudaError_t prepare_product(som_layers* l);  // once per handle
+cudaError_t prepare_norm();                  // once per handle
 
 cudaError_t prepare_plan();  // once per handle
 int plan_blocks(int64_t slots);  // rows of SlotPlan::block_counts

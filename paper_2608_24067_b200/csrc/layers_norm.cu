@@ -6,7 +6,11 @@
 //
 // Bound by HBM: a few operations a value.  Everything between input and output is fp32; the variance is summed from the differences
 // to the mean, not from squares, so that a row far from zero keeps its digits.
+#include <initializer_list>
+#include <type_traits>
+
 #include "layers_host.cuh"
+#include "layers_math.cuh"
 
 namespace lay {
 namespace {
@@ -14,18 +18,19 @@ namespace {
 struct NormArgs {
     const void *x, *residual, *weight, *bias;
     void *sum, *y;
-    int64_t ldx, ldr, lds, ldy;
-    int D;
+    int64_t ldx, ldr, lds, ldy, T;
+    int D, group;  // group: threads of a row (k_norm)
     float eps;
 };
 
 struct NormBackArgs {
     const void *x, *weight, *dy, *dsum;
     void* dx;
-    float* stats;  // [T][2] mean and r of every row, or nullptr
+    float* stats;  // [T][2] mean and r of every row, or nullptr (k_norm_back_any)
+    float* part;   // [blocks][2][D] sums of the block's rows, or nullptr (k_norm_back)
     int64_t ldx, lddy, ldds;
     int64_t T;
-    int D;
+    int D, group;
     float eps;
 };
 
@@ -79,7 +84,256 @@ __device__ __forceinline__ void block_sums(float (&v)[N])
     }
 }
 
-// Any row length and alignment: a block a row, which it walks three times (from L1 or L2 after the first).
+// ---- rows on 16 bytes, held in registers ---------------------------------------------------------------------------
+
+constexpr int HELD = 16;  // values that a thread holds of a row: HELD * sizeof(E) / 16 pieces of 16 bytes, a group's threads apart
+
+template <class E>
+struct Piece {
+    static constexpr int N = 16 / (int)sizeof(E), COUNT = HELD / N;
+    uint4 w;
+    __device__ __forceinline__ void load(const E* p) { w = *reinterpret_cast<const uint4*>(p); }
+    __device__ __forceinline__ void store(E* p) const { *reinterpret_cast<uint4*>(p) = w; }
+    __device__ __forceinline__ void get(float* v) const
+    {
+        if constexpr (sizeof(E) == 4) {
+            v[0] = __uint_as_float(w.x), v[1] = __uint_as_float(w.y), v[2] = __uint_as_float(w.z), v[3] = __uint_as_float(w.w);
+        } else {
+            widen8(w, *reinterpret_cast<float(*)[8]>(v), BF16);
+        }
+    }
+    __device__ __forceinline__ void put(const float* v)
+    {
+        if constexpr (sizeof(E) == 4) w = make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
+        else w = make_uint4(pack2(v[0], v[1], BF16), pack2(v[2], v[3], BF16), pack2(v[4], v[5], BF16), pack2(v[6], v[7], BF16));
+    }
+    static constexpr int BF16 = std::is_same<E, __nv_bfloat16>::value;
+};
+
+// N weights from column i on
+template <class W, int N>
+__device__ __forceinline__ void load_weights(const void* base, int i, float (&v)[N])
+{
+    const W* p = static_cast<const W*>(base) + i;
+    constexpr int EACH = 16 / (int)sizeof(W);
+    if constexpr (EACH <= N) {
+#pragma unroll
+        for (int j = 0; j < N; j += EACH) {
+            Piece<W> q;
+            q.load(p + j);
+            q.get(v + j);
+        }
+    }
+}
+
+// The sums of N values over the `warps` warps of a row's group, to every thread of it; `part` is this group's own, and another one than
+// that of the sums before and after (which is what lets one barrier do).
+template <int N>
+__device__ __forceinline__ void group_sums(float (&v)[N], float (*part)[N], int warps, int warp, int barrier)
+{
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1)
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] += __shfl_xor_sync(0xffffffffu, v[i], d);
+    if (warps == 1) return;
+    if ((threadIdx.x & 31) == 0)
+#pragma unroll
+        for (int i = 0; i < N; ++i) part[warp][i] = v[i];
+    asm volatile("bar.sync %0, %1;" ::"r"(barrier), "r"(32 * warps) : "memory");
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = 0.f;
+    for (int w = 0; w < warps; ++w)
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] += part[w][i];
+}
+
+constexpr int FRONT_THREADS = 256, FRONT_MOST = 1024;  // a block holds as many rows as groups fit into 256 threads, or one
+
+template <class E, class W>
+__global__ void __launch_bounds__(FRONT_MOST) k_norm(const NormArgs a)
+{
+    __shared__ float part0[FRONT_MOST / 32][1], part1[FRONT_MOST / 32][1];
+    using P = Piece<E>;
+    const int group = threadIdx.x / a.group, t = threadIdx.x - group * a.group, warps = a.group / 32, first = group * warps;
+    const int64_t row = (int64_t)blockIdx.x * (blockDim.x / a.group) + group;
+    enter();
+    if (row >= a.T) return;  // (a whole group)
+    const E* x = static_cast<const E*>(a.x) + row * a.ldx;
+    const E* res = a.residual ? static_cast<const E*>(a.residual) + row * a.ldr : nullptr;
+    P px[P::COUNT], pr[P::COUNT];
+#pragma unroll
+    for (int c = 0; c < P::COUNT; ++c) {
+        const int i = (c * a.group + t) * P::N;
+        if (i < a.D) {
+            px[c].load(x + i);
+            if (res) pr[c].load(res + i);
+        }
+    }
+    float v[P::COUNT][P::N], s[1] = {0.f};
+#pragma unroll
+    for (int c = 0; c < P::COUNT; ++c) {
+        const int i = (c * a.group + t) * P::N;
+        if (i < a.D) {
+            px[c].get(v[c]);
+            if (res) {
+                float r[P::N];
+                pr[c].get(r);
+#pragma unroll
+                for (int j = 0; j < P::N; ++j) v[c][j] += r[j];
+                px[c].put(v[c]);
+                px[c].get(v[c]);
+                if (a.sum) px[c].store(static_cast<E*>(a.sum) + row * a.lds + i);
+            }
+#pragma unroll
+            for (int j = 0; j < P::N; ++j) s[0] += v[c][j];
+        }
+    }
+    group_sums(s, part0 + first, warps, threadIdx.x / 32 - first, 1 + group);
+    const float mean = s[0] / (float)a.D;
+    s[0] = 0.f;
+#pragma unroll
+    for (int c = 0; c < P::COUNT; ++c)
+        if ((c * a.group + t) * P::N < a.D)
+#pragma unroll
+            for (int j = 0; j < P::N; ++j) {
+                v[c][j] -= mean;
+                s[0] = fmaf(v[c][j], v[c][j], s[0]);
+            }
+    group_sums(s, part1 + first, warps, threadIdx.x / 32 - first, 1 + group);
+    const float r = 1.f / sqrtf(s[0] / (float)a.D + a.eps);
+#pragma unroll
+    for (int c = 0; c < P::COUNT; ++c) {
+        const int i = (c * a.group + t) * P::N;
+        if (i >= a.D) continue;
+        float w[P::N];
+#pragma unroll
+        for (int j = 0; j < P::N; ++j) v[c][j] *= r;
+        if (a.weight) {
+            load_weights<W>(a.weight, i, w);
+#pragma unroll
+            for (int j = 0; j < P::N; ++j) v[c][j] *= w[j];
+        }
+        if (a.bias) {
+            load_weights<W>(a.bias, i, w);
+#pragma unroll
+            for (int j = 0; j < P::N; ++j) v[c][j] += w[j];
+        }
+        px[c].put(v[c]);
+        px[c].store(static_cast<E*>(a.y) + row * a.ldy + i);
+    }
+}
+
+// The gradient in one pass: blocks stay, and so do a thread's columns, so that dweight and dbias are summed in registers; the next row is
+// fetched while this one is worked on.  A block's groups add up through shared memory and leave one part a block.
+constexpr int BACK_THREADS = 512;
+
+template <class E, class W>
+__global__ void __launch_bounds__(BACK_THREADS, 1) k_norm_back(const NormBackArgs a)
+{
+    __shared__ float part0[BACK_THREADS / 32][2], part1[BACK_THREADS / 32][2];
+    extern __shared__ float columns[];  // [2][D]
+    using P = Piece<E>;
+    const int group = threadIdx.x / a.group, t = threadIdx.x - group * a.group, warps = a.group / 32, first = group * warps, groups = BACK_THREADS / a.group;
+    const int warp = threadIdx.x / 32 - first;
+    enter();
+    float w[P::COUNT][P::N], dw[P::COUNT][P::N], db[P::COUNT][P::N];
+    const float n = (float)a.D;  // (divided by, not multiplied by its inverse: the mean of equal values is that value)
+#pragma unroll
+    for (int c = 0; c < P::COUNT; ++c) {
+        const int i = (c * a.group + t) * P::N;
+#pragma unroll
+        for (int j = 0; j < P::N; ++j) w[c][j] = 1.f, dw[c][j] = db[c][j] = 0.f;
+        if (a.weight && i < a.D) load_weights<W>(a.weight, i, w[c]);
+    }
+    P px[P::COUNT], pg[P::COUNT];
+    auto fetch = [&](int64_t row) {
+#pragma unroll
+        for (int c = 0; c < P::COUNT; ++c) {
+            const int i = (c * a.group + t) * P::N;
+            px[c].w = pg[c].w = make_uint4(0u, 0u, 0u, 0u);
+            if (row < a.T && i < a.D) {
+                px[c].load(static_cast<const E*>(a.x) + row * a.ldx + i);
+                pg[c].load(static_cast<const E*>(a.dy) + row * a.lddy + i);
+            }
+        }
+    };
+    int64_t row = (int64_t)blockIdx.x * groups + group;
+    const int64_t step = (int64_t)gridDim.x * groups;
+    fetch(row);
+    for (; row < a.T; row += step) {
+        float v[P::COUNT][P::N], g[P::COUNT][P::N], s[2] = {0.f, 0.f};
+        P ps[P::COUNT];  // (dsum comes while the row's sums are made)
+#pragma unroll
+        for (int c = 0; c < P::COUNT; ++c) {
+            px[c].get(v[c]);
+            pg[c].get(g[c]);
+#pragma unroll
+            for (int j = 0; j < P::N; ++j) {
+                s[0] += v[c][j];
+                s[1] = fmaf(g[c][j], w[c][j], s[1]);
+            }
+        }
+#pragma unroll
+        for (int c = 0; c < P::COUNT; ++c) {
+            const int i = (c * a.group + t) * P::N;
+            ps[c].w = make_uint4(0u, 0u, 0u, 0u);
+            if (a.dsum && i < a.D) ps[c].load(static_cast<const E*>(a.dsum) + row * a.ldds + i);
+        }
+        fetch(row + step);
+        group_sums(s, part0 + first, warps, warp, 1 + group);
+        const float mean = s[0] / n, d_mean = s[1] / n;
+        s[0] = s[1] = 0.f;
+#pragma unroll
+        for (int c = 0; c < P::COUNT; ++c)
+            if ((c * a.group + t) * P::N < a.D)
+#pragma unroll
+                for (int j = 0; j < P::N; ++j) {
+                    v[c][j] -= mean;
+                    s[0] = fmaf(v[c][j], v[c][j], s[0]);
+                    s[1] = fmaf(v[c][j], g[c][j] * w[c][j], s[1]);
+                }
+        group_sums(s, part1 + first, warps, warp, 1 + group);
+        // n sum (d n) / D = (h - mean) r^2 sum (d (h - mean)) / D
+        const float r = 1.f / sqrtf(s[0] / n + a.eps), along = s[1] / n * r * r;
+#pragma unroll
+        for (int c = 0; c < P::COUNT; ++c) {
+            const int i = (c * a.group + t) * P::N;
+            float out[P::N];
+            ps[c].get(out);
+#pragma unroll
+            for (int j = 0; j < P::N; ++j) {
+                const float d = g[c][j] * w[c][j];
+                dw[c][j] = fmaf(g[c][j], v[c][j] * r, dw[c][j]);
+                db[c][j] += g[c][j];
+                out[j] = fmaf(r, (d - d_mean) - v[c][j] * along, out[j]);
+            }
+            if (a.dx && i < a.D) {
+                ps[c].put(out);
+                ps[c].store(static_cast<E*>(a.dx) + row * a.D + i);
+            }
+        }
+    }
+    if (!a.part) return;
+    for (int k = 0; k < groups; ++k) {  // one group after the other, in their order
+        if (group == k)
+#pragma unroll
+            for (int c = 0; c < P::COUNT; ++c) {
+                const int i = (c * a.group + t) * P::N;
+                if (i < a.D)
+#pragma unroll
+                    for (int j = 0; j < P::N; ++j) {
+                        columns[i + j] = k ? columns[i + j] + dw[c][j] : dw[c][j];
+                        columns[a.D + i + j] = k ? columns[a.D + i + j] + db[c][j] : db[c][j];
+                    }
+            }
+        __syncthreads();
+    }
+    for (int i = threadIdx.x; i < 2 * a.D; i += BACK_THREADS) a.part[(int64_t)blockIdx.x * 2 * a.D + i] = columns[i];
+}
+
+// ---- any row length and alignment ------------------------------------------------------------------------------------
+
+// A block a row, which it walks three times (from L1 or L2 after the first).
 template <class E, class W>
 __global__ void __launch_bounds__(ROW_THREADS) k_norm_any(const NormArgs a)
 {
@@ -211,6 +465,19 @@ int check_norm(const som_layers* l, int type, int weights_type, int64_t T, int64
     return T >= MOST_ROWS || D > MOST_COLS ? SOM_ERR_UNSUPPORTED : SOM_OK;
 }
 
+// Threads of a row that is held in registers: as many warps, a power of two, as hold it.  0: too long, or not on 16 bytes
+int group_of(int64_t D, int most, int bytes, std::initializer_list<const void*> rows, std::initializer_list<int64_t> lds)
+{
+    if (D * bytes % 16 != 0 || D > (int64_t)most * HELD) return 0;
+    for (const void* p : rows)
+        if (!aligned16(p)) return 0;
+    for (int64_t ld : lds)
+        if (ld * bytes % 16 != 0) return 0;
+    int g = 32;
+    while ((int64_t)g * HELD < D) g *= 2;
+    return g;
+}
+
 // rows of a norm's matrix: present, and long enough
 int check_row(const void* p, int64_t ld, int64_t D, int64_t T)
 {
@@ -219,7 +486,23 @@ int check_row(const void* p, int64_t ld, int64_t D, int64_t T)
     return ld >= (int64_t)1 << 32 ? SOM_ERR_UNSUPPORTED : SOM_OK;
 }
 
+template <class E, class W>
+cudaError_t prepare_as()
+{
+    return cudaFuncSetAttribute(k_norm_back<E, W>, cudaFuncAttributeMaxDynamicSharedMemorySize, 2 * BACK_THREADS * HELD * (int)sizeof(float));
+}
+
 }  // namespace
+
+cudaError_t prepare_norm()
+{
+    cudaError_t e = prepare_as<float, float>();
+    if (e == cudaSuccess) e = prepare_as<__half, __half>();
+    if (e == cudaSuccess) e = prepare_as<__half, float>();
+    if (e == cudaSuccess) e = prepare_as<__nv_bfloat16, __nv_bfloat16>();
+    return e == cudaSuccess ? prepare_as<__nv_bfloat16, float>() : e;
+}
+
 }  // namespace lay
 
 using namespace lay;
@@ -236,9 +519,15 @@ int som_norm(som_layers* l, int type, int64_t T, int64_t D, const void* x, int64
     if (sum) LAY_TRY(check_row(sum, lds, D, T));
     if (T == 0) return SOM_OK;
     Guard g(l->device);
-    const NormArgs a = {x, residual, weight, bias, sum, y, ldx, ldr, lds, ldy, (int)D, eps};
+    cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+    const int group = group_of(D, FRONT_MOST, type == SOM_F32 ? 4 : 2, {x, residual, weight, bias, sum, y}, {ldx, residual ? ldr : 0, sum ? lds : 0, ldy});
+    const NormArgs a = {x, residual, weight, bias, sum, y, ldx, ldr, lds, ldy, T, (int)D, group, eps};
     return outcome(l, by_types(type, weights_type, [&](auto e, auto w) {
-                       return launch(l, k_norm_any<decltype(e), decltype(w)>, dim3((unsigned)T), ROW_THREADS, 0, reinterpret_cast<cudaStream_t>(stream), 1, a);
+                       using E = decltype(e);
+                       using W = decltype(w);
+                       if (!group) return launch(l, k_norm_any<E, W>, dim3((unsigned)T), ROW_THREADS, 0, st, 1, a);
+                       const int threads = group < FRONT_THREADS ? FRONT_THREADS : group;
+                       return launch(l, k_norm<E, W>, dim3((unsigned)tiles_of(T, threads / group)), threads, 0, st, 1, a);
                    }));
 }
 
@@ -259,26 +548,40 @@ int som_norm_backward(som_layers* l, int type, int64_t T, int64_t D, const void*
         return SOM_OK;
     }
     const bool columns = dweight || dbias;
-    int64_t parts = 4 * (int64_t)l->sm_count / tiles_of(D, 32);
-    if (parts > T / 64) parts = T / 64;
-    if (parts < 1) parts = 1;
-    Carver c{nullptr, 0};
-    c.take<float>(2 * T);
-    c.take<float>(parts * 2 * D);
-    if (columns) LAY_TRY(ensure(l, c.used));
-    c = Carver{static_cast<unsigned char*>(l->ws), 0};
-    float* stats = columns ? c.take<float>(2 * T) : nullptr;
-    float* part = columns ? c.take<float>(parts * 2 * D) : nullptr;
-    const NormBackArgs a = {x, weight, dy, dsum, dx, stats, ldx, lddy, ldds, T, (int)D, eps};
+    const int group = group_of(D, BACK_THREADS, type == SOM_F32 ? 4 : 2, {x, dy, dsum, dx, weight}, {ldx, lddy, dsum ? ldds : 0});
+    int64_t parts;
+    if (group) {
+        parts = tiles_of(T, BACK_THREADS / group);
+        if (parts > l->sm_count) parts = l->sm_count;
+    } else {
+        parts = 4 * (int64_t)l->sm_count / tiles_of(D, 32);
+        if (parts > T / 64) parts = T / 64;
+        if (parts < 1) parts = 1;
+    }
+    float *stats = nullptr, *part = nullptr;
+    auto carve = [&](Carver c) {
+        if (!group) stats = c.take<float>(2 * T);
+        part = c.take<float>(parts * 2 * D);
+        return c.used;
+    };
+    if (columns) {
+        LAY_TRY(ensure(l, carve(Carver{nullptr, 0})));
+        carve(Carver{static_cast<unsigned char*>(l->ws), 0});
+    }
+    const NormBackArgs a = {x, weight, dy, dsum, dx, stats, part, ldx, lddy, ldds, T, (int)D, group, eps};
     const ColumnArgs b = {x, dy, stats, part, ldx, lddy, T, (int)D, (int)parts};
     const ColumnJoinArgs j = {part, dweight, dbias, (int)D, (int)parts};
     return outcome(l, by_types(type, weights_type, [&](auto e, auto w) {
                        using E = decltype(e);
                        using W = decltype(w);
-                       cudaError_t r = launch(l, k_norm_back_any<E, W>, dim3((unsigned)T), ROW_THREADS, 0, st, 1, a);
+                       cudaError_t r;
+                       if (group) {
+                           r = launch(l, k_norm_back<E, W>, dim3((unsigned)parts), BACK_THREADS, columns ? 2 * D * sizeof(float) : 0, st, 1, a);
+                       } else {
+                           r = launch(l, k_norm_back_any<E, W>, dim3((unsigned)T), ROW_THREADS, 0, st, 1, a);
+                           if (r == cudaSuccess && columns) r = launch(l, k_norm_columns<E>, dim3((unsigned)tiles_of(D, 32), (unsigned)parts), 256, 0, st, 1, b);
+                       }
                        if (r != cudaSuccess || !columns) return r;
-                       r = launch(l, k_norm_columns<E>, dim3((unsigned)tiles_of(D, 32), (unsigned)parts), 256, 0, st, 1, b);
-                       if (r != cudaSuccess) return r;
                        return launch(l, k_norm_join<W>, dim3((unsigned)tiles_of(2 * D, 32)), 256, 0, st, 1, j);
                    }));
 }
