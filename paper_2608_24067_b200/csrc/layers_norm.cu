@@ -107,7 +107,7 @@ struct Piece {
         if constexpr (sizeof(E) == 4) w = make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
         else w = make_uint4(pack2(v[0], v[1], BF16), pack2(v[2], v[3], BF16), pack2(v[4], v[5], BF16), pack2(v[6], v[7], BF16));
     }
-    static constexpr int BF16 = std::is_same<E, __nv_bfloat16>::value;
+    static constexpr int BF16 [[maybe_unused]] = std::is_same<E, __nv_bfloat16>::value;
 };
 
 // N weights from column i on
@@ -223,16 +223,34 @@ __global__ void __launch_bounds__(FRONT_MOST) k_norm(const NormArgs a)
     }
 }
 
-// The gradient in one pass: blocks stay, and so do a thread's columns, so that dweight and dbias are summed in registers; the next row is
-// fetched while this one is worked on.  A block's groups add up through shared memory and leave one part a block.
+// The gradient in one pass: blocks stay, and so do a thread's columns, so that dweight and dbias are summed in registers.  A thread brings its
+// own pieces of the next rows into shared memory (cp.async), three rows ahead (fp32: one), and reads them there itself: no barrier, no registers for
+// what is on its way.  A block's groups add up through shared memory and leave one part a block.
 constexpr int BACK_THREADS = 512;
+template <class E>
+constexpr int back_smem()
+{
+    return 8 / (int)sizeof(E) * 3 * Piece<E>::COUNT * BACK_THREADS * 16;
+}
+
+__device__ __forceinline__ void copy16(void* to, const void* from)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(to)), "l"(from) : "memory");
+}
+__device__ __forceinline__ void copies_end() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void copies_wait()
+{
+    asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
 
 template <class E, class W>
 __global__ void __launch_bounds__(BACK_THREADS, 1) k_norm_back(const NormBackArgs a)
 {
     __shared__ float part0[BACK_THREADS / 32][2], part1[BACK_THREADS / 32][2];
-    extern __shared__ float columns[];  // [2][D]
+    extern __shared__ __align__(16) uint4 ring[];  // [DEPTH][x, dy, dsum][COUNT][BACK_THREADS]; at the end the columns' sums, [2][D]
     using P = Piece<E>;
+    constexpr int DEPTH = 8 / (int)sizeof(E);
     const int group = threadIdx.x / a.group, t = threadIdx.x - group * a.group, warps = a.group / 32, first = group * warps, groups = BACK_THREADS / a.group;
     const int warp = threadIdx.x / 32 - first;
     enter();
@@ -245,41 +263,51 @@ __global__ void __launch_bounds__(BACK_THREADS, 1) k_norm_back(const NormBackArg
         for (int j = 0; j < P::N; ++j) w[c][j] = 1.f, dw[c][j] = db[c][j] = 0.f;
         if (a.weight && i < a.D) load_weights<W>(a.weight, i, w[c]);
     }
-    P px[P::COUNT], pg[P::COUNT];
-    auto fetch = [&](int64_t row) {
+    auto slot = [&](int stage, int what, int c) { return ring + ((stage * 3 + what) * P::COUNT + c) * BACK_THREADS + threadIdx.x; };
+    auto fetch = [&](int64_t row, int stage) {
+        if (row < a.T) {
 #pragma unroll
-        for (int c = 0; c < P::COUNT; ++c) {
-            const int i = (c * a.group + t) * P::N;
-            px[c].w = pg[c].w = make_uint4(0u, 0u, 0u, 0u);
-            if (row < a.T && i < a.D) {
-                px[c].load(static_cast<const E*>(a.x) + row * a.ldx + i);
-                pg[c].load(static_cast<const E*>(a.dy) + row * a.lddy + i);
+            for (int c = 0; c < P::COUNT; ++c) {
+                const int i = (c * a.group + t) * P::N;
+                if (i < a.D) {
+                    copy16(slot(stage, 0, c), static_cast<const E*>(a.x) + row * a.ldx + i);
+                    copy16(slot(stage, 1, c), static_cast<const E*>(a.dy) + row * a.lddy + i);
+                    if (a.dsum) copy16(slot(stage, 2, c), static_cast<const E*>(a.dsum) + row * a.ldds + i);
+                }
             }
         }
+        copies_end();
     };
+    // what is not copied stays zero: columns beyond the row's end, and dsum where there is none
+#pragma unroll
+    for (int stage = 0; stage < DEPTH; ++stage)
+#pragma unroll
+        for (int what = 0; what < 3; ++what)
+#pragma unroll
+            for (int c = 0; c < P::COUNT; ++c)
+                if ((c * a.group + t) * P::N >= a.D || (what == 2 && !a.dsum)) *slot(stage, what, c) = make_uint4(0u, 0u, 0u, 0u);
     int64_t row = (int64_t)blockIdx.x * groups + group;
     const int64_t step = (int64_t)gridDim.x * groups;
-    fetch(row);
+#pragma unroll
+    for (int k = 0; k < DEPTH - 1; ++k) fetch(row + k * step, k);
+    int stage = 0;
     for (; row < a.T; row += step) {
+        fetch(row + (DEPTH - 1) * step, stage == 0 ? DEPTH - 1 : stage - 1);  // (the place of the row before)
+        copies_wait<DEPTH - 1>();
         float v[P::COUNT][P::N], g[P::COUNT][P::N], s[2] = {0.f, 0.f};
-        P ps[P::COUNT];  // (dsum comes while the row's sums are made)
 #pragma unroll
         for (int c = 0; c < P::COUNT; ++c) {
-            px[c].get(v[c]);
-            pg[c].get(g[c]);
+            P q;
+            q.w = *slot(stage, 0, c);
+            q.get(v[c]);
+            q.w = *slot(stage, 1, c);
+            q.get(g[c]);
 #pragma unroll
             for (int j = 0; j < P::N; ++j) {
                 s[0] += v[c][j];
                 s[1] = fmaf(g[c][j], w[c][j], s[1]);
             }
         }
-#pragma unroll
-        for (int c = 0; c < P::COUNT; ++c) {
-            const int i = (c * a.group + t) * P::N;
-            ps[c].w = make_uint4(0u, 0u, 0u, 0u);
-            if (a.dsum && i < a.D) ps[c].load(static_cast<const E*>(a.dsum) + row * a.ldds + i);
-        }
-        fetch(row + step);
         group_sums(s, part0 + first, warps, warp, 1 + group);
         const float mean = s[0] / n, d_mean = s[1] / n;
         s[0] = s[1] = 0.f;
@@ -299,7 +327,9 @@ __global__ void __launch_bounds__(BACK_THREADS, 1) k_norm_back(const NormBackArg
         for (int c = 0; c < P::COUNT; ++c) {
             const int i = (c * a.group + t) * P::N;
             float out[P::N];
-            ps[c].get(out);
+            P q;
+            q.w = *slot(stage, 2, c);
+            q.get(out);
 #pragma unroll
             for (int j = 0; j < P::N; ++j) {
                 const float d = g[c][j] * w[c][j];
@@ -308,11 +338,15 @@ __global__ void __launch_bounds__(BACK_THREADS, 1) k_norm_back(const NormBackArg
                 out[j] = fmaf(r, (d - d_mean) - v[c][j] * along, out[j]);
             }
             if (a.dx && i < a.D) {
-                ps[c].put(out);
-                ps[c].store(static_cast<E*>(a.dx) + row * a.D + i);
+                q.put(out);
+                q.store(static_cast<E*>(a.dx) + row * a.D + i);
             }
         }
+        stage = stage + 1 == DEPTH ? 0 : stage + 1;
     }
+    copies_wait<0>();
+    float* columns = reinterpret_cast<float*>(ring);
+    __syncthreads();  // every thread is done with its places of the ring
     if (!a.part) return;
     for (int k = 0; k < groups; ++k) {  // one group after the other, in their order
         if (group == k)
@@ -489,7 +523,8 @@ int check_row(const void* p, int64_t ld, int64_t D, int64_t T)
 template <class E, class W>
 cudaError_t prepare_as()
 {
-    return cudaFuncSetAttribute(k_norm_back<E, W>, cudaFuncAttributeMaxDynamicSharedMemorySize, 2 * BACK_THREADS * HELD * (int)sizeof(float));
+    static_assert(back_smem<E>() >= 2 * BACK_THREADS * HELD * (int)sizeof(float), "the columns' sums take the ring's place");
+    return cudaFuncSetAttribute(k_norm_back<E, W>, cudaFuncAttributeMaxDynamicSharedMemorySize, back_smem<E>());
 }
 
 }  // namespace
@@ -576,7 +611,7 @@ int som_norm_backward(som_layers* l, int type, int64_t T, int64_t D, const void*
                        using W = decltype(w);
                        cudaError_t r;
                        if (group) {
-                           r = launch(l, k_norm_back<E, W>, dim3((unsigned)parts), BACK_THREADS, columns ? 2 * D * sizeof(float) : 0, st, 1, a);
+                           r = launch(l, k_norm_back<E, W>, dim3((unsigned)parts), BACK_THREADS, back_smem<E>(), st, 1, a);
                        } else {
                            r = launch(l, k_norm_back_any<E, W>, dim3((unsigned)T), ROW_THREADS, 0, st, 1, a);
                            if (r == cudaSuccess && columns) r = launch(l, k_norm_columns<E>, dim3((unsigned)tiles_of(D, 32), (unsigned)parts), 256, 0, st, 1, b);
