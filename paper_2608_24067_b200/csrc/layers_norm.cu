@@ -90,61 +90,83 @@ constexpr int HELD = 16;  // values that a thread holds of a row: HELD * sizeof(
 
 template <class E>
 struct Piece {
-    static constexpr int N = 16 / (int)sizeof(E), COUNT = HELD / N;
+    static constexpr int N = 16 / (int)sizeof(E), PAIRS = N / 2, COUNT = HELD / N;
     uint4 w;
     __device__ __forceinline__ void load(const E* p) { w = *reinterpret_cast<const uint4*>(p); }
     __device__ __forceinline__ void store(E* p) const { *reinterpret_cast<uint4*>(p) = w; }
-    __device__ __forceinline__ void get(float* v) const
+    __device__ __forceinline__ void get(float2* v) const
     {
         if constexpr (sizeof(E) == 4) {
-            v[0] = __uint_as_float(w.x), v[1] = __uint_as_float(w.y), v[2] = __uint_as_float(w.z), v[3] = __uint_as_float(w.w);
+            v[0] = make_float2(__uint_as_float(w.x), __uint_as_float(w.y)), v[1] = make_float2(__uint_as_float(w.z), __uint_as_float(w.w));
         } else {
-            widen8(w, *reinterpret_cast<float(*)[8]>(v), BF16);
+            v[0] = unpack2(w.x, BF16), v[1] = unpack2(w.y, BF16), v[2] = unpack2(w.z, BF16), v[3] = unpack2(w.w, BF16);
         }
     }
-    __device__ __forceinline__ void put(const float* v)
+    __device__ __forceinline__ void put(const float2* v)
     {
-        if constexpr (sizeof(E) == 4) w = make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
-        else w = make_uint4(pack2(v[0], v[1], BF16), pack2(v[2], v[3], BF16), pack2(v[4], v[5], BF16), pack2(v[6], v[7], BF16));
+        if constexpr (sizeof(E) == 4) w = make_uint4(__float_as_uint(v[0].x), __float_as_uint(v[0].y), __float_as_uint(v[1].x), __float_as_uint(v[1].y));
+        else w = make_uint4(pack2(v[0].x, v[0].y, BF16), pack2(v[1].x, v[1].y, BF16), pack2(v[2].x, v[2].y, BF16), pack2(v[3].x, v[3].y, BF16));
     }
     static constexpr int BF16 [[maybe_unused]] = std::is_same<E, __nv_bfloat16>::value;
 };
 
-// N weights from column i on
+// 2 N weights from column i on
 template <class W, int N>
-__device__ __forceinline__ void load_weights(const void* base, int i, float (&v)[N])
+__device__ __forceinline__ void load_weights(const void* base, int i, float2 (&v)[N])
 {
     const W* p = static_cast<const W*>(base) + i;
-    constexpr int EACH = 16 / (int)sizeof(W);
-    if constexpr (EACH <= N) {
 #pragma unroll
-        for (int j = 0; j < N; j += EACH) {
-            Piece<W> q;
-            q.load(p + j);
-            q.get(v + j);
+    for (int j = 0; j < N; j += Piece<W>::PAIRS) {
+        Piece<W> q;
+        q.load(p + 2 * j);
+        q.get(v + j);
+    }
+}
+
+// The arithmetic goes in pairs (one instruction for two values): what bounds these kernels next to HBM is the issue of instructions.
+__device__ __forceinline__ float2 twice(float v) { return make_float2(v, v); }
+
+// The sums of N = 1 or 2 values over the `warps` warps of a row's group, to every thread of it; `part` is this group's own, and another one
+// than that of the sums before and after (which is what lets one barrier do).  Two values: after the first exchange the lower lanes sum the one
+// and the upper lanes the other.
+template <int N>
+__device__ __forceinline__ void group_sums(float (&v)[N], float (*part)[N], int warps, int warp, int barrier)
+{
+    const int lane = threadIdx.x & 31;
+    float s = v[0];
+    if (N == 2) {
+        const float give = lane < 16 ? v[N - 1] : v[0];
+        s = (lane < 16 ? v[0] : v[N - 1]) + __shfl_xor_sync(0xffffffffu, give, 16);
+    } else {
+        s += __shfl_xor_sync(0xffffffffu, s, 16);
+    }
+#pragma unroll
+    for (int d = 8; d > 0; d >>= 1) s += __shfl_xor_sync(0xffffffffu, s, d);
+    if (warps == 1) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = N == 1 ? s : __shfl_sync(0xffffffffu, s, 16 * i);
+        return;
+    }
+    if (N == 1 ? lane == 0 : (lane & 15) == 0) part[warp][lane / 16 % N] = s;
+    asm volatile("bar.sync %0, %1;" ::"r"(barrier), "r"(32 * warps) : "memory");
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = 0.f;
+    for (int w = 0; w < warps; ++w) {
+        if constexpr (N == 2) {
+            const float2 q = *reinterpret_cast<const float2*>(part[w]);
+            v[0] += q.x;
+            v[1] += q.y;
+        } else {
+            v[0] += part[w][0];
         }
     }
 }
 
-// The sums of N values over the `warps` warps of a row's group, to every thread of it; `part` is this group's own, and another one than
-// that of the sums before and after (which is what lets one barrier do).
-template <int N>
-__device__ __forceinline__ void group_sums(float (&v)[N], float (*part)[N], int warps, int warp, int barrier)
+// s / n by n's inverse and one step of correction: the mean of equal values is that value
+__device__ __forceinline__ float over(float s, float n, float inv)
 {
-#pragma unroll
-    for (int d = 16; d > 0; d >>= 1)
-#pragma unroll
-        for (int i = 0; i < N; ++i) v[i] += __shfl_xor_sync(0xffffffffu, v[i], d);
-    if (warps == 1) return;
-    if ((threadIdx.x & 31) == 0)
-#pragma unroll
-        for (int i = 0; i < N; ++i) part[warp][i] = v[i];
-    asm volatile("bar.sync %0, %1;" ::"r"(barrier), "r"(32 * warps) : "memory");
-#pragma unroll
-    for (int i = 0; i < N; ++i) v[i] = 0.f;
-    for (int w = 0; w < warps; ++w)
-#pragma unroll
-        for (int i = 0; i < N; ++i) v[i] += part[w][i];
+    const float q = s * inv;
+    return fmaf(fmaf(-q, n, s), inv, q);
 }
 
 constexpr int FRONT_THREADS = 256, FRONT_MOST = 1024;  // a block holds as many rows as groups fit into 256 threads, or one
@@ -169,54 +191,56 @@ __global__ void __launch_bounds__(FRONT_MOST) k_norm(const NormArgs a)
             if (res) pr[c].load(res + i);
         }
     }
-    float v[P::COUNT][P::N], s[1] = {0.f};
+    float2 v[P::COUNT][P::PAIRS], s2 = twice(0.f);
 #pragma unroll
     for (int c = 0; c < P::COUNT; ++c) {
         const int i = (c * a.group + t) * P::N;
         if (i < a.D) {
             px[c].get(v[c]);
             if (res) {
-                float r[P::N];
+                float2 r[P::PAIRS];
                 pr[c].get(r);
 #pragma unroll
-                for (int j = 0; j < P::N; ++j) v[c][j] += r[j];
+                for (int j = 0; j < P::PAIRS; ++j) v[c][j] = __fadd2_rn(v[c][j], r[j]);
                 px[c].put(v[c]);
                 px[c].get(v[c]);
                 if (a.sum) px[c].store(static_cast<E*>(a.sum) + row * a.lds + i);
             }
 #pragma unroll
-            for (int j = 0; j < P::N; ++j) s[0] += v[c][j];
+            for (int j = 0; j < P::PAIRS; ++j) s2 = __fadd2_rn(s2, v[c][j]);
         }
     }
+    float s[1] = {s2.x + s2.y};
     group_sums(s, part0 + first, warps, threadIdx.x / 32 - first, 1 + group);
-    const float mean = s[0] / (float)a.D;
-    s[0] = 0.f;
+    const float n = (float)a.D, inv = 1.f / n, mean = over(s[0], n, inv);
+    s2 = twice(0.f);
 #pragma unroll
     for (int c = 0; c < P::COUNT; ++c)
         if ((c * a.group + t) * P::N < a.D)
 #pragma unroll
-            for (int j = 0; j < P::N; ++j) {
-                v[c][j] -= mean;
-                s[0] = fmaf(v[c][j], v[c][j], s[0]);
+            for (int j = 0; j < P::PAIRS; ++j) {
+                v[c][j] = __fadd2_rn(v[c][j], twice(-mean));
+                s2 = __ffma2_rn(v[c][j], v[c][j], s2);
             }
+    s[0] = s2.x + s2.y;
     group_sums(s, part1 + first, warps, threadIdx.x / 32 - first, 1 + group);
-    const float r = 1.f / sqrtf(s[0] / (float)a.D + a.eps);
+    const float r = rsqrtf(s[0] * inv + a.eps);
 #pragma unroll
     for (int c = 0; c < P::COUNT; ++c) {
         const int i = (c * a.group + t) * P::N;
         if (i >= a.D) continue;
-        float w[P::N];
+        float2 w[P::PAIRS];
 #pragma unroll
-        for (int j = 0; j < P::N; ++j) v[c][j] *= r;
+        for (int j = 0; j < P::PAIRS; ++j) v[c][j] = __fmul2_rn(v[c][j], twice(r));
         if (a.weight) {
             load_weights<W>(a.weight, i, w);
 #pragma unroll
-            for (int j = 0; j < P::N; ++j) v[c][j] *= w[j];
+            for (int j = 0; j < P::PAIRS; ++j) v[c][j] = __fmul2_rn(v[c][j], w[j]);
         }
         if (a.bias) {
             load_weights<W>(a.bias, i, w);
 #pragma unroll
-            for (int j = 0; j < P::N; ++j) v[c][j] += w[j];
+            for (int j = 0; j < P::PAIRS; ++j) v[c][j] = __fadd2_rn(v[c][j], w[j]);
         }
         px[c].put(v[c]);
         px[c].store(static_cast<E*>(a.y) + row * a.ldy + i);
@@ -233,9 +257,10 @@ constexpr int back_smem()
     return 8 / (int)sizeof(E) * 3 * Piece<E>::COUNT * BACK_THREADS * 16;
 }
 
-__device__ __forceinline__ void copy16(void* to, const void* from)
+template <int OFFSET>
+__device__ __forceinline__ void copy16(uint32_t to, const void* from)
 {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(to)), "l"(from) : "memory");
+    asm volatile("cp.async.cg.shared.global [%0 + %2], [%1], 16;" ::"r"(to), "l"(from), "n"(OFFSET) : "memory");
 }
 __device__ __forceinline__ void copies_end() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>
@@ -247,102 +272,122 @@ __device__ __forceinline__ void copies_wait()
 template <class E, class W>
 __global__ void __launch_bounds__(BACK_THREADS, 1) k_norm_back(const NormBackArgs a)
 {
-    __shared__ float part0[BACK_THREADS / 32][2], part1[BACK_THREADS / 32][2];
+    __shared__ __align__(8) float part0[BACK_THREADS / 32][2], part1[BACK_THREADS / 32][2];
     extern __shared__ __align__(16) uint4 ring[];  // [DEPTH][x, dy, dsum][COUNT][BACK_THREADS]; at the end the columns' sums, [2][D]
     using P = Piece<E>;
     constexpr int DEPTH = 8 / (int)sizeof(E);
     const int group = threadIdx.x / a.group, t = threadIdx.x - group * a.group, warps = a.group / 32, first = group * warps, groups = BACK_THREADS / a.group;
     const int warp = threadIdx.x / 32 - first;
     enter();
-    float w[P::COUNT][P::N], dw[P::COUNT][P::N], db[P::COUNT][P::N];
-    const float n = (float)a.D;  // (divided by, not multiplied by its inverse: the mean of equal values is that value)
+    float2 w[P::COUNT][P::PAIRS], dw[P::COUNT][P::PAIRS], db[P::COUNT][P::PAIRS];
+    const float n = (float)a.D, inv = 1.f / n;
+    constexpr int WHAT = P::COUNT * BACK_THREADS * 16, STAGE = 3 * WHAT, RING = DEPTH * STAGE;  // bytes of one of x, dy and dsum, of a row's place, of all
+    unsigned char* mine = reinterpret_cast<unsigned char*>(ring) + threadIdx.x * 16;
+    const uint32_t mine_at = (uint32_t)__cvta_generic_to_shared(mine);
+    auto piece = [&](int stage, int what, int c) { return reinterpret_cast<uint4*>(mine + stage + what * WHAT + c * (BACK_THREADS * 16)); };
+    const int i0 = t * P::N, far = a.group * P::N;  // this thread's first column, and from one of its pieces to the next
 #pragma unroll
     for (int c = 0; c < P::COUNT; ++c) {
-        const int i = (c * a.group + t) * P::N;
 #pragma unroll
-        for (int j = 0; j < P::N; ++j) w[c][j] = 1.f, dw[c][j] = db[c][j] = 0.f;
-        if (a.weight && i < a.D) load_weights<W>(a.weight, i, w[c]);
+        for (int j = 0; j < P::PAIRS; ++j) w[c][j] = twice(1.f), dw[c][j] = db[c][j] = twice(0.f);
+        if (a.weight && i0 + c * far < a.D) load_weights<W>(a.weight, i0 + c * far, w[c]);
     }
-    auto slot = [&](int stage, int what, int c) { return ring + ((stage * 3 + what) * P::COUNT + c) * BACK_THREADS + threadIdx.x; };
-    auto fetch = [&](int64_t row, int stage) {
-        if (row < a.T) {
-#pragma unroll
-            for (int c = 0; c < P::COUNT; ++c) {
-                const int i = (c * a.group + t) * P::N;
-                if (i < a.D) {
-                    copy16(slot(stage, 0, c), static_cast<const E*>(a.x) + row * a.ldx + i);
-                    copy16(slot(stage, 1, c), static_cast<const E*>(a.dy) + row * a.lddy + i);
-                    if (a.dsum) copy16(slot(stage, 2, c), static_cast<const E*>(a.dsum) + row * a.ldds + i);
-                }
-            }
-        }
-        copies_end();
-    };
     // what is not copied stays zero: columns beyond the row's end, and dsum where there is none
 #pragma unroll
-    for (int stage = 0; stage < DEPTH; ++stage)
+    for (int stage = 0; stage < RING; stage += STAGE)
 #pragma unroll
         for (int what = 0; what < 3; ++what)
 #pragma unroll
             for (int c = 0; c < P::COUNT; ++c)
-                if ((c * a.group + t) * P::N >= a.D || (what == 2 && !a.dsum)) *slot(stage, what, c) = make_uint4(0u, 0u, 0u, 0u);
+                if (i0 + c * far >= a.D || (what == 2 && !a.dsum)) *piece(stage, what, c) = make_uint4(0u, 0u, 0u, 0u);
     int64_t row = (int64_t)blockIdx.x * groups + group;
     const int64_t step = (int64_t)gridDim.x * groups;
+    // the next row to fetch, and where it lies
+    int64_t ahead = row;
+    const E *fx = static_cast<const E*>(a.x) + row * a.ldx + i0, *fg = static_cast<const E*>(a.dy) + row * a.lddy + i0;
+    const E* fs = a.dsum ? static_cast<const E*>(a.dsum) + row * a.ldds + i0 : nullptr;
+    E* to = a.dx ? static_cast<E*>(a.dx) + row * a.D + i0 : nullptr;
+    auto fetch = [&](int stage) {
+        if (ahead < a.T) {
+            auto copy = [&](auto c) {
+                constexpr int C = decltype(c)::value, AT = C * (BACK_THREADS * 16);
+                if (i0 + C * far < a.D) {
+                    copy16<AT>(mine_at + stage, fx + C * far);
+                    copy16<AT + WHAT>(mine_at + stage, fg + C * far);
+                    if (fs) copy16<AT + 2 * WHAT>(mine_at + stage, fs + C * far);
+                }
+            };
+            copy(std::integral_constant<int, 0>());
+            copy(std::integral_constant<int, 1>());
+            if constexpr (P::COUNT == 4) {
+                copy(std::integral_constant<int, 2>());
+                copy(std::integral_constant<int, 3>());
+            }
+            ahead += step;
+            fx += step * a.ldx;
+            fg += step * a.lddy;
+            if (fs) fs += step * a.ldds;
+        }
+        copies_end();
+    };
+    static_assert(P::COUNT == 2 || P::COUNT == 4, "pieces of a thread");
 #pragma unroll
-    for (int k = 0; k < DEPTH - 1; ++k) fetch(row + k * step, k);
+    for (int k = 0; k < DEPTH - 1; ++k) fetch(k * STAGE);
     int stage = 0;
     for (; row < a.T; row += step) {
-        fetch(row + (DEPTH - 1) * step, stage == 0 ? DEPTH - 1 : stage - 1);  // (the place of the row before)
+        fetch(stage == 0 ? RING - STAGE : stage - STAGE);  // (the place of the row before)
         copies_wait<DEPTH - 1>();
-        float v[P::COUNT][P::N], g[P::COUNT][P::N], s[2] = {0.f, 0.f};
+        float2 v[P::COUNT][P::PAIRS], g[P::COUNT][P::PAIRS], s0 = twice(0.f), s1 = twice(0.f);
 #pragma unroll
         for (int c = 0; c < P::COUNT; ++c) {
             P q;
-            q.w = *slot(stage, 0, c);
+            q.w = *piece(stage, 0, c);
             q.get(v[c]);
-            q.w = *slot(stage, 1, c);
+            q.w = *piece(stage, 1, c);
             q.get(g[c]);
 #pragma unroll
-            for (int j = 0; j < P::N; ++j) {
-                s[0] += v[c][j];
-                s[1] = fmaf(g[c][j], w[c][j], s[1]);
+            for (int j = 0; j < P::PAIRS; ++j) {
+                s0 = __fadd2_rn(s0, v[c][j]);
+                s1 = __ffma2_rn(g[c][j], w[c][j], s1);
             }
         }
+        float s[2] = {s0.x + s0.y, s1.x + s1.y};
         group_sums(s, part0 + first, warps, warp, 1 + group);
-        const float mean = s[0] / n, d_mean = s[1] / n;
-        s[0] = s[1] = 0.f;
+        const float mean = over(s[0], n, inv), d_mean = over(s[1], n, inv);
+        s0 = s1 = twice(0.f);
 #pragma unroll
         for (int c = 0; c < P::COUNT; ++c)
-            if ((c * a.group + t) * P::N < a.D)
+            if (i0 + c * far < a.D)
 #pragma unroll
-                for (int j = 0; j < P::N; ++j) {
-                    v[c][j] -= mean;
-                    s[0] = fmaf(v[c][j], v[c][j], s[0]);
-                    s[1] = fmaf(v[c][j], g[c][j] * w[c][j], s[1]);
+                for (int j = 0; j < P::PAIRS; ++j) {
+                    v[c][j] = __fadd2_rn(v[c][j], twice(-mean));
+                    s0 = __ffma2_rn(v[c][j], v[c][j], s0);
+                    s1 = __ffma2_rn(v[c][j], __fmul2_rn(g[c][j], w[c][j]), s1);
                 }
+        s[0] = s0.x + s0.y, s[1] = s1.x + s1.y;
         group_sums(s, part1 + first, warps, warp, 1 + group);
         // n sum (d n) / D = (h - mean) r^2 sum (d (h - mean)) / D
-        const float r = 1.f / sqrtf(s[0] / n + a.eps), along = s[1] / n * r * r;
+        const float r = rsqrtf(s[0] * inv + a.eps), along = -(s[1] * inv) * r * r;
 #pragma unroll
         for (int c = 0; c < P::COUNT; ++c) {
-            const int i = (c * a.group + t) * P::N;
-            float out[P::N];
+            float2 out[P::PAIRS];
             P q;
-            q.w = *slot(stage, 2, c);
+            q.w = *piece(stage, 2, c);
             q.get(out);
 #pragma unroll
-            for (int j = 0; j < P::N; ++j) {
-                const float d = g[c][j] * w[c][j];
-                dw[c][j] = fmaf(g[c][j], v[c][j] * r, dw[c][j]);
-                db[c][j] += g[c][j];
-                out[j] = fmaf(r, (d - d_mean) - v[c][j] * along, out[j]);
+            for (int j = 0; j < P::PAIRS; ++j) {
+                const float2 d = __ffma2_rn(g[c][j], w[c][j], twice(-d_mean));
+                dw[c][j] = __ffma2_rn(g[c][j], __fmul2_rn(v[c][j], twice(r)), dw[c][j]);
+                db[c][j] = __fadd2_rn(db[c][j], g[c][j]);
+                out[j] = __ffma2_rn(twice(r), __ffma2_rn(v[c][j], twice(along), d), out[j]);
             }
-            if (a.dx && i < a.D) {
+            if (to && i0 + c * far < a.D) {
                 q.put(out);
-                q.store(static_cast<E*>(a.dx) + row * a.D + i);
+                q.store(to + c * far);
             }
         }
-        stage = stage + 1 == DEPTH ? 0 : stage + 1;
+        if (to) to += step * a.D;
+        stage = stage + STAGE == RING ? 0 : stage + STAGE;
     }
     copies_wait<0>();
     float* columns = reinterpret_cast<float*>(ring);
@@ -352,12 +397,13 @@ __global__ void __launch_bounds__(BACK_THREADS, 1) k_norm_back(const NormBackArg
         if (group == k)
 #pragma unroll
             for (int c = 0; c < P::COUNT; ++c) {
-                const int i = (c * a.group + t) * P::N;
+                const int i = i0 + c * far;
                 if (i < a.D)
 #pragma unroll
-                    for (int j = 0; j < P::N; ++j) {
-                        columns[i + j] = k ? columns[i + j] + dw[c][j] : dw[c][j];
-                        columns[a.D + i + j] = k ? columns[a.D + i + j] + db[c][j] : db[c][j];
+                    for (int j = 0; j < P::PAIRS; ++j) {
+                        float2 *w0 = reinterpret_cast<float2*>(columns + i) + j, *b0 = reinterpret_cast<float2*>(columns + a.D + i) + j;
+                        *w0 = k ? __fadd2_rn(*w0, dw[c][j]) : dw[c][j];
+                        *b0 = k ? __fadd2_rn(*b0, db[c][j]) : db[c][j];
                     }
             }
         __syncthreads();
@@ -472,7 +518,13 @@ __global__ void __launch_bounds__(256) k_norm_join(const ColumnJoinArgs a)
     const int64_t i = (int64_t)blockIdx.x * 32 + lane;  // of 2 D sums
     float s = 0.f;
     if (i < 2 * (int64_t)a.D)
-        for (int p = warp; p < a.parts; p += 8) s += a.part[(int64_t)p * 2 * a.D + i];
+        for (int p = warp; p < a.parts; p += 64) {  // eight loads on their way at once
+            float v[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[k] = p + 8 * k < a.parts ? a.part[(int64_t)(p + 8 * k) * 2 * a.D + i] : 0.f;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) s += v[k];
+        }
     part[warp][lane] = s;
     __syncthreads();
     if (warp > 0 || i >= 2 * (int64_t)a.D) return;
