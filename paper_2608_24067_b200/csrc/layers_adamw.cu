@@ -24,6 +24,7 @@ namespace lay {
 namespace {
 
 constexpr int ADAM_THREADS = 256, ADAM_BLOCK = 256, ADAM_CHUNK = 8 * ADAM_THREADS;
+constexpr int ADAM_TIMES = 2, ADAM_CHUNK8 = ADAM_TIMES * ADAM_CHUNK;  // of k_adamw8
 
 struct Hyper {
     float keep, rate, b1, c1, b2, c2, k1, k2, eps;  // keep = 1 - rate decay; c = 1 - b; k = 1 / (1 - b^t)
@@ -129,15 +130,24 @@ __device__ __forceinline__ uint2 read_codes(const uint8_t* p, bool whole, int le
         if (i < left) w[i / 4] |= (uint32_t)p[i] << (8 * (i & 3));
     return make_uint2(w[0], w[1]);
 }
-__device__ __forceinline__ void write_codes(uint8_t* p, const uint32_t (&w)[2], bool whole, int left)
+__device__ __forceinline__ void write_codes(uint8_t* p, uint2 c, bool whole, int left)
 {
     if (whole) {
-        *reinterpret_cast<uint2*>(p) = make_uint2(w[0], w[1]);
+        *reinterpret_cast<uint2*>(p) = c;
     } else {
+        const uint32_t w[2] = {c.x, c.y};
 #pragma unroll
         for (int i = 0; i < 8; ++i)
             if (i < left) p[i] = (uint8_t)(w[i / 4] >> (8 * (i & 3)));
     }
+}
+
+// one instruction and its scaling for subnormal numbers, off by 2^-22
+__device__ __forceinline__ float fast_sqrt(float x)
+{
+    float y;
+    asm("sqrt.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
 }
 
 // 2^(e - 127) of an exponent byte; 255 (a block that holds an infinity or NaN) gives infinity, and 0 times it NaN
@@ -145,39 +155,70 @@ __device__ __forceinline__ float power_of(uint32_t e) { return __uint_as_float(e
 // 2^(127 - e), e <= 255
 __device__ __forceinline__ float power_below(uint32_t e) { return __uint_as_float(e < 254u ? (254u - e) << 23 : e == 254u ? 0x00400000u : 0x00200000u); }
 
-// the values of eight codes: a code's bits are the top of a number of the smallest exponents, which TOP lifts to [0, 2)
+__device__ __forceinline__ float2 twice(float v) { return make_float2(v, v); }
+
+// The sum of two products that are rounded by themselves.  (Of a packed product and a packed sum the compiler makes one rounding, whatever they say.)
+__device__ __forceinline__ float2 sum2(float2 a, float2 b) { return make_float2(__fadd_rn(a.x, b.x), __fadd_rn(a.y, b.y)); }
+
+// the values of eight codes: a code's bits are the top of a number of the smallest exponents, which 2^112 (or 2^96) lifts to [0, 2)
 template <bool SIGNED>
-__device__ __forceinline__ void decode8(uint2 c, uint32_t e, float (&v)[8])
+__device__ __forceinline__ void decode8(uint2 c, uint32_t e, float2 (&v)[4])
 {
-    const float by = power_of(e), top = SIGNED ? 0x1p112f : 0x1p96f;
-    const uint32_t w[2] = {c.x, c.y};
+    const float2 by = twice(power_of(e)), top = twice(SIGNED ? 0x1p112f : 0x1p96f);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const uint32_t code = (w[i / 4] >> (8 * (i & 3))) & 255u;
-        const float f = (__uint_as_float((SIGNED ? code & 127u : code) << 20) * top) * by;
-        v[i] = SIGNED && code > 127u ? -f : f;
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t w = i < 2 ? c.x : c.y;
+        const int at = 16 * (i & 1);  // of the lower byte
+        uint32_t lo, hi;
+        if (SIGNED) {  // the sign to the top, the other seven bits to 20..26
+            lo = (uint32_t)((int32_t)(w << (24 - at)) >> 4) & 0x87f00000u;
+            hi = (uint32_t)((int32_t)(w << (16 - at)) >> 4) & 0x87f00000u;
+        } else {
+            lo = (at ? w << 4 : w << 20) & 0x0ff00000u;
+            hi = (at ? w >> 4 : w << 12) & 0x0ff00000u;
+        }
+        v[i] = __fmul2_rn(__fmul2_rn(make_float2(__uint_as_float(lo), __uint_as_float(hi)), top), by);
     }
 }
 
-// codes of eight values of a block of a warp's 256, and the block's exponent; h: 32 random bits for each, the lower half for m, the upper for v
-template <bool SIGNED>
-__device__ __forceinline__ uint32_t encode8(const float (&v)[8], const uint32_t (&h)[8], uint32_t (&w)[2])
+// the larger magnitude, or NaN
+__device__ __forceinline__ float larger(float a, float b)
 {
-    uint32_t most = 0;
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(fabsf(b)));
+    return r;
+}
+
+// codes of eight values of a block of a warp's 256, and the block's exponent; h: 32 random bits for each, the lower half for m, the upper for v.
+// (A code above the largest is met only where the exponent is 255.)
+template <bool SIGNED>
+__device__ __forceinline__ uint32_t encode8(const float2 (&v)[4], const uint32_t (&h)[8], uint2& codes)
+{
+    float most = 0.f;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) most = max(most, __float_as_uint(v[i]) & 0x7fffffffu);
-    const uint32_t e = (min(__reduce_max_sync(0xffffffffu, most), 0x7f800000u) + 0x100000u) >> 23;  // (a fraction of 7 / 8 and more carries)
-    const float up = power_below(e);
-    w[0] = w[1] = 0u;
+    for (int i = 0; i < 4; ++i) most = larger(larger(most, v[i].x), v[i].y);
+    // a fraction of 7 / 8 and more carries into the exponent
+    const uint32_t e = (min(__reduce_max_sync(0xffffffffu, __float_as_uint(most)), 0x7f800000u) + 0x100000u) >> 23;
+    const float2 up = twice(power_below(e)), top = twice(SIGNED ? 0x1p-112f : 0x1p-96f);
+    uint32_t u[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const float a = __fmul_rn(__fmul_rn(fabsf(v[i]), up), SIGNED ? 0x1p-112f : 0x1p-96f);
-        const uint32_t r = SIGNED ? (h[i] & 0xffffu) << 4 : (h[i] >> 16) << 4;
-        uint32_t code = min((__float_as_uint(a) + r) >> 20, SIGNED ? 127u : 255u);
-        if (SIGNED) code |= v[i] < 0.f ? 128u : 0u;
-        else if (v[i] > 0.f) code = max(code, 1u);
-        w[i / 4] |= code << (8 * (i & 3));
+    for (int i = 0; i < 4; ++i) {
+        const float2 a = __fmul2_rn(__ffma2_rn(v[i], up, twice(0.f)), top);  // (-0 becomes 0)
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const float x = k ? v[i].y : v[i].x;
+            const uint32_t bits = __float_as_uint(k ? a.y : a.x), r = h[2 * i + k];
+            if (SIGNED) {
+                const uint32_t sum = bits + ((r << 4) & 0xffff0u);
+                u[2 * i + k] = ((sum >> 20) & 0x7fu) | ((sum >> 24) & 0x80u);
+            } else {
+                u[2 * i + k] = max((bits + ((r >> 12) & 0xffff0u)) >> 20, min(__float_as_uint(x), 1u));
+            }
+        }
     }
+    constexpr uint32_t PICK = 0x40u;  // the lowest bytes of two words
+    codes.x = __byte_perm(__byte_perm(u[0], u[1], PICK), __byte_perm(u[2], u[3], PICK), 0x5410);
+    codes.y = __byte_perm(__byte_perm(u[4], u[5], PICK), __byte_perm(u[6], u[7], PICK), 0x5410);
     return e;
 }
 
@@ -194,36 +235,51 @@ __device__ __forceinline__ int tensor_of(const TABLE& t, uint32_t chunk)
     return lo;
 }
 
+// Where a thread's eight elements lie, and how many of them there are.
+struct Place {
+    int64_t at;
+    int left;
+    bool whole;  // all eight, in vectors
+};
+__device__ __forceinline__ Place place_of(const som_adamw_tensor& it, int64_t at)
+{
+    const uintptr_t all = reinterpret_cast<uintptr_t>(it.param) | reinterpret_cast<uintptr_t>(it.grad) | reinterpret_cast<uintptr_t>(it.copy) |
+                          reinterpret_cast<uintptr_t>(it.m) | reinterpret_cast<uintptr_t>(it.v);
+    const int left = it.n - at >= 8 ? 8 : it.n > at ? (int)(it.n - at) : 0;
+    return {at, left, left == 8 && (all & 15u) == 0};
+}
+
+template <bool P16, bool G16, class TABLE>
+__device__ __forceinline__ void read_params(const TABLE& t, const som_adamw_tensor& it, const Place& q, float (&p)[8], float (&g)[8])
+{
+    if (P16) read8(static_cast<const uint16_t*>(it.param) + q.at, p, q.whole, q.left, t.param_bf16);
+    else read8(static_cast<const float*>(it.param) + q.at, p, q.whole, q.left);
+    if (G16) read8(static_cast<const uint16_t*>(it.grad) + q.at, g, q.whole, q.left, t.grad_bf16);
+    else read8(static_cast<const float*>(it.grad) + q.at, g, q.whole, q.left);
+}
+
+template <bool P16, bool COPY, class TABLE>
+__device__ __forceinline__ void write_params(const TABLE& t, const som_adamw_tensor& it, const Place& q, const float (&p)[8])
+{
+    if (P16) write8(static_cast<uint16_t*>(it.param) + q.at, p, q.whole, q.left, t.param_bf16);
+    else write8(static_cast<float*>(it.param) + q.at, p, q.whole, q.left);
+    if (COPY) write8(static_cast<uint16_t*>(it.copy) + q.at, p, q.whole, q.left, t.copy_bf16);
+}
+
 // P16, G16: 16-bit parameters, gradients; COPY: a 16-bit copy of fp32 parameters
-template <bool P16, bool G16, bool COPY, int BITS, int CAP>
+template <bool P16, bool G16, bool COPY, int CAP>
 __global__ void __launch_bounds__(ADAM_THREADS) k_adamw(const __grid_constant__ AdamTable<CAP> t)
 {
     enter();
     const som_adamw_tensor& it = t.item[tensor_of(t, blockIdx.x)];
-    const int64_t at = (int64_t)(blockIdx.x - it.first_chunk) * ADAM_CHUNK + threadIdx.x * 8;
+    const Place q = place_of(it, (int64_t)(blockIdx.x - it.first_chunk) * ADAM_CHUNK + threadIdx.x * 8);
     const float scale = t.scale ? *t.scale : 1.f;
-    if (!(fabsf(scale) <= 3.4028235e38f)) return;  // an infinity or NaN: the step is left out
-    if (at - (int)(threadIdx.x & 31) * 8 >= it.n) return;  // none of the warp's
+    if (!(fabsf(scale) <= 3.4028235e38f) || q.left == 0) return;  // (an infinity or NaN: the step is left out)
     const Hyper h = t.h_at ? *t.h_at : t.h;
-    const int left = it.n - at >= 8 ? 8 : it.n > at ? (int)(it.n - at) : 0;
-    const uintptr_t all = reinterpret_cast<uintptr_t>(it.param) | reinterpret_cast<uintptr_t>(it.grad) | reinterpret_cast<uintptr_t>(it.copy) |
-                          reinterpret_cast<uintptr_t>(it.m) | reinterpret_cast<uintptr_t>(it.v);
-    const bool whole = left == 8 && (all & 15u) == 0;
-
     float p[8], g[8], m[8], v[8];
-    if (P16) read8(static_cast<const uint16_t*>(it.param) + at, p, whole, left, t.param_bf16);
-    else read8(static_cast<const float*>(it.param) + at, p, whole, left);
-    if (G16) read8(static_cast<const uint16_t*>(it.grad) + at, g, whole, left, t.grad_bf16);
-    else read8(static_cast<const float*>(it.grad) + at, g, whole, left);
-    const int64_t blocks = (it.n + ADAM_BLOCK - 1) / ADAM_BLOCK, block = at / ADAM_BLOCK;
-    if (BITS == 8) {
-        const uint2 mc = read_codes(static_cast<const uint8_t*>(it.m) + at, whole, left), vc = read_codes(static_cast<const uint8_t*>(it.v) + at, whole, left);
-        decode8<true>(mc, it.exponents[block], m);
-        decode8<false>(vc, it.exponents[blocks + block], v);
-    } else {
-        read8(static_cast<const float*>(it.m) + at, m, whole, left);
-        read8(static_cast<const float*>(it.v) + at, v, whole, left);
-    }
+    read_params<P16, G16>(t, it, q, p, g);
+    read8(static_cast<const float*>(it.m) + q.at, m, q.whole, q.left);
+    read8(static_cast<const float*>(it.v) + q.at, v, q.whole, q.left);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         if (t.scale) g[i] = __fmul_rn(g[i], scale);
@@ -232,28 +288,77 @@ __global__ void __launch_bounds__(ADAM_THREADS) k_adamw(const __grid_constant__ 
         const float change = m[i] * h.k1 / (sqrtf(v[i] * h.k2) + h.eps);
         p[i] = p[i] * h.keep - change * h.rate;
     }
-    if (P16) write8(static_cast<uint16_t*>(it.param) + at, p, whole, left, t.param_bf16);
-    else write8(static_cast<float*>(it.param) + at, p, whole, left);
-    if (COPY) write8(static_cast<uint16_t*>(it.copy) + at, p, whole, left, t.copy_bf16);
-    if (BITS == 8) {
-        const uint32_t key = mix(mix((uint32_t)block) ^ (h.seed + it.number * 0x9E3779B9u));
-        uint32_t r[8], w[2];
+    write_params<P16, COPY>(t, it, q, p);
+    write8(static_cast<float*>(it.m) + q.at, m, q.whole, q.left);
+    write8(static_cast<float*>(it.v) + q.at, v, q.whole, q.left);
+}
+
+// The same with moments in 8 bits.  Bound by the issue of instructions as much as by HBM: arithmetic goes in pairs, square root and quotient are
+// the approximations (2^-22 of the change), and a thread takes two times eight elements.
+template <bool P16, bool G16, bool COPY, int CAP>
+__global__ void __launch_bounds__(ADAM_THREADS) k_adamw8(const __grid_constant__ AdamTable<CAP> t)
+{
+    enter();
+    const som_adamw_tensor& it = t.item[tensor_of(t, blockIdx.x)];
+    const float scale = t.scale ? *t.scale : 1.f;
+    if (!(fabsf(scale) <= 3.4028235e38f)) return;
+    const Hyper h = t.h_at ? *t.h_at : t.h;
+    const int lane = threadIdx.x & 31;
+    const int64_t blocks = (it.n + ADAM_BLOCK - 1) / ADAM_BLOCK, first = (int64_t)(blockIdx.x - it.first_chunk) * ADAM_CHUNK8 + threadIdx.x * 8;
+    Place q[ADAM_TIMES];
+    float p[ADAM_TIMES][8], g[ADAM_TIMES][8];
+    uint2 mc[ADAM_TIMES], vc[ADAM_TIMES];
+    uint32_t em[ADAM_TIMES], ev[ADAM_TIMES];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            r[i] = mix(key + ((threadIdx.x & 31) * 8 + i) * 0x6A09E667u);
-            if (i >= left) m[i] = v[i] = 0.f;  // (beyond the tensor's end)
+    for (int k = 0; k < ADAM_TIMES; ++k) {
+        q[k] = place_of(it, first + k * ADAM_CHUNK);
+        if (q[k].at - lane * 8 >= it.n) break;  // none of the warp's
+        read_params<P16, G16>(t, it, q[k], p[k], g[k]);
+        mc[k] = read_codes(static_cast<const uint8_t*>(it.m) + q[k].at, q[k].whole, q[k].left);
+        vc[k] = read_codes(static_cast<const uint8_t*>(it.v) + q[k].at, q[k].whole, q[k].left);
+        const int64_t block = q[k].at / ADAM_BLOCK;
+        em[k] = it.exponents[block];
+        ev[k] = it.exponents[blocks + block];
+    }
+#pragma unroll
+    for (int k = 0; k < ADAM_TIMES; ++k) {
+        if (q[k].at - lane * 8 >= it.n) break;
+        float2 m[4], v[4];
+        decode8<true>(mc[k], em[k], m);
+        decode8<false>(vc[k], ev[k], v);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            float2 gi = make_float2(g[k][2 * i], g[k][2 * i + 1]);
+            if (t.scale) gi = __fmul2_rn(gi, twice(scale));
+            m[i] = sum2(__fmul2_rn(m[i], twice(h.b1)), __fmul2_rn(gi, twice(h.c1)));
+            v[i] = sum2(__fmul2_rn(v[i], twice(h.b2)), __fmul2_rn(__fmul2_rn(gi, gi), twice(h.c2)));
+            const float2 up = __fmul2_rn(m[i], twice(h.k1)), under = __fmul2_rn(v[i], twice(h.k2));
+            const float2 change = make_float2(__fdividef(up.x, fast_sqrt(under.x) + h.eps), __fdividef(up.y, fast_sqrt(under.y) + h.eps));
+            const float2 kept = __fmul2_rn(make_float2(p[k][2 * i], p[k][2 * i + 1]), twice(h.keep)), now = __ffma2_rn(change, twice(-h.rate), kept);
+            p[k][2 * i] = now.x, p[k][2 * i + 1] = now.y;
         }
-        const uint32_t em = encode8<true>(m, r, w);
-        write_codes(static_cast<uint8_t*>(it.m) + at, w, whole, left);
-        const uint32_t ev = encode8<false>(v, r, w);
-        write_codes(static_cast<uint8_t*>(it.v) + at, w, whole, left);
-        if ((threadIdx.x & 31) == 0) {
-            it.exponents[block] = (uint8_t)em;
-            it.exponents[blocks + block] = (uint8_t)ev;
+        write_params<P16, COPY>(t, it, q[k], p[k]);
+        const int64_t block = q[k].at / ADAM_BLOCK;
+        const uint32_t key = mix(mix((uint32_t)block) ^ (h.seed + it.number * 0x9E3779B9u)) + lane * (8u * 0x6A09E667u);
+        uint32_t r[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) r[i] = mix(key + i * 0x6A09E667u);
+        if (q[k].left < 8) {  // (beyond the tensor's end)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if (2 * i >= q[k].left) m[i].x = v[i].x = 0.f;
+                if (2 * i + 1 >= q[k].left) m[i].y = v[i].y = 0.f;
+            }
         }
-    } else {
-        write8(static_cast<float*>(it.m) + at, m, whole, left);
-        write8(static_cast<float*>(it.v) + at, v, whole, left);
+        uint2 codes;
+        const uint32_t e1 = encode8<true>(m, r, codes);
+        write_codes(static_cast<uint8_t*>(it.m) + q[k].at, codes, q[k].whole, q[k].left);
+        const uint32_t e2 = encode8<false>(v, r, codes);
+        write_codes(static_cast<uint8_t*>(it.v) + q[k].at, codes, q[k].whole, q[k].left);
+        if (lane == 0) {
+            it.exponents[block] = (uint8_t)e1;
+            it.exponents[blocks + block] = (uint8_t)e2;
+        }
     }
 }
 
@@ -269,11 +374,13 @@ __global__ void __launch_bounds__(ADAM_THREADS) k_adamw_moments(const __grid_con
     const uintptr_t all = reinterpret_cast<uintptr_t>(it.param) | reinterpret_cast<uintptr_t>(it.copy) | reinterpret_cast<uintptr_t>(it.m) | reinterpret_cast<uintptr_t>(it.v);
     const bool whole = left == 8 && (all & 15u) == 0;
     const int64_t blocks = (it.n + ADAM_BLOCK - 1) / ADAM_BLOCK, block = at / ADAM_BLOCK;
-    float m[8], v[8];
-    decode8<true>(read_codes(static_cast<const uint8_t*>(it.m) + at, whole, left), it.exponents[block], m);
-    decode8<false>(read_codes(static_cast<const uint8_t*>(it.v) + at, whole, left), it.exponents[blocks + block], v);
-    write8(static_cast<uint16_t*>(it.param) + at, m, whole, left, 1);
-    write8(static_cast<uint16_t*>(it.copy) + at, v, whole, left, 1);
+    const uint2 mc = read_codes(static_cast<const uint8_t*>(it.m) + at, whole, left), vc = read_codes(static_cast<const uint8_t*>(it.v) + at, whole, left);
+    const uint32_t em = it.exponents[block], ev = it.exponents[blocks + block];
+    float2 m[4], v[4];
+    decode8<true>(mc, em, m);
+    decode8<false>(vc, ev, v);
+    write8(static_cast<uint16_t*>(it.param) + at, reinterpret_cast<const float(&)[8]>(m), whole, left, 1);
+    write8(static_cast<uint16_t*>(it.copy) + at, reinterpret_cast<const float(&)[8]>(v), whole, left, 1);
 }
 
 // Tensors a launch: what a kernel's parameters hold (32764 bytes), and fewer where there are few, since a launch copies them.
@@ -283,7 +390,8 @@ static_assert(sizeof(AdamTable<MOST_TENSORS>) <= 32764, "kernel parameters");
 template <bool P16, bool G16, bool COPY, int BITS>
 cudaError_t launch_adamw(som_layers* l, const AdamTable<MOST_TENSORS>& t, unsigned chunks, cudaStream_t st)
 {
-    if (t.count > FEW_TENSORS) return launch(l, k_adamw<P16, G16, COPY, BITS, MOST_TENSORS>, dim3(chunks), ADAM_THREADS, 0, st, 1, t);
+    if (t.count > FEW_TENSORS)
+        return launch(l, BITS == 8 ? k_adamw8<P16, G16, COPY, MOST_TENSORS> : k_adamw<P16, G16, COPY, MOST_TENSORS>, dim3(chunks), ADAM_THREADS, 0, st, 1, t);
     AdamTable<FEW_TENSORS> s;
     for (int i = 0; i < t.count; ++i) s.item[i] = t.item[i];
     s.count = t.count;
@@ -291,7 +399,7 @@ cudaError_t launch_adamw(som_layers* l, const AdamTable<MOST_TENSORS>& t, unsign
     s.h = t.h;
     s.h_at = t.h_at;
     s.scale = t.scale;
-    return launch(l, k_adamw<P16, G16, COPY, BITS, FEW_TENSORS>, dim3(chunks), ADAM_THREADS, 0, st, 1, s);
+    return launch(l, BITS == 8 ? k_adamw8<P16, G16, COPY, FEW_TENSORS> : k_adamw<P16, G16, COPY, FEW_TENSORS>, dim3(chunks), ADAM_THREADS, 0, st, 1, s);
 }
 
 template <int BITS>
@@ -308,7 +416,7 @@ bool off_by(const void* p, int bytes) { return (reinterpret_cast<uintptr_t>(p) &
 
 // Hands the tensors out to launches: run(first, count, chunks) with their first_chunk written to `to`
 template <class TABLE, class RUN>
-int in_launches(const som_adamw_tensor* tensors, int32_t count, TABLE& t, RUN&& run)
+int in_launches(const som_adamw_tensor* tensors, int32_t count, int chunk, TABLE& t, RUN&& run)
 {
     int32_t i = 0;
     while (i < count) {
@@ -316,7 +424,7 @@ int in_launches(const som_adamw_tensor* tensors, int32_t count, TABLE& t, RUN&& 
         t.count = 0;
         for (; i < count && t.count < MOST_TENSORS; ++i) {
             if (tensors[i].n == 0) continue;
-            const int64_t more = (tensors[i].n + ADAM_CHUNK - 1) / ADAM_CHUNK;
+            const int64_t more = (tensors[i].n + chunk - 1) / chunk;
             if (chunks + more > MOST_CHUNKS) break;
             som_adamw_tensor& to = t.item[t.count++];
             to = tensors[i];
@@ -378,7 +486,7 @@ int som_adamw(som_layers* l, int param_type, int grad_type, int copy_type, int b
         t.h_at = a.to;
     }
     t.h = hyper_of(step->rate, b1, b2, step->eps, step->decay, step->step_at ? 1 : step->step, step->seed);
-    return in_launches(tensors, count, t, [&](unsigned chunks) {
+    return in_launches(tensors, count, bits == 8 ? ADAM_CHUNK8 : ADAM_CHUNK, t, [&](unsigned chunks) {
         for (int i = 0; i < t.count; ++i)
             if (!copy) t.item[i].copy = nullptr;
         return outcome(l, bits == 8 ? launch_types<8>(l, t, param_type != SOM_F32, grad_type != SOM_F32, copy, chunks, st)
@@ -407,7 +515,7 @@ int som_adamw_moments(som_layers* l, int32_t count, const som_adamw_tensor* tens
             some[i].copy = v[from + i];
         }
         MomentTable<MOST_TENSORS> t;
-        LAY_TRY(in_launches(some, n, t, [&](unsigned chunks) {
+        LAY_TRY(in_launches(some, n, ADAM_CHUNK, t, [&](unsigned chunks) {
             MomentTable<FEW_TENSORS> s;
             for (int i = 0; i < t.count; ++i) s.item[i] = t.item[i];
             s.count = t.count;
