@@ -24,11 +24,14 @@ namespace lay {
 namespace {
 
 constexpr int ADAM_THREADS = 256, ADAM_BLOCK = 256, ADAM_CHUNK = 8 * ADAM_THREADS;
-constexpr int ADAM_TIMES = 2, ADAM_CHUNK8 = ADAM_TIMES * ADAM_CHUNK;  // of k_adamw8
 
 struct Hyper {
     float keep, rate, b1, c1, b2, c2, k1, k2, eps;  // keep = 1 - rate decay; c = 1 - b; k = 1 / (1 - b^t)
     uint32_t seed;
+};
+
+struct HyperPairs {
+    float2 keep, minus_rate, b1, c1, b2, c2, k1, k2, eps;
 };
 
 template <int CAP>
@@ -37,6 +40,7 @@ struct AdamTable {
     int count;
     int param_bf16, grad_bf16, copy_bf16;
     Hyper h;
+    HyperPairs pairs;  // the same
     const Hyper* h_at;  // in its place where the host does not know it
     const float* scale;
 };
@@ -62,6 +66,12 @@ __host__ __device__ inline Hyper hyper_of(double rate, double b1, double b2, dou
             (float)(1.0 / (1.0 - pow(b1, (double)step))), (float)(1.0 / (1.0 - pow(b2, (double)step))), (float)eps, seed};
 }
 
+__host__ __device__ inline HyperPairs pairs_of(const Hyper& h)
+{
+    auto two = [](float v) { return make_float2(v, v); };
+    return {two(h.keep), two(-h.rate), two(h.b1), two(h.c1), two(h.b2), two(h.c2), two(h.k1), two(h.k2), two(h.eps)};
+}
+
 __global__ void k_adamw_hyper(const HyperArgs a)
 {
     enter();
@@ -69,12 +79,17 @@ __global__ void k_adamw_hyper(const HyperArgs a)
     *a.to = hyper_of(a.rate_at ? (double)*a.rate_at : a.rate, a.b1, a.b2, a.eps, a.decay, step, a.step_at ? a.seed + (uint32_t)step : a.seed);
 }
 
-__device__ __forceinline__ uint32_t mix(uint32_t x)
+// mix(x) = y ^ (y >> 16) with y = mix_half(x)
+__device__ __forceinline__ uint32_t mix_half(uint32_t x)
 {
     x ^= x >> 16;
     x *= 0x9E3779B9u;
     x ^= x >> 15;
-    x *= 0xBB67AE85u;
+    return x * 0xBB67AE85u;
+}
+__device__ __forceinline__ uint32_t mix(uint32_t x)
+{
+    x = mix_half(x);
     return x ^ (x >> 16);
 }
 
@@ -142,11 +157,10 @@ __device__ __forceinline__ void write_codes(uint8_t* p, uint2 c, bool whole, int
     }
 }
 
-// one instruction and its scaling for subnormal numbers, off by 2^-22
-__device__ __forceinline__ float fast_sqrt(float x)
+__device__ __forceinline__ float fast_rsqrt(float x)
 {
     float y;
-    asm("sqrt.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
+    asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
 
@@ -171,54 +185,73 @@ __device__ __forceinline__ void decode8(uint2 c, uint32_t e, float2 (&v)[4])
         const int at = 16 * (i & 1);  // of the lower byte
         uint32_t lo, hi;
         if (SIGNED) {  // the sign to the top, the other seven bits to 20..26
-            lo = (uint32_t)((int32_t)(w << (24 - at)) >> 4) & 0x87f00000u;
-            hi = (uint32_t)((int32_t)(w << (16 - at)) >> 4) & 0x87f00000u;
-        } else {
-            lo = (at ? w << 4 : w << 20) & 0x0ff00000u;
-            hi = (at ? w >> 4 : w << 12) & 0x0ff00000u;
+            lo = (uint32_t)((int32_t)(w * (1u << (24 - at))) >> 4) & 0x87f00000u;
+            hi = (uint32_t)((int32_t)(w * (1u << (16 - at))) >> 4) & 0x87f00000u;
+        } else {  // (products: shifts have a pipe of half the width)
+            lo = (w & (0xffu << at)) * (1u << (20 - at));
+            hi = at ? (w >> 4) & 0x0ff00000u : (w & 0xff00u) * (1u << 12);
         }
         v[i] = __fmul2_rn(__fmul2_rn(make_float2(__uint_as_float(lo), __uint_as_float(hi)), top), by);
     }
 }
 
-// the larger magnitude, or NaN
-__device__ __forceinline__ float larger(float a, float b)
+// the largest magnitude, or NaN
+__device__ __forceinline__ float largest(float a, float b, float c)
 {
     float r;
-    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(fabsf(b)));
+    asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
     return r;
 }
 
-// codes of eight values of a block of a warp's 256, and the block's exponent; h: 32 random bits for each, the lower half for m, the upper for v.
+// 16 x; a product, since shifts have a pipe of half the width, and an instruction of its own, since the compiler (12.9) took the top bytes of x
+// itself for those of 16 x where x was negative
+__device__ __forceinline__ uint32_t times16(uint32_t x)
+{
+    uint32_t r;
+    asm("mul.lo.u32 %0, %1, 16;" : "=r"(r) : "r"(x));
+    return r;
+}
+
+__device__ __forceinline__ uint32_t top_bytes(uint32_t a, uint32_t b, uint32_t c, uint32_t d)
+{
+    return __byte_perm(__byte_perm(a, b, 0x0073), __byte_perm(c, d, 0x0073), 0x5410);
+}
+
+// codes of eight values of a block of a warp's 256, and the block's exponent; h: 16 random bits for each.
 // (A code above the largest is met only where the exponent is 255.)
 template <bool SIGNED>
 __device__ __forceinline__ uint32_t encode8(const float2 (&v)[4], const uint32_t (&h)[8], uint2& codes)
 {
     float most = 0.f;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) most = larger(larger(most, v[i].x), v[i].y);
+    for (int i = 0; i < 4; ++i) most = largest(most, v[i].x, v[i].y);
     // a fraction of 7 / 8 and more carries into the exponent
     const uint32_t e = (min(__reduce_max_sync(0xffffffffu, __float_as_uint(most)), 0x7f800000u) + 0x100000u) >> 23;
     const float2 up = twice(power_below(e)), top = twice(SIGNED ? 0x1p-112f : 0x1p-96f);
-    uint32_t u[8];
+    uint32_t u[8], bits[8];  // u: the code in the top byte, but for the sign
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const float2 a = __fmul2_rn(__ffma2_rn(v[i], up, twice(0.f)), top);  // (-0 becomes 0)
+        bits[2 * i] = __float_as_uint(a.x), bits[2 * i + 1] = __float_as_uint(a.y);
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            const float x = k ? v[i].y : v[i].x;
-            const uint32_t bits = __float_as_uint(k ? a.y : a.x), r = h[2 * i + k];
-            if (SIGNED) {
-                const uint32_t sum = bits + ((r << 4) & 0xffff0u);
-                u[2 * i + k] = ((sum >> 20) & 0x7fu) | ((sum >> 24) & 0x80u);
-            } else {
-                u[2 * i + k] = max((bits + ((r >> 12) & 0xffff0u)) >> 20, min(__float_as_uint(x), 1u));
+        for (int k = 2 * i; k < 2 * i + 2; ++k) u[k] = times16(bits[k]) + h[k] * 256u;
+    }
+    codes = make_uint2(top_bytes(u[0], u[1], u[2], u[3]), top_bytes(u[4], u[5], u[6], u[7]));
+    if (SIGNED) {  // (the signs of four at a time)
+        codes.x |= top_bytes(bits[0], bits[1], bits[2], bits[3]) & 0x80808080u;
+        codes.y |= top_bytes(bits[4], bits[5], bits[6], bits[7]) & 0x80808080u;
+    }
+    if (!SIGNED) {  // a code of 0 becomes 1 where the value is not 0
+        if ((((codes.x - 0x01010101u) & ~codes.x) | ((codes.y - 0x01010101u) & ~codes.y)) & 0x80808080u) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                uint32_t& w = i < 2 ? codes.x : codes.y;
+                const int at = 16 * (i & 1);
+                if (v[i].x > 0.f && !(w & (0xffu << at))) w |= 1u << at;
+                if (v[i].y > 0.f && !(w & (0xff00u << at))) w |= 0x100u << at;
             }
         }
     }
-    constexpr uint32_t PICK = 0x40u;  // the lowest bytes of two words
-    codes.x = __byte_perm(__byte_perm(u[0], u[1], PICK), __byte_perm(u[2], u[3], PICK), 0x5410);
-    codes.y = __byte_perm(__byte_perm(u[4], u[5], PICK), __byte_perm(u[6], u[7], PICK), 0x5410);
     return e;
 }
 
@@ -241,12 +274,15 @@ struct Place {
     int left;
     bool whole;  // all eight, in vectors
 };
+__device__ __forceinline__ bool on16(const som_adamw_tensor& it)
+{
+    return ((reinterpret_cast<uintptr_t>(it.param) | reinterpret_cast<uintptr_t>(it.grad) | reinterpret_cast<uintptr_t>(it.copy) |
+             reinterpret_cast<uintptr_t>(it.m) | reinterpret_cast<uintptr_t>(it.v)) & 15u) == 0;
+}
 __device__ __forceinline__ Place place_of(const som_adamw_tensor& it, int64_t at)
 {
-    const uintptr_t all = reinterpret_cast<uintptr_t>(it.param) | reinterpret_cast<uintptr_t>(it.grad) | reinterpret_cast<uintptr_t>(it.copy) |
-                          reinterpret_cast<uintptr_t>(it.m) | reinterpret_cast<uintptr_t>(it.v);
     const int left = it.n - at >= 8 ? 8 : it.n > at ? (int)(it.n - at) : 0;
-    return {at, left, left == 8 && (all & 15u) == 0};
+    return {at, left, left == 8 && on16(it)};
 }
 
 template <bool P16, bool G16, class TABLE>
@@ -294,71 +330,74 @@ __global__ void __launch_bounds__(ADAM_THREADS) k_adamw(const __grid_constant__ 
 }
 
 // The same with moments in 8 bits.  Bound by the issue of instructions as much as by HBM: arithmetic goes in pairs, square root and quotient are
-// the approximations (2^-22 of the change), and a thread takes two times eight elements.
-template <bool P16, bool G16, bool COPY, int CAP>
-__global__ void __launch_bounds__(ADAM_THREADS) k_adamw8(const __grid_constant__ AdamTable<CAP> t)
+// the approximations (2^-22 of the change).  AT: the step's numbers come from memory; else they are operands from the kernel's
+// parameters, in pairs.  210 million elements: bf16 parameters 518 us (4.0 TB/s, issue slots 80 % busy), fp32 with a bf16 copy 576 (5.8 TB/s);
+// in scalars, two and more times eight elements a thread, or with other limits on registers (5 or 8 blocks an SM) 520 to 870.
+template <bool P16, bool G16, bool COPY, int CAP, bool AT>
+__global__ void __launch_bounds__(ADAM_THREADS, 6) k_adamw8(const __grid_constant__ AdamTable<CAP> t)
 {
     enter();
     const som_adamw_tensor& it = t.item[tensor_of(t, blockIdx.x)];
     const float scale = t.scale ? *t.scale : 1.f;
     if (!(fabsf(scale) <= 3.4028235e38f)) return;
-    const Hyper h = t.h_at ? *t.h_at : t.h;
-    const int lane = threadIdx.x & 31;
-    const int64_t blocks = (it.n + ADAM_BLOCK - 1) / ADAM_BLOCK, first = (int64_t)(blockIdx.x - it.first_chunk) * ADAM_CHUNK8 + threadIdx.x * 8;
-    Place q[ADAM_TIMES];
-    float p[ADAM_TIMES][8], g[ADAM_TIMES][8];
-    uint2 mc[ADAM_TIMES], vc[ADAM_TIMES];
-    uint32_t em[ADAM_TIMES], ev[ADAM_TIMES];
-#pragma unroll
-    for (int k = 0; k < ADAM_TIMES; ++k) {
-        q[k] = place_of(it, first + k * ADAM_CHUNK);
-        if (q[k].at - lane * 8 >= it.n) break;  // none of the warp's
-        read_params<P16, G16>(t, it, q[k], p[k], g[k]);
-        mc[k] = read_codes(static_cast<const uint8_t*>(it.m) + q[k].at, q[k].whole, q[k].left);
-        vc[k] = read_codes(static_cast<const uint8_t*>(it.v) + q[k].at, q[k].whole, q[k].left);
-        const int64_t block = q[k].at / ADAM_BLOCK;
-        em[k] = it.exponents[block];
-        ev[k] = it.exponents[blocks + block];
+    HyperPairs at_h;
+    if (AT) at_h = pairs_of(*t.h_at);
+    const HyperPairs& h = AT ? at_h : t.pairs;
+    const uint32_t seed = AT ? t.h_at->seed : t.h.seed;
+    const int lane = threadIdx.x & 31, off = threadIdx.x * 8;
+    const int64_t base = (int64_t)(blockIdx.x - it.first_chunk) * ADAM_CHUNK, blocks = (it.n + ADAM_BLOCK - 1) / ADAM_BLOCK;
+    const int here = (int)(it.n - base < ADAM_CHUNK ? it.n - base : ADAM_CHUNK) - off;  // elements of the tensor from this thread's first on
+    if (here + lane * 8 <= 0) return;  // none of the warp's
+    const Place q = {base + off, here < 8 ? (here > 0 ? here : 0) : 8, here >= 8 && on16(it)};
+    uint8_t* em = it.exponents + base / ADAM_BLOCK + (threadIdx.x >> 5);
+    uint8_t* ev = em + blocks;
+    float p[8], g[8];
+    read_params<P16, G16>(t, it, q, p, g);
+    float2 m[4], v[4];
+    {
+        const uint2 mc = read_codes(static_cast<const uint8_t*>(it.m) + q.at, q.whole, q.left), vc = read_codes(static_cast<const uint8_t*>(it.v) + q.at, q.whole, q.left);
+        decode8<true>(mc, *em, m);
+        decode8<false>(vc, *ev, v);
     }
 #pragma unroll
-    for (int k = 0; k < ADAM_TIMES; ++k) {
-        if (q[k].at - lane * 8 >= it.n) break;
-        float2 m[4], v[4];
-        decode8<true>(mc[k], em[k], m);
-        decode8<false>(vc[k], ev[k], v);
+    for (int i = 0; i < 4; ++i) {
+        const float2 gi = __fmul2_rn(make_float2(g[2 * i], g[2 * i + 1]), twice(scale));  // (by 1 where there is none)
+        m[i] = sum2(__fmul2_rn(m[i], h.b1), __fmul2_rn(gi, h.c1));
+        v[i] = sum2(__fmul2_rn(v[i], h.b2), __fmul2_rn(__fmul2_rn(gi, gi), h.c2));
+        const float2 up = __fmul2_rn(m[i], h.k1), under = __fmul2_rn(v[i], h.k2);
+        // the root as x / sqrt(x + 1e-37): roots below 1e-15 are not right, and nothing next to eps
+        const float2 more = __fadd2_rn(under, twice(1e-37f));
+        float2 root = __fmul2_rn(under, make_float2(fast_rsqrt(more.x), fast_rsqrt(more.y)));
+        if (h.eps.x < 0.999e-8f) root = make_float2(sqrtf(under.x), sqrtf(under.y));
+        root = __fadd2_rn(root, h.eps);
+        const float2 change = __fmul2_rn(up, make_float2(fast_rcp(root.x), fast_rcp(root.y)));
+        const float2 now = __ffma2_rn(change, h.minus_rate, __fmul2_rn(make_float2(p[2 * i], p[2 * i + 1]), h.keep));
+        p[2 * i] = now.x, p[2 * i + 1] = now.y;
+    }
+    write_params<P16, COPY>(t, it, q, p);
+    const uint32_t key = mix(mix((uint32_t)(q.at / ADAM_BLOCK)) ^ (seed + it.number * 0x9E3779B9u)) + lane * (8u * 0x6A09E667u);
+    uint32_t rm[8], rv[8];  // the lower and the upper half of mix()
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const uint32_t y = mix_half(key + i * 0x6A09E667u);
+        rv[i] = y >> 16;
+        rm[i] = (y ^ rv[i]) & 0xffffu;
+    }
+    if (q.left < 8) {  // (beyond the tensor's end)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            float2 gi = make_float2(g[k][2 * i], g[k][2 * i + 1]);
-            if (t.scale) gi = __fmul2_rn(gi, twice(scale));
-            m[i] = sum2(__fmul2_rn(m[i], twice(h.b1)), __fmul2_rn(gi, twice(h.c1)));
-            v[i] = sum2(__fmul2_rn(v[i], twice(h.b2)), __fmul2_rn(__fmul2_rn(gi, gi), twice(h.c2)));
-            const float2 up = __fmul2_rn(m[i], twice(h.k1)), under = __fmul2_rn(v[i], twice(h.k2));
-            const float2 change = make_float2(__fdividef(up.x, fast_sqrt(under.x) + h.eps), __fdividef(up.y, fast_sqrt(under.y) + h.eps));
-            const float2 kept = __fmul2_rn(make_float2(p[k][2 * i], p[k][2 * i + 1]), twice(h.keep)), now = __ffma2_rn(change, twice(-h.rate), kept);
-            p[k][2 * i] = now.x, p[k][2 * i + 1] = now.y;
+            if (2 * i >= q.left) m[i].x = v[i].x = 0.f;
+            if (2 * i + 1 >= q.left) m[i].y = v[i].y = 0.f;
         }
-        write_params<P16, COPY>(t, it, q[k], p[k]);
-        const int64_t block = q[k].at / ADAM_BLOCK;
-        const uint32_t key = mix(mix((uint32_t)block) ^ (h.seed + it.number * 0x9E3779B9u)) + lane * (8u * 0x6A09E667u);
-        uint32_t r[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) r[i] = mix(key + i * 0x6A09E667u);
-        if (q[k].left < 8) {  // (beyond the tensor's end)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                if (2 * i >= q[k].left) m[i].x = v[i].x = 0.f;
-                if (2 * i + 1 >= q[k].left) m[i].y = v[i].y = 0.f;
-            }
-        }
-        uint2 codes;
-        const uint32_t e1 = encode8<true>(m, r, codes);
-        write_codes(static_cast<uint8_t*>(it.m) + q[k].at, codes, q[k].whole, q[k].left);
-        const uint32_t e2 = encode8<false>(v, r, codes);
-        write_codes(static_cast<uint8_t*>(it.v) + q[k].at, codes, q[k].whole, q[k].left);
-        if (lane == 0) {
-            it.exponents[block] = (uint8_t)e1;
-            it.exponents[blocks + block] = (uint8_t)e2;
-        }
+    }
+    uint2 codes;
+    const uint32_t e1 = encode8<true>(m, rm, codes);
+    write_codes(static_cast<uint8_t*>(it.m) + q.at, codes, q.whole, q.left);
+    const uint32_t e2 = encode8<false>(v, rv, codes);
+    write_codes(static_cast<uint8_t*>(it.v) + q.at, codes, q.whole, q.left);
+    if (lane == 0) {
+        *em = (uint8_t)e1;
+        *ev = (uint8_t)e2;
     }
 }
 
@@ -387,19 +426,26 @@ __global__ void __launch_bounds__(ADAM_THREADS) k_adamw_moments(const __grid_con
 constexpr int FEW_TENSORS = 24, MOST_TENSORS = 500;
 static_assert(sizeof(AdamTable<MOST_TENSORS>) <= 32764, "kernel parameters");
 
+template <bool P16, bool G16, bool COPY, int BITS, int CAP>
+cudaError_t launch_table(som_layers* l, const AdamTable<CAP>& t, unsigned chunks, cudaStream_t st)
+{
+    if (BITS == 32) return launch(l, k_adamw<P16, G16, COPY, CAP>, dim3(chunks), ADAM_THREADS, 0, st, 1, t);
+    return launch(l, t.h_at ? k_adamw8<P16, G16, COPY, CAP, true> : k_adamw8<P16, G16, COPY, CAP, false>, dim3(chunks), ADAM_THREADS, 0, st, 1, t);
+}
+
 template <bool P16, bool G16, bool COPY, int BITS>
 cudaError_t launch_adamw(som_layers* l, const AdamTable<MOST_TENSORS>& t, unsigned chunks, cudaStream_t st)
 {
-    if (t.count > FEW_TENSORS)
-        return launch(l, BITS == 8 ? k_adamw8<P16, G16, COPY, MOST_TENSORS> : k_adamw<P16, G16, COPY, MOST_TENSORS>, dim3(chunks), ADAM_THREADS, 0, st, 1, t);
+    if (t.count > FEW_TENSORS) return launch_table<P16, G16, COPY, BITS>(l, t, chunks, st);
     AdamTable<FEW_TENSORS> s;
     for (int i = 0; i < t.count; ++i) s.item[i] = t.item[i];
     s.count = t.count;
     s.param_bf16 = t.param_bf16, s.grad_bf16 = t.grad_bf16, s.copy_bf16 = t.copy_bf16;
     s.h = t.h;
+    s.pairs = t.pairs;
     s.h_at = t.h_at;
     s.scale = t.scale;
-    return launch(l, BITS == 8 ? k_adamw8<P16, G16, COPY, FEW_TENSORS> : k_adamw<P16, G16, COPY, FEW_TENSORS>, dim3(chunks), ADAM_THREADS, 0, st, 1, s);
+    return launch_table<P16, G16, COPY, BITS>(l, s, chunks, st);
 }
 
 template <int BITS>
@@ -416,7 +462,7 @@ bool off_by(const void* p, int bytes) { return (reinterpret_cast<uintptr_t>(p) &
 
 // Hands the tensors out to launches: run(first, count, chunks) with their first_chunk written to `to`
 template <class TABLE, class RUN>
-int in_launches(const som_adamw_tensor* tensors, int32_t count, int chunk, TABLE& t, RUN&& run)
+int in_launches(const som_adamw_tensor* tensors, int32_t count, TABLE& t, RUN&& run)
 {
     int32_t i = 0;
     while (i < count) {
@@ -424,7 +470,7 @@ int in_launches(const som_adamw_tensor* tensors, int32_t count, int chunk, TABLE
         t.count = 0;
         for (; i < count && t.count < MOST_TENSORS; ++i) {
             if (tensors[i].n == 0) continue;
-            const int64_t more = (tensors[i].n + chunk - 1) / chunk;
+            const int64_t more = (tensors[i].n + ADAM_CHUNK - 1) / ADAM_CHUNK;
             if (chunks + more > MOST_CHUNKS) break;
             som_adamw_tensor& to = t.item[t.count++];
             to = tensors[i];
@@ -486,7 +532,8 @@ int som_adamw(som_layers* l, int param_type, int grad_type, int copy_type, int b
         t.h_at = a.to;
     }
     t.h = hyper_of(step->rate, b1, b2, step->eps, step->decay, step->step_at ? 1 : step->step, step->seed);
-    return in_launches(tensors, count, bits == 8 ? ADAM_CHUNK8 : ADAM_CHUNK, t, [&](unsigned chunks) {
+    t.pairs = pairs_of(t.h);
+    return in_launches(tensors, count, t, [&](unsigned chunks) {
         for (int i = 0; i < t.count; ++i)
             if (!copy) t.item[i].copy = nullptr;
         return outcome(l, bits == 8 ? launch_types<8>(l, t, param_type != SOM_F32, grad_type != SOM_F32, copy, chunks, st)
@@ -515,7 +562,7 @@ int som_adamw_moments(som_layers* l, int32_t count, const som_adamw_tensor* tens
             some[i].copy = v[from + i];
         }
         MomentTable<MOST_TENSORS> t;
-        LAY_TRY(in_launches(some, n, ADAM_CHUNK, t, [&](unsigned chunks) {
+        LAY_TRY(in_launches(some, n, t, [&](unsigned chunks) {
             MomentTable<FEW_TENSORS> s;
             for (int i = 0; i < t.count; ++i) s.item[i] = t.item[i];
             s.count = t.count;
