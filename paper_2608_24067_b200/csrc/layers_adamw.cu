@@ -195,14 +195,6 @@ __device__ __forceinline__ void decode8(uint2 c, uint32_t e, float2 (&v)[4])
     }
 }
 
-// the largest magnitude, or NaN
-__device__ __forceinline__ float largest(float a, float b, float c)
-{
-    float r;
-    asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
-    return r;
-}
-
 // 16 x; a product, since shifts have a pipe of half the width, and an instruction of its own, since the compiler (12.9) took the top bytes of x
 // itself for those of 16 x where x was negative
 __device__ __forceinline__ uint32_t times16(uint32_t x)

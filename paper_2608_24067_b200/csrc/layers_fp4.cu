@@ -37,7 +37,7 @@ struct Unit {
 };
 
 template <bool WIDE>
-__global__ void __launch_bounds__(Q_THREADS) k_fp4_quantize(const QuantArgs a)
+__global__ void __launch_bounds__(Q_THREADS, WIDE ? 4 : 5) k_fp4_quantize(const QuantArgs a)
 {
     enter();
     const int lane = threadIdx.x & 31;
@@ -45,37 +45,39 @@ __global__ void __launch_bounds__(Q_THREADS) k_fp4_quantize(const QuantArgs a)
         const Unit at(u, a.tiles);
         const int64_t col = at.tile * 256 + lane * 8;
         const bool in = col < a.D;
-        float v[Q_ROWS][8];
+        uint4 raw[Q_ROWS][WIDE ? 2 : 1];  // eight values of each row
 #pragma unroll
         for (int i = 0; i < Q_ROWS; ++i) {
             const int64_t row = at.row + 32 * i;
-            if (in && row < a.T) {
-                if (WIDE) {
-                    const float4* p = reinterpret_cast<const float4*>(static_cast<const float*>(a.x) + row * a.ldx + col);
-                    const float4 x0 = p[0], x1 = p[1];
-                    v[i][0] = x0.x, v[i][1] = x0.y, v[i][2] = x0.z, v[i][3] = x0.w, v[i][4] = x1.x, v[i][5] = x1.y, v[i][6] = x1.z, v[i][7] = x1.w;
-                } else {
-                    load8(static_cast<const uint16_t*>(a.x) + row * a.ldx + col, v[i], a.bf16);
-                }
-            } else {
 #pragma unroll
-                for (int j = 0; j < 8; ++j) v[i][j] = 0.f;
-            }
+            for (int h = 0; h < (WIDE ? 2 : 1); ++h)
+                raw[i][h] = !in || row >= a.T ? make_uint4(0u, 0u, 0u, 0u)
+                            : WIDE            ? *(reinterpret_cast<const uint4*>(static_cast<const float*>(a.x) + row * a.ldx + col) + h)
+                                              : *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(a.x) + row * a.ldx + col);
         }
         uint32_t four[Q_ROWS];
 #pragma unroll
         for (int i = 0; i < Q_ROWS; ++i) {
-            uint32_t most = 0;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) most = max(most, __float_as_uint(v[i][j]) & 0x7fffffffu);
+            float v[8];
+            if (WIDE) {
+                const uint4 x0 = raw[i][0], x1 = raw[i][WIDE ? 1 : 0];
+                v[0] = __uint_as_float(x0.x), v[1] = __uint_as_float(x0.y), v[2] = __uint_as_float(x0.z), v[3] = __uint_as_float(x0.w);
+                v[4] = __uint_as_float(x1.x), v[5] = __uint_as_float(x1.y), v[6] = __uint_as_float(x1.z), v[7] = __uint_as_float(x1.w);
+            } else {
+                widen8(raw[i][0], v, a.bf16);
+            }
+            float top = largest(v[0], v[1], v[2]);
+            top = largest(top, v[3], v[4]);
+            top = largest(largest(top, v[5], v[6]), v[7], 0.f);
+            uint32_t most = __float_as_uint(top);
             most = max(most, __shfl_xor_sync(0xffffffffu, most, 1));
             most = max(most, __shfl_xor_sync(0xffffffffu, most, 2));
             const uint32_t e = fp4_scale_of(most);
             const float by = fp4_inverse(e);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[i][j] *= by;
+            for (int j = 0; j < 8; ++j) v[j] *= by;
             const int64_t row = at.row + 32 * i;
-            if (in && row < a.T) *reinterpret_cast<uint32_t*>(a.codes + (row * a.D + col) / 2) = e == 255u ? 0u : fp4_codes(v[i]);
+            if (in && row < a.T) *reinterpret_cast<uint32_t*>(a.codes + (row * a.D + col) / 2) = e == 255u ? 0u : fp4_codes(v);
             // four blocks' bytes lie next to each other
             four[i] = e << (8 * ((lane >> 2) & 3));
             four[i] |= __shfl_xor_sync(0xffffffffu, four[i], 4);
@@ -101,30 +103,44 @@ __global__ void __launch_bounds__(Q_THREADS) k_fp4_values(const ValuesArgs a)
     const int lane = threadIdx.x & 31;
     for (uint32_t u = (blockIdx.x * Q_THREADS + threadIdx.x) >> 5; u < a.units; u += gridDim.x * (Q_THREADS / 32)) {
         const Unit at(u, a.tiles);
-        const int64_t col = at.tile * 256 + lane * 8;
-        if (col >= a.D) continue;
-        uint32_t w[Q_ROWS];
+        // Eight columns a lane; fp32: four and, 128 further on, four, so that a store of the warp is 512 bytes in a row.
+        constexpr int PARTS = WIDE ? 2 : 1, N = 8 / PARTS;
+        uint32_t w[Q_ROWS][PARTS];
+        uint4 e[PARTS];
 #pragma unroll
-        for (int i = 0; i < Q_ROWS; ++i)
-            w[i] = at.row + 32 * i < a.T ? *reinterpret_cast<const uint32_t*>(a.codes + ((at.row + 32 * i) * a.D + col) / 2) : 0u;
-        // (the bytes of rows beyond the last are there, and not used)
-        const uint4 e = *reinterpret_cast<const uint4*>(a.scales + fp4_scale_at(at.row, (at.tile * 8 + lane / 4) & ~3, a.tiles));
-        const uint32_t es[Q_ROWS] = {e.x, e.y, e.z, e.w};
+        for (int h = 0; h < PARTS; ++h) {
+            const int64_t col = at.tile * 256 + h * 128 + lane * N;
+            const bool in = col < a.D;
 #pragma unroll
-        for (int i = 0; i < Q_ROWS; ++i) {
-            const int64_t row = at.row + 32 * i;
-            if (row >= a.T) break;
-            const float by = fp4_power((es[i] >> (8 * ((lane >> 2) & 3))) & 255u);
-            float v[8];
+            for (int i = 0; i < Q_ROWS; ++i) {
+                w[i][h] = 0u;
+                if (in && at.row + 32 * i < a.T) {
+                    const uint8_t* p = a.codes + ((at.row + 32 * i) * a.D + col) / 2;
+                    w[i][h] = WIDE ? *reinterpret_cast<const uint16_t*>(p) : *reinterpret_cast<const uint32_t*>(p);
+                }
+            }
+            // (the bytes of rows beyond the last are there, and not used)
+            if (in) e[h] = *reinterpret_cast<const uint4*>(a.scales + fp4_scale_at(at.row, at.tile * 8 + (WIDE ? 4 * h : lane / 16 * 4), a.tiles));
+        }
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] = fp4_value(w[i] >> (4 * j)) * by;
-            if (WIDE) {
-                float4* p = reinterpret_cast<float4*>(static_cast<float*>(a.y) + row * a.ldy + col);
-                p[0] = make_float4(v[0], v[1], v[2], v[3]);
-                p[1] = make_float4(v[4], v[5], v[6], v[7]);
-            } else {
-                *reinterpret_cast<uint4*>(static_cast<uint16_t*>(a.y) + row * a.ldy + col) =
-                    make_uint4(pack2(v[0], v[1], a.bf16), pack2(v[2], v[3], a.bf16), pack2(v[4], v[5], a.bf16), pack2(v[6], v[7], a.bf16));
+        for (int h = 0; h < PARTS; ++h) {
+            const int64_t col = at.tile * 256 + h * 128 + lane * N;
+            if (col >= a.D) continue;
+            const uint32_t es[Q_ROWS] = {e[h].x, e[h].y, e[h].z, e[h].w};
+            const int shift = 8 * (WIDE ? lane >> 3 : (lane >> 2) & 3);
+#pragma unroll
+            for (int i = 0; i < Q_ROWS; ++i) {
+                const int64_t row = at.row + 32 * i;
+                if (row >= a.T) break;
+                const float by = fp4_power((es[i] >> shift) & 255u);
+                float v[8];
+#pragma unroll
+                for (int j = 0; j < N; ++j) v[j] = fp4_value(w[i][h] >> (4 * j)) * by;
+                if (WIDE)
+                    *reinterpret_cast<float4*>(static_cast<float*>(a.y) + row * a.ldy + col) = make_float4(v[0], v[1], v[2], v[3]);
+                else
+                    *reinterpret_cast<uint4*>(static_cast<uint16_t*>(a.y) + row * a.ldy + col) =
+                        make_uint4(pack2(v[0], v[1], a.bf16), pack2(v[2], v[3], a.bf16), pack2(v[4], v[5], a.bf16), pack2(v[6], v[7], a.bf16));
             }
         }
     }

@@ -46,6 +46,14 @@ __device__ __forceinline__ void load8(const uint16_t* p, float (&v)[8], int bf16
     widen8(w, v, bf16);
 }
 
+// the largest magnitude, or NaN
+__device__ __forceinline__ float largest(float a, float b, float c)
+{
+    float r;
+    asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
+
 // one instruction each, subnormal results flushed to zero: 2^x off by 2 units, 1 / x by 1 unit in the last place
 __device__ __forceinline__ float fast_exp2(float x)
 {
