@@ -141,6 +141,7 @@ int som_layers_create(som_layers** out)
     if (e == cudaSuccess) e = prepare_product(l);
     if (e == cudaSuccess) e = prepare_fp4_product(l);
     if (e == cudaSuccess) e = prepare_norm();
+    if (e == cudaSuccess) e = prepare_fp4_few();
     if (e == cudaSuccess) e = prepare_few();
     if (e == cudaSuccess) e = prepare_plan();
     if (e == cudaSuccess) e = cudaMalloc(reinterpret_cast<void**>(&l->flags), 256);

@@ -245,6 +245,7 @@ int som_fp4_linear(som_layers* l, int type, int act, int gated, int64_t T, int64
     p.y = static_cast<uint16_t*>(y);
     p.T = T, p.D = D, p.F = F, p.ldr = ldr, p.ldy = ldy;
     p.act = act, p.gated = gated != 0, p.bf16 = type == SOM_BF16;
+    if (fp4_few_rows(p)) return launch_fp4_few(l, p, static_cast<const uint16_t*>(x), ldx, st);
     uint8_t *codes = nullptr, *scales = nullptr;
     unsigned char* parts = nullptr;
     auto carve = [&](Carver c) {

@@ -65,6 +65,11 @@ cudaError_t prepare_fp4_product(som_layers* l);  // once per handle
 size_t fp4_product_bytes(const som_layers* l, const Fp4Product& p);  // workspace
 int launch_fp4_product(som_layers* l, const Fp4Product& p, unsigned char* ws, cudaStream_t st);
 
+constexpr int FP4_FEW = 4;  // the most rows of launch_fp4_few
+cudaError_t prepare_fp4_few();            // once per handle
+bool fp4_few_rows(const Fp4Product& p);   // whether launch_fp4_few takes them (it quantises x itself)
+int launch_fp4_few(som_layers* l, const Fp4Product& p, const uint16_t* x, int64_t ldx, cudaStream_t st);
+
 int launch_fp4_quantize(som_layers* l, int type, int64_t T, int64_t D, const void* x, int64_t ldx, uint8_t* codes, uint8_t* scales, cudaStream_t st);
 
 }  // namespace lay

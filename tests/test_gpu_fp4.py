@@ -135,6 +135,14 @@ def test_activations_and_gates(L, T, D, F, act):
 
 
 @pytest.mark.parametrize("kind", ["bf16", "fp16"])
+@pytest.mark.parametrize("T", [1, 2, 3, 4])
+@pytest.mark.parametrize("D,F,gated", [(32, 8, False), (96, 136, False), (4096, 640, True), (1056, 1000, False), (7200, 264, False), (64, 4096, False), (2048, 128, True), (20000, 8, False), (544, 72, True)])
+def test_a_few_rows(L, T, D, F, gated, kind):
+    """One row to four: one step of 1024 columns and several, columns shared by warps, features that end inside 128."""
+    check_layer(L, *layer(T, D, F, kind, gated, seed=D, wild=True), act="silu", gated=gated)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "fp16"])
 @pytest.mark.parametrize("T,D,F,gated", [(1500, 1056, 2056, False), (2900, 544, 3200, False), (1300, 512, 1024, True), (1409, 288, 1000, True), (5000, 256, 640, False), (2200, 2080, 2304, True)])
 def test_pairs_of_blocks(L, T, D, F, gated, kind):
     """Tiles of 256 x 256, one to several rounds of them, with rows and columns that end inside a tile."""
