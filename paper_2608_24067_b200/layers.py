@@ -82,6 +82,11 @@ class Fp4Matrix:
         self.scales.record_stream(stream)
 
 
+def _scale_bytes(rows, D):
+    """som_fp4_scale_bytes"""
+    return (rows + 127) // 128 * ((D + 255) // 256) * 1024
+
+
 class Layers:
     """Handle of the dense operators on one device (``som_layers_create``): workspace and status.
 
@@ -335,11 +340,10 @@ class Layers:
         """Addresses of a matrix in 4 bits."""
         if not isinstance(q, Fp4Matrix):
             raise TypeError("%s must be an Fp4Matrix" % name)
-        n = self._lib.som_fp4_scale_bytes(rows, D)
-        if n < 0:
+        if D % 32 or not D:
             raise ValueError("%s must have columns in blocks of 32" % name)
         on = self.device.index
-        return _whole(q.codes, (rows, D // 2), torch.uint8, on, name + ".codes"), _whole(q.scales, (n,), torch.uint8, on, name + ".scales")
+        return _whole(q.codes, (rows, D // 2), torch.uint8, on, name), _whole(q.scales, (_scale_bytes(rows, D),), torch.uint8, on, name)
 
     def quantize_fp4(self, x, stream=None):
         """som_fp4_quantize: x (float32, float16 or bfloat16, columns in blocks of 32) in 4 bits.  Returns an Fp4Matrix."""
@@ -350,10 +354,9 @@ class Layers:
         kind = _code(_TYPES, x.dtype, "x's type")
         T, D = x.shape
         xp, ldx = _matrix(x, T, D, x.dtype, self.device.index, "x")
-        n = self._lib.som_fp4_scale_bytes(T, D)
-        if n < 0:
+        if D % 32 or not D:
             raise ValueError("x must have columns in blocks of 32")
-        codes, scales = x.new_empty((T, D // 2), dtype=torch.uint8), x.new_empty((n,), dtype=torch.uint8)
+        codes, scales = x.new_empty((T, D // 2), dtype=torch.uint8), x.new_empty((_scale_bytes(T, D),), dtype=torch.uint8)
         rc = self._lib.som_fp4_quantize(self._h, kind, T, D, xp, ldx, codes.data_ptr(), scales.data_ptr(), self._stream())
         if rc:
             self._check(rc, "som_fp4_quantize")
@@ -471,7 +474,12 @@ class AdamW:
             self._m = [torch.zeros_like(p, dtype=torch.uint8) for p in self.params]
             self._v = [torch.zeros_like(p, dtype=torch.uint8) for p in self.params]
             self._exponents = [p.new_zeros((2, -(-p.numel() // 256)), dtype=torch.uint8) for p in self.params]
-        self._groups = []
+        self._groups, self._shapes = [], [p.shape for p in self.params]
+        # where moments() puts the values: pieces of one tensor, each on 16 bytes
+        self._places, self._all = [], 0
+        for p in self.params:
+            self._places.append((p.shape, p.stride(), self._all))
+            self._all += -(-p.numel() // 8) * 8
         for (pt, ct), which in groups.items():
             table = (_Tensor * len(which))()
             for t, i in zip(table, which):
@@ -520,9 +528,9 @@ class AdamW:
             if gt is not torch.float32 and (gt is not pt and pt is not torch.float32 or gt not in _TYPES):
                 raise TypeError("gradients must be float32 or 16 bits, beside 16-bit parameters of their type")
             for t, i in zip(table, which):
-                g, p = grads[i], self.params[i]
-                if g.dtype is not gt or g.shape != p.shape or g.get_device() != on or not g.is_contiguous():
-                    _whole(g, p.shape, gt, on, "grads[%d]" % i)
+                g, shape = grads[i], self._shapes[i]
+                if g.dtype is not gt or g.shape != shape or g.get_device() != on or not g.is_contiguous():
+                    _whole(g, shape, gt, on, "grads[%d]" % i)
                 t.grad = g.data_ptr()
             kinds.append(_TYPES[gt])
         for (pt, ct, which, table), gt in zip(self._groups, kinds):
@@ -548,14 +556,14 @@ class AdamW:
             for t in (*out[0], *out[1]):
                 t.record_stream(before)
             return out
-        m = [torch.empty_like(p, dtype=torch.bfloat16) for p in self.params]
-        v = [torch.empty_like(p, dtype=torch.bfloat16) for p in self.params]
+        m, v = torch.empty(self._all, dtype=torch.bfloat16, device=L.device), torch.empty(self._all, dtype=torch.bfloat16, device=L.device)
         for _, _, which, table in self._groups:
-            to = ctypes.c_void_p * len(which)
-            rc = L._lib.som_adamw_moments(L._h, len(table), table, to(*(m[i].data_ptr() for i in which)), to(*(v[i].data_ptr() for i in which)), L._stream())
+            to, mp, vp = ctypes.c_void_p * len(which), m.data_ptr(), v.data_ptr()
+            rc = L._lib.som_adamw_moments(L._h, len(table), table, to(*[mp + 2 * self._places[i][2] for i in which]),
+                                          to(*[vp + 2 * self._places[i][2] for i in which]), L._stream())
             if rc:
                 L._check(rc, "som_adamw_moments")
-        return m, v
+        return [m.as_strided(*place) for place in self._places], [v.as_strided(*place) for place in self._places]
 
     def state(self):
         """What ``load`` takes, for a checkpoint: the moments' own memory, with bits=8 as pairs of codes and exponents."""
