@@ -4,7 +4,7 @@ Sparse binary samples are searched and the map is updated for a few epochs (``So
 two best units' prototypes, projected to D numbers.  A layer of E experts learns to predict a vector that depends on the
 sample's rarer features: the router's logits are a linear layer of the token, ``route`` picks k experts with a balance bias that is
 moved by the counts it returns, ``experts`` adds the chosen experts' outputs to the token, and the three gradients train the
-router and the experts by Adam on fp32 master weights.  At the end single tokens go through the same layer, as in serving.
+router and the experts by ``AdamW`` on fp32 master weights.  At the end single tokens go through the same layer, as in serving.
 
     python examples/experts_on_map.py
 """
@@ -18,7 +18,7 @@ import torch
 sys.path.insert(0, os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
 
 from paper_2608_24067_b200 import synth  # noqa: E402
-from paper_2608_24067_b200.layers import Layers  # noqa: E402
+from paper_2608_24067_b200.layers import AdamW, Layers  # noqa: E402
 from paper_2608_24067_b200.som import Som  # noqa: E402
 
 
@@ -54,15 +54,11 @@ class ExpertLayer:
         new = lambda *s, scale: torch.randn(*s, generator=gen, device="cuda") * scale  # noqa: E731
         self.master = {"router": new(E, D, scale=D ** -0.5), "w1": new(E, 2 * hidden, D, scale=D ** -0.5), "w2": new(E, D, hidden, scale=0.3 * hidden ** -0.5),
                        "b1": torch.zeros(E, 2 * hidden, device="cuda"), "b2": torch.zeros(E, D, device="cuda")}
-        self.moments = {n: (torch.zeros_like(v), torch.zeros_like(v)) for n, v in self.master.items()}
-        self.steps = 0
+        self.w = {n: v.bfloat16() for n, v in self.master.items()}
         self.balance = torch.zeros(E, device="cuda")
         self.k = k
         self.layers = Layers()
-        self.cast()
-
-    def cast(self):
-        self.w = {n: v.bfloat16() for n, v in self.master.items()}
+        self.optimizer = AdamW(self.layers, list(self.master.values()), copies=list(self.w.values()))
 
     def forward(self, x):
         logits = self.layers.linear(x, self.w["router"])
@@ -77,16 +73,10 @@ class ExpertLayer:
         g = self.layers.experts_backward(x, routed["indices"], routed["weights"], self.w["w1"], self.w["w2"], dy, self.w["b1"], self.w["b2"])
         dlogits = self.layers.route_backward(logits, routed["indices"], g["dweights"], score="sigmoid", renorm=True)
         g["drouter"] = self.layers.linear_backward(x, self.w["router"], dlogits)["dweight"]
-        self.steps += 1
-        for n, v in self.master.items():
-            grad, (m, s) = g["d" + n].float(), self.moments[n]
-            m.lerp_(grad, 0.1)
-            s.lerp_(grad * grad, 0.01)
-            v -= rate * (m / (1 - 0.9 ** self.steps)) / ((s / (1 - 0.99 ** self.steps)).sqrt() + 1e-8)
+        self.optimizer.step([g["d" + n] for n in self.master], rate=rate, beta2=0.99, decay=0.0)
         # an expert that gets fewer tokens than its share becomes easier to choose (the choice alone; the weights do not see it)
         counts = routed["counts"].float()
         self.balance += balance_rate * torch.sign(counts.mean() - counts)
-        self.cast()
         return float(error.square().mean()), routed["counts"]
 
 

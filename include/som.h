@@ -562,7 +562,8 @@ typedef struct som_adamw_step {
     double rate, beta1, beta2, eps, decay;
     int64_t step;            /* t, from 1 */
     const float* rate_at;    /* device: in the place of rate, or NULL */
-    const int64_t* step_at;  /* device: in the place of step, and seed + *step_at in the place of seed, or NULL (for captured graphs) */
+    const int64_t* step_at;  /* device: in the place of step, and seed + *step_at in the place of seed, or NULL (for captured
+                              * graphs; below 1 it counts as 1) */
     const float* scale;      /* device: multiplies the gradients; if it is an infinity or NaN nothing is changed; or NULL */
     uint32_t seed;           /* 8-bit moments: of the random bits; another one each step */
 } som_adamw_step;

@@ -75,7 +75,7 @@ __host__ __device__ inline HyperPairs pairs_of(const Hyper& h)
 __global__ void k_adamw_hyper(const HyperArgs a)
 {
     enter();
-    const int64_t step = a.step_at ? *a.step_at : a.step;
+    const int64_t step = a.step_at ? max(*a.step_at, (int64_t)1) : a.step;
     *a.to = hyper_of(a.rate_at ? (double)*a.rate_at : a.rate, a.b1, a.b2, a.eps, a.decay, step, a.step_at ? a.seed + (uint32_t)step : a.seed);
 }
 

@@ -19,8 +19,8 @@ struct NormArgs {
     const void *x, *residual, *weight, *bias;
     void *sum, *y;
     int64_t ldx, ldr, lds, ldy, T;
-    int D, group;  // group: threads of a row (k_norm)
-    float eps;
+    int D, log;  // log: of the threads of a row (k_norm)
+    float inv, eps;  // inv = 1 / D
 };
 
 struct NormBackArgs {
@@ -30,8 +30,8 @@ struct NormBackArgs {
     float* part;   // [blocks][2][D] sums of the block's rows, or nullptr (k_norm_back)
     int64_t ldx, lddy, ldds;
     int64_t T;
-    int D, group;
-    float eps;
+    int D, log;
+    float inv, eps;
 };
 
 struct ColumnArgs {
@@ -176,8 +176,8 @@ __global__ void __launch_bounds__(FRONT_MOST) k_norm(const NormArgs a)
 {
     __shared__ float part0[FRONT_MOST / 32][1], part1[FRONT_MOST / 32][1];
     using P = Piece<E>;
-    const int group = threadIdx.x / a.group, t = threadIdx.x - group * a.group, warps = a.group / 32, first = group * warps;
-    const int64_t row = (int64_t)blockIdx.x * (blockDim.x / a.group) + group;
+    const int group = threadIdx.x >> a.log, threads = 1 << a.log, t = threadIdx.x & (threads - 1), warps = threads / 32, first = group * warps;
+    const int64_t row = (int64_t)blockIdx.x * (blockDim.x >> a.log) + group;
     enter();
     if (row >= a.T) return;  // (a whole group)
     const E* x = static_cast<const E*>(a.x) + row * a.ldx;
@@ -185,7 +185,7 @@ __global__ void __launch_bounds__(FRONT_MOST) k_norm(const NormArgs a)
     P px[P::COUNT], pr[P::COUNT];
 #pragma unroll
     for (int c = 0; c < P::COUNT; ++c) {
-        const int i = (c * a.group + t) * P::N;
+        const int i = (c * threads + t) * P::N;
         if (i < a.D) {
             px[c].load(x + i);
             if (res) pr[c].load(res + i);
@@ -194,7 +194,7 @@ __global__ void __launch_bounds__(FRONT_MOST) k_norm(const NormArgs a)
     float2 v[P::COUNT][P::PAIRS], s2 = twice(0.f);
 #pragma unroll
     for (int c = 0; c < P::COUNT; ++c) {
-        const int i = (c * a.group + t) * P::N;
+        const int i = (c * threads + t) * P::N;
         if (i < a.D) {
             px[c].get(v[c]);
             if (res) {
@@ -204,19 +204,19 @@ __global__ void __launch_bounds__(FRONT_MOST) k_norm(const NormArgs a)
                 for (int j = 0; j < P::PAIRS; ++j) v[c][j] = __fadd2_rn(v[c][j], r[j]);
                 px[c].put(v[c]);
                 px[c].get(v[c]);
-                if (a.sum) px[c].store(static_cast<E*>(a.sum) + row * a.lds + i);
             }
+            if (a.sum) px[c].store(static_cast<E*>(a.sum) + row * a.lds + i);
 #pragma unroll
             for (int j = 0; j < P::PAIRS; ++j) s2 = __fadd2_rn(s2, v[c][j]);
         }
     }
     float s[1] = {s2.x + s2.y};
     group_sums(s, part0 + first, warps, threadIdx.x / 32 - first, 1 + group);
-    const float n = (float)a.D, inv = 1.f / n, mean = over(s[0], n, inv);
+    const float mean = over(s[0], (float)a.D, a.inv);
     s2 = twice(0.f);
 #pragma unroll
     for (int c = 0; c < P::COUNT; ++c)
-        if ((c * a.group + t) * P::N < a.D)
+        if ((c * threads + t) * P::N < a.D)
 #pragma unroll
             for (int j = 0; j < P::PAIRS; ++j) {
                 v[c][j] = __fadd2_rn(v[c][j], twice(-mean));
@@ -224,10 +224,10 @@ __global__ void __launch_bounds__(FRONT_MOST) k_norm(const NormArgs a)
             }
     s[0] = s2.x + s2.y;
     group_sums(s, part1 + first, warps, threadIdx.x / 32 - first, 1 + group);
-    const float r = rsqrtf(s[0] * inv + a.eps);
+    const float r = rsqrtf(s[0] * a.inv + a.eps);
 #pragma unroll
     for (int c = 0; c < P::COUNT; ++c) {
-        const int i = (c * a.group + t) * P::N;
+        const int i = (c * threads + t) * P::N;
         if (i >= a.D) continue;
         float2 w[P::PAIRS];
 #pragma unroll
@@ -276,16 +276,16 @@ __global__ void __launch_bounds__(BACK_THREADS, 1) k_norm_back(const NormBackArg
     extern __shared__ __align__(16) uint4 ring[];  // [DEPTH][x, dy, dsum][COUNT][BACK_THREADS]; at the end the columns' sums, [2][D]
     using P = Piece<E>;
     constexpr int DEPTH = 8 / (int)sizeof(E);
-    const int group = threadIdx.x / a.group, t = threadIdx.x - group * a.group, warps = a.group / 32, first = group * warps, groups = BACK_THREADS / a.group;
+    const int group = threadIdx.x >> a.log, threads = 1 << a.log, t = threadIdx.x & (threads - 1), warps = threads / 32, first = group * warps, groups = BACK_THREADS >> a.log;
     const int warp = threadIdx.x / 32 - first;
     enter();
     float2 w[P::COUNT][P::PAIRS], dw[P::COUNT][P::PAIRS], db[P::COUNT][P::PAIRS];
-    const float n = (float)a.D, inv = 1.f / n;
+    const float n = (float)a.D, inv = a.inv;
     constexpr int WHAT = P::COUNT * BACK_THREADS * 16, STAGE = 3 * WHAT, RING = DEPTH * STAGE;  // bytes of one of x, dy and dsum, of a row's place, of all
     unsigned char* mine = reinterpret_cast<unsigned char*>(ring) + threadIdx.x * 16;
     const uint32_t mine_at = (uint32_t)__cvta_generic_to_shared(mine);
     auto piece = [&](int stage, int what, int c) { return reinterpret_cast<uint4*>(mine + stage + what * WHAT + c * (BACK_THREADS * 16)); };
-    const int i0 = t * P::N, far = a.group * P::N;  // this thread's first column, and from one of its pieces to the next
+    const int i0 = t * P::N, far = threads * P::N;  // this thread's first column, and from one of its pieces to the next
 #pragma unroll
     for (int c = 0; c < P::COUNT; ++c) {
 #pragma unroll
@@ -551,7 +551,7 @@ int check_norm(const som_layers* l, int type, int weights_type, int64_t T, int64
     return T >= MOST_ROWS || D > MOST_COLS ? SOM_ERR_UNSUPPORTED : SOM_OK;
 }
 
-// Threads of a row that is held in registers: as many warps, a power of two, as hold it.  0: too long, or not on 16 bytes
+// Logarithm of the threads of a row that is held in registers: as many warps, a power of two, as hold it.  0: too long, or not on 16 bytes
 int group_of(int64_t D, int most, int bytes, std::initializer_list<const void*> rows, std::initializer_list<int64_t> lds)
 {
     if (D * bytes % 16 != 0 || D > (int64_t)most * HELD) return 0;
@@ -559,9 +559,9 @@ int group_of(int64_t D, int most, int bytes, std::initializer_list<const void*> 
         if (!aligned16(p)) return 0;
     for (int64_t ld : lds)
         if (ld * bytes % 16 != 0) return 0;
-    int g = 32;
-    while ((int64_t)g * HELD < D) g *= 2;
-    return g;
+    int log = 5;
+    while (((int64_t)HELD << log) < D) ++log;
+    return log;
 }
 
 // rows of a norm's matrix: present, and long enough
@@ -607,14 +607,14 @@ int som_norm(som_layers* l, int type, int64_t T, int64_t D, const void* x, int64
     if (T == 0) return SOM_OK;
     Guard g(l->device);
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
-    const int group = group_of(D, FRONT_MOST, type == SOM_F32 ? 4 : 2, {x, residual, weight, bias, sum, y}, {ldx, residual ? ldr : 0, sum ? lds : 0, ldy});
-    const NormArgs a = {x, residual, weight, bias, sum, y, ldx, ldr, lds, ldy, T, (int)D, group, eps};
+    const int log = group_of(D, FRONT_MOST, type == SOM_F32 ? 4 : 2, {x, residual, weight, bias, sum, y}, {ldx, residual ? ldr : 0, sum ? lds : 0, ldy});
+    const NormArgs a = {x, residual, weight, bias, sum, y, ldx, ldr, lds, ldy, T, (int)D, log, 1.f / (float)D, eps};
     return outcome(l, by_types(type, weights_type, [&](auto e, auto w) {
                        using E = decltype(e);
                        using W = decltype(w);
-                       if (!group) return launch(l, k_norm_any<E, W>, dim3((unsigned)T), ROW_THREADS, 0, st, 1, a);
-                       const int threads = group < FRONT_THREADS ? FRONT_THREADS : group;
-                       return launch(l, k_norm<E, W>, dim3((unsigned)tiles_of(T, threads / group)), threads, 0, st, 1, a);
+                       if (!log) return launch(l, k_norm_any<E, W>, dim3((unsigned)T), ROW_THREADS, 0, st, 1, a);
+                       const int threads = (1 << log) < FRONT_THREADS ? FRONT_THREADS : 1 << log;
+                       return launch(l, k_norm<E, W>, dim3((unsigned)tiles_of(T, threads >> log)), threads, 0, st, 1, a);
                    }));
 }
 
@@ -635,10 +635,10 @@ int som_norm_backward(som_layers* l, int type, int64_t T, int64_t D, const void*
         return SOM_OK;
     }
     const bool columns = dweight || dbias;
-    const int group = group_of(D, BACK_THREADS, type == SOM_F32 ? 4 : 2, {x, dy, dsum, dx, weight}, {ldx, lddy, dsum ? ldds : 0});
+    const int log = group_of(D, BACK_THREADS, type == SOM_F32 ? 4 : 2, {x, dy, dsum, dx, weight}, {ldx, lddy, dsum ? ldds : 0});
     int64_t parts;
-    if (group) {
-        parts = tiles_of(T, BACK_THREADS / group);
+    if (log) {
+        parts = tiles_of(T, BACK_THREADS >> log);
         if (parts > l->sm_count) parts = l->sm_count;
     } else {
         parts = 4 * (int64_t)l->sm_count / tiles_of(D, 32);
@@ -647,7 +647,7 @@ int som_norm_backward(som_layers* l, int type, int64_t T, int64_t D, const void*
     }
     float *stats = nullptr, *part = nullptr;
     auto carve = [&](Carver c) {
-        if (!group) stats = c.take<float>(2 * T);
+        if (!log) stats = c.take<float>(2 * T);
         part = c.take<float>(parts * 2 * D);
         return c.used;
     };
@@ -655,14 +655,14 @@ int som_norm_backward(som_layers* l, int type, int64_t T, int64_t D, const void*
         LAY_TRY(ensure(l, carve(Carver{nullptr, 0})));
         carve(Carver{static_cast<unsigned char*>(l->ws), 0});
     }
-    const NormBackArgs a = {x, weight, dy, dsum, dx, stats, part, ldx, lddy, ldds, T, (int)D, group, eps};
+    const NormBackArgs a = {x, weight, dy, dsum, dx, stats, part, ldx, lddy, ldds, T, (int)D, log, 1.f / (float)D, eps};
     const ColumnArgs b = {x, dy, stats, part, ldx, lddy, T, (int)D, (int)parts};
     const ColumnJoinArgs j = {part, dweight, dbias, (int)D, (int)parts};
     return outcome(l, by_types(type, weights_type, [&](auto e, auto w) {
                        using E = decltype(e);
                        using W = decltype(w);
                        cudaError_t r;
-                       if (group) {
+                       if (log) {
                            r = launch(l, k_norm_back<E, W>, dim3((unsigned)parts), BACK_THREADS, back_smem<E>(), st, 1, a);
                        } else {
                            r = launch(l, k_norm_back_any<E, W>, dim3((unsigned)T), ROW_THREADS, 0, st, 1, a);

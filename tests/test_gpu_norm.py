@@ -107,6 +107,14 @@ def test_constant_rows(L, D):
     assert torch.equal(got["dx"], torch.zeros_like(x)) and torch.equal(got["dweight"], torch.zeros(D, device="cuda")) and torch.equal(got["dbias"], torch.full((D,), 3.0, device="cuda"))
 
 
+@pytest.mark.parametrize("D", [512, 333])
+def test_sum_without_a_residual_is_x(L, D):
+    x, _, w, b, _ = inputs(5, D, "fp16", residual=False)
+    total, y = torch.zeros_like(x), torch.zeros_like(x)
+    rc = L._lib.som_norm(L._h, 1, 5, D, x.data_ptr(), D, w.data_ptr(), b.data_ptr(), 1, None, 0, 1e-5, total.data_ptr(), D, y.data_ptr(), D, L._stream())
+    assert rc == 0 and torch.equal(total, x) and torch.equal(y, L.norm(x, w, b))
+
+
 def test_infinities_and_nan_stay_in_their_rows(L):
     x, r, w, b, dy = inputs(6, 640, "bf16", residual=False)
     clean, back = L.norm(x, w, b), L.norm_backward(x, w, dy, b)["dx"]
