@@ -320,8 +320,11 @@ int map_scales(som_layers* l, CUtensorMap* map, const void* base, int64_t rows, 
     return SOM_ERR_CUDA;
 }
 
-// How a product is cut: pairs once narrow tiles pass the SMs; blocks that share a sum where they leave SMs idle.  `joined`: fp32 parts and
-// k_finish, for split sums and for gated products whose halves do not begin on 128 rows of scales.
+// How a product is cut: pairs once narrow tiles pass the SMs (as the 16-bit products); blocks that share a sum where tiles leave SMs idle, four
+// steps of 256 k each at the least.  `joined`: fp32 parts and k_finish, for split sums and for gated products that are not made by pairs
+// (a single block's tile holds no two halves; of pairs each half has to begin on 128 rows of scales).
+// Parts of at least 2 / 4 / 8 steps / none, in us from a graph with x's quantisation: 8 rows, 8192 -> 1024 10.1 / 8.7 / 9.3 / 11.4; 64 rows, 2048 -> 4096
+// 8.6 / 8.3 / 8.4 / 8.4; 200 rows, 1024 -> 1024 8.2 / 7.2 / 7.2 / 7.2; 64 rows, 4096 -> 2 x 1000 10.6 / 8.9 / 10.3 / 11.6.
 struct Cut {
     bool paired, joined;
     int row_tiles, col_tiles, splits;
@@ -336,7 +339,7 @@ Cut cut_of(const som_layers* l, const Fp4Product& p)
     c.splits = 1;
     if (!c.paired) {
         int64_t s = l->sm_count / narrow;
-        if (s > steps / 2) s = steps / 2;
+        if (s > steps / 4) s = steps / 4;
         if (s > 16) s = 16;
         if (s > 1) c.splits = (int)s;
         c.joined = c.splits > 1 || p.gated;
