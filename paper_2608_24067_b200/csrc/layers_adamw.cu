@@ -164,10 +164,18 @@ __device__ __forceinline__ float fast_rsqrt(float x)
     return y;
 }
 
+// off by 2^-22, also where x is subnormal
+__device__ __forceinline__ float near_sqrt(float x)
+{
+    float y;
+    asm("sqrt.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
 // 2^(e - 127) of an exponent byte; 255 (a block that holds an infinity or NaN) gives infinity, and 0 times it NaN
-__device__ __forceinline__ float power_of(uint32_t e) { return __uint_as_float(e ? e << 23 : 0x00400000u); }
-// 2^(127 - e), e <= 255
-__device__ __forceinline__ float power_below(uint32_t e) { return __uint_as_float(e < 254u ? (254u - e) << 23 : e == 254u ? 0x00400000u : 0x00200000u); }
+__device__ __forceinline__ float power_of(uint32_t e) { return __uint_as_float(max(e << 23, 0x00400000u)); }
+// 2^(127 - e), e <= 254
+__device__ __forceinline__ float power_below(uint32_t e) { return __int_as_float(max((254 - (int)e) * (1 << 23), 0x00400000)); }
 
 __device__ __forceinline__ float2 twice(float v) { return make_float2(v, v); }
 
@@ -277,21 +285,22 @@ __device__ __forceinline__ Place place_of(const som_adamw_tensor& it, int64_t at
     return {at, left, left == 8 && on16(it)};
 }
 
-template <bool P16, bool G16, class TABLE>
+// (BF16: the 16-bit tensors are bf16; else the table says what each is)
+template <bool P16, bool G16, bool BF16, class TABLE>
 __device__ __forceinline__ void read_params(const TABLE& t, const som_adamw_tensor& it, const Place& q, float (&p)[8], float (&g)[8])
 {
-    if (P16) read8(static_cast<const uint16_t*>(it.param) + q.at, p, q.whole, q.left, t.param_bf16);
+    if (P16) read8(static_cast<const uint16_t*>(it.param) + q.at, p, q.whole, q.left, BF16 || t.param_bf16);
     else read8(static_cast<const float*>(it.param) + q.at, p, q.whole, q.left);
-    if (G16) read8(static_cast<const uint16_t*>(it.grad) + q.at, g, q.whole, q.left, t.grad_bf16);
+    if (G16) read8(static_cast<const uint16_t*>(it.grad) + q.at, g, q.whole, q.left, BF16 || t.grad_bf16);
     else read8(static_cast<const float*>(it.grad) + q.at, g, q.whole, q.left);
 }
 
-template <bool P16, bool COPY, class TABLE>
+template <bool P16, bool COPY, bool BF16, class TABLE>
 __device__ __forceinline__ void write_params(const TABLE& t, const som_adamw_tensor& it, const Place& q, const float (&p)[8])
 {
-    if (P16) write8(static_cast<uint16_t*>(it.param) + q.at, p, q.whole, q.left, t.param_bf16);
+    if (P16) write8(static_cast<uint16_t*>(it.param) + q.at, p, q.whole, q.left, BF16 || t.param_bf16);
     else write8(static_cast<float*>(it.param) + q.at, p, q.whole, q.left);
-    if (COPY) write8(static_cast<uint16_t*>(it.copy) + q.at, p, q.whole, q.left, t.copy_bf16);
+    if (COPY) write8(static_cast<uint16_t*>(it.copy) + q.at, p, q.whole, q.left, BF16 || t.copy_bf16);
 }
 
 // P16, G16: 16-bit parameters, gradients; COPY: a 16-bit copy of fp32 parameters
@@ -305,7 +314,7 @@ __global__ void __launch_bounds__(ADAM_THREADS) k_adamw(const __grid_constant__ 
     if (!(fabsf(scale) <= 3.4028235e38f) || q.left == 0) return;  // (an infinity or NaN: the step is left out)
     const Hyper h = t.h_at ? *t.h_at : t.h;
     float p[8], g[8], m[8], v[8];
-    read_params<P16, G16>(t, it, q, p, g);
+    read_params<P16, G16, false>(t, it, q, p, g);
     read8(static_cast<const float*>(it.m) + q.at, m, q.whole, q.left);
     read8(static_cast<const float*>(it.v) + q.at, v, q.whole, q.left);
 #pragma unroll
@@ -316,16 +325,17 @@ __global__ void __launch_bounds__(ADAM_THREADS) k_adamw(const __grid_constant__ 
         const float change = m[i] * h.k1 / (sqrtf(v[i] * h.k2) + h.eps);
         p[i] = p[i] * h.keep - change * h.rate;
     }
-    write_params<P16, COPY>(t, it, q, p);
+    write_params<P16, COPY, false>(t, it, q, p);
     write8(static_cast<float*>(it.m) + q.at, m, q.whole, q.left);
     write8(static_cast<float*>(it.v) + q.at, v, q.whole, q.left);
 }
 
-// The same with moments in 8 bits.  Bound by the issue of instructions as much as by HBM: arithmetic goes in pairs, square root and quotient are
-// the approximations (2^-22 of the change).  AT: the step's numbers come from memory; else they are operands from the kernel's
-// parameters, in pairs.  210 million elements: bf16 parameters 518 us (4.0 TB/s, issue slots 80 % busy), fp32 with a bf16 copy 576 (5.8 TB/s);
-// in scalars, two and more times eight elements a thread, or with other limits on registers (5 or 8 blocks an SM) 520 to 870.
-template <bool P16, bool G16, bool COPY, int CAP, bool AT>
+// The same with moments in 8 bits.  Bound by the issue of instructions (67 an element, slots 76 % busy) as much as by HBM: arithmetic goes in
+// pairs, square root and quotient are the approximations (2^-22 of the change).  AT: the step's numbers come from memory; else they are
+// the kernel's parameters, in pairs.  BF16: 16-bit parameters and gradients are bf16 (with fp32 parameters the choice at run time was
+// faster: 553 us, 643 with registers spilled).  210 million elements: bf16 parameters 502 us (4.2 TB/s), fp32 with a bf16 copy 553 (6.1 TB/s).
+// Slower: the arithmetic in scalars (560 and 644), two and four times eight elements a thread (506 to 570 and 610 to 870), 5, 7 or 8 blocks an SM.
+template <bool P16, bool G16, bool COPY, bool BF16, int CAP, bool AT>
 __global__ void __launch_bounds__(ADAM_THREADS, 6) k_adamw8(const __grid_constant__ AdamTable<CAP> t)
 {
     enter();
@@ -336,15 +346,16 @@ __global__ void __launch_bounds__(ADAM_THREADS, 6) k_adamw8(const __grid_constan
     if (AT) at_h = pairs_of(*t.h_at);
     const HyperPairs& h = AT ? at_h : t.pairs;
     const uint32_t seed = AT ? t.h_at->seed : t.h.seed;
-    const int lane = threadIdx.x & 31, off = threadIdx.x * 8;
+    // (the warp's number by a shuffle: what hangs on it alone is then computed once a warp)
+    const int lane = threadIdx.x & 31, off = threadIdx.x * 8, warp = __shfl_sync(0xffffffffu, (int)threadIdx.x >> 5, 0);
     const int64_t base = (int64_t)(blockIdx.x - it.first_chunk) * ADAM_CHUNK, blocks = (it.n + ADAM_BLOCK - 1) / ADAM_BLOCK;
     const int here = (int)(it.n - base < ADAM_CHUNK ? it.n - base : ADAM_CHUNK) - off;  // elements of the tensor from this thread's first on
     if (here + lane * 8 <= 0) return;  // none of the warp's
     const Place q = {base + off, here < 8 ? (here > 0 ? here : 0) : 8, here >= 8 && on16(it)};
-    uint8_t* em = it.exponents + base / ADAM_BLOCK + (threadIdx.x >> 5);
+    uint8_t* em = it.exponents + base / ADAM_BLOCK + warp;
     uint8_t* ev = em + blocks;
     float p[8], g[8];
-    read_params<P16, G16>(t, it, q, p, g);
+    read_params<P16, G16, BF16>(t, it, q, p, g);
     float2 m[4], v[4];
     {
         const uint2 mc = read_codes(static_cast<const uint8_t*>(it.m) + q.at, q.whole, q.left), vc = read_codes(static_cast<const uint8_t*>(it.v) + q.at, q.whole, q.left);
@@ -360,14 +371,14 @@ __global__ void __launch_bounds__(ADAM_THREADS, 6) k_adamw8(const __grid_constan
         // the root as x / sqrt(x + 1e-37): roots below 1e-15 are not right, and nothing next to eps
         const float2 more = __fadd2_rn(under, twice(1e-37f));
         float2 root = __fmul2_rn(under, make_float2(fast_rsqrt(more.x), fast_rsqrt(more.y)));
-        if (h.eps.x < 0.999e-8f) root = make_float2(sqrtf(under.x), sqrtf(under.y));
+        if (h.eps.x < 0.999e-8f) root = make_float2(near_sqrt(under.x), near_sqrt(under.y));
         root = __fadd2_rn(root, h.eps);
         const float2 change = __fmul2_rn(up, make_float2(fast_rcp(root.x), fast_rcp(root.y)));
         const float2 now = __ffma2_rn(change, h.minus_rate, __fmul2_rn(make_float2(p[2 * i], p[2 * i + 1]), h.keep));
         p[2 * i] = now.x, p[2 * i + 1] = now.y;
     }
-    write_params<P16, COPY>(t, it, q, p);
-    const uint32_t key = mix(mix((uint32_t)(q.at / ADAM_BLOCK)) ^ (seed + it.number * 0x9E3779B9u)) + lane * (8u * 0x6A09E667u);
+    write_params<P16, COPY, BF16>(t, it, q, p);
+    const uint32_t key = mix(mix((uint32_t)(base / ADAM_BLOCK) + warp) ^ (seed + it.number * 0x9E3779B9u)) + lane * (8u * 0x6A09E667u);
     uint32_t rm[8], rv[8];  // the lower and the upper half of mix()
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
@@ -418,11 +429,18 @@ __global__ void __launch_bounds__(ADAM_THREADS) k_adamw_moments(const __grid_con
 constexpr int FEW_TENSORS = 24, MOST_TENSORS = 500;
 static_assert(sizeof(AdamTable<MOST_TENSORS>) <= 32764, "kernel parameters");
 
+template <bool P16, bool G16, bool COPY, bool BF16, bool AT, int CAP>
+cudaError_t launch_8(som_layers* l, const AdamTable<CAP>& t, unsigned chunks, cudaStream_t st)
+{
+    return launch(l, k_adamw8<P16, G16, COPY, BF16, CAP, AT>, dim3(chunks), ADAM_THREADS, 0, st, 1, t);
+}
+
 template <bool P16, bool G16, bool COPY, int BITS, int CAP>
 cudaError_t launch_table(som_layers* l, const AdamTable<CAP>& t, unsigned chunks, cudaStream_t st)
 {
     if (BITS == 32) return launch(l, k_adamw<P16, G16, COPY, CAP>, dim3(chunks), ADAM_THREADS, 0, st, 1, t);
-    return launch(l, t.h_at ? k_adamw8<P16, G16, COPY, CAP, true> : k_adamw8<P16, G16, COPY, CAP, false>, dim3(chunks), ADAM_THREADS, 0, st, 1, t);
+    if (P16 && t.param_bf16) return t.h_at ? launch_8<P16, G16, COPY, P16, true>(l, t, chunks, st) : launch_8<P16, G16, COPY, P16, false>(l, t, chunks, st);
+    return t.h_at ? launch_8<P16, G16, COPY, false, true>(l, t, chunks, st) : launch_8<P16, G16, COPY, false, false>(l, t, chunks, st);
 }
 
 template <bool P16, bool G16, bool COPY, int BITS>
