@@ -52,6 +52,22 @@ __device__ __forceinline__ uint32_t fp4_codes(const float (&v)[8])
 // smallest exponents, which 2^126 lifts to [0, 6].
 __device__ __forceinline__ float fp4_value(uint32_t code) { return __uint_as_float(((code & 7u) << 22) | ((code & 8u) << 28)) * 0x1p126f; }
 
+// the values of eight codes over their blocks' power of two, the first in the lowest four bits
+__device__ __forceinline__ void fp4_values(uint32_t w, float2 (&v)[4])
+{
+    uint32_t h[4];
+    asm("{\n\t.reg .b8 a, b, c, d;\n\t"
+        "mov.b32 {a, b, c, d}, %4;\n\t"
+        "cvt.rn.f16x2.e2m1x2 %0, a;\n\t"
+        "cvt.rn.f16x2.e2m1x2 %1, b;\n\t"
+        "cvt.rn.f16x2.e2m1x2 %2, c;\n\t"
+        "cvt.rn.f16x2.e2m1x2 %3, d;\n\t}"
+        : "=r"(h[0]), "=r"(h[1]), "=r"(h[2]), "=r"(h[3])
+        : "r"(w));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = __half22float2(*reinterpret_cast<const __half2*>(&h[i]));
+}
+
 // A product of two matrices in 4 bits with som_linear's epilogue.
 struct Fp4Product {
     const uint8_t *x_codes, *x_scales, *w_codes, *w_scales;
