@@ -508,7 +508,9 @@ __global__ void __launch_bounds__(256) k_norm_columns(const ColumnArgs a)
     }
 }
 
-// the parts' sum, in their order
+constexpr int JOIN_AHEAD = 20;  // parts of a warp: all of 148 at once
+
+// the parts' sum, in a fixed order
 template <class W>
 __global__ void __launch_bounds__(256) k_norm_join(const ColumnJoinArgs a)
 {
@@ -518,12 +520,12 @@ __global__ void __launch_bounds__(256) k_norm_join(const ColumnJoinArgs a)
     const int64_t i = (int64_t)blockIdx.x * 32 + lane;  // of 2 D sums
     float s = 0.f;
     if (i < 2 * (int64_t)a.D)
-        for (int p = warp; p < a.parts; p += 64) {  // eight loads on their way at once
-            float v[8];
+        for (int p = warp; p < a.parts; p += 8 * JOIN_AHEAD) {
+            float v[JOIN_AHEAD];  // on their way at once (beyond the last part its values again, without a branch)
 #pragma unroll
-            for (int k = 0; k < 8; ++k) v[k] = p + 8 * k < a.parts ? a.part[(int64_t)(p + 8 * k) * 2 * a.D + i] : 0.f;
+            for (int k = 0; k < JOIN_AHEAD; ++k) v[k] = a.part[(int64_t)min(p + 8 * k, a.parts - 1) * 2 * a.D + i];
 #pragma unroll
-            for (int k = 0; k < 8; ++k) s += v[k];
+            for (int k = 0; k < JOIN_AHEAD; ++k) s += p + 8 * k < a.parts ? v[k] : 0.f;
         }
     part[warp][lane] = s;
     __syncthreads();
