@@ -6,6 +6,10 @@
 //
 // Bound by HBM: a few operations a value.  Everything between input and output is fp32; the variance is summed from the differences
 // to the mean, not from squares, so that a row far from zero keeps its digits.
+//
+// A row is held in registers by a group of threads, 16 values each, loaded in 16 bytes where rows lie on them and value by value else; longer
+// rows are walked.  8192 x 4096 bf16 with a residual 49 us (5.5 TB/s), its gradient 59 to 61 (4.5); rows of 4095 86 and 167.  The gradient is bound by
+// its chain of sums, with four rows an SM at a time (one of 8192 columns): 31 instructions a value, half of the issue slots.
 #include <initializer_list>
 #include <type_traits>
 
@@ -84,7 +88,7 @@ __device__ __forceinline__ void block_sums(float (&v)[N])
     }
 }
 
-// ---- rows on 16 bytes, held in registers ---------------------------------------------------------------------------
+// ---- rows held in registers ------------------------------------------------------------------------------------------
 
 constexpr int HELD = 16;  // values that a thread holds of a row: HELD * sizeof(E) / 16 pieces of 16 bytes, a group's threads apart
 
@@ -110,18 +114,87 @@ struct Piece {
     static constexpr int BF16 [[maybe_unused]] = std::is_same<E, __nv_bfloat16>::value;
 };
 
-// 2 N weights from column i on
-template <class W, int N>
-__device__ __forceinline__ void load_weights(const void* base, int i, float2 (&v)[N])
-{
-    const W* p = static_cast<const W*>(base) + i;
-#pragma unroll
-    for (int j = 0; j < N; j += Piece<W>::PAIRS) {
-        Piece<W> q;
-        q.load(p + 2 * j);
-        q.get(v + j);
+// Which columns of a row a thread holds.  LINED: rows on 16 bytes, of whole pieces; pieces lie a group's threads apart.  Else any row: single values
+// that are a group's threads apart, each load and store of a warp 32 values in a row.
+template <class E, bool LINED>
+struct Held {
+    using P = Piece<E>;
+    int t, threads, D;
+    __device__ __forceinline__ int column(int c, int j) const { return LINED ? (c * threads + t) * P::N + j : (c * P::N + j) * threads + t; }
+    __device__ __forceinline__ bool has(int c) const { return column(c, 0) < D; }  // any of piece c
+    // all of it: asked once a piece in fp32 (gradient of 16384 x 333 47.5 -> 38.7 us); 16-bit pieces are twice as long, and it cost registers (87 -> 98)
+    __device__ __forceinline__ bool full(int c) const { return sizeof(E) == 4 && column(c, P::N - 1) < D; }
+    // a value of piece c that is not in the row counts as 0
+    __device__ __forceinline__ float2 only(int c, int pair, float2 v) const
+    {
+        return LINED || full(c) ? v : make_float2(column(c, 2 * pair) < D ? v.x : 0.f, column(c, 2 * pair + 1) < D ? v.y : 0.f);
     }
-}
+    __device__ __forceinline__ void load(const E* row, int c, P& q) const
+    {
+        if constexpr (LINED) {
+            if (has(c)) q.load(row + column(c, 0));
+        } else {
+            uint32_t w[P::N];
+            if (full(c)) {
+                const uint32_t* from = reinterpret_cast<const uint32_t*>(row) + column(c, 0);
+#pragma unroll
+                for (int j = 0; j < P::N; ++j) w[j] = from[j * threads];
+            } else {
+#pragma unroll
+                for (int j = 0; j < P::N; ++j) {
+                    const int i = column(c, j);
+                    if constexpr (sizeof(E) == 4) w[j] = i < D ? *(reinterpret_cast<const uint32_t*>(row) + i) : 0u;
+                    else w[j] = i < D ? *(reinterpret_cast<const uint16_t*>(row) + i) : 0u;
+                }
+            }
+            if constexpr (sizeof(E) == 4) q.w = make_uint4(w[0], w[1], w[2], w[3]);
+            else q.w = make_uint4(w[0] | w[1] << 16, w[2] | w[3] << 16, w[4 % P::N] | w[5 % P::N] << 16, w[6 % P::N] | w[7 % P::N] << 16);
+        }
+    }
+    __device__ __forceinline__ void store(E* row, int c, const P& q) const
+    {
+        if constexpr (LINED) {
+            if (has(c)) q.store(row + column(c, 0));
+        } else {
+            const uint32_t w[4] = {q.w.x, q.w.y, q.w.z, q.w.w};
+            if (full(c)) {
+                uint32_t* to = reinterpret_cast<uint32_t*>(row) + column(c, 0);
+#pragma unroll
+                for (int j = 0; j < P::N; ++j) to[j * threads] = w[j % 4];
+            } else {
+#pragma unroll
+                for (int j = 0; j < P::N; ++j) {
+                    const int i = column(c, j);
+                    if constexpr (sizeof(E) == 4) {
+                        if (i < D) *(reinterpret_cast<uint32_t*>(row) + i) = w[j % 4];
+                    } else {
+                        if (i < D) *(reinterpret_cast<uint16_t*>(row) + i) = (uint16_t)(w[j / 2] >> (16 * (j & 1)));
+                    }
+                }
+            }
+        }
+    }
+    // weights of piece c (of a piece that is in the row)
+    template <class W>
+    __device__ __forceinline__ void weights(const void* base, int c, float2 (&v)[P::PAIRS]) const
+    {
+        const W* p = static_cast<const W*>(base);
+        if constexpr (LINED) {
+#pragma unroll
+            for (int j = 0; j < P::PAIRS; j += Piece<W>::PAIRS) {
+                Piece<W> q;
+                q.load(p + column(c, 2 * j));
+                q.get(v + j);
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < P::PAIRS; ++j) {
+                const int i = column(c, 2 * j), k = column(c, 2 * j + 1);
+                v[j] = make_float2(i < D ? wide(p[i]) : 0.f, k < D ? wide(p[k]) : 0.f);
+            }
+        }
+    }
+};
 
 // The arithmetic goes in pairs (one instruction for two values): what bounds these kernels next to HBM is the issue of instructions.
 __device__ __forceinline__ float2 twice(float v) { return make_float2(v, v); }
@@ -171,12 +244,13 @@ __device__ __forceinline__ float over(float s, float n, float inv)
 
 constexpr int FRONT_THREADS = 256, FRONT_MOST = 1024;  // a block holds as many rows as groups fit into 256 threads, or one
 
-template <class E, class W>
+template <class E, class W, bool LINED>
 __global__ void __launch_bounds__(FRONT_MOST) k_norm(const NormArgs a)
 {
     __shared__ float part0[FRONT_MOST / 32][1], part1[FRONT_MOST / 32][1];
     using P = Piece<E>;
     const int group = threadIdx.x >> a.log, threads = 1 << a.log, t = threadIdx.x & (threads - 1), warps = threads / 32, first = group * warps;
+    const Held<E, LINED> held = {t, threads, a.D};
     const int64_t row = (int64_t)blockIdx.x * (blockDim.x >> a.log) + group;
     enter();
     if (row >= a.T) return;  // (a whole group)
@@ -185,17 +259,13 @@ __global__ void __launch_bounds__(FRONT_MOST) k_norm(const NormArgs a)
     P px[P::COUNT], pr[P::COUNT];
 #pragma unroll
     for (int c = 0; c < P::COUNT; ++c) {
-        const int i = (c * threads + t) * P::N;
-        if (i < a.D) {
-            px[c].load(x + i);
-            if (res) pr[c].load(res + i);
-        }
+        held.load(x, c, px[c]);
+        if (res) held.load(res, c, pr[c]);
     }
     float2 v[P::COUNT][P::PAIRS], s2 = twice(0.f);
 #pragma unroll
-    for (int c = 0; c < P::COUNT; ++c) {
-        const int i = (c * threads + t) * P::N;
-        if (i < a.D) {
+    for (int c = 0; c < P::COUNT; ++c)
+        if (held.has(c)) {
             px[c].get(v[c]);
             if (res) {
                 float2 r[P::PAIRS];
@@ -205,21 +275,20 @@ __global__ void __launch_bounds__(FRONT_MOST) k_norm(const NormArgs a)
                 px[c].put(v[c]);
                 px[c].get(v[c]);
             }
-            if (a.sum) px[c].store(static_cast<E*>(a.sum) + row * a.lds + i);
+            if (a.sum) held.store(static_cast<E*>(a.sum) + row * a.lds, c, px[c]);
 #pragma unroll
             for (int j = 0; j < P::PAIRS; ++j) s2 = __fadd2_rn(s2, v[c][j]);
         }
-    }
     float s[1] = {s2.x + s2.y};
     group_sums(s, part0 + first, warps, threadIdx.x / 32 - first, 1 + group);
     const float mean = over(s[0], (float)a.D, a.inv);
     s2 = twice(0.f);
 #pragma unroll
     for (int c = 0; c < P::COUNT; ++c)
-        if ((c * threads + t) * P::N < a.D)
+        if (held.has(c))
 #pragma unroll
             for (int j = 0; j < P::PAIRS; ++j) {
-                v[c][j] = __fadd2_rn(v[c][j], twice(-mean));
+                v[c][j] = held.only(c, j, __fadd2_rn(v[c][j], twice(-mean)));
                 s2 = __ffma2_rn(v[c][j], v[c][j], s2);
             }
     s[0] = s2.x + s2.y;
@@ -227,23 +296,22 @@ __global__ void __launch_bounds__(FRONT_MOST) k_norm(const NormArgs a)
     const float r = rsqrtf(s[0] * a.inv + a.eps);
 #pragma unroll
     for (int c = 0; c < P::COUNT; ++c) {
-        const int i = (c * threads + t) * P::N;
-        if (i >= a.D) continue;
+        if (!held.has(c)) continue;
         float2 w[P::PAIRS];
 #pragma unroll
         for (int j = 0; j < P::PAIRS; ++j) v[c][j] = __fmul2_rn(v[c][j], twice(r));
         if (a.weight) {
-            load_weights<W>(a.weight, i, w);
+            held.template weights<W>(a.weight, c, w);
 #pragma unroll
             for (int j = 0; j < P::PAIRS; ++j) v[c][j] = __fmul2_rn(v[c][j], w[j]);
         }
         if (a.bias) {
-            load_weights<W>(a.bias, i, w);
+            held.template weights<W>(a.bias, c, w);
 #pragma unroll
             for (int j = 0; j < P::PAIRS; ++j) v[c][j] = __fadd2_rn(v[c][j], w[j]);
         }
         px[c].put(v[c]);
-        px[c].store(static_cast<E*>(a.y) + row * a.ldy + i);
+        held.store(static_cast<E*>(a.y) + row * a.ldy, c, px[c]);
     }
 }
 
@@ -269,7 +337,8 @@ __device__ __forceinline__ void copies_wait()
     asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
 }
 
-template <class E, class W>
+// Rows that are not LINED are loaded when their turn comes.
+template <class E, class W, bool LINED>
 __global__ void __launch_bounds__(BACK_THREADS, 1) k_norm_back(const NormBackArgs a)
 {
     __shared__ __align__(8) float part0[BACK_THREADS / 32][2], part1[BACK_THREADS / 32][2];
@@ -278,6 +347,7 @@ __global__ void __launch_bounds__(BACK_THREADS, 1) k_norm_back(const NormBackArg
     constexpr int DEPTH = 8 / (int)sizeof(E);
     const int group = threadIdx.x >> a.log, threads = 1 << a.log, t = threadIdx.x & (threads - 1), warps = threads / 32, first = group * warps, groups = BACK_THREADS >> a.log;
     const int warp = threadIdx.x / 32 - first;
+    const Held<E, LINED> held = {t, threads, a.D};
     enter();
     float2 w[P::COUNT][P::PAIRS], dw[P::COUNT][P::PAIRS], db[P::COUNT][P::PAIRS];
     const float n = (float)a.D, inv = a.inv;
@@ -290,23 +360,24 @@ __global__ void __launch_bounds__(BACK_THREADS, 1) k_norm_back(const NormBackArg
     for (int c = 0; c < P::COUNT; ++c) {
 #pragma unroll
         for (int j = 0; j < P::PAIRS; ++j) w[c][j] = twice(1.f), dw[c][j] = db[c][j] = twice(0.f);
-        if (a.weight && i0 + c * far < a.D) load_weights<W>(a.weight, i0 + c * far, w[c]);
+        if (a.weight && held.has(c)) held.template weights<W>(a.weight, c, w[c]);
     }
-    // what is not copied stays zero: columns beyond the row's end, and dsum where there is none
+    if constexpr (LINED) {  // what is not copied stays zero: columns beyond the row's end, and dsum where there is none
 #pragma unroll
-    for (int stage = 0; stage < RING; stage += STAGE)
+        for (int stage = 0; stage < RING; stage += STAGE)
 #pragma unroll
-        for (int what = 0; what < 3; ++what)
+            for (int what = 0; what < 3; ++what)
 #pragma unroll
-            for (int c = 0; c < P::COUNT; ++c)
-                if (i0 + c * far >= a.D || (what == 2 && !a.dsum)) *piece(stage, what, c) = make_uint4(0u, 0u, 0u, 0u);
+                for (int c = 0; c < P::COUNT; ++c)
+                    if (!held.has(c) || (what == 2 && !a.dsum)) *piece(stage, what, c) = make_uint4(0u, 0u, 0u, 0u);
+    }
     int64_t row = (int64_t)blockIdx.x * groups + group;
     const int64_t step = (int64_t)gridDim.x * groups;
     // the next row to fetch, and where it lies
     int64_t ahead = row;
     const E *fx = static_cast<const E*>(a.x) + row * a.ldx + i0, *fg = static_cast<const E*>(a.dy) + row * a.lddy + i0;
     const E* fs = a.dsum ? static_cast<const E*>(a.dsum) + row * a.ldds + i0 : nullptr;
-    E* to = a.dx ? static_cast<E*>(a.dx) + row * a.D + i0 : nullptr;
+    E* to = a.dx ? static_cast<E*>(a.dx) + row * a.D : nullptr;
     auto fetch = [&](int stage) {
         if (ahead < a.T) {
             auto copy = [&](auto c) {
@@ -331,20 +402,33 @@ __global__ void __launch_bounds__(BACK_THREADS, 1) k_norm_back(const NormBackArg
         copies_end();
     };
     static_assert(P::COUNT == 2 || P::COUNT == 4, "pieces of a thread");
+    if constexpr (LINED)
 #pragma unroll
-    for (int k = 0; k < DEPTH - 1; ++k) fetch(k * STAGE);
+        for (int k = 0; k < DEPTH - 1; ++k) fetch(k * STAGE);
     int stage = 0;
     for (; row < a.T; row += step) {
-        fetch(stage == 0 ? RING - STAGE : stage - STAGE);  // (the place of the row before)
-        copies_wait<DEPTH - 1>();
+        P qx[P::COUNT], qg[P::COUNT], qs[P::COUNT];
+        if constexpr (LINED) {
+            fetch(stage == 0 ? RING - STAGE : stage - STAGE);  // (the place of the row before)
+            copies_wait<DEPTH - 1>();
+        } else {
+#pragma unroll
+            for (int c = 0; c < P::COUNT; ++c) {
+                held.load(static_cast<const E*>(a.x) + row * a.ldx, c, qx[c]);
+                held.load(static_cast<const E*>(a.dy) + row * a.lddy, c, qg[c]);
+                qs[c].w = make_uint4(0u, 0u, 0u, 0u);
+                if (a.dsum) held.load(static_cast<const E*>(a.dsum) + row * a.ldds, c, qs[c]);
+            }
+        }
         float2 v[P::COUNT][P::PAIRS], g[P::COUNT][P::PAIRS], s0 = twice(0.f), s1 = twice(0.f);
 #pragma unroll
         for (int c = 0; c < P::COUNT; ++c) {
-            P q;
-            q.w = *piece(stage, 0, c);
-            q.get(v[c]);
-            q.w = *piece(stage, 1, c);
-            q.get(g[c]);
+            if constexpr (LINED) {
+                qx[c].w = *piece(stage, 0, c);
+                qg[c].w = *piece(stage, 1, c);
+            }
+            qx[c].get(v[c]);
+            qg[c].get(g[c]);
 #pragma unroll
             for (int j = 0; j < P::PAIRS; ++j) {
                 s0 = __fadd2_rn(s0, v[c][j]);
@@ -357,10 +441,10 @@ __global__ void __launch_bounds__(BACK_THREADS, 1) k_norm_back(const NormBackArg
         s0 = s1 = twice(0.f);
 #pragma unroll
         for (int c = 0; c < P::COUNT; ++c)
-            if (i0 + c * far < a.D)
+            if (held.has(c))
 #pragma unroll
                 for (int j = 0; j < P::PAIRS; ++j) {
-                    v[c][j] = __fadd2_rn(v[c][j], twice(-mean));
+                    v[c][j] = held.only(c, j, __fadd2_rn(v[c][j], twice(-mean)));
                     s0 = __ffma2_rn(v[c][j], v[c][j], s0);
                     s1 = __ffma2_rn(v[c][j], __fmul2_rn(g[c][j], w[c][j]), s1);
                 }
@@ -372,7 +456,7 @@ __global__ void __launch_bounds__(BACK_THREADS, 1) k_norm_back(const NormBackArg
         for (int c = 0; c < P::COUNT; ++c) {
             float2 out[P::PAIRS];
             P q;
-            q.w = *piece(stage, 2, c);
+            q.w = LINED ? *piece(stage, 2, c) : qs[c].w;
             q.get(out);
 #pragma unroll
             for (int j = 0; j < P::PAIRS; ++j) {
@@ -381,9 +465,9 @@ __global__ void __launch_bounds__(BACK_THREADS, 1) k_norm_back(const NormBackArg
                 db[c][j] = __fadd2_rn(db[c][j], g[c][j]);
                 out[j] = __ffma2_rn(twice(r), __ffma2_rn(v[c][j], twice(along), d), out[j]);
             }
-            if (to && i0 + c * far < a.D) {
+            if (to) {
                 q.put(out);
-                q.store(to + c * far);
+                held.store(to, c, q);
             }
         }
         if (to) to += step * a.D;
@@ -396,22 +480,22 @@ __global__ void __launch_bounds__(BACK_THREADS, 1) k_norm_back(const NormBackArg
     for (int k = 0; k < groups; ++k) {  // one group after the other, in their order
         if (group == k)
 #pragma unroll
-            for (int c = 0; c < P::COUNT; ++c) {
-                const int i = i0 + c * far;
-                if (i < a.D)
+            for (int c = 0; c < P::COUNT; ++c)
 #pragma unroll
-                    for (int j = 0; j < P::PAIRS; ++j) {
-                        float2 *w0 = reinterpret_cast<float2*>(columns + i) + j, *b0 = reinterpret_cast<float2*>(columns + a.D + i) + j;
-                        *w0 = k ? __fadd2_rn(*w0, dw[c][j]) : dw[c][j];
-                        *b0 = k ? __fadd2_rn(*b0, db[c][j]) : db[c][j];
+                for (int j = 0; j < P::N; ++j) {
+                    const int i = held.column(c, j);
+                    const float dwi = j & 1 ? dw[c][j / 2].y : dw[c][j / 2].x, dbi = j & 1 ? db[c][j / 2].y : db[c][j / 2].x;
+                    if (i < a.D) {
+                        columns[i] = k ? columns[i] + dwi : dwi;
+                        columns[a.D + i] = k ? columns[a.D + i] + dbi : dbi;
                     }
-            }
+                }
         __syncthreads();
     }
     for (int i = threadIdx.x; i < 2 * a.D; i += BACK_THREADS) a.part[(int64_t)blockIdx.x * 2 * a.D + i] = columns[i];
 }
 
-// ---- any row length and alignment ------------------------------------------------------------------------------------
+// ---- rows too long for the registers ---------------------------------------------------------------------------------
 
 // A block a row, which it walks three times (from L1 or L2 after the first).
 template <class E, class W>
@@ -553,17 +637,22 @@ int check_norm(const som_layers* l, int type, int weights_type, int64_t T, int64
     return T >= MOST_ROWS || D > MOST_COLS ? SOM_ERR_UNSUPPORTED : SOM_OK;
 }
 
-// Logarithm of the threads of a row that is held in registers: as many warps, a power of two, as hold it.  0: too long, or not on 16 bytes
-int group_of(int64_t D, int most, int bytes, std::initializer_list<const void*> rows, std::initializer_list<int64_t> lds)
+// Logarithm of the threads of a row that is held in registers: as many warps, a power of two, as hold it.  0: too long
+int group_of(int64_t D, int most)
 {
-    if (D * bytes % 16 != 0 || D > (int64_t)most * HELD) return 0;
-    for (const void* p : rows)
-        if (!aligned16(p)) return 0;
-    for (int64_t ld : lds)
-        if (ld * bytes % 16 != 0) return 0;
+    if (D > (int64_t)most * HELD) return 0;
     int log = 5;
     while (((int64_t)HELD << log) < D) ++log;
     return log;
+}
+
+// whether rows lie on 16 bytes and are whole pieces of them
+bool lined(int64_t D, int bytes, std::initializer_list<const void*> rows, std::initializer_list<int64_t> lds)
+{
+    bool on = D * bytes % 16 == 0;
+    for (const void* p : rows) on = on && aligned16(p);
+    for (int64_t ld : lds) on = on && ld * bytes % 16 == 0;
+    return on;
 }
 
 // rows of a norm's matrix: present, and long enough
@@ -578,7 +667,8 @@ template <class E, class W>
 cudaError_t prepare_as()
 {
     static_assert(back_smem<E>() >= 2 * BACK_THREADS * HELD * (int)sizeof(float), "the columns' sums take the ring's place");
-    return cudaFuncSetAttribute(k_norm_back<E, W>, cudaFuncAttributeMaxDynamicSharedMemorySize, back_smem<E>());
+    const cudaError_t e = cudaFuncSetAttribute(k_norm_back<E, W, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, back_smem<E>());
+    return e == cudaSuccess ? cudaFuncSetAttribute(k_norm_back<E, W, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, back_smem<E>()) : e;
 }
 
 }  // namespace
@@ -609,14 +699,18 @@ int som_norm(som_layers* l, int type, int64_t T, int64_t D, const void* x, int64
     if (T == 0) return SOM_OK;
     Guard g(l->device);
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
-    const int log = group_of(D, FRONT_MOST, type == SOM_F32 ? 4 : 2, {x, residual, weight, bias, sum, y}, {ldx, residual ? ldr : 0, sum ? lds : 0, ldy});
+    int log = group_of(D, FRONT_MOST);
+    const bool on16 = lined(D, type == SOM_F32 ? 4 : 2, {x, residual, weight, bias, sum, y}, {ldx, residual ? ldr : 0, sum ? lds : 0, ldy});
+    // Rows of 16-bit values that are not on 16 bytes: loads of two bytes are what costs, and beyond this length three walks with more threads are as
+    // fast.  Held / walked, with a residual: 16384 x 1001 47 / 66 us, 16384 x 2001 91 / 94, 8192 x 4095 90 / 86, 2000 x 12001 113 / 78; fp32 4096 x 8001 104 / 146.
+    if (!on16 && type != SOM_F32 && D > 2048) log = 0;
     const NormArgs a = {x, residual, weight, bias, sum, y, ldx, ldr, lds, ldy, T, (int)D, log, 1.f / (float)D, eps};
     return outcome(l, by_types(type, weights_type, [&](auto e, auto w) {
                        using E = decltype(e);
                        using W = decltype(w);
                        if (!log) return launch(l, k_norm_any<E, W>, dim3((unsigned)T), ROW_THREADS, 0, st, 1, a);
                        const int threads = (1 << log) < FRONT_THREADS ? FRONT_THREADS : 1 << log;
-                       return launch(l, k_norm<E, W>, dim3((unsigned)tiles_of(T, threads >> log)), threads, 0, st, 1, a);
+                       return launch(l, on16 ? k_norm<E, W, true> : k_norm<E, W, false>, dim3((unsigned)tiles_of(T, threads >> log)), threads, 0, st, 1, a);
                    }));
 }
 
@@ -637,7 +731,8 @@ int som_norm_backward(som_layers* l, int type, int64_t T, int64_t D, const void*
         return SOM_OK;
     }
     const bool columns = dweight || dbias;
-    const int log = group_of(D, BACK_THREADS, type == SOM_F32 ? 4 : 2, {x, dy, dsum, dx, weight}, {ldx, lddy, dsum ? ldds : 0});
+    const int log = group_of(D, BACK_THREADS);
+    const bool on16 = lined(D, type == SOM_F32 ? 4 : 2, {x, dy, dsum, dx, weight}, {ldx, lddy, dsum ? ldds : 0});
     int64_t parts;
     if (log) {
         parts = tiles_of(T, BACK_THREADS >> log);
@@ -665,7 +760,7 @@ int som_norm_backward(som_layers* l, int type, int64_t T, int64_t D, const void*
                        using W = decltype(w);
                        cudaError_t r;
                        if (log) {
-                           r = launch(l, k_norm_back<E, W>, dim3((unsigned)parts), BACK_THREADS, back_smem<E>(), st, 1, a);
+                           r = launch(l, on16 ? k_norm_back<E, W, true> : k_norm_back<E, W, false>, dim3((unsigned)parts), BACK_THREADS, back_smem<E>(), st, 1, a);
                        } else {
                            r = launch(l, k_norm_back_any<E, W>, dim3((unsigned)T), ROW_THREADS, 0, st, 1, a);
                            if (r == cudaSuccess && columns) r = launch(l, k_norm_columns<E>, dim3((unsigned)tiles_of(D, 32), (unsigned)parts), 256, 0, st, 1, b);
