@@ -333,7 +333,7 @@ __global__ void __launch_bounds__(ADAM_THREADS) k_adamw(const __grid_constant__ 
 // The same with moments in 8 bits.  Bound by the issue of instructions (67 an element, slots 76 % busy) as much as by HBM: arithmetic goes in
 // pairs, square root and quotient are the approximations (2^-22 of the change).  AT: the step's numbers come from memory; else they are
 // the kernel's parameters, in pairs.  BF16: 16-bit parameters and gradients are bf16 (with fp32 parameters the choice at run time was
-// faster: 553 us, 643 with registers spilled).  210 million elements: bf16 parameters 502 us (4.2 TB/s), fp32 with a bf16 copy 553 (6.1 TB/s).
+// faster: 546 us, 643 with registers spilled).  210 million elements: bf16 parameters 496 us (4.2 TB/s), fp32 with a bf16 copy 546 (6.1 TB/s).
 // Slower: the arithmetic in scalars (560 and 644), two and four times eight elements a thread (506 to 570 and 610 to 870), 5, 7 or 8 blocks an SM.
 template <bool P16, bool G16, bool COPY, bool BF16, int CAP, bool AT>
 __global__ void __launch_bounds__(ADAM_THREADS, 6) k_adamw8(const __grid_constant__ AdamTable<CAP> t)
@@ -356,26 +356,33 @@ __global__ void __launch_bounds__(ADAM_THREADS, 6) k_adamw8(const __grid_constan
     uint8_t* ev = em + blocks;
     float p[8], g[8];
     read_params<P16, G16, BF16>(t, it, q, p, g);
+    const float top = largest(largest(largest(g[0], g[1], g[2]), g[3], g[4]), largest(g[5], g[6], g[7]), 0.f);
+    const bool by_root = h.eps.x < 0.999e-8f || top * fabsf(scale) >= 1e18f;
     float2 m[4], v[4];
     {
         const uint2 mc = read_codes(static_cast<const uint8_t*>(it.m) + q.at, q.whole, q.left), vc = read_codes(static_cast<const uint8_t*>(it.v) + q.at, q.whole, q.left);
         decode8<true>(mc, *em, m);
         decode8<false>(vc, *ev, v);
     }
+    auto moves = [&](auto root_of) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const float2 gi = __fmul2_rn(make_float2(g[2 * i], g[2 * i + 1]), twice(scale));  // (by 1 where there is none)
-        m[i] = sum2(__fmul2_rn(m[i], h.b1), __fmul2_rn(gi, h.c1));
-        v[i] = sum2(__fmul2_rn(v[i], h.b2), __fmul2_rn(__fmul2_rn(gi, gi), h.c2));
-        const float2 up = __fmul2_rn(m[i], h.k1), under = __fmul2_rn(v[i], h.k2);
-        // the root as x / sqrt(x + 1e-37): roots below 1e-15 are not right, and nothing next to eps
-        const float2 more = __fadd2_rn(under, twice(1e-37f));
-        float2 root = __fmul2_rn(under, make_float2(fast_rsqrt(more.x), fast_rsqrt(more.y)));
-        if (h.eps.x < 0.999e-8f) root = make_float2(near_sqrt(under.x), near_sqrt(under.y));
-        root = __fadd2_rn(root, h.eps);
-        const float2 change = __fmul2_rn(up, make_float2(fast_rcp(root.x), fast_rcp(root.y)));
-        const float2 now = __ffma2_rn(change, h.minus_rate, __fmul2_rn(make_float2(p[2 * i], p[2 * i + 1]), h.keep));
-        p[2 * i] = now.x, p[2 * i + 1] = now.y;
+        for (int i = 0; i < 4; ++i) {
+            const float2 gi = __fmul2_rn(make_float2(g[2 * i], g[2 * i + 1]), twice(scale));  // (by 1 where there is none)
+            m[i] = sum2(__fmul2_rn(m[i], h.b1), __fmul2_rn(gi, h.c1));
+            v[i] = sum2(__fmul2_rn(v[i], h.b2), __fmul2_rn(__fmul2_rn(gi, gi), h.c2));
+            const float2 up = __fmul2_rn(m[i], h.k1), root = __fadd2_rn(root_of(__fmul2_rn(v[i], h.k2)), h.eps);
+            const float2 change = __fmul2_rn(up, make_float2(fast_rcp(root.x), fast_rcp(root.y)));
+            const float2 now = __ffma2_rn(change, h.minus_rate, __fmul2_rn(make_float2(p[2 * i], p[2 * i + 1]), h.keep));
+            p[2 * i] = now.x, p[2 * i + 1] = now.y;
+        }
+    };
+    if (by_root) {
+        moves([](float2 x) { return make_float2(near_sqrt(x.x), near_sqrt(x.y)); });
+    } else {  // as x / sqrt(x + 1e-37): roots below 1e-15 are not right, and nothing next to eps; not for an infinite x
+        moves([](float2 x) {
+            const float2 more = __fadd2_rn(x, twice(1e-37f));
+            return __fmul2_rn(x, make_float2(fast_rsqrt(more.x), fast_rsqrt(more.y)));
+        });
     }
     write_params<P16, COPY, BF16>(t, it, q, p);
     const uint32_t key = mix(mix((uint32_t)(base / ADAM_BLOCK) + warp) ^ (seed + it.number * 0x9E3779B9u)) + lane * (8u * 0x6A09E667u);

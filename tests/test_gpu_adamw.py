@@ -147,6 +147,21 @@ def test_a_bad_gradient_stays_in_its_block(L):
 
 
 @pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("eps", [1e-8, 1e-3, 1e-10, 0.0])
+def test_ends_of_the_range(L, bits, eps):
+    """Gradients whose squares are infinite, subnormal or 0 in fp32: an infinite second moment moves nothing, without eps the step's size is the rate."""
+    size = [1e25, 1e10, 1.0, 1e-10, 1e-17] + ([] if eps == 0.0 else [1e-22, 0.0])
+    g = torch.tensor(size, device="cuda").repeat_interleave(256)
+    p = torch.ones_like(g)
+    opt = AdamW(L, [p], bits=bits)
+    opt.step([g], rate=0.25, decay=0.0, eps=eps)
+    m, v = ref.moments_step(np.zeros(g.numel(), np.float32), np.zeros(g.numel(), np.float32), host(g), 0.9, 0.999)
+    want, tol = ref.param_step(np.ones(g.numel(), np.float32), m, v, 0.25, 0.9, 0.999, np.float64(np.float32(eps)), 0.0, 1)
+    # (a subnormal second moment keeps few digits, the same here and there; the smallest that 1e-17 leaves has 2^20 steps)
+    assert (np.abs(host(p) - want) <= tol).all()
+
+
+@pytest.mark.parametrize("bits", [32, 8])
 def test_a_scale_that_is_not_finite_leaves_all_as_it_was(L, bits):
     params, grads, copies = tensors(ODD, "fp32", "bf16", "bf16", steps=1)
     opt = AdamW(L, params, copies, bits)
