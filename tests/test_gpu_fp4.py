@@ -201,6 +201,23 @@ def test_same_bits_every_time_and_in_a_graph(L, T, D, F):
     assert torch.equal(first, again)
 
 
+def test_offsets_beyond_32_bits(L):
+    """Rows whose elements lie beyond 2^31 get what they get by themselves, in a product of the same tiles."""
+    T, D, F, last = 1100000, 2048, 64, 40000
+    x = torch.zeros(T, D, device="cuda", dtype=torch.bfloat16)
+    gen = torch.Generator(device="cuda").manual_seed(2)
+    x[-last:] = torch.randn(last, D, generator=gen, device="cuda").bfloat16()
+    part = x[-last:].clone()
+    a, b = L.quantize_fp4(x), L.quantize_fp4(part)
+    assert torch.equal(a.codes[-last:], b.codes)
+    values = L.values_fp4(a)
+    assert torch.equal(values[-last:], L.values_fp4(b)) and not bool(values[:-last].any())
+    del values
+    w = L.quantize_fp4(torch.randn(F, D, generator=gen, device="cuda").bfloat16())
+    y = L.linear_fp4(x, w)
+    assert torch.equal(y[-last:], L.linear_fp4(part, w)) and not bool(y[:-last].any()) and L.device_flags() == 0
+
+
 def test_strided_operands(L):
     x, w, b, r = layer(70, 512, 256, "fp16")
     wide, far = torch.zeros(70, 640, device="cuda", dtype=torch.float16), torch.zeros(70, 512, device="cuda", dtype=torch.float16)

@@ -165,6 +165,25 @@ def test_another_stream(L):
     assert torch.equal(got["y"], want["y"]) and torch.equal(got["sum"], want["sum"])
 
 
+def test_offsets_beyond_32_bits(L):
+    """Rows whose elements lie beyond 2^31 get what they get by themselves."""
+    T, D, last = 1100000, 2048, 333
+    x = torch.zeros(T, D, device="cuda", dtype=torch.bfloat16)
+    gen = torch.Generator(device="cuda").manual_seed(2)
+    x[-last:] = torch.randn(last, D, generator=gen, device="cuda").bfloat16()
+    w, b = torch.randn(D, generator=gen, device="cuda").bfloat16(), torch.randn(D, generator=gen, device="cuda").bfloat16()
+    y, alone = L.norm(x, w, b, x), L.norm(x[-last:].clone(), w, b, x[-last:].clone())
+    assert torch.equal(y["y"][-last:], alone["y"]) and torch.equal(y["sum"][-last:], alone["sum"])
+    del y
+    dy = torch.zeros_like(x)
+    dy[-last:] = torch.randn(last, D, generator=gen, device="cuda").bfloat16()
+    got, alone = L.norm_backward(x, w, dy, b), L.norm_backward(x[-last:].clone(), w, dy[-last:].clone(), b)
+    assert torch.equal(got["dx"][-last:], alone["dx"]) and not bool(got["dx"][:-last].any())
+    for n in ("dweight", "dbias"):  # the same terms in other parts: sums of 333 of size 1 in fp32, rounded to bf16
+        off = (got[n].float() - alone[n].float()).abs()
+        assert bool((off <= 2.0 ** -7 * alone[n].float().abs() + 333 * 2.0 ** -18).all())
+
+
 def test_against_differences(L):
     """The gradient against (f(x + h) - f(x - h)) / 2 h of the forward call in fp32, f = sum(dy y), along random directions."""
     x, _, w, b, dy = inputs(4, 300, "fp32", residual=False, seed=5)
