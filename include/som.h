@@ -572,7 +572,9 @@ typedef struct som_adamw_step {
  * som_adamw - one step over `count` tensors (a host array, read within the call; no two may share memory):
  *   g = scale * grad, m = beta1 m + (1 - beta1) g, v = beta2 v + (1 - beta2) g^2,
  *   param = param (1 - rate decay) - rate (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps)
- * in fp32, param rounded once to param_type, copy (copy_type SOM_F16 or SOM_BF16 beside fp32 parameters, -1 = none) to its type.
+ * in fp32, param rounded once to param_type, copy (copy_type SOM_F16 or SOM_BF16 beside fp32 parameters, -1 = none) to its type.  The
+ * hyperparameters' terms (1 - rate decay, 1 - beta, 1 / (1 - beta^t)) are computed in 64 bits and rounded to fp32.  With moments in fp32 every
+ * operation is rounded by itself, to the nearest: p = p keep - ((m k1) / (sqrt(v k2) + eps)) rate.
  * grad_type: SOM_F32, or 16 bits (beside 16-bit parameters their own type).
  * bits 32: moments in fp32.  bits 8: 256 consecutive elements share a power of two 2^(e - 127), that of their largest magnitude, or the next
  * where that is 1.875 times it or more (e = 255: it is not finite, and the block's values are infinities and NaN); an element is a code of 8 bits: m a sign, 4 bits of exponent E and 3 of fraction

@@ -12,7 +12,8 @@
 // positive v never becomes 0 (the quotient would lose its measure).  The fp32 value that a code is made from is the one that the step used.
 //
 // Products and sums that the codes come from are rounded one by one (no fused multiply-add): which code is taken is then a matter of
-// the definition, not of the compiler.
+// the definition, not of the compiler.  With moments in 32 bits all operations are, the parameter's too: a 16-bit copy that a fused last product
+// moves to its other neighbour now and then (5 of a million) is not the one of the formula in fp32.
 //
 // Bound by HBM: 28 bytes an element with fp32 parameters, a bf16 copy and bf16 gradients, 10 with 8-bit moments and bf16
 // parameters.  A block takes 2048 elements of one tensor, a thread eight in a row, a warp the 256 that share a power; the tensors'
@@ -322,8 +323,8 @@ __global__ void __launch_bounds__(ADAM_THREADS) k_adamw(const __grid_constant__ 
         if (t.scale) g[i] = __fmul_rn(g[i], scale);
         m[i] = __fadd_rn(__fmul_rn(m[i], h.b1), __fmul_rn(g[i], h.c1));
         v[i] = __fadd_rn(__fmul_rn(v[i], h.b2), __fmul_rn(__fmul_rn(g[i], g[i]), h.c2));
-        const float change = m[i] * h.k1 / (sqrtf(v[i] * h.k2) + h.eps);
-        p[i] = p[i] * h.keep - change * h.rate;
+        const float change = __fmul_rn(m[i], h.k1) / __fadd_rn(sqrtf(__fmul_rn(v[i], h.k2)), h.eps);
+        p[i] = __fsub_rn(__fmul_rn(p[i], h.keep), __fmul_rn(change, h.rate));
     }
     write_params<P16, COPY, false>(t, it, q, p);
     write8(static_cast<float*>(it.m) + q.at, m, q.whole, q.left);
