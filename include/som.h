@@ -577,8 +577,9 @@ typedef struct som_adamw_step {
  * operation is rounded by itself, to the nearest: p = p keep - ((m k1) / (sqrt(v k2) + eps)) rate.
  * grad_type: SOM_F32, or 16 bits (beside 16-bit parameters their own type).
  * bits 32: moments in fp32.  bits 8: 256 consecutive elements share a power of two 2^(e - 127), that of their largest magnitude, or the next
- * where that is 1.875 times it or more (e = 255: it is not finite, and the block's values are infinities and NaN); an element is a code of 8 bits: m a sign, 4 bits of exponent E and 3 of fraction
- * f, (1 + f / 8) 2^(E - 15), f / 8 2^-14 for E = 0; v the same with 5 bits and no sign, 2^(E - 31) and 2^-30.  A new value is rounded to one
+ * where that is 1.875 times it or more (e = 255: it is not finite, and the block's values are infinities, and NaN where the code is 0); an
+ * element is a code of 8 bits: m a sign, 4 bits of exponent E and 3 of fraction f, (1 + f / 8) 2^(E - 15), f / 8 2^-14 for E = 0; v the
+ * same with 5 bits and no sign, 2^(E - 31) and 2^-30.  An infinite v moves nothing, in either form.  A new value is rounded to one
  * of its two neighbours by 16 random bits that are a function of (seed, number, element), so that the mean is right; v > 0 does not
  * become 0.  The step itself uses the value before that rounding.
  */

@@ -358,12 +358,14 @@ __global__ void __launch_bounds__(ADAM_THREADS, 6) k_adamw8(const __grid_constan
     float p[8], g[8];
     read_params<P16, G16, BF16>(t, it, q, p, g);
     const float top = largest(largest(largest(g[0], g[1], g[2]), g[3], g[4]), largest(g[5], g[6], g[7]), 0.f);
-    const bool by_root = h.eps.x < 0.999e-8f || top * fabsf(scale) >= 1e18f;
+    const uint32_t e_v = *ev;
+    // (otherwise v k2 is below 2 power k2 + 1e36, and so finite; a NaN among the gradients counts as a large one)
+    const bool by_root = h.eps.x < 0.999e-8f || !(top * fabsf(scale) < 1e18f) || !(power_of(e_v) * h.k2.x < 1e38f);
     float2 m[4], v[4];
     {
         const uint2 mc = read_codes(static_cast<const uint8_t*>(it.m) + q.at, q.whole, q.left), vc = read_codes(static_cast<const uint8_t*>(it.v) + q.at, q.whole, q.left);
         decode8<true>(mc, *em, m);
-        decode8<false>(vc, *ev, v);
+        decode8<false>(vc, e_v, v);
     }
     auto moves = [&](auto root_of) {
 #pragma unroll
@@ -379,7 +381,7 @@ __global__ void __launch_bounds__(ADAM_THREADS, 6) k_adamw8(const __grid_constan
     };
     if (by_root) {
         moves([](float2 x) { return make_float2(near_sqrt(x.x), near_sqrt(x.y)); });
-    } else {  // as x / sqrt(x + 1e-37): roots below 1e-15 are not right, and nothing next to eps; not for an infinite x
+    } else {  // as x / sqrt(x + 1e-37): roots below 1e-15 are not right, and nothing next to eps; an infinite x would give NaN
         moves([](float2 x) {
             const float2 more = __fadd2_rn(x, twice(1e-37f));
             return __fmul2_rn(x, make_float2(fast_rsqrt(more.x), fast_rsqrt(more.y)));
