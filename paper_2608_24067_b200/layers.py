@@ -10,7 +10,9 @@ them part of a graph).  Neither do ``AdamW``'s steps, which write the parameters
 """
 from __future__ import annotations
 
+import array
 import ctypes
+import operator
 
 import torch
 
@@ -438,18 +440,24 @@ class _Step(ctypes.Structure):
                 ("step", ctypes.c_int64), ("rate_at", ctypes.c_void_p), ("step_at", ctypes.c_void_p), ("scale", ctypes.c_void_p), ("seed", ctypes.c_uint32)]
 
 
+# of many tensors, by map(): a loop over the same checks takes up to twice the time
+_address, _numel, _contiguous, _gpu = torch.Tensor.data_ptr, torch.Tensor.numel, torch.Tensor.is_contiguous, torch.Tensor.get_device
+_dtype, _shape = operator.attrgetter("dtype"), operator.attrgetter("shape")
+
+
 class AdamW:
     """AdamW over many tensors (``som_adamw``): it keeps their moments, in 32 bits or in 8, and ``step`` moves all of them in one launch (one for
     each combination of types, and for each 500 tensors).
 
     params: contiguous CUDA tensors (float32, float16 or bfloat16) on the handle's device that share no memory; copies: for each float32
-    parameter a 16-bit tensor that gets its new value, or None.  The first step has number 1."""
+    parameter a 16-bit tensor that gets its new value, or None.  Both keep their memory: a step refuses one whose memory, type or size was
+    exchanged (``p.data = ...``, ``Module.half``), and a new optimiser takes over with ``state`` and ``load``.  The first step has number 1."""
 
     def __init__(self, layers, params, copies=None, bits=32):
         if bits not in (8, 32):
             raise ValueError("bits must be 8 or 32")
-        self._layers, self.bits, self.params, self.steps = layers, bits, list(params), 0
-        self.copies = [None] * len(self.params) if copies is None else list(copies)
+        self._layers, self.bits, self.params, self.steps = layers, bits, tuple(params), 0
+        self.copies = (None,) * len(self.params) if copies is None else tuple(copies)
         if len(self.copies) != len(self.params):
             raise ValueError("copies must be as many as params")
         on, spans, groups = layers.device.index, [], {}
@@ -474,7 +482,10 @@ class AdamW:
             self._m = [torch.zeros_like(p, dtype=torch.uint8) for p in self.params]
             self._v = [torch.zeros_like(p, dtype=torch.uint8) for p in self.params]
             self._exponents = [p.new_zeros((2, -(-p.numel() // 256)), dtype=torch.uint8) for p in self.params]
-        self._groups, self._shapes = [], [p.shape for p in self.params]
+        self._groups = []
+        # what the tables say of the parameters and their copies
+        self._written = [t for t in (*self.params, *self.copies) if t is not None]
+        self._homes = [list(map(f, self._written)) for f in (_address, _dtype, _numel)]
         # where moments() puts the values: pieces of one tensor, each on 16 bytes
         self._places, self._all = [], 0
         for p in self.params:
@@ -486,7 +497,9 @@ class AdamW:
                 p, c, e = self.params[i], self.copies[i], self._exponents[i]
                 t.param, t.copy, t.m, t.v = p.data_ptr(), 0 if c is None else c.data_ptr(), self._m[i].data_ptr(), self._v[i].data_ptr()
                 t.exponents, t.n, t.number = 0 if e is None else e.data_ptr(), p.numel(), i
-            self._groups.append((pt, -1 if ct is None else _TYPES[ct], which, table))
+            # the gradients' addresses in it, and their shapes
+            column = memoryview(table).cast("B").cast("Q")[_Tensor.grad.offset // 8::ctypes.sizeof(_Tensor) // 8]
+            self._groups.append((pt, -1 if ct is None else _TYPES[ct], which, table, column, [self.params[i].shape for i in which]))
 
     def _record(self, stream, more=()):
         for t in (*self.params, *self.copies, *self._m, *self._v, *self._exponents, *more):
@@ -507,7 +520,10 @@ class AdamW:
             return self._record(stream, [*grads, *(t for t in (rate, step, scale) if isinstance(t, torch.Tensor))])
         if len(grads) != len(self.params):
             raise ValueError("there must be as many grads as params")
-        on = L.device.index
+        on, mine = L.device.index, self._written
+        address, dtype, numel = self._homes
+        if list(map(_address, mine)) != address or list(map(_dtype, mine)) != dtype or list(map(_numel, mine)) != numel or not all(map(_contiguous, mine)):
+            raise ValueError("the memory of a parameter or copy was exchanged after the optimiser was made")
         how = _Step(beta1=beta1, beta2=beta2, eps=eps, decay=decay)
         if isinstance(rate, torch.Tensor):
             how.rate_at = _whole(rate.view(1) if rate.dim() == 0 else rate, (1,), torch.float32, on, "rate")
@@ -523,17 +539,17 @@ class AdamW:
             how.scale = _whole(scale.view(1) if scale.dim() == 0 else scale, (1,), torch.float32, on, "scale")
         how.seed = (seed if seed is not None else 0 if isinstance(step, torch.Tensor) else step) & 0xFFFFFFFF
         kinds = []
-        for pt, _, which, table in self._groups:  # all is checked before anything is changed
-            gt = grads[which[0]].dtype
+        for pt, _, which, _, column, shapes in self._groups:  # all is checked before anything is changed
+            some = [grads[i] for i in which]
+            gt = some[0].dtype
             if gt is not torch.float32 and (gt is not pt and pt is not torch.float32 or gt not in _TYPES):
                 raise TypeError("gradients must be float32 or 16 bits, beside 16-bit parameters of their type")
-            for t, i in zip(table, which):
-                g, shape = grads[i], self._shapes[i]
-                if g.dtype is not gt or g.shape != shape or g.get_device() != on or not g.is_contiguous():
+            if list(map(_dtype, some)) != [gt] * len(some) or list(map(_shape, some)) != shapes or list(map(_gpu, some)) != [on] * len(some) or not all(map(_contiguous, some)):
+                for g, shape, i in zip(some, shapes, which):
                     _whole(g, shape, gt, on, "grads[%d]" % i)
-                t.grad = g.data_ptr()
+            column[:] = array.array("Q", map(_address, some))
             kinds.append(_TYPES[gt])
-        for (pt, ct, which, table), gt in zip(self._groups, kinds):
+        for (pt, ct, which, table, _, _), gt in zip(self._groups, kinds):
             rc = L._lib.som_adamw(L._h, _TYPES[pt], gt, ct, self.bits, len(table), table, ctypes.byref(how), L._stream())
             if rc:
                 L._check(rc, "som_adamw")
@@ -557,7 +573,7 @@ class AdamW:
                 t.record_stream(before)
             return out
         m, v = torch.empty(self._all, dtype=torch.bfloat16, device=L.device), torch.empty(self._all, dtype=torch.bfloat16, device=L.device)
-        for _, _, which, table in self._groups:
+        for _, _, which, table, _, _ in self._groups:
             to, mp, vp = ctypes.c_void_p * len(which), m.data_ptr(), v.data_ptr()
             rc = L._lib.som_adamw_moments(L._h, len(table), table, to(*[mp + 2 * self._places[i][2] for i in which]),
                                           to(*[vp + 2 * self._places[i][2] for i in which]), L._stream())
