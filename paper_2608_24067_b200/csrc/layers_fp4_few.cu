@@ -30,6 +30,10 @@ struct FewFp4Args {
     int rows, D, F, share, act, bf16;
 };
 
+// The sums are held times this: a block's sum (4608 at most, of doubled values) times the weights' power of two alone is then finite, and only what
+// the row's sum itself is may be infinite.  Sums below 2^-116 keep steps of 2^-139; half the smallest output is 2^-134 (bf16).
+constexpr float DOWN = 0x1p-10f;
+
 constexpr uint32_t LOW = 0x03020100u, HIGH = 0x0c080604u;  // twice the values of the codes 0 to 7
 
 // twice the positive and the negative values of four codes (the lowest 16 bits), the others 0
@@ -120,9 +124,9 @@ __global__ void __launch_bounds__(THREADS, 2) k_fp4_few(const FewFp4Args a)
             }
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const float by = fp4_power((es[i] >> (8 * (j & 3))) & 255u);
+                const float by = fp4_power((es[i] >> (8 * (j & 3))) & 255u) * (0.25f * DOWN);  // (both were doubled)
 #pragma unroll
-                for (int r = 0; r < ROWS; ++r) acc[i][r] = fmaf((float)sum[i][r] * 0.25f * by, powers[r * blocks + j], acc[i][r]);  // (both doubled)
+                for (int r = 0; r < ROWS; ++r) acc[i][r] = fmaf((float)sum[i][r] * by, powers[r * blocks + j], acc[i][r]);
             }
         }
         j0 += 32 * a.share * STEPS;
@@ -152,6 +156,8 @@ __global__ void __launch_bounds__(THREADS, 2) k_fp4_few(const FewFp4Args a)
         z += part[u * each + k * HALVES][i * ROWS + r];
         if (HALVES == 2) g += part[u * each + k * HALVES + HALVES - 1][i * ROWS + r];
     }
+    z *= 1.f / DOWN;
+    g *= 1.f / DOWN;
     if (a.bias) {
         z += unpack1(a.bias[col], a.bf16);
         if (HALVES == 2) g += unpack1(a.bias[a.F + col], a.bf16);
