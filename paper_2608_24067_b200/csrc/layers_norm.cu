@@ -739,6 +739,7 @@ int som_norm_backward(som_layers* l, int type, int64_t T, int64_t D, const void*
         if (parts > l->sm_count) parts = l->sm_count;
     } else {
         parts = 4 * (int64_t)l->sm_count / tiles_of(D, 32);
+        if (parts < 8) parts = 8;  // a thread adds at most a 64th of the rows one after the other (or eight): what bounds the sums' error
         if (parts > T / 64) parts = T / 64;
         if (parts < 1) parts = 1;
     }
