@@ -451,7 +451,7 @@ class AdamW:
 
     params: contiguous CUDA tensors (float32, float16 or bfloat16) on the handle's device that share no memory; copies: for each float32
     parameter a 16-bit tensor that gets its new value, or None.  Both keep their memory: a step refuses one whose memory, type or size was
-    exchanged (``p.data = ...``, ``Module.half``), and a new optimiser takes over with ``state`` and ``load``.  The first step has number 1."""
+    exchanged (``p.data = ...``, ``Module.half``), and a new optimiser takes over with ``state`` and ``load``.  The moments are zeroed on the current stream.  The first step has number 1."""
 
     def __init__(self, layers, params, copies=None, bits=32):
         if bits not in (8, 32):
@@ -510,7 +510,8 @@ class AdamW:
         """som_adamw: one step.  grads: as params, contiguous, float32 or 16 bits (beside 16-bit parameters their type); parameters of one type
         have gradients of one type.  rate: a number, or a float32 CUDA tensor of one element; step: its number, by default one more than the
         last, or an int64 CUDA tensor of one element; scale: None, or a float32 CUDA tensor of one element that multiplies the gradients (where
-        it is an infinity or NaN the step changes nothing).  seed: of the random bits that round 8-bit moments, by default the step's number."""
+        it is an infinity or NaN the step changes no tensor, but counts: the host does not learn of it, and a caller who does gives ``step``).
+        seed: of the random bits that round 8-bit moments, by default the step's number."""
         L = self._layers
         if stream is not None:
             if stream.device != L.device:

@@ -90,3 +90,26 @@ def test_nan_beside_an_oversized_gradient(L, bits, at):
     want[8:16] = 1.0
     keep = torch.arange(256, device="cuda") != 8 + at
     assert bool(p[8 + at].isnan()) and bool(((p[keep] - want[keep]).abs() <= 2.0 ** -20).all())
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_a_step_that_was_left_out_is_counted(L, bits):
+    """A scale that is not finite changes no tensor, but the number of the step goes on (the host does not learn of it); a caller who knows gives it."""
+    gen = torch.Generator(device="cuda").manual_seed(2)
+    g, start = torch.randn(700, generator=gen, device="cuda"), torch.randn(700, generator=gen, device="cuda")
+    bad = torch.tensor([float("inf")], device="cuda")
+
+    def after(skipped, **kw):
+        p = start.clone()
+        opt = AdamW(L, [p], bits=bits)
+        for _ in range(skipped):
+            opt.step([g], scale=bad)
+        opt.step([g], seed=5, **kw)
+        return p, opt.steps
+
+    plain, n = after(0)
+    counted, n2 = after(1)
+    given, n3 = after(1, step=1)
+    second, _ = after(0, step=2)
+    assert (n, n2, n3) == (1, 2, 1)
+    assert torch.equal(given, plain) and torch.equal(counted, second) and not torch.equal(counted, plain)
