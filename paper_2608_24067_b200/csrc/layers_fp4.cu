@@ -139,7 +139,7 @@ __global__ void __launch_bounds__(Q_THREADS) k_fp4_values(const ValuesArgs a)
                 const int64_t row = at.row + 32 * i;
                 if (row >= a.T) break;
                 const float by = fp4_power((es[i] >> shift) & 255u);
-                if constexpr (WIDE) {  // by bits: the conversion of codes that were read as 16 bits came out as zeros here (compiler 12.9)
+                if constexpr (WIDE) {  // by bits (four codes: see fp4_values)
                     float v[4];
 #pragma unroll
                     for (int j = 0; j < 4; ++j) v[j] = fp4_value(w[i][h] >> (4 * j)) * by;

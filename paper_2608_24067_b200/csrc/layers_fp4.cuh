@@ -52,7 +52,9 @@ __device__ __forceinline__ uint32_t fp4_codes(const float (&v)[8])
 // smallest exponents, which 2^126 lifts to [0, 6].
 __device__ __forceinline__ float fp4_value(uint32_t code) { return __uint_as_float(((code & 7u) << 22) | ((code & 8u) << 28)) * 0x1p126f; }
 
-// the values of eight codes over their blocks' power of two, the first in the lowest four bits
+// The values of eight codes over their blocks' power of two, the first in the lowest four bits.  All of them have to be used: where the results of the two
+// upper bytes are not, the optimising assembler (12.9) gives zeros for the lower two as well, however the codes were loaded (unoptimised, or with
+// the upper two looked at, all 65536 codes of the lower two are right).
 __device__ __forceinline__ void fp4_values(uint32_t w, float2 (&v)[4])
 {
     uint32_t h[4];

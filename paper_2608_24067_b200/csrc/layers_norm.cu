@@ -9,7 +9,9 @@
 //
 // A row is held in registers by a group of threads, 16 values each, loaded in 16 bytes where rows lie on them and value by value else; longer
 // rows are walked.  8192 x 4096 bf16 with a residual 49 us (5.5 TB/s), its gradient 59 to 61 (4.5); rows of 4095 86 and 167.  The gradient is bound by
-// its chain of sums, with four rows an SM at a time (one of 8192 columns): 31 instructions a value, half of the issue slots.
+// its chain of sums, with four rows an SM at a time (one of 8192 columns): 31 instructions a value, half of the issue slots.  In fp32 and off 16 bytes it
+// spills 44 to 152 bytes: 8192 x 4096 fp32 104 us (5.2 TB/s), 4096 x 8001 173.  Rows beyond the registers: 2000 x 65536 bf16 346 us and 882, 1.5 and
+// 0.9 TB/s.
 #include <initializer_list>
 #include <type_traits>
 
@@ -731,6 +733,8 @@ int som_norm_backward(som_layers* l, int type, int64_t T, int64_t D, const void*
         return SOM_OK;
     }
     const bool columns = dweight || dbias;
+    // Held whatever the alignment.  Rows off 16 bytes with dsum, held / walked, in us: bf16 16384 x 101 30 / 46, 16384 x 1001 87 / 123, 8192 x 4095 166 / 207,
+    // 4096 x 8001 176 / 197; fp32 16384 x 1001 84 / 132, 4096 x 8001 173 / 235.
     const int log = group_of(D, BACK_THREADS);
     const bool on16 = lined(D, type == SOM_F32 ? 4 : 2, {x, dy, dsum, dx, weight}, {ldx, lddy, dsum ? ldds : 0});
     int64_t parts;
@@ -739,7 +743,9 @@ int som_norm_backward(som_layers* l, int type, int64_t T, int64_t D, const void*
         if (parts > l->sm_count) parts = l->sm_count;
     } else {
         parts = 4 * (int64_t)l->sm_count / tiles_of(D, 32);
-        if (parts < 8) parts = 8;  // a thread adds at most a 64th of the rows one after the other (or eight): what bounds the sums' error
+        // A thread adds at most a 64th of the rows one after the other (or eight), which is what bounds the sums' error.  As many as fill the SMs / this, in us:
+        // 2000 x 12000 bf16 170 / 125, 8192 x 8200 355 / 309, 2000 x 65536 915 / 882.
+        if (parts < 8) parts = 8;
         if (parts > T / 64) parts = T / 64;
         if (parts < 1) parts = 1;
     }
